@@ -46,7 +46,7 @@ extern "C" {
 #endif
 
 typedef enum { PSA_FULL = 0, PSA_SYMMETRIC = 1, PSA_MASKED = 2 } psa_scheme;
-typedef enum { PSA_F32 = 0, PSA_BF16 = 1 } psa_dtype;
+typedef enum { PSA_F32 = 0, PSA_BF16 = 1, PSA_F16 = 2 /* the serving entry points only */ } psa_dtype;
 
 typedef enum {
     PSA_OK = 0,
@@ -278,6 +278,102 @@ int psa_measure_pipe_rates(psa_pipe_rates* rates, void* stream);
  * Nothing traps or spins without a bound.
  */
 int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
+
+/*
+ * ---- Serving: prompts of different lengths, and a paged cache held in 4 bits ----
+ * (The paper has no counterpart: these are the forms in which its masked scheme, Sec. 5, is needed to answer with a language model.)
+ * Conventions of these entry points, beside those above:
+ *   - heads = kv_heads * group: query head h reads key/value head h / group.  dtype is PSA_BF16 or PSA_F16 (everything that is not
+ *     said to be of another type); sums, softmax statistics and log-sum-exps are fp32.
+ *   - Tokens of several sequences lie one after another ("packed"): sequence b owns rows starts[b] .. starts[b + 1] - 1 of a
+ *     [rows, heads, d_k] tensor, `starts` being sequences + 1 ascending device ints.  A length may be zero; rows outside
+ *     starts[0] .. starts[sequences] are neither read nor written.  Strides are elements between rows, a multiple of 8; the heads of a row lie side by side.
+ *   - `out` is dense, [rows, heads * d_k]; `lse`, where given, dense fp32 [rows, heads]: log(sum_j exp(scale q_i k_j)), natural, by which
+ *     results over different keys can be joined.  A row that sees no key gets zeros and -inf.
+ *   - What a row does not see has no influence on it, NaN and infinities included.
+ *   - Lengths, tables and lists are read on the device, in stream order; the host needs none of them.  A call with zero rows (or an empty list) returns PSA_OK and
+ *     launches nothing.  Device-side arguments that name no place (a sequence or page that does not exist, a token beyond the table)
+ *     are left out, and psa_last_issued returns PSA_ERR_SHAPE for that call.
+ *   - psa_last_issued reports these calls' status; its counts are those of psa_prompt_attention's blocks, else zero.
+ */
+
+/*
+ * Attention over packed prompts, causal: query i of a sequence with nq queries and nk keys sees keys j <= i + nk - nq (the queries are the last nq of the nk tokens;
+ * nk < nq leaves the first rows without keys).
+ *   Q [q_rows, heads, d_k], K and V [k_rows, kv_heads, d_k] with row strides q_stride, k_stride, v_stride (they may be parts of one tensor)
+ *   q_starts, k_starts   device ints, sequences + 1 each; k_starts = NULL: the keys are the queries' tokens (k_rows = q_rows)
+ *   scale                > 0, usually 1 / sqrt(d_k)
+ * Supported: d_k any multiple of 8 up to 128, group (heads / kv_heads) up to 128.  `out` must not overlap Q, K, V.
+ */
+int psa_prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts,
+                         const int* k_starts, int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d_k, float scale, int dtype, void* out,
+                         float* lse, void* stream);
+
+/*
+ * A layer's cache: keys and values in pages of `page_size` tokens (a multiple of 16), every token, head and group of 32 channels with 4-bit codes c and two fp16
+ * numbers S, M; a number reads back as M + S (1 + c / 16), 5 bits each altogether.  Numbers beyond 20000 in size are held as that; a NaN makes its group NaN.
+ * A page is [kv_heads][page_size / 16] blocks of 20 d_k bytes (psa_cache_page_bytes), independent of what its other tokens hold: pages may be copied as bytes.
+ *   pool     device, [pages][page bytes], 16-byte aligned       tables  device ints [slots, width]: a sequence's pages in order, -1 behind the last
+ *   lens     device ints [slots]: tokens of each sequence
+ * Supported: d_k = 32, 64, 96, 128, 256; width * page_size < 2^31.
+ */
+typedef struct {
+    void* pool;
+    const int* tables;
+    const int* lens;
+    int pages, slots, width, page_size, kv_heads, d_k;
+} psa_cache;
+size_t psa_cache_page_bytes(int kv_heads, int page_size, int d_k);      /* 0: unsupported */
+
+/*
+ * Quantises new keys and values and writes them into the pages: row r of sequence b (slot seqs[b]) becomes token lens[seqs[b]] - starts[b + 1] + r, i.e. the
+ * lengths include the new tokens already (psa_pages_reserve adds them).  Tokens beside the new ones are not touched.
+ *   K, V             device, [rows, kv_heads, d_k] with row strides k_stride, v_stride
+ *   k_held, v_held   device, dense [rows, kv_heads, d_k] or NULL: what the cache now holds for these rows, rounded to dtype (they may be K and V if those are dense)
+ */
+int psa_cache_append(const psa_cache* cache, const void* K, const void* V, long long k_stride, long long v_stride, const int* seqs, const int* starts,
+                     int sequences, int rows, int dtype, void* k_held, void* v_held, void* stream);
+
+/*
+ * Attention of the last query tokens of each sequence over its cache: query i of nq sees tokens j <= lens[seqs[b]] - nq + i.  One query per sequence
+ * is the single-token step; several are guessed tokens checked at once, or the rest of a prompt.
+ *   Q      device, [rows, heads, d_k] with row stride q_stride; sequence b owns rows q_starts[b] .. q_starts[b + 1] - 1
+ *   max_q  >= 1, the caller's bound on the queries of a sequence (it chooses the kernel's tiles; larger counts are worked off all the same)
+ * Workspace: psa_cache_workspace_bytes.
+ */
+int psa_cache_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
+                        int max_q, float scale, int dtype, void* out, float* lse, void* stream);
+size_t psa_cache_workspace_bytes(int d_k);
+
+/*
+ * Who holds which page.  tables and lens as in psa_cache (the same arrays serve all layers), refs: device ints [pages], how many tables name a page; a page with
+ * none is free.  All calls work in stream order on the device; free pages are handed out in ascending order, in the order of the list.
+ * Lists hold distinct slots.  Pools are [layers][pages][page_bytes], page_bytes a multiple of 16.
+ *   psa_pages_free     the sequences give back a reference to each of their pages; their rows become -1 and their lengths 0
+ *   psa_pages_fork     child i, a slot without pages, gets parent i's pages (one reference more each) and length; a child is no parent in the same call
+ *   psa_pages_reserve  room for add[i] more tokens of sequence i: lens grows by add[i], pages are taken as needed, and a partly filled last page that is
+ *                      shared is replaced by a copy of its own in all layers.  All or nothing: if pages are missing, *short_by (device int, else 0) says how many and
+ *                      nothing changes.  Up to 4096 sequences a call.  short_by is written by every call that launches.
+ *   psa_pages_compact  the n live pages take places 0 .. n - 1: those there stay, the k-th live page beyond goes to the k-th hole.  new_tables, new_refs and new_pool
+ *                      (same shapes) receive the result and may be the old ones (then only pages that move are copied); *live (device int) = n.  Places beyond n of a
+ *                      new pool keep their bytes.  pages->lens is not used.
+ *   psa_pages_copy     page src[i] of one pool to page dst[i] of another (or the same, the lists then sharing no page)
+ */
+typedef struct {
+    int* tables;
+    int* lens;
+    int* refs;
+    int slots, width, pages, page_size;
+} psa_pages;
+int psa_pages_free(const psa_pages* pages, const int* seqs, int count, void* stream);
+int psa_pages_fork(const psa_pages* pages, const int* parents, const int* children, int count, void* stream);
+int psa_pages_reserve(const psa_pages* pages, void* pool, long long page_bytes, int layers, const int* seqs, const int* add, int count, int* short_by,
+                      void* stream);
+int psa_pages_compact(const psa_pages* pages, const void* pool, long long page_bytes, int layers, int* new_tables, int* new_refs, void* new_pool, int* live,
+                      void* stream);
+int psa_pages_copy(const void* pool, int pages, void* new_pool, int new_pages, long long page_bytes, int layers, const int* src, const int* dst, int count,
+                   void* stream);
+size_t psa_pages_workspace_bytes(int pages, int count);      /* of psa_pages_reserve (count sequences) and psa_pages_compact */
 
 /* Text for a psa_status; never NULL. */
 const char* psa_status_string(int status);

@@ -13,7 +13,7 @@ import os
 import torch
 
 FULL, SYMMETRIC, MASKED = 0, 1, 2
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 OK = 0
 ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ERR_ALIGN, ERR_SCHEME_ARGS, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_NUMERIC = range(1, 10)
 
@@ -23,7 +23,9 @@ LIB_PATH = os.path.join(_HERE, "libpsa.so")
 EXPORTS = ("psa_attention", "psa_attention_f32", "psa_attention_core", "psa_attention_host", "psa_skip_count",
            "psa_last_issued", "psa_workspace_bytes", "psa_set_workspace", "psa_status_string",
            "psa_last_cuda_error", "psa_profile_begin", "psa_profile_end", "psa_attention_sym_f32_noalloc",
-           "psa_attention_block", "psa_block_workspace_bytes", "psa_last_rescales", "psa_selftest_wait_expiry", "psa_measure_pipe_rates", "psa_attention_core_host", "psa_attention_block_residual")
+           "psa_attention_block", "psa_block_workspace_bytes", "psa_last_rescales", "psa_selftest_wait_expiry", "psa_measure_pipe_rates", "psa_attention_core_host", "psa_attention_block_residual",
+           "psa_prompt_attention", "psa_cache_page_bytes", "psa_cache_append", "psa_cache_attention", "psa_cache_workspace_bytes", "psa_pages_free",
+           "psa_pages_fork", "psa_pages_reserve", "psa_pages_compact", "psa_pages_copy", "psa_pages_workspace_bytes")
 
 
 class PsaError(RuntimeError):
@@ -45,6 +47,16 @@ class Counts(ctypes.Structure):
 class PipeRates(ctypes.Structure):
     _fields_ = [("ex2_per_clk_per_sm", ctypes.c_double), ("fma_per_clk_per_sm", ctypes.c_double),
                 ("softmax_weights_per_clk_per_sm", ctypes.c_double), ("sm_count", ctypes.c_int)]
+
+
+class Cache(ctypes.Structure):
+    """psa_cache: a layer's pool with the tables and lengths of its sequences."""
+    _fields_ = [(k, ctypes.c_void_p) for k in ("pool", "tables", "lens")] + [(k, ctypes.c_int) for k in ("pages", "slots", "width", "page_size", "kv_heads", "d_k")]
+
+
+class Pages(ctypes.Structure):
+    """psa_pages: tables, lengths and reference counts."""
+    _fields_ = [(k, ctypes.c_void_p) for k in ("tables", "lens", "refs")] + [(k, ctypes.c_int) for k in ("slots", "width", "pages", "page_size")]
 
 
 _lib = None
@@ -93,6 +105,24 @@ def lib() -> ctypes.CDLL:
         L.psa_last_rescales.restype = ci
         L.psa_attention_sym_f32_noalloc.argtypes = [vp, ci, ci, ci, ci, vp, vp]
         L.psa_attention_sym_f32_noalloc.restype = ci
+        ll, cf, cs = ctypes.c_longlong, ctypes.c_float, ctypes.c_size_t
+        cache, pages = ctypes.POINTER(Cache), ctypes.POINTER(Pages)
+        L.psa_prompt_attention.argtypes = [vp, vp, vp, ll, ll, ll, vp, vp, ci, ci, ci, ci, ci, ci, cf, ci, vp, vp, vp]
+        L.psa_cache_append.argtypes = [cache, vp, vp, ll, ll, vp, vp, ci, ci, ci, vp, vp, vp]
+        L.psa_cache_attention.argtypes = [cache, vp, ll, vp, vp, ci, ci, ci, ci, cf, ci, vp, vp, vp]
+        L.psa_pages_free.argtypes = [pages, vp, ci, vp]
+        L.psa_pages_fork.argtypes = [pages, vp, vp, ci, vp]
+        L.psa_pages_reserve.argtypes = [pages, vp, ll, ci, vp, vp, ci, vp, vp]
+        L.psa_pages_compact.argtypes = [pages, vp, ll, ci, vp, vp, vp, vp, vp]
+        L.psa_pages_copy.argtypes = [vp, ci, vp, ci, ll, ci, vp, vp, ci, vp]
+        L.psa_cache_page_bytes.argtypes = [ci, ci, ci]
+        L.psa_cache_workspace_bytes.argtypes = [ci]
+        L.psa_pages_workspace_bytes.argtypes = [ci, ci]
+        for f in ("psa_cache_page_bytes", "psa_cache_workspace_bytes", "psa_pages_workspace_bytes"):
+            getattr(L, f).restype = cs
+        for f in ("psa_prompt_attention", "psa_cache_append", "psa_cache_attention", "psa_pages_free", "psa_pages_fork", "psa_pages_reserve",
+                  "psa_pages_compact", "psa_pages_copy"):
+            getattr(L, f).restype = ci
         for f in ("psa_attention", "psa_attention_f32", "psa_attention_core", "psa_attention_host",
                   "psa_skip_count", "psa_last_issued", "psa_set_workspace"):
             getattr(L, f).restype = ci
@@ -336,3 +366,164 @@ def psa_attention_sym_f32_noalloc(X, out=None, stream=None):
             err.args = (err.args[0] + ": " + detail,)
         raise err
     return out
+
+
+# ---------------------------------------------------------------- serving
+_SERVING = {torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _rows(t, name, heads, d, dtype=None):
+    """Row stride of a [rows, heads, d] tensor whose heads lie side by side."""
+    if not t.is_cuda or t.dim() != 3 or (dtype is not None and t.dtype != dtype) or t.dtype not in _SERVING:
+        raise ValueError("%s must be a CUDA tensor [rows, heads, d_k] of bf16 or fp16, like the other operands" % name)
+    if (heads is not None and t.shape[1] != heads) or t.shape[2] != d or (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d))):
+        raise ValueError("%s must be [rows, heads, d_k] with the heads of a row side by side" % name)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * d
+
+
+def _ints(t, name, count=None):
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or (count is not None and t.numel() != count):
+        raise ValueError("%s must be a contiguous CUDA tensor of int32%s" % (name, "" if count is None else " with %d numbers" % count))
+    return t.data_ptr()
+
+
+def _result(t, name, shape, dtype, device):
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.numel() != shape[0] * shape[1]:
+        raise ValueError("%s must be a contiguous CUDA tensor %s of dtype %s" % (name, list(shape), dtype))
+    return t
+
+
+def _lse(t, rows, heads):
+    return None if t is None else _result(t, "lse", (rows, heads), torch.float32, t.device).data_ptr()
+
+
+def _raise(rc, where):
+    if rc != OK:
+        raise PsaError(rc, where)
+
+
+def psa_prompt_attention(Q, K, V, q_starts, k_starts=None, scale=None, out=None, lse=None, stream=None):
+    """Causal attention over packed prompts.  Q [q_rows, heads, d], K, V [k_rows, kv_heads, d] (bf16 or fp16; rows may have a stride), q_starts, k_starts int32
+    [sequences + 1] -> out [q_rows, heads * d].  k_starts None: the keys are the queries' tokens.  lse: fp32 [q_rows, heads] to be filled, or None."""
+    rows, heads, d = Q.shape
+    dtype = Q.dtype
+    kv_heads = K.shape[1]
+    if kv_heads == 0 or heads % kv_heads or V.shape != K.shape:
+        raise ValueError("K and V must be [k_rows, kv_heads, d_k] with kv_heads a divisor of Q's heads")
+    strides = _rows(Q, "Q", heads, d), _rows(K, "K", kv_heads, d, dtype), _rows(V, "V", kv_heads, d, dtype)
+    n = q_starts.numel() - 1
+    out = _result(out, "out", (rows, heads * d), dtype, Q.device)
+    _raise(lib().psa_prompt_attention(Q.data_ptr(), K.data_ptr(), V.data_ptr(), *strides, _ints(q_starts, "q_starts"), _ints(k_starts, "k_starts", n + 1), n, rows,
+                                      K.shape[0], heads, kv_heads, d, d ** -0.5 if scale is None else scale, _SERVING[dtype], out.data_ptr(), _lse(lse, rows, heads),
+                                      _stream(stream)), "psa_prompt_attention")
+    return out
+
+
+def psa_cache_page_bytes(kv_heads, page_size, d_k) -> int:
+    """Bytes of a page of the cache in 4 bits; 0 if no such cache is supported."""
+    return int(lib().psa_cache_page_bytes(kv_heads, page_size, d_k))
+
+
+def psa_cache_workspace_bytes(d_k) -> int:
+    return int(lib().psa_cache_workspace_bytes(d_k))
+
+
+def psa_pages_workspace_bytes(pages, count) -> int:
+    return int(lib().psa_pages_workspace_bytes(pages, count))
+
+
+def _cache(pool, tables, lens, kv_heads, page_size, d):
+    if not pool.is_cuda or pool.dtype != torch.uint8 or pool.dim() != 2 or not pool.is_contiguous() or tables.dim() != 2:
+        raise ValueError("pool must be a contiguous CUDA tensor [pages, page bytes] of uint8, tables [slots, width]")
+    if pool.shape[1] * 16 != kv_heads * page_size * 20 * d:
+        raise ValueError("pool pages must have psa_cache_page_bytes(%d, %d, %d) bytes" % (kv_heads, page_size, d))
+    return Cache(pool.data_ptr(), _ints(tables, "tables"), _ints(lens, "lens", tables.shape[0]), pool.shape[0], tables.shape[0], tables.shape[1], page_size, kv_heads, d)
+
+
+def psa_cache_append(K, V, pool, tables, lens, seqs, starts, page_size, k_held=None, v_held=None, stream=None):
+    """Quantises K, V [rows, kv_heads, d] (rows may have a stride) to 4 bits and writes them as the last tokens of slots seqs, sequence b being rows starts[b] ..
+    starts[b + 1] - 1; lens includes them already.  k_held, v_held (dense, or None) receive what the cache now holds."""
+    rows, kv_heads, d = K.shape
+    dtype = K.dtype
+    if V.shape != K.shape:
+        raise ValueError("K and V must have one shape")
+    strides = _rows(K, "K", kv_heads, d), _rows(V, "V", kv_heads, d, dtype)
+    for t, nm in ((k_held, "k_held"), (v_held, "v_held")):
+        if t is not None and (not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.shape != K.shape):
+            raise ValueError("%s must be a contiguous CUDA tensor like K" % nm)
+    n = seqs.numel()
+    cache = _cache(pool, tables, lens, kv_heads, page_size, d)
+    _raise(lib().psa_cache_append(cache, K.data_ptr(), V.data_ptr(), *strides, _ints(seqs, "seqs"), _ints(starts, "starts", n + 1), n, rows, _SERVING[dtype],
+                                  _ptr(k_held), _ptr(v_held), _stream(stream)), "psa_cache_append")
+
+
+def psa_cache_attention(Q, pool, tables, lens, seqs, q_starts, kv_heads, page_size, max_q=1, scale=None, out=None, lse=None, stream=None):
+    """Attention of the last query tokens of slots seqs over the cache in 4 bits: Q [rows, heads, d] (rows may have a stride), sequence b owns rows q_starts[b] ..
+    q_starts[b + 1] - 1 -> out [rows, heads * d].  max_q: bound on the queries of a sequence."""
+    rows, heads, d = Q.shape
+    if kv_heads <= 0 or heads % kv_heads:
+        raise ValueError("kv_heads must divide Q's heads")
+    q_stride, n = _rows(Q, "Q", heads, d), seqs.numel()
+    cache = _cache(pool, tables, lens, kv_heads, page_size, d)
+    out = _result(out, "out", (rows, heads * d), Q.dtype, Q.device)
+    _raise(lib().psa_cache_attention(cache, Q.data_ptr(), q_stride, _ints(seqs, "seqs"), _ints(q_starts, "q_starts", n + 1), n, rows, heads, max_q,
+                                     d ** -0.5 if scale is None else scale, _SERVING[Q.dtype], out.data_ptr(), _lse(lse, rows, heads), _stream(stream)),
+           "psa_cache_attention")
+    return out
+
+
+def _pages(tables, lens, refs, page_size):
+    if tables.dim() != 2:
+        raise ValueError("tables must be [slots, width]")
+    return Pages(_ints(tables, "tables"), None if lens is None else _ints(lens, "lens", tables.shape[0]), _ints(refs, "refs"), tables.shape[0], tables.shape[1],
+                 refs.numel(), page_size)
+
+
+def _pool(t, pages):
+    """(address, page bytes, layers) of a pool [pages, page bytes] or [layers, pages, page bytes]."""
+    if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous() or t.dim() not in (2, 3) or t.shape[-2] != pages:
+        raise ValueError("a pool must be a contiguous CUDA tensor [pages, page bytes] or [layers, pages, page bytes] of uint8")
+    return t.data_ptr(), t.shape[-1], t.shape[0] if t.dim() == 3 else 1
+
+
+def psa_pages_free(tables, lens, refs, seqs, page_size, stream=None):
+    """The sequences in slots seqs end: their pages lose a reference, their rows become -1, their lengths 0."""
+    _raise(lib().psa_pages_free(_pages(tables, lens, refs, page_size), _ints(seqs, "seqs"), seqs.numel(), _stream(stream)), "psa_pages_free")
+
+
+def psa_pages_fork(tables, lens, refs, parents, children, page_size, stream=None):
+    """Slot children[i], which holds no pages, gets the pages and the length of slot parents[i]."""
+    n = parents.numel()
+    _raise(lib().psa_pages_fork(_pages(tables, lens, refs, page_size), _ints(parents, "parents"), _ints(children, "children", n), n, _stream(stream)), "psa_pages_fork")
+
+
+def psa_pages_reserve(tables, lens, refs, pool, seqs, add, page_size, short, stream=None):
+    """Room for add[i] more tokens of slot seqs[i]: lens grows, pages are taken, a shared last page that is written to is copied in all layers of the pool.
+    short (int32, one number): how many pages are missing; if any, nothing changes."""
+    n = seqs.numel()
+    _raise(lib().psa_pages_reserve(_pages(tables, lens, refs, page_size), *_pool(pool, refs.numel()), _ints(seqs, "seqs"), _ints(add, "add", n), n,
+                                   _ints(short, "short", 1), _stream(stream)), "psa_pages_reserve")
+
+
+def psa_pages_compact(tables, refs, pool, new_tables, new_refs, new_pool, live, stream=None):
+    """Live pages take the first places: those beyond move into the holes before them, in order.  The new tensors may be the old ones.  live (int32, one number)."""
+    if new_tables.shape != tables.shape or new_refs.shape != refs.shape or new_pool.shape != pool.shape:
+        raise ValueError("new_tables, new_refs and new_pool must have the shapes of tables, refs and pool")
+    address, page_bytes, layers = _pool(pool, refs.numel())
+    _raise(lib().psa_pages_compact(_pages(tables, None, refs, 1), address, page_bytes, layers, _ints(new_tables, "new_tables"), _ints(new_refs, "new_refs"),
+                                   _pool(new_pool, refs.numel())[0], _ints(live, "live", 1), _stream(stream)), "psa_pages_compact")
+
+
+def psa_pages_copy(pool, new_pool, src, dst, stream=None):
+    """Page src[i] of pool to page dst[i] of new_pool (which may be the same, the lists then sharing no page), in all layers."""
+    n = src.numel()
+    address, page_bytes, layers = _pool(pool, pool.shape[-2])
+    new_address, new_bytes, new_layers = _pool(new_pool, new_pool.shape[-2])
+    if (new_bytes, new_layers) != (page_bytes, layers):
+        raise ValueError("both pools must have the same layers and page bytes")
+    _raise(lib().psa_pages_copy(address, pool.shape[-2], new_address, new_pool.shape[-2], page_bytes, layers, _ints(src, "src"), _ints(dst, "dst", n), n,
+                                _stream(stream)), "psa_pages_copy")

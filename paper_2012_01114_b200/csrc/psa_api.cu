@@ -314,6 +314,81 @@ int layer_entry(const void* X, const void* Wq, const void* Wk, const void* Wv, i
                      static_cast<cudaStream_t>(stream), true, ws, L);
 }
 
+// ---- serving entry points
+// Counter blocks of a call that takes no part of the layer's workspace: as in run_layer, whose blocks these are.
+struct OpCall {
+    char* ws;                 // scratch of the call: ws + COUNTER_BYTES
+    DeviceCounters *dc, *dc_next;
+    bool captured;
+    int block;
+};
+int begin_op(Context& cx, size_t scratch, cudaStream_t stream, OpCall* c) {
+    c->ws = acquire_ws(cx, COUNTER_BYTES + scratch);
+    if (!c->ws) return PSA_ERR_WORKSPACE;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    cudaError_t e = cudaStreamIsCapturing(stream, &capture);
+    if (e != cudaSuccess) { set_cuda_error(e, "cudaStreamIsCapturing"); return PSA_ERR_CUDA; }
+    c->captured = capture != cudaStreamCaptureStatusNone;
+    c->block = 0;
+    if (c->captured) {
+        c->block = CAPTURE_BLOCK;
+        e = cudaMemsetAsync(c->ws + CAPTURE_BLOCK * COUNTER_BLOCK_BYTES, 0, COUNTER_BLOCK_BYTES, stream);
+    } else if (cx.clean_ws == c->ws) {
+        c->block = cx.next_block;
+    } else {
+        e = cudaMemsetAsync(c->ws, 0, TURN_BLOCKS * COUNTER_BLOCK_BYTES, stream);
+    }
+    if (e != cudaSuccess) { set_cuda_error(e, "cudaMemsetAsync(counters)"); return PSA_ERR_CUDA; }
+    if (!c->captured) cx.clean_ws = nullptr;
+    c->dc = reinterpret_cast<DeviceCounters*>(c->ws + c->block * COUNTER_BLOCK_BYTES);
+    c->dc_next = c->captured ? nullptr : reinterpret_cast<DeviceCounters*>(c->ws + (c->block ^ 1) * COUNTER_BLOCK_BYTES);
+    cx.last_dc = c->dc;
+    memset(&cx.last_useful, 0, sizeof(psa_counts));
+    return PSA_OK;
+}
+int end_op(Context& cx, const OpCall& c, int rc) {
+    if (rc == PSA_OK && !c.captured) {
+        cx.clean_ws = c.ws;
+        cx.next_block = c.block ^ 1;
+    }
+    return rc;
+}
+template <class Run>
+int run_op(size_t scratch, void* stream, Run run) {
+    Context* cp = current_ctx();
+    if (!cp) return PSA_ERR_CUDA;
+    std::lock_guard<std::mutex> lock(cp->mu);
+    OpCall c;
+    const int rc = begin_op(*cp, scratch, static_cast<cudaStream_t>(stream), &c);
+    return rc != PSA_OK ? rc : end_op(*cp, c, run(c));
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+bool serving_dtype(int dtype) { return dtype == PSA_BF16 || dtype == PSA_F16; }
+bool good_scale(float scale) { return scale > 0.f && scale <= 3.0e38f; }
+bool cache_head(int d) { return d == 32 || d == 64 || d == 96 || d == 128 || d == 256; }
+bool good_stride(long long stride, long long least) { return stride >= least && stride % 8 == 0 && stride <= (1LL << 38); }
+
+int check_cache(const psa_cache* c) {
+    if (!c || !c->pool || !c->tables || !c->lens) return PSA_ERR_NULL;
+    if (c->pages <= 0 || c->slots <= 0 || c->width <= 0 || c->page_size <= 0 || c->kv_heads <= 0 || c->d_k <= 0) return PSA_ERR_SHAPE;
+    if ((long long)c->width * c->page_size > 0x7fffffffLL || (long long)c->kv_heads * c->d_k > 0x7fffffffLL) return PSA_ERR_SHAPE;
+    if (psa_cache_page_bytes(c->kv_heads, c->page_size, c->d_k) == 0) return PSA_ERR_UNSUPPORTED;
+    if (!aligned16(c->pool) || !aligned4(c->tables) || !aligned4(c->lens)) return PSA_ERR_ALIGN;
+    return PSA_OK;
+}
+int check_pages(const psa_pages* p) {
+    if (!p || !p->tables || !p->refs) return PSA_ERR_NULL;
+    if (p->slots <= 0 || p->width <= 0 || p->pages <= 0 || p->page_size <= 0) return PSA_ERR_SHAPE;
+    if (!aligned4(p->tables) || !aligned4(p->lens) || !aligned4(p->refs)) return PSA_ERR_ALIGN;
+    return PSA_OK;
+}
+int check_pool(const void* pool, long long page_bytes, int layers) {
+    if (!pool) return PSA_ERR_NULL;
+    if (page_bytes <= 0 || layers <= 0) return PSA_ERR_SHAPE;
+    return aligned16(pool) && page_bytes % 16 == 0 ? PSA_OK : PSA_ERR_ALIGN;
+}
+
 }  // namespace
 
 int device_setup(DeviceSetup* st, cudaError_t (*configure)(), const char* what, int* device) {
@@ -794,6 +869,135 @@ int psa_profile_end(float* proj_ms_sum, float* attn_ms_sum, int* calls) {
     cx.prof_calls = 0;
     cx.prof_max = 0;
     return rc;
+}
+
+int psa_prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts,
+                         const int* k_starts, int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d_k, float scale, int dtype, void* out,
+                         float* lse, void* stream) {
+    g_err_text[0] = 0;
+    if (sequences <= 0 || q_rows < 0 || k_rows < 0 || heads <= 0 || kv_heads <= 0 || d_k <= 0 || heads % kv_heads) return PSA_ERR_SHAPE;
+    if (!k_starts && k_rows != q_rows) return PSA_ERR_SHAPE;
+    if (!serving_dtype(dtype) || d_k > 128 || d_k % 8 || heads / kv_heads > 128 || !good_scale(scale)) return PSA_ERR_UNSUPPORTED;
+    if (q_rows == 0) return PSA_OK;
+    if (!Q || !q_starts || !out || (k_rows > 0 && (!K || !V))) return PSA_ERR_NULL;
+    if ((long long)heads * d_k > 0x7fffffffLL || !good_stride(q_stride, (long long)heads * d_k)) return PSA_ERR_SHAPE;
+    if (k_rows > 0 && (!good_stride(k_stride, (long long)kv_heads * d_k) || !good_stride(v_stride, (long long)kv_heads * d_k))) return PSA_ERR_SHAPE;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(out) || !aligned4(lse) || !aligned4(q_starts) || !aligned4(k_starts)) return PSA_ERR_ALIGN;
+    return run_op(0, stream, [&](const OpCall& c) {
+        return prompt_attention(Q, K, V, q_stride, k_stride, v_stride, q_starts, k_starts ? k_starts : q_starts, sequences, q_rows, k_rows, heads, kv_heads, d_k, scale,
+                                dtype, out, lse, c.dc, &c.dc->next_item, c.dc_next, static_cast<cudaStream_t>(stream));
+    });
+}
+
+size_t psa_cache_page_bytes(int kv_heads, int page_size, int d_k) {
+    if (kv_heads <= 0 || page_size <= 0 || page_size % 16 || !cache_head(d_k)) return 0;
+    return (size_t)kv_heads * (page_size / 16) * 20 * d_k;
+}
+
+int psa_cache_append(const psa_cache* cache, const void* K, const void* V, long long k_stride, long long v_stride, const int* seqs, const int* starts,
+                     int sequences, int rows, int dtype, void* k_held, void* v_held, void* stream) {
+    g_err_text[0] = 0;
+    const int rc = check_cache(cache);
+    if (rc != PSA_OK) return rc;
+    if (sequences <= 0 || rows < 0) return PSA_ERR_SHAPE;
+    if (!serving_dtype(dtype)) return PSA_ERR_UNSUPPORTED;
+    if (rows == 0) return PSA_OK;
+    if (!K || !V || !seqs || !starts) return PSA_ERR_NULL;
+    const long long least = (long long)cache->kv_heads * cache->d_k;
+    if (!good_stride(k_stride, least) || !good_stride(v_stride, least) || ((long long)rows + 1) / 2 * cache->kv_heads > 8LL * 0x7ffffff0LL) return PSA_ERR_SHAPE;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(k_held) || !aligned16(v_held) || !aligned4(seqs) || !aligned4(starts)) return PSA_ERR_ALIGN;
+    return run_op(0, stream, [&](const OpCall& c) {
+        return cache_append(*cache, K, V, k_stride, v_stride, seqs, starts, sequences, rows, dtype, k_held, v_held, c.dc, c.dc_next, static_cast<cudaStream_t>(stream));
+    });
+}
+
+size_t psa_cache_workspace_bytes(int d_k) { return cache_head(d_k) ? COUNTER_BYTES + cache_attention_scratch_bytes(d_k) : 0; }
+
+int psa_cache_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
+                        int max_q, float scale, int dtype, void* out, float* lse, void* stream) {
+    g_err_text[0] = 0;
+    const int rc = check_cache(cache);
+    if (rc != PSA_OK) return rc;
+    if (sequences <= 0 || rows < 0 || heads <= 0 || heads % cache->kv_heads || max_q <= 0) return PSA_ERR_SHAPE;
+    if (!serving_dtype(dtype) || !good_scale(scale)) return PSA_ERR_UNSUPPORTED;
+    if (rows == 0) return PSA_OK;
+    if (!Q || !seqs || !q_starts || !out) return PSA_ERR_NULL;
+    if (!good_stride(q_stride, (long long)heads * cache->d_k) || (long long)rows * (heads / cache->kv_heads) > 0x7fffff00LL) return PSA_ERR_SHAPE;
+    if (!aligned16(Q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) || !aligned4(q_starts)) return PSA_ERR_ALIGN;
+    return run_op(cache_attention_scratch_bytes(cache->d_k), stream, [&](const OpCall& c) {
+        return cache_attention(*cache, Q, q_stride, seqs, q_starts, sequences, rows, heads, max_q, scale, dtype, out, lse, c.ws + COUNTER_BYTES, c.dc, c.dc_next,
+                               static_cast<cudaStream_t>(stream));
+    });
+}
+
+int psa_pages_free(const psa_pages* pages, const int* seqs, int count, void* stream) {
+    g_err_text[0] = 0;
+    const int rc = check_pages(pages);
+    if (rc != PSA_OK) return rc;
+    if (count < 0) return PSA_ERR_SHAPE;
+    if (count == 0) return PSA_OK;
+    if (!pages->lens || !seqs) return PSA_ERR_NULL;
+    if (!aligned4(seqs)) return PSA_ERR_ALIGN;
+    return run_op(0, stream, [&](const OpCall& c) { return pages_free(*pages, seqs, count, c.dc, c.dc_next, static_cast<cudaStream_t>(stream)); });
+}
+
+int psa_pages_fork(const psa_pages* pages, const int* parents, const int* children, int count, void* stream) {
+    g_err_text[0] = 0;
+    const int rc = check_pages(pages);
+    if (rc != PSA_OK) return rc;
+    if (count < 0) return PSA_ERR_SHAPE;
+    if (count == 0) return PSA_OK;
+    if (!pages->lens || !parents || !children) return PSA_ERR_NULL;
+    if (!aligned4(parents) || !aligned4(children)) return PSA_ERR_ALIGN;
+    return run_op(0, stream, [&](const OpCall& c) { return pages_fork(*pages, parents, children, count, c.dc, c.dc_next, static_cast<cudaStream_t>(stream)); });
+}
+
+int psa_pages_reserve(const psa_pages* pages, void* pool, long long page_bytes, int layers, const int* seqs, const int* add, int count, int* short_by,
+                      void* stream) {
+    g_err_text[0] = 0;
+    int rc = check_pages(pages);
+    if (rc == PSA_OK) rc = check_pool(pool, page_bytes, layers);
+    if (rc != PSA_OK) return rc;
+    if (count < 0 || (long long)pages->width * pages->page_size > 0x7fffffffLL) return PSA_ERR_SHAPE;
+    if (count > 4096) return PSA_ERR_UNSUPPORTED;
+    if (count == 0) return PSA_OK;
+    if (!pages->lens || !seqs || !add || !short_by) return PSA_ERR_NULL;
+    if (!aligned4(seqs) || !aligned4(add) || !aligned4(short_by)) return PSA_ERR_ALIGN;
+    return run_op(pages_reserve_scratch_bytes(pages->pages, count), stream, [&](const OpCall& c) {
+        return pages_reserve(*pages, pool, page_bytes, layers, seqs, add, count, short_by, c.ws + COUNTER_BYTES, c.dc, c.dc_next, static_cast<cudaStream_t>(stream));
+    });
+}
+
+int psa_pages_compact(const psa_pages* pages, const void* pool, long long page_bytes, int layers, int* new_tables, int* new_refs, void* new_pool, int* live,
+                      void* stream) {
+    g_err_text[0] = 0;
+    int rc = check_pages(pages);
+    if (rc == PSA_OK) rc = check_pool(pool, page_bytes, layers);
+    if (rc == PSA_OK) rc = check_pool(new_pool, page_bytes, layers);
+    if (rc != PSA_OK) return rc;
+    if (!new_tables || !new_refs || !live) return PSA_ERR_NULL;
+    if (!aligned4(new_tables) || !aligned4(new_refs) || !aligned4(live)) return PSA_ERR_ALIGN;
+    return run_op(pages_compact_scratch_bytes(pages->pages), stream, [&](const OpCall& c) {
+        return pages_compact(*pages, pool, page_bytes, layers, new_tables, new_refs, new_pool, live, c.ws + COUNTER_BYTES, c.dc, c.dc_next, static_cast<cudaStream_t>(stream));
+    });
+}
+
+int psa_pages_copy(const void* pool, int pages, void* new_pool, int new_pages, long long page_bytes, int layers, const int* src, const int* dst, int count,
+                   void* stream) {
+    g_err_text[0] = 0;
+    int rc = check_pool(pool, page_bytes, layers);
+    if (rc == PSA_OK) rc = check_pool(new_pool, page_bytes, layers);
+    if (rc != PSA_OK) return rc;
+    if (pages <= 0 || new_pages <= 0 || count < 0) return PSA_ERR_SHAPE;
+    if (count == 0) return PSA_OK;
+    if (!src || !dst) return PSA_ERR_NULL;
+    if (!aligned4(src) || !aligned4(dst)) return PSA_ERR_ALIGN;
+    return run_op(0, stream, [&](const OpCall& c) { return pages_copy(pool, pages, new_pool, new_pages, page_bytes, layers, src, dst, count, c.dc, c.dc_next, static_cast<cudaStream_t>(stream)); });
+}
+
+size_t psa_pages_workspace_bytes(int pages, int count) {
+    if (pages <= 0 || count < 0 || count > 4096) return 0;
+    return COUNTER_BYTES + std::max(pages_reserve_scratch_bytes(pages, count), pages_compact_scratch_bytes(pages));
 }
 
 const char* psa_status_string(int status) {

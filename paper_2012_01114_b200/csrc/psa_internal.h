@@ -90,6 +90,27 @@ int bf16_attention_persist(const void* Q, const void* K, const void* V, void* ou
                            float scale, int scheme, DeviceCounters* dc, unsigned int* cursor, DeviceCounters* dc_next,
                            cudaStream_t stream);
 
+// ---- serving (psa_prompt.cu, psa_cache_append.cu, psa_cache_attn.cu, psa_pages.cu) ----
+// Arguments are checked by the caller; each returns a psa_status.  dc: the call's counter block, dc_next (may be null): cleared by the call's first kernel.
+int prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts, const int* k_starts,
+                     int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, DeviceCounters* dc,
+                     unsigned int* cursor, DeviceCounters* dc_next, cudaStream_t stream);
+int cache_append(const psa_cache& c, const void* K, const void* V, long long k_stride, long long v_stride, const int* seqs, const int* starts, int sequences, int rows,
+                 int dtype, void* k_held, void* v_held, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+size_t cache_attention_scratch_bytes(int d);
+int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const int* seqs, const int* q_starts, int sequences, int rows, int heads, int max_q,
+                    float scale, int dtype, void* out, float* lse, void* scratch, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+int pages_free(const psa_pages& p, const int* seqs, int count, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+int pages_fork(const psa_pages& p, const int* parents, const int* children, int count, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+size_t pages_reserve_scratch_bytes(int pages, int count);
+int pages_reserve(const psa_pages& p, void* pool, long long page_bytes, int layers, const int* seqs, const int* add, int count, int* short_by, void* scratch,
+                  DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+size_t pages_compact_scratch_bytes(int pages);
+int pages_compact(const psa_pages& p, const void* pool, long long page_bytes, int layers, int* new_tables, int* new_refs, void* new_pool, int* live, void* scratch,
+                  DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+int pages_copy(const void* pool, int pages, void* new_pool, int new_pages, long long page_bytes, int layers, const int* src, const int* dst, int count,
+               DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+
 // Once-per-device set-up of a kernel family.  Function attributes (the dynamic shared-memory limit) belong to the
 // device that is current when they are set, and the SM count differs between devices, so both are kept per
 // device ordinal.  device_setup() returns the current device's SM count (> 0), having run `configure` (which sets

@@ -1,0 +1,895 @@
+// Attention over packed prompts: sequences of different lengths one after another, heads in groups that share keys and values, causal.
+//
+//     out_i = sum_j w_ij v_j / sum_j w_ij,   w_ij = exp(scale q_i k_j),   j <= i + nk - nq      (nq queries, the last of nk tokens)
+//
+// The kernel is built like attn_persist_kernel (psa_attn_persist.cu, where the layout of the CTA and its pipeline are explained): S = Q K^T and O += P V by tcgen05 MMAs
+// with the accumulators and P in tensor memory, operands staged by TMA, softmax and epilogue by sixteen warps in the quad layout, one persistent CTA per
+// SM.  What is different:
+//   * A row tile holds the queries of all heads of a group: row r is token r / group, head r % group of the group, 128 / group tokens a tile (one box of the
+//     query's tensor map).  Keys and values are loaded once for the group, short prompts fill tiles, and any group size works alike; groups that do not divide
+//     128 leave up to 7 % of the rows empty.
+//   * The host does not know the lengths.  Every CTA derives the work list from `starts` by itself (sequences sorted by length in shared memory): the heaviest pairs of row
+//     tiles of all sequences first, heads innermost, taken from a device counter, as in attn_persist_kernel.
+//   * A tile may reach into the next sequence.  Its rows beyond the sequence are computed and not stored, so the output is stored row by row; keys beyond it carry
+//     no weight, and neither do non-finite values there (a weight of zero would not keep them out of the sum): in blocks that some row of the tile does
+//     not see in full the softmax warps look through the tile of V before P V and set what is not finite to zero; rows that do see such a value get it
+//     back in the epilogue.
+#include <type_traits>
+
+#include <cuda_fp16.h>
+
+#include "psa_internal.h"
+#include "psa_sched.h"
+#include "psa_softmax.cuh"
+#include "psa_tma.h"
+#include "sm100.cuh"
+
+namespace psa {
+
+namespace {
+
+template <int D>
+struct PCfg {
+    static constexpr int SUB = D / 64;                  // 64-column sub-tiles per 128-row tile
+    static constexpr int TILE_BYTES = 128 * D * 2;      // one Q, K or V tile
+    static constexpr int KSTAGES = D == 128 ? 2 : 4;
+    static constexpr int VSTAGES = D == 128 ? 2 : 4;
+    // output staging: one [16 rows x 32 columns] buffer per softmax warp, used for each 32 columns in turn
+    static constexpr int STAGE_BYTES = 16 * 32 * 2;
+    static constexpr int STAGE_BUFS = 2 * SOFTMAX_WARPS_PER_TILE;
+    static constexpr int SMEM = (2 + KSTAGES + VSTAGES) * TILE_BYTES + STAGE_BUFS * STAGE_BYTES + 1024;
+    static constexpr bool SEP_P = D == 64;
+    static constexpr int TMEM_S = 0, TMEM_P = 256, TMEM_O = SEP_P ? 384 : 256;
+};
+
+struct PMaps {
+    CUtensorMap q, k, v;
+};
+constexpr int SEQS = 512;               // sequences of one launch
+constexpr int SEQ_BITS = 9;
+
+struct PromptArgs {
+    const int *q_starts, *k_starts;
+    int sequences, q_rows, k_rows, heads, kv_heads, group, tokens, d;     // tokens: of a row tile, 128 / group
+    long long v_stride;
+    const uint16_t* v;                  // (the epilogue's look at values that are not finite)
+    uint16_t* out;
+    float* lse;
+    float sl2;
+    FastDiv by_group, by_heads;
+};
+// A work item: two row tiles of one sequence and key/value head.
+struct __align__(16) Item {
+    int q0, k0;                         // first rows of the sequence
+    int i0, nq, nk;                     // first token of the first tile, lengths
+    int h;                              // key/value head
+    int nkv0, nkv1;                     // key blocks of the two tiles (0: no rows, or rows without keys)
+};
+
+struct PBars {
+    uint64_t item_full[2], item_empty[2];
+    uint64_t q_full[2], q_empty[2];
+    uint64_t k_full[8], k_empty[8], v_full[4], v_empty[4];
+    uint64_t s_full[2], s_free[2], p_ready[2], o_done[2];
+};
+
+constexpr float LN2 = 0.6931471805599453f;
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    if constexpr (F16) {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        return pack_bf16x2(lo, hi);
+    }
+}
+// exp_quad64 (psa_softmax.cuh) for either type of P.
+template <bool F16>
+__device__ __forceinline__ void exp_quad(const uint32_t (&s)[32], float sl2, float negmA, float negmB, uint32_t (&pk)[16], float& sumA, float& sumB) {
+    if constexpr (!F16) {
+        exp_quad64(s, sl2, negmA, negmB, pk, sumA, sumB);
+    } else {
+        float sa0 = 0.f, sa1 = 0.f, sb0 = 0.f, sb1 = 0.f;
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            const float p0 = ex2_mufu(fmaf(__uint_as_float(s[4 * g]), sl2, negmA)), p1 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 1]), sl2, negmA));
+            const float p2 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 2]), sl2, negmB)), p3 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 3]), sl2, negmB));
+            sa0 += p0; sa1 += p1; sb0 += p2; sb1 += p3;
+            pk[2 * g] = pack<true>(p0, p1);
+            pk[2 * g + 1] = pack<true>(p2, p3);
+        }
+        sumA += sa0 + sa1;
+        sumB += sb0 + sb1;
+    }
+}
+// kind::f16 with operands of either type (bf16: type 1, fp16: type 0) and fp32 accumulation.
+template <bool F16>
+__host__ __device__ constexpr uint32_t idesc(uint32_t M, uint32_t N, uint32_t a_major, uint32_t b_major) {
+    return umma_idesc_bf16(M, N, a_major, b_major) & ~(F16 ? (1u << 7) | (1u << 10) : 0u);
+}
+__device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, uint64_t* bar, int x, int h, int y) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(h), "r"(y)
+        : "memory");
+}
+
+// d = 64 has an MMA-issuing thread per row tile slot (warp 1 for slot 0, the last warp for slot 1): a block there is
+// half the tensor work of d = 128 but as many instructions to issue, and one thread was measured to be the limit.
+constexpr int ISSUER1_WARP = CTRL_WARPS + 2 * SOFTMAX_WARPS_PER_TILE;
+template <int D> __host__ __device__ constexpr int persist_threads() { return ATTN_THREADS + (D == 64 ? 32 : 0); }
+template <int D> __host__ __device__ constexpr int item_readers() { return (D == 64 ? 2 : 1) + 2 * SOFTMAX_WARPS_PER_TILE; }   // issuers + one lane per softmax warp
+
+// D: columns of a tile in shared memory, KS: 16-column steps of phase 1, and of phase 3's output, that hold columns of the head (the rest are zeros;
+// the census counts blocks, each of D columns).
+// F16: fp16 instead of bf16 in memory and as operands.
+template <int D, int KS, bool F16>
+__global__ void __launch_bounds__(persist_threads<D>(), 1)
+prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ PromptArgs pa, DeviceCounters* dc, unsigned int* cursor, DeviceCounters* dc_next) {
+    using Cfg = PCfg<D>;
+    constexpr bool SEP = Cfg::SEP_P;
+    constexpr int VST = Cfg::VSTAGES;
+    constexpr int KST = Cfg::KSTAGES;
+    // d = 128: V_j and K_{j+1} are needed by the same step of the issuing thread and released by
+    // it together, so they travel as one stage (K slot s and V slot s, one full and one empty barrier: v_full / v_empty):
+    // pair p of an item is (V_{p-1}, K_p), p = 0 .. blocks, the first without a V and the last without a K.  The
+    // issuing thread then probes one barrier and commits one release per key block instead of two of each.
+    constexpr bool PAIRED = !SEP;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* sQ = smem;                                          // 2 tiles
+    uint8_t* sK = sQ + 2 * Cfg::TILE_BYTES;                      // KSTAGES tiles
+    uint8_t* sV = sK + Cfg::KSTAGES * Cfg::TILE_BYTES;           // VSTAGES tiles
+    uint8_t* sStage = sV + VST * Cfg::TILE_BYTES;                // STAGE_BUFS output staging tiles
+    __shared__ PBars bars;
+    __shared__ uint32_t tmem_base_s;
+    __shared__ int abort_flag;
+    __shared__ Item item_ring[2];
+    __shared__ int v_bad;                        // count of the last item in which V held something that is not finite, see above
+    // the work list: sequences by falling number of pairs of row tiles (key = pairs << SEQ_BITS | SEQS - 1 - sequence), see `decode`
+    __shared__ uint32_t key[SEQS];
+    __shared__ int base[SEQS + 1], starts_s[2][SEQS + 1];
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        v_bad = 0;
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&bars.item_full[t], 1);
+            mbar_init(&bars.item_empty[t], item_readers<D>());
+            mbar_init(&bars.q_full[t], 1);
+            mbar_init(&bars.q_empty[t], 1);
+            mbar_init(&bars.s_full[t], 1);
+            mbar_init(&bars.s_free[t], SOFTMAX_WARPS_PER_TILE);       // one arrival per softmax warp
+            mbar_init(&bars.p_ready[t], SOFTMAX_WARPS_PER_TILE);
+            mbar_init(&bars.o_done[t], 1);
+        }
+        for (int s = 0; s < 8; ++s) {
+            // (with an issuer per slot, an operand tile collects one release from each of them)
+            mbar_init(&bars.k_full[s], 1); mbar_init(&bars.k_empty[s], SEP ? 2 : 1);
+        }
+        for (int s = 0; s < 4; ++s) { mbar_init(&bars.v_full[s], 1); mbar_init(&bars.v_empty[s], SEP ? 2 : 1); }
+        fence_mbar_init();
+    }
+    if (warp == 1) { tmem_alloc(&tmem_base_s, 512); tmem_relinquish(); }
+    // rows of a tile that no box reaches (groups that do not divide 128) stay zero
+    if (pa.tokens * pa.group < TILE)
+        for (int i = threadIdx.x; i < 2 * Cfg::TILE_BYTES / 16; i += persist_threads<D>()) reinterpret_cast<uint4*>(sQ)[i] = make_uint4(0, 0, 0, 0);
+    volatile int* abortp = &abort_flag;
+    // Everything above (barriers, TMEM) overlaps the end of the kernel before this one in the stream; global memory
+    // is touched only from here on.  The kernel after this one is let in when a CTA's work is done: let in at once, its
+    // waiting CTAs cost a layer of n = 512 0.9 us (31.8 -> 30.9) and a block of n = 1024 1.4 us.
+    grid_dependency_wait();
+    // the counter block of the NEXT call on this workspace is cleared here, off that call's critical path
+    if (threadIdx.x == 0 && blockIdx.x == 0 && dc_next) *dc_next = DeviceCounters{0, 0, 0, 0, 0, 0, 0};
+    // ---- the work list
+    int n2 = 1;                                  // sequences, rounded up to a power of two
+    while (n2 < pa.sequences) n2 *= 2;
+    for (int i = threadIdx.x; i <= pa.sequences; i += persist_threads<D>()) {
+        starts_s[0][i] = min(max(pa.q_starts[i], 0), pa.q_rows);
+        starts_s[1][i] = min(max(pa.k_starts[i], 0), pa.k_rows);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n2; i += persist_threads<D>()) {
+        const int nq = i < pa.sequences ? max(starts_s[0][i + 1] - starts_s[0][i], 0) : 0;
+        key[i] = (uint32_t)((nq + 2 * pa.tokens - 1) / (2 * pa.tokens)) << SEQ_BITS | (uint32_t)(SEQS - 1 - i);
+    }
+    for (int k = 2; k <= n2; k *= 2)             // bitonic, descending
+        for (int j = k / 2; j > 0; j /= 2) {
+            __syncthreads();
+            const int i = 2 * j * ((int)threadIdx.x / j) + (int)threadIdx.x % j;
+            if (i + j < n2 && (int)threadIdx.x < n2 / 2) {
+                const uint32_t x = key[i], y = key[i + j];
+                if ((x < y) == ((i & k) == 0)) { key[i] = y; key[i + j] = x; }
+            }
+        }
+    __syncthreads();
+    if (warp == 0) {
+        // base[k]: items (of one head) ahead of the levels that exactly the k + 1 longest sequences have
+        long long sum = 0;
+        for (int k0 = 0; k0 < pa.sequences; k0 += 32) {
+            const int k = k0 + lane;
+            const int mine = k < pa.sequences ? (int)(key[k] >> SEQ_BITS) : 0, next = k + 1 < pa.sequences ? (int)(key[k + 1] >> SEQ_BITS) : 0;
+            const long long own = k < pa.sequences ? (long long)(mine - next) * (k + 1) : 0;
+            long long x = own;
+#pragma unroll
+            for (int s = 1; s < 32; s *= 2) {
+                const long long y = __shfl_up_sync(0xffffffffu, x, s);
+                if (lane >= s) x += y;
+            }
+            if (k < pa.sequences) base[k] = (int)(sum + x - own);
+            sum += __shfl_sync(0xffffffffu, x, 31);
+        }
+        if (lane == 0) {
+            // (more rows than there are: `starts` that do not ascend; nothing is computed, and the call reports it)
+            const bool bad = sum > pa.q_rows / (2 * pa.tokens) + pa.sequences;
+            if (bad) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
+            base[pa.sequences] = bad ? 0 : (int)sum;
+        }
+    }
+    fence_async_smem();                          // (the zeroed rows, ahead of the loads beside them)
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_s;
+    const int nitems = base[pa.sequences] * pa.kv_heads;
+    // Item idx: the pairs of row tiles are counted level by level from the last one of the longest sequence down to the first of all, heads innermost.
+    auto decode = [&](int idx) -> Item {
+        const int e = (int)fastdiv((uint32_t)idx, pa.by_heads);
+        int lo = 0, hi = pa.sequences - 1;       // the last k with base[k] <= e
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (base[mid] <= e) lo = mid; else hi = mid - 1;
+        }
+        const int r = e - base[lo], level = (int)(key[lo] >> SEQ_BITS) - 1 - r / (lo + 1);
+        const int b = SEQS - 1 - (int)(key[r % (lo + 1)] & (SEQS - 1));
+        Item w;
+        w.q0 = starts_s[0][b]; w.k0 = starts_s[1][b];
+        w.nq = starts_s[0][b + 1] - w.q0; w.nk = max(starts_s[1][b + 1] - w.k0, 0);
+        w.i0 = 2 * level * pa.tokens;
+        w.h = idx - e * pa.kv_heads;
+        // blocks up to the last key that the tile's last row sees
+        auto blocks = [&](int i0) { return i0 >= w.nq ? 0 : max(min(i0 + pa.tokens, w.nq) + w.nk - w.nq + TILE - 1, 0) / TILE; };
+        w.nkv0 = blocks(w.i0);
+        w.nkv1 = blocks(w.i0 + pa.tokens);
+        return w;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            // ------------------------------------------------------------ scheduler + TMA producer
+            // kc, vc: K and V tiles requested so far (ring position); qc[t]: loads of Q buffer t so far.
+            uint32_t kc = 0, vc = 0, qc[2] = {0, 0};
+            int idx = blockIdx.x;          // the grid never exceeds the item count
+            bool ok = true;
+            for (uint32_t it = 0; ok; ++it) {
+                const int slot = it & 1;
+                if (it >= 2) ok = mbar_wait(&bars.item_empty[slot], ((it >> 1) - 1) & 1, abortp);
+                if (!ok) break;
+                if (idx >= nitems) {
+                    item_ring[slot].h = -1;
+                    mbar_arrive(&bars.item_full[slot]);
+                    break;
+                }
+                const Item work = decode(idx);
+                item_ring[slot] = work;
+                mbar_arrive(&bars.item_full[slot]);
+                int next = -1;
+                const int h = work.h, nkv[2] = {work.nkv0, work.nkv1};
+                const int maxkv = max(nkv[0], nkv[1]);
+                auto take_next = [&] { next = cursor ? (int)gridDim.x + (int)atomicAdd(cursor, 1u) : idx + (int)gridDim.x; };
+                if (maxkv == 0) {                // rows without keys: nothing to load
+                    take_next();
+                    idx = next;
+                    continue;
+                }
+                auto load_q = [&] {
+                    for (int t = 0; t < 2 && ok; ++t) {
+                        if (nkv[t] == 0) continue;
+                        if (qc[t] > 0) ok = mbar_wait(&bars.q_empty[t], (qc[t] - 1) & 1, abortp);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx(&bars.q_full[t], Cfg::SUB * pa.tokens * pa.group * 128);
+                        for (int u = 0; u < Cfg::SUB; ++u)
+                            tma_load_4d(sQ + t * Cfg::TILE_BYTES + u * 16384, &maps.q, &bars.q_full[t], 64 * u, 0, h, work.q0 + work.i0 + t * pa.tokens);
+                        ++qc[t];
+                    }
+                };
+                if constexpr (PAIRED) {
+                    for (int p = 0; p <= maxkv && ok; ++p) {           // pair p = (V_{p-1}, K_p); vc counts pairs here
+                        const int s = vc % VST;
+                        if (vc >= (uint32_t)VST) ok = mbar_wait(&bars.v_empty[s], ((vc / VST) - 1) & 1, abortp);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx(&bars.v_full[s], ((p > 0) + (p < maxkv)) * Cfg::TILE_BYTES);
+                        if (p < maxkv)
+                            for (int u = 0; u < Cfg::SUB; ++u)
+                                tma_load_3d(sK + s * Cfg::TILE_BYTES + u * 16384, &maps.k, &bars.v_full[s], 64 * u, h, work.k0 + p * TILE);
+                        if (p > 0)
+                            for (int u = 0; u < Cfg::SUB; ++u)
+                                tma_load_3d(sV + s * Cfg::TILE_BYTES + u * 16384, &maps.v, &bars.v_full[s], 64 * u, h, work.k0 + (p - 1) * TILE);
+                        ++vc;
+                        if (p == 0) {
+                            load_q();
+                            if (!ok) break;
+                        }
+                        // the next item's index is fetched behind the item's first loads and long before it is needed
+                        if (p == 1) take_next();
+                    }
+                } else {
+                    for (int j = 0; j < maxkv && ok; ++j) {
+                        {
+                            const int s = kc % KST;
+                            if (kc >= (uint32_t)KST) ok = mbar_wait(&bars.k_empty[s], ((kc / KST) - 1) & 1, abortp);
+                            if (!ok) break;
+                            mbar_arrive_expect_tx(&bars.k_full[s], Cfg::TILE_BYTES);
+                            for (int u = 0; u < Cfg::SUB; ++u)
+                                tma_load_3d(sK + s * Cfg::TILE_BYTES + u * 16384, &maps.k, &bars.k_full[s], 64 * u, h, work.k0 + j * TILE);
+                            ++kc;
+                        }
+                        if (j == 0) {
+                            load_q();
+                            if (!ok) break;
+                        }
+                        {
+                            const int s = vc % VST;
+                            if (vc >= (uint32_t)VST) ok = mbar_wait(&bars.v_empty[s], ((vc / VST) - 1) & 1, abortp);
+                            if (!ok) break;
+                            mbar_arrive_expect_tx(&bars.v_full[s], Cfg::TILE_BYTES);
+                            for (int u = 0; u < Cfg::SUB; ++u)
+                                tma_load_3d(sV + s * Cfg::TILE_BYTES + u * 16384, &maps.v, &bars.v_full[s], 64 * u, h, work.k0 + j * TILE);
+                            ++vc;
+                        }
+                        // the next item's index is fetched behind the item's first loads (the atomic's round trip of about
+                        // a thousand cycles would otherwise delay them) and long before it is needed
+                        if (j == 0) take_next();
+                    }
+                }
+                idx = next;
+            }
+            if (*abortp) {  // let copies already issued land before shared memory is released
+                for (int t = 0; t < 2; ++t)
+                    if (qc[t] > 0) mbar_wait_drain(&bars.q_full[t], (qc[t] - 1) & 1);
+                for (uint32_t c = kc > (uint32_t)KST ? kc - KST : 0; c < kc; ++c)
+                    mbar_wait_drain(&bars.k_full[c % KST], (c / KST) & 1);
+                for (uint32_t c = vc > (uint32_t)VST ? vc - VST : 0; c < vc; ++c)
+                    mbar_wait_drain(&bars.v_full[c % VST], (c / VST) & 1);
+            }
+        }
+    } else if (SEP && (warp == 1 || warp == ISSUER1_WARP)) {
+        if (elect_one()) {
+            // ------------------------------------------------------------ MMA issuer of row tile slot t (d = 64)
+            // (One elected lane of the converged warp: `lane == 0` is 5 % slower here, 128 heads of n = 4096, FULL 849 and 805 us; with one
+            // issuer for both slots, below, it is the other way round, 256 heads of n = 4096, d = 128 1821 and 1940 us.)
+            // The slot's blocks form a chain S_0, S_1 | PV_0, S_2 | PV_1, ...: with P in its own TMEM columns S_{j+1}
+            // needs only that the softmax warps have read S_j, PV_j needs P_j.  The thread issues the links in that
+            // order, sleeping on the barriers of each; the two slots' threads walk the item list independently.
+            const int t = warp == 1 ? 0 : 1;
+            const uint32_t idescS = idesc<F16>(128, 128, UMMA_K_MAJOR, UMMA_K_MAJOR);
+            const uint32_t idescO = idesc<F16>(128, 16 * KS, UMMA_K_MAJOR, UMMA_MN_MAJOR);
+            unsigned long long qk_blocks = 0, pv_blocks = 0;
+            const uint32_t q_lo = umma_desc_lo_kmajor(smem_u32(sQ + t * Cfg::TILE_BYTES));
+            const uint32_t k_lo = umma_desc_lo_kmajor(smem_u32(sK));
+            const uint32_t v_lo = umma_desc_lo_mnmajor(smem_u32(sV), 16384);
+            const uint32_t dS = tmem + Cfg::TMEM_S + t * 128, dO = tmem + Cfg::TMEM_O + t * D;
+            const uint32_t aP = tmem + Cfg::TMEM_P + t * 64;
+            uint32_t kbase = 0, vbase = 0;      // ring positions of the current item's first K and V tile
+            uint32_t parts = 0;                 // earlier items in which this slot had rows
+            uint32_t blk0 = 0;                  // blocks of this slot in all earlier items
+            bool ok = true;
+            auto mma_S = [&](uint32_t kc) {     // S = Q K^T with K at ring position kc (phase 1, Eq. 1)
+                const uint32_t k = k_lo + (kc % KST) * (Cfg::TILE_BYTES >> 4);
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) {
+                    const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+                    umma_ss(dS, umma_desc_join(q_lo + off, UMMA_DESC_HI_SW128), umma_desc_join(k + off, UMMA_DESC_HI_SW128),
+                            idescS, kk != 0);
+                }
+                ++qk_blocks;
+            };
+            auto mma_PV = [&](uint32_t vc, bool first) {   // O (+)= P V with V at ring position vc (phase 3, Eq. 3)
+                const uint32_t v = v_lo + (vc % VST) * (Cfg::TILE_BYTES >> 4);
+                if (first) {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        umma_ts(dO, aP + kk * 8, umma_desc_join(v + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, kk != 0);
+                } else {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        umma_ts(dO, aP + kk * 8, umma_desc_join(v + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, 1);
+                }
+                ++pv_blocks;
+            };
+            // an operand tile has two releases to collect, one per slot; a slot whose partner has no block j gives both
+            auto release = [&](uint64_t* bar, bool both) {
+                umma_commit(bar);
+                if (both) umma_commit(bar);
+            };
+            for (uint32_t it = 0; ok; ++it) {
+                ok = mbar_wait(&bars.item_full[it & 1], (it >> 1) & 1, abortp);
+                if (!ok) break;
+                const int head = item_ring[it & 1].h, nk0 = item_ring[it & 1].nkv0, nk1 = item_ring[it & 1].nkv1;
+                mbar_arrive(&bars.item_empty[it & 1]);
+                if (head < 0) break;
+                const int nkv = t ? nk1 : nk0, nkv_other = t ? nk0 : nk1;
+                if (nkv > 0) {
+                    // first scores of the item (the softmax warps must have taken the slot's previous scores out of TMEM)
+                    ok = mbar_wait(&bars.q_full[t], parts & 1, abortp) &&
+                         mbar_wait(&bars.k_full[kbase % KST], (kbase / KST) & 1, abortp);
+                    if (ok && blk0 > 0) ok = mbar_wait(&bars.s_free[t], (blk0 - 1) & 1, abortp);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_S(kbase);
+                    umma_commit(&bars.s_full[t]);
+                    release(&bars.k_empty[kbase % KST], 0 >= nkv_other);
+                    if (nkv == 1) umma_commit(&bars.q_empty[t]);
+                    for (int j = 0; j < nkv && ok; ++j) {
+                        const uint32_t vc = vbase + j, kc = kbase + j + 1;
+                        if (j + 1 < nkv) {
+                            // S_{j+1} as soon as S_j has been read: it runs under the exponentials of block j
+                            ok = mbar_wait(&bars.k_full[kc % KST], (kc / KST) & 1, abortp) &&
+                                 mbar_wait(&bars.s_free[t], (blk0 + j) & 1, abortp);
+                            if (!ok) break;
+                            tc_fence_after();
+                            mma_S(kc);
+                            umma_commit(&bars.s_full[t]);
+                            release(&bars.k_empty[kc % KST], j + 1 >= nkv_other);
+                            if (j + 1 == nkv - 1) umma_commit(&bars.q_empty[t]);
+                        }
+                        ok = mbar_wait(&bars.v_full[vc % VST], (vc / VST) & 1, abortp);
+                        if (ok) ok = mbar_wait(&bars.p_ready[t], (blk0 + j) & 1, abortp);
+                        if (!ok) break;
+                        tc_fence_after();
+                        mma_PV(vc, j == 0);
+                        umma_commit(&bars.o_done[t]);
+                        release(&bars.v_empty[vc % VST], j >= nkv_other);
+                    }
+                    ++parts;
+                    blk0 += nkv;
+                }
+                // loads for the other slot alone: seen to land, so that no barrier is ever waited for two phases ahead
+                for (int j = nkv; j < nkv_other && ok; ++j)
+                    ok = mbar_wait(&bars.k_full[(kbase + j) % KST], ((kbase + j) / KST) & 1, abortp) && mbar_wait(&bars.v_full[(vbase + j) % VST], ((vbase + j) / VST) & 1, abortp);
+                kbase += max(nk0, nk1);
+                vbase += max(nk0, nk1);
+            }
+            const unsigned long long block_macs = (unsigned long long)TILE * TILE * D;
+            if (qk_blocks) atomicAdd(&dc->qk_macs, qk_blocks * block_macs);
+            if (pv_blocks) {
+                atomicAdd(&dc->pv_macs, pv_blocks * block_macs);
+                atomicAdd(&dc->exps, pv_blocks * (unsigned long long)(TILE * TILE));
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            // ------------------------------------------------------------ MMA issuer
+            // (d = 128) Each row tile's blocks form a chain S_0, PV_0, S_1, PV_1, ...  The two tiles' chains are issued
+            // alternately: while the softmax warps of one tile work on their scores, the tensor pipe runs the
+            // other tile's MMAs, and it is this half-step offset that keeps the pipe busy.  P overlays S, so PV_j
+            // and S_{j+1} of a tile go back to back under one commit, and the thread sleeps on what each link
+            // needs, tile 0 then tile 1 then tile 0 ...
+            const uint32_t idescS = idesc<F16>(128, 128, UMMA_K_MAJOR, UMMA_K_MAJOR);
+            const uint32_t idescO = idesc<F16>(128, 16 * KS, UMMA_K_MAJOR, UMMA_MN_MAJOR);
+            unsigned long long qk_blocks = 0, pv_blocks = 0;
+            const uint32_t q_lo[2] = {umma_desc_lo_kmajor(smem_u32(sQ)), umma_desc_lo_kmajor(smem_u32(sQ + Cfg::TILE_BYTES))};
+            const uint32_t k_lo = umma_desc_lo_kmajor(smem_u32(sK));
+            const uint32_t v_lo = umma_desc_lo_mnmajor(smem_u32(sV), 16384);
+            const uint32_t tS0 = tmem + Cfg::TMEM_S, tO0 = tmem + Cfg::TMEM_O;
+            uint32_t kbase = 0, vbase = 0;      // ring positions of the current item's first K and V tile
+            uint32_t parts[2] = {0, 0};         // earlier items in which tile slot t had rows
+            uint32_t blk0[2] = {0, 0};          // blocks of tile slot t in all earlier items
+            bool ok = true;
+            // S_t = Q_t K^T with K at ring position kc (phase 1, Eq. 1): D/16 MMAs of 128x128x16.
+            auto mma_S = [&](int t, uint32_t kc) {
+                const uint32_t q = q_lo[t], k = k_lo + (kc % KST) * (Cfg::TILE_BYTES >> 4);
+                const uint32_t dS = tS0 + t * 128;
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) {
+                    const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+                    umma_ss(dS, umma_desc_join(q + off, UMMA_DESC_HI_SW128), umma_desc_join(k + off, UMMA_DESC_HI_SW128),
+                            idescS, kk != 0);
+                }
+                ++qk_blocks;
+            };
+            // O_t (+)= P_t V with V at ring position vc (phase 3, Eq. 3): 8 MMAs of 128 x D x 16.
+            auto mma_PV = [&](int t, uint32_t vc, bool first) {
+                const uint32_t v = v_lo + (vc % VST) * (Cfg::TILE_BYTES >> 4);
+                const uint32_t dO = tO0 + t * D;
+                const uint32_t aP = SEP ? tmem + Cfg::TMEM_P + t * 64 : tS0 + t * 128;
+                if (first) {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        umma_ts(dO, aP + kk * 8,
+                                umma_desc_join(v + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, kk != 0);
+                } else {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        umma_ts(dO, aP + kk * 8,
+                                umma_desc_join(v + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, 1);
+                }
+                ++pv_blocks;
+            };
+            for (uint32_t it = 0; ok; ++it) {
+                ok = mbar_wait(&bars.item_full[it & 1], (it >> 1) & 1, abortp);
+                if (!ok) break;
+                const int head = item_ring[it & 1].h, nkv[2] = {item_ring[it & 1].nkv0, item_ring[it & 1].nkv1};
+                mbar_arrive(&bars.item_empty[it & 1]);
+                if (head < 0) break;
+                const int maxkv = max(nkv[0], nkv[1]);
+                if (maxkv == 0) continue;
+                {
+                    // first scores of both tiles (PAIRED: kbase = vbase = the ring position of the item's pair 0, which
+                    // holds K_0 alone; pair j + 1 holds V_j and K_{j+1})
+                    if constexpr (PAIRED) ok = mbar_wait(&bars.v_full[vbase % VST], (vbase / VST) & 1, abortp);
+                    else ok = mbar_wait(&bars.k_full[kbase % KST], (kbase / KST) & 1, abortp);
+                    for (int t = 0; t < 2 && ok; ++t) {
+                        if (nkv[t] == 0) continue;
+                        ok = mbar_wait(&bars.q_full[t], parts[t] & 1, abortp);
+                        if (!ok) break;
+                        tc_fence_after();
+                        mma_S(t, kbase);
+                        umma_commit(&bars.s_full[t]);
+                        if (nkv[t] == 1) umma_commit(&bars.q_empty[t]);
+                    }
+                    if (!ok) break;
+                    if constexpr (PAIRED) umma_commit(&bars.v_empty[vbase % VST]);
+                    else umma_commit(&bars.k_empty[kbase % KST]);
+                    for (int j = 0; j < maxkv && ok; ++j) {
+                        for (int t = 0; t < 2 && ok; ++t) {
+                            if (j >= nkv[t]) continue;
+                            const uint32_t vc = vbase + j + (PAIRED ? 1 : 0), kc = kbase + j + 1;
+                            const bool has_next = j + 1 < nkv[t];
+                            // Operand tiles first.  A probe of a barrier costs this thread 150-200 cycles beside the
+                            // busy softmax warps, so slot 1 does not repeat the ones slot 0 made for the same block.
+                            if (t == 0 || j >= nkv[0]) ok = mbar_wait(&bars.v_full[vc % VST], (vc / VST) & 1, abortp);
+                            if constexpr (!PAIRED)
+                                if (ok && has_next && (t == 0 || j + 1 >= nkv[0]))
+                                    ok = mbar_wait(&bars.k_full[kc % KST], (kc / KST) & 1, abortp);
+                            if (ok) ok = mbar_wait(&bars.p_ready[t], (blk0[t] + j) & 1, abortp);
+                            if (!ok) break;
+                            tc_fence_after();
+                            mma_PV(t, vc, j == 0);
+                            if (has_next) mma_S(t, kc);
+                            umma_commit(&bars.o_done[t]);
+                            // an operand tile is released behind its last user in this fixed order
+                            const bool last_v = t == 1 || j >= nkv[1];
+                            if (last_v) umma_commit(&bars.v_empty[vc % VST]);
+                            if (has_next) {
+                                if constexpr (!PAIRED)
+                                    if (t == 1 || j + 1 >= nkv[1]) umma_commit(&bars.k_empty[kc % KST]);
+                                if (j + 1 == nkv[t] - 1) umma_commit(&bars.q_empty[t]);
+                            }
+                        }
+                    }
+                }
+                kbase += maxkv + (PAIRED ? 1 : 0);
+                vbase += maxkv + (PAIRED ? 1 : 0);
+                for (int t = 0; t < 2; ++t) { parts[t] += nkv[t] > 0; blk0[t] += nkv[t]; }
+            }
+            const unsigned long long block_macs = (unsigned long long)TILE * TILE * D;
+            if (qk_blocks) atomicAdd(&dc->qk_macs, qk_blocks * block_macs);
+            if (pv_blocks) {
+                atomicAdd(&dc->pv_macs, pv_blocks * block_macs);
+                atomicAdd(&dc->exps, pv_blocks * (unsigned long long)(TILE * TILE));
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ softmax + epilogue
+        // Eight warps per row tile.  A warp owns 16 rows (TMEM lanes) and reads them in the quad layout (sm100.cuh): the
+        // four threads of a quad share two rows, A and B = A + 8, each holding every fourth pair of their columns, so a
+        // row maximum or row sum is two shuffles inside the quad and the warps never wait for one another.
+        const int sw = warp - CTRL_WARPS;
+        const int t = sw / SOFTMAX_WARPS_PER_TILE;              // row tile slot of this warp
+        const int wq = sw % SOFTMAX_WARPS_PER_TILE;             // warp inside the slot
+        const int q = warp & 3;                                 // TMEM lane quarter this warp may access
+        const int row0 = q * 32 + (wq >> 2) * 16;               // first of the warp's 16 rows inside the tile
+        const int rA = row0 + (lane >> 2), rB = rA + 8;         // this thread's rows
+        const int cq = 2 * (lane & 3);                          // its first column inside every group of 8
+        const uint32_t lane_off = static_cast<uint32_t>(row0) << 16;
+        const uint32_t tS = tmem + Cfg::TMEM_S + t * 128 + lane_off;
+        const uint32_t tO = tmem + Cfg::TMEM_O + t * D + lane_off;
+        const uint32_t tP = SEP ? tmem + Cfg::TMEM_P + t * 64 + lane_off : tS;     // P: 64 columns, over S at d = 128
+        uint8_t* stage = sStage + (t * SOFTMAX_WARPS_PER_TILE + wq) * Cfg::STAGE_BYTES;   // this warp's output staging buffer
+        uint32_t my_items = 0;                                  // items this tile slot took part in
+        uint32_t blk = 0;                                       // blocks this tile slot has processed, all items
+        uint32_t vbase = 0;                                     // ring position of the item's first V tile (PAIRED: of its pair 0)
+        bool ok = true;
+        // this thread's rows as tokens of a tile and heads of a group; rows that the warp stores: lane / 4 and lane / 4 + 8
+        const int tokA = (int)fastdiv((uint32_t)rA, pa.by_group), tokB = (int)fastdiv((uint32_t)rB, pa.by_group);
+        const int headA = rA - tokA * pa.group, headB = rB - tokB * pa.group;
+        // Takes entry `it` of the item ring; h = -1 at the end of the list, -2 when the wait ran out.
+        auto take_item = [&](uint32_t it) -> Item {
+            Item w;
+            w.h = -2;
+            if (!__all_sync(0xffffffffu, mbar_wait(&bars.item_full[it & 1], (it >> 1) & 1, abortp))) return w;
+            w = item_ring[it & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.item_empty[it & 1]);
+            return w;
+        };
+        uint32_t it = 0;
+        Item work = take_item(it++);
+        while (work.h >= 0) {
+            const int nkv = t ? work.nkv1 : work.nkv0, i0 = work.i0 + t * pa.tokens;
+            const int vfirst = vbase + (PAIRED ? 1 : 0);
+            if (max(work.nkv0, work.nkv1) > 0) vbase += max(work.nkv0, work.nkv1) + (PAIRED ? 1 : 0);
+            const bool liveA = i0 + tokA < work.nq && tokA < pa.tokens, liveB = i0 + tokB < work.nq && tokB < pa.tokens;
+            const size_t outA = (size_t)(work.q0 + i0 + tokA) * pa.heads + work.h * pa.group + headA, outB = (size_t)(work.q0 + i0 + tokB) * pa.heads + work.h * pa.group + headB;
+            if (nkv == 0) {                                     // rows without keys, or no rows
+                if (liveA || liveB)
+                    for (int c = 8 * (lane & 3); c < pa.d; c += 32) {
+                        if (liveA) *reinterpret_cast<uint4*>(pa.out + outA * pa.d + c) = make_uint4(0, 0, 0, 0);
+                        if (liveB) *reinterpret_cast<uint4*>(pa.out + outB * pa.d + c) = make_uint4(0, 0, 0, 0);
+                    }
+                if (pa.lse && (lane & 3) == 0) {
+                    if (liveA) pa.lse[outA] = -INFINITY;
+                    if (liveB) pa.lse[outB] = -INFINITY;
+                }
+                work = take_item(it++);
+                continue;
+            }
+            // the last keys that the rows see, and the first block that not all rows of the tile see in full
+            const int off = work.nk - work.nq;
+            const int limA = min(i0 + tokA + off, work.nk - 1), limB = min(i0 + tokB + off, work.nk - 1);
+            const int part0 = max(i0 + off + 1, 0) / TILE;
+            float mA = -INFINITY, mB = -INFINITY, lA = 0.f, lB = 0.f;       // running maxima (log2 units) and row sums
+            for (int j = 0; j < nkv; ++j, ++blk) {
+                if (SEP) {
+                    ok = mbar_wait(&bars.s_full[t], blk & 1, abortp);                 // every S has its own commit
+                } else {
+                    // block 0 waits for the item's first S; later blocks for the commit behind PV_{j-1} and S_j
+                    if (j == 0) ok = mbar_wait(&bars.s_full[t], my_items & 1, abortp);
+                    else ok = mbar_wait(&bars.o_done[t], (blk - 1) & 1, abortp);
+                }
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const bool diag = j >= part0;
+                const int cbA = limA - j * TILE, cbB = limB - j * TILE;         // last kept columns
+                // ---- the rows' 2 x 64 scores of this block
+                uint32_t s0[32], s1[32];
+                tc_fence_after();
+                tmem_ld_quad64(tS, s0);
+                tmem_ld_quad64(tS + 64, s1);
+                tc_wait_ld();
+                if (SEP) {
+                    // S is in registers: the issuer may overwrite it with the next scores while the exponentials run
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.s_free[t]);
+                }
+                // ---- pass 1: row maxima of the block, completed inside the quad
+                float bA = -INFINITY, bB = -INFINITY;
+                if (diag) {
+                    mask_quad64(s0, cq, cbA, cbB);
+                    mask_quad64(s1, 64 + cq, cbA, cbB);
+                }
+                max_quad64(s0, bA, bB);
+                max_quad64(s1, bA, bB);
+                bA = quad_max(bA) * pa.sl2;
+                bB = quad_max(bB) * pa.sl2;
+                float alphaA = 1.f, alphaB = 1.f;
+                if (bA > mA + RESCALE_THRESHOLD) {   // also taken on the first block (m = -inf)
+                    alphaA = ex2_mufu(mA - bA);
+                    mA = bA;
+                }
+                if (bB > mB + RESCALE_THRESHOLD) {
+                    alphaB = ex2_mufu(mB - bB);
+                    mB = bB;
+                }
+                // ---- pass 2: P = exp2(S*sl2 - m) as bf16, keys 0-63 then keys 64-127
+                float sumA = 0.f, sumB = 0.f;
+                uint32_t pk[16];
+                const float nmA = mA == -INFINITY ? 0.f : -mA, nmB = mB == -INFINITY ? 0.f : -mB;     // (rows that have seen no key)
+                exp_quad<F16>(s0, pa.sl2, nmA, nmB, pk, sumA, sumB);
+                if (SEP && blk > 0) {
+                    // P and O are still in use by the PV before this one until its commit
+                    ok = mbar_wait(&bars.o_done[t], (blk - 1) & 1, abortp);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                tmem_st_quad32(tP, pk);
+                exp_quad<F16>(s1, pa.sl2, nmA, nmB, pk, sumA, sumB);
+                tmem_st_quad32(tP + 32, pk);
+                lA = fmaf(lA, alphaA, sumA);
+                lB = fmaf(lB, alphaB, sumB);
+                if (j > 0 && __any_sync(0xffffffffu, alphaA != 1.f || alphaB != 1.f)) {   // rare: a row maximum grew by > 2^8
+                    const int nA = __popc(__ballot_sync(0xffffffffu, (lane & 3) == 0 && alphaA != 1.f));
+                    const int nB = __popc(__ballot_sync(0xffffffffu, (lane & 3) == 0 && alphaB != 1.f));
+                    if (lane == 0) atomicAdd(&dc->rescales, (unsigned long long)(nA + nB));
+#pragma unroll 1
+                    for (int c = 0; c < D / 64; ++c) {
+                        uint32_t v[32];
+                        tmem_ld_quad64(tO + 64 * c, v);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) {
+                            v[4 * g] = __float_as_uint(__uint_as_float(v[4 * g]) * alphaA);
+                            v[4 * g + 1] = __float_as_uint(__uint_as_float(v[4 * g + 1]) * alphaA);
+                            v[4 * g + 2] = __float_as_uint(__uint_as_float(v[4 * g + 2]) * alphaB);
+                            v[4 * g + 3] = __float_as_uint(__uint_as_float(v[4 * g + 3]) * alphaB);
+                        }
+                        tmem_st_quad64(tO + 64 * c, v);
+                    }
+                }
+                if (diag) {
+                    // the warp's share of the tile of V: what is not finite becomes zero
+                    const uint32_t vc = vfirst + j;
+                    ok = __all_sync(0xffffffffu, mbar_wait(&bars.v_full[vc % VST], (vc / VST) & 1, abortp));
+                    if (!ok) break;
+                    uint4* v = reinterpret_cast<uint4*>(sV + (vc % VST) * Cfg::TILE_BYTES) + wq * (Cfg::TILE_BYTES / 16 / SOFTMAX_WARPS_PER_TILE) + lane;
+                    constexpr uint32_t EXP = F16 ? 0x7c007c00u : 0x7f807f80u, ONE = F16 ? 0x04000400u : 0x00800080u;
+                    uint32_t bad = 0;
+#pragma unroll
+                    for (int i = 0; i < Cfg::TILE_BYTES / 16 / SOFTMAX_WARPS_PER_TILE / 32; ++i) {
+                        const uint4 x = v[32 * i];
+                        bad |= ((x.x & EXP) + ONE) | ((x.y & EXP) + ONE) | ((x.z & EXP) + ONE) | ((x.w & EXP) + ONE);
+                    }
+                    if (__any_sync(0xffffffffu, bad & 0x80008000u)) {
+                        if (lane == 0) atomicMax(&v_bad, (int)it);      // (it: items taken so far, this one included)
+                        __threadfence_block();
+                        __syncwarp();
+                        for (int i = 0; i < Cfg::TILE_BYTES / 16 / SOFTMAX_WARPS_PER_TILE / 32; ++i) {
+                            uint32_t* x = reinterpret_cast<uint32_t*>(v + 32 * i);
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t m = ((x[k] & EXP) + ONE) & 0x80008000u;
+                                if (m) x[k] &= ~((m >> 15) * 0xffffu);
+                            }
+                        }
+                        fence_async_smem();
+                    }
+                }
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.p_ready[t]);      // (one arrival per warp: 32 on one barrier serialise)
+            }
+            if (!ok) break;
+            // The next item is taken now, while the last PV runs, rather than after the epilogue.
+            const int items_now = (int)it;
+            const Item work_next = take_item(it++);
+            if (work_next.h == -2) break;
+            ok = mbar_wait(&bars.o_done[t], (blk - 1) & 1, abortp);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            // ---- epilogue: O / l, 32 columns at a time through the warp's staging buffer (chunks of 16 bytes swizzled) to whole sectors of the rows
+            tc_fence_after();
+            lA = quad_sum(lA);
+            lB = quad_sum(lB);
+            const float invA = lA == 0.f ? 0.f : 1.f / lA, invB = lB == 0.f ? 0.f : 1.f / lB;
+            if (pa.lse && (lane & 3) == 0) {
+                if (liveA) pa.lse[outA] = lA == 0.f ? -INFINITY : (mA + log2f(lA)) * LN2;
+                if (liveB) pa.lse[outB] = lB == 0.f ? -INFINITY : (mB + log2f(lB)) * LN2;
+            }
+            const bool bad = *reinterpret_cast<volatile int*>(&v_bad) >= items_now;
+#pragma unroll
+            for (int u = 0; u < Cfg::SUB; ++u) {
+                uint32_t v[32];
+                tmem_ld_quad64(tO + 64 * u, v);
+                tc_wait_ld();
+                if (bad) {
+                    // values that are not finite were left out of the blocks from the item's first partial one on: rows that see them get them back
+                    const int first = max(work.i0 + off + 1, 0) / TILE * TILE;
+                    for (int k = first; k <= max(limA, limB); ++k) {
+                        const uint16_t* row = pa.v + (size_t)(work.k0 + k) * pa.v_stride + work.h * pa.d;
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) {
+                            const int c = 64 * u + 8 * g + cq;
+                            if (c >= pa.d) continue;
+                            const float2 x = F16 ? __half22float2(*reinterpret_cast<const __half2*>(row + c)) : __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(row + c));
+                            const float ax = isfinite(x.x) ? 0.f : x.x, ay = isfinite(x.y) ? 0.f : x.y;
+                            if (k <= limA) { v[4 * g] = __float_as_uint(__uint_as_float(v[4 * g]) + ax); v[4 * g + 1] = __float_as_uint(__uint_as_float(v[4 * g + 1]) + ay); }
+                            if (k <= limB) { v[4 * g + 2] = __float_as_uint(__uint_as_float(v[4 * g + 2]) + ax); v[4 * g + 3] = __float_as_uint(__uint_as_float(v[4 * g + 3]) + ay); }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int r = lane >> 2;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {               // chunk c of the rows' 64 bytes: columns 8 (4 half + c) + cq, + 1
+                        const int e = 4 * (4 * half + c);
+                        const uint32_t a = pack<F16>(__uint_as_float(v[e]) * invA, __uint_as_float(v[e + 1]) * invA);
+                        const uint32_t bb = pack<F16>(__uint_as_float(v[e + 2]) * invB, __uint_as_float(v[e + 3]) * invB);
+                        const int at = r * 64 + ((c ^ (r >> 1)) & 3) * 16 + 2 * cq;
+                        *reinterpret_cast<uint32_t*>(stage + at) = a;
+                        *reinterpret_cast<uint32_t*>(stage + at + 512) = bb;
+                    }
+                    __syncwarp();
+                    const int at = r * 64 + (((lane & 3) ^ (r >> 1)) & 3) * 16, col = 64 * u + 32 * half + 8 * (lane & 3);
+                    if (col < pa.d) {
+                        if (liveA) *reinterpret_cast<uint4*>(pa.out + outA * pa.d + col) = *reinterpret_cast<const uint4*>(stage + at);
+                        if (liveB) *reinterpret_cast<uint4*>(pa.out + outB * pa.d + col) = *reinterpret_cast<const uint4*>(stage + at + 512);
+                    }
+                    __syncwarp();
+                }
+            }
+            // (the next write to O_t, PV_0 of the tile's next item, waits for P of that item, which every
+            // thread of the tile signals only after these reads)
+            tc_fence_before();
+            ++my_items;
+            work = work_next;
+        }
+        if (sw == 0 && lane == 0) grid_launch_dependents();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && abort_flag) atomicExch(&dc->status, (int)PSA_ERR_TIMEOUT);
+    if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// Row tiles of queries: boxes of `tokens` rows x all heads of a group x 64 columns.
+bool query_map(CUtensorMap* m, const void* Q, int rows, int kv_heads, int group, int d, long long stride, int tokens) {
+    const uint64_t dims[4] = {(uint64_t)d, (uint64_t)group, (uint64_t)kv_heads, (uint64_t)rows}, strides[3] = {(uint64_t)d * 2, (uint64_t)group * d * 2, (uint64_t)stride * 2};
+    const uint32_t box[4] = {64, (uint32_t)group, 1, (uint32_t)tokens};
+    return make_tensor_map_16bit(m, Q, 4, dims, strides, box);
+}
+bool key_map(CUtensorMap* m, const void* K, int rows, int kv_heads, int d, long long stride) {
+    const uint64_t dims[3] = {(uint64_t)d, (uint64_t)kv_heads, (uint64_t)rows}, strides[2] = {(uint64_t)d * 2, (uint64_t)stride * 2};
+    const uint32_t box[3] = {64, 1, TILE};
+    return make_tensor_map_16bit(m, K, 3, dims, strides, box);
+}
+
+template <int D, int KS, bool F16>
+int launch_prompt(const PMaps& maps, const PromptArgs& all, DeviceCounters* dc, unsigned int* cursor, DeviceCounters* dc_next, cudaStream_t stream) {
+    using Cfg = PCfg<D>;
+    static DeviceSetup setup;
+    const int sm_count = device_setup(&setup, [] {
+        return cudaFuncSetAttribute(prompt_kernel<D, KS, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, PCfg<D>::SMEM);
+    }, "prompt kernel set-up");
+    if (sm_count <= 0) return PSA_ERR_CUDA;
+    for (int s0 = 0; s0 < all.sequences; s0 += SEQS) {
+        PromptArgs pa = all;
+        pa.sequences = all.sequences - s0 < SEQS ? all.sequences - s0 : SEQS;
+        pa.q_starts += s0;
+        pa.k_starts += s0;
+        // (an upper bound: the lengths are known on the device only)
+        const long long items = ((long long)pa.q_rows / (2 * pa.tokens) + pa.sequences) * pa.kv_heads;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(items < sm_count ? items : sm_count));
+        cfg.blockDim = dim3(persist_threads<D>());
+        cfg.dynamicSmemBytes = Cfg::SMEM;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // the kernel waits for its predecessor itself
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        // (the counter serves the first launch; the items of further ones go round in turn)
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, prompt_kernel<D, KS, F16>, maps, pa, dc, s0 == 0 ? cursor : nullptr, s0 == 0 ? dc_next : nullptr);
+        if (e != cudaSuccess) { set_cuda_error(e, "prompt_kernel launch"); return PSA_ERR_CUDA; }
+    }
+    return PSA_OK;
+}
+
+}  // namespace
+
+int prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts, const int* k_starts,
+                     int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, DeviceCounters* dc,
+                     unsigned int* cursor, DeviceCounters* dc_next, cudaStream_t stream) {
+    const int group = heads / kv_heads, tokens = TILE / group;
+    if ((long long)q_rows / (2 * tokens) >= 1LL << (32 - SEQ_BITS) || ((long long)q_rows / (2 * tokens) + SEQS) * kv_heads > 0x7fff0000LL) return PSA_ERR_SHAPE;
+    PMaps maps;
+    if (!query_map(&maps.q, Q, q_rows, kv_heads, group, d, q_stride, tokens)) return PSA_ERR_CUDA;
+    maps.k = maps.v = maps.q;                    // (without keys no block of them is ever loaded)
+    if (k_rows > 0 && (!key_map(&maps.k, K, k_rows, kv_heads, d, k_stride) || !key_map(&maps.v, V, k_rows, kv_heads, d, v_stride))) return PSA_ERR_CUDA;
+    const PromptArgs pa = {q_starts, k_starts, sequences, q_rows, k_rows, heads, kv_heads, group, tokens, d, v_stride, static_cast<const uint16_t*>(V),
+                           static_cast<uint16_t*>(out), lse, scale * LOG2E, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)kv_heads)};
+    auto launch = [&](auto width, auto steps) {
+        constexpr int D = decltype(width)::value, KS = decltype(steps)::value;
+        return dtype == PSA_F16 ? launch_prompt<D, KS, true>(maps, pa, dc, cursor, dc_next, stream) : launch_prompt<D, KS, false>(maps, pa, dc, cursor, dc_next, stream);
+    };
+    using std::integral_constant;
+    const integral_constant<int, 64> narrow;
+    const integral_constant<int, 128> wide;
+    // (column steps as in bf16_attention_persist, which gives the measurements)
+    switch ((d + 15) / 16) {
+        case 1: case 2: return launch(narrow, integral_constant<int, 2>{});
+        case 3: case 4: return launch(narrow, integral_constant<int, 4>{});
+        case 5: return launch(wide, integral_constant<int, 5>{});
+        case 6: return launch(wide, integral_constant<int, 6>{});
+        default: return launch(wide, integral_constant<int, 8>{});
+    }
+}
+
+}  // namespace psa

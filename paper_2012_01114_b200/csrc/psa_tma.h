@@ -18,4 +18,8 @@ bool make_tensor_map_bf16(CUtensorMap* map, const void* base, uint64_t rows, uin
 bool make_tensor_map_bf16_4d(CUtensorMap* map, const void* base, uint64_t batch, uint64_t n, uint64_t heads, uint64_t d,
                              uint32_t box_rows);
 
+// Tensor map of `rank` dimensions (innermost first) over 2-byte numbers of any kind; strides[i]: bytes between neighbours in dimension i + 1; boxes of 64
+// elements in the innermost one.
+bool make_tensor_map_16bit(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
+
 }  // namespace psa
