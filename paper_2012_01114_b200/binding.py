@@ -252,7 +252,7 @@ def psa_last_issued(stream=None):
     """(device status, measured census) of the last call; waits for the stream."""
     c = Counts()
     rc = lib().psa_last_issued(_stream(stream), ctypes.byref(c))
-    if rc not in (OK, ERR_TIMEOUT):
+    if rc not in (OK, ERR_TIMEOUT, ERR_SHAPE):
         raise PsaError(rc, "psa_last_issued")
     return rc, c.as_dict()
 
