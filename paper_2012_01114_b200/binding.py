@@ -369,36 +369,39 @@ def psa_attention_sym_f32_noalloc(X, out=None, stream=None):
 
 
 # ---------------------------------------------------------------- serving
+# (On small calls the host side is what takes the time: a function call per argument costs 0.2 us, an attribute of a tensor 0.04.  The checks are
+# therefore written out where they are needed, and what is wrong is named only once something is.)
 _SERVING = {torch.bfloat16: BF16, torch.float16: F16}
+_INT = torch.int32
 
 
-def _rows(t, name, heads, d, dtype=None):
-    """Row stride of a [rows, heads, d] tensor whose heads lie side by side."""
-    if not t.is_cuda or t.dim() != 3 or (dtype is not None and t.dtype != dtype) or t.dtype not in _SERVING:
+def _bad_rows(t, name, heads, d, dtype):
+    if not t.is_cuda or t.dim() != 3 or t.dtype not in _SERVING or t.dtype is not dtype:
         raise ValueError("%s must be a CUDA tensor [rows, heads, d_k] of bf16 or fp16, like the other operands" % name)
-    if (heads is not None and t.shape[1] != heads) or t.shape[2] != d or (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d))):
-        raise ValueError("%s must be [rows, heads, d_k] with the heads of a row side by side" % name)
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * d
+    raise ValueError("%s must be [rows, %d, %d] with the heads of a row side by side" % (name, heads, d))
+
+
+def _rows(t, name, heads, d, dtype):
+    """Row stride of a [rows, heads, d] tensor whose heads lie side by side."""
+    if not t.is_cuda or t.dtype is not dtype or dtype not in _SERVING or t.dim() != 3:
+        _bad_rows(t, name, heads, d, dtype)
+    n, h, c = t.shape
+    row, head, one = t.stride()
+    if h != heads or c != d or (n and h and c and (one != 1 or (h > 1 and head != d))):
+        _bad_rows(t, name, heads, d, dtype)
+    return row if n > 1 else heads * d
 
 
 def _ints(t, name, count=None):
-    if t is None:
-        return None
-    if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or (count is not None and t.numel() != count):
+    if t.dtype is not _INT or not t.is_cuda or not t.is_contiguous() or (count is not None and t.numel() != count):
         raise ValueError("%s must be a contiguous CUDA tensor of int32%s" % (name, "" if count is None else " with %d numbers" % count))
     return t.data_ptr()
 
 
-def _result(t, name, shape, dtype, device):
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.numel() != shape[0] * shape[1]:
-        raise ValueError("%s must be a contiguous CUDA tensor %s of dtype %s" % (name, list(shape), dtype))
-    return t
-
-
-def _lse(t, rows, heads):
-    return None if t is None else _result(t, "lse", (rows, heads), torch.float32, t.device).data_ptr()
+def _given(t, name, rows, cols, dtype):
+    if not t.is_cuda or t.dtype is not dtype or not t.is_contiguous() or t.numel() != rows * cols:
+        raise ValueError("%s must be a contiguous CUDA tensor [%d, %d] of dtype %s" % (name, rows, cols, dtype))
+    return t.data_ptr()
 
 
 def _raise(rc, where):
@@ -411,15 +414,19 @@ def psa_prompt_attention(Q, K, V, q_starts, k_starts=None, scale=None, out=None,
     [sequences + 1] -> out [q_rows, heads * d].  k_starts None: the keys are the queries' tokens.  lse: fp32 [q_rows, heads] to be filled, or None."""
     rows, heads, d = Q.shape
     dtype = Q.dtype
-    kv_heads = K.shape[1]
+    k_rows, kv_heads, _ = K.shape
     if kv_heads == 0 or heads % kv_heads or V.shape != K.shape:
         raise ValueError("K and V must be [k_rows, kv_heads, d_k] with kv_heads a divisor of Q's heads")
-    strides = _rows(Q, "Q", heads, d), _rows(K, "K", kv_heads, d, dtype), _rows(V, "V", kv_heads, d, dtype)
     n = q_starts.numel() - 1
-    out = _result(out, "out", (rows, heads * d), dtype, Q.device)
-    _raise(lib().psa_prompt_attention(Q.data_ptr(), K.data_ptr(), V.data_ptr(), *strides, _ints(q_starts, "q_starts"), _ints(k_starts, "k_starts", n + 1), n, rows,
-                                      K.shape[0], heads, kv_heads, d, d ** -0.5 if scale is None else scale, _SERVING[dtype], out.data_ptr(), _lse(lse, rows, heads),
-                                      _stream(stream)), "psa_prompt_attention")
+    q_stride, k_stride, v_stride = _rows(Q, "Q", heads, d, dtype), _rows(K, "K", kv_heads, d, dtype), _rows(V, "V", kv_heads, d, dtype)
+    if out is None:
+        out = Q.new_empty((rows, heads * d))
+    rc = (_lib or lib()).psa_prompt_attention(Q.data_ptr(), K.data_ptr(), V.data_ptr(), q_stride, k_stride, v_stride, _ints(q_starts, "q_starts"),
+                                              None if k_starts is None else _ints(k_starts, "k_starts", n + 1), n, rows, k_rows, heads, kv_heads, d,
+                                              d ** -0.5 if scale is None else scale, _SERVING[dtype], _given(out, "out", rows, heads * d, dtype),
+                                              None if lse is None else _given(lse, "lse", rows, heads, torch.float32), _stream(stream))
+    if rc != OK:
+        raise PsaError(rc, "psa_prompt_attention")
     return out
 
 
@@ -437,11 +444,12 @@ def psa_pages_workspace_bytes(pages, count) -> int:
 
 
 def _cache(pool, tables, lens, kv_heads, page_size, d):
-    if not pool.is_cuda or pool.dtype != torch.uint8 or pool.dim() != 2 or not pool.is_contiguous() or tables.dim() != 2:
+    if not pool.is_cuda or pool.dtype is not torch.uint8 or pool.dim() != 2 or not pool.is_contiguous() or tables.dim() != 2:
         raise ValueError("pool must be a contiguous CUDA tensor [pages, page bytes] of uint8, tables [slots, width]")
-    if pool.shape[1] * 16 != kv_heads * page_size * 20 * d:
+    (pages, size), (slots, width) = pool.shape, tables.shape
+    if size * 16 != kv_heads * page_size * 20 * d:
         raise ValueError("pool pages must have psa_cache_page_bytes(%d, %d, %d) bytes" % (kv_heads, page_size, d))
-    return Cache(pool.data_ptr(), _ints(tables, "tables"), _ints(lens, "lens", tables.shape[0]), pool.shape[0], tables.shape[0], tables.shape[1], page_size, kv_heads, d)
+    return Cache(pool.data_ptr(), _ints(tables, "tables"), _ints(lens, "lens", slots), pages, slots, width, page_size, kv_heads, d)
 
 
 def psa_cache_append(K, V, pool, tables, lens, seqs, starts, page_size, k_held=None, v_held=None, stream=None):
@@ -451,14 +459,13 @@ def psa_cache_append(K, V, pool, tables, lens, seqs, starts, page_size, k_held=N
     dtype = K.dtype
     if V.shape != K.shape:
         raise ValueError("K and V must have one shape")
-    strides = _rows(K, "K", kv_heads, d), _rows(V, "V", kv_heads, d, dtype)
-    for t, nm in ((k_held, "k_held"), (v_held, "v_held")):
-        if t is not None and (not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.shape != K.shape):
-            raise ValueError("%s must be a contiguous CUDA tensor like K" % nm)
-    n = seqs.numel()
+    k_stride, v_stride, n = _rows(K, "K", kv_heads, d, dtype), _rows(V, "V", kv_heads, d, dtype), seqs.numel()
     cache = _cache(pool, tables, lens, kv_heads, page_size, d)
-    _raise(lib().psa_cache_append(cache, K.data_ptr(), V.data_ptr(), *strides, _ints(seqs, "seqs"), _ints(starts, "starts", n + 1), n, rows, _SERVING[dtype],
-                                  _ptr(k_held), _ptr(v_held), _stream(stream)), "psa_cache_append")
+    rc = (_lib or lib()).psa_cache_append(cache, K.data_ptr(), V.data_ptr(), k_stride, v_stride, _ints(seqs, "seqs"), _ints(starts, "starts", n + 1), n, rows, _SERVING[dtype],
+                                          None if k_held is None else _given(k_held, "k_held", rows, kv_heads * d, dtype),
+                                          None if v_held is None else _given(v_held, "v_held", rows, kv_heads * d, dtype), _stream(stream))
+    if rc != OK:
+        raise PsaError(rc, "psa_cache_append")
 
 
 def psa_cache_attention(Q, pool, tables, lens, seqs, q_starts, kv_heads, page_size, max_q=1, scale=None, out=None, lse=None, stream=None):
@@ -467,20 +474,24 @@ def psa_cache_attention(Q, pool, tables, lens, seqs, q_starts, kv_heads, page_si
     rows, heads, d = Q.shape
     if kv_heads <= 0 or heads % kv_heads:
         raise ValueError("kv_heads must divide Q's heads")
-    q_stride, n = _rows(Q, "Q", heads, d), seqs.numel()
+    dtype = Q.dtype
+    q_stride, n = _rows(Q, "Q", heads, d, dtype), seqs.numel()
     cache = _cache(pool, tables, lens, kv_heads, page_size, d)
-    out = _result(out, "out", (rows, heads * d), Q.dtype, Q.device)
-    _raise(lib().psa_cache_attention(cache, Q.data_ptr(), q_stride, _ints(seqs, "seqs"), _ints(q_starts, "q_starts", n + 1), n, rows, heads, max_q,
-                                     d ** -0.5 if scale is None else scale, _SERVING[Q.dtype], out.data_ptr(), _lse(lse, rows, heads), _stream(stream)),
-           "psa_cache_attention")
+    if out is None:
+        out = Q.new_empty((rows, heads * d))
+    rc = (_lib or lib()).psa_cache_attention(cache, Q.data_ptr(), q_stride, _ints(seqs, "seqs"), _ints(q_starts, "q_starts", n + 1), n, rows, heads, max_q,
+                                             d ** -0.5 if scale is None else scale, _SERVING[dtype], _given(out, "out", rows, heads * d, dtype),
+                                             None if lse is None else _given(lse, "lse", rows, heads, torch.float32), _stream(stream))
+    if rc != OK:
+        raise PsaError(rc, "psa_cache_attention")
     return out
 
 
 def _pages(tables, lens, refs, page_size):
     if tables.dim() != 2:
         raise ValueError("tables must be [slots, width]")
-    return Pages(_ints(tables, "tables"), None if lens is None else _ints(lens, "lens", tables.shape[0]), _ints(refs, "refs"), tables.shape[0], tables.shape[1],
-                 refs.numel(), page_size)
+    slots, width = tables.shape
+    return Pages(_ints(tables, "tables"), None if lens is None else _ints(lens, "lens", slots), _ints(refs, "refs"), slots, width, refs.numel(), page_size)
 
 
 def _pool(t, pages):

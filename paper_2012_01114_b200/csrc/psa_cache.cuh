@@ -27,10 +27,20 @@ struct CacheBlock {
     static constexpr int K_CODES = 0, K_SCALES = 8 * D, V_CODES = 10 * D, V_SCALES = 18 * D, BYTES = 20 * D;
 };
 
-// Four codes of a word as 1 + c / 16, a pair of them in a register.
-__device__ __forceinline__ uint32_t cache_ones(uint32_t w, int j) {
-    const uint32_t s = j == 0 ? w << 6 : j == 1 ? w << 2 : j == 2 ? w >> 2 : w >> 6;
-    return (s & 0x03C003C0u) | 0x3C003C00u;
-}
+// The numbers 1 + c / 16 of four pairs of codes in a word.  The two constants are kept in registers (opaque to the compiler, which would put them into
+// instructions of their own each time): a shift and one three-way operation a pair.
+struct CacheOnes {
+    uint32_t mask, one;
+    __device__ __forceinline__ CacheOnes() {
+        asm volatile("mov.b32 %0, 0x03C003C0;" : "=r"(mask));
+        asm volatile("mov.b32 %0, 0x3C003C00;" : "=r"(one));
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t w, int j) const {
+        const uint32_t s = j == 0 ? w << 6 : j == 1 ? w << 2 : j == 2 ? w >> 2 : w >> 6;
+        uint32_t r;
+        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(s), "r"(mask), "r"(one));      // (s & mask) | one
+        return r;
+    }
+};
 
 }  // namespace psa

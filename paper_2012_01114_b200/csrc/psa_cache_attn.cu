@@ -4,38 +4,47 @@
 //
 // Bound by memory, if the instructions between the loads and the products stay few: at the measured 6.45 TB/s an SM gets 23 bytes of cache a clock, 37
 // codes.  The heads of a group are the columns of one product, so that a code is looked at once for all of them:
-//   phase 1  S^T = K Q^T     mma.m16n8k16, 16 tokens x 8 columns (heads of the group x query tokens).  The operand holds 1 + c / 16 exactly; S and M of a
-//                            token enter behind the product, in fp32 (S_w (K Q)_w + M_w sum_w q, w a group of 32 channels): the scores have no rounding
-//                            but that of Q to fp16, which a power of two per row keeps in range.
-//   phase 2  running maximum and sum per column, 16 tokens at a time; the maximum is raised (and sums and output rescaled) only when a score passes it by 2^8
+//   phase 1  S^T = K Q^T     mma.m16n8k16, 16 tokens x 8 columns (heads of the group x query tokens).  The operand holds the codes themselves: four bits at the low
+//                            end of a half are the subnormal fp16 number c 2^-24, one place further up c 2^-20, so that a mask is all that it takes; the
+//                            queries carry the powers of two that belong to that.  S and M enter in fp32 behind the products of a group of 32 channels,
+//                            S_w sum c q / 16, and by one more product, sum_w (M_w + S_w) (sum_w q) with the sums in two fp16 numbers each.  No rounding but
+//                            that of Q to fp16, which a power of two per row keeps in range.
+//   phase 2  running maximum and sum per column, 32 tokens at a time; the maximum is raised (and sums and output rescaled) only when a score passes it by 2^8
 //   phase 3  O^T += V^T P^T  one fp16 fma per pair of codes gives v (rounded to fp16), the weights change sides by a transposing move
-// Work is split over the long axis: all (sequence, head, tile of columns) rows of all their 16-token steps form one list, of which every CTA takes an
-// equal piece whatever the lengths are (the kernel finds its piece from the lengths; nothing has to be known on the host).  The warps of a CTA take the
-// steps of a row in turn, each with a ring of blocks of its own filled by bulk copies, and are joined through shared memory; a row that several CTAs share is
-// joined by the one that finishes last, in the order of the list, so that results do not depend on who that is.
+// Work is split over the long axis: a row (sequence, head, tile of columns) of more 32-token steps than a piece is cut into parts of equal length, the piece being chosen on the
+// device from all lengths so that the parts fill the GPU (nothing has to be known on the host).  A CTA takes a part: its warps take the steps in turn, each with a
+// ring of blocks of its own filled by bulk copies, and are joined through shared memory; a row of several parts is joined by the CTA that finishes last, in
+// the parts' order, so that results do not depend on who that is.
+#include <type_traits>
+
 #include "psa_cache.cuh"
 #include "psa_internal.h"
+#include "psa_sched.h"
 #include "sm100.cuh"
 
 namespace psa {
 
 namespace {
 
-constexpr int WARPS = 4;
+constexpr int WARPS = 8;                        // of a CTA.  (Four, twice as many CTAs: one sequence of 131,072 tokens, 8 heads of 128 47.8 -> 53.2 us, 64 of 1 to 8000 37.5 -> 43.0)
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float RAISE = 8.f;                    // log2 units, see phase 2
-constexpr int MAX_CTAS = 148 * 4 + 64;          // partial results and arrival counts are kept per CTA
-constexpr int LEAST_STEPS = 2 * WARPS;          // a CTA's piece is not shorter than this
+constexpr int STEP_BLOCKS = 2, STEP = STEP_BLOCKS * CACHE_BLOCK;              // blocks and tokens of a step
+constexpr int MAX_CTAS = 148 * 4 + 64;          // partial results and arrival counts: two per CTA
+constexpr int SEQ_BITS = 9, SEQS = 1 << SEQ_BITS;                            // sequences of one launch
+constexpr int LEAST_PIECE = 16;                 // steps: a row is not cut into less (joining parts costs about as much)
 
 template <int D, int NT>
 struct ACfg {
-    static constexpr int COLS = 8 * NT;
-    static constexpr int CTAS = D * NT <= 128 ? 4 : 2;
-    static constexpr int STAGES = D >= 256 ? 4 : D == 128 ? 5 : D == 96 ? 6 : 8;
-    static constexpr int RING = WARPS * STAGES * CacheBlock<D>::BYTES;
+    static constexpr int COLS = 8 * NT, THREADS = 32 * WARPS;
+    static constexpr int CTAS = (D * NT <= 128 ? 16 : 8) / WARPS;            // per SM: 128 registers a thread, or 255
+    static constexpr int STAGES = D >= 256 || (D == 128 && NT == 1) ? 2 : D == 96 ? 3 : 4;       // steps that a warp has in flight or in hand
+    static constexpr int STAGE_BYTES = STEP_BLOCKS * CacheBlock<D>::BYTES;
+    static constexpr int RING = WARPS * STAGES * STAGE_BYTES;
     static constexpr int OPITCH = D + 4;        // floats between columns of the joining buffer (keeps its 16-byte stores off each other's banks)
     static constexpr int JOIN = WARPS * COLS * OPITCH * 4;
     static constexpr int SMEM = RING > JOIN ? RING : JOIN;
+    static constexpr int MOST_PARTS = (SMEM - THREADS * 16) / (8 * COLS);    // of a row: two numbers a column each, and a result a thread
 };
 
 struct AttnArgs {
@@ -43,15 +52,23 @@ struct AttnArgs {
     const int *tables, *lens, *seqs, *q_starts;
     const uint16_t* q;
     uint16_t* out;
-    float *lse, *part;                          // part: 2 per CTA, [COLS][D] outputs, then [COLS] maxima and [COLS] sums
+    float *lse, *part;                          // part: per part of a row [COLS][D] outputs, then [COLS] maxima and [COLS] sums
     long long q_stride;
     int pages, slots, width, page_size, kv_heads, group, sequences, rows, f16;
     float scale;
+    FastDiv by_group, by_blocks;                // by query heads of a group, by blocks of a page
 };
 
-// Arrivals on a row that several CTAs share, at the index of the first of them.  Every arrival that completes a row wraps its count to zero again, and a CTA
+// Arrivals on a row of several parts, at the number of its first part.  Every arrival that completes a row wraps its count to zero again, and a CTA
 // that gave up a wait arrives all the same: the counts are zero between calls.
-__device__ unsigned g_arrived[MAX_CTAS];
+__device__ unsigned g_arrived[2 * MAX_CTAS];
+
+// Counts an arrival behind everything that the CTA's threads stored before the barrier ahead of it; true for the one that completes the row.
+__device__ __forceinline__ bool arrive(unsigned* count, unsigned last) {
+    unsigned old;
+    asm volatile("fence.acq_rel.gpu;\n\tatom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(old) : "l"(count), "r"(last) : "memory");
+    return old == last;
+}
 
 template <int N>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&r)[N]) {
@@ -73,12 +90,16 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&r)[N]) {
     }
 }
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 __device__ __forceinline__ float ex2(float x) {
@@ -90,10 +111,9 @@ __device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cas
 __device__ __forceinline__ __half2 bits_h2(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
 
-// One sequence of the call: tokens held, query rows, and the steps of the work list that it has.
+// One sequence of the call: tokens held, query rows, tiles of columns, steps.
 struct Seq {
-    int slot, len, q0, nq, qtiles, steps;
-    long long units;
+    int slot, len, q0, nq, qtiles, steps, bad;   // bad: no such slot, or longer than its table
 };
 template <int COLS>
 __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
@@ -102,150 +122,243 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
     const bool there = s.slot >= 0 && s.slot < a.slots;
     s.q0 = min(max(a.q_starts[b], 0), a.rows);
     s.nq = max(min(max(a.q_starts[b + 1], 0), a.rows) - s.q0, 0);
-    s.len = there ? (int)min((long long)max(a.lens[s.slot], 0), (long long)a.width * a.page_size) : 0;
+    const int held = there ? max(a.lens[s.slot], 0) : 0;
+    s.len = min(held, a.width * a.page_size);
+    s.bad = !there || held != s.len;
     s.qtiles = (int)(((long long)s.nq * a.group + COLS - 1) / COLS);
-    s.steps = max((s.len + CACHE_BLOCK - 1) / CACHE_BLOCK, 1);
-    s.units = (long long)s.steps * s.qtiles * a.kv_heads;
+    s.steps = max((s.len + STEP - 1) / STEP, 1);
     return s;
 }
 
+// A part of a row: steps [step0, step1) of it, part `part` of `parts`, whose results have numbers `first`, `first` + 1, .. (if there are several).
+struct Piece {
+    Seq s;
+    int there, h, qt, step0, step1, part, parts, first;
+};
+struct Totals {
+    uint32_t steps, rows;
+};
+// Item `r` of a sequence whose rows are cut into pieces of at most `piece` steps.
+__device__ __forceinline__ Piece piece_of(const Seq& s, int r, int piece, int first) {
+    const int parts = (s.steps + piece - 1) / piece, row = parts == 1 ? r : r / parts, each = parts == 1 ? s.steps : (s.steps + parts - 1) / parts;
+    Piece p;
+    p.s = s;
+    p.there = 1;
+    p.h = s.qtiles == 1 ? row : row / s.qtiles;
+    p.qt = row - p.h * s.qtiles;
+    p.part = r - row * parts;
+    p.parts = parts;
+    p.step0 = p.part * each;
+    p.step1 = min(p.step0 + each, s.steps);
+    p.first = first + row * parts;
+    return p;
+}
+
 template <int D, int NT>
-__global__ void __launch_bounds__(32 * WARPS, ACfg<D, NT>::CTAS)
+__global__ void __launch_bounds__(ACfg<D, NT>::THREADS, ACfg<D, NT>::CTAS)
 cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next) {
     using Cfg = ACfg<D, NT>;
     using B = CacheBlock<D>;
-    constexpr int G = B::G, COLS = Cfg::COLS, ST = Cfg::STAGES;
+    constexpr int G = B::G, GQ = (G + 3) / 4, COLS = Cfg::COLS, ST = Cfg::STAGES, THREADS = Cfg::THREADS;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint64_t full[WARPS][ST];
     __shared__ float m_s[WARPS][COLS], l_s[WARPS][COLS], top_s[COLS], sum_s[COLS];
-    __shared__ long long scan_s[WARPS];
-    __shared__ int abort_flag, last_s, found_b;
-    __shared__ long long found_first;
+    __shared__ unsigned long long scan_s[WARPS];
+    __shared__ Totals total_s[WARPS];
+    __shared__ __align__(16) uint32_t unsorted_s[SEQS];                      // steps of a sequence's items << SEQ_BITS | SEQS - 1 - sequence
+    __shared__ uint16_t order_s[SEQS];                                       // where items are handed out: the sequences, longest items first
+    __shared__ int abort_flag, last_s;
+    __shared__ int base_s[SEQS + 1], split_s[SEQS];                          // items ahead of a sequence, and parts that are joined with others
+    __shared__ Piece pieces[2];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     if (tid == 0) {
         abort_flag = 0;
         for (int w = 0; w < WARPS; ++w)
-            for (int s = 0; s < ST; ++s) mbar_init(&full[w][s], 1);
+            for (int s = 0; s < ST; ++s) mbar_init(&full[w][s], STEP_BLOCKS);
         fence_mbar_init();
     }
     volatile int* abortp = &abort_flag;
     grid_dependency_wait();
     if (tid == 0 && blockIdx.x == 0 && dc_next) *dc_next = DeviceCounters{0, 0, 0, 0, 0, 0, 0};
 
-    // ---- this CTA's piece of the list: units [begin, end) of all, and the sequence that `begin` lies in
-    long long mine0 = 0;                        // (units of sequence tid: the only chunk, up to 128 sequences)
-    auto block_scan = [&](long long v, long long* total) -> long long {      // exclusive
-        long long x = v;
+    // ---- the list: how long a piece is, and the items ahead of every sequence
+    auto block_scan = [&](unsigned long long v, unsigned long long* total) {                 // exclusive; two 32-bit sums at a time
+        unsigned long long x = v;
 #pragma unroll
         for (int s = 1; s < 32; s *= 2) {
-            const long long y = __shfl_up_sync(0xffffffffu, x, s);
+            const unsigned long long y = __shfl_up_sync(0xffffffffu, x, s);
             if (lane >= s) x += y;
         }
         __syncthreads();
         if (lane == 31) scan_s[warp] = x;
         __syncthreads();
-        long long before = 0, all = 0;
+        unsigned long long before = 0, all = 0;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) { if (w < warp) before += scan_s[w]; all += scan_s[w]; }
         *total = all;
         return before + x - v;
     };
-    long long W = 0;
-    for (int b0 = 0; b0 < a.sequences; b0 += 32 * WARPS) {
-        long long all;
-        const long long v = b0 + tid < a.sequences ? sequence<COLS>(a, b0 + tid).units : 0;
-        block_scan(v, &all);
-        if (b0 == 0) mine0 = v;
-        W += all;
+    Seq s0 = {};                                 // sequence tid
+    uint32_t steps = 0, rows = 0;
+    bool descends = false;
+    for (int b = tid; b < a.sequences; b += THREADS) {
+        const Seq x = sequence<COLS>(a, b);
+        descends |= a.q_starts[b + 1] < a.q_starts[b];
+        if (b == tid) s0 = x;
+        const uint32_t r = (uint32_t)x.qtiles * a.kv_heads;
+        steps += r * x.steps;
+        rows += r;
     }
-    const long long ctas = min((long long)gridDim.x, max(W / LEAST_STEPS, 1LL));
-    if (W == 0 || blockIdx.x >= ctas) return;
-    const long long begin = W * blockIdx.x / ctas, end = W * (blockIdx.x + 1) / ctas;
-    {
-        long long done = 0;
-        for (int b0 = 0; b0 < a.sequences && done <= begin; b0 += 32 * WARPS) {
-            long long all;
-            const long long v = b0 == 0 ? mine0 : b0 + tid < a.sequences ? sequence<COLS>(a, b0 + tid).units : 0;
-            const long long first = done + block_scan(v, &all);
-            if (v > 0 && first <= begin && begin < first + v) { found_b = b0 + tid; found_first = first; }
-            done += all;
+    steps = __reduce_add_sync(0xffffffffu, steps);
+    rows = __reduce_add_sync(0xffffffffu, rows);
+    if (lane == 0) total_s[warp] = Totals{steps, rows};
+    if (__syncthreads_or(descends)) {            // rows counted more than once: the numbers below would not hold; nothing is computed, and the call reports it
+        if (tid == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
+        return;
+    }
+    steps = rows = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) { steps += total_s[w].steps; rows += total_s[w].rows; }
+    // Rows cut into pieces of steps / (CTAs - rows) make no more parts than there are CTAs; where rows alone are that many, long ones are still cut.
+    const uint32_t ctas = min(gridDim.x, (uint32_t)Cfg::MOST_PARTS), budget = max((int)ctas - (int)min(rows, ctas), (int)(ctas + 1) / 2);
+    const int piece = max((steps + budget - 1) / budget, (uint32_t)LEAST_PIECE);
+    // With more rows than CTAs, items are handed out one by one, the longest first.
+    const bool sorted = rows > gridDim.x;
+    if (sorted) {
+        for (int b = tid; b < (a.sequences + 3) / 4 * 4; b += THREADS) {
+            uint32_t each = 0;
+            if (b < a.sequences) {
+                const Seq x = b == tid ? s0 : sequence<COLS>(a, b);
+                const int parts = (x.steps + piece - 1) / piece;
+                each = min((uint32_t)(x.steps + parts - 1) / parts, (1u << (32 - SEQ_BITS)) - 2) + 1;
+            }
+            unsorted_s[b] = each << SEQ_BITS | (uint32_t)(SEQS - 1 - b);     // (no two alike)
+        }
+        __syncthreads();
+        for (int b = tid; b < a.sequences; b += THREADS) {                   // as many places down as there are larger ones
+            const uint32_t x = unsorted_s[b];
+            int rank = 0;
+            for (int k = 0; k < a.sequences; k += 4) {
+                const uint4 y = *reinterpret_cast<const uint4*>(unsorted_s + k);
+                rank += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
+            }
+            order_s[rank] = (uint16_t)b;
         }
         __syncthreads();
     }
-    int b = found_b;
-    long long seq_first = found_first;          // unit index of the sequence's first step
-    Seq s = sequence<COLS>(a, b);
-    auto cta_of = [&](long long u) { return (int)(((u + 1) * ctas - 1) / W); };
+    auto nth = [&](int k) { return sorted ? (int)order_s[k] : k; };        // the k-th sequence of the list
+    uint32_t items = 0, splits = 0;
+    for (int k0 = 0; k0 < a.sequences; k0 += THREADS) {
+        unsigned long long all;
+        const int k = k0 + tid;
+        Seq x = s0;
+        if ((k0 > 0 || sorted) && k < a.sequences) x = sequence<COLS>(a, nth(k));
+        const uint32_t parts = (x.steps + piece - 1) / piece, n = k < a.sequences ? (uint32_t)x.qtiles * a.kv_heads * parts : 0u;
+        const unsigned long long before = block_scan((unsigned long long)n << 32 | (parts > 1 ? n : 0u), &all);
+        if (k < a.sequences) { base_s[k] = (int)(items + (uint32_t)(before >> 32)); split_s[k] = (int)(splits + (uint32_t)before); }
+        const int r = (int)blockIdx.x - (int)(items + (uint32_t)(before >> 32));
+        if (r >= 0 && r < (int)n) pieces[0] = piece_of(x, r, piece, (int)(splits + (uint32_t)before));         // this CTA's first item
+        items += (uint32_t)(all >> 32);
+        splits += (uint32_t)all;
+    }
+    if (tid == 0) {
+        base_s[a.sequences] = (int)items;
+        pieces[1].there = 0;
+    }
+    if (blockIdx.x >= items) return;
+    const bool more = items > gridDim.x;
+    // Decodes item `i` (by one warp).
+    auto decode = [&](int i, Piece* to) {
+        for (int k = lane; k < a.sequences; k += 32)
+            if (base_s[k] <= i && i < base_s[k + 1]) *to = piece_of(sequence<COLS>(a, nth(k)), i - base_s[k], piece, split_s[k]);
+    };
 
-    uint8_t* const ring = smem + warp * ST * B::BYTES;
+    uint8_t* const ring = smem + warp * ST * Cfg::STAGE_BYTES;
     float* const join = reinterpret_cast<float*>(smem);
-    uint32_t loaded = 0;                        // blocks this warp has asked for so far (position in the ring)
-    uint32_t used = 0;                          // blocks it has worked off
+    int load_slot = 0, use_slot = 0;            // places of the ring: next to be filled, next to be worked off
+    uint32_t use_phase = 0, in_flight = 0;
     bool ok = true;
-    const int blocks = a.page_size / CACHE_BLOCK;
 
-    for (long long u = begin; u < end;) {
-        while (u >= seq_first + s.units) { seq_first += s.units; s = sequence<COLS>(a, ++b); }
-        const int row = (int)((u - seq_first) / s.steps), step0 = (int)((u - seq_first) - (long long)row * s.steps);
-        const int h = row / s.qtiles, qt = row - h * s.qtiles;
-        const int step1 = (int)min((long long)s.steps, step0 + (end - u));
-        const long long row_first = u - step0;
-        const bool whole = step0 == 0 && step1 == s.steps;
-        if (tid == 0 && (s.slot < 0 || s.slot >= a.slots || a.lens[s.slot] != s.len)) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
+    for (int turn = 0;; turn ^= 1) {
+        __syncthreads();                         // (the piece is there; the one before it is done with)
+        Piece& pc = pieces[turn];
+        if (!pc.there) break;
+        const int step0 = pc.step0, qt = pc.qt, h = pc.h, len = pc.s.len, nq = pc.s.nq, q0 = pc.s.q0;
+        const bool whole = pc.parts == 1;
 
-        // ---- blocks: lane l looks up the block of the warp's step first + l, 32 at a time
-        const int nsteps = (step1 - step0 - warp + WARPS - 1) / WARPS;       // steps of this warp: step0 + warp + WARPS i
+        // ---- the row's queries, column n = g of tile nt, channels 32 w + 8 t .. + 7: asked for ahead of all that has to be looked up first
+        uint4 raw[NT][G];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int rho = qt * COLS + nt * 8 + g, token = (int)fastdiv((uint32_t)rho, a.by_group);
+#pragma unroll
+            for (int w = 0; w < G; ++w) {
+                raw[nt][w] = make_uint4(0, 0, 0, 0);
+                if (token < nq)
+                    raw[nt][w] = *reinterpret_cast<const uint4*>(a.q + (size_t)(q0 + token) * a.q_stride + ((size_t)h * a.group + (rho - token * a.group)) * D + 32 * w + 8 * t);
+            }
+        }
+        // ---- blocks: lane l looks up, and asks for, block l % 2 of steps l / 2, l / 2 + 16, .. of the warp's (step0 + warp + WARPS i)
+        const int nsteps = (pc.step1 - step0 - warp + WARPS - 1) / WARPS;
         const uint8_t* addr = nullptr;
-        int looked = 0;
+        uint32_t there[2] = {0, 0};             // blocks that exist (not those behind the end, nor in a page that does not exist), of these and the 16 steps before
         auto look_up = [&](int i0) {
-            const int step = step0 + warp + WARPS * (i0 + lane);
+            const int i = i0 + (lane >> 1), block = (step0 + warp + WARPS * i) * STEP_BLOCKS + (lane & 1);
             addr = nullptr;
-            if (i0 + lane < nsteps && step * CACHE_BLOCK < s.len) {
-                const int col = step / blocks;
-                const int page = a.tables[(size_t)s.slot * a.width + col];
-                if (page >= 0 && page < a.pages) addr = a.pool + (((size_t)page * a.kv_heads + h) * blocks + (step - col * blocks)) * B::BYTES;
+            if (i < nsteps && block * CACHE_BLOCK < len) {
+                const int blocks = (int)a.by_blocks.d, col = (int)fastdiv((uint32_t)block, a.by_blocks);
+                const int page = a.tables[(size_t)pc.s.slot * a.width + col];
+                if (page >= 0 && page < a.pages) addr = a.pool + (((size_t)page * a.kv_heads + h) * blocks + (block - col * blocks)) * B::BYTES;
                 else atomicExch(&dc->status, (int)PSA_ERR_SHAPE);            // (no such page: its tokens are left out, and the call reports it)
             }
+            there[1] = there[0];
+            there[0] = __ballot_sync(0xffffffffu, addr != nullptr);
         };
-        // Step i of the warp into the ring; a step without a block (an empty sequence, a page that does not exist) takes no place in it.
-        uint32_t missing = 0;                   // bit i % 32: step i has no block
+        // Step i into the ring.
         auto load = [&](int i) {
             if (i >= nsteps) return;
-            if ((i & 31) == 0) look_up(i);
-            const unsigned long long p = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(addr), i & 31);
-            const uint32_t bit = 1u << (i & 31);
-            missing = p ? missing & ~bit : missing | bit;
-            if (!p) return;
-            if (lane == 0) {
-                uint64_t* bar = &full[warp][loaded % ST];
-                mbar_arrive_expect_tx(bar, B::BYTES);
-                bulk_load_1d(ring + (loaded % ST) * B::BYTES, reinterpret_cast<const void*>(p), B::BYTES, bar);
+            if ((i & 15) == 0) look_up(i);
+            if ((lane >> 1) == (i & 15)) {
+                uint64_t* bar = &full[warp][load_slot];
+                if (addr) {
+                    mbar_arrive_expect_tx(bar, B::BYTES);
+                    bulk_load_1d(ring + load_slot * Cfg::STAGE_BYTES + (lane & 1) * B::BYTES, addr, B::BYTES, bar);
+                } else {
+                    mbar_arrive(bar);
+                }
             }
-            ++loaded;
+            load_slot = load_slot + 1 == ST ? 0 : load_slot + 1;
+            ++in_flight;
         };
         if (ok)
-            for (; looked < ST - 1; ++looked) load(looked);
+            for (int i = 0; i < ST - 1; ++i) load(i);
+        if (warp == 0) {                         // while the first blocks are on their way: the next item
+            if (more) {
+                int i = 0;
+                if (lane == 0) i = (int)gridDim.x + (int)atomicAdd(&dc->next_item, 1u);
+                i = __shfl_sync(0xffffffffu, i, 0);
+                if (lane == 0) pieces[turn ^ 1].there = 0;
+                __syncwarp();
+                if (i < base_s[a.sequences]) decode(i, &pieces[turn ^ 1]);
+            } else if (lane == 0) {
+                pieces[turn ^ 1].there = 0;
+            }
+            if (lane == 0 && pc.s.bad) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
+        }
 
-        // ---- the row's queries as the second operand: column n = g of tile nt, channels 32 w + 8 t .. + 7
+        // ---- the queries as the second operand
         uint32_t qb[NT][G][4];
-        float cs[NT][2], qsum[NT][G][2];        // of columns 2t, 2t + 1: score factor (log2 units) and sums over the groups
+        uint32_t qaff[NT][GQ][2];               // sums of the queries over groups t, t + 4, ..: leading and trailing part, each twice
+        float cs[NT][2];                        // of columns 2t, 2t + 1: score factor (log2 units)
         int limit[NT][2];                       // the last token that the column sees
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int rho = qt * COLS + nt * 8 + g, token = rho / a.group;
-            uint4 raw[G];
             float top = 0.f;
-#pragma unroll
-            for (int w = 0; w < G; ++w) {
-                raw[w] = make_uint4(0, 0, 0, 0);
-                if (token < s.nq)
-                    raw[w] = *reinterpret_cast<const uint4*>(a.q + (size_t)(s.q0 + token) * a.q_stride + ((size_t)h * a.group + (rho - token * a.group)) * D + 32 * w + 8 * t);
-            }
             float f[G][8];
 #pragma unroll
             for (int w = 0; w < G; ++w) {
-                const uint32_t x[4] = {raw[w].x, raw[w].y, raw[w].z, raw[w].w};
+                const uint32_t x[4] = {raw[nt][w].x, raw[nt][w].y, raw[nt][w].z, raw[nt][w].w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     if (a.f16) {
@@ -259,7 +372,8 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
             }
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            // 2^e <= top < 2^(e+1): the row goes in as q 2^-e, exact but for what lies 2^14 below its largest number
+            // 2^e <= top < 2^(e+1): the row goes in as q 2^(13 - e) beside codes at a half's low end and as q 2^(9 - e) beside those one place up, exact but for
+            // what lies 2^23 below its largest number.  A product of a code c is then c q 2^(-11 - e): 2^(7 + e) short of (c / 16) q, which the factor has.
             const uint32_t e = min(max(__float_as_uint(top) >> 23, 1u), 253u);
             const float down = __uint_as_float((254u - e) << 23), up = __uint_as_float(e << 23);
             float part[G];
@@ -268,173 +382,206 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                 part[w] = 0.f;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const __half2 v = __floats2half2_rn(f[w][2 * k] * down, f[w][2 * k + 1] * down);
+                    const float place = k & 1 ? 512.f : 8192.f;
+                    const __half2 v = __floats2half2_rn(f[w][2 * k] * down * place, f[w][2 * k + 1] * down * place);
                     qb[nt][w][k] = h2_bits(v);
                     const float2 r = __half22float2(v);
-                    part[w] += r.x + r.y;
+                    part[w] = fmaf(r.x + r.y, 1.f / (128.f * place), part[w]);
                 }
                 part[w] += __shfl_xor_sync(0xffffffffu, part[w], 1);
                 part[w] += __shfl_xor_sync(0xffffffffu, part[w], 2);
             }
+#pragma unroll
+            for (int x = 0; x < GQ; ++x) {
+                float mine = 0.f;
+#pragma unroll
+                for (int w = 4 * x; w < 4 * x + 4 && w < G; ++w)
+                    if (t == w - 4 * x) mine = part[w];
+                const __half hi = __float2half_rn(mine), lo = __float2half_rn(mine - __half2float(hi));
+                qaff[nt][x][0] = h2_bits(__half2half2(hi));
+                qaff[nt][x][1] = h2_bits(__half2half2(lo));
+            }
             // from the lanes that hold column g to those that own it behind the product
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int from = (2 * t + c) * 4;
-                cs[nt][c] = __shfl_sync(0xffffffffu, up, from) * (a.scale * LOG2E);
-#pragma unroll
-                for (int w = 0; w < G; ++w) qsum[nt][w][c] = __shfl_sync(0xffffffffu, part[w], from);
-                limit[nt][c] = s.len - s.nq + min((qt * COLS + nt * 8 + 2 * t + c) / a.group, s.nq - 1);
+                const int owner = (2 * t + c) * 4;
+                cs[nt][c] = fmaxf(__shfl_sync(0xffffffffu, up, owner) * (a.scale * LOG2E * 128.f), 1.2e-38f);
+                limit[nt][c] = len - nq + min((int)fastdiv(qt * COLS + nt * 8 + 2 * t + c, a.by_group), nq - 1);
             }
         }
-        const int seen_by_all = s.len - s.nq + qt * COLS / a.group;          // the last token that every column sees
+        const int seen_by_all = len - nq + (int)fastdiv(qt * COLS, a.by_group);          // the last token that every column sees
 
-        float o[NT][2 * G][4], m[NT][2], l[NT][2];
+        const CacheOnes cache_ones;
+        // m: running maximum of the scores before their factor; limit_up: where it is raised; shift: -m in log2 units
+        float o[NT][2 * G][4], m[NT][2], limit_up[NT][2], shift[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int i = 0; i < 2 * G; ++i)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[nt][i][c] = 0.f;
-            m[nt][0] = m[nt][1] = -INFINITY;
+            m[nt][0] = m[nt][1] = limit_up[nt][0] = limit_up[nt][1] = -INFINITY;
+            shift[nt][0] = shift[nt][1] = 0.f;
             l[nt][0] = l[nt][1] = 0.f;
         }
 
         for (int i = 0; i < nsteps && ok; ++i) {
-            const bool skip = (missing >> (i & 31)) & 1u;
-            load(looked++);                      // (into the place that step i - 1 has left)
-            if (skip) continue;
-            ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][used % ST], (used / ST) & 1, abortp));
+            load(i + ST - 1);                    // (into the place that step i - 1 has left)
+            ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][use_slot], use_phase, abortp));
             if (!ok) break;
-            const uint8_t* blk = ring + (used % ST) * B::BYTES;
-            ++used;
-            const int tok0 = (step0 + warp + WARPS * i) * CACHE_BLOCK;
-            const bool masked = tok0 + CACHE_BLOCK - 1 > seen_by_all;
+            const uint8_t* const stage = ring + use_slot * Cfg::STAGE_BYTES;
+            --in_flight;
+            if (++use_slot == ST) { use_slot = 0; use_phase ^= 1; }
+            const int tok0 = (step0 + warp + WARPS * i) * STEP;
+            // (step i is one of the 16 looked up last, or of those before)
+            const uint32_t have = ((i >> 4) == (min(i + ST - 1, nsteps - 1) >> 4) ? there[0] : there[1]) >> (2 * (i & 15)) & 3u;
+            const bool masked = tok0 + STEP - 1 > seen_by_all || have != 3u;
             // ---- phase 1
-            float sc[NT][4];
+            float sc[STEP_BLOCKS][NT][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
-            {
+            for (int s = 0; s < STEP_BLOCKS; ++s) {
+                const uint8_t* const blk = stage + s * B::BYTES;
                 uint32_t ka[G], kb[G], sa[G], sb[G];
                 load_words<G>(blk + B::K_CODES + g * (D / 2) + t * G * 4, ka);
                 load_words<G>(blk + B::K_CODES + (g + 8) * (D / 2) + t * G * 4, kb);
                 load_words<G>(blk + B::K_SCALES + g * G * 4, sa);
                 load_words<G>(blk + B::K_SCALES + (g + 8) * G * 4, sb);
 #pragma unroll
+                for (int x = 0; x < GQ; ++x) {   // (lanes beyond the last group repeat one, against sums of zero)
+                    const int w = 4 * x + t < G ? 4 * x + t : 0;
+                    const uint32_t fa = *reinterpret_cast<const uint32_t*>(blk + B::K_SCALES + (g * G + w) * 4), fb = *reinterpret_cast<const uint32_t*>(blk + B::K_SCALES + ((g + 8) * G + w) * 4);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        if (x == 0) mma16816_first(sc[s][nt], fa, fb, fa, fb, qaff[nt][0][0], qaff[nt][0][1]);
+                        else mma16816(sc[s][nt], fa, fb, fa, fb, qaff[nt][x][0], qaff[nt][x][1]);
+                }
+#pragma unroll
                 for (int w = 0; w < G; ++w) {
-                    const float2 fa = __half22float2(bits_h2(sa[w])), fb = __half22float2(bits_h2(sb[w]));
+                    const float fa = __low2float(bits_h2(sa[w])), fb = __low2float(bits_h2(sb[w]));
+                    const uint32_t ha = ka[w] >> 8, hb = kb[w] >> 8;
                     float d[NT][4];
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) d[nt][0] = d[nt][1] = d[nt][2] = d[nt][3] = 0.f;
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const uint32_t a0 = cache_ones(ka[w], 2 * k), a1 = cache_ones(kb[w], 2 * k), a2 = cache_ones(ka[w], 2 * k + 1), a3 = cache_ones(kb[w], 2 * k + 1);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16816(d[nt], a0, a1, a2, a3, qb[nt][w][2 * k], qb[nt][w][2 * k + 1]);
-                    }
-#pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        sc[nt][0] = fmaf(fa.x, d[nt][0], fmaf(fa.y, qsum[nt][w][0], sc[nt][0]));
-                        sc[nt][1] = fmaf(fa.x, d[nt][1], fmaf(fa.y, qsum[nt][w][1], sc[nt][1]));
-                        sc[nt][2] = fmaf(fb.x, d[nt][2], fmaf(fb.y, qsum[nt][w][0], sc[nt][2]));
-                        sc[nt][3] = fmaf(fb.x, d[nt][3], fmaf(fb.y, qsum[nt][w][1], sc[nt][3]));
+                        mma16816_first(d[nt], ka[w] & 0x000F000Fu, kb[w] & 0x000F000Fu, ka[w] & 0x00F000F0u, kb[w] & 0x00F000F0u, qb[nt][w][0], qb[nt][w][1]);
+                        mma16816(d[nt], ha & 0x000F000Fu, hb & 0x000F000Fu, ha & 0x00F000F0u, hb & 0x00F000F0u, qb[nt][w][2], qb[nt][w][3]);
+                        sc[s][nt][0] = fmaf(fa, d[nt][0], sc[s][nt][0]);
+                        sc[s][nt][1] = fmaf(fa, d[nt][1], sc[s][nt][1]);
+                        sc[s][nt][2] = fmaf(fb, d[nt][2], sc[s][nt][2]);
+                        sc[s][nt][3] = fmaf(fb, d[nt][3], sc[s][nt][3]);
                     }
                 }
             }
             // ---- phase 2
-            uint32_t pb[NT][2];
+            if (masked) {
+#pragma unroll
+                for (int s = 0; s < STEP_BLOCKS; ++s)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (tok0 + s * CACHE_BLOCK + g + 8 * (c >> 1) > limit[nt][c & 1] || !(have >> s & 1u)) sc[s][nt][c] = -INFINITY;
+            }
             bool raise = false;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) sc[nt][c] *= cs[nt][c & 1];
-                if (masked) {
+                for (int c = 0; c < 2; ++c) {
+                    float x = fmaxf(sc[0][nt][c], sc[0][nt][c + 2]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (tok0 + g + 8 * (c >> 1) > limit[nt][c & 1]) sc[nt][c] = -INFINITY;
+                    for (int s = 1; s < STEP_BLOCKS; ++s) x = fmaxf(x, fmaxf(sc[s][nt][c], sc[s][nt][c + 2]));
+                    raise |= x > limit_up[nt][c];
                 }
-                raise |= fmaxf(sc[nt][0], sc[nt][2]) > m[nt][0] + RAISE || fmaxf(sc[nt][1], sc[nt][3]) > m[nt][1] + RAISE;
-            }
             if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float x = fmaxf(sc[nt][c], sc[nt][c + 2]);
+                        float x = fmaxf(sc[0][nt][c], sc[0][nt][c + 2]);
+#pragma unroll
+                        for (int s = 1; s < STEP_BLOCKS; ++s) x = fmaxf(x, fmaxf(sc[s][nt][c], sc[s][nt][c + 2]));
                         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                        const float top = fmaxf(m[nt][c], x), f = ex2(m[nt][c] - finite_or_zero(top));
+                        const float top = fmaxf(m[nt][c], x), f = ex2((m[nt][c] - finite_or_zero(top)) * cs[nt][c]);
                         m[nt][c] = top;
+                        limit_up[nt][c] = top + RAISE / cs[nt][c];
+                        shift[nt][c] = -finite_or_zero(top) * cs[nt][c];
                         l[nt][c] *= f;
 #pragma unroll
                         for (int k = 0; k < 2 * G; ++k) { o[nt][k][c] *= f; o[nt][k][c + 2] *= f; }
                     }
             }
+            uint32_t pb[STEP_BLOCKS][NT][2];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const float m0 = finite_or_zero(m[nt][0]), m1 = finite_or_zero(m[nt][1]);
-                const float p0 = ex2(sc[nt][0] - m0), p1 = ex2(sc[nt][1] - m1), p2 = ex2(sc[nt][2] - m0), p3 = ex2(sc[nt][3] - m1);
-                l[nt][0] += p0 + p2;
-                l[nt][1] += p1 + p3;
-                pb[nt][0] = transpose8x8(h2_bits(__floats2half2_rn(p0, p1)));
-                pb[nt][1] = transpose8x8(h2_bits(__floats2half2_rn(p2, p3)));
-            }
+            for (int s = 0; s < STEP_BLOCKS; ++s)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float p0 = ex2(fmaf(sc[s][nt][0], cs[nt][0], shift[nt][0])), p1 = ex2(fmaf(sc[s][nt][1], cs[nt][1], shift[nt][1]));
+                    const float p2 = ex2(fmaf(sc[s][nt][2], cs[nt][0], shift[nt][0])), p3 = ex2(fmaf(sc[s][nt][3], cs[nt][1], shift[nt][1]));
+                    l[nt][0] += p0 + p2;
+                    l[nt][1] += p1 + p3;
+                    pb[s][nt][0] = transpose8x8(h2_bits(__floats2half2_rn(p0, p1)));
+                    pb[s][nt][1] = transpose8x8(h2_bits(__floats2half2_rn(p2, p3)));
+                }
             // ---- phase 3
-            uint32_t va[G], vb[G], ma[2 * G], mb[2 * G];
-            load_words<G>(blk + B::V_CODES + t * D + g * G * 4, va);
-            load_words<G>(blk + B::V_CODES + (t + 4) * D + g * G * 4, vb);
-            load_words<2 * G>(blk + B::V_SCALES + t * G * 8, ma);
-            load_words<2 * G>(blk + B::V_SCALES + (t + 4) * G * 8, mb);
-            uint32_t nans[G];                    // tokens of the block whose group reads back as NaN, if the block has any that a column must not see
-            bool any_nan = false;
-            if (masked) {
-                // Behind the sequence's end lies whatever the page held before; and a weight of zero does not keep a NaN out of the sum.  Such groups
-                // go in as zeros here, and come back below for the columns that do see their token.
-                const int ta = tok0 + 2 * t, tb = ta + 8;
-                const uint32_t keep_a = (ta < s.len ? 0xffffu : 0u) | (ta + 1 < s.len ? 0xffff0000u : 0u), keep_b = (tb < s.len ? 0xffffu : 0u) | (tb + 1 < s.len ? 0xffff0000u : 0u);
+#pragma unroll
+            for (int s = 0; s < STEP_BLOCKS; ++s) {
+                const uint8_t* const blk = stage + s * B::BYTES;
+                uint32_t va[G], vb[G], ma[2 * G], mb[2 * G];
+                load_words<G>(blk + B::V_CODES + t * D + g * G * 4, va);
+                load_words<G>(blk + B::V_CODES + (t + 4) * D + g * G * 4, vb);
+                load_words<2 * G>(blk + B::V_SCALES + t * G * 8, ma);
+                load_words<2 * G>(blk + B::V_SCALES + (t + 4) * G * 8, mb);
+                uint32_t nans[G];                // tokens of the block whose group reads back as NaN, if the block has any that a column must not see
+                bool any_nan = false;
+                if (masked) {
+                    // Behind the sequence's end lies whatever the page held before; and a weight of zero does not keep a NaN out of the sum.  Such groups
+                    // go in as zeros here, and come back below for the columns that do see their token.
+                    const int ta = tok0 + s * CACHE_BLOCK + 2 * t, tb = ta + 8, end_tok = (have >> s & 1u) ? len : 0;
+                    const uint32_t keep_a = (ta < end_tok ? 0xffffu : 0u) | (ta + 1 < end_tok ? 0xffff0000u : 0u), keep_b = (tb < end_tok ? 0xffffu : 0u) | (tb + 1 < end_tok ? 0xffff0000u : 0u);
+#pragma unroll
+                    for (int w = 0; w < G; ++w) {
+                        uint32_t bits = 0;
+                        auto one = [&](uint32_t& S, uint32_t& M, uint32_t keep, int at) {
+                            S &= keep; M &= keep;
+                            // (an exponent of all ones, in either half of either word)
+                            const uint32_t x = (((S & 0x7c007c00u) + 0x04000400u) | ((M & 0x7c007c00u) + 0x04000400u)) & 0x80008000u;
+                            const uint32_t drop = (x >> 15) * 0xffffu;
+                            S &= ~drop; M &= ~drop;
+                            bits |= ((x >> 15 & 1u) | (x >> 30 & 2u)) << at;
+                        };
+                        one(ma[2 * w], ma[2 * w + 1], keep_a, 2 * t);
+                        one(mb[2 * w], mb[2 * w + 1], keep_b, 2 * t + 8);
+                        nans[w] = __reduce_or_sync(0xffffffffu, bits);
+                        any_nan |= nans[w] != 0;
+                    }
+                }
 #pragma unroll
                 for (int w = 0; w < G; ++w) {
-                    uint32_t bits = 0;
-                    auto one = [&](uint32_t& S, uint32_t& M, uint32_t keep, int at) {
-                        S &= keep; M &= keep;
-                        const __half2 hs = bits_h2(S), hm = bits_h2(M);
-                        const bool lo = __hisnan(__low2half(hs)) || __hisinf(__low2half(hs)) || __hisnan(__low2half(hm)) || __hisinf(__low2half(hm));
-                        const bool hi = __hisnan(__high2half(hs)) || __hisinf(__high2half(hs)) || __hisnan(__high2half(hm)) || __hisinf(__high2half(hm));
-                        const uint32_t drop = (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u);
-                        S &= ~drop; M &= ~drop;
-                        bits |= (lo ? 1u << at : 0u) | (hi ? 2u << at : 0u);
-                    };
-                    one(ma[2 * w], ma[2 * w + 1], keep_a, 2 * t);
-                    one(mb[2 * w], mb[2 * w + 1], keep_b, 2 * t + 8);
-                    nans[w] = __reduce_or_sync(0xffffffffu, bits);
-                    any_nan |= nans[w] != 0;
-                }
-            }
+                    const __half2 Sa = bits_h2(ma[2 * w]), Ma = bits_h2(ma[2 * w + 1]), Sb = bits_h2(mb[2 * w]), Mb = bits_h2(mb[2 * w + 1]);
 #pragma unroll
-            for (int w = 0; w < G; ++w) {
-                const __half2 Sa = bits_h2(ma[2 * w]), Ma = bits_h2(ma[2 * w + 1]), Sb = bits_h2(mb[2 * w]), Mb = bits_h2(mb[2 * w + 1]);
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t a0 = h2_bits(__hfma2(bits_h2(cache_ones(va[w], 2 * k)), Sa, Ma)), a1 = h2_bits(__hfma2(bits_h2(cache_ones(va[w], 2 * k + 1)), Sa, Ma));
+                        const uint32_t a2 = h2_bits(__hfma2(bits_h2(cache_ones(vb[w], 2 * k)), Sb, Mb)), a3 = h2_bits(__hfma2(bits_h2(cache_ones(vb[w], 2 * k + 1)), Sb, Mb));
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t a0 = h2_bits(__hfma2(bits_h2(cache_ones(va[w], 2 * k)), Sa, Ma)), a1 = h2_bits(__hfma2(bits_h2(cache_ones(va[w], 2 * k + 1)), Sa, Ma));
-                    const uint32_t a2 = h2_bits(__hfma2(bits_h2(cache_ones(vb[w], 2 * k)), Sb, Mb)), a3 = h2_bits(__hfma2(bits_h2(cache_ones(vb[w], 2 * k + 1)), Sb, Mb));
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][2 * w + k], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
-                }
-            }
-            if (any_nan) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const int n = limit[nt][c] - tok0 + 1;               // tokens of the block that the column sees
-                        const uint32_t sees = n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
-#pragma unroll
-                        for (int w = 0; w < G; ++w)
-                            if (nans[w] & sees) {
-#pragma unroll
-                                for (int k = 0; k < 2; ++k) { o[nt][2 * w + k][c] = NAN; o[nt][2 * w + k][c + 2] = NAN; }
-                            }
+                        for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][2 * w + k], a0, a1, a2, a3, pb[s][nt][0], pb[s][nt][1]);
                     }
+                }
+                if (any_nan) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const int n = limit[nt][c] - (tok0 + s * CACHE_BLOCK) + 1;       // tokens of the block that the column sees
+                            const uint32_t sees = n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
+#pragma unroll
+                            for (int w = 0; w < G; ++w)
+                                if (nans[w] & sees) {
+#pragma unroll
+                                    for (int k = 0; k < 2; ++k) { o[nt][2 * w + k][c] = NAN; o[nt][2 * w + k][c + 2] = NAN; }
+                                }
+                        }
+                }
             }
             __syncwarp();                        // all lanes are done with the block before it is overwritten
         }
@@ -444,6 +591,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
+                if (m[nt][c] > -INFINITY) m[nt][c] *= cs[nt][c];             // log2 units from here on
                 l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 4);
                 l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 8);
                 l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 16);
@@ -472,21 +620,21 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                     *reinterpret_cast<float4*>(to + 32 * w) = make_float4(o[nt][2 * w][c] * f, o[nt][2 * w][c + 2] * f, o[nt][2 * w + 1][c] * f, o[nt][2 * w + 1][c + 2] * f);
             }
         __syncthreads();
-        const int cols = min(COLS, s.nq * a.group - qt * COLS);              // columns that are rows of the call
-        float* const slot = a.part + (size_t)(2 * blockIdx.x + (u == begin ? 0 : 1)) * COLS * (D + 2);
+        const int cols = min(COLS, nq * a.group - qt * COLS);              // columns that are rows of the call
+        float* const slot = a.part + (size_t)(pc.first + pc.part) * COLS * (D + 2);
         auto store = [&](int col, int ch, float4 v, float inv) {             // four channels of a column, final
-            const int rho = qt * COLS + col, token = rho / a.group;
-            const size_t at = ((size_t)(s.q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)) * D + ch;
+            const int rho = qt * COLS + col, token = (int)fastdiv((uint32_t)rho, a.by_group);
+            const size_t at = ((size_t)(q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)) * D + ch;
             uint2 y;
             if (a.f16) y = make_uint2(h2_bits(__floats2half2_rn(v.x * inv, v.y * inv)), h2_bits(__floats2half2_rn(v.z * inv, v.w * inv)));
             else y = make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
             *reinterpret_cast<uint2*>(a.out + at) = y;
         };
         auto store_lse = [&](int col, float top, float sum) {
-            const int rho = qt * COLS + col, token = rho / a.group;
-            a.lse[(size_t)(s.q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)] = sum == 0.f ? -INFINITY : (finite_or_zero(top) + log2f(sum)) * LN2;
+            const int rho = qt * COLS + col, token = (int)fastdiv((uint32_t)rho, a.by_group);
+            a.lse[(size_t)(q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)] = sum == 0.f ? -INFINITY : (finite_or_zero(top) + log2f(sum)) * LN2;
         };
-        for (int e = tid; e < cols * (D / 4); e += 32 * WARPS) {
+        for (int e = tid; e < cols * (D / 4); e += THREADS) {
             const int col = e / (D / 4), ch = 4 * (e - col * (D / 4));
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -502,76 +650,134 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
             else if (a.lse) store_lse(tid, top_s[tid], sum_s[tid]);
         }
         if (!whole) {
-            const int c0 = cta_of(row_first), c1 = cta_of(row_first + s.steps - 1), parts = c1 - c0 + 1;
-            __threadfence();
+            const int parts = pc.parts;
             __syncthreads();
-            if (tid == 0) last_s = atomicInc(&g_arrived[c0], (unsigned)(parts - 1)) == (unsigned)(parts - 1);
+            if (tid == 0) last_s = arrive(&g_arrived[pc.first], (unsigned)(parts - 1));
             __syncthreads();
-            if (last_s) {                        // all other parts are there: join them in the order of the list
-                __threadfence();
-                const bool c0_first = W * c0 / ctas == row_first;            // the row's first part is its CTA's first piece, or its last
-                auto part_of = [&](int p) { return a.part + (size_t)(2 * (c0 + p) + (p > 0 || c0_first ? 0 : 1)) * COLS * (D + 2); };
-                if (tid < COLS) {
-                    float top = -INFINITY, sum = 0.f;
-                    if (tid < cols) {
-                        for (int p = 0; p < parts; ++p) top = fmaxf(top, __ldcg(part_of(p) + COLS * D + tid));
-                        for (int p = 0; p < parts; ++p) sum += __ldcg(part_of(p) + COLS * (D + 1) + tid) * ex2(__ldcg(part_of(p) + COLS * D + tid) - finite_or_zero(top));
-                        if (a.lse) store_lse(tid, top, sum);
-                    }
-                    top_s[tid] = top;
-                    sum_s[tid] = sum;
+            if (last_s) {                        // all other parts are there: join them in their order
+                auto part_of = [&](int p) { return a.part + (size_t)(pc.first + p) * COLS * (D + 2); };
+                // With fewer groups of four channels than threads, several threads share one and take its parts in turn; what a thread needs first is asked
+                // for ahead of the factors.
+                constexpr int AHEAD = 8;
+                const int n = cols * (D / 4), sharers = max(THREADS / n, 1), mine = sharers > 1 ? tid / n : 0, step = sharers;
+                const int e1 = sharers > 1 ? tid - mine * n : tid;
+                auto part_at = [&](int p, int e) { return __ldcg(reinterpret_cast<const float4*>(part_of(p) + 4 * e)); };      // (column e / (D / 4): they lie one after another)
+                float4 x[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const int p = mine + k * step;
+                    x[k] = e1 < n && mine < sharers && p < parts ? part_at(p, e1) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                // the parts' maxima and sums; maxima become factors.  (parts <= MOST_PARTS: they fit the ring)
+                float* const mp = join;
+                float* const lp = join + parts * COLS;
+#pragma unroll 4
+                for (int e = tid; e < parts * COLS; e += THREADS) {
+                    const int p = e / COLS, col = e - p * COLS;
+                    const float* from = part_of(p) + COLS * D + col;
+                    mp[e] = col < cols ? __ldcg(from) : -INFINITY;
+                    lp[e] = col < cols ? __ldcg(from + COLS) : 0.f;
                 }
                 __syncthreads();
-                for (int e = tid; e < cols * (D / 4); e += 32 * WARPS) {
-                    const int col = e / (D / 4), ch = 4 * (e - col * (D / 4));
-                    const float top = finite_or_zero(top_s[col]);
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                    for (int p = 0; p < parts; ++p) {
-                        const float* from = part_of(p);
-                        const float f = ex2(__ldcg(from + COLS * D + col) - top);
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(from + col * D + ch));
-                        v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+                {
+                    constexpr int PER = THREADS / COLS < 32 ? THREADS / COLS : 32;       // neighbouring lanes on a column
+                    const int col = tid / PER, part = tid % PER;
+                    if (tid < COLS * PER) {
+                        float top = -INFINITY, sum = 0.f;
+                        for (int p = part; p < parts; p += PER) top = fmaxf(top, mp[p * COLS + col]);
+#pragma unroll
+                        for (int s = 1; s < PER; s *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+                        for (int p = part; p < parts; p += PER) {
+                            const float f = ex2(mp[p * COLS + col] - finite_or_zero(top));
+                            mp[p * COLS + col] = f;
+                            sum += f * lp[p * COLS + col];
+                        }
+#pragma unroll
+                        for (int s = 1; s < PER; s *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+                        if (part == 0) {
+                            sum_s[col] = sum;
+                            if (a.lse && col < cols) store_lse(col, top, sum);
+                        }
                     }
-                    store(col, ch, v, sum_s[col] == 0.f ? 0.f : 1.f / sum_s[col]);
+                }
+                __syncthreads();
+                float4* const some = reinterpret_cast<float4*>(join + (2 * parts * COLS + 3) / 4 * 4);
+                for (int e = e1; e - e1 < n; e += THREADS) {                 // (one round where threads share)
+                    const int col = e / (D / 4);
+                    const bool takes = e < n && mine < sharers;
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int p0 = mine; p0 < parts; p0 += AHEAD * step) {
+                        if (e != e1 || p0 != mine) {
+#pragma unroll
+                            for (int k = 0; k < AHEAD; ++k) {
+                                const int p = p0 + k * step;
+                                x[k] = takes && p < parts ? part_at(p, e) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < AHEAD; ++k) {
+                            const int p = p0 + k * step;
+                            const float f = takes && p < parts ? mp[p * COLS + col] : 0.f;
+                            v.x = fmaf(f, x[k].x, v.x); v.y = fmaf(f, x[k].y, v.y); v.z = fmaf(f, x[k].z, v.z); v.w = fmaf(f, x[k].w, v.w);
+                        }
+                    }
+                    if (sharers > 1) {
+                        some[tid] = v;
+                        __syncthreads();
+                        for (int k = 1; k < sharers && mine == 0; ++k) {
+                            const float4 y = some[k * n + e];
+                            v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
+                        }
+                    }
+                    if (takes && mine == 0) store(col, 4 * (e - col * (D / 4)), v, sum_s[col] == 0.f ? 0.f : 1.f / sum_s[col]);
                 }
             }
         }
         fence_async_smem();                      // the ring is written by copies again
-        __syncthreads();
-        u += step1 - step0;
     }
     if (!ok)                                     // copies already asked for land before shared memory is released
-        for (uint32_t c = used; c < loaded; ++c) mbar_wait_drain(&full[warp][c % ST], (c / ST) & 1);
+        for (; in_flight > 0; --in_flight) {
+            mbar_wait_drain(&full[warp][use_slot], use_phase);
+            if (++use_slot == ST) { use_slot = 0; use_phase ^= 1; }
+        }
     if (lane == 0 && abort_flag) atomicExch(&dc->status, (int)PSA_ERR_TIMEOUT);
 }
 
 template <int D, int NT>
-int launch_attn(const AttnArgs& a, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
+int launch_attn(const AttnArgs& all, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
     using Cfg = ACfg<D, NT>;
     static DeviceSetup setup;
     const int sms = device_setup(&setup, [] {
         return cudaFuncSetAttribute(cache_attn_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, ACfg<D, NT>::SMEM);
     }, "cache attention set-up");
     if (sms <= 0) return PSA_ERR_CUDA;
-    // every CTA works on at least one step: no more of them than the tables have room for
-    const long long tiles = ((long long)a.rows * a.group + Cfg::COLS - 1) / Cfg::COLS + a.sequences;
-    const long long most = tiles * a.kv_heads * (((long long)a.width * a.page_size + CACHE_BLOCK - 1) / CACHE_BLOCK);
-    long long grid = (long long)sms * Cfg::CTAS;
-    if (grid > MAX_CTAS) grid = MAX_CTAS;
-    if (grid > (most + LEAST_STEPS - 1) / LEAST_STEPS) grid = (most + LEAST_STEPS - 1) / LEAST_STEPS;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(32 * WARPS);
-    cfg.dynamicSmemBytes = Cfg::SMEM;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, cache_attn_kernel<D, NT>, a, dc, dc_next);
-    if (e != cudaSuccess) { set_cuda_error(e, "cache_attn_kernel launch"); return PSA_ERR_CUDA; }
+    for (int b0 = 0; b0 < all.sequences; b0 += SEQS) {
+        AttnArgs a = all;
+        a.sequences = all.sequences - b0 < SEQS ? all.sequences - b0 : SEQS;
+        a.seqs += b0;
+        a.q_starts += b0;
+        // (upper bounds: the lengths are known on the device only)
+        const long long tiles = ((long long)a.rows * a.group + Cfg::COLS - 1) / Cfg::COLS + a.sequences;
+        const long long most = tiles * a.kv_heads * (((long long)a.width * a.page_size + STEP - 1) / STEP);
+        if (most > 0x7fffffffLL) return PSA_ERR_UNSUPPORTED;
+        long long grid = (long long)sms * Cfg::CTAS;
+        if (grid > MAX_CTAS) grid = MAX_CTAS;
+        if (grid > most) grid = most;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)grid);
+        cfg.blockDim = dim3(Cfg::THREADS);
+        cfg.dynamicSmemBytes = Cfg::SMEM;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        // (the counter that items are handed out by serves one launch)
+        cudaError_t e = b0 == 0 ? cudaSuccess : cudaMemsetAsync(&dc->next_item, 0, sizeof(dc->next_item), stream);
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, cache_attn_kernel<D, NT>, a, dc, b0 == 0 ? dc_next : nullptr);
+        if (e != cudaSuccess) { set_cuda_error(e, "cache_attn_kernel launch"); return PSA_ERR_CUDA; }
+    }
     return PSA_OK;
 }
 
@@ -583,14 +789,20 @@ int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const
                     float scale, int dtype, void* out, float* lse, void* scratch, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
     const AttnArgs a = {static_cast<const uint8_t*>(c.pool), c.tables, c.lens, seqs, q_starts, static_cast<const uint16_t*>(Q), static_cast<uint16_t*>(out), lse,
                         static_cast<float*>(scratch), q_stride, c.pages, c.slots, c.width, c.page_size, c.kv_heads, heads / c.kv_heads, sequences, rows,
-                        dtype == PSA_F16, scale};
+                        dtype == PSA_F16, scale, fastdiv_make((uint32_t)(heads / c.kv_heads)), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
     const bool wide = (long long)max_q * a.group > 8;        // more than eight columns: two tiles of them share a block's codes
+    auto launch = [&](auto width, auto tiles_of_columns) {
+        return launch_attn<decltype(width)::value, decltype(tiles_of_columns)::value>(a, dc, dc_next, stream);
+    };
+    using std::integral_constant;
+    const integral_constant<int, 1> one;
+    const integral_constant<int, 2> two;
     switch (c.d_k) {
-        case 32: return wide ? launch_attn<32, 2>(a, dc, dc_next, stream) : launch_attn<32, 1>(a, dc, dc_next, stream);
-        case 64: return wide ? launch_attn<64, 2>(a, dc, dc_next, stream) : launch_attn<64, 1>(a, dc, dc_next, stream);
-        case 96: return wide ? launch_attn<96, 2>(a, dc, dc_next, stream) : launch_attn<96, 1>(a, dc, dc_next, stream);
-        case 128: return wide ? launch_attn<128, 2>(a, dc, dc_next, stream) : launch_attn<128, 1>(a, dc, dc_next, stream);
-        case 256: return launch_attn<256, 1>(a, dc, dc_next, stream);       // (two tiles' output and queries would not fit the registers)
+        case 32: return wide ? launch(integral_constant<int, 32>{}, two) : launch(integral_constant<int, 32>{}, one);
+        case 64: return wide ? launch(integral_constant<int, 64>{}, two) : launch(integral_constant<int, 64>{}, one);
+        case 96: return wide ? launch(integral_constant<int, 96>{}, two) : launch(integral_constant<int, 96>{}, one);
+        case 128: return wide ? launch(integral_constant<int, 128>{}, two) : launch(integral_constant<int, 128>{}, one);
+        case 256: return launch(integral_constant<int, 256>{}, one);         // (two tiles' output and queries would not fit the registers)
         default: return PSA_ERR_UNSUPPORTED;
     }
 }

@@ -247,3 +247,20 @@ def test_offsets_beyond_32_bits():
     psa.psa_cache_append(K, V, pool, tables, small.lens, small.seqs, ref.starts([1, 1]), page)
     psa.psa_cache_append(K, V, small.pool, small.tables, small.lens, small.seqs, ref.starts([1, 1]), page)
     assert torch.equal(pool[pages - small.pages:], small.pool)
+
+
+def test_starts_that_descend():
+    c = Made([40, 20, 30], 1, 64, 16, 26)
+    Q = _queries(9, 2, 64, BF)
+    bad = torch.tensor([0, 9, 0, 9], dtype=torch.int32, device="cuda")
+    out = psa.psa_cache_attention(Q, c.pool, c.tables, c.lens, c.seqs, bad, 1, 16, max_q=9, out=torch.full((9, 128), 3.0, dtype=BF, device="cuda"))
+    assert psa.psa_last_issued()[0] == psa.ERR_SHAPE and (out == 3).all()
+    far = torch.tensor([-3, 4, 4, 1000], dtype=torch.int32, device="cuda")               # rows outside the tensor are not touched
+    assert torch.equal(psa.psa_cache_attention(Q, c.pool, c.tables, c.lens, c.seqs, far, 1, 16, max_q=9), c.attend(Q, [4, 0, 5], max_q=9))
+    assert psa.psa_last_issued()[0] == psa.OK
+
+
+def test_more_sequences_than_a_launch_takes():
+    lens = [(i * 37) % 70 for i in range(700)]
+    c = Made(lens, 1, 32, 16, 27)
+    _check(c, [i % 3 for i in range(700)], 2, BF)
