@@ -308,6 +308,8 @@ int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
 int psa_prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts,
                          const int* k_starts, int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d_k, float scale, int dtype, void* out,
                          float* lse, void* stream);
+/* Workspace of such a call: more than the counters where prompts are few and keys many, so that key blocks are shared out among CTAs and joined (43 MB at d_k = 128). */
+size_t psa_prompt_workspace_bytes(int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d_k);
 
 /*
  * A layer's cache: keys and values in pages of `page_size` tokens (a multiple of 16), every token, head and group of 32 channels with 4-bit codes c and two fp16

@@ -724,6 +724,7 @@ int psa_last_issued(void* stream, psa_counts* c) {
     c->qk_macs = h.qk_macs;
     c->pv_macs = h.pv_macs;
     c->exps = h.exps;
+    if (h.status == PSA_ERR_TIMEOUT && (e = prompt_reset()) != cudaSuccess) { set_cuda_error(e, "psa_last_issued"); return PSA_ERR_CUDA; }
     return h.status;
 }
 
@@ -883,10 +884,16 @@ int psa_prompt_attention(const void* Q, const void* K, const void* V, long long 
     if ((long long)heads * d_k > 0x7fffffffLL || !good_stride(q_stride, (long long)heads * d_k)) return PSA_ERR_SHAPE;
     if (k_rows > 0 && (!good_stride(k_stride, (long long)kv_heads * d_k) || !good_stride(v_stride, (long long)kv_heads * d_k))) return PSA_ERR_SHAPE;
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(out) || !aligned4(lse) || !aligned4(q_starts) || !aligned4(k_starts)) return PSA_ERR_ALIGN;
-    return run_op(0, stream, [&](const OpCall& c) {
+    const size_t scratch = prompt_scratch_bytes(sequences, q_rows, k_rows, heads, kv_heads, d_k);
+    return run_op(scratch, stream, [&](const OpCall& c) {
         return prompt_attention(Q, K, V, q_stride, k_stride, v_stride, q_starts, k_starts ? k_starts : q_starts, sequences, q_rows, k_rows, heads, kv_heads, d_k, scale,
-                                dtype, out, lse, c.dc, &c.dc->next_item, c.dc_next, static_cast<cudaStream_t>(stream));
+                                dtype, out, lse, scratch ? c.ws + COUNTER_BYTES : nullptr, c.dc, &c.dc->next_item, c.dc_next, static_cast<cudaStream_t>(stream));
     });
+}
+
+size_t psa_prompt_workspace_bytes(int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d_k) {
+    if (sequences <= 0 || q_rows < 0 || k_rows < 0 || heads <= 0 || kv_heads <= 0 || d_k <= 0 || heads % kv_heads || d_k > 128 || d_k % 8 || heads / kv_heads > 128) return 0;
+    return COUNTER_BYTES + prompt_scratch_bytes(sequences, q_rows, k_rows, heads, kv_heads, d_k);
 }
 
 size_t psa_cache_page_bytes(int kv_heads, int page_size, int d_k) {

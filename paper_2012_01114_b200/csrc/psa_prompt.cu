@@ -10,6 +10,8 @@
 //     128 leave up to 7 % of the rows empty.
 //   * The host does not know the lengths.  Every CTA derives the work list from `starts` by itself (sequences sorted by length in shared memory): the heaviest pairs of row
 //     tiles of all sequences first, heads innermost, taken from a device counter, as in attn_persist_kernel.
+//   * Where the pairs of row tiles are fewer than the CTAs (a few prompts, or pieces of them, behind long contexts) their key blocks are cut into parts as well: a warp then
+//     stores its rows' sums in fp32, and the one that comes last joins the parts of its sixteen rows, in their order.  Nobody else is waited for.
 //   * A tile may reach into the next sequence.  Its rows beyond the sequence are computed and not stored, so the output is stored row by row; keys beyond it carry
 //     no weight, and neither do non-finite values there (a weight of zero would not keep them out of the sum): in blocks that some row of the tile does
 //     not see in full the softmax warps look through the tile of V before P V and set what is not finite to zero; rows that do see such a value get it
@@ -45,8 +47,9 @@ struct PCfg {
 struct PMaps {
     CUtensorMap q, k, v;
 };
-constexpr int SEQS = 512;               // sequences of one launch
-constexpr int SEQ_BITS = 9;
+constexpr int SEQ_BITS = 9, SEQS = 1 << SEQ_BITS;      // sequences of one launch
+constexpr int MAX_CTAS = 160;           // partial results and arrival counts: two parts per CTA
+constexpr int LEAST_PIECE = 4;          // key blocks: what storing and joining a part costs, 6000 cycles, is two to three of them
 
 struct PromptArgs {
     const int *q_starts, *k_starts;
@@ -54,7 +57,7 @@ struct PromptArgs {
     long long v_stride;
     const uint16_t* v;                  // (the epilogue's look at values that are not finite)
     uint16_t* out;
-    float* lse;
+    float *lse, *part;                  // part (null: nothing is cut): [2 MAX_CTAS][2 tiles][128 rows][D] sums, then as many rows' maxima and sums
     float sl2;
     FastDiv by_group, by_heads;
 };
@@ -63,8 +66,18 @@ struct __align__(16) Item {
     int q0, k0;                         // first rows of the sequence
     int i0, nq, nk;                     // first token of the first tile, lengths
     int h;                              // key/value head
-    int nkv0, nkv1;                     // key blocks of the two tiles (0: no rows, or rows without keys)
+    int nkv0, nkv1;                     // key blocks of the two tiles, from block j0 on (0: no rows, or rows that see no key of these blocks)
+    int j0, slot, part, parts;          // slot: of the first part's results, if there are several
 };
+// Arrivals of the warps on rows of several parts, by slot of the first part, tile and warp.  The arrival that completes a count wraps it to zero again.
+__device__ unsigned g_prompt_arrived[2 * MAX_CTAS][2][SOFTMAX_WARPS_PER_TILE];
+// Counts a warp's arrival behind what its lanes have stored; true in all of them for the one that completes the rows.
+__device__ __forceinline__ bool warp_arrive(unsigned* count, unsigned last, int lane) {
+    unsigned old = 0;
+    __syncwarp();
+    if (lane == 0) asm volatile("fence.acq_rel.gpu;\n\tatom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(old) : "l"(count), "r"(last) : "memory");
+    return __shfl_sync(0xffffffffu, old, 0) == last;
+}
 
 struct PBars {
     uint64_t item_full[2], item_empty[2];
@@ -149,7 +162,11 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     __shared__ int v_bad;                        // count of the last item in which V held something that is not finite, see above
     // the work list: sequences by falling number of pairs of row tiles (key = pairs << SEQ_BITS | SEQS - 1 - sequence), see `decode`
     __shared__ uint32_t key[SEQS];
-    __shared__ int base[SEQS + 1], starts_s[2][SEQS + 1];
+    __shared__ __align__(16) int base[SEQS + 4];
+    __shared__ int starts_s[2][SEQS + 1];
+    __shared__ uint32_t cut[SEQS + 1], cut_sum[ISSUER1_WARP + 1];       // with pairs cut into parts: items << 16 | results ahead of a pair
+    __shared__ Item own[2 * SOFTMAX_WARPS_PER_TILE][2];                 // a softmax warp's items, this one and the next
+    __shared__ Item first_item;                  // this CTA's first item, found by the thread that knows its sequence or pair
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -185,26 +202,26 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     // the counter block of the NEXT call on this workspace is cleared here, off that call's critical path
     if (threadIdx.x == 0 && blockIdx.x == 0 && dc_next) *dc_next = DeviceCounters{0, 0, 0, 0, 0, 0, 0};
     // ---- the work list
-    int n2 = 1;                                  // sequences, rounded up to a power of two
-    while (n2 < pa.sequences) n2 *= 2;
     for (int i = threadIdx.x; i <= pa.sequences; i += persist_threads<D>()) {
         starts_s[0][i] = min(max(pa.q_starts[i], 0), pa.q_rows);
         starts_s[1][i] = min(max(pa.k_starts[i], 0), pa.k_rows);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < n2; i += persist_threads<D>()) {
+    uint32_t* const unsorted = reinterpret_cast<uint32_t*>(base);
+    for (int i = threadIdx.x; i < (pa.sequences + 3) / 4 * 4; i += persist_threads<D>()) {
         const int nq = i < pa.sequences ? max(starts_s[0][i + 1] - starts_s[0][i], 0) : 0;
-        key[i] = (uint32_t)((nq + 2 * pa.tokens - 1) / (2 * pa.tokens)) << SEQ_BITS | (uint32_t)(SEQS - 1 - i);
+        unsorted[i] = i < pa.sequences ? (uint32_t)((nq + 2 * pa.tokens - 1) / (2 * pa.tokens)) << SEQ_BITS | (uint32_t)(SEQS - 1 - i) : 0u;
     }
-    for (int k = 2; k <= n2; k *= 2)             // bitonic, descending
-        for (int j = k / 2; j > 0; j /= 2) {
-            __syncthreads();
-            const int i = 2 * j * ((int)threadIdx.x / j) + (int)threadIdx.x % j;
-            if (i + j < n2 && (int)threadIdx.x < n2 / 2) {
-                const uint32_t x = key[i], y = key[i + j];
-                if ((x < y) == ((i & k) == 0)) { key[i] = y; key[i + j] = x; }
-            }
+    __syncthreads();
+    for (int i = threadIdx.x; i < pa.sequences; i += persist_threads<D>()) {     // as many places down as there are larger ones (no two are alike)
+        const uint32_t x = unsorted[i];
+        int rank = 0;
+        for (int k = 0; k < pa.sequences; k += 4) {
+            const uint4 y = *reinterpret_cast<const uint4*>(unsorted + k);
+            rank += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
         }
+        key[rank] = x;
+    }
     __syncthreads();
     if (warp == 0) {
         // base[k]: items (of one head) ahead of the levels that exactly the k + 1 longest sequences have
@@ -234,26 +251,103 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base_s;
-    const int nitems = base[pa.sequences] * pa.kv_heads;
-    // Item idx: the pairs of row tiles are counted level by level from the last one of the longest sequence down to the first of all, heads innermost.
-    auto decode = [&](int idx) -> Item {
-        const int e = (int)fastdiv((uint32_t)idx, pa.by_heads);
+    const int pairs = base[pa.sequences];
+    // Pair e, which lies behind base[k]: pairs are counted level by level from the last one of the longest sequence down to the first of all.
+    auto pair_behind = [&](int k, int e) -> Item {
+        const int r = e - base[k], down = k == 0 ? r : r / (k + 1), level = (int)(key[k] >> SEQ_BITS) - 1 - down;
+        const int b = SEQS - 1 - (int)(key[r - down * (k + 1)] & (SEQS - 1));
+        Item w;
+        w.q0 = starts_s[0][b]; w.k0 = starts_s[1][b];
+        w.nq = starts_s[0][b + 1] - w.q0; w.nk = max(starts_s[1][b + 1] - w.k0, 0);
+        w.i0 = 2 * level * pa.tokens;
+        // blocks up to the last key that the tile's last row sees
+        auto blocks = [&](int i0) { return i0 >= w.nq ? 0 : max(min(i0 + pa.tokens, w.nq) + w.nk - w.nq + TILE - 1, 0) / TILE; };
+        w.nkv0 = blocks(w.i0);
+        w.nkv1 = blocks(w.i0 + pa.tokens);
+        w.h = w.j0 = w.slot = w.part = 0;
+        w.parts = 1;
+        return w;
+    };
+    auto pair_of = [&](int e) -> Item {
         int lo = 0, hi = pa.sequences - 1;       // the last k with base[k] <= e
         while (lo < hi) {
             const int mid = (lo + hi + 1) / 2;
             if (base[mid] <= e) lo = mid; else hi = mid - 1;
         }
-        const int r = e - base[lo], level = (int)(key[lo] >> SEQ_BITS) - 1 - r / (lo + 1);
-        const int b = SEQS - 1 - (int)(key[r % (lo + 1)] & (SEQS - 1));
+        return pair_behind(lo, e);
+    };
+    // Part `part` of a pair that is cut into `parts`, whose results for all heads begin at slot `at`.
+    auto part_of_pair = [&](Item w, int part, int parts, int at, int h) -> Item {
+        const int each = (max(w.nkv0, w.nkv1) + parts - 1) / parts;
+        w.part = part;
+        w.parts = parts;
+        w.slot = at * pa.kv_heads + h * parts;
+        w.j0 = part * each;
+        w.nkv0 = min(max(w.nkv0 - w.j0, 0), each);
+        w.nkv1 = min(max(w.nkv1 - w.j0, 0), each);
+        return w;
+    };
+    const int x0 = (int)fastdiv(blockIdx.x, pa.by_heads), h0 = (int)blockIdx.x - x0 * pa.kv_heads;       // the CTA's first item
+    // Fewer pairs than CTAs: their key blocks are cut into pieces of blocks / (CTAs - pairs), which makes no more parts than there are CTAs.
+    const bool cuts = pa.part && pairs > 0 && pairs <= SEQS && pairs * pa.kv_heads < (int)gridDim.x;
+    if (!cuts) {
+        for (int k = threadIdx.x; k < pa.sequences; k += persist_threads<D>())
+            if (base[k] <= x0 && x0 < base[k + 1]) { first_item = pair_behind(k, x0); first_item.h = h0; }
+    } else {
+        int blocks = 0;
         Item w;
-        w.q0 = starts_s[0][b]; w.k0 = starts_s[1][b];
-        w.nq = starts_s[0][b + 1] - w.q0; w.nk = max(starts_s[1][b + 1] - w.k0, 0);
-        w.i0 = 2 * level * pa.tokens;
-        w.h = idx - e * pa.kv_heads;
-        // blocks up to the last key that the tile's last row sees
-        auto blocks = [&](int i0) { return i0 >= w.nq ? 0 : max(min(i0 + pa.tokens, w.nq) + w.nk - w.nq + TILE - 1, 0) / TILE; };
-        w.nkv0 = blocks(w.i0);
-        w.nkv1 = blocks(w.i0 + pa.tokens);
+        if ((int)threadIdx.x < pairs) {
+            w = pair_of(threadIdx.x);
+            blocks = max(w.nkv0, w.nkv1);
+        }
+        const int in_warp = __reduce_add_sync(0xffffffffu, blocks);
+        if (lane == 0) cut_sum[warp] = (uint32_t)in_warp;
+        __syncthreads();
+        uint32_t all = 0;
+        for (int w = 0; w < persist_threads<D>() / 32; ++w) all += cut_sum[w];
+        const uint32_t budget = max((int)gridDim.x - pairs * pa.kv_heads, ((int)gridDim.x + 1) / 2);
+        const uint32_t piece = max((all * pa.kv_heads + budget - 1) / budget, (uint32_t)LEAST_PIECE);
+        const uint32_t parts = (int)threadIdx.x < pairs ? max((blocks + piece - 1) / piece, 1u) : 0u, mine = parts << 16 | (parts > 1 ? parts : 0u);
+        uint32_t x = mine;
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, x, s);
+            if (lane >= s) x += y;
+        }
+        __syncthreads();
+        if (lane == 31) cut_sum[warp] = x;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) x += cut_sum[w];
+        if ((int)threadIdx.x < pairs) {
+            const uint32_t at = x - mine;
+            cut[threadIdx.x] = at;
+            if ((int)threadIdx.x == pairs - 1) cut[pairs] = x;
+            const int part = x0 - (int)(at >> 16);
+            if (part >= 0 && part < (int)parts) {
+                first_item = parts > 1 ? part_of_pair(w, part, parts, (int)(at & 0xffffu), h0) : w;
+                first_item.h = h0;
+            }
+        }
+    }
+    __syncthreads();
+    const int nitems = (cuts ? (int)(cut[pairs] >> 16) : pairs) * pa.kv_heads;
+    // Item idx: part by part of the pairs, heads innermost.
+    auto decode = [&](int idx) -> Item {
+        const int x = (int)fastdiv((uint32_t)idx, pa.by_heads), h = idx - x * pa.kv_heads;
+        Item w;
+        if (!cuts) {
+            w = pair_of(x);
+        } else {
+            int lo = 0, hi = pairs - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if ((int)(cut[mid] >> 16) <= x) lo = mid; else hi = mid - 1;
+            }
+            const int before = (int)(cut[lo] >> 16), parts = (int)(cut[lo + 1] >> 16) - before;
+            w = pair_of(lo);
+            if (parts > 1) w = part_of_pair(w, x - before, parts, (int)(cut[lo] & 0xffffu), h);
+        }
+        w.h = h;
         return w;
     };
 
@@ -273,7 +367,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
                     mbar_arrive(&bars.item_full[slot]);
                     break;
                 }
-                const Item work = decode(idx);
+                const Item work = it == 0 ? first_item : decode(idx);
                 item_ring[slot] = work;
                 mbar_arrive(&bars.item_full[slot]);
                 int next = -1;
@@ -304,17 +398,18 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
                         mbar_arrive_expect_tx(&bars.v_full[s], ((p > 0) + (p < maxkv)) * Cfg::TILE_BYTES);
                         if (p < maxkv)
                             for (int u = 0; u < Cfg::SUB; ++u)
-                                tma_load_3d(sK + s * Cfg::TILE_BYTES + u * 16384, &maps.k, &bars.v_full[s], 64 * u, h, work.k0 + p * TILE);
+                                tma_load_3d(sK + s * Cfg::TILE_BYTES + u * 16384, &maps.k, &bars.v_full[s], 64 * u, h, work.k0 + (work.j0 + p) * TILE);
                         if (p > 0)
                             for (int u = 0; u < Cfg::SUB; ++u)
-                                tma_load_3d(sV + s * Cfg::TILE_BYTES + u * 16384, &maps.v, &bars.v_full[s], 64 * u, h, work.k0 + (p - 1) * TILE);
+                                tma_load_3d(sV + s * Cfg::TILE_BYTES + u * 16384, &maps.v, &bars.v_full[s], 64 * u, h, work.k0 + (work.j0 + p - 1) * TILE);
                         ++vc;
                         if (p == 0) {
                             load_q();
                             if (!ok) break;
                         }
-                        // the next item's index is fetched behind the item's first loads and long before it is needed
-                        if (p == 1) take_next();
+                        // the next item is taken behind the item's last load, one or two blocks before it is needed (behind the first one, a CTA in a
+                        // long item held on to what others were free for: 28 short items behind 128 parts of 18 blocks, 64 -> 57 us)
+                        if (p == maxkv) take_next();
                     }
                 } else {
                     for (int j = 0; j < maxkv && ok; ++j) {
@@ -324,7 +419,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
                             if (!ok) break;
                             mbar_arrive_expect_tx(&bars.k_full[s], Cfg::TILE_BYTES);
                             for (int u = 0; u < Cfg::SUB; ++u)
-                                tma_load_3d(sK + s * Cfg::TILE_BYTES + u * 16384, &maps.k, &bars.k_full[s], 64 * u, h, work.k0 + j * TILE);
+                                tma_load_3d(sK + s * Cfg::TILE_BYTES + u * 16384, &maps.k, &bars.k_full[s], 64 * u, h, work.k0 + (work.j0 + j) * TILE);
                             ++kc;
                         }
                         if (j == 0) {
@@ -337,12 +432,10 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
                             if (!ok) break;
                             mbar_arrive_expect_tx(&bars.v_full[s], Cfg::TILE_BYTES);
                             for (int u = 0; u < Cfg::SUB; ++u)
-                                tma_load_3d(sV + s * Cfg::TILE_BYTES + u * 16384, &maps.v, &bars.v_full[s], 64 * u, h, work.k0 + j * TILE);
+                                tma_load_3d(sV + s * Cfg::TILE_BYTES + u * 16384, &maps.v, &bars.v_full[s], 64 * u, h, work.k0 + (work.j0 + j) * TILE);
                             ++vc;
                         }
-                        // the next item's index is fetched behind the item's first loads (the atomic's round trip of about
-                        // a thousand cycles would otherwise delay them) and long before it is needed
-                        if (j == 0) take_next();
+                        if (j == maxkv - 1) take_next();         // (behind the item's last load, as above)
                     }
                 }
                 idx = next;
@@ -594,43 +687,44 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
         uint32_t blk = 0;                                       // blocks this tile slot has processed, all items
         uint32_t vbase = 0;                                     // ring position of the item's first V tile (PAIRED: of its pair 0)
         bool ok = true;
-        // this thread's rows as tokens of a tile and heads of a group; rows that the warp stores: lane / 4 and lane / 4 + 8
-        const int tokA = (int)fastdiv((uint32_t)rA, pa.by_group), tokB = (int)fastdiv((uint32_t)rB, pa.by_group);
-        const int headA = rA - tokA * pa.group, headB = rB - tokB * pa.group;
-        // Takes entry `it` of the item ring; h = -1 at the end of the list, -2 when the wait ran out.
-        auto take_item = [&](uint32_t it) -> Item {
-            Item w;
-            w.h = -2;
-            if (!__all_sync(0xffffffffu, mbar_wait(&bars.item_full[it & 1], (it >> 1) & 1, abortp))) return w;
-            w = item_ring[it & 1];
+        // Takes entry `it` of the item ring to the warp's own copy (what is needed of it is read from there again and again rather than kept in
+        // registers); its head, -1 at the end of the list, -2 when the wait ran out.
+        auto take_item = [&](uint32_t it) -> int {
+            if (!__all_sync(0xffffffffu, mbar_wait(&bars.item_full[it & 1], (it >> 1) & 1, abortp))) return -2;
+            const int h = item_ring[it & 1].h;
+            if (lane < (int)(sizeof(Item) / 4)) reinterpret_cast<int*>(&own[sw][it & 1])[lane] = reinterpret_cast<const int*>(&item_ring[it & 1])[lane];
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.item_empty[it & 1]);
-            return w;
+            return h;
+        };
+        // Output rows of this thread's two rows (rows as tokens of a tile and heads of a group), -1 for a row of the tile that is none of the sequence's.
+        auto out_row = [&](const Item& w, int r) -> long long {
+            const int tok = (int)fastdiv((uint32_t)r, pa.by_group), i = w.i0 + t * pa.tokens + tok;
+            return tok < pa.tokens && i < w.nq ? (long long)(w.q0 + i) * pa.heads + w.h * pa.group + (r - tok * pa.group) : -1;
         };
         uint32_t it = 0;
-        Item work = take_item(it++);
-        while (work.h >= 0) {
-            const int nkv = t ? work.nkv1 : work.nkv0, i0 = work.i0 + t * pa.tokens;
+        int head = take_item(it++);
+        while (head >= 0) {
+            const Item& work = own[sw][(it - 1) & 1];
+            const int nkv = t ? work.nkv1 : work.nkv0, j0 = work.j0;
             const int vfirst = vbase + (PAIRED ? 1 : 0);
             if (max(work.nkv0, work.nkv1) > 0) vbase += max(work.nkv0, work.nkv1) + (PAIRED ? 1 : 0);
-            const bool liveA = i0 + tokA < work.nq && tokA < pa.tokens, liveB = i0 + tokB < work.nq && tokB < pa.tokens;
-            const size_t outA = (size_t)(work.q0 + i0 + tokA) * pa.heads + work.h * pa.group + headA, outB = (size_t)(work.q0 + i0 + tokB) * pa.heads + work.h * pa.group + headB;
-            if (nkv == 0) {                                     // rows without keys, or no rows
-                if (liveA || liveB)
-                    for (int c = 8 * (lane & 3); c < pa.d; c += 32) {
-                        if (liveA) *reinterpret_cast<uint4*>(pa.out + outA * pa.d + c) = make_uint4(0, 0, 0, 0);
-                        if (liveB) *reinterpret_cast<uint4*>(pa.out + outB * pa.d + c) = make_uint4(0, 0, 0, 0);
-                    }
-                if (pa.lse && (lane & 3) == 0) {
-                    if (liveA) pa.lse[outA] = -INFINITY;
-                    if (liveB) pa.lse[outB] = -INFINITY;
+            if (nkv == 0 && work.parts == 1) {                  // rows without keys, or no rows
+                const long long outA = out_row(work, rA), outB = out_row(work, rB);
+                for (int c = 8 * (lane & 3); c < pa.d; c += 32) {
+                    if (outA >= 0) *reinterpret_cast<uint4*>(pa.out + outA * pa.d + c) = make_uint4(0, 0, 0, 0);
+                    if (outB >= 0) *reinterpret_cast<uint4*>(pa.out + outB * pa.d + c) = make_uint4(0, 0, 0, 0);
                 }
-                work = take_item(it++);
+                if (pa.lse && (lane & 3) == 0) {
+                    if (outA >= 0) pa.lse[outA] = -INFINITY;
+                    if (outB >= 0) pa.lse[outB] = -INFINITY;
+                }
+                head = take_item(it++);
                 continue;
             }
             // the last keys that the rows see, and the first block that not all rows of the tile see in full
-            const int off = work.nk - work.nq;
-            const int limA = min(i0 + tokA + off, work.nk - 1), limB = min(i0 + tokB + off, work.nk - 1);
+            const int i0 = work.i0 + t * pa.tokens, off = work.nk - work.nq;
+            const int limA = min(i0 + (int)fastdiv((uint32_t)rA, pa.by_group) + off, work.nk - 1), limB = min(i0 + (int)fastdiv((uint32_t)rB, pa.by_group) + off, work.nk - 1);
             const int part0 = max(i0 + off + 1, 0) / TILE;
             float mA = -INFINITY, mB = -INFINITY, lA = 0.f, lB = 0.f;       // running maxima (log2 units) and row sums
             for (int j = 0; j < nkv; ++j, ++blk) {
@@ -643,8 +737,8 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                const bool diag = j >= part0;
-                const int cbA = limA - j * TILE, cbB = limB - j * TILE;         // last kept columns
+                const bool diag = j0 + j >= part0;
+                const int cbA = limA - (j0 + j) * TILE, cbB = limB - (j0 + j) * TILE;       // last kept columns
                 // ---- the rows' 2 x 64 scores of this block
                 uint32_t s0[32], s1[32];
                 tc_fence_after();
@@ -747,30 +841,25 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
             if (!ok) break;
             // The next item is taken now, while the last PV runs, rather than after the epilogue.
             const int items_now = (int)it;
-            const Item work_next = take_item(it++);
-            if (work_next.h == -2) break;
-            ok = mbar_wait(&bars.o_done[t], (blk - 1) & 1, abortp);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
+            const int head_next = take_item(it++);
+            if (head_next == -2) break;
+            if (nkv > 0) {
+                ok = mbar_wait(&bars.o_done[t], (blk - 1) & 1, abortp);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+            }
             // ---- epilogue: O / l, 32 columns at a time through the warp's staging buffer (chunks of 16 bytes swizzled) to whole sectors of the rows
             tc_fence_after();
             lA = quad_sum(lA);
             lB = quad_sum(lB);
-            const float invA = lA == 0.f ? 0.f : 1.f / lA, invB = lB == 0.f ? 0.f : 1.f / lB;
-            if (pa.lse && (lane & 3) == 0) {
-                if (liveA) pa.lse[outA] = lA == 0.f ? -INFINITY : (mA + log2f(lA)) * LN2;
-                if (liveB) pa.lse[outB] = lB == 0.f ? -INFINITY : (mB + log2f(lB)) * LN2;
-            }
-            const bool bad = *reinterpret_cast<volatile int*>(&v_bad) >= items_now;
-#pragma unroll
-            for (int u = 0; u < Cfg::SUB; ++u) {
-                uint32_t v[32];
+            const bool bad = nkv > 0 && *reinterpret_cast<volatile int*>(&v_bad) >= items_now;
+            // 64 columns of O, with values that are not finite put back: they were left out of the blocks from the item's first partial one on
+            auto load_o = [&](int u, uint32_t (&v)[32]) {
                 tmem_ld_quad64(tO + 64 * u, v);
                 tc_wait_ld();
                 if (bad) {
-                    // values that are not finite were left out of the blocks from the item's first partial one on: rows that see them get them back
-                    const int first = max(work.i0 + off + 1, 0) / TILE * TILE;
-                    for (int k = first; k <= max(limA, limB); ++k) {
+                    const int first = max(max(work.i0 + off + 1, 0) / TILE, j0) * TILE, last = min(max(limA, limB), (j0 + nkv) * TILE - 1);
+                    for (int k = first; k <= last; ++k) {
                         const uint16_t* row = pa.v + (size_t)(work.k0 + k) * pa.v_stride + work.h * pa.d;
 #pragma unroll
                         for (int g = 0; g < 8; ++g) {
@@ -783,32 +872,101 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
                         }
                     }
                 }
+            };
+            bool mine = true;                                   // whether this warp stores the rows' outputs
+            const int parts = work.parts;
+            // A part's sums as the warp holds them: [SUB][8][32 lanes] of four, lane by lane next to each other.
+            auto part_sums = [&](int p, int u) { return reinterpret_cast<float4*>(pa.part) + ((((size_t)(work.slot + p) * 2 + t) * SOFTMAX_WARPS_PER_TILE + wq) * Cfg::SUB + u) * 256 + lane; };
+            float2* const ml = reinterpret_cast<float2*>(pa.part + (size_t)2 * MAX_CTAS * 2 * TILE * D);
+            auto part_row = [&](int p, int r) { return (size_t)((work.slot + p) * 2 + t) * TILE + r; };
+            if (parts > 1) {
+                if (nkv > 0) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int r = lane >> 2;
+                    for (int u = 0; u < Cfg::SUB; ++u) {
+                        uint32_t v[32];
+                        load_o(u, v);
+                        float4* to = part_sums(work.part, u);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {               // chunk c of the rows' 64 bytes: columns 8 (4 half + c) + cq, + 1
-                        const int e = 4 * (4 * half + c);
-                        const uint32_t a = pack<F16>(__uint_as_float(v[e]) * invA, __uint_as_float(v[e + 1]) * invA);
-                        const uint32_t bb = pack<F16>(__uint_as_float(v[e + 2]) * invB, __uint_as_float(v[e + 3]) * invB);
-                        const int at = r * 64 + ((c ^ (r >> 1)) & 3) * 16 + 2 * cq;
-                        *reinterpret_cast<uint32_t*>(stage + at) = a;
-                        *reinterpret_cast<uint32_t*>(stage + at + 512) = bb;
+                        for (int g = 0; g < 8; ++g)
+                            __stcg(to + 32 * g, make_float4(__uint_as_float(v[4 * g]), __uint_as_float(v[4 * g + 1]), __uint_as_float(v[4 * g + 2]), __uint_as_float(v[4 * g + 3])));
                     }
-                    __syncwarp();
-                    const int at = r * 64 + (((lane & 3) ^ (r >> 1)) & 3) * 16, col = 64 * u + 32 * half + 8 * (lane & 3);
-                    if (col < pa.d) {
-                        if (liveA) *reinterpret_cast<uint4*>(pa.out + outA * pa.d + col) = *reinterpret_cast<const uint4*>(stage + at);
-                        if (liveB) *reinterpret_cast<uint4*>(pa.out + outB * pa.d + col) = *reinterpret_cast<const uint4*>(stage + at + 512);
+                }
+                if ((lane & 3) == 0) {
+                    __stcg(ml + part_row(work.part, rA), make_float2(mA, lA));
+                    __stcg(ml + part_row(work.part, rB), make_float2(mB, lB));
+                }
+                mine = warp_arrive(&g_prompt_arrived[work.slot][t][wq], (unsigned)(parts - 1), lane);
+                if (mine) {                                     // the rows' maxima and sums over all parts
+                    float topA = -INFINITY, topB = -INFINITY, sumA = 0.f, sumB = 0.f;
+#pragma unroll 4
+                    for (int p = 0; p < parts; ++p) {
+                        topA = fmaxf(topA, __ldcg(ml + part_row(p, rA)).x);
+                        topB = fmaxf(topB, __ldcg(ml + part_row(p, rB)).x);
                     }
-                    __syncwarp();
+#pragma unroll 4
+                    for (int p = 0; p < parts; ++p) {
+                        const float2 a = __ldcg(ml + part_row(p, rA)), bb = __ldcg(ml + part_row(p, rB));
+                        if (a.y != 0.f) sumA += a.y * ex2_mufu(a.x - (topA == -INFINITY ? 0.f : topA));
+                        if (bb.y != 0.f) sumB += bb.y * ex2_mufu(bb.x - (topB == -INFINITY ? 0.f : topB));
+                    }
+                    mA = topA; mB = topB; lA = sumA; lB = sumB;
+                }
+            }
+            if (mine) {
+                const long long outA = out_row(work, rA), outB = out_row(work, rB);
+                const float invA = lA == 0.f ? 0.f : 1.f / lA, invB = lB == 0.f ? 0.f : 1.f / lB;
+                if (pa.lse && (lane & 3) == 0) {
+                    if (outA >= 0) pa.lse[outA] = lA == 0.f ? -INFINITY : (mA + log2f(lA)) * LN2;
+                    if (outB >= 0) pa.lse[outB] = lB == 0.f ? -INFINITY : (mB + log2f(lB)) * LN2;
+                }
+#pragma unroll
+                for (int u = 0; u < Cfg::SUB; ++u) {
+                    uint32_t v[32];
+                    if (parts == 1) {
+                        load_o(u, v);
+                    } else {
+#pragma unroll
+                        for (int g = 0; g < 32; ++g) v[g] = 0u;
+                        for (int p = 0; p < parts; ++p) {
+                            const float2 ma = __ldcg(ml + part_row(p, rA)), mb = __ldcg(ml + part_row(p, rB));
+                            // (a part without keys for the row has no sums; its place holds anything)
+                            const float fA = ma.y == 0.f ? 0.f : ex2_mufu(ma.x - (mA == -INFINITY ? 0.f : mA)), fB = mb.y == 0.f ? 0.f : ex2_mufu(mb.x - (mB == -INFINITY ? 0.f : mB));
+                            const float4* from = part_sums(p, u);
+#pragma unroll
+                            for (int g = 0; g < 8; ++g) {
+                                const float4 x = __ldcg(from + 32 * g);
+                                if (fA != 0.f) { v[4 * g] = __float_as_uint(fmaf(fA, x.x, __uint_as_float(v[4 * g]))); v[4 * g + 1] = __float_as_uint(fmaf(fA, x.y, __uint_as_float(v[4 * g + 1]))); }
+                                if (fB != 0.f) { v[4 * g + 2] = __float_as_uint(fmaf(fB, x.z, __uint_as_float(v[4 * g + 2]))); v[4 * g + 3] = __float_as_uint(fmaf(fB, x.w, __uint_as_float(v[4 * g + 3]))); }
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const int r = lane >> 2;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {           // chunk c of the rows' 64 bytes: columns 8 (4 half + c) + cq, + 1
+                            const int e = 4 * (4 * half + c);
+                            const uint32_t a = pack<F16>(__uint_as_float(v[e]) * invA, __uint_as_float(v[e + 1]) * invA);
+                            const uint32_t bb = pack<F16>(__uint_as_float(v[e + 2]) * invB, __uint_as_float(v[e + 3]) * invB);
+                            const int at = r * 64 + ((c ^ (r >> 1)) & 3) * 16 + 2 * cq;
+                            *reinterpret_cast<uint32_t*>(stage + at) = a;
+                            *reinterpret_cast<uint32_t*>(stage + at + 512) = bb;
+                        }
+                        __syncwarp();
+                        const int at = r * 64 + (((lane & 3) ^ (r >> 1)) & 3) * 16, col = 64 * u + 32 * half + 8 * (lane & 3);
+                        if (col < pa.d) {
+                            if (outA >= 0) *reinterpret_cast<uint4*>(pa.out + outA * pa.d + col) = *reinterpret_cast<const uint4*>(stage + at);
+                            if (outB >= 0) *reinterpret_cast<uint4*>(pa.out + outB * pa.d + col) = *reinterpret_cast<const uint4*>(stage + at + 512);
+                        }
+                        __syncwarp();
+                    }
                 }
             }
             // (the next write to O_t, PV_0 of the tile's next item, waits for P of that item, which every
             // thread of the tile signals only after these reads)
             tc_fence_before();
-            ++my_items;
-            work = work_next;
+            if (nkv > 0) ++my_items;
+            head = head_next;
         }
         if (sw == 0 && lane == 0) grid_launch_dependents();
     }
@@ -844,9 +1002,11 @@ int launch_prompt(const PMaps& maps, const PromptArgs& all, DeviceCounters* dc, 
         pa.q_starts += s0;
         pa.k_starts += s0;
         // (an upper bound: the lengths are known on the device only)
-        const long long items = ((long long)pa.q_rows / (2 * pa.tokens) + pa.sequences) * pa.kv_heads;
+        long long items = ((long long)pa.q_rows / (2 * pa.tokens) + pa.sequences) * pa.kv_heads;
+        if (pa.part) items *= ((long long)pa.k_rows + TILE * LEAST_PIECE - 1) / (TILE * LEAST_PIECE);
+        const int ctas = sm_count < MAX_CTAS ? sm_count : MAX_CTAS;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(items < sm_count ? items : sm_count));
+        cfg.gridDim = dim3((unsigned)(items < ctas ? items : ctas));
         cfg.blockDim = dim3(persist_threads<D>());
         cfg.dynamicSmemBytes = Cfg::SMEM;
         cfg.stream = stream;
@@ -864,8 +1024,21 @@ int launch_prompt(const PMaps& maps, const PromptArgs& all, DeviceCounters* dc, 
 
 }  // namespace
 
+// Whether a call may have fewer pairs of row tiles than CTAs, with enough key blocks to be cut; and what that needs: a result in fp32 per part.
+size_t prompt_scratch_bytes(int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d) {
+    const int group = heads / kv_heads, tokens = TILE / group;
+    if ((long long)q_rows / (2 * tokens) * kv_heads >= MAX_CTAS || k_rows <= 2 * LEAST_PIECE * TILE || sequences > SEQS) return 0;
+    return (size_t)2 * MAX_CTAS * 2 * TILE * ((d <= 64 ? 64 : 128) + 2) * sizeof(float);
+}
+cudaError_t prompt_reset() {
+    void* p = nullptr;
+    cudaError_t e = cudaGetSymbolAddress(&p, g_prompt_arrived);
+    if (e == cudaSuccess) e = cudaMemset(p, 0, sizeof(g_prompt_arrived));
+    return e;
+}
+
 int prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts, const int* k_starts,
-                     int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, DeviceCounters* dc,
+                     int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, void* scratch, DeviceCounters* dc,
                      unsigned int* cursor, DeviceCounters* dc_next, cudaStream_t stream) {
     const int group = heads / kv_heads, tokens = TILE / group;
     if ((long long)q_rows / (2 * tokens) >= 1LL << (32 - SEQ_BITS) || ((long long)q_rows / (2 * tokens) + SEQS) * kv_heads > 0x7fff0000LL) return PSA_ERR_SHAPE;
@@ -874,7 +1047,7 @@ int prompt_attention(const void* Q, const void* K, const void* V, long long q_st
     maps.k = maps.v = maps.q;                    // (without keys no block of them is ever loaded)
     if (k_rows > 0 && (!key_map(&maps.k, K, k_rows, kv_heads, d, k_stride) || !key_map(&maps.v, V, k_rows, kv_heads, d, v_stride))) return PSA_ERR_CUDA;
     const PromptArgs pa = {q_starts, k_starts, sequences, q_rows, k_rows, heads, kv_heads, group, tokens, d, v_stride, static_cast<const uint16_t*>(V),
-                           static_cast<uint16_t*>(out), lse, scale * LOG2E, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)kv_heads)};
+                           static_cast<uint16_t*>(out), lse, static_cast<float*>(scratch), scale * LOG2E, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)kv_heads)};
     auto launch = [&](auto width, auto steps) {
         constexpr int D = decltype(width)::value, KS = decltype(steps)::value;
         return dtype == PSA_F16 ? launch_prompt<D, KS, true>(maps, pa, dc, cursor, dc_next, stream) : launch_prompt<D, KS, false>(maps, pa, dc, cursor, dc_next, stream);

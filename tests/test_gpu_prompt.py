@@ -188,3 +188,26 @@ def test_longer_than_one_piece():
         r = ref.attend(Q[i:i + 1], K[:i + 1], V[:i + 1], 1 / 8)
         ref.close(out[i:i + 1], None, r, BF, n, 2 * ref.UNIT[BF])
     assert math.isfinite(float(out.float().sum()))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("q,k,H,Hkv,d", [([3], [5000], 8, 1, 64), ([70, 1, 0], [3000, 1500, 900], 4, 2, 128), ([200], [2400], 1, 1, 80), ([5, 5, 5], [1025, 4000, 2], 12, 4, 128), ([260], [2200], 2, 2, 64),
+                                         ([1], [9000], 32, 8, 128), ([1500], [1400], 2, 1, 64)])
+def test_keys_in_parts(q, k, H, Hkv, d, dtype):
+    """Few rows and many keys: the key blocks are shared out among CTAs.  The result does not depend on who joins the parts."""
+    Q, K, V = _inputs(q, k, H, Hkv, d, dtype, 12)
+    want = _check(Q, K, V, q, k)
+    for _ in range(3):
+        assert torch.equal(want, psa.psa_prompt_attention(Q, K, V, ref.starts(q), ref.starts(k)))
+    K2, V2 = K.clone(), V.clone()
+    K2[k[0] - 1], V2[k[0] - 1] = float("nan"), float("nan")         # the last token of the first sequence: its last row sees it, nobody else
+    got = psa.psa_prompt_attention(Q, K2, V2, ref.starts(q), ref.starts(k))
+    same = [i for i in range(sum(q)) if i != q[0] - 1]
+    assert torch.equal(got[same], want[same]) and torch.isnan(got[q[0] - 1]).all()
+    V2.copy_(V)
+    V2[k[0] // 2, :, 1] = float("inf")
+    got = psa.psa_prompt_attention(Q, K, V2, ref.starts(q), ref.starts(k)).view(-1, H, d)
+    sees = [i for i in range(q[0]) if i + k[0] - q[0] >= k[0] // 2]
+    assert (got[sees, :, 1] == float("inf")).all()
+    got[sees, :, 1] = want.view(-1, H, d)[sees, :, 1]
+    assert torch.equal(got.view(-1, H * d), want)
