@@ -876,7 +876,7 @@ int psa_prompt_attention(const void* Q, const void* K, const void* V, long long 
                          const int* k_starts, int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d_k, float scale, int dtype, void* out,
                          float* lse, void* stream) {
     g_err_text[0] = 0;
-    if (sequences <= 0 || q_rows < 0 || k_rows < 0 || heads <= 0 || kv_heads <= 0 || d_k <= 0 || heads % kv_heads) return PSA_ERR_SHAPE;
+    if (sequences < 0 || q_rows < 0 || (sequences == 0 && q_rows > 0) || k_rows < 0 || heads <= 0 || kv_heads <= 0 || d_k <= 0 || heads % kv_heads) return PSA_ERR_SHAPE;
     if (!k_starts && k_rows != q_rows) return PSA_ERR_SHAPE;
     if (!serving_dtype(dtype) || d_k > 128 || d_k % 8 || heads / kv_heads > 128 || !good_scale(scale)) return PSA_ERR_UNSUPPORTED;
     if (q_rows == 0) return PSA_OK;
@@ -906,7 +906,7 @@ int psa_cache_append(const psa_cache* cache, const void* K, const void* V, long 
     g_err_text[0] = 0;
     const int rc = check_cache(cache);
     if (rc != PSA_OK) return rc;
-    if (sequences <= 0 || rows < 0) return PSA_ERR_SHAPE;
+    if (sequences < 0 || rows < 0 || (sequences == 0 && rows > 0)) return PSA_ERR_SHAPE;
     if (!serving_dtype(dtype)) return PSA_ERR_UNSUPPORTED;
     if (rows == 0) return PSA_OK;
     if (!K || !V || !seqs || !starts) return PSA_ERR_NULL;
@@ -925,7 +925,7 @@ int psa_cache_attention(const psa_cache* cache, const void* Q, long long q_strid
     g_err_text[0] = 0;
     const int rc = check_cache(cache);
     if (rc != PSA_OK) return rc;
-    if (sequences <= 0 || rows < 0 || heads <= 0 || heads % cache->kv_heads || max_q <= 0) return PSA_ERR_SHAPE;
+    if (sequences < 0 || rows < 0 || (sequences == 0 && rows > 0) || heads <= 0 || heads % cache->kv_heads || max_q <= 0) return PSA_ERR_SHAPE;
     if (!serving_dtype(dtype) || !good_scale(scale)) return PSA_ERR_UNSUPPORTED;
     if (rows == 0) return PSA_OK;
     if (!Q || !seqs || !q_starts || !out) return PSA_ERR_NULL;

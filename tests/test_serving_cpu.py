@@ -128,3 +128,9 @@ def test_reference_layouts_agree(d):
     ones = tuple(torch.full_like(x, 15) if i == 0 else torch.full_like(x, -1).view(torch.int16).fill_(-1).view(torch.float16) for i, x in enumerate(kq))
     assert (ref.block_images(ones, ones, 32) == 255).all()
     assert ((ref.held(*kq) - k.double()).abs().unflatten(-1, (-1, 32)).amax(-1) <= kq[1].double() / 32 * 1.001 + 2.0 ** -10 * (kq[1].double() + kq[2].double().abs())).all()
+
+
+def test_empty_batches_are_no_error(lib):
+    assert _prompt(lib, n=0, q_rows=0) == binding.OK
+    assert lib.psa_cache_append(_cache(), None, None, 128, 128, None, None, 0, 0, binding.BF16, None, None, None) == binding.OK
+    assert lib.psa_cache_attention(_cache(), None, 256, None, None, 0, 0, 4, 1, 0.1, binding.BF16, None, None, None) == binding.OK
