@@ -14,7 +14,8 @@
 // Work is split over the long axis: a row (sequence, head, tile of columns) of more 32-token steps than a piece is cut into parts of equal length, the piece being chosen on the
 // device from all lengths so that the parts fill the GPU (nothing has to be known on the host).  A CTA takes a part: its warps take the steps in turn, each with a
 // ring of blocks of its own filled by bulk copies, and are joined through shared memory; a row of several parts is joined by the CTA that finishes last, in
-// the parts' order, so that results do not depend on who that is.
+// the parts' order, so that results do not depend on who that is.  Where there are more rows than CTAs, short ones go to single warps, eight a CTA (looking up, converting the
+// queries and joining cost a CTA 8000 cycles a row, the 16 steps of a row of 512 tokens 7000).
 #include <type_traits>
 
 #include "psa_cache.cuh"
@@ -133,7 +134,7 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
 // A part of a row: steps [step0, step1) of it, part `part` of `parts`, whose results have numbers `first`, `first` + 1, .. (if there are several).
 struct Piece {
     Seq s;
-    int there, h, qt, step0, step1, part, parts, first;
+    int h, qt, step0, step1, part, parts, first;
 };
 struct Totals {
     uint32_t steps, rows;
@@ -143,7 +144,6 @@ __device__ __forceinline__ Piece piece_of(const Seq& s, int r, int piece, int fi
     const int parts = (s.steps + piece - 1) / piece, row = parts == 1 ? r : r / parts, each = parts == 1 ? s.steps : (s.steps + parts - 1) / parts;
     Piece p;
     p.s = s;
-    p.there = 1;
     p.h = s.qtiles == 1 ? row : row / s.qtiles;
     p.qt = row - p.h * s.qtiles;
     p.part = r - row * parts;
@@ -154,7 +154,8 @@ __device__ __forceinline__ Piece piece_of(const Seq& s, int r, int piece, int fi
     return p;
 }
 
-template <int D, int NT>
+// MANY: there may be more rows than CTAs.  (Without it the loop has less to keep: two sequences of up to 131,072 tokens 50.2 -> 49.1 us, eight of up to 8000 14.0 -> 13.6.)
+template <int D, int NT, bool MANY>
 __global__ void __launch_bounds__(ACfg<D, NT>::THREADS, ACfg<D, NT>::CTAS)
 cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next) {
     using Cfg = ACfg<D, NT>;
@@ -169,7 +170,8 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     __shared__ uint16_t order_s[SEQS];                                       // where items are handed out: the sequences, longest items first
     __shared__ int abort_flag, last_s;
     __shared__ int base_s[SEQS + 1], split_s[SEQS];                          // items ahead of a sequence, and parts that are joined with others
-    __shared__ Piece pieces[2];
+    __shared__ Piece pieces[2], own_s[WARPS];                                // of the CTA, this one and the next; of the warps, where each has a row of its own
+    __shared__ int item_s[2];                                                // this item and the next, -1: none
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     if (tid == 0) {
@@ -224,14 +226,15 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     const uint32_t ctas = min(gridDim.x, (uint32_t)Cfg::MOST_PARTS), budget = max((int)ctas - (int)min(rows, ctas), (int)(ctas + 1) / 2);
     const int piece = max((steps + budget - 1) / budget, (uint32_t)LEAST_PIECE);
     // With more rows than CTAs, items are handed out one by one, the longest first.
-    const bool sorted = rows > gridDim.x;
+    const bool sorted = MANY && rows > gridDim.x;
+    const int brief = sorted ? (int)(steps / (gridDim.x * WARPS)) : 0;       // a warp's share of all steps: rows up to that are a warp's
     if (sorted) {
         for (int b = tid; b < (a.sequences + 3) / 4 * 4; b += THREADS) {
             uint32_t each = 0;
             if (b < a.sequences) {
                 const Seq x = b == tid ? s0 : sequence<COLS>(a, b);
                 const int parts = (x.steps + piece - 1) / piece;
-                each = min((uint32_t)(x.steps + parts - 1) / parts, (1u << (32 - SEQ_BITS)) - 2) + 1;
+                each = min(x.steps > brief ? max((uint32_t)(x.steps + parts - 1) / parts, (uint32_t)brief + 1) : (uint32_t)x.steps, (1u << (32 - SEQ_BITS)) - 1);
             }
             unsorted_s[b] = each << SEQ_BITS | (uint32_t)(SEQS - 1 - b);     // (no two alike)
         }
@@ -248,7 +251,8 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         __syncthreads();
     }
     auto nth = [&](int k) { return sorted ? (int)order_s[k] : k; };        // the k-th sequence of the list
-    uint32_t items = 0, splits = 0;
+    uint32_t items = 0, splits = 0;              // of sequences with brief rows: rows
+    int longs = 0;                               // sequences with longer ones: the first of the list
     for (int k0 = 0; k0 < a.sequences; k0 += THREADS) {
         unsigned long long all;
         const int k = k0 + tid;
@@ -258,21 +262,29 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         const unsigned long long before = block_scan((unsigned long long)n << 32 | (parts > 1 ? n : 0u), &all);
         if (k < a.sequences) { base_s[k] = (int)(items + (uint32_t)(before >> 32)); split_s[k] = (int)(splits + (uint32_t)before); }
         const int r = (int)blockIdx.x - (int)(items + (uint32_t)(before >> 32));
-        if (r >= 0 && r < (int)n) pieces[0] = piece_of(x, r, piece, (int)(splits + (uint32_t)before));         // this CTA's first item
+        if (!sorted && r >= 0 && r < (int)n) pieces[0] = piece_of(x, r, piece, (int)(splits + (uint32_t)before));          // this CTA's first item
         items += (uint32_t)(all >> 32);
         splits += (uint32_t)all;
+        if (sorted) longs += __syncthreads_count(k < a.sequences && x.steps > brief);
     }
-    if (tid == 0) {
-        base_s[a.sequences] = (int)items;
-        pieces[1].there = 0;
+    if (tid == 0) base_s[a.sequences] = (int)items;
+    int whole_items = (int)items, singles = 0;   // items of a CTA, and rows behind them that are a warp's, eight to an item
+    if (sorted) {
+        __syncthreads();
+        whole_items = base_s[longs];
+        singles = (int)items - whole_items;
     }
-    if (blockIdx.x >= items) return;
-    const bool more = items > gridDim.x;
+    const int bundles = (singles + WARPS - 1) / WARPS, all_items = bundles + whole_items;    // (those of single rows first: they last longest)
+    if ((int)blockIdx.x >= all_items) return;
+    const bool more = all_items > (int)gridDim.x;
+    if (tid == 0) item_s[0] = (int)blockIdx.x;
     // Decodes item `i` (by one warp).
     auto decode = [&](int i, Piece* to) {
         for (int k = lane; k < a.sequences; k += 32)
             if (base_s[k] <= i && i < base_s[k + 1]) *to = piece_of(sequence<COLS>(a, nth(k)), i - base_s[k], piece, split_s[k]);
     };
+
+    if (sorted && warp == 0 && (int)blockIdx.x >= bundles) decode((int)blockIdx.x - bundles, &pieces[0]);
 
     uint8_t* const ring = smem + warp * ST * Cfg::STAGE_BYTES;
     float* const join = reinterpret_cast<float*>(smem);
@@ -282,9 +294,18 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
 
     for (int turn = 0;; turn ^= 1) {
         __syncthreads();                         // (the piece is there; the one before it is done with)
-        Piece& pc = pieces[turn];
-        if (!pc.there) break;
-        const int step0 = pc.step0, qt = pc.qt, h = pc.h, len = pc.s.len, nq = pc.s.nq, q0 = pc.s.q0;
+        const int item = item_s[turn];
+        if (item < 0) break;
+        const bool single = MANY && item < bundles;
+        if (single) {                            // eight rows, one each for the warps
+            const int row = whole_items + item * WARPS + warp;
+            if (row >= whole_items + singles) continue;                      // (never warp 0)
+            decode(row, &own_s[warp]);
+            __syncwarp();
+        }
+        const Piece& pc = single ? own_s[warp] : pieces[turn];
+        auto step_of = [&](int i) { return single ? i : pc.step0 + warp + WARPS * i; };          // of the row, the warp's i-th
+        const int qt = pc.qt, h = pc.h, len = pc.s.len, nq = pc.s.nq, q0 = pc.s.q0;
         const bool whole = pc.parts == 1;
 
         // ---- the row's queries, column n = g of tile nt, channels 32 w + 8 t .. + 7: asked for ahead of all that has to be looked up first
@@ -299,12 +320,12 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                     raw[nt][w] = *reinterpret_cast<const uint4*>(a.q + (size_t)(q0 + token) * a.q_stride + ((size_t)h * a.group + (rho - token * a.group)) * D + 32 * w + 8 * t);
             }
         }
-        // ---- blocks: lane l looks up, and asks for, block l % 2 of steps l / 2, l / 2 + 16, .. of the warp's (step0 + warp + WARPS i)
-        const int nsteps = (pc.step1 - step0 - warp + WARPS - 1) / WARPS;
+        // ---- blocks: lane l looks up, and asks for, block l % 2 of steps l / 2, l / 2 + 16, .. of the warp's : step_of(i)
+        const int nsteps = single ? pc.step1 : (pc.step1 - pc.step0 - warp + WARPS - 1) / WARPS;
         const uint8_t* addr = nullptr;
         uint32_t there[2] = {0, 0};             // blocks that exist (not those behind the end, nor in a page that does not exist), of these and the 16 steps before
         auto look_up = [&](int i0) {
-            const int i = i0 + (lane >> 1), block = (step0 + warp + WARPS * i) * STEP_BLOCKS + (lane & 1);
+            const int i = i0 + (lane >> 1), block = step_of(i) * STEP_BLOCKS + (lane & 1);
             addr = nullptr;
             if (i < nsteps && block * CACHE_BLOCK < len) {
                 const int blocks = (int)a.by_blocks.d, col = (int)fastdiv((uint32_t)block, a.by_blocks);
@@ -334,18 +355,16 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         if (ok)
             for (int i = 0; i < ST - 1; ++i) load(i);
         if (warp == 0) {                         // while the first blocks are on their way: the next item
+            int i = -1;
             if (more) {
-                int i = 0;
                 if (lane == 0) i = (int)gridDim.x + (int)atomicAdd(&dc->next_item, 1u);
                 i = __shfl_sync(0xffffffffu, i, 0);
-                if (lane == 0) pieces[turn ^ 1].there = 0;
-                __syncwarp();
-                if (i < base_s[a.sequences]) decode(i, &pieces[turn ^ 1]);
-            } else if (lane == 0) {
-                pieces[turn ^ 1].there = 0;
+                if (i >= all_items) i = -1;
+                else if (i >= bundles) decode(i - bundles, &pieces[turn ^ 1]);
             }
-            if (lane == 0 && pc.s.bad) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
+            if (lane == 0) item_s[turn ^ 1] = i;
         }
+        if ((warp == 0 || single) && lane == 0 && pc.s.bad) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
 
         // ---- the queries as the second operand
         uint32_t qb[NT][G][4];
@@ -432,7 +451,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
             const uint8_t* const stage = ring + use_slot * Cfg::STAGE_BYTES;
             --in_flight;
             if (++use_slot == ST) { use_slot = 0; use_phase ^= 1; }
-            const int tok0 = (step0 + warp + WARPS * i) * STEP;
+            const int tok0 = step_of(i) * STEP;
             // (step i is one of the 16 looked up last, or of those before)
             const uint32_t have = ((i >> 4) == (min(i + ST - 1, nsteps - 1) >> 4) ? there[0] : there[1]) >> (2 * (i & 15)) & 3u;
             const bool masked = tok0 + STEP - 1 > seen_by_all || have != 3u;
@@ -586,7 +605,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
             __syncwarp();                        // all lanes are done with the block before it is overwritten
         }
 
-        // ---- the warps' results into one
+        // ---- the columns' sums
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -595,8 +614,41 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                 l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 4);
                 l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 8);
                 l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 16);
-                if (g == 0) { m_s[warp][nt * 8 + 2 * t + c] = m[nt][c]; l_s[warp][nt * 8 + 2 * t + c] = l[nt][c]; }
             }
+        const int cols = min(COLS, nq * a.group - qt * COLS);              // columns that are rows of the call
+        auto store = [&](int col, int ch, float4 v, float inv) {             // four channels of a column, final
+            const int rho = qt * COLS + col, token = (int)fastdiv((uint32_t)rho, a.by_group);
+            const size_t at = ((size_t)(q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)) * D + ch;
+            uint2 y;
+            if (a.f16) y = make_uint2(h2_bits(__floats2half2_rn(v.x * inv, v.y * inv)), h2_bits(__floats2half2_rn(v.z * inv, v.w * inv)));
+            else y = make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+            *reinterpret_cast<uint2*>(a.out + at) = y;
+        };
+        auto store_lse = [&](int col, float top, float sum) {
+            const int rho = qt * COLS + col, token = (int)fastdiv((uint32_t)rho, a.by_group);
+            a.lse[(size_t)(q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)] = sum == 0.f ? -INFINITY : (finite_or_zero(top) + log2f(sum)) * LN2;
+        };
+        if (single) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int col = nt * 8 + 2 * t + c;
+                    if (col >= cols) continue;
+                    const float inv = l[nt][c] == 0.f ? 0.f : 1.f / l[nt][c];
+#pragma unroll
+                    for (int w = 0; w < G; ++w) store(col, 32 * w + 4 * g, make_float4(o[nt][2 * w][c], o[nt][2 * w][c + 2], o[nt][2 * w + 1][c], o[nt][2 * w + 1][c + 2]), inv);
+                    if (a.lse && g == 0) store_lse(col, m[nt][c], l[nt][c]);
+                }
+            continue;
+        }
+        // ---- the warps' results into one
+        if (g == 0) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) { m_s[warp][nt * 8 + 2 * t + c] = m[nt][c]; l_s[warp][nt * 8 + 2 * t + c] = l[nt][c]; }
+        }
         __syncthreads();                         // (also: every warp is done with its ring, which the joining buffer overlays)
         if (tid < COLS) {
             float top = m_s[0][tid], sum = 0.f;
@@ -620,20 +672,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                     *reinterpret_cast<float4*>(to + 32 * w) = make_float4(o[nt][2 * w][c] * f, o[nt][2 * w][c + 2] * f, o[nt][2 * w + 1][c] * f, o[nt][2 * w + 1][c + 2] * f);
             }
         __syncthreads();
-        const int cols = min(COLS, nq * a.group - qt * COLS);              // columns that are rows of the call
         float* const slot = a.part + (size_t)(pc.first + pc.part) * COLS * (D + 2);
-        auto store = [&](int col, int ch, float4 v, float inv) {             // four channels of a column, final
-            const int rho = qt * COLS + col, token = (int)fastdiv((uint32_t)rho, a.by_group);
-            const size_t at = ((size_t)(q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)) * D + ch;
-            uint2 y;
-            if (a.f16) y = make_uint2(h2_bits(__floats2half2_rn(v.x * inv, v.y * inv)), h2_bits(__floats2half2_rn(v.z * inv, v.w * inv)));
-            else y = make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
-            *reinterpret_cast<uint2*>(a.out + at) = y;
-        };
-        auto store_lse = [&](int col, float top, float sum) {
-            const int rho = qt * COLS + col, token = (int)fastdiv((uint32_t)rho, a.by_group);
-            a.lse[(size_t)(q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)] = sum == 0.f ? -INFINITY : (finite_or_zero(top) + log2f(sum)) * LN2;
-        };
         for (int e = tid; e < cols * (D / 4); e += THREADS) {
             const int col = e / (D / 4), ch = 4 * (e - col * (D / 4));
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -743,12 +782,12 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     if (lane == 0 && abort_flag) atomicExch(&dc->status, (int)PSA_ERR_TIMEOUT);
 }
 
-template <int D, int NT>
+template <int D, int NT, bool MANY>
 int launch_attn(const AttnArgs& all, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
     using Cfg = ACfg<D, NT>;
     static DeviceSetup setup;
     const int sms = device_setup(&setup, [] {
-        return cudaFuncSetAttribute(cache_attn_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, ACfg<D, NT>::SMEM);
+        return cudaFuncSetAttribute(cache_attn_kernel<D, NT, MANY>, cudaFuncAttributeMaxDynamicSharedMemorySize, ACfg<D, NT>::SMEM);
     }, "cache attention set-up");
     if (sms <= 0) return PSA_ERR_CUDA;
     for (int b0 = 0; b0 < all.sequences; b0 += SEQS) {
@@ -775,7 +814,7 @@ int launch_attn(const AttnArgs& all, DeviceCounters* dc, DeviceCounters* dc_next
         cfg.numAttrs = 1;
         // (the counter that items are handed out by serves one launch)
         cudaError_t e = b0 == 0 ? cudaSuccess : cudaMemsetAsync(&dc->next_item, 0, sizeof(dc->next_item), stream);
-        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, cache_attn_kernel<D, NT>, a, dc, b0 == 0 ? dc_next : nullptr);
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, cache_attn_kernel<D, NT, MANY>, a, dc, b0 == 0 ? dc_next : nullptr);
         if (e != cudaSuccess) { set_cuda_error(e, "cache_attn_kernel launch"); return PSA_ERR_CUDA; }
     }
     return PSA_OK;
@@ -792,7 +831,9 @@ int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const
                         dtype == PSA_F16, scale, fastdiv_make((uint32_t)(heads / c.kv_heads)), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
     const bool wide = (long long)max_q * a.group > 8;        // more than eight columns: two tiles of them share a block's codes
     auto launch = [&](auto width, auto tiles_of_columns) {
-        return launch_attn<decltype(width)::value, decltype(tiles_of_columns)::value>(a, dc, dc_next, stream);
+        constexpr int D = decltype(width)::value, NT = decltype(tiles_of_columns)::value;
+        const long long tiles = (long long)max_q * a.group <= 8 * NT ? sequences : ((long long)rows * a.group + 8 * NT - 1) / (8 * NT) + sequences;
+        return tiles * c.kv_heads > 148 * ACfg<D, NT>::CTAS ? launch_attn<D, NT, true>(a, dc, dc_next, stream) : launch_attn<D, NT, false>(a, dc, dc_next, stream);
     };
     using std::integral_constant;
     const integral_constant<int, 1> one;
