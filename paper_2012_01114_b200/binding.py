@@ -8,6 +8,7 @@ an explicit error.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 
 import torch
@@ -370,65 +371,35 @@ def psa_attention_sym_f32_noalloc(X, out=None, stream=None):
 
 
 # ---------------------------------------------------------------- serving
-# (On small calls the host side is what takes the time: a function call per argument costs 0.2 us, an attribute of a tensor 0.04.  The checks are
-# therefore written out where they are needed, and what is wrong is named only once something is.)
-_SERVING = {torch.bfloat16: BF16, torch.float16: F16}
-_INT = torch.int32
+# (Single-token steps are shorter than their marshalling in Python, 6 to 8 us a call: that of the serving entry points is compiled, csrc/psa_marshal.cpp.)
+MARSHAL_PATH = os.path.join(_HERE, "psa_marshal.so")
+_marshal = None
 
 
-def _bad_rows(t, name, heads, d, dtype):
-    if not t.is_cuda or t.dim() != 3 or t.dtype not in _SERVING or t.dtype is not dtype:
-        raise ValueError("%s must be a CUDA tensor [rows, heads, d_k] of bf16 or fp16, like the other operands" % name)
-    raise ValueError("%s must be [rows, %d, %d] with the heads of a row side by side" % (name, heads, d))
+def marshal():
+    """The compiled marshalling, bound to the loaded library.  Raises if it has not been built; there is no fallback."""
+    global _marshal
+    if _marshal is None:
+        if not os.path.exists(MARSHAL_PATH):
+            raise RuntimeError("psa_marshal.so is missing at %s: build it with `python -m paper_2012_01114_b200.build`; there is no fallback path" % MARSHAL_PATH)
+        spec = importlib.util.spec_from_file_location("psa_marshal", MARSHAL_PATH)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        L = lib()
+        m.bind([ctypes.cast(f, ctypes.c_void_p).value for f in (L.psa_prompt_attention, L.psa_cache_append, L.psa_cache_attention, L.psa_pages_free, L.psa_pages_fork,
+                                                                L.psa_pages_reserve, L.psa_pages_compact, L.psa_pages_copy)], PsaError)
+        _marshal = m
+    return _marshal
 
 
-def _rows(t, name, heads, d, dtype):
-    """Row stride of a [rows, heads, d] tensor whose heads lie side by side."""
-    if not t.is_cuda or t.dtype is not dtype or dtype not in _SERVING or t.dim() != 3:
-        _bad_rows(t, name, heads, d, dtype)
-    n, h, c = t.shape
-    row, head, one = t.stride()
-    if h != heads or c != d or (n and h and c and (one != 1 or (h > 1 and head != d))):
-        _bad_rows(t, name, heads, d, dtype)
-    return row if n > 1 else heads * d
-
-
-def _ints(t, name, count=None):
-    if t.dtype is not _INT or not t.is_cuda or not t.is_contiguous() or (count is not None and t.numel() != count):
-        raise ValueError("%s must be a contiguous CUDA tensor of int32%s" % (name, "" if count is None else " with %d numbers" % count))
-    return t.data_ptr()
-
-
-def _given(t, name, rows, cols, dtype):
-    if not t.is_cuda or t.dtype is not dtype or not t.is_contiguous() or t.numel() != rows * cols:
-        raise ValueError("%s must be a contiguous CUDA tensor [%d, %d] of dtype %s" % (name, rows, cols, dtype))
-    return t.data_ptr()
-
-
-def _raise(rc, where):
-    if rc != OK:
-        raise PsaError(rc, where)
+def _handle(stream):
+    return None if stream is None else stream.cuda_stream
 
 
 def psa_prompt_attention(Q, K, V, q_starts, k_starts=None, scale=None, out=None, lse=None, stream=None):
     """Causal attention over packed prompts.  Q [q_rows, heads, d], K, V [k_rows, kv_heads, d] (bf16 or fp16; rows may have a stride), q_starts, k_starts int32
     [sequences + 1] -> out [q_rows, heads * d].  k_starts None: the keys are the queries' tokens.  lse: fp32 [q_rows, heads] to be filled, or None."""
-    rows, heads, d = Q.shape
-    dtype = Q.dtype
-    k_rows, kv_heads, _ = K.shape
-    if kv_heads == 0 or heads % kv_heads or V.shape != K.shape:
-        raise ValueError("K and V must be [k_rows, kv_heads, d_k] with kv_heads a divisor of Q's heads")
-    n = q_starts.numel() - 1
-    q_stride, k_stride, v_stride = _rows(Q, "Q", heads, d, dtype), _rows(K, "K", kv_heads, d, dtype), _rows(V, "V", kv_heads, d, dtype)
-    if out is None:
-        out = Q.new_empty((rows, heads * d))
-    rc = (_lib or lib()).psa_prompt_attention(Q.data_ptr(), K.data_ptr(), V.data_ptr(), q_stride, k_stride, v_stride, _ints(q_starts, "q_starts"),
-                                              None if k_starts is None else _ints(k_starts, "k_starts", n + 1), n, rows, k_rows, heads, kv_heads, d,
-                                              d ** -0.5 if scale is None else scale, _SERVING[dtype], _given(out, "out", rows, heads * d, dtype),
-                                              None if lse is None else _given(lse, "lse", rows, heads, torch.float32), _stream(stream))
-    if rc != OK:
-        raise PsaError(rc, "psa_prompt_attention")
-    return out
+    return (_marshal or marshal()).prompt(Q, K, V, q_starts, k_starts, scale, out, lse, _handle(stream))
 
 
 def psa_prompt_workspace_bytes(sequences, q_rows, k_rows, heads, kv_heads, d_k) -> int:
@@ -448,98 +419,40 @@ def psa_pages_workspace_bytes(pages, count) -> int:
     return int(lib().psa_pages_workspace_bytes(pages, count))
 
 
-def _cache(pool, tables, lens, kv_heads, page_size, d):
-    if not pool.is_cuda or pool.dtype is not torch.uint8 or pool.dim() != 2 or not pool.is_contiguous() or tables.dim() != 2:
-        raise ValueError("pool must be a contiguous CUDA tensor [pages, page bytes] of uint8, tables [slots, width]")
-    (pages, size), (slots, width) = pool.shape, tables.shape
-    if size * 16 != kv_heads * page_size * 20 * d:
-        raise ValueError("pool pages must have psa_cache_page_bytes(%d, %d, %d) bytes" % (kv_heads, page_size, d))
-    return Cache(pool.data_ptr(), _ints(tables, "tables"), _ints(lens, "lens", slots), pages, slots, width, page_size, kv_heads, d)
-
-
 def psa_cache_append(K, V, pool, tables, lens, seqs, starts, page_size, k_held=None, v_held=None, stream=None):
     """Quantises K, V [rows, kv_heads, d] (rows may have a stride) to 4 bits and writes them as the last tokens of slots seqs, sequence b being rows starts[b] ..
-    starts[b + 1] - 1; lens includes them already.  k_held, v_held (dense, or None) receive what the cache now holds."""
-    rows, kv_heads, d = K.shape
-    dtype = K.dtype
-    if V.shape != K.shape:
-        raise ValueError("K and V must have one shape")
-    k_stride, v_stride, n = _rows(K, "K", kv_heads, d, dtype), _rows(V, "V", kv_heads, d, dtype), seqs.numel()
-    cache = _cache(pool, tables, lens, kv_heads, page_size, d)
-    rc = (_lib or lib()).psa_cache_append(cache, K.data_ptr(), V.data_ptr(), k_stride, v_stride, _ints(seqs, "seqs"), _ints(starts, "starts", n + 1), n, rows, _SERVING[dtype],
-                                          None if k_held is None else _given(k_held, "k_held", rows, kv_heads * d, dtype),
-                                          None if v_held is None else _given(v_held, "v_held", rows, kv_heads * d, dtype), _stream(stream))
-    if rc != OK:
-        raise PsaError(rc, "psa_cache_append")
+    starts[b + 1] - 1; lens includes them already.  pool: uint8 [pages, page bytes]; tables: int32 [slots, width]; lens: int32 [slots].  k_held, v_held (dense, or
+    None) receive what the cache now holds."""
+    (_marshal or marshal()).append(K, V, pool, tables, lens, seqs, starts, page_size, k_held, v_held, _handle(stream))
 
 
 def psa_cache_attention(Q, pool, tables, lens, seqs, q_starts, kv_heads, page_size, max_q=1, scale=None, out=None, lse=None, stream=None):
     """Attention of the last query tokens of slots seqs over the cache in 4 bits: Q [rows, heads, d] (rows may have a stride), sequence b owns rows q_starts[b] ..
     q_starts[b + 1] - 1 -> out [rows, heads * d].  max_q: bound on the queries of a sequence."""
-    rows, heads, d = Q.shape
-    if kv_heads <= 0 or heads % kv_heads:
-        raise ValueError("kv_heads must divide Q's heads")
-    dtype = Q.dtype
-    q_stride, n = _rows(Q, "Q", heads, d, dtype), seqs.numel()
-    cache = _cache(pool, tables, lens, kv_heads, page_size, d)
-    if out is None:
-        out = Q.new_empty((rows, heads * d))
-    rc = (_lib or lib()).psa_cache_attention(cache, Q.data_ptr(), q_stride, _ints(seqs, "seqs"), _ints(q_starts, "q_starts", n + 1), n, rows, heads, max_q,
-                                             d ** -0.5 if scale is None else scale, _SERVING[dtype], _given(out, "out", rows, heads * d, dtype),
-                                             None if lse is None else _given(lse, "lse", rows, heads, torch.float32), _stream(stream))
-    if rc != OK:
-        raise PsaError(rc, "psa_cache_attention")
-    return out
-
-
-def _pages(tables, lens, refs, page_size):
-    if tables.dim() != 2:
-        raise ValueError("tables must be [slots, width]")
-    slots, width = tables.shape
-    return Pages(_ints(tables, "tables"), None if lens is None else _ints(lens, "lens", slots), _ints(refs, "refs"), slots, width, refs.numel(), page_size)
-
-
-def _pool(t, pages):
-    """(address, page bytes, layers) of a pool [pages, page bytes] or [layers, pages, page bytes]."""
-    if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous() or t.dim() not in (2, 3) or t.shape[-2] != pages:
-        raise ValueError("a pool must be a contiguous CUDA tensor [pages, page bytes] or [layers, pages, page bytes] of uint8")
-    return t.data_ptr(), t.shape[-1], t.shape[0] if t.dim() == 3 else 1
+    return (_marshal or marshal()).attention(Q, pool, tables, lens, seqs, q_starts, kv_heads, page_size, max_q, scale, out, lse, _handle(stream))
 
 
 def psa_pages_free(tables, lens, refs, seqs, page_size, stream=None):
     """The sequences in slots seqs end: their pages lose a reference, their rows become -1, their lengths 0."""
-    _raise(lib().psa_pages_free(_pages(tables, lens, refs, page_size), _ints(seqs, "seqs"), seqs.numel(), _stream(stream)), "psa_pages_free")
+    (_marshal or marshal()).pages_free(tables, lens, refs, seqs, page_size, _handle(stream))
 
 
 def psa_pages_fork(tables, lens, refs, parents, children, page_size, stream=None):
     """Slot children[i], which holds no pages, gets the pages and the length of slot parents[i]."""
-    n = parents.numel()
-    _raise(lib().psa_pages_fork(_pages(tables, lens, refs, page_size), _ints(parents, "parents"), _ints(children, "children", n), n, _stream(stream)), "psa_pages_fork")
+    (_marshal or marshal()).pages_fork(tables, lens, refs, parents, children, page_size, _handle(stream))
 
 
 def psa_pages_reserve(tables, lens, refs, pool, seqs, add, page_size, short, stream=None):
-    """Room for add[i] more tokens of slot seqs[i]: lens grows, pages are taken, a shared last page that is written to is copied in all layers of the pool.
-    short (int32, one number): how many pages are missing; if any, nothing changes."""
-    n = seqs.numel()
-    _raise(lib().psa_pages_reserve(_pages(tables, lens, refs, page_size), *_pool(pool, refs.numel()), _ints(seqs, "seqs"), _ints(add, "add", n), n,
-                                   _ints(short, "short", 1), _stream(stream)), "psa_pages_reserve")
+    """Room for add[i] more tokens of slot seqs[i]: lens grows, pages are taken, a shared last page that is written to is copied in all layers of the pool
+    ([pages, page bytes] or [layers, pages, page bytes]).  short (int32, one number): how many pages are missing; if any, nothing changes."""
+    (_marshal or marshal()).pages_reserve(tables, lens, refs, pool, seqs, add, page_size, short, _handle(stream))
 
 
 def psa_pages_compact(tables, refs, pool, new_tables, new_refs, new_pool, live, stream=None):
     """Live pages take the first places: those beyond move into the holes before them, in order.  The new tensors may be the old ones.  live (int32, one number)."""
-    if new_tables.shape != tables.shape or new_refs.shape != refs.shape or new_pool.shape != pool.shape:
-        raise ValueError("new_tables, new_refs and new_pool must have the shapes of tables, refs and pool")
-    address, page_bytes, layers = _pool(pool, refs.numel())
-    _raise(lib().psa_pages_compact(_pages(tables, None, refs, 1), address, page_bytes, layers, _ints(new_tables, "new_tables"), _ints(new_refs, "new_refs"),
-                                   _pool(new_pool, refs.numel())[0], _ints(live, "live", 1), _stream(stream)), "psa_pages_compact")
+    (_marshal or marshal()).pages_compact(tables, refs, pool, new_tables, new_refs, new_pool, live, _handle(stream))
 
 
 def psa_pages_copy(pool, new_pool, src, dst, stream=None):
     """Page src[i] of pool to page dst[i] of new_pool (which may be the same, the lists then sharing no page), in all layers."""
-    n = src.numel()
-    address, page_bytes, layers = _pool(pool, pool.shape[-2])
-    new_address, new_bytes, new_layers = _pool(new_pool, new_pool.shape[-2])
-    if (new_bytes, new_layers) != (page_bytes, layers):
-        raise ValueError("both pools must have the same layers and page bytes")
-    _raise(lib().psa_pages_copy(address, pool.shape[-2], new_address, new_pool.shape[-2], page_bytes, layers, _ints(src, "src"), _ints(dst, "dst", n), n,
-                                _stream(stream)), "psa_pages_copy")
+    (_marshal or marshal()).pages_copy(pool, new_pool, src, dst, _handle(stream))

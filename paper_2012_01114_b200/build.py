@@ -1,8 +1,8 @@
-"""Builds libpsa.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a.
+"""Builds libpsa.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and psa_marshal.so, the compiled part of the Python binding, with g++.
 
     python -m paper_2012_01114_b200.build [--force] [--verbose]
 
-The shared object lands next to this file so that it travels with the source tree.
+The shared objects land next to this file so that they travel with the source tree.
 """
 from __future__ import annotations
 
@@ -13,6 +13,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpsa.so")
+MARSHAL = os.path.join(HERE, "psa_marshal.so")
 SOURCES = ["psa_api.cu", "psa_f32.cu", "psa_f32_tensor.cu", "psa_f32_attn_tensor.cu", "psa_gemm.cu", "psa_attn.cu", "psa_attn_persist.cu", "psa_attn_wide.cu", "psa_noalloc.cu", "psa_selftest.cu", "psa_pipes.cu", "psa_prompt.cu", "psa_cache_append.cu", "psa_cache_attn.cu", "psa_pages.cu"]
 
 
@@ -27,7 +28,31 @@ def _deps():
     return out
 
 
+def build_marshal(force: bool = False, verbose: bool = False) -> str:
+    """psa_marshal.so, against the installed torch (whose libraries are in the process when it is loaded)."""
+    source = os.path.join(CSRC, "psa_marshal.cpp")
+    newest = max(os.path.getmtime(p) for p in (source, os.path.join(os.path.dirname(HERE), "include", "psa.h")))
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= newest:
+        return MARSHAL
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    tmp = MARSHAL + ".%d.tmp" % os.getpid()
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-DTORCH_EXTENSION_NAME=psa_marshal", "-DTORCH_API_INCLUDE_EXTENSION_H",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    cmd += ["-I" + d for d in (os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"], os.path.join(cuda, "include"))]
+    cmd += ["-o", tmp, source, "-L" + os.path.join(root, "lib")] + ["-l" + n for n in ("c10", "c10_cuda", "torch_cpu", "torch", "torch_python")]
+    if verbose:
+        print(" ".join(cmd))
+    subprocess.check_call(cmd)
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_marshal(force, verbose)
     newest = max(os.path.getmtime(p) for p in _deps())
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= newest:
         return LIB
