@@ -17,6 +17,7 @@ namespace psa {
 namespace {
 
 constexpr int META_THREADS = 1024;
+constexpr int FREE_NEAR = 2048;                 // free pages of a call that are kept in shared memory
 constexpr int RESERVE_MOST = 4096;              // sequences of one call (their last pages are compared in shared memory)
 
 struct PageArgs {
@@ -86,6 +87,38 @@ __device__ __forceinline__ int cta_scan(int v, int* tmp, int* total) {
     return __shfl_sync(0xffffffffu, w, warp) - tmp[warp] + x - v;
 }
 
+// Pages are looked through 16 at a time and thread, one round of the CTA per 16,384: bit c of the result says whether `what` holds of the count of page first + c.
+constexpr int PER_THREAD = 16, ROUND = META_THREADS * PER_THREAD;
+struct Counts16 {
+    int4 c[PER_THREAD / 4];
+};
+__device__ __forceinline__ Counts16 load_counts(const int* refs, int pages, long long first) {
+    Counts16 r;
+    const bool aligned = (reinterpret_cast<uintptr_t>(refs) & 15u) == 0;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD / 4; ++i) {
+        const long long at = first + 4 * i;
+        r.c[i] = make_int4(-1, -1, -1, -1);      // (no such page: neither free nor live)
+        if (at + 3 < pages && aligned) {
+            r.c[i] = *reinterpret_cast<const int4*>(refs + at);
+        } else {
+            if (at < pages) r.c[i].x = refs[at];
+            if (at + 1 < pages) r.c[i].y = refs[at + 1];
+            if (at + 2 < pages) r.c[i].z = refs[at + 2];
+            if (at + 3 < pages) r.c[i].w = refs[at + 3];
+        }
+    }
+    return r;
+}
+template <class What>
+__device__ __forceinline__ uint32_t bits_of(const Counts16& r, What what) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD / 4; ++i)
+        m |= ((what(r.c[i].x) ? 1u : 0u) | (what(r.c[i].y) ? 2u : 0u) | (what(r.c[i].z) ? 4u : 0u) | (what(r.c[i].w) ? 8u : 0u)) << (4 * i);
+    return m;
+}
+
 // What reserve does to sequence i of the list.
 struct Need {
     int seq, held, add, have, want, last;       // last: its last page, if that is partly filled and about to be written to (else -1)
@@ -110,6 +143,7 @@ __device__ __forceinline__ Need need_of(const PageArgs& p, const int* seqs, cons
 __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageArgs p, const int* seqs, const int* add, int count, int* short_by, int* free_list,
                                                                      int2* pairs, DeviceCounters* dc, DeviceCounters* dc_next) {
     __shared__ __align__(16) int last_s[RESERVE_MOST];
+    __shared__ int free_near[FREE_NEAR];
     __shared__ int tmp[32];
     __shared__ int bad_s;
     const int tid = threadIdx.x;
@@ -117,31 +151,37 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
     grid_dependency_wait();
     next_block(dc_next);
     grid_launch_dependents();
-    for (int i = tid; i < count; i += META_THREADS) last_s[i] = need_of(p, seqs, add, i).last;
-    __syncthreads();
-    // pages that each sequence needs: those that it grows by, and one for a shared last page.  Of several in the list that share one, all but the
-    // last reference copy it, in the order of the list: the one that is left alone with the page keeps it.
+    Counts16 counts = load_counts(p.refs, p.pages, (long long)tid * PER_THREAD);         // (asked for ahead: nothing below depends on it for long)
     constexpr int PER = RESERVE_MOST / META_THREADS;
     Need n[PER];
-    int first[PER], total = 0;
-    bool copy[PER];
     bool bad = false;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int i = k * META_THREADS + tid;
         n[k] = Need{-1, 0, 0, 0, 0, -1};
-        copy[k] = false;
-        if (k * META_THREADS >= count) continue;        // (uniform)
         if (i < count) {
             n[k] = need_of(p, seqs, add, i);
             bad |= n[k].seq < 0;
-            if (n[k].seq >= 0 && n[k].last >= 0) {
-                const int refs = p.refs[n[k].last];
-                if (refs > 1) {
-                    int before = 0;
-                    for (int j = 0; j < i; ++j) before += last_s[j] == n[k].last;
-                    copy[k] = refs - before > 1;
-                }
+            last_s[i] = n[k].seq < 0 ? -1 : n[k].last;
+        }
+    }
+    __syncthreads();
+    // pages that each sequence needs: those that it grows by, and one for a shared last page.  Of several in the list that share one, all but the
+    // last reference copy it, in the order of the list: the one that is left alone with the page keeps it.
+    int first[PER], total = 0;
+    bool copy[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int i = k * META_THREADS + tid;
+        copy[k] = false;
+        first[k] = 0;
+        if (k * META_THREADS >= count) continue;        // (uniform)
+        if (i < count && n[k].seq >= 0 && n[k].last >= 0) {
+            const int refs = p.refs[n[k].last];
+            if (refs > 1) {
+                int before = 0;
+                for (int j = 0; j < i; ++j) before += last_s[j] == n[k].last;
+                copy[k] = refs - before > 1;
             }
         }
         int all;
@@ -149,27 +189,22 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
         total += all;
     }
     if (bad) bad_s = 1;
-    // ---- the first `total` pages without references, ascending
-    constexpr int CHUNK = 16;                   // per thread and round
+    // ---- the first `total` pages without references, ascending: in shared memory, those that it has no room for behind
     int found = 0;
-    for (long long at = 0; at < p.pages && found < total; at += META_THREADS * CHUNK) {
-        const long long mine = at + (long long)tid * CHUNK;
-        uint32_t is_free = 0;
-#pragma unroll
-        for (int c = 0; c < CHUNK; c += 4) {
-            if (mine + c + 3 < p.pages && (reinterpret_cast<uintptr_t>(p.refs) & 15u) == 0) {
-                const int4 r = *reinterpret_cast<const int4*>(p.refs + mine + c);
-                is_free |= (r.x == 0 ? 1u : 0u) << c | (r.y == 0 ? 2u : 0u) << c | (r.z == 0 ? 4u : 0u) << c | (r.w == 0 ? 8u : 0u) << c;
-            } else {
-                for (int e = 0; e < 4; ++e)
-                    if (mine + c + e < p.pages && p.refs[mine + c + e] == 0) is_free |= 1u << (c + e);
-            }
-        }
+    for (long long at = 0; at < p.pages && found < total; at += ROUND) {
+        const long long mine = at + (long long)tid * PER_THREAD;
+        if (at > 0) counts = load_counts(p.refs, p.pages, mine);
+        const uint32_t is_free = bits_of(counts, [](int c) { return c == 0; });
         int all, k = found + cta_scan(__popc(is_free), tmp, &all);
-        for (uint32_t m = is_free; m && k < total; m &= m - 1) free_list[k++] = (int)(mine + __ffs(m) - 1);
+        for (uint32_t m = is_free; m && k < total; m &= m - 1, ++k) {
+            const int page = (int)(mine + __ffs(m) - 1);
+            if (k < FREE_NEAR) free_near[k] = page;
+            else free_list[k] = page;
+        }
         found += all;
     }
-    __syncthreads();                            // (free_list is read by other threads of this CTA; bad_s is complete)
+    __syncthreads();                            // (the list is read by other threads of this CTA; bad_s is complete)
+    auto free_page = [&](int k) { return k < FREE_NEAR ? free_near[k] : free_list[k]; };
     const bool go = !bad_s && found >= total;
     if (tid == 0) {
         *short_by = found >= total ? 0 : total - found;
@@ -184,14 +219,14 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
             int* row = p.tables + (size_t)n[k].seq * p.width;
             int at = first[k];
             if (copy[k]) {
-                const int page = free_list[at++];
+                const int page = free_page(at++);
                 pair = make_int2(n[k].last, page);
                 row[n[k].have - 1] = page;
                 p.refs[page] = 1;
                 atomicSub(p.refs + n[k].last, 1);
             }
             for (int c = n[k].have; c < n[k].want; ++c) {
-                const int page = free_list[at++];
+                const int page = free_page(at++);
                 row[c] = page;
                 p.refs[page] = 1;
             }
@@ -255,21 +290,30 @@ __global__ void __launch_bounds__(META_THREADS) compact_map_kernel(const int* re
     grid_dependency_wait();
     next_block(dc_next);
     grid_launch_dependents();
-    int n = 0;
-    for (int i = tid; i < pages; i += META_THREADS) n += refs[i] > 0;
+    auto is_live = [](int c) { return c > 0; };
+    Counts16 counts = load_counts(refs, pages, (long long)tid * PER_THREAD);
+    int n = __popc(bits_of(counts, is_live));
+    for (long long at = ROUND; at < pages; at += ROUND) n += __popc(bits_of(load_counts(refs, pages, at + (long long)tid * PER_THREAD), is_live));
     int L;
     cta_scan(n, tmp, &L);
     int nholes = 0, nmovers = 0;
-    for (int at = 0; at < pages; at += META_THREADS) {
-        const int i = at + tid;
-        const bool is_live = i < pages && refs[i] > 0;
-        // a chunk may hold both kinds, before and behind L: counted together, holes in the low half
-        const bool hole = i < L && !is_live, mover = is_live && i >= L;
+    for (long long at = 0; at < pages; at += ROUND) {
+        const long long mine = at + (long long)tid * PER_THREAD;
+        if (at > 0) counts = load_counts(refs, pages, mine);
+        const uint32_t live_bits = bits_of(counts, is_live);
+        // pages of the thread before L: bits below `front`
+        const int front = (int)min(max((long long)L - mine, 0LL), (long long)PER_THREAD), there = (int)min(max((long long)pages - mine, 0LL), (long long)PER_THREAD);
+        const uint32_t before = (1u << front) - 1u, hole = ~live_bits & before, mover = live_bits & ~before;
+        // a round may hold both kinds: counted together, holes in the low half
         int all;
-        const int k = cta_scan((hole ? 1 : 0) | (mover ? 1 << 16 : 0), tmp, &all);
-        if (hole) holes[nholes + (k & 0xffff)] = i;
-        if (mover) movers[nmovers + (k >> 16)] = i;
-        if (i < pages && !mover) map[i] = is_live ? i : -1;
+        const int k = cta_scan(__popc(hole) | __popc(mover) << 16, tmp, &all);
+        int h = nholes + (k & 0xffff), v = nmovers + (k >> 16);
+        for (int c = 0; c < there; ++c) {
+            const int i = (int)mine + c;
+            if (hole >> c & 1u) holes[h++] = i;
+            if (mover >> c & 1u) movers[v++] = i;
+            else map[i] = live_bits >> c & 1u ? i : -1;
+        }
         nholes += all & 0xffff;
         nmovers += all >> 16;
     }
