@@ -295,6 +295,9 @@ int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
  *     launches nothing.  Device-side arguments that name no place (a sequence or page that does not exist, a token beyond the table)
  *     are left out, and psa_last_issued returns PSA_ERR_SHAPE for that call.
  *   - psa_last_issued reports these calls' status; its counts are those of psa_prompt_attention's blocks, else zero.
+ *   - Parts of long rows are joined by counts that belong to the library, one set per device: calls of psa_prompt_attention, and calls of
+ *     psa_cache_attention, must not overlap on the GPU even where each has a workspace of its own (graphs replayed on different streams without an event
+ *     between them).  After PSA_ERR_TIMEOUT the next such call is in order once psa_last_issued has reported it.
  */
 
 /*

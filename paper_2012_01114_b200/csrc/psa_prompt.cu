@@ -137,7 +137,9 @@ template <int D> __host__ __device__ constexpr int item_readers() { return (D ==
 // D: columns of a tile in shared memory, KS: 16-column steps of phase 1, and of phase 3's output, that hold columns of the head (the rest are zeros;
 // the census counts blocks, each of D columns).
 // F16: fp16 instead of bf16 in memory and as operands.
-template <int D, int KS, bool F16>
+// CUT: pairs may be cut into parts.  Calls that have pairs enough whatever the lengths are (prompt_scratch_bytes) run without: the code of the parts costs the
+// softmax warps registers (two prompts of 2737 tokens, 28 heads of d = 96: 127.3 us with it, 121.2 without; two of up to 8192, 32 heads of d = 128: 505 and 493).
+template <int D, int KS, bool F16, bool CUT>
 __global__ void __launch_bounds__(persist_threads<D>(), 1)
 prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ PromptArgs pa, DeviceCounters* dc, unsigned int* cursor, DeviceCounters* dc_next) {
     using Cfg = PCfg<D>;
@@ -289,7 +291,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     };
     const int x0 = (int)fastdiv(blockIdx.x, pa.by_heads), h0 = (int)blockIdx.x - x0 * pa.kv_heads;       // the CTA's first item
     // Fewer pairs than CTAs: their key blocks are cut into pieces of blocks / (CTAs - pairs), which makes no more parts than there are CTAs.
-    const bool cuts = pa.part && pairs > 0 && pairs <= SEQS && pairs * pa.kv_heads < (int)gridDim.x;
+    const bool cuts = CUT && pairs > 0 && pairs <= SEQS && pairs * pa.kv_heads < (int)gridDim.x;
     if (!cuts) {
         for (int k = threadIdx.x; k < pa.sequences; k += persist_threads<D>())
             if (base[k] <= x0 && x0 < base[k + 1]) { first_item = pair_behind(k, x0); first_item.h = h0; }
@@ -709,7 +711,8 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
             const int nkv = t ? work.nkv1 : work.nkv0, j0 = work.j0;
             const int vfirst = vbase + (PAIRED ? 1 : 0);
             if (max(work.nkv0, work.nkv1) > 0) vbase += max(work.nkv0, work.nkv1) + (PAIRED ? 1 : 0);
-            if (nkv == 0 && work.parts == 1) {                  // rows without keys, or no rows
+            const int parts = CUT ? work.parts : 1;
+            if (nkv == 0 && parts == 1) {                  // rows without keys, or no rows
                 const long long outA = out_row(work, rA), outB = out_row(work, rB);
                 for (int c = 8 * (lane & 3); c < pa.d; c += 32) {
                     if (outA >= 0) *reinterpret_cast<uint4*>(pa.out + outA * pa.d + c) = make_uint4(0, 0, 0, 0);
@@ -874,7 +877,6 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
                 }
             };
             bool mine = true;                                   // whether this warp stores the rows' outputs
-            const int parts = work.parts;
             // A part's sums as the warp holds them: [SUB][8][32 lanes] of four, lane by lane next to each other.
             auto part_sums = [&](int p, int u) { return reinterpret_cast<float4*>(pa.part) + ((((size_t)(work.slot + p) * 2 + t) * SOFTMAX_WARPS_PER_TILE + wq) * Cfg::SUB + u) * 256 + lane; };
             float2* const ml = reinterpret_cast<float2*>(pa.part + (size_t)2 * MAX_CTAS * 2 * TILE * D);
@@ -988,12 +990,12 @@ bool key_map(CUtensorMap* m, const void* K, int rows, int kv_heads, int d, long 
     return make_tensor_map_16bit(m, K, 3, dims, strides, box);
 }
 
-template <int D, int KS, bool F16>
+template <int D, int KS, bool F16, bool CUT>
 int launch_prompt(const PMaps& maps, const PromptArgs& all, DeviceCounters* dc, unsigned int* cursor, DeviceCounters* dc_next, cudaStream_t stream) {
     using Cfg = PCfg<D>;
     static DeviceSetup setup;
     const int sm_count = device_setup(&setup, [] {
-        return cudaFuncSetAttribute(prompt_kernel<D, KS, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, PCfg<D>::SMEM);
+        return cudaFuncSetAttribute(prompt_kernel<D, KS, F16, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, PCfg<D>::SMEM);
     }, "prompt kernel set-up");
     if (sm_count <= 0) return PSA_ERR_CUDA;
     for (int s0 = 0; s0 < all.sequences; s0 += SEQS) {
@@ -1003,7 +1005,7 @@ int launch_prompt(const PMaps& maps, const PromptArgs& all, DeviceCounters* dc, 
         pa.k_starts += s0;
         // (an upper bound: the lengths are known on the device only)
         long long items = ((long long)pa.q_rows / (2 * pa.tokens) + pa.sequences) * pa.kv_heads;
-        if (pa.part) items *= ((long long)pa.k_rows + TILE * LEAST_PIECE - 1) / (TILE * LEAST_PIECE);
+        if (CUT) items *= ((long long)pa.k_rows + TILE * LEAST_PIECE - 1) / (TILE * LEAST_PIECE);
         const int ctas = sm_count < MAX_CTAS ? sm_count : MAX_CTAS;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(items < ctas ? items : ctas));
@@ -1016,7 +1018,7 @@ int launch_prompt(const PMaps& maps, const PromptArgs& all, DeviceCounters* dc, 
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         // (the counter serves the first launch; the items of further ones go round in turn)
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, prompt_kernel<D, KS, F16>, maps, pa, dc, s0 == 0 ? cursor : nullptr, s0 == 0 ? dc_next : nullptr);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, prompt_kernel<D, KS, F16, CUT>, maps, pa, dc, s0 == 0 ? cursor : nullptr, s0 == 0 ? dc_next : nullptr);
         if (e != cudaSuccess) { set_cuda_error(e, "prompt_kernel launch"); return PSA_ERR_CUDA; }
     }
     return PSA_OK;
@@ -1050,7 +1052,8 @@ int prompt_attention(const void* Q, const void* K, const void* V, long long q_st
                            static_cast<uint16_t*>(out), lse, static_cast<float*>(scratch), scale * LOG2E, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)kv_heads)};
     auto launch = [&](auto width, auto steps) {
         constexpr int D = decltype(width)::value, KS = decltype(steps)::value;
-        return dtype == PSA_F16 ? launch_prompt<D, KS, true>(maps, pa, dc, cursor, dc_next, stream) : launch_prompt<D, KS, false>(maps, pa, dc, cursor, dc_next, stream);
+        if (scratch) return dtype == PSA_F16 ? launch_prompt<D, KS, true, true>(maps, pa, dc, cursor, dc_next, stream) : launch_prompt<D, KS, false, true>(maps, pa, dc, cursor, dc_next, stream);
+        return dtype == PSA_F16 ? launch_prompt<D, KS, true, false>(maps, pa, dc, cursor, dc_next, stream) : launch_prompt<D, KS, false, false>(maps, pa, dc, cursor, dc_next, stream);
     };
     using std::integral_constant;
     const integral_constant<int, 64> narrow;
