@@ -8,9 +8,10 @@
 //     10 d   V codes   [8 pairs of tokens][8 g][G] words: bits 4j hold channel 32 w + 4 g + j of the even token, bits 16 + 4j of the odd one
 //     18 d   V scales  [8 pairs of tokens][G] (S even, S odd, M even, M odd)
 // The words are those that a lane (g = lane / 4, t = lane % 4) of mma.m16n8k16 needs for its A operand, K with a token per row and V with a
-// channel per row, so that a lane reads its words in one piece, a word gives four operand registers with a shift and a three-way
-// logic operation each, and nothing is transposed.  Bytes still belong to one token each: appending a token touches no other.
-// A code shifted to bits 6-9 of a half and joined with 0x3c00 is the fp16 number 1 + c / 16, hence the form of the grid.
+// channel per row, so that a lane reads its words in one piece and nothing is transposed.  Bytes still belong to one token each: appending a token
+// touches no other.  K's words give four operand registers with a mask each (a code at the low end of a half is the subnormal fp16 number c 2^-24) and one
+// shift, V's with a shift, a three-way logic operation and an fma each: a code shifted to bits 6-9 and joined with 0x3c00 is the fp16 number 1 + c / 16,
+// hence the form of the grid.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -10,12 +10,18 @@
 //                            S_w sum c q / 16, and by one more product, sum_w (M_w + S_w) (sum_w q) with the sums in two fp16 numbers each.  No rounding but
 //                            that of Q to fp16, which a power of two per row keeps in range.
 //   phase 2  running maximum and sum per column, 32 tokens at a time; the maximum is raised (and sums and output rescaled) only when a score passes it by 2^8
-//   phase 3  O^T += V^T P^T  one fp16 fma per pair of codes gives v (rounded to fp16), the weights change sides by a transposing move
+//   phase 3  O^T += V^T P^T  one fp16 fma per pair of codes gives v (rounded to fp16), the weights change sides by a transposing move.  (V's codes
+//                            as the operand too, the weights times S, M by a product of its own, is 207 -> 170 instructions per block of 16 tokens and slower
+//                            all the same, 49.0 -> 52.2 us and 33.1 -> 35.8 for the calls below: more that has to wait for another; and its error is
+//                            2^-12 of a group's range instead of 2^-12 of the number.)
 // Work is split over the long axis: a row (sequence, head, tile of columns) of more 32-token steps than a piece is cut into parts of equal length, the piece being chosen on the
 // device from all lengths so that the parts fill the GPU (nothing has to be known on the host).  A CTA takes a part: its warps take the steps in turn, each with a
 // ring of blocks of its own filled by bulk copies, and are joined through shared memory; a row of several parts is joined by the CTA that finishes last, in
 // the parts' order, so that results do not depend on who that is.  Where there are more rows than CTAs, short ones go to single warps, eight a CTA (looking up, converting the
 // queries and joining cost a CTA 8000 cycles a row, the 16 steps of a row of 512 tokens 7000).
+// Measured, 32 heads on 8 of d = 128, one query each: two sequences of up to 131,072 tokens 49.0 us a call (204 MB: 4.2 TB/s; over a million tokens 5.3 TB/s, the
+// loads without the products 6.4), 64 of up to 8000 33.1 us (68 MB: 2.1 TB/s).  Bound by the issue of instructions (59 % of the slots, 48 % of the memory's rate at the
+// first size), and by what comes once a call: finding the parts 2.5 us, look-ups and queries 1.6, the CTA's join 3, the join of the parts 4 to 5.
 #include <type_traits>
 
 #include "psa_cache.cuh"

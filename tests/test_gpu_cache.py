@@ -264,3 +264,44 @@ def test_more_sequences_than_a_launch_takes():
     lens = [(i * 37) % 70 for i in range(700)]
     c = Made(lens, 1, 32, 16, 27)
     _check(c, [i % 3 for i in range(700)], 2, BF)
+
+
+def test_calls_in_a_row_in_one_graph():
+    """Each call of a graph has a status and work counter of its own, clear at every replay, whatever ran in between; other calls of the library among them."""
+    c = Made([100, 3000], 2, 64, 16, 29)
+    starts = ref.starts([70, 130])
+    Q, K, V = _queries(200, 8, 64, BF), _queries(200, 2, 64, BF, 1), _queries(200, 2, 64, BF, 2)
+    Q1, one = _queries(2, 8, 64, BF, 4), ref.starts([1, 1])
+    X = _queries(1, 256, 128, BF, 5).view(1, 256, 2, 64)
+    outs = [torch.empty(200, 512, dtype=BF, device="cuda") for _ in range(3)] + [torch.empty(2, 512, dtype=BF, device="cuda") for _ in range(3)]
+
+    def calls():
+        psa.psa_prompt_attention(Q, K, V, starts, out=outs[0])
+        psa.psa_prompt_attention(Q, K, V, starts, out=outs[1])
+        psa.psa_cache_attention(Q1, c.pool, c.tables, c.lens, c.seqs, one, 2, 16, out=outs[3])
+        psa.psa_attention_core(X, X, X, psa.MASKED)
+        psa.psa_prompt_attention(Q, K, V, starts, out=outs[2])
+        psa.psa_cache_attention(Q1, c.pool, c.tables, c.lens, c.seqs, one, 2, 16, out=outs[4])
+        psa.psa_cache_attention(Q1, c.pool, c.tables, c.lens, c.seqs, one, 2, 16, out=outs[5])
+
+    calls()
+    want = [o.clone() for o in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    place = c.tables[c.slot[1], 3].clone()
+    for bad in (False, True, False, True, True, False):
+        c.tables[c.slot[1], 3] = -1 if bad else place
+        for o in outs:
+            o.fill_(7)
+        graph.replay()
+        assert psa.psa_last_issued()[0] == (psa.ERR_SHAPE if bad else psa.OK)
+        if not bad:
+            assert all(torch.equal(a, b) for a, b in zip(outs, want))
+        graph.replay()
+        torch.cuda.synchronize()
+        c.tables[c.slot[1], 3] = place
+        psa.psa_cache_attention(Q1, c.pool, c.tables, c.lens, c.seqs, one, 2, 16)
+        assert psa.psa_last_issued()[0] == psa.OK
+        with torch.cuda.graph(graph := torch.cuda.CUDAGraph()):        # (a capture of its own starts clear as well)
+            calls()
