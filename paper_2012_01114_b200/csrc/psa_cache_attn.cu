@@ -39,6 +39,7 @@ constexpr float RAISE = 8.f;                    // log2 units, see phase 2
 constexpr int STEP_BLOCKS = 2, STEP = STEP_BLOCKS * CACHE_BLOCK;              // blocks and tokens of a step
 constexpr int MAX_CTAS = 148 * 4 + 64;          // partial results and arrival counts: two per CTA
 constexpr int SEQ_BITS = 9, SEQS = 1 << SEQ_BITS;                            // sequences of one launch
+constexpr int BRIEFS = 4;                       // see `brief`
 constexpr int LEAST_PIECE = 16;                 // steps: a row is not cut into less (joining parts costs about as much)
 
 template <int D, int NT>
@@ -172,6 +173,8 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     __shared__ float m_s[WARPS][COLS], l_s[WARPS][COLS], top_s[COLS], sum_s[COLS];
     __shared__ unsigned long long scan_s[WARPS];
     __shared__ Totals total_s[WARPS];
+    __shared__ uint32_t briefs_s[2 * BRIEFS];
+    __shared__ uint2 seq_s[MANY ? SEQS : 1];     // of the sequences: steps and tiles of columns of a row; then steps of an item, and items of a head * 2 + whether rows are cut
     __shared__ __align__(16) uint32_t unsorted_s[SEQS];                      // steps of a sequence's items << SEQ_BITS | SEQS - 1 - sequence
     __shared__ uint16_t order_s[SEQS];                                       // where items are handed out: the sequences, longest items first
     __shared__ int abort_flag, last_s;
@@ -180,6 +183,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     __shared__ int item_s[2];                                                // this item and the next, -1: none
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    if (tid < 2 * BRIEFS) briefs_s[tid] = 0;
     if (tid == 0) {
         abort_flag = 0;
         for (int w = 0; w < WARPS; ++w)
@@ -214,6 +218,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         const Seq x = sequence<COLS>(a, b);
         descends |= a.q_starts[b + 1] < a.q_starts[b];
         if (b == tid) s0 = x;
+        if (MANY) seq_s[b] = make_uint2((uint32_t)x.steps, (uint32_t)x.qtiles);
         const uint32_t r = (uint32_t)x.qtiles * a.kv_heads;
         steps += r * x.steps;
         rows += r;
@@ -233,15 +238,37 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     const int piece = max((steps + budget - 1) / budget, (uint32_t)LEAST_PIECE);
     // With more rows than CTAs, items are handed out one by one, the longest first.
     const bool sorted = MANY && rows > gridDim.x;
-    const int brief = sorted ? (int)(steps / (gridDim.x * WARPS)) : 0;       // a warp's share of all steps: rows up to that are a warp's
+    // Rows up to `brief` steps are a warp's, eight to an item: a warp's share of all steps, or the first of 1, 2, 4 and 8 with which the CTAs need one item each, else 8.
+    // (A CTA takes as long for a row of a step as a warp takes for 16 steps; but a row that has a CTA of its own is done sooner.  us a call, by share alone, with at least 1, 4
+    // and 8, and so, one query, 32 heads on 8 of d = 128: 64 sequences of up to 300 tokens 16.0 10.8 14.2 18.8 11.1, 40 of up to 600 17.8 13.1 16.0 19.7 13.6, 256 of up to 100
+    // 22.6 22.7 16.4 16.4 16.7, 64 of up to 8000 33.2 33.1 32.8 32.7 32.6.)
+    int brief = 0;
     if (sorted) {
-        for (int b = tid; b < (a.sequences + 3) / 4 * 4; b += THREADS) {
-            uint32_t each = 0;
-            if (b < a.sequences) {
-                const Seq x = b == tid ? s0 : sequence<COLS>(a, b);
-                const int parts = (x.steps + piece - 1) / piece;
-                each = min(x.steps > brief ? max((uint32_t)(x.steps + parts - 1) / parts, (uint32_t)brief + 1) : (uint32_t)x.steps, (1u << (32 - SEQ_BITS)) - 1);
+        brief = (int)(steps / (gridDim.x * WARPS));
+        uint32_t count[2 * BRIEFS] = {};         // rows up to 2^k steps, and parts of longer ones
+        for (int b = tid; b < a.sequences; b += THREADS) {
+            const uint2 x = seq_s[b];
+            const uint32_t parts = (x.x + piece - 1) / (uint32_t)piece, each = parts == 1 ? x.x : (x.x + parts - 1) / parts, n = x.y * parts;
+            seq_s[b] = make_uint2(each, n << 1 | (parts > 1));              // (parts are longer than half a piece, and so than `brief`)
+#pragma unroll
+            for (int k = 0; k < BRIEFS; ++k) { count[k] += each <= 1u << k ? n : 0u; count[BRIEFS + k] += each <= 1u << k ? 0u : n; }
+        }
+        if (brief < 1 << (BRIEFS - 1)) {
+#pragma unroll
+            for (int k = 0; k < 2 * BRIEFS; ++k) {
+                const uint32_t all = __reduce_add_sync(0xffffffffu, count[k]);
+                if (lane == k) count[0] = all;
             }
+            if (lane < 2 * BRIEFS) atomicAdd(&briefs_s[lane], count[0]);
+            __syncthreads();
+            int first = 1 << (BRIEFS - 1);
+#pragma unroll
+            for (int k = BRIEFS - 2; k >= 0; --k)
+                if ((briefs_s[k] * a.kv_heads + WARPS - 1) / WARPS + briefs_s[BRIEFS + k] * a.kv_heads <= gridDim.x) first = 1 << k;
+            brief = max(brief, first);
+        }
+        for (int b = tid; b < (a.sequences + 3) / 4 * 4; b += THREADS) {
+            const uint32_t each = b < a.sequences ? min(seq_s[b].x, (1u << (32 - SEQ_BITS)) - 1) : 0u;
             unsorted_s[b] = each << SEQ_BITS | (uint32_t)(SEQS - 1 - b);     // (no two alike)
         }
         __syncthreads();
@@ -263,15 +290,27 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         unsigned long long all;
         const int k = k0 + tid;
         Seq x = s0;
-        if ((k0 > 0 || sorted) && k < a.sequences) x = sequence<COLS>(a, nth(k));
-        const uint32_t parts = (x.steps + piece - 1) / piece, n = k < a.sequences ? (uint32_t)x.qtiles * a.kv_heads * parts : 0u;
-        const unsigned long long before = block_scan((unsigned long long)n << 32 | (parts > 1 ? n : 0u), &all);
+        uint32_t n = 0, cut = 0, each = 0;       // items, those of several parts a row, steps of one
+        if (sorted) {
+            if (k < a.sequences) {
+                const uint2 y = seq_s[order_s[k]];
+                each = y.x;
+                n = (y.y >> 1) * a.kv_heads;
+                cut = y.y & 1 ? n : 0u;
+            }
+        } else if (k < a.sequences) {
+            if (k0 > 0) x = sequence<COLS>(a, k);
+            const uint32_t parts = (uint32_t)(x.steps + piece - 1) / (uint32_t)piece;
+            n = (uint32_t)x.qtiles * a.kv_heads * parts;
+            cut = parts > 1 ? n : 0u;
+        }
+        const unsigned long long before = block_scan((unsigned long long)n << 32 | cut, &all);
         if (k < a.sequences) { base_s[k] = (int)(items + (uint32_t)(before >> 32)); split_s[k] = (int)(splits + (uint32_t)before); }
         const int r = (int)blockIdx.x - (int)(items + (uint32_t)(before >> 32));
         if (!sorted && r >= 0 && r < (int)n) pieces[0] = piece_of(x, r, piece, (int)(splits + (uint32_t)before));          // this CTA's first item
         items += (uint32_t)(all >> 32);
         splits += (uint32_t)all;
-        if (sorted) longs += __syncthreads_count(k < a.sequences && x.steps > brief);
+        if (sorted) longs += __syncthreads_count((int)each > brief);
     }
     if (tid == 0) base_s[a.sequences] = (int)items;
     int whole_items = (int)items, singles = 0;   // items of a CTA, and rows behind them that are a warp's, eight to an item

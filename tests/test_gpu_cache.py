@@ -305,3 +305,11 @@ def test_calls_in_a_row_in_one_graph():
         assert psa.psa_last_issued()[0] == psa.OK
         with torch.cuda.graph(graph := torch.cuda.CUDAGraph()):        # (a capture of its own starts clear as well)
             calls()
+
+
+@pytest.mark.parametrize("d,longest,n", [(128, 32, 120), (128, 70, 160), (64, 300, 90), (96, 6, 87), (256, 150, 90), (128, 900, 60)])
+def test_batches_with_more_rows_than_ctas(d, longest, n):
+    """Rows of 1, 2, .. steps, one to a warp or to a CTA by how many there are of each."""
+    g = torch.Generator().manual_seed(n)
+    lens = [longest] + [int(longest ** float(torch.rand(1, generator=g))) for _ in range(n - 1)]
+    _check(Made(lens, 8 if d < 256 else 4, d, 32, 30), [1 + i % 2 for i in range(n)], 2, HF)
