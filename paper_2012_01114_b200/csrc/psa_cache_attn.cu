@@ -40,6 +40,7 @@ constexpr int STEP_BLOCKS = 2, STEP = STEP_BLOCKS * CACHE_BLOCK;              //
 constexpr int MAX_CTAS = 148 * 4 + 64;          // partial results and arrival counts: two per CTA
 constexpr int SEQ_BITS = 9, SEQS = 1 << SEQ_BITS;                            // sequences of one launch
 constexpr int BRIEFS = 4;                       // see `brief`
+constexpr int LONG_PIECE = 48;                  // see `crowded`
 constexpr int LEAST_PIECE = 16;                 // steps: a row is not cut into less (joining parts costs about as much)
 
 template <int D, int NT>
@@ -161,7 +162,7 @@ __device__ __forceinline__ Piece piece_of(const Seq& s, int r, int piece, int fi
     return p;
 }
 
-// MANY: there may be more rows than CTAs.  (Without it the loop has less to keep: two sequences of up to 131,072 tokens 50.2 -> 49.1 us, eight of up to 8000 14.0 -> 13.6.)
+// MANY: there may be more items than CTAs, that is, rows by more than a half (parts are no more than CTAs by a half).  (Without it the loop has less to keep: two sequences of up to 131,072 tokens 50.2 -> 49.1 us, eight of up to 8000 14.0 -> 13.6.)
 template <int D, int NT, bool MANY>
 __global__ void __launch_bounds__(ACfg<D, NT>::THREADS, ACfg<D, NT>::CTAS)
 cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next) {
@@ -233,17 +234,21 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     steps = rows = 0;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) { steps += total_s[w].steps; rows += total_s[w].rows; }
-    // Rows cut into pieces of steps / (CTAs - rows) make no more parts than there are CTAs; where rows alone are that many, long ones are still cut.
-    const uint32_t ctas = min(gridDim.x, (uint32_t)Cfg::MOST_PARTS), budget = max((int)ctas - (int)min(rows, ctas), (int)(ctas + 1) / 2);
-    const int piece = max((steps + budget - 1) / budget, (uint32_t)LEAST_PIECE);
-    // With more rows than CTAs, items are handed out one by one, the longest first.
-    const bool sorted = MANY && rows > gridDim.x;
+    // Rows cut into pieces of steps / (CTAs - rows) make no more parts than there are CTAs.  Where rows alone are that many, or leave so few CTAs that pieces get long, they are
+    // cut into more parts than that, and items are handed out one by one, the longest first.  (us a call, one query, 32 heads on 8 of d = 128, by the first rule alone and so:
+    // 30 sequences of up to 8000 tokens 39.3 and 28.1, 32 of up to 2000 20.3 and 15.9; what looking costs where pieces are short: 20 of up to 4000 13.0 and 13.7.)
+    const uint32_t ctas = min(gridDim.x, (uint32_t)Cfg::MOST_PARTS), half = (ctas + 1) / 2;
+    auto piece_of_budget = [&](uint32_t budget) { return (int)max((steps + budget - 1) / budget, (uint32_t)LEAST_PIECE); };
+    int piece = piece_of_budget(rows < ctas ? ctas - rows : half);
+    const bool crowded = MANY && (rows >= ctas || (rows > half && piece > LONG_PIECE));
+    if (crowded) piece = piece_of_budget(half);
+    bool sorted = MANY && rows > gridDim.x;
     // Rows up to `brief` steps are a warp's, eight to an item: a warp's share of all steps, or the first of 1, 2, 4 and 8 with which the CTAs need one item each, else 8.
     // (A CTA takes as long for a row of a step as a warp takes for 16 steps; but a row that has a CTA of its own is done sooner.  us a call, by share alone, with at least 1, 4
     // and 8, and so, one query, 32 heads on 8 of d = 128: 64 sequences of up to 300 tokens 16.0 10.8 14.2 18.8 11.1, 40 of up to 600 17.8 13.1 16.0 19.7 13.6, 256 of up to 100
-    // 22.6 22.7 16.4 16.4 16.7, 64 of up to 8000 33.2 33.1 32.8 32.7 32.6.)
+    // 22.6 22.7 16.4 16.4 16.6, 64 of up to 8000 33.2 33.1 32.8 32.7 32.6.)
     int brief = 0;
-    if (sorted) {
+    if (crowded) {
         brief = (int)(steps / (gridDim.x * WARPS));
         uint32_t count[2 * BRIEFS] = {};         // rows up to 2^k steps, and parts of longer ones
         for (int b = tid; b < a.sequences; b += THREADS) {
@@ -253,7 +258,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
 #pragma unroll
             for (int k = 0; k < BRIEFS; ++k) { count[k] += each <= 1u << k ? n : 0u; count[BRIEFS + k] += each <= 1u << k ? 0u : n; }
         }
-        if (brief < 1 << (BRIEFS - 1)) {
+        if (!sorted || brief < 1 << (BRIEFS - 1)) {
 #pragma unroll
             for (int k = 0; k < 2 * BRIEFS; ++k) {
                 const uint32_t all = __reduce_add_sync(0xffffffffu, count[k]);
@@ -261,12 +266,15 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
             }
             if (lane < 2 * BRIEFS) atomicAdd(&briefs_s[lane], count[0]);
             __syncthreads();
+            sorted = (briefs_s[0] + briefs_s[BRIEFS]) * a.kv_heads > gridDim.x;
             int first = 1 << (BRIEFS - 1);
 #pragma unroll
             for (int k = BRIEFS - 2; k >= 0; --k)
                 if ((briefs_s[k] * a.kv_heads + WARPS - 1) / WARPS + briefs_s[BRIEFS + k] * a.kv_heads <= gridDim.x) first = 1 << k;
             brief = max(brief, first);
         }
+    }
+    if (sorted) {
         for (int b = tid; b < (a.sequences + 3) / 4 * 4; b += THREADS) {
             const uint32_t each = b < a.sequences ? min(seq_s[b].x, (1u << (32 - SEQ_BITS)) - 1) : 0u;
             unsorted_s[b] = each << SEQ_BITS | (uint32_t)(SEQS - 1 - b);     // (no two alike)
@@ -878,7 +886,7 @@ int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const
     auto launch = [&](auto width, auto tiles_of_columns) {
         constexpr int D = decltype(width)::value, NT = decltype(tiles_of_columns)::value;
         const long long tiles = (long long)max_q * a.group <= 8 * NT ? sequences : ((long long)rows * a.group + 8 * NT - 1) / (8 * NT) + sequences;
-        return tiles * c.kv_heads > 148 * ACfg<D, NT>::CTAS ? launch_attn<D, NT, true>(a, dc, dc_next, stream) : launch_attn<D, NT, false>(a, dc, dc_next, stream);
+        return 2 * tiles * c.kv_heads > 148 * ACfg<D, NT>::CTAS ? launch_attn<D, NT, true>(a, dc, dc_next, stream) : launch_attn<D, NT, false>(a, dc, dc_next, stream);
     };
     using std::integral_constant;
     const integral_constant<int, 1> one;

@@ -307,8 +307,8 @@ def test_calls_in_a_row_in_one_graph():
             calls()
 
 
-@pytest.mark.parametrize("d,longest,n", [(128, 32, 120), (128, 70, 160), (64, 300, 90), (96, 6, 87), (256, 150, 90), (128, 900, 60)])
-def test_batches_with_more_rows_than_ctas(d, longest, n):
+@pytest.mark.parametrize("d,longest,n", [(128, 32, 120), (128, 70, 160), (64, 300, 90), (96, 6, 87), (256, 150, 90), (128, 900, 60), (128, 6000, 30), (64, 3000, 36)])
+def test_batches_of_about_as_many_rows_as_ctas_and_more(d, longest, n):
     """Rows of 1, 2, .. steps, one to a warp or to a CTA by how many there are of each."""
     g = torch.Generator().manual_seed(n)
     lens = [longest] + [int(longest ** float(torch.rand(1, generator=g))) for _ in range(n - 1)]
