@@ -41,7 +41,9 @@ constexpr int MAX_CTAS = 148 * 4 + 64;          // partial results and arrival c
 constexpr int SEQ_BITS = 9, SEQS = 1 << SEQ_BITS;                            // sequences of one launch
 constexpr int BRIEFS = 4;                       // see `brief`
 constexpr int LONG_PIECE = 48;                  // see `crowded`
-constexpr int LEAST_PIECE = 16;                 // steps: a row is not cut into less (joining parts costs about as much)
+// Steps: a row up to LEAST_CUT is not cut, longer ones not into less than LEAST_PIECE.  (One sequence, 32 heads on 8 of d = 128 / 8 on 2 of 64, whole and in parts of 16: 600 tokens
+// 9.4 10.6 / 7.4 9.1 us, 1000 11.2 11.1 / 8.7 9.4, 1300 13.5 11.0 / 10.1 9.4, 4000 26.7 11.1 / 19.9 9.4; in parts of 32: 13.8 / 11.5.)
+constexpr int LEAST_CUT = 32, LEAST_PIECE = 16;
 
 template <int D, int NT>
 struct ACfg {
@@ -147,9 +149,10 @@ struct Piece {
 struct Totals {
     uint32_t steps, rows;
 };
+__device__ __forceinline__ int parts_of(int steps, int piece) { return steps <= LEAST_CUT ? 1 : (int)((uint32_t)(steps + piece - 1) / (uint32_t)piece); }
 // Item `r` of a sequence whose rows are cut into pieces of at most `piece` steps.
 __device__ __forceinline__ Piece piece_of(const Seq& s, int r, int piece, int first) {
-    const int parts = (s.steps + piece - 1) / piece, row = parts == 1 ? r : r / parts, each = parts == 1 ? s.steps : (s.steps + parts - 1) / parts;
+    const int parts = parts_of(s.steps, piece), row = parts == 1 ? r : r / parts, each = parts == 1 ? s.steps : (s.steps + parts - 1) / parts;
     Piece p;
     p.s = s;
     p.h = s.qtiles == 1 ? row : row / s.qtiles;
@@ -253,7 +256,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         uint32_t count[2 * BRIEFS] = {};         // rows up to 2^k steps, and parts of longer ones
         for (int b = tid; b < a.sequences; b += THREADS) {
             const uint2 x = seq_s[b];
-            const uint32_t parts = (x.x + piece - 1) / (uint32_t)piece, each = parts == 1 ? x.x : (x.x + parts - 1) / parts, n = x.y * parts;
+            const uint32_t parts = (uint32_t)parts_of((int)x.x, piece), each = parts == 1 ? x.x : (x.x + parts - 1) / parts, n = x.y * parts;
             seq_s[b] = make_uint2(each, n << 1 | (parts > 1));              // (parts are longer than half a piece, and so than `brief`)
 #pragma unroll
             for (int k = 0; k < BRIEFS; ++k) { count[k] += each <= 1u << k ? n : 0u; count[BRIEFS + k] += each <= 1u << k ? 0u : n; }
@@ -308,7 +311,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
             }
         } else if (k < a.sequences) {
             if (k0 > 0) x = sequence<COLS>(a, k);
-            const uint32_t parts = (uint32_t)(x.steps + piece - 1) / (uint32_t)piece;
+            const uint32_t parts = (uint32_t)parts_of(x.steps, piece);
             n = (uint32_t)x.qtiles * a.kv_heads * parts;
             cut = parts > 1 ? n : 0u;
         }
