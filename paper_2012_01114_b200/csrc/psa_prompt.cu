@@ -8,6 +8,7 @@
 //   * A row tile holds the queries of all heads of a group: row r is token r / group, head r % group of the group, 128 / group tokens a tile (one box of the
 //     query's tensor map).  Keys and values are loaded once for the group, short prompts fill tiles, and any group size works alike; groups that do not divide
 //     128 leave up to 7 % of the rows empty.
+//   * Where there are CTAs enough and little to do, an item is one row tile and not two (launch_prompt).
 //   * The host does not know the lengths.  Every CTA derives the work list from `starts` by itself (sequences sorted by length in shared memory): the heaviest pairs of row
 //     tiles of all sequences first, heads innermost, taken from a device counter, as in attn_persist_kernel.
 //   * Where the pairs of row tiles are fewer than the CTAs (a few prompts, or pieces of them, behind long contexts) their key blocks are cut into parts as well: a warp then
@@ -54,6 +55,7 @@ constexpr int LEAST_PIECE = 4;          // key blocks: what storing and joining 
 struct PromptArgs {
     const int *q_starts, *k_starts;
     int sequences, q_rows, k_rows, heads, kv_heads, group, tokens, d;     // tokens: of a row tile, 128 / group
+    int tiles;                          // row tiles of an item: 2, or 1 (see launch_prompt)
     long long v_stride;
     const uint16_t* v;                  // (the epilogue's look at values that are not finite)
     uint16_t* out;
@@ -61,7 +63,7 @@ struct PromptArgs {
     float sl2;
     FastDiv by_group, by_heads;
 };
-// A work item: two row tiles of one sequence and key/value head.
+// A work item: two row tiles (or one, PromptArgs::tiles) of one sequence and key/value head.
 struct __align__(16) Item {
     int q0, k0;                         // first rows of the sequence
     int i0, nq, nk;                     // first token of the first tile, lengths
@@ -212,7 +214,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     uint32_t* const unsorted = reinterpret_cast<uint32_t*>(base);
     for (int i = threadIdx.x; i < (pa.sequences + 3) / 4 * 4; i += persist_threads<D>()) {
         const int nq = i < pa.sequences ? max(starts_s[0][i + 1] - starts_s[0][i], 0) : 0;
-        unsorted[i] = i < pa.sequences ? (uint32_t)((nq + 2 * pa.tokens - 1) / (2 * pa.tokens)) << SEQ_BITS | (uint32_t)(SEQS - 1 - i) : 0u;
+        unsorted[i] = i < pa.sequences ? (uint32_t)((nq + pa.tiles * pa.tokens - 1) / (pa.tiles * pa.tokens)) << SEQ_BITS | (uint32_t)(SEQS - 1 - i) : 0u;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < pa.sequences; i += persist_threads<D>()) {     // as many places down as there are larger ones (no two are alike)
@@ -243,7 +245,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
         }
         if (lane == 0) {
             // (more rows than there are: `starts` that do not ascend; nothing is computed, and the call reports it)
-            const bool bad = sum > pa.q_rows / (2 * pa.tokens) + pa.sequences;
+            const bool bad = sum > pa.q_rows / (pa.tiles * pa.tokens) + pa.sequences;
             if (bad) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
             base[pa.sequences] = bad ? 0 : (int)sum;
         }
@@ -261,11 +263,11 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
         Item w;
         w.q0 = starts_s[0][b]; w.k0 = starts_s[1][b];
         w.nq = starts_s[0][b + 1] - w.q0; w.nk = max(starts_s[1][b + 1] - w.k0, 0);
-        w.i0 = 2 * level * pa.tokens;
+        w.i0 = pa.tiles * level * pa.tokens;
         // blocks up to the last key that the tile's last row sees
         auto blocks = [&](int i0) { return i0 >= w.nq ? 0 : max(min(i0 + pa.tokens, w.nq) + w.nk - w.nq + TILE - 1, 0) / TILE; };
         w.nkv0 = blocks(w.i0);
-        w.nkv1 = blocks(w.i0 + pa.tokens);
+        w.nkv1 = pa.tiles == 2 ? blocks(w.i0 + pa.tokens) : 0;
         w.h = w.j0 = w.slot = w.part = 0;
         w.parts = 1;
         return w;
@@ -702,7 +704,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
         // Output rows of this thread's two rows (rows as tokens of a tile and heads of a group), -1 for a row of the tile that is none of the sequence's.
         auto out_row = [&](const Item& w, int r) -> long long {
             const int tok = (int)fastdiv((uint32_t)r, pa.by_group), i = w.i0 + t * pa.tokens + tok;
-            return tok < pa.tokens && i < w.nq ? (long long)(w.q0 + i) * pa.heads + w.h * pa.group + (r - tok * pa.group) : -1;
+            return tok < pa.tokens && t < pa.tiles && i < w.nq ? (long long)(w.q0 + i) * pa.heads + w.h * pa.group + (r - tok * pa.group) : -1;
         };
         uint32_t it = 0;
         int head = take_item(it++);
@@ -712,7 +714,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
             const int vfirst = vbase + (PAIRED ? 1 : 0);
             if (max(work.nkv0, work.nkv1) > 0) vbase += max(work.nkv0, work.nkv1) + (PAIRED ? 1 : 0);
             const int parts = CUT ? work.parts : 1;
-            if (nkv == 0 && parts == 1) {                  // rows without keys, or no rows
+            if (nkv == 0 && (parts == 1 || t >= pa.tiles || work.i0 + t * pa.tokens >= work.nq)) {         // rows without keys, or no rows
                 const long long outA = out_row(work, rA), outB = out_row(work, rB);
                 for (int c = 8 * (lane & 3); c < pa.d; c += 32) {
                     if (outA >= 0) *reinterpret_cast<uint4*>(pa.out + outA * pa.d + c) = make_uint4(0, 0, 0, 0);
@@ -1004,9 +1006,15 @@ int launch_prompt(const PMaps& maps, const PromptArgs& all, DeviceCounters* dc, 
         pa.q_starts += s0;
         pa.k_starts += s0;
         // (an upper bound: the lengths are known on the device only)
-        long long items = ((long long)pa.q_rows / (2 * pa.tokens) + pa.sequences) * pa.kv_heads;
-        if (CUT) items *= ((long long)pa.k_rows + TILE * LEAST_PIECE - 1) / (TILE * LEAST_PIECE);
+        // Two tiles a CTA keep the tensor pipe busier (3560 cycles a pair of key blocks of d = 128), one alone is done sooner: each has a CTA of its own where there are CTAs
+        // enough and little to do for each, by what the host knows (that is, sequences of one length).  (us, two and one, 32 heads on 8 of d = 128: 256 tokens 14.2 12.1,
+        // 512 18.2 15.9, 512 behind 500 26.8 23.9, 128 behind 4000 39.6 34.5, 64 behind 8000 50.9 41.4, with 7 blocks a CTA; 512 behind 1000 33.4 32.6, behind 2000
+        // 40.9 46.8, 256 behind 4000 41.5 46.9, with 10, 17 and 14.)
         const int ctas = sm_count < MAX_CTAS ? sm_count : MAX_CTAS;
+        const long long blocks = (long long)pa.q_rows * pa.kv_heads / pa.tokens * ((pa.k_rows / pa.sequences + TILE - 1) / TILE);
+        pa.tiles = ((long long)pa.q_rows / pa.tokens + pa.sequences) * pa.kv_heads <= ctas && blocks <= 8 * ctas ? 1 : 2;
+        long long items = ((long long)pa.q_rows / (pa.tiles * pa.tokens) + pa.sequences) * pa.kv_heads;
+        if (CUT) items *= ((long long)pa.k_rows + TILE * LEAST_PIECE - 1) / (TILE * LEAST_PIECE);
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(items < ctas ? items : ctas));
         cfg.blockDim = dim3(persist_threads<D>());
@@ -1048,7 +1056,7 @@ int prompt_attention(const void* Q, const void* K, const void* V, long long q_st
     if (!query_map(&maps.q, Q, q_rows, kv_heads, group, d, q_stride, tokens)) return PSA_ERR_CUDA;
     maps.k = maps.v = maps.q;                    // (without keys no block of them is ever loaded)
     if (k_rows > 0 && (!key_map(&maps.k, K, k_rows, kv_heads, d, k_stride) || !key_map(&maps.v, V, k_rows, kv_heads, d, v_stride))) return PSA_ERR_CUDA;
-    const PromptArgs pa = {q_starts, k_starts, sequences, q_rows, k_rows, heads, kv_heads, group, tokens, d, v_stride, static_cast<const uint16_t*>(V),
+    const PromptArgs pa = {q_starts, k_starts, sequences, q_rows, k_rows, heads, kv_heads, group, tokens, d, 2, v_stride, static_cast<const uint16_t*>(V),
                            static_cast<uint16_t*>(out), lse, static_cast<float*>(scratch), scale * LOG2E, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)kv_heads)};
     auto launch = [&](auto width, auto steps) {
         constexpr int D = decltype(width)::value, KS = decltype(steps)::value;

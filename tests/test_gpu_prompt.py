@@ -211,3 +211,11 @@ def test_keys_in_parts(q, k, H, Hkv, d, dtype):
     assert (got[sees, :, 1] == float("inf")).all()
     got[sees, :, 1] = want.view(-1, H, d)[sees, :, 1]
     assert torch.equal(got.view(-1, H * d), want)
+
+
+@pytest.mark.parametrize("q,k", [([300], [300]), ([64], [3000]), ([33, 1, 64], [900, 700, 40]), ([130, 0, 5], [2000, 50, 1]), ([520, 260], [520, 300])])
+@pytest.mark.parametrize("H,Hkv,d,dtype", [(4, 2, 64, BF), (8, 2, 128, HF), (6, 2, 96, BF)])
+def test_few_tiles_and_many_keys(q, k, H, Hkv, d, dtype):
+    """One row tile a CTA or two, whole or in parts, by how much there is to do."""
+    _check(*_inputs(q, k, H, Hkv, d, dtype, 9), q, k)
+    _check(*_inputs(q * 3, k * 3, H, Hkv, d, dtype, 10), q * 3, k * 3)
