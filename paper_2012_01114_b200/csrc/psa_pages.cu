@@ -19,6 +19,7 @@ namespace {
 
 constexpr int META_THREADS = 1024;
 constexpr int FREE_NEAR = 2048;                 // free pages of a call that are kept in shared memory
+constexpr int PAIRWISE = 256;                   // see pages_reserve_kernel
 constexpr int RESERVE_MOST = 4096;              // sequences of one call (their last pages are compared in shared memory)
 
 struct PageArgs {
@@ -140,8 +141,8 @@ __device__ __forceinline__ Need need_of(const PageArgs& p, const int* seqs, cons
     return n;
 }
 
-// free_list: room for p.pages numbers; pairs: (from, to) per sequence of the list, -1 where nothing is to be copied.
-__global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageArgs p, const int* seqs, const int* add, int count, int* short_by, int* free_list,
+// free_list: room for p.pages numbers, marks: for twice as many (long lists only); pairs: (from, to) per sequence of the list, -1 where nothing is to be copied.
+__global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageArgs p, const int* seqs, const int* add, int count, int* short_by, int* free_list, int* marks,
                                                                      int2* pairs, DeviceCounters* dc, DeviceCounters* dc_next) {
     __shared__ __align__(16) int last_s[RESERVE_MOST];
     __shared__ int free_near[FREE_NEAR];
@@ -168,8 +169,19 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
     }
     __syncthreads();
     // pages that each sequence needs: those that it grows by, and one for a shared last page.  Of several in the list that share one, all but the
-    // last reference copy it, in the order of the list: the one that is left alone with the page keeps it.  (Pair by pair: 1024 sequences that all share theirs, freed, forked
-    // and reserved for, 27 us, 2048 68, up to 256 19; four entries a load are no faster.)
+    // last reference copy it, in the order of the list: the one that is left alone with the page keeps it.
+    // Longer lists count the references to a page that are in the list, and find the last one, beside the page (1024 sequences that all share their last page, freed,
+    // forked and reserved for, 19 us so and 27 by looking at all entries before, 2048 22.5 and 68.6, 256 19 either way, which is the host's side of the three calls).
+    auto listed = [&](int page) { return marks + 2 * (size_t)page; };
+    auto latest = [&](int page) { return marks + 2 * (size_t)page + 1; };
+    if (count > PAIRWISE) {
+        for (int i = tid; i < count; i += META_THREADS)
+            if (last_s[i] >= 0) *reinterpret_cast<int2*>(listed(last_s[i])) = make_int2(0, 0);
+        __syncthreads();
+        for (int i = tid; i < count; i += META_THREADS)
+            if (last_s[i] >= 0) { atomicAdd(listed(last_s[i]), 1); atomicMax(latest(last_s[i]), i + 1); }
+        __syncthreads();
+    }
     int first[PER], total = 0;
     bool copy[PER];
 #pragma unroll
@@ -178,13 +190,15 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
         copy[k] = false;
         first[k] = 0;
         if (k * META_THREADS >= count) continue;        // (uniform)
-        if (i < count && n[k].seq >= 0 && n[k].last >= 0) {
-            const int refs = p.refs[n[k].last];
+        const int refs = i < count && n[k].seq >= 0 && n[k].last >= 0 ? p.refs[n[k].last] : 0;
+        if (count <= PAIRWISE) {
             if (refs > 1) {
                 int before = 0;
                 for (int j = 0; j < i; ++j) before += last_s[j] == n[k].last;
                 copy[k] = refs - before > 1;
             }
+        } else {
+            copy[k] = refs > 1 && (__ldcg(listed(n[k].last)) < refs || __ldcg(latest(n[k].last)) != i + 1);
         }
         int all;
         first[k] = total + cta_scan(n[k].seq >= 0 ? n[k].want - n[k].have + copy[k] : 0, tmp, &all);
@@ -379,13 +393,14 @@ int pages_free(const psa_pages& p, const int* seqs, int count, DeviceCounters* d
 int pages_fork(const psa_pages& p, const int* parents, const int* children, int count, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
     return status_of(launch(pages_fork_kernel, dim3(count), 128, stream, args_of(p), parents, children, dc, dc_next), "pages_fork_kernel launch");
 }
-size_t pages_reserve_scratch_bytes(int pages, int count) { return ((size_t)pages * 4 + 255) / 256 * 256 + (size_t)count * 8; }
+size_t pages_reserve_scratch_bytes(int pages, int count) { return ((size_t)pages * 4 + 255) / 256 * 256 + ((size_t)count * 8 + 255) / 256 * 256 + (count > PAIRWISE ? (size_t)pages * 8 : 0); }
 int pages_reserve(const psa_pages& p, void* pool, long long page_bytes, int layers, const int* seqs, const int* add, int count, int* short_by, void* scratch,
                   DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
     if (count > RESERVE_MOST) return PSA_ERR_UNSUPPORTED;
     int* free_list = static_cast<int*>(scratch);
     int2* pairs = reinterpret_cast<int2*>(static_cast<char*>(scratch) + ((size_t)p.pages * 4 + 255) / 256 * 256);
-    const int rc = status_of(launch(pages_reserve_kernel, dim3(1), META_THREADS, stream, args_of(p), seqs, add, count, short_by, free_list, pairs, dc, dc_next), "pages_reserve_kernel launch");
+    int* marks = reinterpret_cast<int*>(reinterpret_cast<char*>(pairs) + ((size_t)count * 8 + 255) / 256 * 256);
+    const int rc = status_of(launch(pages_reserve_kernel, dim3(1), META_THREADS, stream, args_of(p), seqs, add, count, short_by, free_list, marks, pairs, dc, dc_next), "pages_reserve_kernel launch");
     if (rc != PSA_OK) return rc;
     const long long layer = page_bytes * p.pages;
     const PoolCopy c = {static_cast<const uint8_t*>(pool), static_cast<uint8_t*>(pool), page_bytes, layer, layer, p.pages, p.pages, layers, count};

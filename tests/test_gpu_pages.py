@@ -191,3 +191,17 @@ def test_graph_replay():
         b.book.fork([0, 1, 1], [2, 3, 4])
         assert b.book.reserve([2, 3, 4], [3, 1, 20]) == int(b.short) == 0
         b.same()
+
+
+@pytest.mark.parametrize("n", [255, 256, 257, 700])
+def test_long_lists_that_share_pages(n):
+    """Children of three parents with a partly filled page each, in the order of chance: with the parents in the list the last one keeps the page, without one parent all copy."""
+    b = Both(n + 3, 3, 2 * n + 20, 16, layers=1, page_bytes=16)
+    b.reserve([0, 1, 2], [21, 5, 16])
+    b.fork([i % 3 for i in range(n)], [3 + i for i in range(n)])
+    r = random.Random(n)
+    every = list(range(1, n + 3))
+    r.shuffle(every)
+    for _ in range(2):
+        assert b.reserve(every[:n], [1 if r.random() < 0.9 else 0 for _ in range(n)]) == 0
+        b.same()
