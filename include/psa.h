@@ -291,6 +291,8 @@ int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
  *   - `out` is dense, [rows, heads * d_k]; `lse`, where given, dense fp32 [rows, heads]: log(sum_j exp(scale q_i k_j)), natural, by which
  *     results over different keys can be joined.  A row that sees no key gets zeros and -inf.
  *   - What a row does not see has no influence on it, NaN and infinities included.
+ *   - A weight is rounded to 16 bits for the product with V: to dtype by psa_prompt_attention, to fp16 by psa_cache_attention.  In fp16 it keeps 11 bits down to 2^-21
+ *     of the largest weight among the keys that are worked on together, and an error of 2^-32 of that one below.
  *   - Lengths, tables and lists are read on the device, in stream order; the host needs none of them.  A call with zero rows (or an empty list) returns PSA_OK and
  *     launches nothing.  Device-side arguments that name no place (a sequence or page that does not exist, a token beyond the table)
  *     are left out, and psa_last_issued returns PSA_ERR_SHAPE for that call.

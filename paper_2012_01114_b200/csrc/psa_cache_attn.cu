@@ -36,6 +36,8 @@ namespace {
 constexpr int WARPS = 8;                        // of a CTA.  (Four, twice as many CTAs: one sequence of 131,072 tokens, 8 heads of 128 47.8 -> 53.2 us, 64 of 1 to 8000 37.5 -> 43.0)
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float RAISE = 8.f;                    // log2 units, see phase 2
+// Weights are held 2^HEADROOM times as large, and so are their sums: see HEADROOM in psa_prompt.cu.  2^(RAISE + HEADROOM) is half of what fp16 takes.
+constexpr float HEADROOM = 7.f;
 constexpr int STEP_BLOCKS = 2, STEP = STEP_BLOCKS * CACHE_BLOCK;              // blocks and tokens of a step
 constexpr int MAX_CTAS = 148 * 4 + 64;          // partial results and arrival counts: two per CTA
 constexpr int SEQ_BITS = 9, SEQS = 1 << SEQ_BITS;                            // sequences of one launch
@@ -116,6 +118,11 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_weights(float lo, float hi) {      // (to fp16; never to infinity)
+    uint32_t y;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
     return y;
 }
 __device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
@@ -487,7 +494,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         const int seen_by_all = len - nq + (int)fastdiv(qt * COLS, a.by_group);          // the last token that every column sees
 
         const CacheOnes cache_ones;
-        // m: running maximum of the scores before their factor; limit_up: where it is raised; shift: -m in log2 units
+        // m: running maximum of the scores before their factor; limit_up: where it is raised; shift: HEADROOM - m in log2 units
         float o[NT][2 * G][4], m[NT][2], limit_up[NT][2], shift[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -580,7 +587,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                         const float top = fmaxf(m[nt][c], x), f = ex2((m[nt][c] - finite_or_zero(top)) * cs[nt][c]);
                         m[nt][c] = top;
                         limit_up[nt][c] = top + RAISE / cs[nt][c];
-                        shift[nt][c] = -finite_or_zero(top) * cs[nt][c];
+                        shift[nt][c] = fmaf(-finite_or_zero(top), cs[nt][c], HEADROOM);
                         l[nt][c] *= f;
 #pragma unroll
                         for (int k = 0; k < 2 * G; ++k) { o[nt][k][c] *= f; o[nt][k][c + 2] *= f; }
@@ -595,8 +602,8 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                     const float p2 = ex2(fmaf(sc[s][nt][2], cs[nt][0], shift[nt][0])), p3 = ex2(fmaf(sc[s][nt][3], cs[nt][1], shift[nt][1]));
                     l[nt][0] += p0 + p2;
                     l[nt][1] += p1 + p3;
-                    pb[s][nt][0] = transpose8x8(h2_bits(__floats2half2_rn(p0, p1)));
-                    pb[s][nt][1] = transpose8x8(h2_bits(__floats2half2_rn(p2, p3)));
+                    pb[s][nt][0] = transpose8x8(pack_weights(p0, p1));
+                    pb[s][nt][1] = transpose8x8(pack_weights(p2, p3));
                 }
             // ---- phase 3
 #pragma unroll
@@ -682,7 +689,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         };
         auto store_lse = [&](int col, float top, float sum) {
             const int rho = qt * COLS + col, token = (int)fastdiv((uint32_t)rho, a.by_group);
-            a.lse[(size_t)(q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)] = sum == 0.f ? -INFINITY : (finite_or_zero(top) + log2f(sum)) * LN2;
+            a.lse[(size_t)(q0 + token) * a.kv_heads * a.group + (size_t)h * a.group + (rho - token * a.group)] = sum == 0.f ? -INFINITY : (finite_or_zero(top) - HEADROOM + log2f(sum)) * LN2;
         };
         if (single) {
 #pragma unroll

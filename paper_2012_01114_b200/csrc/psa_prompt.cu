@@ -102,6 +102,16 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         return pack_bf16x2(lo, hi);
     }
 }
+// P = exp2(s - m) is held 2^HEADROOM times as large in fp16, whose normal numbers end at 2^-14 and the others at 2^-24: beside one key that outweighs all others
+// the rest of a row would lose its bits, or vanish (256 keys, one of which outweighs the others by e^14, e^16, e^18 and has a value of
+// zero, d = 128: relative error of the output 9e-4, 6e-2 and 1 without the factor, 1.6e-4, 1.9e-4 and 3.3e-4 with it; no call took longer).  m lags up to 2^8 behind the largest score, so that a weight is at most 2^15 of the 2^16 that the type takes; beyond scores of 2^23,
+// whose own rounding exceeds the rest, weights stay at its largest number.  The sums carry the factor too: it cancels in the output and leaves the log-sum-exp.
+template <bool F16> constexpr float HEADROOM = F16 ? 7.f : 0.f;
+__device__ __forceinline__ uint32_t pack_weights_f16(float lo, float hi) {
+    uint32_t v;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
+    return v;
+}
 // exp_quad64 (psa_softmax.cuh) for either type of P.
 template <bool F16>
 __device__ __forceinline__ void exp_quad(const uint32_t (&s)[32], float sl2, float negmA, float negmB, uint32_t (&pk)[16], float& sumA, float& sumB) {
@@ -114,8 +124,8 @@ __device__ __forceinline__ void exp_quad(const uint32_t (&s)[32], float sl2, flo
             const float p0 = ex2_mufu(fmaf(__uint_as_float(s[4 * g]), sl2, negmA)), p1 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 1]), sl2, negmA));
             const float p2 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 2]), sl2, negmB)), p3 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 3]), sl2, negmB));
             sa0 += p0; sa1 += p1; sb0 += p2; sb1 += p3;
-            pk[2 * g] = pack<true>(p0, p1);
-            pk[2 * g + 1] = pack<true>(p2, p3);
+            pk[2 * g] = pack_weights_f16(p0, p1);
+            pk[2 * g + 1] = pack_weights_f16(p2, p3);
         }
         sumA += sa0 + sa1;
         sumB += sb0 + sb1;
@@ -781,7 +791,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
                 // ---- pass 2: P = exp2(S*sl2 - m) as bf16, keys 0-63 then keys 64-127
                 float sumA = 0.f, sumB = 0.f;
                 uint32_t pk[16];
-                const float nmA = mA == -INFINITY ? 0.f : -mA, nmB = mB == -INFINITY ? 0.f : -mB;     // (rows that have seen no key)
+                const float nmA = mA == -INFINITY ? 0.f : HEADROOM<F16> - mA, nmB = mB == -INFINITY ? 0.f : HEADROOM<F16> - mB;     // (rows that have seen no key)
                 exp_quad<F16>(s0, pa.sl2, nmA, nmB, pk, sumA, sumB);
                 if (SEP && blk > 0) {
                     // P and O are still in use by the PV before this one until its commit
@@ -923,8 +933,8 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
                 const long long outA = out_row(work, rA), outB = out_row(work, rB);
                 const float invA = lA == 0.f ? 0.f : 1.f / lA, invB = lB == 0.f ? 0.f : 1.f / lB;
                 if (pa.lse && (lane & 3) == 0) {
-                    if (outA >= 0) pa.lse[outA] = lA == 0.f ? -INFINITY : (mA + log2f(lA)) * LN2;
-                    if (outB >= 0) pa.lse[outB] = lB == 0.f ? -INFINITY : (mB + log2f(lB)) * LN2;
+                    if (outA >= 0) pa.lse[outA] = lA == 0.f ? -INFINITY : (mA - HEADROOM<F16> + log2f(lA)) * LN2;
+                    if (outB >= 0) pa.lse[outB] = lB == 0.f ? -INFINITY : (mB - HEADROOM<F16> + log2f(lB)) * LN2;
                 }
 #pragma unroll
                 for (int u = 0; u < Cfg::SUB; ++u) {
