@@ -275,6 +275,7 @@ int psa_measure_pipe_rates(psa_pipe_rates* rates, void* stream);
  * the same skeleton whose barrier nobody completes, with a wait limit of `limit_us` microseconds
  * (1 .. 100000).  It returns PSA_OK once the kernel is queued; the following psa_last_issued(stream, &c)
  * must then return PSA_ERR_TIMEOUT with all counters zero, and later calls on the same context work as usual.
+ * It also leaves what a psa_prompt_attention whose waits ran out leaves of the library's arrival counts; the calls behind it must not mind.
  * Nothing traps or spins without a bound.
  */
 int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
@@ -299,7 +300,7 @@ int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
  *   - psa_last_issued reports these calls' status; its counts are those of psa_prompt_attention's blocks, else zero.
  *   - Parts of long rows are joined by counts that belong to the library, one set per device: calls of psa_prompt_attention, and calls of
  *     psa_cache_attention, must not overlap on the GPU even where each has a workspace of its own (graphs replayed on different streams without an event
- *     between them).  After PSA_ERR_TIMEOUT the next such call is in order once psa_last_issued has reported it.
+ *     between them).  A call behind one whose waits ran out (PSA_ERR_TIMEOUT) is in order, whether or not the status was asked for in between.
  */
 
 /*

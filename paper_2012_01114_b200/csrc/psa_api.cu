@@ -326,7 +326,7 @@ struct OpCall {
     char* ws;                 // scratch of the call: ws + COUNTER_BYTES
     DeviceCounters *dc, *dc_next;
     bool captured;
-    int block;
+    int block, call;          // call: number of the call
     unsigned long long capture_id;
 };
 int begin_op(Context& cx, size_t scratch, cudaStream_t stream, OpCall* c) {
@@ -350,6 +350,7 @@ int begin_op(Context& cx, size_t scratch, cudaStream_t stream, OpCall* c) {
     }
     if (e != cudaSuccess) { set_cuda_error(e, "cudaMemsetAsync(counters)"); return PSA_ERR_CUDA; }
     (c->captured ? cx.capture_ws : cx.clean_ws) = nullptr;
+    c->call = next_mark(cx);
     c->dc = reinterpret_cast<DeviceCounters*>(c->ws + c->block * COUNTER_BLOCK_BYTES);
     c->dc_next = reinterpret_cast<DeviceCounters*>(c->ws + (c->block ^ 1) * COUNTER_BLOCK_BYTES);
     cx.last_dc = c->dc;
@@ -738,7 +739,6 @@ int psa_last_issued(void* stream, psa_counts* c) {
     c->qk_macs = h.qk_macs;
     c->pv_macs = h.pv_macs;
     c->exps = h.exps;
-    if (h.status == PSA_ERR_TIMEOUT && (e = prompt_reset()) != cudaSuccess) { set_cuda_error(e, "psa_last_issued"); return PSA_ERR_CUDA; }
     return h.status;
 }
 
@@ -794,6 +794,7 @@ int psa_selftest_wait_expiry(unsigned limit_us, void* stream_v) {
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
     cudaError_t e = cudaMemsetAsync(ws, 0, COUNTER_BLOCK_BYTES, stream);
     if (e == cudaSuccess) e = launch_wait_expiry(reinterpret_cast<DeviceCounters*>(ws), limit_us, stream);
+    if (e == cudaSuccess) e = launch_prompt_expired(stream);
     if (e != cudaSuccess) { set_cuda_error(e, "psa_selftest_wait_expiry"); return PSA_ERR_CUDA; }
     cx.clean_ws = nullptr;
     cx.last_dc = reinterpret_cast<DeviceCounters*>(ws);
@@ -901,7 +902,7 @@ int psa_prompt_attention(const void* Q, const void* K, const void* V, long long 
     const size_t scratch = prompt_scratch_bytes(sequences, q_rows, k_rows, heads, kv_heads, d_k);
     return run_op(scratch, stream, [&](const OpCall& c) {
         return prompt_attention(Q, K, V, q_stride, k_stride, v_stride, q_starts, k_starts ? k_starts : q_starts, sequences, q_rows, k_rows, heads, kv_heads, d_k, scale,
-                                dtype, out, lse, scratch ? c.ws + COUNTER_BYTES : nullptr, c.dc, &c.dc->next_item, c.dc_next, static_cast<cudaStream_t>(stream));
+                                dtype, out, lse, scratch ? c.ws + COUNTER_BYTES : nullptr, c.call, c.dc, &c.dc->next_item, c.dc_next, static_cast<cudaStream_t>(stream));
     });
 }
 

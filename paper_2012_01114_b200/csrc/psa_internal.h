@@ -93,10 +93,10 @@ int bf16_attention_persist(const void* Q, const void* K, const void* V, void* ou
 // ---- serving (psa_prompt.cu, psa_cache_append.cu, psa_cache_attn.cu, psa_pages.cu) ----
 // Arguments are checked by the caller; each returns a psa_status.  dc: the call's counter block, dc_next (may be null): cleared by the call's first kernel.
 int prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts, const int* k_starts,
-                     int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, void* scratch, DeviceCounters* dc,
-                     unsigned int* cursor, DeviceCounters* dc_next, cudaStream_t stream);
+                     int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, void* scratch, int call, DeviceCounters* dc,
+                     unsigned int* cursor, DeviceCounters* dc_next, cudaStream_t stream);     // call: a number > 0 of its own
 size_t prompt_scratch_bytes(int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d);      // 0: none is used
-cudaError_t prompt_reset();                    // after a call whose waits ran out: the counts that such a call may have left behind
+cudaError_t launch_prompt_expired(cudaStream_t stream);       // self-test: the counts that a call leaves whose waits ran out
 int cache_append(const psa_cache& c, const void* K, const void* V, long long k_stride, long long v_stride, const int* seqs, const int* starts, int sequences, int rows,
                  int dtype, void* k_held, void* v_held, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
 size_t cache_attention_scratch_bytes(int d);

@@ -59,6 +59,7 @@ struct PromptArgs {
     const int *q_starts, *k_starts;
     int sequences, q_rows, k_rows, heads, kv_heads, group, tokens, d;     // tokens: of a row tile, 128 / group
     int tiles;                          // row tiles of an item: 2, or 1 (see launch_prompt)
+    int call;                           // number of the call, > 0
     long long v_stride;
     const uint16_t* v;                  // (the epilogue's look at values that are not finite)
     uint16_t* out;
@@ -76,6 +77,11 @@ struct __align__(16) Item {
 };
 // Arrivals of the warps on rows of several parts, by slot of the first part, tile and warp.  The arrival that completes a count wraps it to zero again.
 __device__ unsigned g_prompt_arrived[2 * MAX_CTAS][2][SOFTMAX_WARPS_PER_TILE];
+// A call whose waits ran out leaves counts that are not zero.  g_prompt_left is EXPIRED behind it; the next call that could cut cuts nothing, clears the counts and puts its
+// own number here (which its other CTAs take for the same order), the one after that cuts again and leaves 0.  Nobody has to ask for the status in between.  (A graph that is
+// replayed with no other such call in between goes on without parts.)
+__device__ int g_prompt_left;
+constexpr int EXPIRED = -1;
 // Counts a warp's arrival behind what its lanes have stored; true in all of them for the one that completes the rows.
 __device__ __forceinline__ bool warp_arrive(unsigned* count, unsigned last, int lane) {
     unsigned old = 0;
@@ -183,6 +189,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     __shared__ int starts_s[2][SEQS + 1];
     __shared__ uint32_t cut[SEQS + 1], cut_sum[ISSUER1_WARP + 1];       // with pairs cut into parts: items << 16 | results ahead of a pair
     __shared__ Item own[2 * SOFTMAX_WARPS_PER_TILE][2];                 // a softmax warp's items, this one and the next
+    __shared__ int left_s;                       // g_prompt_left, as the CTA found it
     __shared__ Item first_item;                  // this CTA's first item, found by the thread that knows its sequence or pair
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -219,6 +226,7 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     // the counter block of the NEXT call on this workspace is cleared here, off that call's critical path
     if (threadIdx.x == 0 && blockIdx.x == 0 && dc_next) *dc_next = DeviceCounters{0, 0, 0, 0, 0, 0, 0};
     // ---- the work list
+    if (CUT && threadIdx.x == persist_threads<D>() - 1) left_s = *const_cast<const volatile int*>(&g_prompt_left);
     for (int i = threadIdx.x; i <= pa.sequences; i += persist_threads<D>()) {
         starts_s[0][i] = min(max(pa.q_starts[i], 0), pa.q_rows);
         starts_s[1][i] = min(max(pa.k_starts[i], 0), pa.k_rows);
@@ -306,7 +314,13 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     };
     const int x0 = (int)fastdiv(blockIdx.x, pa.by_heads), h0 = (int)blockIdx.x - x0 * pa.kv_heads;       // the CTA's first item
     // Fewer pairs than CTAs: their key blocks are cut into pieces of blocks / (CTAs - pairs), which makes no more parts than there are CTAs.
-    const bool cuts = CUT && pairs > 0 && pairs <= SEQS && pairs * pa.kv_heads < (int)gridDim.x;
+    const bool counts_good = CUT && left_s != EXPIRED && left_s != pa.call;
+    if (CUT && left_s != 0 && blockIdx.x == 0) {
+        if (!counts_good)
+            for (int i = threadIdx.x; i < (int)(sizeof(g_prompt_arrived) / sizeof(unsigned)); i += persist_threads<D>()) (&g_prompt_arrived[0][0][0])[i] = 0u;
+        if (threadIdx.x == 0) atomicCAS(&g_prompt_left, left_s, counts_good ? 0 : pa.call);      // (unless a wait of this very call has run out)
+    }
+    const bool cuts = counts_good && pairs > 0 && pairs <= SEQS && pairs * pa.kv_heads < (int)gridDim.x;
     if (!cuts) {
         for (int k = threadIdx.x; k < pa.sequences; k += persist_threads<D>())
             if (base[k] <= x0 && x0 < base[k + 1]) { first_item = pair_behind(k, x0); first_item.h = h0; }
@@ -989,7 +1003,10 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     }
     tc_fence_before();
     __syncthreads();
-    if (threadIdx.x == 0 && abort_flag) atomicExch(&dc->status, (int)PSA_ERR_TIMEOUT);
+    if (threadIdx.x == 0 && abort_flag) {
+        atomicExch(&dc->status, (int)PSA_ERR_TIMEOUT);
+        if (cuts) atomicExch(&g_prompt_left, EXPIRED);
+    }
     if (warp == 1) tmem_dealloc(tmem, 512);
 }
 
@@ -1053,15 +1070,18 @@ size_t prompt_scratch_bytes(int sequences, int q_rows, int k_rows, int heads, in
     if ((long long)q_rows / (2 * tokens) * kv_heads >= MAX_CTAS || k_rows <= 2 * LEAST_PIECE * TILE || sequences > SEQS) return 0;
     return (size_t)2 * MAX_CTAS * 2 * TILE * ((d <= 64 ? 64 : 128) + 2) * sizeof(float);
 }
-cudaError_t prompt_reset() {
-    void* p = nullptr;
-    cudaError_t e = cudaGetSymbolAddress(&p, g_prompt_arrived);
-    if (e == cudaSuccess) e = cudaMemset(p, 0, sizeof(g_prompt_arrived));
-    return e;
+// For the self-test of the failure path: what a call that had cut its pairs when its waits ran out leaves behind.
+static __global__ void prompt_expired_kernel() {
+    for (int i = threadIdx.x; i < (int)(sizeof(g_prompt_arrived) / sizeof(unsigned)); i += blockDim.x) (&g_prompt_arrived[0][0][0])[i] = 1u;
+    if (threadIdx.x == 0) atomicExch(&g_prompt_left, EXPIRED);
+}
+cudaError_t launch_prompt_expired(cudaStream_t stream) {
+    prompt_expired_kernel<<<1, 256, 0, stream>>>();
+    return cudaGetLastError();
 }
 
 int prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts, const int* k_starts,
-                     int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, void* scratch, DeviceCounters* dc,
+                     int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, void* scratch, int call, DeviceCounters* dc,
                      unsigned int* cursor, DeviceCounters* dc_next, cudaStream_t stream) {
     const int group = heads / kv_heads, tokens = TILE / group;
     if ((long long)q_rows / (2 * tokens) >= 1LL << (32 - SEQ_BITS) || ((long long)q_rows / (2 * tokens) + SEQS) * kv_heads > 0x7fff0000LL) return PSA_ERR_SHAPE;
@@ -1069,7 +1089,7 @@ int prompt_attention(const void* Q, const void* K, const void* V, long long q_st
     if (!query_map(&maps.q, Q, q_rows, kv_heads, group, d, q_stride, tokens)) return PSA_ERR_CUDA;
     maps.k = maps.v = maps.q;                    // (without keys no block of them is ever loaded)
     if (k_rows > 0 && (!key_map(&maps.k, K, k_rows, kv_heads, d, k_stride) || !key_map(&maps.v, V, k_rows, kv_heads, d, v_stride))) return PSA_ERR_CUDA;
-    const PromptArgs pa = {q_starts, k_starts, sequences, q_rows, k_rows, heads, kv_heads, group, tokens, d, 2, v_stride, static_cast<const uint16_t*>(V),
+    const PromptArgs pa = {q_starts, k_starts, sequences, q_rows, k_rows, heads, kv_heads, group, tokens, d, 2, call, v_stride, static_cast<const uint16_t*>(V),
                            static_cast<uint16_t*>(out), lse, static_cast<float*>(scratch), scale * LOG2E, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)kv_heads)};
     auto launch = [&](auto width, auto steps) {
         constexpr int D = decltype(width)::value, KS = decltype(steps)::value;
