@@ -360,8 +360,8 @@ size_t psa_cache_workspace_bytes(int d_k);
  *   psa_pages_free     the sequences give back a reference to each of their pages; their rows become -1 and their lengths 0
  *   psa_pages_fork     child i, a slot without pages, gets parent i's pages (one reference more each) and length; a child is no parent in the same call
  *   psa_pages_reserve  room for add[i] more tokens of sequence i: lens grows by add[i], pages are taken as needed, and a partly filled last page that is
- *                      shared is replaced by a copy of its own in all layers.  All or nothing: if pages are missing, *short_by (device int, else 0) says how many and
- *                      nothing changes.  Up to 4096 sequences a call.  short_by is written by every call that launches.
+ *                      shared is replaced by a copy of its own in all layers.  All or nothing: if pages are missing, *short_by (device int, else 0) says how many (at most
+ *                      2^31 - 1) and nothing changes.  Up to 4096 sequences a call.  short_by is written by every call that launches.
  *   psa_pages_compact  the n live pages take places 0 .. n - 1: those there stay, the k-th live page beyond goes to the k-th hole.  new_tables, new_refs and new_pool
  *                      (same shapes) receive the result and may be the old ones (then only pages that move are copied); *live (device int) = n.  Places beyond n of a
  *                      new pool keep their bytes.  pages->lens is not used.

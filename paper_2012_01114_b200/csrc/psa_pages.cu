@@ -21,6 +21,8 @@ constexpr int META_THREADS = 1024;
 constexpr int FREE_NEAR = 2048;                 // free pages of a call that are kept in shared memory
 constexpr int PAIRWISE = 256;                   // see pages_reserve_kernel
 constexpr int RESERVE_MOST = 4096;              // sequences of one call (their last pages are compared in shared memory)
+// A list in which a sequence grows by more pages is summed up in 64 bits (which costs a call of 64 sequences 0.3 us of 18): RESERVE_MOST times this is no more than 31 bits take.
+constexpr int MANY_PAGES = 1 << 18;
 
 struct PageArgs {
     int *tables, *lens, *refs;
@@ -68,21 +70,22 @@ __global__ void __launch_bounds__(128) pages_fork_kernel(const PageArgs p, const
 }
 
 // Exclusive sum over the CTA; *total: of all.  `tmp`: 32 numbers of shared memory.
-__device__ __forceinline__ int cta_scan(int v, int* tmp, int* total) {
+template <class T>
+__device__ __forceinline__ T cta_scan(T v, T* tmp, T* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int x = v;
+    T x = v;
 #pragma unroll
     for (int s = 1; s < 32; s *= 2) {
-        const int y = __shfl_up_sync(0xffffffffu, x, s);
+        const T y = __shfl_up_sync(0xffffffffu, x, s);
         if (lane >= s) x += y;
     }
     __syncthreads();
     if (lane == 31) tmp[warp] = x;
     __syncthreads();
-    int w = tmp[lane];                          // META_THREADS / 32 = 32 warps
+    T w = tmp[lane];                            // META_THREADS / 32 = 32 warps
 #pragma unroll
     for (int s = 1; s < 32; s *= 2) {
-        const int y = __shfl_up_sync(0xffffffffu, w, s);
+        const T y = __shfl_up_sync(0xffffffffu, w, s);
         if (lane >= s) w += y;
     }
     *total = __shfl_sync(0xffffffffu, w, 31);
@@ -147,6 +150,7 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
     __shared__ __align__(16) int last_s[RESERVE_MOST];
     __shared__ int free_near[FREE_NEAR];
     __shared__ int tmp[32];
+    __shared__ long long tmp_long[32];
     __shared__ int bad_s;
     const int tid = threadIdx.x;
     if (tid == 0) bad_s = 0;
@@ -156,7 +160,7 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
     Counts16 counts = load_counts(p.refs, p.pages, (long long)tid * PER_THREAD);         // (asked for ahead: nothing below depends on it for long)
     constexpr int PER = RESERVE_MOST / META_THREADS;
     Need n[PER];
-    bool bad = false;
+    bool bad = false, many = false;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int i = k * META_THREADS + tid;
@@ -165,9 +169,10 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
             n[k] = need_of(p, seqs, add, i);
             bad |= n[k].seq < 0;
             last_s[i] = n[k].seq < 0 ? -1 : n[k].last;
+            many |= n[k].want - n[k].have > MANY_PAGES;
         }
     }
-    __syncthreads();
+    many = __syncthreads_or(many);
     // pages that each sequence needs: those that it grows by, and one for a shared last page.  Of several in the list that share one, all but the
     // last reference copy it, in the order of the list: the one that is left alone with the page keeps it.
     // Longer lists count the references to a page that are in the list, and find the last one, beside the page (1024 sequences that all share their last page, freed,
@@ -182,7 +187,8 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
             if (last_s[i] >= 0) { atomicAdd(listed(last_s[i]), 1); atomicMax(latest(last_s[i]), i + 1); }
         __syncthreads();
     }
-    int first[PER], total = 0;
+    long long total = 0;
+    int first[PER];                              // (read only if the pages are there, so that it fits)
     bool copy[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
@@ -200,9 +206,16 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
         } else {
             copy[k] = refs > 1 && (__ldcg(listed(n[k].last)) < refs || __ldcg(latest(n[k].last)) != i + 1);
         }
-        int all;
-        first[k] = total + cta_scan(n[k].seq >= 0 ? n[k].want - n[k].have + copy[k] : 0, tmp, &all);
-        total += all;
+        const int need = n[k].seq >= 0 ? n[k].want - n[k].have + copy[k] : 0;
+        if (many) {
+            long long all;
+            first[k] = (int)(total + cta_scan((long long)need, tmp_long, &all));
+            total += all;
+        } else {
+            int all;
+            first[k] = (int)total + cta_scan(need, tmp, &all);
+            total += all;
+        }
     }
     if (bad) bad_s = 1;
     // ---- the first `total` pages without references, ascending: in shared memory, those that it has no room for behind
@@ -223,7 +236,7 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
     auto free_page = [&](int k) { return k < FREE_NEAR ? free_near[k] : free_list[k]; };
     const bool go = !bad_s && found >= total;
     if (tid == 0) {
-        *short_by = found >= total ? 0 : total - found;
+        *short_by = (int)min(max(total - found, 0LL), 0x7fffffffLL);
         if (bad_s) bad_argument(dc);
     }
 #pragma unroll
