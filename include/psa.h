@@ -321,7 +321,7 @@ size_t psa_prompt_workspace_bytes(int sequences, int q_rows, int k_rows, int hea
  * A layer's cache: keys and values in pages of `page_size` tokens (a multiple of 16), every token, head and group of 32 channels with 4-bit codes c and two fp16
  * numbers S, M; a number reads back as M + S (1 + c / 16), 5 bits each altogether.  Numbers beyond 20000 in size are held as that; a NaN makes its group NaN.
  * A page is [kv_heads][page_size / 16] blocks of 20 d_k bytes (psa_cache_page_bytes), independent of what its other tokens hold: pages may be copied as bytes.
- *   pool     device, [pages][page bytes], 16-byte aligned       tables  device ints [slots, width]: a sequence's pages in order, -1 behind the last
+ *   pool     device, [pages][page bytes], 16-byte aligned       tables  device ints [slots, width]: a sequence's pages in order, -1 behind the last (pages behind its length are not read)
  *   lens     device ints [slots]: tokens of each sequence
  * Supported: d_k = 32, 64, 96, 128, 256; width * page_size < 2^31.
  */
@@ -361,7 +361,8 @@ size_t psa_cache_workspace_bytes(int d_k);
  *   psa_pages_fork     child i, a slot without pages, gets parent i's pages (one reference more each) and length; a child is no parent in the same call
  *   psa_pages_reserve  room for add[i] more tokens of sequence i: lens grows by add[i], pages are taken as needed, and a partly filled last page that is
  *                      shared is replaced by a copy of its own in all layers.  All or nothing: if pages are missing, *short_by (device int, else 0) says how many (at most
- *                      2^31 - 1) and nothing changes.  Up to 4096 sequences a call.  short_by is written by every call that launches.
+ *                      2^31 - 1) and nothing changes.  A program may take lengths back (guessed tokens that were refused): pages behind the length stay with the
+ *                      sequence until it is in such a list, with any add[i], and are given back then, ahead of everything else (even if pages are missing).  Up to 4096 sequences a call.  short_by is written by every call that launches.
  *   psa_pages_compact  the n live pages take places 0 .. n - 1: those there stay, the k-th live page beyond goes to the k-th hole.  new_tables, new_refs and new_pool
  *                      (same shapes) receive the result and may be the old ones (then only pages that move are copied); *live (device int) = n.  Places beyond n of a
  *                      new pool keep their bytes.  pages->lens is not used.

@@ -3,7 +3,8 @@
 //
 //   free     the pages of a sequence lose a reference each, its row and length are cleared
 //   fork     a sequence without pages gets those of another, one reference more each
-//   reserve  room for so many more tokens of each sequence; a page that is partly filled and shared is copied before it is written to
+//   reserve  room for so many more tokens of each sequence; a page that is partly filled and shared is copied before it is written to, pages behind a length that was
+//            taken back are given back first (left in the table they would be overwritten there, and stay counted for ever)
 //   compact  live pages beyond the first `live` ones move into the holes before them
 //   copy     pages by list
 // Free pages are those without references, and are handed out in ascending order in the order of the list: what a call does depends on its arguments alone,
@@ -127,9 +128,10 @@ __device__ __forceinline__ uint32_t bits_of(const Counts16& r, What what) {
 // What reserve does to sequence i of the list.
 struct Need {
     int seq, held, add, have, want, last;       // last: its last page, if that is partly filled and about to be written to (else -1)
+    bool over;                                  // it holds pages behind its length (which was taken back): they are given back
 };
 __device__ __forceinline__ Need need_of(const PageArgs& p, const int* seqs, const int* add, int i) {
-    Need n = {seqs[i], 0, 0, 0, 0, -1};
+    Need n = {seqs[i], 0, 0, 0, 0, -1, false};
     if (n.seq < 0 || n.seq >= p.slots) { n.seq = -1; return n; }
     n.held = max(p.lens[n.seq], 0);
     n.add = max(add[i], 0);
@@ -137,9 +139,13 @@ __device__ __forceinline__ Need need_of(const PageArgs& p, const int* seqs, cons
     const long long want = ((long long)n.held + n.add + p.page_size - 1) / p.page_size;
     if (want > p.width || n.have > p.width) { n.seq = -1; return n; }
     n.want = (int)want;
-    if (n.add > 0 && n.held % p.page_size) {
-        n.last = p.tables[(size_t)n.seq * p.width + n.have - 1];
-        if (n.last < 0 || n.last >= p.pages) n.seq = -1;
+    const int* row = p.tables + (size_t)n.seq * p.width;
+    const bool part = n.add > 0 && n.held % p.page_size;
+    const int last = part ? row[n.have - 1] : -1, behind = n.have < p.width ? row[n.have] : -1;      // (asked for together)
+    n.over = behind >= 0;
+    if (part) {
+        n.last = last;
+        if (last < 0 || last >= p.pages) n.seq = -1;
     }
     return n;
 }
@@ -160,19 +166,38 @@ __global__ void __launch_bounds__(META_THREADS) pages_reserve_kernel(const PageA
     Counts16 counts = load_counts(p.refs, p.pages, (long long)tid * PER_THREAD);         // (asked for ahead: nothing below depends on it for long)
     constexpr int PER = RESERVE_MOST / META_THREADS;
     Need n[PER];
-    bool bad = false, many = false;
+    bool bad = false, many = false, over = false;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int i = k * META_THREADS + tid;
-        n[k] = Need{-1, 0, 0, 0, 0, -1};
+        n[k] = Need{-1, 0, 0, 0, 0, -1, false};
         if (i < count) {
             n[k] = need_of(p, seqs, add, i);
             bad |= n[k].seq < 0;
             last_s[i] = n[k].seq < 0 ? -1 : n[k].last;
             many |= n[k].want - n[k].have > MANY_PAGES;
+            over |= n[k].over;
         }
     }
-    many = __syncthreads_or(many);
+    if (__syncthreads_or(bad || many || over)) {         // (rare)
+        many = __syncthreads_or(many);
+        if (__syncthreads_or(over)) {
+            auto behind = [&](auto what) {               // the columns behind the lengths, up to the first without a page
+                for (int k = 0; k < PER; ++k)
+                    if (n[k].seq >= 0 && n[k].over)
+                        for (int c = n[k].have; c < p.width && p.tables[(size_t)n[k].seq * p.width + c] >= 0; ++c) what(p.tables + (size_t)n[k].seq * p.width + c);
+            };
+            behind([&](int* at) { bad |= *at >= p.pages; });
+            if (!__syncthreads_or(bad)) {
+                behind([&](int* at) {
+                    const int page = atomicExch(at, -1);
+                    if (page >= 0) atomicSub(p.refs + page, 1);
+                });
+                __syncthreads();
+                counts = load_counts(p.refs, p.pages, (long long)tid * PER_THREAD);
+            }
+        }
+    }
     // pages that each sequence needs: those that it grows by, and one for a shared last page.  Of several in the list that share one, all but the
     // last reference copy it, in the order of the list: the one that is left alone with the page keeps it.
     // Longer lists count the references to a page that are in the list, and find the last one, beside the page (1024 sequences that all share their last page, freed,
