@@ -296,7 +296,8 @@ int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
  *     of the largest weight among the keys that are worked on together, and an error of 2^-32 of that one below.
  *   - Lengths, tables and lists are read on the device, in stream order; the host needs none of them.  A call with zero rows (or an empty list) returns PSA_OK and
  *     launches nothing.  Device-side arguments that name no place (a sequence or page that does not exist, a token beyond the table)
- *     are left out, and psa_last_issued returns PSA_ERR_SHAPE for that call.
+ *     are left out, and psa_last_issued returns PSA_ERR_SHAPE for that call.  So it does for `starts` of psa_prompt_attention and psa_cache_attention that descend
+ *     somewhere: the rows between starts[512 c] and starts[512 (c + 1)] are then not computed, for every c in whose part they do.
  *   - psa_last_issued reports these calls' status; its counts are those of psa_prompt_attention's blocks, else zero.
  *   - Parts of long rows are joined by counts that belong to the library, one set per device: calls of psa_prompt_attention, and calls of
  *     psa_cache_attention, must not overlap on the GPU even where each has a workspace of its own (graphs replayed on different streams without an event

@@ -227,11 +227,14 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
     if (threadIdx.x == 0 && blockIdx.x == 0 && dc_next) *dc_next = DeviceCounters{0, 0, 0, 0, 0, 0, 0};
     // ---- the work list
     if (CUT && threadIdx.x == persist_threads<D>() - 1) left_s = *const_cast<const volatile int*>(&g_prompt_left);
+    bool descends = false;                       // `starts` that do not ascend name rows more than once, or keys that are not there: nothing is computed, and the call reports it
     for (int i = threadIdx.x; i <= pa.sequences; i += persist_threads<D>()) {
-        starts_s[0][i] = min(max(pa.q_starts[i], 0), pa.q_rows);
-        starts_s[1][i] = min(max(pa.k_starts[i], 0), pa.k_rows);
+        const int next = min(i + 1, pa.sequences), q = pa.q_starts[i], k = pa.k_starts[i];
+        descends |= pa.q_starts[next] < q || pa.k_starts[next] < k;
+        starts_s[0][i] = min(max(q, 0), pa.q_rows);
+        starts_s[1][i] = min(max(k, 0), pa.k_rows);
     }
-    __syncthreads();
+    descends = __syncthreads_or(descends);
     uint32_t* const unsorted = reinterpret_cast<uint32_t*>(base);
     for (int i = threadIdx.x; i < (pa.sequences + 3) / 4 * 4; i += persist_threads<D>()) {
         const int nq = i < pa.sequences ? max(starts_s[0][i + 1] - starts_s[0][i], 0) : 0;
@@ -265,10 +268,8 @@ prompt_kernel(const __grid_constant__ PMaps maps, const __grid_constant__ Prompt
             sum += __shfl_sync(0xffffffffu, x, 31);
         }
         if (lane == 0) {
-            // (more rows than there are: `starts` that do not ascend; nothing is computed, and the call reports it)
-            const bool bad = sum > pa.q_rows / (pa.tiles * pa.tokens) + pa.sequences;
-            if (bad) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
-            base[pa.sequences] = bad ? 0 : (int)sum;
+            if (descends) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
+            base[pa.sequences] = descends ? 0 : (int)sum;
         }
     }
     fence_async_smem();                          // (the zeroed rows, ahead of the loads beside them)
