@@ -348,7 +348,7 @@ int psa_cache_append(const psa_cache* cache, const void* K, const void* V, long 
  * is the single-token step; several are guessed tokens checked at once, or the rest of a prompt.
  *   Q      device, [rows, heads, d_k] with row stride q_stride; sequence b owns rows q_starts[b] .. q_starts[b + 1] - 1
  *   max_q  >= 1, the caller's bound on the queries of a sequence (it chooses the kernel's tiles; larger counts are worked off all the same)
- * Workspace: psa_cache_workspace_bytes.
+ * Workspace: psa_cache_workspace_bytes.  Supported: (rows * heads / kv_heads / 8 + 1 + sequences) * kv_heads up to 2^30, whatever the tables have room for.
  */
 int psa_cache_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
                         int max_q, float scale, int dtype, void* out, float* lse, void* stream);

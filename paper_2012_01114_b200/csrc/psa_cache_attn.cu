@@ -46,6 +46,8 @@ constexpr int LONG_PIECE = 48;                  // see `crowded`
 // Steps: a row up to LEAST_CUT is not cut, longer ones not into less than LEAST_PIECE.  (One sequence, 32 heads on 8 of d = 128 / 8 on 2 of 64, whole and in parts of 16: 600 tokens
 // 9.4 10.6 / 7.4 9.1 us, 1000 11.2 11.1 / 8.7 9.4, 1300 13.5 11.0 / 10.1 9.4, 4000 26.7 11.1 / 19.9 9.4; in parts of 32: 13.8 / 11.5.)
 constexpr int LEAST_CUT = 32, LEAST_PIECE = 16;
+constexpr int MOST_ROWS = 1 << 30;              // of a call; parts are two per CTA more at most
+constexpr int MOST_STEPS = 1 << 27;             // no row has as many
 
 template <int D, int NT>
 struct ACfg {
@@ -68,6 +70,7 @@ struct AttnArgs {
     float *lse, *part;                          // part: per part of a row [COLS][D] outputs, then [COLS] maxima and [COLS] sums
     long long q_stride;
     int pages, slots, width, page_size, kv_heads, group, sequences, rows, f16;
+    int wide;                                   // the steps of all rows may be more than 32 bits count, by the tables' width (many rows and room for 2^20 tokens and more)
     float scale;
     FastDiv by_group, by_blocks;                // by query heads of a group, by blocks of a page
 };
@@ -155,6 +158,7 @@ struct Piece {
 };
 struct Totals {
     uint32_t steps, rows;
+    float about;                                // AttnArgs::wide: the steps, which may be more than 32 bits count
 };
 __device__ __forceinline__ int parts_of(int steps, int piece) { return steps <= LEAST_CUT ? 1 : (int)((uint32_t)(steps + piece - 1) / (uint32_t)piece); }
 // Item `r` of a sequence whose rows are cut into pieces of at most `piece` steps.
@@ -224,6 +228,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     };
     Seq s0 = {};                                 // sequence tid
     uint32_t steps = 0, rows = 0;
+    float about = 0.f;
     bool descends = false;
     for (int b = tid; b < a.sequences; b += THREADS) {
         const Seq x = sequence<COLS>(a, b);
@@ -233,10 +238,14 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
         const uint32_t r = (uint32_t)x.qtiles * a.kv_heads;
         steps += r * x.steps;
         rows += r;
+        about = fmaf((float)r, (float)x.steps, about);
     }
+    if (a.wide)
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) about += __shfl_xor_sync(0xffffffffu, about, s);
     steps = __reduce_add_sync(0xffffffffu, steps);
     rows = __reduce_add_sync(0xffffffffu, rows);
-    if (lane == 0) total_s[warp] = Totals{steps, rows};
+    if (lane == 0) total_s[warp] = Totals{steps, rows, about};
     if (__syncthreads_or(descends)) {            // rows counted more than once: the numbers below would not hold; nothing is computed, and the call reports it
         if (tid == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
         return;
@@ -244,11 +253,19 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     steps = rows = 0;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) { steps += total_s[w].steps; rows += total_s[w].rows; }
+    bool beyond = false;                         // more steps than 32 bits count
+    if (a.wide) {
+        about = 0.f;
+        for (int w = 0; w < WARPS; ++w) about += total_s[w].about;
+        beyond = about > 2.0e9f;
+    }
+    // (steps + up) / n, there somewhat more
+    auto share_of_steps = [&](uint32_t n, uint32_t up) -> int { return beyond ? (int)fminf(__fdividef(about * 1.0001f, (float)n) + 1.f, (float)MOST_STEPS) : (int)((steps + up) / n); };
     // Rows cut into pieces of steps / (CTAs - rows) make no more parts than there are CTAs.  Where rows alone are that many, or leave so few CTAs that pieces get long, they are
     // cut into more parts than that, and items are handed out one by one, the longest first.  (us a call, one query, 32 heads on 8 of d = 128, by the first rule alone and so:
     // 30 sequences of up to 8000 tokens 39.3 and 28.1, 32 of up to 2000 20.3 and 15.9; what looking costs where pieces are short: 20 of up to 4000 13.0 and 13.7.)
     const uint32_t ctas = min(gridDim.x, (uint32_t)Cfg::MOST_PARTS), half = (ctas + 1) / 2;
-    auto piece_of_budget = [&](uint32_t budget) { return (int)max((steps + budget - 1) / budget, (uint32_t)LEAST_PIECE); };
+    auto piece_of_budget = [&](uint32_t budget) { return max(share_of_steps(budget, budget - 1), LEAST_PIECE); };
     int piece = piece_of_budget(rows < ctas ? ctas - rows : half);
     const bool crowded = MANY && (rows >= ctas || (rows > half && piece > LONG_PIECE));
     if (crowded) piece = piece_of_budget(half);
@@ -259,7 +276,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     // 22.6 22.7 16.4 16.4 16.6, 64 of up to 8000 33.2 33.1 32.8 32.7 32.6.)
     int brief = 0;
     if (crowded) {
-        brief = (int)(steps / (gridDim.x * WARPS));
+        brief = share_of_steps(gridDim.x * WARPS, 0);
         uint32_t count[2 * BRIEFS] = {};         // rows up to 2^k steps, and parts of longer ones
         for (int b = tid; b < a.sequences; b += THREADS) {
             const uint2 x = seq_s[b];
@@ -860,8 +877,9 @@ int launch_attn(const AttnArgs& all, DeviceCounters* dc, DeviceCounters* dc_next
         a.q_starts += b0;
         // (upper bounds: the lengths are known on the device only)
         const long long tiles = ((long long)a.rows * a.group + Cfg::COLS - 1) / Cfg::COLS + a.sequences;
+        if (tiles > MOST_ROWS / a.kv_heads) return PSA_ERR_UNSUPPORTED;
         const long long most = tiles * a.kv_heads * (((long long)a.width * a.page_size + STEP - 1) / STEP);
-        if (most > 0x7fffffffLL) return PSA_ERR_UNSUPPORTED;
+        a.wide = most > 0x7fffffffLL;
         long long grid = (long long)sms * Cfg::CTAS;
         if (grid > MAX_CTAS) grid = MAX_CTAS;
         if (grid > most) grid = most;
@@ -891,7 +909,7 @@ int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const
                     float scale, int dtype, void* out, float* lse, void* scratch, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
     const AttnArgs a = {static_cast<const uint8_t*>(c.pool), c.tables, c.lens, seqs, q_starts, static_cast<const uint16_t*>(Q), static_cast<uint16_t*>(out), lse,
                         static_cast<float*>(scratch), q_stride, c.pages, c.slots, c.width, c.page_size, c.kv_heads, heads / c.kv_heads, sequences, rows,
-                        dtype == PSA_F16, scale, fastdiv_make((uint32_t)(heads / c.kv_heads)), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
+                        dtype == PSA_F16, 0, scale, fastdiv_make((uint32_t)(heads / c.kv_heads)), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
     const bool wide = (long long)max_q * a.group > 8;        // more than eight columns: two tiles of them share a block's codes
     auto launch = [&](auto width, auto tiles_of_columns) {
         constexpr int D = decltype(width)::value, NT = decltype(tiles_of_columns)::value;
