@@ -147,7 +147,7 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
     s.len = min(held, a.width * a.page_size);
     s.bad = !there || held != s.len;
     s.qtiles = (int)(((long long)s.nq * a.group + COLS - 1) / COLS);
-    s.steps = max((s.len + STEP - 1) / STEP, 1);
+    s.steps = max((int)(((uint32_t)s.len + STEP - 1) / STEP), 1);         // (a length may come within STEP of 2^31)
     return s;
 }
 

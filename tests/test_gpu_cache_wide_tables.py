@@ -26,3 +26,27 @@ def test_wide_tables(lens, q, G, Hkv, d):
         tables[:, :c.tables.shape[1]] = c.tables
         got = psa.psa_cache_attention(Q, c.pool, tables, c.lens, c.seqs, ref.starts(q), Hkv, 16, max_q=max(q))
         assert psa.psa_last_issued()[0] == psa.OK and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("n", [1, 66])
+def test_as_many_tokens_as_a_table_may_hold(n):
+    """2^31 - 16 tokens: the columns of the table name one page over and over, whose tokens carry next to no weight, and at the end another.  66 rows of them have more steps than
+    32 bits count."""
+    d, page, width = 32, 16, (1 << 27) - 1
+    tables = torch.zeros(1, width, dtype=torch.int32, device="cuda")
+    tables[0, -1] = 1
+    g = torch.Generator().manual_seed(8)
+    K, V = torch.randn(32, 1, d, generator=g) * 0.1, torch.randn(32, 1, d, generator=g)
+    K[:16] -= 100 * d ** -0.5
+    K, V = K.to(BF), V.to(BF)
+    pool = torch.zeros(2, psa.psa_cache_page_bytes(1, page, d), dtype=torch.uint8, device="cuda")
+    zero = torch.zeros(n, dtype=torch.int32, device="cuda")
+    two = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda")
+    psa.psa_cache_append(K.cuda(), V.cuda(), pool, two, torch.tensor([32], dtype=torch.int32, device="cuda"), zero[:1], ref.starts([32]), page)
+    k, v = (ref.held(*ref.quantise(x)) for x in (K, V))
+    Q, lse = torch.ones(n, 2, d, dtype=BF, device="cuda"), torch.empty(n, 2, device="cuda")
+    out = psa.psa_cache_attention(Q, pool, tables, torch.tensor([width * page], dtype=torch.int32, device="cuda"), zero, ref.starts([1] * n), 1, page, lse=lse)
+    assert psa.psa_last_issued()[0] == psa.OK
+    # (weights of e^-100: 2^31 of them are 10^-34)
+    ref.close(out[:1], lse[:1], ref.attend(Q[:1], k[16:], v[16:], d ** -0.5), BF, 16, 2 * 2.0 ** -11 + ref.UNIT[BF])
+    assert (out == out[0]).all() and (lse == lse[0]).all()
