@@ -310,7 +310,7 @@ int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
  *   Q [q_rows, heads, d_k], K and V [k_rows, kv_heads, d_k] with row strides q_stride, k_stride, v_stride (they may be parts of one tensor)
  *   q_starts, k_starts   device ints, sequences + 1 each; k_starts = NULL: the keys are the queries' tokens (k_rows = q_rows)
  *   scale                > 0, usually 1 / sqrt(d_k)
- * Supported: d_k any multiple of 8 up to 128, group (heads / kv_heads) up to 128.  `out` must not overlap Q, K, V.
+ * Supported: d_k any multiple of 8 up to 128, group (heads / kv_heads) up to 128, q_rows and k_rows up to 2^31 - 512.  `out` must not overlap Q, K, V.
  */
 int psa_prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts,
                          const int* k_starts, int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d_k, float scale, int dtype, void* out,

@@ -381,6 +381,7 @@ int run_op(size_t scratch, void* stream, Run run) {
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 bool serving_dtype(int dtype) { return dtype == PSA_BF16 || dtype == PSA_F16; }
 bool good_scale(float scale) { return scale > 0.f && scale <= 3.0e38f; }
+constexpr int MOST_PROMPT_ROWS = 0x7ffffe00;    // the kernel rounds tokens and keys up to tiles in 32 bits
 bool cache_head(int d) { return d == 32 || d == 64 || d == 96 || d == 128 || d == 256; }
 bool good_stride(long long stride, long long least) { return stride >= least && stride % 8 == 0 && stride <= (1LL << 38); }
 
@@ -893,6 +894,7 @@ int psa_prompt_attention(const void* Q, const void* K, const void* V, long long 
     g_err_text[0] = 0;
     if (sequences < 0 || q_rows < 0 || (sequences == 0 && q_rows > 0) || k_rows < 0 || heads <= 0 || kv_heads <= 0 || d_k <= 0 || heads % kv_heads) return PSA_ERR_SHAPE;
     if (!k_starts && k_rows != q_rows) return PSA_ERR_SHAPE;
+    if (q_rows > MOST_PROMPT_ROWS || k_rows > MOST_PROMPT_ROWS) return PSA_ERR_SHAPE;
     if (!serving_dtype(dtype) || d_k > 128 || d_k % 8 || heads / kv_heads > 128 || !good_scale(scale)) return PSA_ERR_UNSUPPORTED;
     if (q_rows == 0) return PSA_OK;
     if (!Q || !q_starts || !out || (k_rows > 0 && (!K || !V))) return PSA_ERR_NULL;
