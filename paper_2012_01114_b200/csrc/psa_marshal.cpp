@@ -25,7 +25,14 @@ using at::Tensor;
 using Maybe = std::optional<Tensor>;
 
 [[noreturn]] void refuse(const std::string& text) { throw py::value_error(text); }
-void check(int status, const char* where) {
+// Calls an entry point, without the interpreter's lock: the library may be waiting for a stream in another thread (psa_last_issued), and a call then waits for the library.
+template <class Entry, class... Args>
+void call(const char* where, Entry entry, Args... args) {
+    int status;
+    {
+        py::gil_scoped_release unlocked;
+        status = entry(args...);
+    }
     if (status == PSA_OK) return;
     PyObject* e = PyObject_CallFunction(g_error, "is", status, where);
     if (e) {
@@ -76,10 +83,9 @@ Tensor prompt(const Tensor& Q, const Tensor& K, const Tensor& V, const Tensor& q
     const int64_t kv_heads = K.size(1), n = q_starts.numel() - 1;
     const long long qs = rows_of(Q, "Q", heads, d, Q), ks = rows_of(K, "K", kv_heads, d, Q), vs = rows_of(V, "V", kv_heads, d, Q);
     Tensor o = out ? *out : at::empty({rows, heads * d}, Q.options());
-    check(g_prompt(Q.data_ptr(), K.data_ptr(), V.data_ptr(), qs, ks, vs, ints(q_starts, "q_starts"), k_starts ? ints(*k_starts, "k_starts", n + 1) : nullptr, small(n, "q_starts"),
+    call("psa_prompt_attention", g_prompt, Q.data_ptr(), K.data_ptr(), V.data_ptr(), qs, ks, vs, ints(q_starts, "q_starts"), k_starts ? ints(*k_starts, "k_starts", n + 1) : nullptr, small(n, "q_starts"),
                    small(rows, "Q"), small(K.size(0), "K"), small(heads, "Q"), (int)kv_heads, small(d, "Q"), scale_of(scale, d), type, given(o, "out", rows, heads * d, Q.scalar_type()),
-                   lse ? static_cast<float*>(given(*lse, "lse", rows, heads, at::kFloat)) : nullptr, stream_of(stream)),
-          "psa_prompt_attention");
+                   lse ? static_cast<float*>(given(*lse, "lse", rows, heads, at::kFloat)) : nullptr, stream_of(stream));
     return o;
 }
 
@@ -99,10 +105,9 @@ void append(const Tensor& K, const Tensor& V, const Tensor& pool, const Tensor& 
     if (K.sizes() != V.sizes()) refuse("K and V must have one shape");
     const long long ks = rows_of(K, "K", kv_heads, d, K), vs = rows_of(V, "V", kv_heads, d, K);
     const psa_cache cache = cache_of(pool, tables, lens, kv_heads, page_size, d);
-    check(g_append(&cache, K.data_ptr(), V.data_ptr(), ks, vs, ints(seqs, "seqs"), ints(starts, "starts", n + 1), small(n, "seqs"), small(rows, "K"), type,
+    call("psa_cache_append", g_append, &cache, K.data_ptr(), V.data_ptr(), ks, vs, ints(seqs, "seqs"), ints(starts, "starts", n + 1), small(n, "seqs"), small(rows, "K"), type,
                    k_held ? given(*k_held, "k_held", rows, kv_heads * d, K.scalar_type()) : nullptr, v_held ? given(*v_held, "v_held", rows, kv_heads * d, K.scalar_type()) : nullptr,
-                   stream_of(stream)),
-          "psa_cache_append");
+                   stream_of(stream));
 }
 
 Tensor attention(const Tensor& Q, const Tensor& pool, const Tensor& tables, const Tensor& lens, const Tensor& seqs, const Tensor& q_starts, int64_t kv_heads, int64_t page_size,
@@ -113,10 +118,9 @@ Tensor attention(const Tensor& Q, const Tensor& pool, const Tensor& tables, cons
     const long long qs = rows_of(Q, "Q", heads, d, Q);
     const psa_cache cache = cache_of(pool, tables, lens, kv_heads, page_size, d);
     Tensor o = out ? *out : at::empty({rows, heads * d}, Q.options());
-    check(g_attention(&cache, Q.data_ptr(), qs, ints(seqs, "seqs"), ints(q_starts, "q_starts", n + 1), small(n, "seqs"), small(rows, "Q"), small(heads, "Q"), small(max_q, "max_q"),
+    call("psa_cache_attention", g_attention, &cache, Q.data_ptr(), qs, ints(seqs, "seqs"), ints(q_starts, "q_starts", n + 1), small(n, "seqs"), small(rows, "Q"), small(heads, "Q"), small(max_q, "max_q"),
                       scale_of(scale, d), type, given(o, "out", rows, heads * d, Q.scalar_type()), lse ? static_cast<float*>(given(*lse, "lse", rows, heads, at::kFloat)) : nullptr,
-                      stream_of(stream)),
-          "psa_cache_attention");
+                      stream_of(stream));
     return o;
 }
 
@@ -138,18 +142,17 @@ Pool pool_of(const Tensor& t, int64_t pages) {
 }
 void pages_free(const Tensor& tables, const Tensor& lens, const Tensor& refs, const Tensor& seqs, int64_t page_size, std::optional<int64_t> stream) {
     const psa_pages p = pages_of(tables, lens, refs, page_size);
-    check(g_free(&p, ints(seqs, "seqs"), small(seqs.numel(), "seqs"), stream_of(stream)), "psa_pages_free");
+    call("psa_pages_free", g_free, &p, ints(seqs, "seqs"), small(seqs.numel(), "seqs"), stream_of(stream));
 }
 void pages_fork(const Tensor& tables, const Tensor& lens, const Tensor& refs, const Tensor& parents, const Tensor& children, int64_t page_size, std::optional<int64_t> stream) {
     const psa_pages p = pages_of(tables, lens, refs, page_size);
-    check(g_fork(&p, ints(parents, "parents"), ints(children, "children", parents.numel()), small(parents.numel(), "parents"), stream_of(stream)), "psa_pages_fork");
+    call("psa_pages_fork", g_fork, &p, ints(parents, "parents"), ints(children, "children", parents.numel()), small(parents.numel(), "parents"), stream_of(stream));
 }
 void pages_reserve(const Tensor& tables, const Tensor& lens, const Tensor& refs, const Tensor& pool, const Tensor& seqs, const Tensor& add, int64_t page_size, const Tensor& short_by,
                    std::optional<int64_t> stream) {
     const psa_pages p = pages_of(tables, lens, refs, page_size);
     const Pool q = pool_of(pool, refs.numel());
-    check(g_reserve(&p, q.at, q.page_bytes, q.layers, ints(seqs, "seqs"), ints(add, "add", seqs.numel()), small(seqs.numel(), "seqs"), ints_out(short_by, "short", 1), stream_of(stream)),
-          "psa_pages_reserve");
+    call("psa_pages_reserve", g_reserve, &p, q.at, q.page_bytes, q.layers, ints(seqs, "seqs"), ints(add, "add", seqs.numel()), small(seqs.numel(), "seqs"), ints_out(short_by, "short", 1), stream_of(stream));
 }
 void pages_compact(const Tensor& tables, const Tensor& refs, const Tensor& pool, const Tensor& new_tables, const Tensor& new_refs, const Tensor& new_pool, const Tensor& live,
                    std::optional<int64_t> stream) {
@@ -157,13 +160,12 @@ void pages_compact(const Tensor& tables, const Tensor& refs, const Tensor& pool,
         refuse("new_tables, new_refs and new_pool must have the shapes of tables, refs and pool");
     const psa_pages p = pages_of(tables, std::nullopt, refs, 1);
     const Pool q = pool_of(pool, refs.numel()), r = pool_of(new_pool, refs.numel());
-    check(g_compact(&p, q.at, q.page_bytes, q.layers, ints_out(new_tables, "new_tables"), ints_out(new_refs, "new_refs"), r.at, ints_out(live, "live", 1), stream_of(stream)),
-          "psa_pages_compact");
+    call("psa_pages_compact", g_compact, &p, q.at, q.page_bytes, q.layers, ints_out(new_tables, "new_tables"), ints_out(new_refs, "new_refs"), r.at, ints_out(live, "live", 1), stream_of(stream));
 }
 void pages_copy(const Tensor& pool, const Tensor& new_pool, const Tensor& src, const Tensor& dst, std::optional<int64_t> stream) {
     const Pool q = pool_of(pool, -1), r = pool_of(new_pool, -1);
     if (q.layers != r.layers || q.page_bytes != r.page_bytes) refuse("both pools must have the same layers and page bytes");
-    check(g_copy(q.at, q.pages, r.at, r.pages, q.page_bytes, q.layers, ints(src, "src"), ints(dst, "dst", src.numel()), small(src.numel(), "src"), stream_of(stream)), "psa_pages_copy");
+    call("psa_pages_copy", g_copy, q.at, q.pages, r.at, r.pages, q.page_bytes, q.layers, ints(src, "src"), ints(dst, "dst", src.numel()), small(src.numel(), "src"), stream_of(stream));
 }
 
 void bind(const std::vector<uintptr_t>& f, py::object error) {
