@@ -83,9 +83,9 @@ Tensor prompt(const Tensor& Q, const Tensor& K, const Tensor& V, const Tensor& q
     const int64_t kv_heads = K.size(1), n = q_starts.numel() - 1;
     const long long qs = rows_of(Q, "Q", heads, d, Q), ks = rows_of(K, "K", kv_heads, d, Q), vs = rows_of(V, "V", kv_heads, d, Q);
     Tensor o = out ? *out : at::empty({rows, heads * d}, Q.options());
-    call("psa_prompt_attention", g_prompt, Q.data_ptr(), K.data_ptr(), V.data_ptr(), qs, ks, vs, ints(q_starts, "q_starts"), k_starts ? ints(*k_starts, "k_starts", n + 1) : nullptr, small(n, "q_starts"),
-                   small(rows, "Q"), small(K.size(0), "K"), small(heads, "Q"), (int)kv_heads, small(d, "Q"), scale_of(scale, d), type, given(o, "out", rows, heads * d, Q.scalar_type()),
-                   lse ? static_cast<float*>(given(*lse, "lse", rows, heads, at::kFloat)) : nullptr, stream_of(stream));
+    call("psa_prompt_attention", g_prompt, Q.data_ptr(), K.data_ptr(), V.data_ptr(), qs, ks, vs, ints(q_starts, "q_starts"), k_starts ? ints(*k_starts, "k_starts", n + 1) : nullptr,
+         small(n, "q_starts"), small(rows, "Q"), small(K.size(0), "K"), small(heads, "Q"), (int)kv_heads, small(d, "Q"), scale_of(scale, d), type, given(o, "out", rows, heads * d, Q.scalar_type()),
+         lse ? static_cast<float*>(given(*lse, "lse", rows, heads, at::kFloat)) : nullptr, stream_of(stream));
     return o;
 }
 
@@ -106,8 +106,8 @@ void append(const Tensor& K, const Tensor& V, const Tensor& pool, const Tensor& 
     const long long ks = rows_of(K, "K", kv_heads, d, K), vs = rows_of(V, "V", kv_heads, d, K);
     const psa_cache cache = cache_of(pool, tables, lens, kv_heads, page_size, d);
     call("psa_cache_append", g_append, &cache, K.data_ptr(), V.data_ptr(), ks, vs, ints(seqs, "seqs"), ints(starts, "starts", n + 1), small(n, "seqs"), small(rows, "K"), type,
-                   k_held ? given(*k_held, "k_held", rows, kv_heads * d, K.scalar_type()) : nullptr, v_held ? given(*v_held, "v_held", rows, kv_heads * d, K.scalar_type()) : nullptr,
-                   stream_of(stream));
+         k_held ? given(*k_held, "k_held", rows, kv_heads * d, K.scalar_type()) : nullptr, v_held ? given(*v_held, "v_held", rows, kv_heads * d, K.scalar_type()) : nullptr,
+         stream_of(stream));
 }
 
 Tensor attention(const Tensor& Q, const Tensor& pool, const Tensor& tables, const Tensor& lens, const Tensor& seqs, const Tensor& q_starts, int64_t kv_heads, int64_t page_size,
@@ -118,9 +118,9 @@ Tensor attention(const Tensor& Q, const Tensor& pool, const Tensor& tables, cons
     const long long qs = rows_of(Q, "Q", heads, d, Q);
     const psa_cache cache = cache_of(pool, tables, lens, kv_heads, page_size, d);
     Tensor o = out ? *out : at::empty({rows, heads * d}, Q.options());
-    call("psa_cache_attention", g_attention, &cache, Q.data_ptr(), qs, ints(seqs, "seqs"), ints(q_starts, "q_starts", n + 1), small(n, "seqs"), small(rows, "Q"), small(heads, "Q"), small(max_q, "max_q"),
-                      scale_of(scale, d), type, given(o, "out", rows, heads * d, Q.scalar_type()), lse ? static_cast<float*>(given(*lse, "lse", rows, heads, at::kFloat)) : nullptr,
-                      stream_of(stream));
+    call("psa_cache_attention", g_attention, &cache, Q.data_ptr(), qs, ints(seqs, "seqs"), ints(q_starts, "q_starts", n + 1), small(n, "seqs"), small(rows, "Q"), small(heads, "Q"),
+         small(max_q, "max_q"), scale_of(scale, d), type, given(o, "out", rows, heads * d, Q.scalar_type()), lse ? static_cast<float*>(given(*lse, "lse", rows, heads, at::kFloat)) : nullptr,
+         stream_of(stream));
     return o;
 }
 
@@ -152,7 +152,8 @@ void pages_reserve(const Tensor& tables, const Tensor& lens, const Tensor& refs,
                    std::optional<int64_t> stream) {
     const psa_pages p = pages_of(tables, lens, refs, page_size);
     const Pool q = pool_of(pool, refs.numel());
-    call("psa_pages_reserve", g_reserve, &p, q.at, q.page_bytes, q.layers, ints(seqs, "seqs"), ints(add, "add", seqs.numel()), small(seqs.numel(), "seqs"), ints_out(short_by, "short", 1), stream_of(stream));
+    call("psa_pages_reserve", g_reserve, &p, q.at, q.page_bytes, q.layers, ints(seqs, "seqs"), ints(add, "add", seqs.numel()), small(seqs.numel(), "seqs"), ints_out(short_by, "short", 1),
+         stream_of(stream));
 }
 void pages_compact(const Tensor& tables, const Tensor& refs, const Tensor& pool, const Tensor& new_tables, const Tensor& new_refs, const Tensor& new_pool, const Tensor& live,
                    std::optional<int64_t> stream) {
