@@ -6,6 +6,7 @@ The shared objects land next to this file so that they travel with the source tr
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
@@ -51,8 +52,8 @@ def build_marshal(force: bool = False, verbose: bool = False) -> str:
     return MARSHAL
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    build_marshal(force, verbose)
+def build_library(force: bool = False, verbose: bool = False) -> str:
+    """libpsa.so; needs nvcc and its host compiler only."""
     newest = max(os.path.getmtime(p) for p in _deps())
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= newest:
         return LIB
@@ -67,6 +68,16 @@ def build(force: bool = False, verbose: bool = False) -> str:
     subprocess.check_call(cmd)
     os.replace(tmp, LIB)
     return LIB
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    """The library, and behind it the binding's compiled part, which needs torch: without torch there is no Python to call it from, and the library stands alone."""
+    lib = build_library(force, verbose)
+    if importlib.util.find_spec("torch") is None:
+        print("torch is not installed: psa_marshal.so, the compiled part of the Python binding, is not built", file=sys.stderr)
+    else:
+        build_marshal(force, verbose)
+    return lib
 
 
 if __name__ == "__main__":
