@@ -444,7 +444,7 @@ def psa_pages_fork(tables, lens, refs, parents, children, page_size, stream=None
 
 def psa_pages_reserve(tables, lens, refs, pool, seqs, add, page_size, short, stream=None):
     """Room for add[i] more tokens of slot seqs[i]: lens grows, pages are taken, a shared last page that is written to is copied in all layers of the pool
-    ([pages, page bytes] or [layers, pages, page bytes]).  short (int32, one number): how many pages are missing; if any, nothing changes."""
+    ([pages, page bytes] or [layers, pages, page bytes]), pages behind a length that was taken back are given back first.  short (int32, one number): how many pages are missing; if any, nothing changes."""
     (_marshal or marshal()).pages_reserve(tables, lens, refs, pool, seqs, add, page_size, short, _handle(stream))
 
 

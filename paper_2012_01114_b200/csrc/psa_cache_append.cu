@@ -7,10 +7,10 @@
 //
 // To read and write: 2 bytes and 5 bits per number, 2 bytes more when the held values are asked for.  A warp takes the two tokens of a pair (they share
 // the words of V's codes and scales), K and V, eight lanes a group (four channels each, one load of 8 bytes), for one head after another, the loads of the next
-// head ahead of the work on this one.  Where there are few tokens a warp has one head.  What bounds this is the number of instructions (a plain form has 50 a number, this
-// one 29): least and greatest numbers are found in the inputs' own 16 bits, two at a time, the greatest as the least of the negated ones in the other half of the
+// head ahead of the work on this one.  Where there are few tokens a warp has one head.  What it spends its time on is instructions (the first form had 50 a number, this
+// one 29, and 68 % of the issue slots; the rest are waits for their results): least and greatest numbers are found in the inputs' own 16 bits, two at a time, the greatest as the least of the negated ones in the other half of the
 // same register; the numbers of a group are worked out once, a group per lane, and handed round; and a code is the low end of y + 1.5 2^23.
-// Measured: 16 prompts of up to 2500 tokens, 8 heads of 128 (14 million numbers) with held values 18.1 us, 3.7 TB/s, 68 % of the issue slots; the plain form 30.7.
+// Measured: 16 prompts of up to 2500 tokens, 8 heads of 128 (14 million numbers) with held values 18.1 us, 3.7 TB/s; the first form 30.7.
 #include <algorithm>
 #include <type_traits>
 

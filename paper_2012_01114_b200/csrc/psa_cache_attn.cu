@@ -19,9 +19,10 @@
 // ring of blocks of its own filled by bulk copies, and are joined through shared memory; a row of several parts is joined by the CTA that finishes last, in
 // the parts' order, so that results do not depend on who that is.  Where there are more rows than CTAs, short ones go to single warps, eight a CTA (looking up, converting the
 // queries and joining cost a CTA 8000 cycles a row, the 16 steps of a row of 512 tokens 7000).
-// Measured, 32 heads on 8 of d = 128, one query each: two sequences of up to 131,072 tokens 49.0 us a call (204 MB: 4.2 TB/s; over a million tokens 5.3 TB/s, the
-// loads without the products 6.4), 64 of up to 8000 31.8 us (68 MB: 2.2 TB/s).  Bound by the issue of instructions (59 % of the slots, 48 % of the memory's rate at the
-// first size), and by what comes once a call: finding the parts 2.5 us, look-ups and queries 1.6, the CTA's join 3, the join of the parts 4 to 5.
+// Measured, 32 heads on 8 of d = 128, one query each: two sequences of up to 131,072 tokens 49.1 us a call (204 MB: 4.2 TB/s; over a million tokens 5.3 TB/s, the
+// loads without the products 6.4), 64 of up to 8000 32.0 us (68 MB: 2.2 TB/s).  59 % of the issue slots and 48 % of the memory's rate at the first size: warps wait for each
+// other's slots, for results of a fixed latency and for the integer pipe in turn.
+// What comes once a call: finding the parts 2.5 us, look-ups and queries 1.6, the CTA's join 3, the join of the parts 4 to 5.
 #include <type_traits>
 
 #include "psa_cache.cuh"

@@ -9,8 +9,9 @@
 //   copy     pages by list
 // Free pages are those without references, and are handed out in ascending order in the order of the list: what a call does depends on its arguments alone,
 // not on the order in which CTAs run.  Tables and counts are a few hundred KB at most and are worked on by one CTA (latency bounds it); pages are
-// moved by the whole GPU (the copy rate of the memory bounds it).  Measured: compaction of a pool of 16 layers, 330 MB read and written
-// in 57 us (5.8 TB/s), 7 of them the map.
+// moved by the whole GPU (the copy rate of the memory bounds it).  Measured: compaction of a pool of one layer, 330 MB read and written
+// in 57 us (5.8 TB/s), 7 of them the map.  All new pages of a sequence are written by one thread: room for a prompt of 131,072 tokens in pages of 16 takes 450 us, for 64 of
+// 2048 25.
 #include "psa_internal.h"
 #include "sm100.cuh"
 
