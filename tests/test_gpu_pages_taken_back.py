@@ -92,6 +92,7 @@ def test_shared_pages_behind_a_length(n):
 def test_drafts_at_random(seed):
     r = random.Random(seed)
     b = Both(30, 9, 100, r.choice([16, 32]), seed=seed)
+    b.reserve([0], [0])                                      # (a call, for whose status `same` asks)
     alive = []
     for step in range(60):
         what = r.random()
