@@ -355,6 +355,67 @@ int psa_cache_attention(const psa_cache* cache, const void* Q, long long q_strid
 size_t psa_cache_workspace_bytes(int d_k);
 
 /*
+ * Answering with drafted tokens: a small model drafts tokens for a sequence, the large one looks at all of them in one pass, random numbers decide which stand, and the cache keeps those.
+ * Drafted tokens form a tree.  `parents` (device ints [rows]) names each row's parent among the rows of its sequence, an earlier one (0 .. its own place - 1), or -1; a chain is -1, 0, 1, ...
+ * Anything else is taken for -1 and reported (PSA_ERR_SHAPE).  Up to PSA_TREE_MOST rows a sequence: one with more is left out and reported.
+ */
+#define PSA_TREE_MOST 1024
+
+/*
+ * psa_cache_append with the position rotation applied on the way, and the queries of the same tokens turned in the same launch.  A pair of channels (x, y) of a query or key becomes
+ * amplitude * (x cos a - y sin a, y cos a + x sin a), a = position * freqs[i], i < rot / 2 the number of the pair: channels i and i + rot / 2 of the head, or, interleaved, 2 i and 2 i + 1.  The
+ * head's channels from `rot` on, and values, stay as they are.  Row r of sequence b has position lens[seqs[b]] - (starts[b + 1] - starts[b]) + depths[r]: its depth is counted from the
+ * sequence's first new token, and tokens of one depth have one position.  depths NULL: rows follow one another (0, 1, ...).  Where a token is stored does not depend on its depth.
+ * Angles are formed in 64 bits and lose nothing at far positions.  A turned key is rounded to dtype, and the cache then holds what psa_cache_append would make of it.
+ *   freqs       device doubles [rot / 2], radians per position, finite (whatever scaling long contexts need is in them and in the amplitude)
+ *   Q           device, [rows, heads, d_k] with row stride q_stride, or NULL      q_out   dense, same shape; may be Q if that is dense
+ * Everything else as for psa_cache_append (k_held receives the turned keys as the cache holds them; NULL: not wanted).  Rows of a slot that does not exist are left alone.
+ * Supported: rot any multiple of 8 up to d_k, any finite amplitude; rows * d_k / 8 up to 2^31 - 2^16 where Q is given.
+ */
+typedef struct {
+    const double* freqs;
+    float amplitude;
+    int rot, interleaved;
+} psa_rotary;
+int psa_cache_append_rotary(const psa_cache* cache, const psa_rotary* rotary, const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride,
+                            const int* depths, const int* seqs, const int* starts, int sequences, int rows, int heads, int dtype, void* q_out, void* k_held, void* v_held, void* stream);
+
+/*
+ * psa_cache_attention for trees: the sequence's last nq tokens are the tree's, in the order of its queries, and query i sees of these its own token and its ancestors', and all tokens ahead of
+ * them.  (With a chain for parents it is psa_cache_attention.)  max_q up to PSA_TREE_MOST.  Workspace psa_cache_workspace_bytes; everything else as there.
+ */
+int psa_tree_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
+                       int max_q, float scale, int dtype, void* out, float* lse, void* stream);
+
+/*
+ * Which drafted tokens stand.  A sequence's first row is its last known token, the root; row r's logits say what follows its token.  From the root on, the children of a row are tried in their
+ * order.  With p = softmax(logits / temperature), q = softmax(drafts / temperature) of the row and w = p, Z = 1 at first, child m with token x stands if u q(x) Z < w(x), u being
+ * its number in `uniform`; otherwise w becomes max(w / Z - q, 0) and Z its sum.  distinct != 0: siblings were drawn without replacement, and q, behind every one of them, is what is left
+ * of it without that token, made to sum to one again (a token that a sibling has had is passed over).  drafts NULL: the drafts are certain, q is one at the child's token (with these, too, a token
+ * that a sibling has had is passed over).  The path goes on from a child that stands.  Where none does, the next token is drawn: the first one at which the sum of w over tokens 0, 1, .. passes
+ * u of the root's row times Z (from p, where nothing is left of w).  Tokens that stand, with the next one behind them, are distributed as the large model's own.
+ * temperature 0: a child stands if its token is the likeliest (the first of equal ones), which is else the next token; drafts and uniform are not used.
+ *   logits, drafts      device, [rows, vocab] with row strides >= vocab (any, and of any alignment), of dtype PSA_F32, PSA_BF16 or PSA_F16; -inf: never.  Rows that are not on the path are not read
+ *   tokens, parents     device ints [rows]; the roots' are not used (a root's parent is -1).  Rows of -1 but the first are not reached.  A token outside 0 .. vocab - 1 never stands, and is reported
+ *   uniform             device floats [rows], 0 <= u < 1        temperatures   device floats [sequences], >= 0, finite; NULL: 1
+ *   path                device ints [rows]: behind starts[b], the places in the sequence of the root (0) and of the tokens that stand, then -1
+ *   accepted, next      device ints [sequences]: how many stand (without the root), and the token behind them
+ * A sequence without rows gets 0 and -1, and so does one whose rows are too many or whose temperature is none (reported).  A row on the path with a NaN, with +inf or with nothing but -inf ends
+ * it there: the next token is -1, and psa_last_issued returns PSA_ERR_NUMERIC.
+ */
+int psa_verify_drafts(const void* logits, long long logit_stride, const void* drafts, long long draft_stride, int vocab, int dtype, const int* tokens, const int* parents,
+                      const int* starts, int sequences, int rows, const float* temperatures, const float* uniform, int distinct, int* path, int* accepted, int* next, void* stream);
+
+/*
+ * The cache keeps what stands: of a sequence's last nq = starts[b + 1] - starts[b] tokens those at places path[starts[b] + i], i = 0 .. accepted[b], become the first ones, in all layers, and the
+ * length becomes lens - nq + 1 + accepted[b].  (path and accepted as psa_verify_drafts leaves them.)  cache->pool is [layers][pages][page bytes]; the pages must be the sequence's own as
+ * far as the tree's tokens are in them, as psa_pages_reserve makes them.  Pages behind the new length are given back by the next psa_pages_reserve.
+ *   new_lens   device ints [slots], may be cache->lens; lengths of the listed slots are written, of the others not
+ * Lists hold distinct slots.  A sequence whose path does not ascend from 0 within the tree, or that holds fewer tokens than the tree, is left as it is and reported; one without rows is left as it is.
+ */
+int psa_cache_keep(const psa_cache* cache, int layers, const int* seqs, const int* starts, const int* path, const int* accepted, int sequences, int rows, int* new_lens, void* stream);
+
+/*
  * Who holds which page.  tables and lens as in psa_cache (the same arrays serve all layers), refs: device ints [pages], how many tables name a page; a page with
  * none is free.  All calls work in stream order on the device; free pages are handed out in ascending order, in the order of the list.
  * Lists hold distinct slots.  Pools are [layers][pages][page_bytes], page_bytes a multiple of 16.

@@ -26,7 +26,7 @@ EXPORTS = ("psa_attention", "psa_attention_f32", "psa_attention_core", "psa_atte
            "psa_last_cuda_error", "psa_profile_begin", "psa_profile_end", "psa_attention_sym_f32_noalloc",
            "psa_attention_block", "psa_block_workspace_bytes", "psa_last_rescales", "psa_selftest_wait_expiry", "psa_measure_pipe_rates", "psa_attention_core_host", "psa_attention_block_residual",
            "psa_prompt_attention", "psa_prompt_workspace_bytes", "psa_cache_page_bytes", "psa_cache_append", "psa_cache_attention", "psa_cache_workspace_bytes", "psa_pages_free",
-           "psa_pages_fork", "psa_pages_reserve", "psa_pages_compact", "psa_pages_copy", "psa_pages_workspace_bytes")
+           "psa_cache_append_rotary", "psa_tree_attention", "psa_verify_drafts", "psa_cache_keep", "psa_pages_fork", "psa_pages_reserve", "psa_pages_compact", "psa_pages_copy", "psa_pages_workspace_bytes")
 
 
 class PsaError(RuntimeError):
@@ -53,6 +53,11 @@ class PipeRates(ctypes.Structure):
 class Cache(ctypes.Structure):
     """psa_cache: a layer's pool with the tables and lengths of its sequences."""
     _fields_ = [(k, ctypes.c_void_p) for k in ("pool", "tables", "lens")] + [(k, ctypes.c_int) for k in ("pages", "slots", "width", "page_size", "kv_heads", "d_k")]
+
+
+class Rotary(ctypes.Structure):
+    """psa_rotary: what turns by a token's position."""
+    _fields_ = [("freqs", ctypes.c_void_p), ("amplitude", ctypes.c_float), ("rot", ctypes.c_int), ("interleaved", ctypes.c_int)]
 
 
 class Pages(ctypes.Structure):
@@ -111,6 +116,10 @@ def lib() -> ctypes.CDLL:
         L.psa_prompt_attention.argtypes = [vp, vp, vp, ll, ll, ll, vp, vp, ci, ci, ci, ci, ci, ci, cf, ci, vp, vp, vp]
         L.psa_cache_append.argtypes = [cache, vp, vp, ll, ll, vp, vp, ci, ci, ci, vp, vp, vp]
         L.psa_cache_attention.argtypes = [cache, vp, ll, vp, vp, ci, ci, ci, ci, cf, ci, vp, vp, vp]
+        L.psa_cache_append_rotary.argtypes = [cache, ctypes.POINTER(Rotary), vp, vp, vp, ll, ll, ll, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, vp]
+        L.psa_tree_attention.argtypes = [cache, vp, ll, vp, vp, vp, ci, ci, ci, ci, cf, ci, vp, vp, vp]
+        L.psa_verify_drafts.argtypes = [vp, ll, vp, ll, ci, ci, vp, vp, vp, ci, ci, vp, vp, ci, vp, vp, vp, vp]
+        L.psa_cache_keep.argtypes = [cache, ci, vp, vp, vp, vp, ci, ci, vp, vp]
         L.psa_pages_free.argtypes = [pages, vp, ci, vp]
         L.psa_pages_fork.argtypes = [pages, vp, vp, ci, vp]
         L.psa_pages_reserve.argtypes = [pages, vp, ll, ci, vp, vp, ci, vp, vp]
@@ -123,7 +132,7 @@ def lib() -> ctypes.CDLL:
         for f in ("psa_prompt_workspace_bytes", "psa_cache_page_bytes", "psa_cache_workspace_bytes", "psa_pages_workspace_bytes"):
             getattr(L, f).restype = cs
         for f in ("psa_prompt_attention", "psa_cache_append", "psa_cache_attention", "psa_pages_free", "psa_pages_fork", "psa_pages_reserve",
-                  "psa_pages_compact", "psa_pages_copy"):
+                  "psa_pages_compact", "psa_pages_copy", "psa_cache_append_rotary", "psa_tree_attention", "psa_verify_drafts", "psa_cache_keep"):
             getattr(L, f).restype = ci
         for f in ("psa_attention", "psa_attention_f32", "psa_attention_core", "psa_attention_host",
                   "psa_skip_count", "psa_last_issued", "psa_set_workspace"):
@@ -254,7 +263,7 @@ def psa_last_issued(stream=None):
     """(device status, measured census) of the last call; waits for the stream."""
     c = Counts()
     rc = lib().psa_last_issued(_stream(stream), ctypes.byref(c))
-    if rc not in (OK, ERR_TIMEOUT, ERR_SHAPE):
+    if rc not in (OK, ERR_TIMEOUT, ERR_SHAPE, ERR_NUMERIC):
         raise PsaError(rc, "psa_last_issued")
     return rc, c.as_dict()
 
@@ -387,7 +396,8 @@ def marshal():
         spec.loader.exec_module(m)
         L = lib()
         m.bind([ctypes.cast(f, ctypes.c_void_p).value for f in (L.psa_prompt_attention, L.psa_cache_append, L.psa_cache_attention, L.psa_pages_free, L.psa_pages_fork,
-                                                                L.psa_pages_reserve, L.psa_pages_compact, L.psa_pages_copy)], PsaError)
+                                                                L.psa_pages_reserve, L.psa_pages_compact, L.psa_pages_copy, L.psa_cache_append_rotary, L.psa_tree_attention,
+                                                                L.psa_verify_drafts, L.psa_cache_keep)], PsaError)
         _marshal = m
     return _marshal
 
@@ -430,6 +440,29 @@ def psa_cache_attention(Q, pool, tables, lens, seqs, q_starts, kv_heads, page_si
     """Attention of the last query tokens of slots seqs over the cache in 4 bits: Q [rows, heads, d] (rows may have a stride), sequence b owns rows q_starts[b] ..
     q_starts[b + 1] - 1 -> out [rows, heads * d].  max_q: bound on the queries of a sequence."""
     return (_marshal or marshal()).attention(Q, pool, tables, lens, seqs, q_starts, kv_heads, page_size, max_q, scale, out, lse, _handle(stream))
+
+
+def psa_cache_append_rotary(K, V, pool, tables, lens, seqs, starts, page_size, freqs, Q=None, depths=None, interleaved=False, amplitude=1.0, q_out=None, k_held=None, v_held=None, stream=None):
+    """psa_cache_append of keys turned by their positions, and the queries of the same tokens turned likewise -> q_out (None without Q).  freqs: float64 [rot / 2], radians per position, for the
+    first rot channels of a head; depths: int32 [rows], positions counted from the sequence's first new token (None: 0, 1, ..); Q [rows, heads, d], q_out dense (may be Q)."""
+    return (_marshal or marshal()).append_rotary(K, V, pool, tables, lens, seqs, starts, page_size, freqs, Q, depths, interleaved, amplitude, q_out, k_held, v_held, _handle(stream))
+
+
+def psa_tree_attention(Q, pool, tables, lens, seqs, q_starts, parents, kv_heads, page_size, max_q, scale=None, out=None, lse=None, stream=None):
+    """psa_cache_attention for trees of drafted tokens: a query sees the tokens ahead of the tree, its own and its ancestors'.  parents: int32 [rows], places in the sequence's rows or -1."""
+    return (_marshal or marshal()).tree(Q, pool, tables, lens, seqs, q_starts, parents, kv_heads, page_size, max_q, scale, out, lse, _handle(stream))
+
+
+def psa_verify_drafts(logits, tokens, parents, starts, uniform, path=None, accepted=None, next_token=None, drafts=None, temperatures=None, distinct=True, stream=None):
+    """Which drafted tokens stand -> path [rows], accepted [sequences], next token [sequences], all int32.  logits, drafts (None: certain) [rows, vocab]; tokens, parents int32 [rows], a sequence's
+    first row its last known token; uniform fp32 [rows]; temperatures fp32 [sequences] (None: 1; 0: the likeliest token); distinct: siblings were drawn without replacement."""
+    return (_marshal or marshal()).verify(logits, tokens, parents, starts, uniform, path, accepted, next_token, drafts, temperatures, distinct, _handle(stream))
+
+
+def psa_cache_keep(pool, tables, lens, seqs, starts, path, accepted, kv_heads, page_size, new_lens=None, stream=None):
+    """The tokens on the path move to the front of their tree, in all layers of the pool ([pages, page bytes] or [layers, pages, page bytes]), and the sequences end behind them.  new_lens: where
+    the lengths go (None: lens)."""
+    (_marshal or marshal()).keep(pool, tables, lens, seqs, starts, path, accepted, kv_heads, page_size, new_lens, _handle(stream))
 
 
 def psa_pages_free(tables, lens, refs, seqs, page_size, stream=None):

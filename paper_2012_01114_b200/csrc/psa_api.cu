@@ -931,26 +931,94 @@ int psa_cache_append(const psa_cache* cache, const void* K, const void* V, long 
     if (!good_stride(k_stride, least) || !good_stride(v_stride, least) || ((long long)rows + 1) / 2 * cache->kv_heads > 8LL * 0x7ffffff0LL) return PSA_ERR_SHAPE;
     if (!aligned16(K) || !aligned16(V) || !aligned16(k_held) || !aligned16(v_held) || !aligned4(seqs) || !aligned4(starts)) return PSA_ERR_ALIGN;
     return run_op(0, stream, [&](const OpCall& c) {
-        return cache_append(*cache, K, V, k_stride, v_stride, seqs, starts, sequences, rows, dtype, k_held, v_held, c.dc, c.dc_next, static_cast<cudaStream_t>(stream));
+        return cache_append(*cache, nullptr, nullptr, K, V, 0, k_stride, v_stride, nullptr, seqs, starts, sequences, rows, 0, dtype, nullptr, k_held, v_held, c.dc, c.dc_next,
+                            static_cast<cudaStream_t>(stream));
+    });
+}
+
+int psa_cache_append_rotary(const psa_cache* cache, const psa_rotary* rotary, const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride,
+                            const int* depths, const int* seqs, const int* starts, int sequences, int rows, int heads, int dtype, void* q_out, void* k_held, void* v_held, void* stream) {
+    g_err_text[0] = 0;
+    const int rc = check_cache(cache);
+    if (rc != PSA_OK) return rc;
+    if (sequences < 0 || rows < 0 || (sequences == 0 && rows > 0)) return PSA_ERR_SHAPE;
+    if (!rotary || !rotary->freqs) return PSA_ERR_NULL;
+    if (rotary->rot <= 0 || rotary->rot > cache->d_k) return PSA_ERR_SHAPE;
+    if (!serving_dtype(dtype) || rotary->rot % 8 || !(rotary->amplitude >= -3.0e38f && rotary->amplitude <= 3.0e38f)) return PSA_ERR_UNSUPPORTED;
+    if (Q && (heads <= 0 || (long long)heads * cache->d_k > 0x7fffffffLL || (long long)rows * (cache->d_k / 8) > 0x7fff0000LL)) return PSA_ERR_SHAPE;
+    if (rows == 0) return PSA_OK;
+    if (!K || !V || !seqs || !starts || (Q && !q_out)) return PSA_ERR_NULL;
+    const long long least = (long long)cache->kv_heads * cache->d_k;
+    if (!good_stride(k_stride, least) || !good_stride(v_stride, least) || ((long long)rows + 1) / 2 * cache->kv_heads > 8LL * 0x7ffffff0LL) return PSA_ERR_SHAPE;
+    if (Q && !good_stride(q_stride, (long long)heads * cache->d_k)) return PSA_ERR_SHAPE;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(q_out) || !aligned16(k_held) || !aligned16(v_held) || !aligned4(depths) || !aligned4(seqs) || !aligned4(starts) ||
+        (reinterpret_cast<uintptr_t>(rotary->freqs) & 7u))
+        return PSA_ERR_ALIGN;
+    return run_op(0, stream, [&](const OpCall& c) {
+        return cache_append(*cache, rotary, Q, K, V, q_stride, k_stride, v_stride, depths, seqs, starts, sequences, rows, heads, dtype, q_out, k_held, v_held, c.dc, c.dc_next,
+                            static_cast<cudaStream_t>(stream));
     });
 }
 
 size_t psa_cache_workspace_bytes(int d_k) { return cache_head(d_k) ? COUNTER_BYTES + cache_attention_scratch_bytes(d_k) : 0; }
 
-int psa_cache_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
-                        int max_q, float scale, int dtype, void* out, float* lse, void* stream) {
+static int attend_to_cache(const psa_cache* cache, const void* Q, long long q_stride, bool tree, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
+                           int max_q, float scale, int dtype, void* out, float* lse, void* stream) {
     g_err_text[0] = 0;
     const int rc = check_cache(cache);
     if (rc != PSA_OK) return rc;
     if (sequences < 0 || rows < 0 || (sequences == 0 && rows > 0) || heads <= 0 || heads % cache->kv_heads || max_q <= 0) return PSA_ERR_SHAPE;
-    if (!serving_dtype(dtype) || !good_scale(scale)) return PSA_ERR_UNSUPPORTED;
+    if (!serving_dtype(dtype) || !good_scale(scale) || (tree && max_q > PSA_TREE_MOST)) return PSA_ERR_UNSUPPORTED;
     if (rows == 0) return PSA_OK;
-    if (!Q || !seqs || !q_starts || !out) return PSA_ERR_NULL;
+    if (!Q || !seqs || !q_starts || !out || (tree && !parents)) return PSA_ERR_NULL;
     if (!good_stride(q_stride, (long long)heads * cache->d_k) || (long long)rows * (heads / cache->kv_heads) > 0x7fffff00LL) return PSA_ERR_SHAPE;
-    if (!aligned16(Q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) || !aligned4(q_starts)) return PSA_ERR_ALIGN;
+    if (!aligned16(Q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) || !aligned4(q_starts) || !aligned4(parents)) return PSA_ERR_ALIGN;
     return run_op(cache_attention_scratch_bytes(cache->d_k), stream, [&](const OpCall& c) {
-        return cache_attention(*cache, Q, q_stride, seqs, q_starts, sequences, rows, heads, max_q, scale, dtype, out, lse, c.ws + COUNTER_BYTES, c.dc, c.dc_next,
+        return cache_attention(*cache, Q, q_stride, parents, seqs, q_starts, sequences, rows, heads, max_q, scale, dtype, out, lse, c.ws + COUNTER_BYTES, c.dc, c.dc_next,
                                static_cast<cudaStream_t>(stream));
+    });
+}
+
+int psa_cache_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
+                        int max_q, float scale, int dtype, void* out, float* lse, void* stream) {
+    return attend_to_cache(cache, Q, q_stride, false, nullptr, seqs, q_starts, sequences, rows, heads, max_q, scale, dtype, out, lse, stream);
+}
+
+int psa_tree_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
+                       int max_q, float scale, int dtype, void* out, float* lse, void* stream) {
+    return attend_to_cache(cache, Q, q_stride, true, parents, seqs, q_starts, sequences, rows, heads, max_q, scale, dtype, out, lse, stream);
+}
+
+int psa_verify_drafts(const void* logits, long long logit_stride, const void* drafts, long long draft_stride, int vocab, int dtype, const int* tokens, const int* parents,
+                      const int* starts, int sequences, int rows, const float* temperatures, const float* uniform, int distinct, int* path, int* accepted, int* next, void* stream) {
+    g_err_text[0] = 0;
+    if (sequences < 0 || rows < 0 || (sequences == 0 && rows > 0) || vocab <= 0) return PSA_ERR_SHAPE;
+    if (!serving_dtype(dtype) && dtype != PSA_F32) return PSA_ERR_UNSUPPORTED;
+    if (sequences == 0) return PSA_OK;
+    if (!starts || !accepted || !next || (rows > 0 && (!logits || !tokens || !parents || !uniform || !path))) return PSA_ERR_NULL;
+    const long long most = 1LL << 38;
+    if (rows > 0 && (logit_stride < vocab || logit_stride > most || (drafts && (draft_stride < vocab || draft_stride > most)))) return PSA_ERR_SHAPE;
+    const uintptr_t item = dtype == PSA_F32 ? 4 : 2;
+    if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(drafts)) & (item - 1)) return PSA_ERR_ALIGN;
+    if (!aligned4(tokens) || !aligned4(parents) || !aligned4(starts) || !aligned4(temperatures) || !aligned4(uniform) || !aligned4(path) || !aligned4(accepted) || !aligned4(next))
+        return PSA_ERR_ALIGN;
+    return run_op(0, stream, [&](const OpCall& c) {
+        return verify_drafts(logits, logit_stride, drafts, draft_stride, vocab, dtype, tokens, parents, starts, sequences, rows, temperatures, uniform, distinct != 0, path, accepted,
+                             next, c.dc, c.dc_next, static_cast<cudaStream_t>(stream));
+    });
+}
+
+int psa_cache_keep(const psa_cache* cache, int layers, const int* seqs, const int* starts, const int* path, const int* accepted, int sequences, int rows, int* new_lens, void* stream) {
+    g_err_text[0] = 0;
+    const int rc = check_cache(cache);
+    if (rc != PSA_OK) return rc;
+    if (layers <= 0 || sequences < 0 || rows < 0 || (sequences == 0 && rows > 0)) return PSA_ERR_SHAPE;
+    if (sequences == 0 || rows == 0) return PSA_OK;
+    if (!seqs || !starts || !path || !accepted || !new_lens) return PSA_ERR_NULL;
+    if ((long long)layers * cache->kv_heads > 0x7fffffffLL || (long long)layers * cache->kv_heads * sequences > 0x7fffff00LL) return PSA_ERR_SHAPE;
+    if (!aligned4(seqs) || !aligned4(starts) || !aligned4(path) || !aligned4(accepted) || !aligned4(new_lens)) return PSA_ERR_ALIGN;
+    return run_op(0, stream, [&](const OpCall& c) {
+        return cache_keep(*cache, layers, seqs, starts, path, accepted, sequences, rows, new_lens, c.dc, c.dc_next, static_cast<cudaStream_t>(stream));
     });
 }
 

@@ -11,6 +11,12 @@
 // one 29, and 68 % of the issue slots; the rest are waits for their results): least and greatest numbers are found in the inputs' own 16 bits, two at a time, the greatest as the least of the negated ones in the other half of the
 // same register; the numbers of a group are worked out once, a group per lane, and handed round; and a code is the low end of y + 1.5 2^23.
 // Measured: 16 prompts of up to 2500 tokens, 8 heads of 128 (14 million numbers) with held values 18.1 us, 3.7 TB/s; the first form 30.7.
+//
+// With rotation (ROT): a pair of channels (a, b) of a key becomes A (a cos - b sin, b cos + a sin), the angle being the token's position times the pair's frequency, and
+// is rounded to the inputs' type, so that the cache holds the same bytes as if a turned tensor had been appended.  Angles are kept as fractions of a turn in 64 bits: a
+// frequency becomes one once, and the product with the position wraps by itself where whole turns drop out, so that position 2^31 costs no accuracy and no division; sine and
+// cosine of what is left are good to 2^-23.  They are worked out once a token and channel for all heads that a warp takes.  The queries are turned by further blocks of the
+// same launch: a thread has four pairs of channels of one token, for one head after another.
 #include <algorithm>
 #include <type_traits>
 
@@ -35,6 +41,29 @@ struct AppendArgs {
     int heads_per_warp, units;                  // units: pairs of tokens, see unit_of
     FastDiv by_chunks, by_page;                 // by warps per unit, by tokens of a page
 };
+// What turns, and the queries (q null: none).
+struct RotaryArgs {
+    const double* freqs;
+    const int* depths;
+    float amplitude;
+    int rot, interleaved;
+    const uint16_t* q;
+    uint16_t* q_out;
+    long long q_stride;
+    int heads, key_blocks;                      // blocks below key_blocks append, those from there on turn queries
+    FastDiv by_slots, by_groups;                // by threads of a head (eight channels each), by groups of heads of a row
+};
+
+// Position times frequency, as sine and cosine.  freq / 2 pi is rounded to 2^-54 of itself, to 2^-64 of a turn, and what is left of the product to 2^-25 of half a turn.
+__device__ __forceinline__ long long turns_of(double freq) {
+    double t = freq * 0.15915494309189533577;                                // 1 / 2 pi
+    t -= rint(t);
+    return __double2ll_rn(t * 18446744073709551616.0);
+}
+__device__ __forceinline__ void sin_cos(long long turns, long long position, float& s, float& c) {
+    const unsigned long long at = (unsigned long long)turns * (unsigned long long)position;
+    sincospif((float)(int)(at >> 32) * 4.656612873077392578125e-10f, &s, &c);
+}
 
 // Units are pairs of neighbouring tokens, the first at an even position.  Sequence b has those from starts[b] / 2 + b on (one more than it can need
 // where its tokens begin at an even position, so that the numbers follow from `starts` alone).  The sequence of unit u: the last b with starts[b] / 2 + b <= u,
@@ -71,13 +100,96 @@ __device__ __forceinline__ float high_of(uint32_t x) {
     else return __uint_as_float(x & 0xffff0000u);
 }
 
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    if constexpr (F16) {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        return pack_bf16x2(lo, hi);
+    }
+}
+
+// The queries' part: thread = (row, group of heads, slot of eight channels).  A slot that turns has channels 4 s .. and their partners half a part further on, or
+// eight neighbours (interleaved); one that does not copies eight neighbours.
 template <int D, bool F16>
-__global__ void __launch_bounds__(32 * APPEND_WARPS) cache_append_kernel(const AppendArgs a, DeviceCounters* dc, DeviceCounters* dc_next) {
+__device__ __forceinline__ void turn_queries(const AppendArgs& a, const RotaryArgs& ro) {
+    const uint32_t id = (blockIdx.x - ro.key_blocks) * (32 * APPEND_WARPS) + threadIdx.x;
+    const uint32_t rest = fastdiv(id, ro.by_slots), row_of = fastdiv(rest, ro.by_groups);
+    const int slot = (int)(id - rest * ro.by_slots.d), h0 = (int)(rest - row_of * ro.by_groups.d);
+    if (row_of >= (uint32_t)a.rows) return;
+    const int r = (int)row_of;
+    const bool turns = 8 * slot < ro.rot;
+    long long f[4] = {0, 0, 0, 0};
+    if (turns)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = turns_of(ro.freqs[4 * slot + e]);
+    int lo = 0, n = a.sequences;                // the last sequence that begins at or before the row
+    while (n > 1) {
+        const int half = n / 2;
+        if (a.starts[lo + half] <= r) lo += half;
+        n -= half;
+    }
+    const int first = max(a.starts[lo], 0), end = min(max(a.starts[lo + 1], 0), a.rows), seq = a.seqs[lo];
+    if (r < first || r >= end || seq < 0 || seq >= a.slots) return;
+    const long long position = (long long)a.lens[seq] - (end - first) + (ro.depths ? ro.depths[r] : r - first);
+    float s[4], c[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        s[e] = 0.f;
+        c[e] = 1.f;
+        if (turns) {
+            sin_cos(f[e], position, s[e], c[e]);
+            s[e] *= ro.amplitude;
+            c[e] *= ro.amplitude;
+        }
+    }
+    const bool halves = turns && !ro.interleaved;
+    const int ca = halves ? 4 * slot : 8 * slot, cb = halves ? ca + ro.rot / 2 : ca + 4;
+    const uint16_t* from = ro.q + (size_t)r * ro.q_stride;
+    uint16_t* to = ro.q_out + (size_t)r * ro.heads * D;
+    const int step = (int)ro.by_groups.d;
+    constexpr int AHEAD = 4;
+    for (int h = h0; h < ro.heads; h += AHEAD * step) {
+        uint2 xa[AHEAD], xb[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (h + k * step < ro.heads) {
+                xa[k] = *reinterpret_cast<const uint2*>(from + (size_t)(h + k * step) * D + ca);
+                xb[k] = *reinterpret_cast<const uint2*>(from + (size_t)(h + k * step) * D + cb);
+            }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (h + k * step < ro.heads) {
+                if (turns) {
+                    const float x[8] = {low_of<F16>(xa[k].x), high_of<F16>(xa[k].x), low_of<F16>(xa[k].y), high_of<F16>(xa[k].y),
+                                        low_of<F16>(xb[k].x), high_of<F16>(xb[k].x), low_of<F16>(xb[k].y), high_of<F16>(xb[k].y)};
+                    float y[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float u = ro.interleaved ? x[2 * e] : x[e], v = ro.interleaved ? x[2 * e + 1] : x[e + 4];
+                        const float p = fmaf(u, c[e], -v * s[e]), w = fmaf(v, c[e], u * s[e]);
+                        if (ro.interleaved) { y[2 * e] = p; y[2 * e + 1] = w; }
+                        else { y[e] = p; y[e + 4] = w; }
+                    }
+                    xa[k] = make_uint2(pack2<F16>(y[0], y[1]), pack2<F16>(y[2], y[3]));
+                    xb[k] = make_uint2(pack2<F16>(y[4], y[5]), pack2<F16>(y[6], y[7]));
+                }
+                *reinterpret_cast<uint2*>(to + (size_t)(h + k * step) * D + ca) = xa[k];
+                *reinterpret_cast<uint2*>(to + (size_t)(h + k * step) * D + cb) = xb[k];
+            }
+    }
+}
+
+template <int D, bool F16, bool ROT>
+__global__ void __launch_bounds__(32 * APPEND_WARPS) cache_append_kernel(const AppendArgs a, const RotaryArgs ro, DeviceCounters* dc, DeviceCounters* dc_next) {
     constexpr int G = D / 32;
     constexpr bool SAME_LANE = G % 4 == 0;      // both tokens' codes come to the same lane, G / 4 rounds apart: whole words of V
     using B = CacheBlock<D>;
     grid_dependency_wait();
     if (threadIdx.x == 0 && blockIdx.x == 0 && dc_next) *dc_next = DeviceCounters{0, 0, 0, 0, 0, 0, 0};
+    if constexpr (ROT)
+        if ((int)blockIdx.x >= ro.key_blocks) return turn_queries<D, F16>(a, ro);
     const int lane = threadIdx.x & 31;
     const uint32_t id = blockIdx.x * APPEND_WARPS + (threadIdx.x >> 5);
     const int unit = (int)fastdiv(id, a.by_chunks);
@@ -119,8 +231,45 @@ __global__ void __launch_bounds__(32 * APPEND_WARPS) cache_append_kernel(const A
         codes_at[it] = kv_of(it) ? B::V_CODES + (t16 >> 1) * D + (q * G + w) * 4 : B::K_CODES + tok * (D / 2) + ((q >> 1) * G + w) * 4;
         scales_at[it] = kv_of(it) ? B::V_SCALES + ((t16 >> 1) * G + w) * 8 + q * 4 : B::K_SCALES + (tok * G + w) * 4;
     }
+    // ---- rotation: of the lane's four channels in each round of keys, cosines and signed sines; `other`: from the channels to their partners
+    constexpr int KR = ROT ? (G + 1) / 2 : 0;    // rounds that have keys
+    [[maybe_unused]] float cs[KR + 1][4], sn[KR + 1][4];
+    [[maybe_unused]] int other[KR + 1];          // (0: the partners are among the four, or nothing turns)
+    [[maybe_unused]] uint2 partner[KR + 1], partner_ahead[KR + 1];
+    if constexpr (ROT) {
+#pragma unroll
+        for (int it = 0; it < KR; ++it) {
+            const int c0 = 32 * ((it * 4 + (lane >> 3)) % G) + 4 * q, half = ro.rot / 2, row = r + parity_of(it);
+            const bool turns = kv_of(it) == 0 && c0 < ro.rot && (parity_of(it) ? has1 : has0), upper = c0 >= half;
+            other[it] = turns && !ro.interleaved ? (upper ? -half : half) : 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) { cs[it][c] = 1.f; sn[it][c] = 0.f; }
+            if (turns) {
+                const long long position = ro.depths ? (long long)pos0 + ro.depths[row] : (long long)pos + parity_of(it);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (ro.interleaved && (c & 1)) {
+                        cs[it][c] = cs[it][c - 1];
+                        sn[it][c] = -sn[it][c - 1];
+                        continue;
+                    }
+                    float s, co;
+                    sin_cos(turns_of(ro.freqs[ro.interleaved ? (c0 + c) / 2 : c0 + c - (upper ? half : 0)]), position, s, co);
+                    cs[it][c] = co * ro.amplitude;
+                    sn[it][c] = (ro.interleaved || !upper ? -s : s) * ro.amplitude;
+                }
+            }
+        }
+    }
     uint2 x[G], ahead[G];
     auto load = [&] {                            // (of the next head)
+        if constexpr (ROT) {
+#pragma unroll
+            for (int it = 0; it < KR; ++it) {
+                partner_ahead[it] = make_uint2(0, 0);
+                if (other[it]) partner_ahead[it] = *reinterpret_cast<const uint2*>(src[it] + other[it]);
+            }
+        }
 #pragma unroll
         for (int it = 0; it < G; ++it) {
             ahead[it] = make_uint2(0, 0);
@@ -133,7 +282,24 @@ __global__ void __launch_bounds__(32 * APPEND_WARPS) cache_append_kernel(const A
     for (int h = h0; h < h1; ++h) {
 #pragma unroll
         for (int it = 0; it < G; ++it) x[it] = ahead[it];
+        if constexpr (ROT) {
+#pragma unroll
+            for (int it = 0; it < KR; ++it) partner[it] = partner_ahead[it];
+        }
         if (h + 1 < h1) load();
+        if constexpr (ROT) {
+#pragma unroll
+            for (int it = 0; it < KR; ++it) {
+                const int c0 = 32 * ((it * 4 + (lane >> 3)) % G) + 4 * q;
+                if (kv_of(it) != 0 || c0 >= ro.rot) continue;
+                const float u[4] = {low_of<F16>(x[it].x), high_of<F16>(x[it].x), low_of<F16>(x[it].y), high_of<F16>(x[it].y)};
+                const float v[4] = {low_of<F16>(partner[it].x), high_of<F16>(partner[it].x), low_of<F16>(partner[it].y), high_of<F16>(partner[it].y)};
+                float y[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) y[c] = fmaf(u[c], cs[it][c], (ro.interleaved ? u[c ^ 1] : v[c]) * sn[it][c]);
+                x[it] = make_uint2(pack2<F16>(y[0], y[1]), pack2<F16>(y[2], y[3]));
+            }
+        }
         // ---- least and (negated) greatest number of every group; lane l then has those of group l of the 4 G that the warp works on
         uint32_t mine = 0;
 #pragma unroll
@@ -221,11 +387,24 @@ __global__ void __launch_bounds__(32 * APPEND_WARPS) cache_append_kernel(const A
     }
 }
 
-template <int D, bool F16>
-cudaError_t launch_append(const AppendArgs& a, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
+template <int D, bool F16, bool ROT>
+cudaError_t launch_append(const AppendArgs& a, RotaryArgs ro, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
     const long long warps = (long long)a.units * a.by_chunks.d;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((warps + APPEND_WARPS - 1) / APPEND_WARPS));
+    ro.key_blocks = (int)((warps + APPEND_WARPS - 1) / APPEND_WARPS);
+    long long blocks = ro.key_blocks;
+    if (ro.q) {
+        // A thread takes one head while the GPU has room for more threads, then up to eight (the angles are worked out once), or so many that all threads can be counted.
+        const long long slots = D / 8, full = 148LL * 2048, most = 0x7fffff00LL - 64 * APPEND_WARPS;
+        long long groups = ro.heads;
+        if (groups * slots * a.rows > full) groups = std::max(std::max((long long)(ro.heads + 7) / 8, std::min(groups, full / (slots * a.rows))), 1LL);
+        if (groups * slots * a.rows > most) groups = std::max(most / (slots * a.rows), 1LL);
+        if (groups * slots * a.rows > most) return cudaErrorInvalidConfiguration;      // (refused ahead of this)
+        ro.by_slots = fastdiv_make((uint32_t)slots);
+        ro.by_groups = fastdiv_make((uint32_t)groups);
+        blocks += (groups * slots * a.rows + 32 * APPEND_WARPS - 1) / (32 * APPEND_WARPS);
+    }
+    cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(32 * APPEND_WARPS);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -233,13 +412,14 @@ cudaError_t launch_append(const AppendArgs& a, DeviceCounters* dc, DeviceCounter
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, cache_append_kernel<D, F16>, a, dc, dc_next);
+    return cudaLaunchKernelEx(&cfg, cache_append_kernel<D, F16, ROT>, a, ro, dc, dc_next);
 }
 
 }  // namespace
 
-int cache_append(const psa_cache& c, const void* K, const void* V, long long k_stride, long long v_stride, const int* seqs, const int* starts,
-                 int sequences, int rows, int dtype, void* k_held, void* v_held, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
+int cache_append(const psa_cache& c, const psa_rotary* rotary, const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride,
+                 const int* depths, const int* seqs, const int* starts, int sequences, int rows, int heads, int dtype, void* q_out, void* k_held, void* v_held, DeviceCounters* dc,
+                 DeviceCounters* dc_next, cudaStream_t stream) {
     if ((long long)rows / 2 + sequences > 0x7fffffffLL) return PSA_ERR_SHAPE;
     const int units = rows / 2 + sequences;
     // one head a warp until the GPU is full of warps, then up to eight (their look-ups are made once)
@@ -250,14 +430,24 @@ int cache_append(const psa_cache& c, const void* K, const void* V, long long k_s
                           static_cast<uint16_t*>(k_held), static_cast<uint16_t*>(v_held), k_stride, v_stride,
                           c.pages, c.slots, c.width, c.page_size, c.kv_heads, sequences, rows, per_warp, units, fastdiv_make((uint32_t)chunks),
                           fastdiv_make((uint32_t)c.page_size)};
+    RotaryArgs ro = {};
+    if (rotary)
+        ro = RotaryArgs{rotary->freqs, depths, rotary->amplitude, rotary->rot, rotary->interleaved != 0, static_cast<const uint16_t*>(Q), static_cast<uint16_t*>(q_out), q_stride, heads,
+                        0, FastDiv{}, FastDiv{}};
     cudaError_t e = cudaErrorInvalidValue;
     const bool f16 = dtype == PSA_F16;
+    auto launch = [&](auto width) {
+        constexpr int D = decltype(width)::value;
+        if (rotary) return f16 ? launch_append<D, true, true>(a, ro, dc, dc_next, stream) : launch_append<D, false, true>(a, ro, dc, dc_next, stream);
+        return f16 ? launch_append<D, true, false>(a, ro, dc, dc_next, stream) : launch_append<D, false, false>(a, ro, dc, dc_next, stream);
+    };
+    using std::integral_constant;
     switch (c.d_k) {
-        case 32: e = f16 ? launch_append<32, true>(a, dc, dc_next, stream) : launch_append<32, false>(a, dc, dc_next, stream); break;
-        case 64: e = f16 ? launch_append<64, true>(a, dc, dc_next, stream) : launch_append<64, false>(a, dc, dc_next, stream); break;
-        case 96: e = f16 ? launch_append<96, true>(a, dc, dc_next, stream) : launch_append<96, false>(a, dc, dc_next, stream); break;
-        case 128: e = f16 ? launch_append<128, true>(a, dc, dc_next, stream) : launch_append<128, false>(a, dc, dc_next, stream); break;
-        case 256: e = f16 ? launch_append<256, true>(a, dc, dc_next, stream) : launch_append<256, false>(a, dc, dc_next, stream); break;
+        case 32: e = launch(integral_constant<int, 32>{}); break;
+        case 64: e = launch(integral_constant<int, 64>{}); break;
+        case 96: e = launch(integral_constant<int, 96>{}); break;
+        case 128: e = launch(integral_constant<int, 128>{}); break;
+        case 256: e = launch(integral_constant<int, 256>{}); break;
         default: return PSA_ERR_UNSUPPORTED;
     }
     if (e != cudaSuccess) { set_cuda_error(e, "cache_append_kernel launch"); return PSA_ERR_CUDA; }

@@ -74,6 +74,7 @@ struct AttnArgs {
     int wide;                                   // the steps of all rows may be more than 32 bits count, by the tables' width (many rows and room for 2^20 tokens and more)
     float scale;
     FastDiv by_group, by_blocks;                // by query heads of a group, by blocks of a page
+    const int* parents;                         // TREE: of every query, its parent among the sequence's queries or -1
 };
 
 // Arrivals on a row of several parts, at the number of its first part.  Every arrival that completes a row wraps its count to zero again, and a CTA
@@ -137,13 +138,14 @@ __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY
 struct Seq {
     int slot, len, q0, nq, qtiles, steps, bad;   // bad: no such slot, or longer than its table
 };
-template <int COLS>
+template <int COLS, bool TREE>
 __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
     Seq s;
     s.slot = a.seqs[b];
     const bool there = s.slot >= 0 && s.slot < a.slots;
     s.q0 = min(max(a.q_starts[b], 0), a.rows);
     s.nq = max(min(max(a.q_starts[b + 1], 0), a.rows) - s.q0, 0);
+    if (TREE && s.nq > PSA_TREE_MOST) s.nq = 0;
     const int held = there ? max(a.lens[s.slot], 0) : 0;
     s.len = min(held, a.width * a.page_size);
     s.bad = !there || held != s.len;
@@ -177,8 +179,10 @@ __device__ __forceinline__ Piece piece_of(const Seq& s, int r, int piece, int fi
     return p;
 }
 
+// TREE: the sequence's last nq tokens are a tree, and query i sees, of these, itself and its ancestors.  A step that has tokens of the tree looks their bits up in a word a column; the others
+// run as before.  The bits are found by a lane a column, that follows the parents, in the warps that have such steps, while their first blocks are on their way.
 // MANY: there may be more items than CTAs, that is, rows by more than a half (parts are no more than CTAs by a half).  (Without it the loop has less to keep: two sequences of up to 131,072 tokens 50.2 -> 49.1 us, eight of up to 8000 14.0 -> 13.6.)
-template <int D, int NT, bool MANY>
+template <int D, int NT, bool MANY, bool TREE>
 __global__ void __launch_bounds__(ACfg<D, NT>::THREADS, ACfg<D, NT>::CTAS)
 cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next) {
     using Cfg = ACfg<D, NT>;
@@ -197,6 +201,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     __shared__ int base_s[SEQS + 1], split_s[SEQS];                          // items ahead of a sequence, and parts that are joined with others
     __shared__ Piece pieces[2], own_s[WARPS];                                // of the CTA, this one and the next; of the warps, where each has a row of its own
     __shared__ int item_s[2];                                                // this item and the next, -1: none
+    __shared__ uint32_t tree_s[TREE ? WARPS : 1][TREE ? COLS : 1][TREE ? PSA_TREE_MOST / 32 + 1 : 1];      // tokens of the tree that a column sees, by warp
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     if (tid < 2 * BRIEFS) briefs_s[tid] = 0;
@@ -232,7 +237,8 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     float about = 0.f;
     bool descends = false;
     for (int b = tid; b < a.sequences; b += THREADS) {
-        const Seq x = sequence<COLS>(a, b);
+        const Seq x = sequence<COLS, TREE>(a, b);
+        if (TREE && x.nq == 0 && a.q_starts[b + 1] > a.q_starts[b] && blockIdx.x == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);       // (a tree that is too large, or rows that are not there)
         descends |= a.q_starts[b + 1] < a.q_starts[b];
         if (b == tid) s0 = x;
         if (MANY) seq_s[b] = make_uint2((uint32_t)x.steps, (uint32_t)x.qtiles);
@@ -335,7 +341,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                 cut = y.y & 1 ? n : 0u;
             }
         } else if (k < a.sequences) {
-            if (k0 > 0) x = sequence<COLS>(a, k);
+            if (k0 > 0) x = sequence<COLS, TREE>(a, k);
             const uint32_t parts = (uint32_t)parts_of(x.steps, piece);
             n = (uint32_t)x.qtiles * a.kv_heads * parts;
             cut = parts > 1 ? n : 0u;
@@ -362,7 +368,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     // Decodes item `i` (by one warp).
     auto decode = [&](int i, Piece* to) {
         for (int k = lane; k < a.sequences; k += 32)
-            if (base_s[k] <= i && i < base_s[k + 1]) *to = piece_of(sequence<COLS>(a, nth(k)), i - base_s[k], piece, split_s[k]);
+            if (base_s[k] <= i && i < base_s[k + 1]) *to = piece_of(sequence<COLS, TREE>(a, nth(k)), i - base_s[k], piece, split_s[k]);
     };
 
     if (sorted && warp == 0 && (int)blockIdx.x >= bundles) decode((int)blockIdx.x - bundles, &pieces[0]);
@@ -506,10 +512,27 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
             for (int c = 0; c < 2; ++c) {
                 const int owner = (2 * t + c) * 4;
                 cs[nt][c] = fmaxf(__shfl_sync(0xffffffffu, up, owner) * (a.scale * LOG2E * 128.f), 1.2e-38f);
-                limit[nt][c] = len - nq + min((int)fastdiv(qt * COLS + nt * 8 + 2 * t + c, a.by_group), nq - 1);
+                limit[nt][c] = TREE ? 0 : len - nq + min((int)fastdiv(qt * COLS + nt * 8 + 2 * t + c, a.by_group), nq - 1);
             }
         }
-        const int seen_by_all = len - nq + (int)fastdiv(qt * COLS, a.by_group);          // the last token that every column sees
+        const int seen_by_all = TREE ? len - nq - 1 : len - nq + (int)fastdiv(qt * COLS, a.by_group);          // the last token that every column sees
+        [[maybe_unused]] const int tree_words = (nq + 31) / 32;
+        if constexpr (TREE) {
+            if (nsteps > 0 && step_of(nsteps - 1) * STEP + STEP - 1 > seen_by_all) {
+                for (int e = lane; e < COLS * tree_words; e += 32) tree_s[warp][e / tree_words][e % tree_words] = 0u;
+                __syncwarp();
+                if (lane < COLS) {
+                    int at = min((int)fastdiv((uint32_t)(qt * COLS + lane), a.by_group), nq - 1);
+                    while (at >= 0) {
+                        tree_s[warp][lane][at >> 5] |= 1u << (at & 31);
+                        const int up = __ldg(a.parents + q0 + at);
+                        if (up < -1 || up >= at) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);        // (no earlier token: taken for the root of a tree of its own)
+                        at = up < at ? up : -1;
+                    }
+                }
+                __syncwarp();
+            }
+        }
 
         const CacheOnes cache_ones;
         // m: running maximum of the scores before their factor; limit_up: where it is raised; shift: HEADROOM - m in log2 units
@@ -572,6 +595,20 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                 }
             }
             // ---- phase 2
+            [[maybe_unused]] uint32_t sees[NT][2];                           // TREE: of the step's tokens, those that the columns see
+            if constexpr (TREE) {
+                if (masked) {
+                    const int at = tok0 - (len - nq), word = at >> 5;       // (of the tree; before it everything is seen, behind it nothing)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const uint32_t* const bits = tree_s[warp][nt * 8 + 2 * t + c];
+                            const uint32_t lo = word < 0 ? 0xffffffffu : word < tree_words ? bits[word] : 0u, hi = word + 1 < 0 ? 0xffffffffu : word + 1 < tree_words ? bits[word + 1] : 0u;
+                            sees[nt][c] = __funnelshift_r(lo, hi, at);
+                        }
+                }
+            }
             if (masked) {
 #pragma unroll
                 for (int s = 0; s < STEP_BLOCKS; ++s)
@@ -579,7 +616,8 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
-                            if (tok0 + s * CACHE_BLOCK + g + 8 * (c >> 1) > limit[nt][c & 1] || !(have >> s & 1u)) sc[s][nt][c] = -INFINITY;
+                            if ((TREE ? !(sees[nt][c & 1] >> (s * CACHE_BLOCK + g + 8 * (c >> 1)) & 1u) : tok0 + s * CACHE_BLOCK + g + 8 * (c >> 1) > limit[nt][c & 1]) || !(have >> s & 1u))
+                                sc[s][nt][c] = -INFINITY;
             }
             bool raise = false;
 #pragma unroll
@@ -673,10 +711,10 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             const int n = limit[nt][c] - (tok0 + s * CACHE_BLOCK) + 1;       // tokens of the block that the column sees
-                            const uint32_t sees = n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
+                            const uint32_t seen = TREE ? sees[nt][c] >> (s * CACHE_BLOCK) & 0xffffu : n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
 #pragma unroll
                             for (int w = 0; w < G; ++w)
-                                if (nans[w] & sees) {
+                                if (nans[w] & seen) {
 #pragma unroll
                                     for (int k = 0; k < 2; ++k) { o[nt][2 * w + k][c] = NAN; o[nt][2 * w + k][c + 2] = NAN; }
                                 }
@@ -863,12 +901,12 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     if (lane == 0 && abort_flag) atomicExch(&dc->status, (int)PSA_ERR_TIMEOUT);
 }
 
-template <int D, int NT, bool MANY>
+template <int D, int NT, bool MANY, bool TREE>
 int launch_attn(const AttnArgs& all, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
     using Cfg = ACfg<D, NT>;
     static DeviceSetup setup;
     const int sms = device_setup(&setup, [] {
-        return cudaFuncSetAttribute(cache_attn_kernel<D, NT, MANY>, cudaFuncAttributeMaxDynamicSharedMemorySize, ACfg<D, NT>::SMEM);
+        return cudaFuncSetAttribute(cache_attn_kernel<D, NT, MANY, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, ACfg<D, NT>::SMEM);
     }, "cache attention set-up");
     if (sms <= 0) return PSA_ERR_CUDA;
     for (int b0 = 0; b0 < all.sequences; b0 += SEQS) {
@@ -896,7 +934,7 @@ int launch_attn(const AttnArgs& all, DeviceCounters* dc, DeviceCounters* dc_next
         cfg.numAttrs = 1;
         // (the counter that items are handed out by serves one launch)
         cudaError_t e = b0 == 0 ? cudaSuccess : cudaMemsetAsync(&dc->next_item, 0, sizeof(dc->next_item), stream);
-        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, cache_attn_kernel<D, NT, MANY>, a, dc, b0 == 0 ? dc_next : nullptr);
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, cache_attn_kernel<D, NT, MANY, TREE>, a, dc, b0 == 0 ? dc_next : nullptr);
         if (e != cudaSuccess) { set_cuda_error(e, "cache_attn_kernel launch"); return PSA_ERR_CUDA; }
     }
     return PSA_OK;
@@ -906,16 +944,20 @@ int launch_attn(const AttnArgs& all, DeviceCounters* dc, DeviceCounters* dc_next
 
 size_t cache_attention_scratch_bytes(int d) { return (size_t)2 * MAX_CTAS * 16 * (d + 2) * sizeof(float); }
 
-int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const int* seqs, const int* q_starts, int sequences, int rows, int heads, int max_q,
+int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads, int max_q,
                     float scale, int dtype, void* out, float* lse, void* scratch, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
     const AttnArgs a = {static_cast<const uint8_t*>(c.pool), c.tables, c.lens, seqs, q_starts, static_cast<const uint16_t*>(Q), static_cast<uint16_t*>(out), lse,
                         static_cast<float*>(scratch), q_stride, c.pages, c.slots, c.width, c.page_size, c.kv_heads, heads / c.kv_heads, sequences, rows,
-                        dtype == PSA_F16, 0, scale, fastdiv_make((uint32_t)(heads / c.kv_heads)), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
+                        dtype == PSA_F16, 0, scale, fastdiv_make((uint32_t)(heads / c.kv_heads)), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK)), parents};
     const bool wide = (long long)max_q * a.group > 8;        // more than eight columns: two tiles of them share a block's codes
-    auto launch = [&](auto width, auto tiles_of_columns) {
+    auto launch_for = [&](auto width, auto tiles_of_columns, auto tree) {
         constexpr int D = decltype(width)::value, NT = decltype(tiles_of_columns)::value;
+        constexpr bool TREE = decltype(tree)::value;
         const long long tiles = (long long)max_q * a.group <= 8 * NT ? sequences : ((long long)rows * a.group + 8 * NT - 1) / (8 * NT) + sequences;
-        return 2 * tiles * c.kv_heads > 148 * ACfg<D, NT>::CTAS ? launch_attn<D, NT, true>(a, dc, dc_next, stream) : launch_attn<D, NT, false>(a, dc, dc_next, stream);
+        return 2 * tiles * c.kv_heads > 148 * ACfg<D, NT>::CTAS ? launch_attn<D, NT, true, TREE>(a, dc, dc_next, stream) : launch_attn<D, NT, false, TREE>(a, dc, dc_next, stream);
+    };
+    auto launch = [&](auto width, auto tiles_of_columns) {
+        return parents ? launch_for(width, tiles_of_columns, std::true_type{}) : launch_for(width, tiles_of_columns, std::false_type{});
     };
     using std::integral_constant;
     const integral_constant<int, 1> one;

@@ -90,18 +90,26 @@ int bf16_attention_persist(const void* Q, const void* K, const void* V, void* ou
                            float scale, int scheme, DeviceCounters* dc, unsigned int* cursor, DeviceCounters* dc_next,
                            cudaStream_t stream);
 
-// ---- serving (psa_prompt.cu, psa_cache_append.cu, psa_cache_attn.cu, psa_pages.cu) ----
+// ---- serving (psa_prompt.cu, psa_cache_append.cu, psa_cache_attn.cu, psa_drafts.cu, psa_pages.cu) ----
 // Arguments are checked by the caller; each returns a psa_status.  dc: the call's counter block, dc_next (may be null): cleared by the call's first kernel.
 int prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts, const int* k_starts,
                      int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, void* scratch, int call, DeviceCounters* dc,
                      unsigned int* cursor, DeviceCounters* dc_next, cudaStream_t stream);     // call: a number > 0 of its own
 size_t prompt_scratch_bytes(int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d);      // 0: none is used
 cudaError_t launch_prompt_expired(cudaStream_t stream);       // self-test: the counts that a call leaves whose waits ran out
-int cache_append(const psa_cache& c, const void* K, const void* V, long long k_stride, long long v_stride, const int* seqs, const int* starts, int sequences, int rows,
-                 int dtype, void* k_held, void* v_held, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+// rotary null: nothing turns, and Q, depths, heads and q_out have no meaning.
+int cache_append(const psa_cache& c, const psa_rotary* rotary, const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride,
+                 const int* depths, const int* seqs, const int* starts, int sequences, int rows, int heads, int dtype, void* q_out, void* k_held, void* v_held, DeviceCounters* dc,
+                 DeviceCounters* dc_next, cudaStream_t stream);
 size_t cache_attention_scratch_bytes(int d);
-int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const int* seqs, const int* q_starts, int sequences, int rows, int heads, int max_q,
+// parents null: a sequence's queries are a chain.
+int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads, int max_q,
                     float scale, int dtype, void* out, float* lse, void* scratch, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+int verify_drafts(const void* logits, long long logit_stride, const void* drafts, long long draft_stride, int vocab, int dtype, const int* tokens, const int* parents, const int* starts,
+                  int sequences, int rows, const float* temperatures, const float* uniform, int distinct, int* path, int* accepted, int* next, DeviceCounters* dc,
+                  DeviceCounters* dc_next, cudaStream_t stream);
+int cache_keep(const psa_cache& c, int layers, const int* seqs, const int* starts, const int* path, const int* accepted, int sequences, int rows, int* new_lens, DeviceCounters* dc,
+               DeviceCounters* dc_next, cudaStream_t stream);
 int pages_free(const psa_pages& p, const int* seqs, int count, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
 int pages_fork(const psa_pages& p, const int* parents, const int* children, int count, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
 size_t pages_reserve_scratch_bytes(int pages, int count);

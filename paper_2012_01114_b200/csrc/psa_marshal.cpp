@@ -19,6 +19,10 @@ decltype(&psa_pages_fork) g_fork;
 decltype(&psa_pages_reserve) g_reserve;
 decltype(&psa_pages_compact) g_compact;
 decltype(&psa_pages_copy) g_copy;
+decltype(&psa_cache_append_rotary) g_append_rotary;
+decltype(&psa_tree_attention) g_tree;
+decltype(&psa_verify_drafts) g_verify;
+decltype(&psa_cache_keep) g_keep;
 PyObject* g_error;                       // PsaError(status, where)
 
 using at::Tensor;
@@ -124,6 +128,76 @@ Tensor attention(const Tensor& Q, const Tensor& pool, const Tensor& tables, cons
     return o;
 }
 
+void* dense_like(const Maybe& t, const char* name, int64_t rows, int64_t cols, const Tensor& like) { return t ? given(*t, name, rows, cols, like.scalar_type()) : nullptr; }
+
+std::optional<Tensor> append_rotary(const Tensor& K, const Tensor& V, const Tensor& pool, const Tensor& tables, const Tensor& lens, const Tensor& seqs, const Tensor& starts, int64_t page_size,
+                                    const Tensor& freqs, const Maybe& Q, const Maybe& depths, bool interleaved, double amplitude, const Maybe& q_out, const Maybe& k_held, const Maybe& v_held,
+                                    std::optional<int64_t> stream) {
+    const int type = serving_type(K, "K");
+    const int64_t rows = K.size(0), kv_heads = K.size(1), d = K.size(2), n = seqs.numel();
+    if (K.sizes() != V.sizes()) refuse("K and V must have one shape");
+    if (!freqs.is_cuda() || freqs.scalar_type() != at::kDouble || freqs.dim() != 1 || !freqs.is_contiguous()) refuse("freqs must be a contiguous CUDA tensor [rot / 2] of float64");
+    if (Q && (Q->dim() != 3 || Q->size(0) != rows)) refuse("Q must be [rows, heads, d_k] with the rows of K");
+    if (!Q && q_out) refuse("q_out is given without Q");
+    const long long ks = rows_of(K, "K", kv_heads, d, K), vs = rows_of(V, "V", kv_heads, d, K), qs = Q ? rows_of(*Q, "Q", Q->size(1), d, K) : 0;
+    const psa_cache cache = cache_of(pool, tables, lens, kv_heads, page_size, d);
+    const psa_rotary rotary = {static_cast<const double*>(freqs.data_ptr()), (float)amplitude, small(2 * freqs.numel(), "freqs"), interleaved};
+    std::optional<Tensor> o = q_out;
+    if (Q && !o) o = at::empty({rows, Q->size(1), d}, Q->options());
+    call("psa_cache_append_rotary", g_append_rotary, &cache, &rotary, Q ? Q->data_ptr() : nullptr, K.data_ptr(), V.data_ptr(), qs, ks, vs, depths ? ints(*depths, "depths", rows) : nullptr,
+         ints(seqs, "seqs"), ints(starts, "starts", n + 1), small(n, "seqs"), small(rows, "K"), Q ? small(Q->size(1), "Q") : 0, type,
+         Q ? given(*o, "q_out", rows, Q->size(1) * d, K.scalar_type()) : nullptr, dense_like(k_held, "k_held", rows, kv_heads * d, K), dense_like(v_held, "v_held", rows, kv_heads * d, K),
+         stream_of(stream));
+    return o;
+}
+
+Tensor tree(const Tensor& Q, const Tensor& pool, const Tensor& tables, const Tensor& lens, const Tensor& seqs, const Tensor& q_starts, const Tensor& parents, int64_t kv_heads, int64_t page_size,
+            int64_t max_q, std::optional<double> scale, const Maybe& out, const Maybe& lse, std::optional<int64_t> stream) {
+    const int type = serving_type(Q, "Q");
+    const int64_t rows = Q.size(0), heads = Q.size(1), d = Q.size(2), n = seqs.numel();
+    if (kv_heads <= 0 || heads % kv_heads) refuse("kv_heads must divide Q's heads");
+    const long long qs = rows_of(Q, "Q", heads, d, Q);
+    const psa_cache cache = cache_of(pool, tables, lens, kv_heads, page_size, d);
+    Tensor o = out ? *out : at::empty({rows, heads * d}, Q.options());
+    call("psa_tree_attention", g_tree, &cache, Q.data_ptr(), qs, ints(parents, "parents", rows), ints(seqs, "seqs"), ints(q_starts, "q_starts", n + 1), small(n, "seqs"), small(rows, "Q"),
+         small(heads, "Q"), small(max_q, "max_q"), scale_of(scale, d), type, given(o, "out", rows, heads * d, Q.scalar_type()),
+         lse ? static_cast<float*>(given(*lse, "lse", rows, heads, at::kFloat)) : nullptr, stream_of(stream));
+    return o;
+}
+
+// Row stride of [rows, vocab] numbers.
+long long vocabulary(const Tensor& t, const char* name, const Tensor& like) {
+    if (!t.is_cuda() || t.dim() != 2 || t.sizes() != like.sizes() || t.scalar_type() != like.scalar_type() || (t.numel() && t.size(1) > 1 && t.stride(1) != 1))
+        refuse(std::string(name) + " must be a CUDA tensor [rows, vocab] of the logits' shape and type, the numbers of a row side by side");
+    return t.size(0) > 1 ? t.stride(0) : t.size(1);
+}
+std::tuple<Tensor, Tensor, Tensor> verify(const Tensor& logits, const Tensor& tokens, const Tensor& parents, const Tensor& starts, const Tensor& uniform, const Maybe& path, const Maybe& accepted,
+                                          const Maybe& next, const Maybe& drafts, const Maybe& temperatures, bool distinct, std::optional<int64_t> stream) {
+    if (logits.dim() != 2) refuse("logits must be [rows, vocab]");
+    const int64_t rows = logits.size(0), n = starts.numel() - 1;
+    const int type = logits.scalar_type() == at::kFloat ? PSA_F32 : logits.scalar_type() == at::kBFloat16 ? PSA_BF16 : logits.scalar_type() == at::kHalf ? PSA_F16 : -1;
+    if (type < 0) refuse("logits must be of fp32, bf16 or fp16");
+    const long long ls = vocabulary(logits, "logits", logits), ds = drafts ? vocabulary(*drafts, "drafts", logits) : 0;
+    const auto numbers = [](const Tensor& t, const char* name, int64_t count) { return static_cast<const float*>(given(t, name, count, 1, at::kFloat)); };
+    const auto int_like = starts.options();
+    Tensor p = path ? *path : at::empty({rows}, int_like), a = accepted ? *accepted : at::empty({std::max<int64_t>(n, 0)}, int_like), x = next ? *next : at::empty({std::max<int64_t>(n, 0)}, int_like);
+    call("psa_verify_drafts", g_verify, logits.data_ptr(), ls, drafts ? drafts->data_ptr() : nullptr, ds, small(logits.size(1), "logits"), type, ints(tokens, "tokens", rows),
+         ints(parents, "parents", rows), ints(starts, "starts"), small(n, "starts"), small(rows, "logits"), temperatures ? numbers(*temperatures, "temperatures", n) : nullptr,
+         numbers(uniform, "uniform", rows), (int)distinct, ints_out(p, "path", rows), ints_out(a, "accepted", n), ints_out(x, "next", n), stream_of(stream));
+    return {p, a, x};
+}
+
+void keep(const Tensor& pool, const Tensor& tables, const Tensor& lens, const Tensor& seqs, const Tensor& starts, const Tensor& path, const Tensor& accepted, int64_t kv_heads, int64_t page_size,
+          const Maybe& new_lens, std::optional<int64_t> stream) {
+    if (!pool.is_cuda() || pool.scalar_type() != at::kByte || !pool.is_contiguous() || (pool.dim() != 2 && pool.dim() != 3) || kv_heads <= 0 || page_size <= 0 ||
+        pool.size(-1) % (kv_heads * page_size * 5) || pool.size(-1) / (kv_heads * page_size * 5) * 4 > 0x7fffffff || pool.numel() == 0)
+        refuse("pool must be a contiguous CUDA tensor [pages, page bytes] or [layers, pages, page bytes] of uint8, pages of psa_cache_page_bytes(kv_heads, page_size, d_k) bytes");
+    const int64_t d = pool.size(-1) / (kv_heads * page_size * 5) * 4, n = seqs.numel();
+    const psa_cache cache = cache_of(pool.dim() == 3 ? pool[0] : pool, tables, lens, kv_heads, page_size, d);
+    call("psa_cache_keep", g_keep, &cache, pool.dim() == 3 ? small(pool.size(0), "pool") : 1, ints(seqs, "seqs"), ints(starts, "starts", n + 1), ints(path, "path"),
+         ints(accepted, "accepted", n), small(n, "seqs"), small(path.numel(), "path"), ints_out(new_lens ? *new_lens : lens, "new_lens", tables.size(0)), stream_of(stream));
+}
+
 psa_pages pages_of(const Tensor& tables, const Maybe& lens, const Tensor& refs, int64_t page_size) {
     if (tables.dim() != 2) refuse("tables must be [slots, width]");
     return psa_pages{ints_out(tables, "tables"), lens ? ints_out(*lens, "lens", tables.size(0)) : nullptr, ints_out(refs, "refs"), small(tables.size(0), "tables"),
@@ -170,7 +244,7 @@ void pages_copy(const Tensor& pool, const Tensor& new_pool, const Tensor& src, c
 }
 
 void bind(const std::vector<uintptr_t>& f, py::object error) {
-    if (f.size() != 8) refuse("eight entry points are wanted");
+    if (f.size() != 12) refuse("twelve entry points are wanted");
     g_prompt = reinterpret_cast<decltype(g_prompt)>(f[0]);
     g_append = reinterpret_cast<decltype(g_append)>(f[1]);
     g_attention = reinterpret_cast<decltype(g_attention)>(f[2]);
@@ -179,6 +253,10 @@ void bind(const std::vector<uintptr_t>& f, py::object error) {
     g_reserve = reinterpret_cast<decltype(g_reserve)>(f[5]);
     g_compact = reinterpret_cast<decltype(g_compact)>(f[6]);
     g_copy = reinterpret_cast<decltype(g_copy)>(f[7]);
+    g_append_rotary = reinterpret_cast<decltype(g_append_rotary)>(f[8]);
+    g_tree = reinterpret_cast<decltype(g_tree)>(f[9]);
+    g_verify = reinterpret_cast<decltype(g_verify)>(f[10]);
+    g_keep = reinterpret_cast<decltype(g_keep)>(f[11]);
     g_error = error.release().ptr();
 }
 
@@ -189,6 +267,10 @@ PYBIND11_MODULE(psa_marshal, m) {
     m.def("prompt", &prompt);
     m.def("append", &append);
     m.def("attention", &attention);
+    m.def("append_rotary", &append_rotary);
+    m.def("tree", &tree);
+    m.def("verify", &verify);
+    m.def("keep", &keep);
     m.def("pages_free", &pages_free);
     m.def("pages_fork", &pages_fork);
     m.def("pages_reserve", &pages_reserve);
