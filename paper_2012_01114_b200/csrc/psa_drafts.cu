@@ -7,12 +7,14 @@
 // max(a p - b q, 0) throughout, and a child that is refused costs two numbers and one sum over the row.  Where nobody stands the next token is the first one at
 // which the sum of w along the vocabulary passes u_root times the whole.
 //
-// A number next to a border decides about a token, so exponentials and sums are in 64 bits: the sums along the row have up to 10^5 borders, and with an error of
-// 2^-24 of a likely token's weight one draw in a hundred would fall on the other side of one.  Sums are formed in an order that depends on the sizes alone.
+// A number next to a border decides about a token.  A draw has as many borders as the vocabulary has tokens, and with sums in 32 bits one draw in a hundred would fall on the other side of one:
+// it is made from exponentials and sums in 64 bits (11 operations of that pipe a number, a sixth of a clock on an SM).  Whether a child stands is one comparison: it is made with sums of
+// 32-bit exponentials first, and only where both sides are nearer to each other than those may be off, or where a child with drafts is refused, with the others.
+// Sums are formed in an order that depends on the sizes alone.
 //
 // To read: the rows of the tokens on the path, and no others; which ones these are is known one after the other, so that what counts is how fast one row is read.  A
-// cluster of CTAs shares the rows of a sequence, each a part that it keeps in shared memory while the token is looked at; a row costs one exchange of partial maxima and sums
-// between the CTAs, a child that is refused another.
+// cluster of CTAs shares the rows of a sequence; a row costs one pass with a running maximum and one exchange of partial maxima and sums between the CTAs, a child with drafts that is refused two
+// more passes over what is then in the L2 cache.
 #include <algorithm>
 #include <type_traits>
 
@@ -25,9 +27,11 @@ namespace psa {
 
 namespace {
 
-constexpr int V_WARPS = 16, V_THREADS = 32 * V_WARPS;
+constexpr int V_WARPS = 8, V_THREADS = 32 * V_WARPS;
 constexpr int MOST_CLUSTER = 8;
-constexpr int MOST_SLICE_BYTES = 100 * 1024;    // of a row's part that is kept in shared memory, target and drafts each
+// Relative error of a sum of 32-bit exponentials: their argument goes through two roundings of 2^-24 of itself, 30 at most where a weight counts (2^-18.6 of the weight), ex2 gives 2^-22, and a number
+// takes part in no more than 8 + 64 additions before the sums go on in 64 bits (2^-17.8): below 2^-17 altogether.
+constexpr double COARSE = 1.0 / 65536;
 
 struct VerifyArgs {
     const void *logits, *drafts;
@@ -37,7 +41,6 @@ struct VerifyArgs {
     int *path, *accepted, *next;
     int vocab, sequences, rows, distinct;
     int slice;                                  // of a CTA: numbers of the vocabulary
-    int staged;                                 // the parts of a row are kept in shared memory
 };
 
 template <class T> __device__ __forceinline__ float number(T x) { return static_cast<float>(x); }
@@ -65,15 +68,150 @@ __device__ __forceinline__ X read_cluster(const X* p, uint32_t rank) {      // o
     return x;
 }
 
+// exp2(z / 32) for z <= 0, called by all lanes of a warp together, to 2^-50: 2^(k / 32) (1 + e) with k the nearest whole number, the power from a table of 32 (one a lane), e by its Taylor series
+// (table-driven exponentials: Tang, 1989).
+struct Exp {
+    double power;                                // 2^(lane / 32)
+    __device__ __forceinline__ Exp(int lane) : power(exp2(lane / 32.0)) {}
+    __device__ __forceinline__ double operator()(double z) const {
+        constexpr double L = 0.69314718055994530942 / 32;
+        z = fmax(z, -32704.0);                   // 2^-1022
+        const double t = z + 6755399441055744.0, s = z - (t - 6755399441055744.0);
+        const int k = __double2loint(t);
+        const double e = s * fma(s, fma(s, fma(s, fma(s, L * L * L * L * L / 120, L * L * L * L / 24), L * L * L / 6), L * L / 2), L);
+        const double p = __hiloint2double(__shfl_sync(0xffffffffu, __double2hiint(power), k & 31), __shfl_sync(0xffffffffu, __double2loint(power), k & 31));
+        const double w = fma(p, e, p);
+        return k <= -32672 ? 0.0 : __hiloint2double(__double2hiint(w) + (k >> 5) * 1048576, __double2loint(w));
+    }
+};
+
+// f(number of the first row, number of the second, v, whether there is such a v) for v = low .. high - 1, by a warp, every call by all lanes.  The rows may begin anywhere: up to a
+// boundary of 16 bytes, and behind the last, numbers are read one by one, and all are where the rows lie differently.
+template <class T, bool TWO, class F>
+__device__ __forceinline__ void over(const T* p, const T* q, int low, int high, int lane, F f) {
+    constexpr int VEC = 16 / sizeof(T);
+    if (low >= high) return;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p + low), too = TWO ? reinterpret_cast<uintptr_t>(q + low) : at;
+    const bool alike = ((at ^ too) & 15u) == 0;
+    const int lead = alike ? min((int)((16 - (at & 15u)) % 16 / sizeof(T)), high - low) : high - low, vecs = (high - low - lead) / VEC;
+    auto singly = [&](int from, int to) {
+        for (int v0 = from; v0 < to; v0 += 32) {
+            const int v = v0 + lane;
+            const bool is = v < to;
+            f(is ? number(p[v]) : -INFINITY, TWO && is ? number(q[v]) : -INFINITY, v, is);
+        }
+    };
+    singly(low, low + lead);
+    const uint4* const p4 = reinterpret_cast<const uint4*>(p + low + lead);
+    const uint4* const q4 = TWO ? reinterpret_cast<const uint4*>(q + low + lead) : p4;
+    constexpr int AHEAD = 4;
+    for (int i0 = 0; i0 < vecs; i0 += 32 * AHEAD) {
+        uint4 x[AHEAD], y[TWO ? AHEAD : 1];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = min(i0 + 32 * k + lane, vecs - 1);
+            x[k] = __ldg(p4 + i);
+            if (TWO) y[TWO ? k : 0] = __ldg(q4 + i);
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (i0 + 32 * k >= vecs) break;
+            const int i = i0 + 32 * k + lane;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                f(i < vecs ? number(reinterpret_cast<const T*>(&x[k])[e]) : -INFINITY, TWO && i < vecs ? number(reinterpret_cast<const T*>(&y[TWO ? k : 0])[e]) : -INFINITY, low + lead + i * VEC + e,
+                  i < vecs);
+        }
+    }
+    singly(low + lead + vecs * VEC, high);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Greatest number of a part of a row, the first place that has it (ARG), whether a number is NaN or infinite, and the sum of 2^(c (x - greatest)) in 32 bits (SUM).  Threads take vectors of 16 bytes in turn.
+struct Part {
+    float top;
+    int arg;
+    bool bad;
+    double sum;
+};
+template <class T, bool GREEDY>
+__device__ __forceinline__ Part part_of_row(const T* row, int low, int high, float c, int tid) {
+    constexpr int VEC = 16 / sizeof(T);
+    Part r = {-INFINITY, 0x7fffffff, false, 0.0};
+    float sum = 0.f;
+    int chains = 0;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + low);
+    const int n = high - low, lead = min((int)((16 - (at & 15u)) % 16 / sizeof(T)), n), vecs = (n - lead) / VEC, done = lead + vecs * VEC;
+    auto raise = [&](float m) {                  // a new greatest number
+        const float f = r.top > -INFINITY ? exp2_fast(c * (r.top - m)) : 0.f;
+        sum *= f;
+        r.sum *= (double)f;
+        r.top = m;
+    };
+    auto one = [&](int v) {
+        const float x = number(row[v]);
+        r.bad |= !(x <= 3.402823466e38f);
+        if (GREEDY) {
+            if (x > r.top || (x == r.top && v < r.arg)) { r.top = x; r.arg = v; }
+        } else if (x > -INFINITY) {
+            if (x > r.top) raise(x);
+            sum += exp2_fast(c * (x - r.top));
+        }
+    };
+    if (tid < lead) one(low + tid);
+    const uint4* const row4 = reinterpret_cast<const uint4*>(row + low + lead);
+    constexpr int AHEAD = 4;
+    for (int i0 = 0; i0 < vecs; i0 += AHEAD * V_THREADS) {
+        uint4 x[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (i0 + k * V_THREADS + tid < vecs) x[k] = __ldg(row4 + i0 + k * V_THREADS + tid);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k * V_THREADS + tid;
+            if (i >= vecs) break;
+            float y[VEC], m = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                y[e] = number(reinterpret_cast<const T*>(&x[k])[e]);
+                r.bad |= !(y[e] <= 3.402823466e38f);
+                m = fmaxf(m, y[e]);
+            }
+            if (GREEDY) {
+                if (m > r.top) {
+                    r.top = m;
+#pragma unroll
+                    for (int e = VEC - 1; e >= 0; --e)
+                        if (y[e] == m) r.arg = low + lead + i * VEC + e;
+                }
+            } else {
+                if (m > r.top) raise(m);
+                const float from = r.top > -INFINITY ? r.top : 0.f;
+                float s = 0.f;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s += exp2_fast(c * (y[e] - from));
+                sum += s;
+                if (++chains == 64) { r.sum += (double)sum; sum = 0.f; chains = 0; }
+            }
+        }
+    }
+    if (tid < n - done) one(low + done + tid);
+    r.sum += (double)sum;
+    return r;
+}
+
 template <class T>
 __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, DeviceCounters* dc, DeviceCounters* dc_next) {
-    extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int parent_s[PSA_TREE_MOST], token_s[PSA_TREE_MOST], tried_s[PSA_TREE_MOST];
     __shared__ double sums_s[V_WARPS], sums2_s[V_WARPS];
     __shared__ float max_s[V_WARPS], max2_s[V_WARPS];
     __shared__ int arg_s[V_WARPS], bad_s[V_WARPS], drawn_s;
     __shared__ Record records[2];               // told in turn
-    __shared__ double totals[2];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int ranks = (int)gridDim.x, rank = (int)blockIdx.x, b = (int)blockIdx.y;       // (a cluster is a row of the grid)
@@ -81,7 +219,7 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
     if (tid == 0 && rank == 0 && b == 0 && dc_next) *dc_next = DeviceCounters{0, 0, 0, 0, 0, 0, 0};
     const int first = min(max(a.starts[b], 0), a.rows), count = max(min(max(a.starts[b + 1], 0), a.rows) - first, 0);
     const float temperature = a.temperatures ? a.temperatures[b] : 1.f;
-    const bool greedy = temperature == 0.f;
+    const bool greedy = temperature < 1.17549435e-38f;     // (zero, and what 1 / T could not be formed of)
     const bool refused = count > PSA_TREE_MOST || !(temperature >= 0.f && temperature <= 3.0e38f);
     if (refused || count == 0) {
         if (rank == 0) {
@@ -94,7 +232,6 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
         }
         return;                                  // (the whole cluster)
     }
-    const double c = greedy ? 1.0 : 1.0 / (double)temperature;
     bool strange = false;                        // a parent that is no earlier token, or a token that the vocabulary does not have
     for (int i = tid; i < count; i += V_THREADS) {
         const int p = a.parents[first + i], x = a.tokens[first + i];
@@ -106,152 +243,152 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
     }
     if (__syncthreads_or(strange) && tid == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
 
+    const double C = greedy ? 1.0 : 46.166241308446828384 / (double)temperature;         // 32 / (T ln 2): units of Exp
+    const float c = (float)(C / 32);
+    const Exp exp_of(lane);
     const T* const all_logits = static_cast<const T*>(a.logits);
     const T* const all_drafts = static_cast<const T*>(a.drafts);
     const int low = min(rank * a.slice, a.vocab), high = min(low + a.slice, a.vocab);    // this CTA's part of the vocabulary
     const int each = (high - low + V_WARPS - 1) / V_WARPS;                               // of its warps, one after another
     const int w_low = min(low + warp * each, high), w_high = min(w_low + each, high);
-    constexpr int VEC = 16 / sizeof(T);
 
-    int turn = 0;                                // of records and totals
+    int turn = 0;                                // of records
     int node = 0, stood = 0, next = -1;
     for (;;) {
         const T* const lrow = all_logits + (size_t)(first + node) * a.logit_stride;
         bool leaf = true;
         for (int i = node + 1 + tid; i < count; i += V_THREADS) leaf &= parent_s[i] != node;
-        leaf = !__syncthreads_or(!leaf);
+        leaf = !__syncthreads_or(!leaf);         // (also: what the token before left in shared memory is done with)
         const bool use_q = all_drafts && !greedy && !leaf;
         const T* const qrow = all_drafts + (use_q ? (size_t)(first + node) * a.draft_stride : 0);
-        // ---- the row's part into shared memory (at the place in 16 bytes that it has in memory), its greatest number
-        const T *lp = lrow, *qp = qrow;          // the part's number v is lp[v]
+        // ---- the rows' greatest numbers and sums: of the threads, the CTA, the cluster
+        Part p = greedy ? part_of_row<T, true>(lrow, low, high, 0.f, tid) : part_of_row<T, false>(lrow, low, high, c, tid);
+        Part q = {-INFINITY, 0, false, 0.0};
+        if (use_q) q = part_of_row<T, false>(qrow, low, high, c, tid);
+        auto warp_joined = [&](Part& x) {
+            float top = x.top;
+            int arg = x.arg;
+#pragma unroll
+            for (int s = 16; s > 0; s /= 2) {
+                const float y = __shfl_xor_sync(0xffffffffu, top, s);
+                const int k = __shfl_xor_sync(0xffffffffu, arg, s);
+                if (y > top || (y == top && k < arg)) { top = y; arg = k; }
+            }
+            x.sum = warp_sum(x.top > -INFINITY ? x.sum * (double)exp2_fast(c * (x.top - top)) : 0.0);
+            x.top = top;
+            x.arg = arg;
+            x.bad = __any_sync(0xffffffffu, x.bad);
+        };
+        warp_joined(p);
+        if (use_q) warp_joined(q);
+        if (lane == 0) { max_s[warp] = p.top; max2_s[warp] = q.top; arg_s[warp] = p.arg; bad_s[warp] = p.bad || q.bad; sums_s[warp] = p.sum; sums2_s[warp] = q.sum; }
+        __syncthreads();
+        if (tid == 0) {
+            Record r = {0.0, 0.0, -INFINITY, -INFINITY, 0x7fffffff, 0};
+            for (int w = 0; w < V_WARPS; ++w) {
+                if (max_s[w] > r.p_max || (max_s[w] == r.p_max && arg_s[w] < r.likeliest)) { r.p_max = max_s[w]; r.likeliest = arg_s[w]; }
+                r.q_max = fmaxf(r.q_max, max2_s[w]);
+                r.bad |= bad_s[w];
+            }
+            for (int w = 0; w < V_WARPS; ++w) {
+                if (max_s[w] > -INFINITY) r.p_sum += sums_s[w] * (double)exp2_fast(c * (max_s[w] - r.p_max));
+                if (max2_s[w] > -INFINITY) r.q_sum += sums2_s[w] * (double)exp2_fast(c * (max2_s[w] - r.q_max));
+            }
+            records[turn] = r;
+        }
+        cluster_sync();
         float top = -INFINITY, q_top = -INFINITY;
         int arg = 0x7fffffff;
         bool bad = false;
-        auto fetch = [&](const T* row, uint8_t* to, float& m, bool with_arg) -> const T* {
-            const T* const from = row + low;
-            const int n = high - low, shift = (int)((reinterpret_cast<uintptr_t>(from) & 15u) / sizeof(T)), lead = min((VEC - shift) % VEC, n), vecs = (n - lead) / VEC;
-            T* const dst = reinterpret_cast<T*>(to) + shift;
-            auto look = [&](T x, int v) {
-                const float f = number(x);
-                bad |= !(f <= 3.402823466e38f);
-                if (f > m) { m = f; if (with_arg) arg = v; }
-            };
-            if (tid < lead) { if (a.staged) dst[tid] = from[tid]; look(from[tid], low + tid); }
-            const uint4* const src4 = reinterpret_cast<const uint4*>(from + lead);
-            uint4* const dst4 = reinterpret_cast<uint4*>(dst + lead);
-            constexpr int AHEAD = 4;
-            for (int i = tid; i < vecs; i += AHEAD * V_THREADS) {
-                uint4 x[AHEAD];
-#pragma unroll
-                for (int k = 0; k < AHEAD; ++k)
-                    if (i + k * V_THREADS < vecs) x[k] = __ldg(src4 + i + k * V_THREADS);
-#pragma unroll
-                for (int k = 0; k < AHEAD; ++k)
-                    if (i + k * V_THREADS < vecs) {
-                        if (a.staged) dst4[i + k * V_THREADS] = x[k];
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) look(reinterpret_cast<const T*>(&x[k])[e], low + lead + (i + k * V_THREADS) * VEC + e);
-                    }
-            }
-            const int done = lead + vecs * VEC;
-            if (tid < n - done) { if (a.staged) dst[done + tid] = from[done + tid]; look(from[done + tid], low + done + tid); }
-            return a.staged ? dst - low : row;
-        };
-        __syncthreads();                         // (the part before is done with)
-        const int part_bytes = (a.slice * (int)sizeof(T) + 31) / 16 * 16;
-        lp = fetch(lrow, smem, top, greedy);
-        if (use_q) qp = fetch(qrow, smem + part_bytes, q_top, false);
-        // greatest numbers of the CTA; of equal ones the first
-#pragma unroll
-        for (int s = 16; s > 0; s /= 2) {
-            const float y = __shfl_xor_sync(0xffffffffu, top, s), z = __shfl_xor_sync(0xffffffffu, q_top, s);
-            const int k = __shfl_xor_sync(0xffffffffu, arg, s);
-            if (y > top || (y == top && k < arg)) { top = y; arg = k; }
-            q_top = fmaxf(q_top, z);
-        }
-        bad = __any_sync(0xffffffffu, bad);
-        if (lane == 0) { max_s[warp] = top; max2_s[warp] = q_top; arg_s[warp] = arg; bad_s[warp] = bad; }
-        __syncthreads();
-        top = q_top = -INFINITY;
-        arg = 0x7fffffff;
-        bad = false;
-        for (int w = 0; w < V_WARPS; ++w) {
-            if (max_s[w] > top || (max_s[w] == top && arg_s[w] < arg)) { top = max_s[w]; arg = arg_s[w]; }
-            q_top = fmaxf(q_top, max2_s[w]);
-            bad |= bad_s[w] != 0;
-        }
-        // ---- its sums
         double p_sum = 0, q_sum = 0;
-        if (!greedy && !bad) {
-            if (top > -INFINITY)
-                for (int v = w_low + lane; v < w_high; v += 32) p_sum += exp(((double)number(lp[v]) - (double)top) * c);
-            if (use_q && q_top > -INFINITY)
-                for (int v = w_low + lane; v < w_high; v += 32) q_sum += exp(((double)number(qp[v]) - (double)q_top) * c);
-            p_sum = warp_sum(p_sum);
-            q_sum = warp_sum(q_sum);
-        }
-        if (lane == 0) { sums_s[warp] = p_sum; sums2_s[warp] = q_sum; }
-        __syncthreads();
-        p_sum = q_sum = 0;
-        for (int w = 0; w < V_WARPS; ++w) { p_sum += sums_s[w]; q_sum += sums2_s[w]; }
-        // ---- of all CTAs
-        if (tid == 0) records[turn] = Record{p_sum, q_sum, top, q_top, arg, bad};
-        cluster_sync();
         {
-            float t = -INFINITY, qt = -INFINITY;
-            arg = 0x7fffffff;
-            for (int k = 0; k < ranks; ++k) {
-                const Record r = read_cluster(&records[turn], k);
-                if (r.p_max > t || (r.p_max == t && r.likeliest < arg)) { t = r.p_max; arg = r.likeliest; }
-                qt = fmaxf(qt, r.q_max);
-                bad |= r.bad != 0;
+            const Record r = lane < ranks ? read_cluster(&records[turn], lane) : Record{0.0, 0.0, -INFINITY, -INFINITY, 0x7fffffff, 0};
+            top = r.p_max;
+            arg = r.likeliest;
+            q_top = r.q_max;
+#pragma unroll
+            for (int s = MOST_CLUSTER / 2; s > 0; s /= 2) {
+                const float y = __shfl_xor_sync(0xffffffffu, top, s);
+                const int k = __shfl_xor_sync(0xffffffffu, arg, s);
+                if (y > top || (y == top && k < arg)) { top = y; arg = k; }
+                q_top = fmaxf(q_top, __shfl_xor_sync(0xffffffffu, q_top, s));
             }
-            p_sum = q_sum = 0;
-            for (int k = 0; k < ranks; ++k) {
-                const Record r = read_cluster(&records[turn], k);
-                if (r.p_max > -INFINITY) p_sum += r.p_sum * exp(((double)r.p_max - (double)t) * c);
-                if (r.q_max > -INFINITY) q_sum += r.q_sum * exp(((double)r.q_max - (double)qt) * c);
+            bad = __any_sync(0xffffffffu, r.bad != 0);
+            p_sum = r.p_max > -INFINITY ? r.p_sum * (double)exp2_fast(c * (r.p_max - top)) : 0.0;
+            q_sum = r.q_max > -INFINITY ? r.q_sum * (double)exp2_fast(c * (r.q_max - q_top)) : 0.0;
+#pragma unroll
+            for (int s = MOST_CLUSTER / 2; s > 0; s /= 2) {
+                p_sum += __shfl_xor_sync(0xffffffffu, p_sum, s);
+                q_sum += __shfl_xor_sync(0xffffffffu, q_sum, s);
             }
-            top = t;
-            q_top = qt;
+            // (lanes from MOST_CLUSTER on hold nothing: the first one's are the cluster's)
+            top = __shfl_sync(0xffffffffu, top, 0);
+            arg = __shfl_sync(0xffffffffu, arg, 0);
+            q_top = __shfl_sync(0xffffffffu, q_top, 0);
+            p_sum = __shfl_sync(0xffffffffu, p_sum, 0);
+            q_sum = __shfl_sync(0xffffffffu, q_sum, 0);
         }
         turn ^= 1;
         if (bad || top == -INFINITY || (use_q && q_top == -INFINITY)) {      // numbers that are no distribution
             if (rank == 0 && tid == 0) atomicExch(&dc->status, (int)PSA_ERR_NUMERIC);
             break;
         }
-        const double p_scale = 1.0 / p_sum, q_scale = use_q ? 1.0 / q_sum : 0.0;
-        auto p_of = [&](float l) { return exp(((double)l - (double)top) * c) * p_scale; };
-        auto q_of = [&](float g) { return exp(((double)g - (double)q_top) * c) * q_scale; };
-        // ---- w = max(ka p - kb q, 0), or p without the children that were refused
+        // ---- in 64 bits: sums over the warps' parts into sums_s (and sums2_s), of all CTAs into the two results; every CTA tells its own
+        const double p_top = top, q_high = use_q ? q_top : 0.f;
+        double told[2];
+        auto exchange = [&](double x, double y) {
+            x = warp_sum(x);
+            y = warp_sum(y);
+            __syncthreads();
+            if (lane == 0) { sums_s[warp] = x; sums2_s[warp] = y; }
+            __syncthreads();
+            if (tid == 0) {
+                Record& r = records[turn];
+                r.p_sum = r.q_sum = 0;
+                for (int w = 0; w < V_WARPS; ++w) { r.p_sum += sums_s[w]; r.q_sum += sums2_s[w]; }
+            }
+            cluster_sync();
+            const double mine = lane < ranks ? read_cluster(&records[turn].p_sum, lane) : 0.0, mine2 = lane < ranks ? read_cluster(&records[turn].q_sum, lane) : 0.0;
+            told[0] = told[1] = 0;
+            for (int k = 0; k < ranks; ++k) {
+                told[0] += __shfl_sync(0xffffffffu, mine, k);
+                told[1] += __shfl_sync(0xffffffffu, mine2, k);
+            }
+            turn ^= 1;
+        };
+        bool sharp = false;                      // p_sum and q_sum are in 64 bits
+        auto sharpen = [&] {
+            if (sharp) return;
+            sharp = true;
+            double x = 0, y = 0;
+            over<T, false>(lrow, nullptr, w_low, w_high, lane, [&](float l, float, int, bool is) { const double w = exp_of(((double)l - p_top) * C); x += is ? w : 0.0; });
+            if (use_q) over<T, false>(qrow, nullptr, w_low, w_high, lane, [&](float l, float, int, bool is) { const double w = exp_of(((double)l - q_high) * C); y += is ? w : 0.0; });
+            exchange(x, y);
+            p_sum = told[0];
+            q_sum = told[1];
+        };
+        // ---- w = max(ka p - kb q, 0), or p without the children that were refused; not divided by p's sum
         double ka = 1, kb = 0, Z = 1, rest = 1;
         int tried = 0;
         bool only_p = true;                      // nothing was refused yet, or nothing is left
-        auto weight = [&](int v) -> double {
-            const double p = p_of(number(lp[v]));
-            if (only_p) return p;
-            if (use_q) return fmax(ka * p - kb * q_of(number(qp[v])), 0.0);
-            for (int k = 0; k < tried; ++k)
-                if (tried_s[k] == v) return 0.0;
-            return p;
+        double over_q = 0;                       // p_sum / q_sum
+        auto weight = [&](float l, float g, int v, bool is) -> double {
+            const double pw = exp_of(((double)l - p_top) * C);
+            if (!only_p && use_q) {
+                const double qw = exp_of(((double)g - q_high) * C);          // (by all lanes, also those that have no v)
+                return is ? fmax(ka * pw - kb * over_q * qw, 0.0) : 0.0;
+            }
+            bool gone = !is;
+            if (!only_p)
+                for (int k = 0; k < tried; ++k) gone |= tried_s[k] == v;
+            return gone ? 0.0 : pw;
         };
-        // Sums of w over the warps' parts into sums_s; the CTA's own; of all CTAs (every CTA tells its own).
-        double own_sum = 0;
         auto sum_weights = [&]() -> double {
             double s = 0;
-            for (int v = w_low + lane; v < w_high; v += 32) s += weight(v);
-            s = warp_sum(s);
-            __syncthreads();
-            if (lane == 0) sums_s[warp] = s;
-            __syncthreads();
-            own_sum = 0;
-            for (int w = 0; w < V_WARPS; ++w) own_sum += sums_s[w];
-            if (tid == 0) totals[turn] = own_sum;
-            cluster_sync();
-            double all = 0;
-            for (int k = 0; k < ranks; ++k) all += read_cluster(&totals[turn], k);
-            turn ^= 1;
-            return all;
+            if (!only_p && use_q) over<T, true>(lrow, qrow, w_low, w_high, lane, [&](float l, float g, int v, bool is) { s += weight(l, g, v, is); });
+            else over<T, false>(lrow, nullptr, w_low, w_high, lane, [&](float l, float g, int v, bool is) { s += weight(l, g, v, is); });
+            exchange(s, 0.0);
+            return told[0];
         };
         int taken = -1;
         bool summed = false, nothing = false;
@@ -266,25 +403,35 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
             if (!use_q || a.distinct)
                 for (int k = 0; k < tried; ++k) again |= tried_s[k] == x;
             if (again) continue;
-            const double u = a.uniform[first + i], px = p_of(number(lrow[x]));
-            if (!use_q) {
-                if (u * Z < px) { taken = i; continue; }
-                Z -= px;
-            } else {
-                const double qx = q_of(number(qrow[x])), part = a.distinct ? 1.0 / fmax(rest, 1e-300) : 1.0;
-                if (u * (qx * part) * Z < (only_p ? px : fmax(ka * px - kb * qx, 0.0))) { taken = i; continue; }
+            const double u = a.uniform[first + i], px = exp_of(((double)number(lrow[x]) - p_top) * C);
+            const double qx = use_q ? exp_of(((double)number(qrow[x]) - q_high) * C) : 0.0, part = use_q && a.distinct ? 1.0 / fmax(rest, 1e-300) : 1.0;
+            double left, right;
+            auto sides = [&] {
+                left = use_q ? u * (qx / q_sum * part) * Z : u * Z;
+                right = only_p || !use_q ? px / p_sum : fmax(ka * (px / p_sum) - kb * (qx / q_sum), 0.0);
+            };
+            sides();
+            if (!sharp && fabs(left - right) <= 3 * COARSE * (use_q ? fmax(left, right) : 1.0)) {
+                sharpen();
+                sides();
+            }
+            if (left < right) { taken = i; continue; }
+            if (use_q) {
+                sharpen();
                 kb = kb / Z + part;
                 ka = ka / Z;
-                rest -= qx;
+                rest -= qx / q_sum;
+            } else {
+                Z -= px / p_sum;
             }
             __syncthreads();
             if (tid == 0) tried_s[tried] = x;
             ++tried;
             __syncthreads();
             only_p = false;
-            summed = false;
             if (use_q) {
-                Z = sum_weights();
+                over_q = p_sum / q_sum;
+                Z = sum_weights() / p_sum;
                 summed = true;
                 nothing = !(Z > 0);
             }
@@ -301,51 +448,49 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
         }
         // ---- the draw: the first token at which the running sum of w passes u times the whole
         if (nothing) { only_p = true; summed = false; }
-        double all = summed ? Z : sum_weights();
+        double all = summed ? told[0] : sum_weights();
         if (!(all > 0)) { only_p = true; all = sum_weights(); }              // (all of p refused)
         // which CTA, then which warp's part; where roundings leave none behind the target, the last one with any weight
         double target = (double)a.uniform[first] * all, before = 0;
         int owner = -1, last = 0;
         for (int k = 0; k < ranks && owner < 0; ++k) {
-            const double s = read_cluster(&totals[turn ^ 1], k);
+            const double s = read_cluster(&records[turn ^ 1].p_sum, k);
             if (s > 0) last = k;
             if (s > 0 && before + s > target) owner = k; else before += s;
         }
         bool end = owner < 0;                    // the last one with any weight is meant
         if (end) owner = last;
         if (owner == rank) {
+            auto pick = [&](const double* sums) {        // of the warps' parts; target: from there on
+                int part = -1;
+                before = 0;
+                last = 0;
+                for (int w = 0; w < V_WARPS && part < 0; ++w) {
+                    if (sums[w] > 0) last = w;
+                    if (!end && sums[w] > 0 && before + sums[w] > target) part = w; else before += sums[w];
+                }
+                if (part < 0) { part = last; end = true; }
+                target -= before;
+                return part;
+            };
             target -= before;
-            before = 0;
-            int part = -1;
-            last = 0;
-            for (int w = 0; w < V_WARPS && part < 0; ++w) {
-                if (sums_s[w] > 0) last = w;
-                if (!end && sums_s[w] > 0 && before + sums_s[w] > target) part = w; else before += sums_s[w];
-            }
-            if (part < 0) { part = last; end = true; }
-            target -= before;
-            // that part once more, a sixteenth a warp
+            const int part = pick(sums_s);
+            // that part once more, an eighth a warp
+            const bool two = !only_p && use_q;
             const int p_low = min(low + part * each, high), p_high = min(p_low + each, high), fine = (p_high - p_low + V_WARPS - 1) / V_WARPS;
             const int f_low = min(p_low + warp * fine, p_high), f_high = min(f_low + fine, p_high);
+            auto at = [&](int v) { const bool is = v < f_high; return weight(is ? number(lrow[v]) : -INFINITY, is && two ? number(qrow[v]) : -INFINITY, v, is); };
             double s = 0;
-            for (int v = f_low + lane; v < f_high; v += 32) s += weight(v);
+            for (int v0 = f_low; v0 < f_high; v0 += 32) s += at(v0 + lane);
             s = warp_sum(s);
+            __syncthreads();
             if (lane == 0) sums2_s[warp] = s;
             __syncthreads();
-            before = 0;
-            part = -1;
-            last = 0;
-            for (int w = 0; w < V_WARPS && part < 0; ++w) {
-                if (sums2_s[w] > 0) last = w;
-                if (!end && sums2_s[w] > 0 && before + sums2_s[w] > target) part = w; else before += sums2_s[w];
-            }
-            if (part < 0) { part = last; end = true; }
-            target -= before;
-            if (warp == part) {
+            if (warp == pick(sums2_s)) {
                 before = 0;
                 int found = -1, some = -1;
                 for (int v0 = f_low; v0 < f_high && found < 0; v0 += 32) {
-                    const double x = v0 + lane < f_high ? weight(v0 + lane) : 0.0;
+                    const double x = at(v0 + lane);
                     double sum = x;
 #pragma unroll
                     for (int k = 1; k < 32; k *= 2) {
@@ -360,8 +505,7 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
                 if (lane == 0) drawn_s = found >= 0 ? found : some;
             }
             __syncthreads();
-            next = drawn_s;
-            if (tid == 0) a.next[b] = next;
+            if (tid == 0) a.next[b] = drawn_s;
         }
         if (rank == 0 && tid == 0) a.accepted[b] = stood;
         cluster_sync();                          // (nobody leaves while its shared memory is read)
@@ -517,18 +661,10 @@ cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t stre
 
 template <class T>
 int launch_verify(VerifyArgs a, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
-    static DeviceSetup setup;
-    const int sms = device_setup(&setup, [] {
-        return cudaFuncSetAttribute(verify_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (MOST_SLICE_BYTES + 32));
-    }, "verification set-up");
-    if (sms <= 0) return PSA_ERR_CUDA;
-    // as many CTAs a sequence as fit the GPU, of 2048 numbers at least
+    // as many CTAs a sequence as the GPU holds at a time, two an SM, of 2048 numbers at least
     int ranks = 1;
-    while (ranks < MOST_CLUSTER && 2LL * ranks * a.sequences <= sms && a.vocab > 2048 * ranks) ranks *= 2;
+    while (ranks < MOST_CLUSTER && 2LL * ranks * a.sequences <= 2 * 148 && a.vocab > 2048 * ranks) ranks *= 2;
     a.slice = ((a.vocab + ranks - 1) / ranks + 7) / 8 * 8;
-    const size_t part = ((size_t)a.slice * sizeof(T) + 31) / 16 * 16;
-    a.staged = part <= MOST_SLICE_BYTES;
-    const size_t smem = a.staged ? part * (a.drafts ? 2 : 1) : 0;
     cudaLaunchAttribute attr[2];
     for (int b0 = 0; b0 < a.sequences; b0 += 65535) {
         VerifyArgs x = a;
@@ -537,7 +673,7 @@ int launch_verify(VerifyArgs a, DeviceCounters* dc, DeviceCounters* dc_next, cud
         x.accepted += b0;
         x.next += b0;
         if (x.temperatures) x.temperatures += b0;
-        const cudaLaunchConfig_t cfg = config(dim3(ranks, x.sequences), V_THREADS, smem, stream, attr, ranks);
+        const cudaLaunchConfig_t cfg = config(dim3(ranks, x.sequences), V_THREADS, 0, stream, attr, ranks);
         const cudaError_t e = cudaLaunchKernelEx(&cfg, verify_kernel<T>, x, dc, b0 == 0 ? dc_next : nullptr);
         if (e != cudaSuccess) { set_cuda_error(e, "verify_kernel launch"); return PSA_ERR_CUDA; }
     }
@@ -556,7 +692,7 @@ cudaError_t launch_keep(const KeepArgs& a, DeviceCounters* dc, DeviceCounters* d
 int verify_drafts(const void* logits, long long logit_stride, const void* drafts, long long draft_stride, int vocab, int dtype, const int* tokens, const int* parents, const int* starts,
                   int sequences, int rows, const float* temperatures, const float* uniform, int distinct, int* path, int* accepted, int* next, DeviceCounters* dc,
                   DeviceCounters* dc_next, cudaStream_t stream) {
-    const VerifyArgs a = {logits, drafts, logit_stride, draft_stride, tokens, parents, starts, temperatures, uniform, path, accepted, next, vocab, sequences, rows, distinct, 0, 0};
+    const VerifyArgs a = {logits, drafts, logit_stride, draft_stride, tokens, parents, starts, temperatures, uniform, path, accepted, next, vocab, sequences, rows, distinct, 0};
     switch (dtype) {
         case PSA_F32: return launch_verify<float>(a, dc, dc_next, stream);
         case PSA_BF16: return launch_verify<__nv_bfloat16>(a, dc, dc_next, stream);
