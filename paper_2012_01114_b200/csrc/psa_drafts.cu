@@ -15,6 +15,7 @@
 // To read: the rows of the tokens on the path, and no others; which ones these are is known one after the other, so that what counts is how fast one row is read.  A
 // cluster of CTAs shares the rows of a sequence; a row costs one pass with a running maximum and one exchange of partial maxima and sums between the CTAs, a child with drafts that is refused two
 // more passes over what is then in the L2 cache.
+#include <string.h>
 #include <algorithm>
 #include <type_traits>
 
@@ -27,11 +28,11 @@ namespace psa {
 
 namespace {
 
-constexpr int V_WARPS = 8, V_THREADS = 32 * V_WARPS;
 constexpr int MOST_CLUSTER = 8;
-// Relative error of a sum of 32-bit exponentials: their argument goes through two roundings of 2^-24 of itself, 30 at most where a weight counts (2^-18.6 of the weight), ex2 gives 2^-22, and a number
-// takes part in no more than 8 + 64 additions before the sums go on in 64 bits (2^-17.8): below 2^-17 altogether.
-constexpr double COARSE = 1.0 / 65536;
+constexpr int V_CTAS = 3;                       // an SM
+// Relative error of a sum of 32-bit exponentials: their argument goes through two roundings of 2^-24 of itself, 30 at most where a weight counts (2^-18.6 of the weight), ex2 gives 2^-22, a number
+// takes part in no more than 36 additions before the sums go on in 64 bits and in 13 of the threads', warps' and CTAs' sums (2^-18.4): below 2^-17 altogether.
+constexpr float COARSE = 1.f / 65536;
 
 struct VerifyArgs {
     const void *logits, *drafts;
@@ -47,11 +48,13 @@ template <class T> __device__ __forceinline__ float number(T x) { return static_
 template <> __device__ __forceinline__ float number<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <> __device__ __forceinline__ float number<__half>(__half x) { return __half2float(x); }
 
-// What the CTAs of a cluster tell each other about a row.
-struct Record {
-    double p_sum, q_sum;
-    float p_max, q_max;
-    int likeliest, bad;
+// What the CTAs of a cluster tell each other: about a row, greatest numbers and sums in 32 bits; about a pass in 64 bits, sums.
+struct __align__(16) Record {
+    float p_max, q_max, p_sum, q_sum;
+    int likeliest, bad, unused[2];
+};
+struct __align__(16) Sums {
+    double p, q, a, b;
 };
 
 __device__ __forceinline__ double warp_sum(double x) {
@@ -59,71 +62,112 @@ __device__ __forceinline__ double warp_sum(double x) {
     for (int s = 16; s > 0; s /= 2) x += __shfl_xor_sync(0xffffffffu, x, s);
     return x;
 }
+// x to the same place in CTA `rank`'s shared memory; X: words of 16 bytes.
 template <class X>
-__device__ __forceinline__ X read_cluster(const X* p, uint32_t rank) {      // of CTA `rank`; X: words of 32 bits
-    X x;
-    const uint32_t a = cluster_map(p, rank);
+__device__ __forceinline__ void tell(X* to, const X& x, uint32_t rank) {
+    static_assert(sizeof(X) % 16 == 0 && alignof(X) == 16, "");
+    const uint32_t a = cluster_map(to, rank);
+    uint4 words[sizeof(X) / 16];
+    memcpy(words, &x, sizeof(X));
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(X) / 4); ++i) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(reinterpret_cast<uint32_t*>(&x)[i]) : "r"(a + 4 * i) : "memory");
-    return x;
+    for (int i = 0; i < (int)(sizeof(X) / 16); ++i) {
+        const uint4 v = words[i];
+        asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a + 16 * i), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    }
 }
 
-// exp2(z / 32) for z <= 0, called by all lanes of a warp together, to 2^-50: 2^(k / 32) (1 + e) with k the nearest whole number, the power from a table of 32 (one a lane), e by its Taylor series
-// (table-driven exponentials: Tang, 1989).
+// exp((x - top) / T) for x <= top, called by all lanes of a warp together, to 2^-50: with z = 32 (x - top) / (T ln 2), 2^(k / 32) (1 + e), k being the nearest whole number, the power from a table of
+// 32 (one a lane), e by its Taylor series (table-driven exponentials: Tang, 1989).  Zero below 2^-1018 and for -inf.
 struct Exp {
-    double power;                                // 2^(lane / 32)
-    __device__ __forceinline__ Exp(int lane) : power(exp2(lane / 32.0)) {}
-    __device__ __forceinline__ double operator()(double z) const {
+    double power, top, C;                        // 2^(lane / 32); C: 32 / (T ln 2)
+    float top32, c;                              // the same in 32 bits; c: 1 / (T ln 2)
+    __device__ __forceinline__ Exp(double power_, float top_, double C_) : power(power_), top(top_), C(C_), top32(top_), c((float)(C_ / 32)) {}
+    __device__ __forceinline__ double operator()(float x) const {
         constexpr double L = 0.69314718055994530942 / 32;
-        z = fmax(z, -32704.0);                   // 2^-1022
-        const double t = z + 6755399441055744.0, s = z - (t - 6755399441055744.0);
+        const double z = ((double)x - top) * C, t = z + 6755399441055744.0, s = z - (t - 6755399441055744.0);
         const int k = __double2loint(t);
         const double e = s * fma(s, fma(s, fma(s, fma(s, L * L * L * L * L / 120, L * L * L * L / 24), L * L * L / 6), L * L / 2), L);
         const double p = __hiloint2double(__shfl_sync(0xffffffffu, __double2hiint(power), k & 31), __shfl_sync(0xffffffffu, __double2loint(power), k & 31));
         const double w = fma(p, e, p);
-        return k <= -32672 ? 0.0 : __hiloint2double(__double2hiint(w) + (k >> 5) * 1048576, __double2loint(w));
+        return c * (x - top32) > -1018.f ? __hiloint2double(__double2hiint(w) + (k >> 5) * 1048576, __double2loint(w)) : 0.0;
     }
 };
 
-// f(number of the first row, number of the second, v, whether there is such a v) for v = low .. high - 1, by a warp, every call by all lanes.  The rows may begin anywhere: up to a
-// boundary of 16 bytes, and behind the last, numbers are read one by one, and all are where the rows lie differently.
+// f(number of the first row, number of the second, v) for v = low .. high - 1, by a warp, every call by all lanes: those that have no v call it with -inf.  Numbers are read two at a time,
+// one by one up to a boundary of two and where the rows lie differently.
 template <class T, bool TWO, class F>
 __device__ __forceinline__ void over(const T* p, const T* q, int low, int high, int lane, F f) {
-    constexpr int VEC = 16 / sizeof(T);
     if (low >= high) return;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p + low), too = TWO ? reinterpret_cast<uintptr_t>(q + low) : at;
-    const bool alike = ((at ^ too) & 15u) == 0;
-    const int lead = alike ? min((int)((16 - (at & 15u)) % 16 / sizeof(T)), high - low) : high - low, vecs = (high - low - lead) / VEC;
-    auto singly = [&](int from, int to) {
-        for (int v0 = from; v0 < to; v0 += 32) {
-            const int v = v0 + lane;
-            const bool is = v < to;
-            f(is ? number(p[v]) : -INFINITY, TWO && is ? number(q[v]) : -INFINITY, v, is);
-        }
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p + low) / sizeof(T), too = TWO ? reinterpret_cast<uintptr_t>(q + low) / sizeof(T) : at;
+    const bool alike = ((at ^ too) & 1u) == 0;
+    struct __align__(2 * sizeof(T)) Two { T x, y; };
+    const int lead = alike ? (int)(at & 1u) : high - low, pairs = (high - low - lead) / 2;
+    const Two* const p2 = reinterpret_cast<const Two*>(p + low + lead);
+    const Two* const q2 = TWO ? reinterpret_cast<const Two*>(q + low + lead) : p2;
+    constexpr int AHEAD = 2;                     // rounds
+    Two x[AHEAD], y[AHEAD];
+    auto load = [&](int i, int k) {
+        if (i >= pairs) return;
+        x[k] = p2[i];
+        if (TWO) y[k] = q2[i];
     };
-    singly(low, low + lead);
-    const uint4* const p4 = reinterpret_cast<const uint4*>(p + low + lead);
-    const uint4* const q4 = TWO ? reinterpret_cast<const uint4*>(q + low + lead) : p4;
-    constexpr int AHEAD = 4;
-    for (int i0 = 0; i0 < vecs; i0 += 32 * AHEAD) {
-        uint4 x[AHEAD], y[TWO ? AHEAD : 1];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int i = min(i0 + 32 * k + lane, vecs - 1);
-            x[k] = __ldg(p4 + i);
-            if (TWO) y[TWO ? k : 0] = __ldg(q4 + i);
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            if (i0 + 32 * k >= vecs) break;
-            const int i = i0 + 32 * k + lane;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                f(i < vecs ? number(reinterpret_cast<const T*>(&x[k])[e]) : -INFINITY, TWO && i < vecs ? number(reinterpret_cast<const T*>(&y[TWO ? k : 0])[e]) : -INFINITY, low + lead + i * VEC + e,
-                  i < vecs);
-        }
+    load(lane, 0);
+    load(lane + 32, 1);
+#pragma unroll 1
+    for (int i0 = 0; i0 < pairs; i0 += 32) {
+        const Two x0 = x[0], y0 = y[0];
+        const int i = i0 + lane, v = low + lead + 2 * i;
+        x[0] = x[1];
+        if (TWO) y[0] = y[1];
+        load(i + 32 * AHEAD, 1);
+        const bool is = i < pairs;
+        f(is ? number(x0.x) : -INFINITY, TWO && is ? number(y0.x) : -INFINITY, v);
+        f(is ? number(x0.y) : -INFINITY, TWO && is ? number(y0.y) : -INFINITY, v + 1);
     }
-    singly(low + lead + vecs * VEC, high);
+#pragma unroll 1
+    for (int v0 = low; v0 < high;) {             // one by one: those ahead of the pairs, then those behind
+        const int end = v0 < low + lead ? low + lead : high, v = v0 + lane;
+        if (end == high && v0 < low + lead + 2 * pairs && v0 >= low + lead) { v0 = low + lead + 2 * pairs; continue; }
+        f(v < end ? number(p[v]) : -INFINITY, TWO && v < end ? number(q[v]) : -INFINITY, v);
+        v0 = min(v0 + 32, end);
+    }
+}
+// Sum of exp over a part of a row, without the tokens of a list.
+template <class T>
+__device__ __noinline__ double sum_one(const T* row, int low, int high, const Exp& exp_of, const int* without, int n, int lane) {
+    const Exp e = exp_of;
+    double sum = 0;
+    over<T, false>(row, nullptr, low, high, lane, [&](float x, float, int v) {
+        double w = e(x);
+        for (int k = 0; k < n; ++k)
+            if (without[k] == v) w = 0;
+        sum += w;
+    });
+    return sum;
+}
+// Over a part of two rows: sums of exp_p and of exp_q, and of both where exp_p > k exp_q.
+template <class T>
+__device__ __noinline__ Sums sum_both(const T* p, const T* q, int low, int high, const Exp& exp_p, const Exp& exp_q, double k, int lane) {
+    const Exp ep = exp_p, eq = exp_q;
+    Sums s = {0, 0, 0, 0};
+    over<T, true>(p, q, low, high, lane, [&](float x, float y, int) {
+        const double pw = ep(x), qw = eq(y);     // (by all lanes)
+        s.p += pw;
+        s.q += qw;
+        if (pw > k * qw) { s.a += pw; s.b += qw; }
+    });
+    return s;
+}
+// Sum of max(exp_p - k exp_q, 0).
+template <class T>
+__device__ __noinline__ double sum_rest(const T* p, const T* q, int low, int high, const Exp& exp_p, const Exp& exp_q, double k, int lane) {
+    const Exp ep = exp_p, eq = exp_q;
+    double sum = 0;
+    over<T, true>(p, q, low, high, lane, [&](float x, float y, int) {
+        const double pw = ep(x), qw = eq(y);
+        sum += fmax(fma(-k, qw, pw), 0.0);
+    });
+    return sum;
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -131,87 +175,123 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Two numbers at a time.
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 pair_as(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
 
-// Greatest number of a part of a row, the first place that has it (ARG), whether a number is NaN or infinite, and the sum of 2^(c (x - greatest)) in 32 bits (SUM).  Threads take vectors of 16 bytes in turn.
+// Of a thread's share of a part of a row (vectors of 16 bytes in turn): the greatest number, the first place that has it (GREEDY), whether a number is NaN or +inf, and the sum of
+// 2^(c (x - greatest)) in 32 bits (not GREEDY).  Bound by ex2, 16 a clock on an SM: everything else is done two numbers at a time, and a NaN is found in the sum.
 struct Part {
-    float top;
+    float top, sum;
     int arg;
     bool bad;
-    double sum;
 };
-template <class T, bool GREEDY>
+template <class T, int THREADS, bool GREEDY>
 __device__ __forceinline__ Part part_of_row(const T* row, int low, int high, float c, int tid) {
-    constexpr int VEC = 16 / sizeof(T);
-    Part r = {-INFINITY, 0x7fffffff, false, 0.0};
-    float sum = 0.f;
-    int chains = 0;
+    constexpr int VEC = 16 / sizeof(T), LONGEST = 8;     // vectors whose sum is formed in 32 bits
+    Part r = {-INFINITY, 0.f, 0x7fffffff, false};
+    uint64_t sum2 = 0;
+    double whole = 0;
+    int chain = 0;
     const uintptr_t at = reinterpret_cast<uintptr_t>(row + low);
     const int n = high - low, lead = min((int)((16 - (at & 15u)) % 16 / sizeof(T)), n), vecs = (n - lead) / VEC, done = lead + vecs * VEC;
     auto raise = [&](float m) {                  // a new greatest number
         const float f = r.top > -INFINITY ? exp2_fast(c * (r.top - m)) : 0.f;
-        sum *= f;
-        r.sum *= (double)f;
+        sum2 = mul2(sum2, pair_of(f, f));
+        whole *= (double)f;
         r.top = m;
     };
     auto one = [&](int v) {
         const float x = number(row[v]);
-        r.bad |= !(x <= 3.402823466e38f);
         if (GREEDY) {
+            r.bad |= !(x <= 3.402823466e38f);
             if (x > r.top || (x == r.top && v < r.arg)) { r.top = x; r.arg = v; }
-        } else if (x > -INFINITY) {
+        } else {
             if (x > r.top) raise(x);
-            sum += exp2_fast(c * (x - r.top));
+            sum2 = add2(sum2, pair_of(exp2_fast(c * (x - (r.top > -INFINITY ? r.top : 0.f))), 0.f));
         }
     };
     if (tid < lead) one(low + tid);
     const uint4* const row4 = reinterpret_cast<const uint4*>(row + low + lead);
     constexpr int AHEAD = 4;
-    for (int i0 = 0; i0 < vecs; i0 += AHEAD * V_THREADS) {
+    for (int i0 = 0; i0 < vecs; i0 += AHEAD * THREADS) {
         uint4 x[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
-            if (i0 + k * V_THREADS + tid < vecs) x[k] = __ldg(row4 + i0 + k * V_THREADS + tid);
+            if (i0 + k * THREADS + tid < vecs) x[k] = __ldg(row4 + i0 + k * THREADS + tid);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            const int i = i0 + k * V_THREADS + tid;
-            if (i >= vecs) break;
-            float y[VEC], m = -INFINITY;
+            const int i = i0 + k * THREADS + tid;
+            if (i < vecs) {
+                float y[VEC], m = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                y[e] = number(reinterpret_cast<const T*>(&x[k])[e]);
-                r.bad |= !(y[e] <= 3.402823466e38f);
-                m = fmaxf(m, y[e]);
-            }
-            if (GREEDY) {
-                if (m > r.top) {
-                    r.top = m;
-#pragma unroll
-                    for (int e = VEC - 1; e >= 0; --e)
-                        if (y[e] == m) r.arg = low + lead + i * VEC + e;
+                for (int e = 0; e < VEC; ++e) {
+                    y[e] = number(reinterpret_cast<const T*>(&x[k])[e]);
+                    if (GREEDY) r.bad |= !(y[e] <= 3.402823466e38f);
+                    m = fmaxf(m, y[e]);
                 }
-            } else {
-                if (m > r.top) raise(m);
-                const float from = r.top > -INFINITY ? r.top : 0.f;
-                float s = 0.f;
+                if (GREEDY) {
+                    if (m > r.top) {
+                        r.top = m;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) s += exp2_fast(c * (y[e] - from));
-                sum += s;
-                if (++chains == 64) { r.sum += (double)sum; sum = 0.f; chains = 0; }
+                        for (int e = VEC - 1; e >= 0; --e)
+                            if (y[e] == m) r.arg = low + lead + i * VEC + e;
+                    }
+                } else {
+                    if (m > r.top) raise(m);
+                    const float from = r.top > -INFINITY ? -r.top : 0.f;
+                    const uint64_t from2 = pair_of(from, from), c2 = pair_of(c, c);
+#pragma unroll
+                    for (int e = 0; e < VEC; e += 2) {
+                        const float2 z = pair_as(mul2(add2(pair_of(y[e], y[e + 1]), from2), c2));
+                        sum2 = add2(sum2, pair_of(exp2_fast(z.x), exp2_fast(z.y)));
+                    }
+                    if (++chain == LONGEST) {
+                        whole += (double)pair_as(sum2).x + (double)pair_as(sum2).y;
+                        sum2 = 0;
+                        chain = 0;
+                    }
+                }
             }
         }
     }
     if (tid < n - done) one(low + done + tid);
-    r.sum += (double)sum;
+    if (!GREEDY) {
+        r.sum = (float)(whole + (double)(pair_as(sum2).x + pair_as(sum2).y));
+        r.bad = !(r.sum < INFINITY) || r.top == INFINITY;
+    }
     return r;
 }
 
-template <class T>
-__global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, DeviceCounters* dc, DeviceCounters* dc_next) {
+template <class T, int V_WARPS>
+__global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verify_kernel(const VerifyArgs a, DeviceCounters* dc, DeviceCounters* dc_next) {
+    constexpr int V_THREADS = 32 * V_WARPS;
     __shared__ int parent_s[PSA_TREE_MOST], token_s[PSA_TREE_MOST], tried_s[PSA_TREE_MOST];
-    __shared__ double sums_s[V_WARPS], sums2_s[V_WARPS];
-    __shared__ float max_s[V_WARPS], max2_s[V_WARPS];
-    __shared__ int arg_s[V_WARPS], bad_s[V_WARPS], drawn_s;
-    __shared__ Record records[2];               // told in turn
+    __shared__ Record warps_s[V_WARPS];
+    __shared__ Sums parts_s[V_WARPS];
+    __shared__ double sums_s[V_WARPS], fine_s[V_WARPS];
+    __shared__ int drawn_s;
+    // What the CTAs tell each other, in two places by turns: written ahead of a barrier, read behind it.  (Each writes to all others.  Read from there by every warp it was 3 us a token with 32 warps.)
+    __shared__ Record records[2][MOST_CLUSTER];
+    __shared__ Sums sums[2][MOST_CLUSTER];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int ranks = (int)gridDim.x, rank = (int)blockIdx.x, b = (int)blockIdx.y;       // (a cluster is a row of the grid)
@@ -243,186 +323,206 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
     }
     if (__syncthreads_or(strange) && tid == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
 
+    // (shared memory of another CTA is there once that one has begun: arrived here, waited for ahead of the first word to it)
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    bool met = false;
     const double C = greedy ? 1.0 : 46.166241308446828384 / (double)temperature;         // 32 / (T ln 2): units of Exp
     const float c = (float)(C / 32);
-    const Exp exp_of(lane);
     const T* const all_logits = static_cast<const T*>(a.logits);
     const T* const all_drafts = static_cast<const T*>(a.drafts);
     const int low = min(rank * a.slice, a.vocab), high = min(low + a.slice, a.vocab);    // this CTA's part of the vocabulary
     const int each = (high - low + V_WARPS - 1) / V_WARPS;                               // of its warps, one after another
     const int w_low = min(low + warp * each, high), w_high = min(w_low + each, high);
 
-    int turn = 0;                                // of records
+    int turn = 0;                                // of records and sums: one exchange, one turn
     int node = 0, stood = 0, next = -1;
     for (;;) {
         const T* const lrow = all_logits + (size_t)(first + node) * a.logit_stride;
-        bool leaf = true;
-        for (int i = node + 1 + tid; i < count; i += V_THREADS) leaf &= parent_s[i] != node;
-        leaf = !__syncthreads_or(!leaf);         // (also: what the token before left in shared memory is done with)
-        const bool use_q = all_drafts && !greedy && !leaf;
+        // the token's first child, and what it is tried with (asked for here, used behind the exchange)
+        int child = count;
+        for (int i0 = node + 1; i0 < count && child == count; i0 += 32) {
+            const uint32_t m = __ballot_sync(0xffffffffu, i0 + lane < count && parent_s[min(i0 + lane, count - 1)] == node);
+            if (m) child = i0 + __ffs(m) - 1;
+        }
+        const bool use_q = all_drafts && !greedy && child < count;
         const T* const qrow = all_drafts + (use_q ? (size_t)(first + node) * a.draft_stride : 0);
-        // ---- the rows' greatest numbers and sums: of the threads, the CTA, the cluster
-        Part p = greedy ? part_of_row<T, true>(lrow, low, high, 0.f, tid) : part_of_row<T, false>(lrow, low, high, c, tid);
-        Part q = {-INFINITY, 0, false, 0.0};
-        if (use_q) q = part_of_row<T, false>(qrow, low, high, c, tid);
-        auto warp_joined = [&](Part& x) {
-            float top = x.top;
-            int arg = x.arg;
+        float child_u = 0.f, child_l = 0.f, child_q = 0.f;
+        if (!greedy && child < count && token_s[child] >= 0) {
+            child_u = a.uniform[first + child];
+            child_l = number(lrow[token_s[child]]);
+            child_q = number((use_q ? qrow : lrow)[token_s[child]]);
+        }
+        // ---- the rows' greatest numbers and sums: of the threads, the warp, the CTA, the cluster
+        Part p = greedy ? part_of_row<T, V_THREADS, true>(lrow, low, high, 0.f, tid) : part_of_row<T, V_THREADS, false>(lrow, low, high, c, tid);
+        Part q = {-INFINITY, 0.f, 0, false};
+        if (use_q) q = part_of_row<T, V_THREADS, false>(qrow, low, high, c, tid);
+        auto joined = [&](Record r, int most) {  // of a lane each, as one (those of lanes from `most` on hold nothing)
+            float t = r.p_max, qt = r.q_max;
 #pragma unroll
             for (int s = 16; s > 0; s /= 2) {
-                const float y = __shfl_xor_sync(0xffffffffu, top, s);
-                const int k = __shfl_xor_sync(0xffffffffu, arg, s);
-                if (y > top || (y == top && k < arg)) { top = y; arg = k; }
+                if (s >= most) continue;
+                const float y = __shfl_xor_sync(0xffffffffu, t, s);
+                if (greedy) {
+                    const int k = __shfl_xor_sync(0xffffffffu, r.likeliest, s);
+                    if (y > t || (y == t && k < r.likeliest)) r.likeliest = k;
+                }
+                t = fmaxf(t, y);
+                if (use_q) qt = fmaxf(qt, __shfl_xor_sync(0xffffffffu, qt, s));
             }
-            x.sum = warp_sum(x.top > -INFINITY ? x.sum * (double)exp2_fast(c * (x.top - top)) : 0.0);
-            x.top = top;
-            x.arg = arg;
-            x.bad = __any_sync(0xffffffffu, x.bad);
+            r.bad = __any_sync(0xffffffffu, r.bad != 0);
+            if (!greedy) {
+                r.p_sum = r.p_max > -INFINITY ? r.p_sum * exp2_fast(c * (r.p_max - t)) : 0.f;
+                r.q_sum = r.q_max > -INFINITY ? r.q_sum * exp2_fast(c * (r.q_max - qt)) : 0.f;
+#pragma unroll
+                for (int s = 16; s > 0; s /= 2) {
+                    if (s >= most) continue;
+                    r.p_sum += __shfl_xor_sync(0xffffffffu, r.p_sum, s);
+                    if (use_q) r.q_sum += __shfl_xor_sync(0xffffffffu, r.q_sum, s);
+                }
+            }
+            r.p_max = t;
+            r.q_max = qt;
+            return r;
         };
-        warp_joined(p);
-        if (use_q) warp_joined(q);
-        if (lane == 0) { max_s[warp] = p.top; max2_s[warp] = q.top; arg_s[warp] = p.arg; bad_s[warp] = p.bad || q.bad; sums_s[warp] = p.sum; sums2_s[warp] = q.sum; }
-        __syncthreads();
-        if (tid == 0) {
-            Record r = {0.0, 0.0, -INFINITY, -INFINITY, 0x7fffffff, 0};
-            for (int w = 0; w < V_WARPS; ++w) {
-                if (max_s[w] > r.p_max || (max_s[w] == r.p_max && arg_s[w] < r.likeliest)) { r.p_max = max_s[w]; r.likeliest = arg_s[w]; }
-                r.q_max = fmaxf(r.q_max, max2_s[w]);
-                r.bad |= bad_s[w];
-            }
-            for (int w = 0; w < V_WARPS; ++w) {
-                if (max_s[w] > -INFINITY) r.p_sum += sums_s[w] * (double)exp2_fast(c * (max_s[w] - r.p_max));
-                if (max2_s[w] > -INFINITY) r.q_sum += sums2_s[w] * (double)exp2_fast(c * (max2_s[w] - r.q_max));
-            }
-            records[turn] = r;
-        }
-        cluster_sync();
-        float top = -INFINITY, q_top = -INFINITY;
-        int arg = 0x7fffffff;
-        bool bad = false;
-        double p_sum = 0, q_sum = 0;
+        const Record none = {-INFINITY, -INFINITY, 0.f, 0.f, 0x7fffffff, 0, {0, 0}};
         {
-            const Record r = lane < ranks ? read_cluster(&records[turn], lane) : Record{0.0, 0.0, -INFINITY, -INFINITY, 0x7fffffff, 0};
-            top = r.p_max;
-            arg = r.likeliest;
-            q_top = r.q_max;
-#pragma unroll
-            for (int s = MOST_CLUSTER / 2; s > 0; s /= 2) {
-                const float y = __shfl_xor_sync(0xffffffffu, top, s);
-                const int k = __shfl_xor_sync(0xffffffffu, arg, s);
-                if (y > top || (y == top && k < arg)) { top = y; arg = k; }
-                q_top = fmaxf(q_top, __shfl_xor_sync(0xffffffffu, q_top, s));
-            }
-            bad = __any_sync(0xffffffffu, r.bad != 0);
-            p_sum = r.p_max > -INFINITY ? r.p_sum * (double)exp2_fast(c * (r.p_max - top)) : 0.0;
-            q_sum = r.q_max > -INFINITY ? r.q_sum * (double)exp2_fast(c * (r.q_max - q_top)) : 0.0;
-#pragma unroll
-            for (int s = MOST_CLUSTER / 2; s > 0; s /= 2) {
-                p_sum += __shfl_xor_sync(0xffffffffu, p_sum, s);
-                q_sum += __shfl_xor_sync(0xffffffffu, q_sum, s);
-            }
-            // (lanes from MOST_CLUSTER on hold nothing: the first one's are the cluster's)
-            top = __shfl_sync(0xffffffffu, top, 0);
-            arg = __shfl_sync(0xffffffffu, arg, 0);
-            q_top = __shfl_sync(0xffffffffu, q_top, 0);
-            p_sum = __shfl_sync(0xffffffffu, p_sum, 0);
-            q_sum = __shfl_sync(0xffffffffu, q_sum, 0);
+            const Record r = joined(Record{p.top, q.top, p.sum, q.sum, p.arg, p.bad || q.bad, {0, 0}}, 32);
+            if (lane == 0) warps_s[warp] = r;
         }
+        if (!met) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        met = true;
+        __syncthreads();
+        if (warp == 0) {
+            const Record r = joined(lane < V_WARPS ? warps_s[lane] : none, 32);
+            if (lane < ranks) tell(&records[turn][rank], r, lane);
+        }
+        __syncwarp();
+        cluster_sync();
+        static_assert((MOST_CLUSTER & (MOST_CLUSTER - 1)) == 0, "");
+        const Record row = joined(lane % MOST_CLUSTER < ranks ? records[turn][lane % MOST_CLUSTER] : none, MOST_CLUSTER);        // (the same in every group of lanes)
         turn ^= 1;
-        if (bad || top == -INFINITY || (use_q && q_top == -INFINITY)) {      // numbers that are no distribution
+        if (row.bad || row.p_max == -INFINITY || (use_q && row.q_max == -INFINITY)) {      // numbers that are no distribution
             if (rank == 0 && tid == 0) atomicExch(&dc->status, (int)PSA_ERR_NUMERIC);
             break;
         }
-        // ---- in 64 bits: sums over the warps' parts into sums_s (and sums2_s), of all CTAs into the two results; every CTA tells its own
-        const double p_top = top, q_high = use_q ? q_top : 0.f;
-        double told[2];
-        auto exchange = [&](double x, double y) {
-            x = warp_sum(x);
-            y = warp_sum(y);
-            __syncthreads();
-            if (lane == 0) { sums_s[warp] = x; sums2_s[warp] = y; }
-            __syncthreads();
-            if (tid == 0) {
-                Record& r = records[turn];
-                r.p_sum = r.q_sum = 0;
-                for (int w = 0; w < V_WARPS; ++w) { r.p_sum += sums_s[w]; r.q_sum += sums2_s[w]; }
+        const float top = row.p_max, q_top = use_q ? row.q_max : 0.f;
+        int taken = -1;
+        if (greedy) {
+            for (int i0 = child; i0 < count && taken < 0; i0 += 32) {
+                const int i = min(i0 + lane, count - 1);
+                const uint32_t m = __ballot_sync(0xffffffffu, i0 + lane < count && parent_s[i] == node && token_s[i] == row.likeliest);
+                if (m) taken = i0 + __ffs(m) - 1;
             }
+            if (taken < 0) {
+                next = row.likeliest;
+                break;
+            }
+            node = taken;
+            ++stood;
+            if (rank == 0 && tid == 0) a.path[first + stood] = taken;
+            continue;
+        }
+        // ---- the first child by the sums in 32 bits: taken where that is certain
+        if (child < count && token_s[child] >= 0) {
+            const float px = exp2_fast(c * (child_l - top)) / row.p_sum;
+            const float left = use_q ? child_u * (exp2_fast(c * (child_q - q_top)) / row.q_sum) : child_u, right = px;
+            if (right - left > 3 * COARSE * (use_q ? right : 1.f)) {
+                node = child;
+                ++stood;
+                if (rank == 0 && tid == 0) a.path[first + stood] = child;
+                continue;
+            }
+        }
+        // ---- in 64 bits from here on: w = max(p - k q, 0) with k = kb / ka times what brings q to p's size, or p without the children that were refused
+        const double power = exp2(lane / 32.0);
+        const Exp exp_p(power, top, C), exp_q(power, q_top, C);
+        Sums told = {0, 0, 0, 0};                // of all CTAs, by `exchange`, which leaves the warps' in parts_s
+        auto exchange = [&](Sums s) {
+            s.p = warp_sum(s.p);
+            s.q = warp_sum(s.q);
+            if (use_q) {
+                s.a = warp_sum(s.a);
+                s.b = warp_sum(s.b);
+            }
+            __syncthreads();
+            if (lane == 0) parts_s[warp] = s;
+            __syncthreads();
+            if (warp == 0) {
+                Sums x = lane < V_WARPS ? parts_s[lane] : Sums{0, 0, 0, 0};
+                x = Sums{warp_sum(x.p), warp_sum(x.q), warp_sum(x.a), warp_sum(x.b)};
+                if (lane < ranks) tell(&sums[turn][rank], x, lane);
+            }
+            __syncwarp();
             cluster_sync();
-            const double mine = lane < ranks ? read_cluster(&records[turn].p_sum, lane) : 0.0, mine2 = lane < ranks ? read_cluster(&records[turn].q_sum, lane) : 0.0;
-            told[0] = told[1] = 0;
+            told = Sums{0, 0, 0, 0};
             for (int k = 0; k < ranks; ++k) {
-                told[0] += __shfl_sync(0xffffffffu, mine, k);
-                told[1] += __shfl_sync(0xffffffffu, mine2, k);
+                const Sums x = sums[turn][k];
+                told.p += x.p;
+                told.q += x.q;
+                told.a += x.a;
+                told.b += x.b;
             }
             turn ^= 1;
         };
-        bool sharp = false;                      // p_sum and q_sum are in 64 bits
-        auto sharpen = [&] {
-            if (sharp) return;
-            sharp = true;
-            double x = 0, y = 0;
-            over<T, false>(lrow, nullptr, w_low, w_high, lane, [&](float l, float, int, bool is) { const double w = exp_of(((double)l - p_top) * C); x += is ? w : 0.0; });
-            if (use_q) over<T, false>(qrow, nullptr, w_low, w_high, lane, [&](float l, float, int, bool is) { const double w = exp_of(((double)l - q_high) * C); y += is ? w : 0.0; });
-            exchange(x, y);
-            p_sum = told[0];
-            q_sum = told[1];
-        };
-        // ---- w = max(ka p - kb q, 0), or p without the children that were refused; not divided by p's sum
-        double ka = 1, kb = 0, Z = 1, rest = 1;
+        double p_sum = 0, q_sum = 0;
+        bool sharp = false;                      // these are known
+        double ka = 1, kb = 0, Z = 1, rest = 1, k = 0;
         int tried = 0;
         bool only_p = true;                      // nothing was refused yet, or nothing is left
-        double over_q = 0;                       // p_sum / q_sum
-        auto weight = [&](float l, float g, int v, bool is) -> double {
-            const double pw = exp_of(((double)l - p_top) * C);
-            if (!only_p && use_q) {
-                const double qw = exp_of(((double)g - q_high) * C);          // (by all lanes, also those that have no v)
-                return is ? fmax(ka * pw - kb * over_q * qw, 0.0) : 0.0;
-            }
-            bool gone = !is;
-            if (!only_p)
-                for (int k = 0; k < tried; ++k) gone |= tried_s[k] == v;
-            return gone ? 0.0 : pw;
+        // How the sums of w follow from parts_s and sums: a part's is p, or a - k b where both were summed over the numbers that are left.
+        bool by_ab = false, summed = false, nothing = false;
+        auto part_sum = [&](const Sums& s) { return by_ab ? fmax(fma(-k, s.b, s.a), 0.0) : s.p; };
+        auto sum_weights = [&] {
+            by_ab = false;
+            const double s = !only_p && use_q ? sum_rest(lrow, qrow, w_low, w_high, exp_p, exp_q, k, lane) : sum_one(lrow, w_low, w_high, exp_p, tried_s, only_p ? 0 : tried, lane);
+            exchange(Sums{s, 0, 0, 0});
+            summed = true;
         };
-        auto sum_weights = [&]() -> double {
-            double s = 0;
-            if (!only_p && use_q) over<T, true>(lrow, qrow, w_low, w_high, lane, [&](float l, float g, int v, bool is) { s += weight(l, g, v, is); });
-            else over<T, false>(lrow, nullptr, w_low, w_high, lane, [&](float l, float g, int v, bool is) { s += weight(l, g, v, is); });
-            exchange(s, 0.0);
-            return told[0];
-        };
-        int taken = -1;
-        bool summed = false, nothing = false;
-        for (int i = node + 1; i < count && taken < 0 && !nothing; ++i) {
+        for (int i = child; i < count && taken < 0 && !nothing; ++i) {
             if (parent_s[i] != node || token_s[i] < 0) continue;
             const int x = token_s[i];
-            if (greedy) {
-                if (x == arg) taken = i;
-                continue;
-            }
             bool again = false;                  // a sibling with the same token was refused: nothing is left of it
             if (!use_q || a.distinct)
-                for (int k = 0; k < tried; ++k) again |= tried_s[k] == x;
+                for (int n = 0; n < tried; ++n) again |= tried_s[n] == x;
             if (again) continue;
-            const double u = a.uniform[first + i], px = exp_of(((double)number(lrow[x]) - p_top) * C);
-            const double qx = use_q ? exp_of(((double)number(qrow[x]) - q_high) * C) : 0.0, part = use_q && a.distinct ? 1.0 / fmax(rest, 1e-300) : 1.0;
-            double left, right;
-            auto sides = [&] {
-                left = use_q ? u * (qx / q_sum * part) * Z : u * Z;
-                right = only_p || !use_q ? px / p_sum : fmax(ka * (px / p_sum) - kb * (qx / q_sum), 0.0);
-            };
-            sides();
-            if (!sharp && fabs(left - right) <= 3 * COARSE * (use_q ? fmax(left, right) : 1.0)) {
-                sharpen();
-                sides();
+            const double u = a.uniform[first + i], px = exp_p(number(lrow[x])), qx = use_q ? exp_q(number(qrow[x])) : 0.0;
+            // Refused for certain by the sums in 32 bits?  (Without drafts the comparison is sharpened only where it is near; with drafts w needs the sums anyway.)
+            const bool clear = !sharp && only_p && use_q && u * (qx / (double)row.q_sum) - px / (double)row.p_sum > 3 * (double)COARSE * u * (qx / (double)row.q_sum);
+            if (clear) {
+                // both rows' sums and those over the numbers that are left, by k in 32 bits, in one pass.  The numbers that k's last bits move from one side to the other are second order in its error,
+                // relative to what is left squared; where that is more than 1e-12 the pass is made again.
+                const double k0 = (double)row.p_sum / (double)row.q_sum;
+                exchange(sum_both(lrow, qrow, w_low, w_high, exp_p, exp_q, k0, lane));
+                p_sum = told.p;
+                q_sum = told.q;
+                sharp = true;
+                k = p_sum / q_sum;
+                const double off = k0 / k - 1, left = fmax(fma(-k, told.b, told.a), 0.0) / p_sum;
+                by_ab = summed = off * off <= 1e-12 * left * left;
+            } else {
+                if (!sharp && (use_q || fabs(u * Z - px / (double)row.p_sum) <= 3 * (double)COARSE)) {
+                    exchange(Sums{sum_one(lrow, w_low, w_high, exp_p, tried_s, 0, lane), use_q ? sum_one(qrow, w_low, w_high, exp_q, tried_s, 0, lane) : 0.0, 0, 0});
+                    p_sum = told.p;
+                    q_sum = told.q;
+                    sharp = true;
+                    if (!use_q) {                // (what was refused before, again)
+                        Z = 1;
+                        for (int n = 0; n < tried; ++n) Z -= exp_p(number(lrow[tried_s[n]])) / p_sum;
+                    }
+                }
+                const double part = use_q && a.distinct ? 1.0 / fmax(rest, 1e-300) : 1.0, pp = px / (sharp ? p_sum : (double)row.p_sum), qq = use_q ? qx / q_sum : 0.0;
+                if (use_q ? u * (qq * part) * Z < (only_p ? pp : fmax(ka * pp - kb * qq, 0.0)) : u * Z < pp) {
+                    taken = i;
+                    continue;
+                }
+                by_ab = summed = false;
+                if (!use_q) Z -= pp;
             }
-            if (left < right) { taken = i; continue; }
             if (use_q) {
-                sharpen();
-                kb = kb / Z + part;
+                kb = kb / Z + (a.distinct ? 1.0 / fmax(rest, 1e-300) : 1.0);
                 ka = ka / Z;
                 rest -= qx / q_sum;
-            } else {
-                Z -= px / p_sum;
+                k = kb / ka * (p_sum / q_sum);
             }
             __syncthreads();
             if (tid == 0) tried_s[tried] = x;
@@ -430,9 +530,8 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
             __syncthreads();
             only_p = false;
             if (use_q) {
-                over_q = p_sum / q_sum;
-                Z = sum_weights() / p_sum;
-                summed = true;
+                if (!summed) sum_weights();
+                Z = ka * (by_ab ? fmax(fma(-k, told.b, told.a), 0.0) : told.p) / p_sum;
                 nothing = !(Z > 0);
             }
         }
@@ -442,60 +541,75 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
             if (rank == 0 && tid == 0) a.path[first + stood] = taken;
             continue;
         }
-        if (greedy) {
-            next = arg;
-            break;
-        }
         // ---- the draw: the first token at which the running sum of w passes u times the whole
         if (nothing) { only_p = true; summed = false; }
-        double all = summed ? told[0] : sum_weights();
-        if (!(all > 0)) { only_p = true; all = sum_weights(); }              // (all of p refused)
+        if (!summed) sum_weights();
+        auto whole = [&] {
+            double s = 0;
+            for (int n = 0; n < ranks; ++n) s += part_sum(sums[turn ^ 1][n]);
+            return s;
+        };
+        double all = whole();
+        if (!(all > 0)) {                        // (all of p refused)
+            only_p = true;
+            sum_weights();
+            all = whole();
+        }
         // which CTA, then which warp's part; where roundings leave none behind the target, the last one with any weight
         double target = (double)a.uniform[first] * all, before = 0;
         int owner = -1, last = 0;
-        for (int k = 0; k < ranks && owner < 0; ++k) {
-            const double s = read_cluster(&records[turn ^ 1].p_sum, k);
-            if (s > 0) last = k;
-            if (s > 0 && before + s > target) owner = k; else before += s;
+        for (int n = 0; n < ranks && owner < 0; ++n) {
+            const double s = part_sum(sums[turn ^ 1][n]);
+            if (s > 0) last = n;
+            if (s > 0 && before + s > target) owner = n; else before += s;
         }
         bool end = owner < 0;                    // the last one with any weight is meant
         if (end) owner = last;
         if (owner == rank) {
-            auto pick = [&](const double* sums) {        // of the warps' parts; target: from there on
+            auto pick = [&](const double* of_warps) {    // of the warps' parts; target: from there on
                 int part = -1;
                 before = 0;
                 last = 0;
                 for (int w = 0; w < V_WARPS && part < 0; ++w) {
-                    if (sums[w] > 0) last = w;
-                    if (!end && sums[w] > 0 && before + sums[w] > target) part = w; else before += sums[w];
+                    const double s = of_warps[w];
+                    if (s > 0) last = w;
+                    if (!end && s > 0 && before + s > target) part = w; else before += s;
                 }
                 if (part < 0) { part = last; end = true; }
                 target -= before;
                 return part;
             };
+            if (tid < V_WARPS) sums_s[tid] = part_sum(parts_s[tid]);
+            __syncthreads();
             target -= before;
             const int part = pick(sums_s);
-            // that part once more, an eighth a warp
+            // that part once more, each warp a part of it
             const bool two = !only_p && use_q;
             const int p_low = min(low + part * each, high), p_high = min(p_low + each, high), fine = (p_high - p_low + V_WARPS - 1) / V_WARPS;
             const int f_low = min(p_low + warp * fine, p_high), f_high = min(f_low + fine, p_high);
-            auto at = [&](int v) { const bool is = v < f_high; return weight(is ? number(lrow[v]) : -INFINITY, is && two ? number(qrow[v]) : -INFINITY, v, is); };
-            double s = 0;
-            for (int v0 = f_low; v0 < f_high; v0 += 32) s += at(v0 + lane);
-            s = warp_sum(s);
+            auto at = [&](int v) -> double {
+                const double pw = exp_p(v < f_high ? number(lrow[v]) : -INFINITY);
+                if (two) {
+                    const double qw = exp_q(v < f_high ? number(qrow[v]) : -INFINITY);
+                    return fmax(fma(-k, qw, pw), 0.0);
+                }
+                bool gone = false;
+                for (int n = 0; n < tried && !only_p; ++n) gone |= tried_s[n] == v;
+                return gone ? 0.0 : pw;
+            };
+            const double s = warp_sum(two ? sum_rest(lrow, qrow, f_low, f_high, exp_p, exp_q, k, lane) : sum_one(lrow, f_low, f_high, exp_p, tried_s, only_p ? 0 : tried, lane));
+            if (lane == 0) fine_s[warp] = s;
             __syncthreads();
-            if (lane == 0) sums2_s[warp] = s;
-            __syncthreads();
-            if (warp == pick(sums2_s)) {
+            if (warp == pick(fine_s)) {
                 before = 0;
                 int found = -1, some = -1;
                 for (int v0 = f_low; v0 < f_high && found < 0; v0 += 32) {
                     const double x = at(v0 + lane);
                     double sum = x;
 #pragma unroll
-                    for (int k = 1; k < 32; k *= 2) {
-                        const double y = __shfl_up_sync(0xffffffffu, sum, k);
-                        if (lane >= k) sum += y;
+                    for (int n = 1; n < 32; n *= 2) {
+                        const double y = __shfl_up_sync(0xffffffffu, sum, n);
+                        if (lane >= n) sum += y;
                     }
                     const uint32_t past = __ballot_sync(0xffffffffu, !end && x > 0 && before + sum > target), any = __ballot_sync(0xffffffffu, x > 0);
                     if (past) found = v0 + __ffs(past) - 1;
@@ -508,14 +622,12 @@ __global__ void __launch_bounds__(V_THREADS) verify_kernel(const VerifyArgs a, D
             if (tid == 0) a.next[b] = drawn_s;
         }
         if (rank == 0 && tid == 0) a.accepted[b] = stood;
-        cluster_sync();                          // (nobody leaves while its shared memory is read)
         return;
     }
     if (rank == 0 && tid == 0) {
         a.accepted[b] = stood;
         a.next[b] = next;
     }
-    cluster_sync();
 }
 
 // ---------------------------------------------------------------- what the cache keeps
@@ -661,9 +773,11 @@ cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t stre
 
 template <class T>
 int launch_verify(VerifyArgs a, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
-    // as many CTAs a sequence as the GPU holds at a time, two an SM, of 2048 numbers at least
+    // As many CTAs a sequence as make two rounds of those that the GPU holds (sequences end at different levels), of 2048 numbers at least; with no more than one an SM, of 16 warps, else of 8.
+    // (us a call, with one / two / four rounds: 64 chains of 6, 128,000 numbers 182, 174, 196; with 8 and 16 warps: the same 139, 175, 16 trees of 33, 50,001 numbers 74, 59.)
     int ranks = 1;
-    while (ranks < MOST_CLUSTER && 2LL * ranks * a.sequences <= 2 * 148 && a.vocab > 2048 * ranks) ranks *= 2;
+    while (ranks < MOST_CLUSTER && 2LL * ranks * a.sequences <= 2 * V_CTAS * 148 && a.vocab > 2048 * ranks) ranks *= 2;
+    const bool few = (long long)ranks * a.sequences <= 148;
     a.slice = ((a.vocab + ranks - 1) / ranks + 7) / 8 * 8;
     cudaLaunchAttribute attr[2];
     for (int b0 = 0; b0 < a.sequences; b0 += 65535) {
@@ -673,8 +787,9 @@ int launch_verify(VerifyArgs a, DeviceCounters* dc, DeviceCounters* dc_next, cud
         x.accepted += b0;
         x.next += b0;
         if (x.temperatures) x.temperatures += b0;
-        const cudaLaunchConfig_t cfg = config(dim3(ranks, x.sequences), V_THREADS, 0, stream, attr, ranks);
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, verify_kernel<T>, x, dc, b0 == 0 ? dc_next : nullptr);
+        const cudaLaunchConfig_t cfg = config(dim3(ranks, x.sequences), few ? 512 : 256, 0, stream, attr, ranks);
+        DeviceCounters* const next = b0 == 0 ? dc_next : nullptr;
+        const cudaError_t e = few ? cudaLaunchKernelEx(&cfg, verify_kernel<T, 16>, x, dc, next) : cudaLaunchKernelEx(&cfg, verify_kernel<T, 8>, x, dc, next);
         if (e != cudaSuccess) { set_cuda_error(e, "verify_kernel launch"); return PSA_ERR_CUDA; }
     }
     return PSA_OK;
