@@ -382,10 +382,11 @@ int psa_cache_append_rotary(const psa_cache* cache, const psa_rotary* rotary, co
 
 /*
  * psa_cache_attention for trees: the sequence's last nq tokens are the tree's, in the order of its queries, and query i sees of these its own token and its ancestors', and all tokens ahead of
- * them.  (With a chain for parents it is psa_cache_attention.)  max_q up to PSA_TREE_MOST.  Workspace psa_cache_workspace_bytes; everything else as there.
+ * them.  (With a chain for parents it is psa_cache_attention.)  max_q up to PSA_TREE_MOST.  Workspace psa_tree_workspace_bytes; everything else as there.
  */
 int psa_tree_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
                        int max_q, float scale, int dtype, void* out, float* lse, void* stream);
+size_t psa_tree_workspace_bytes(int d_k);
 
 /*
  * Which drafted tokens stand.  A sequence's first row is its last known token, the root; row r's logits say what follows its token.  From the root on, the children of a row are tried in their

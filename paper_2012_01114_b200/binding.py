@@ -26,7 +26,7 @@ EXPORTS = ("psa_attention", "psa_attention_f32", "psa_attention_core", "psa_atte
            "psa_last_cuda_error", "psa_profile_begin", "psa_profile_end", "psa_attention_sym_f32_noalloc",
            "psa_attention_block", "psa_block_workspace_bytes", "psa_last_rescales", "psa_selftest_wait_expiry", "psa_measure_pipe_rates", "psa_attention_core_host", "psa_attention_block_residual",
            "psa_prompt_attention", "psa_prompt_workspace_bytes", "psa_cache_page_bytes", "psa_cache_append", "psa_cache_attention", "psa_cache_workspace_bytes", "psa_pages_free",
-           "psa_cache_append_rotary", "psa_tree_attention", "psa_verify_drafts", "psa_cache_keep", "psa_pages_fork", "psa_pages_reserve", "psa_pages_compact", "psa_pages_copy", "psa_pages_workspace_bytes")
+           "psa_cache_append_rotary", "psa_tree_attention", "psa_tree_workspace_bytes", "psa_verify_drafts", "psa_cache_keep", "psa_pages_fork", "psa_pages_reserve", "psa_pages_compact", "psa_pages_copy", "psa_pages_workspace_bytes")
 
 
 class PsaError(RuntimeError):
@@ -126,10 +126,10 @@ def lib() -> ctypes.CDLL:
         L.psa_pages_compact.argtypes = [pages, vp, ll, ci, vp, vp, vp, vp, vp]
         L.psa_pages_copy.argtypes = [vp, ci, vp, ci, ll, ci, vp, vp, ci, vp]
         L.psa_cache_page_bytes.argtypes = [ci, ci, ci]
-        L.psa_cache_workspace_bytes.argtypes = [ci]
+        L.psa_cache_workspace_bytes.argtypes = L.psa_tree_workspace_bytes.argtypes = [ci]
         L.psa_prompt_workspace_bytes.argtypes = [ci] * 6
         L.psa_pages_workspace_bytes.argtypes = [ci, ci]
-        for f in ("psa_prompt_workspace_bytes", "psa_cache_page_bytes", "psa_cache_workspace_bytes", "psa_pages_workspace_bytes"):
+        for f in ("psa_prompt_workspace_bytes", "psa_cache_page_bytes", "psa_cache_workspace_bytes", "psa_tree_workspace_bytes", "psa_pages_workspace_bytes"):
             getattr(L, f).restype = cs
         for f in ("psa_prompt_attention", "psa_cache_append", "psa_cache_attention", "psa_pages_free", "psa_pages_fork", "psa_pages_reserve",
                   "psa_pages_compact", "psa_pages_copy", "psa_cache_append_rotary", "psa_tree_attention", "psa_verify_drafts", "psa_cache_keep"):
@@ -423,6 +423,10 @@ def psa_cache_page_bytes(kv_heads, page_size, d_k) -> int:
 
 def psa_cache_workspace_bytes(d_k) -> int:
     return int(lib().psa_cache_workspace_bytes(d_k))
+
+
+def psa_tree_workspace_bytes(d_k) -> int:
+    return int(lib().psa_tree_workspace_bytes(d_k))
 
 
 def psa_pages_workspace_bytes(pages, count) -> int:

@@ -2,6 +2,7 @@
 // scheduler (psa_skip_count) and dispatch to the fp32 and bf16 kernel families.
 #include <math.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -962,6 +963,14 @@ int psa_cache_append_rotary(const psa_cache* cache, const psa_rotary* rotary, co
 
 size_t psa_cache_workspace_bytes(int d_k) { return cache_head(d_k) ? COUNTER_BYTES + cache_attention_scratch_bytes(d_k) : 0; }
 
+// Whether a tree's rows go to the tensor core's tiles of 128 rows (psa_tree.cu) or, sixteen at a time, to psa_cache_attn.cu.
+static bool tree_on_tiles(int max_q, int group, int d) {
+    static const int C = getenv("TC") ? atoi(getenv("TC")) : 16;
+    return d <= 128 && (long long)max_q * group > C;
+}
+
+size_t psa_tree_workspace_bytes(int d_k) { return cache_head(d_k) ? COUNTER_BYTES + std::max(cache_attention_scratch_bytes(d_k), tree_attention_scratch_bytes(d_k)) : 0; }
+
 static int attend_to_cache(const psa_cache* cache, const void* Q, long long q_stride, bool tree, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
                            int max_q, float scale, int dtype, void* out, float* lse, void* stream) {
     g_err_text[0] = 0;
@@ -973,7 +982,9 @@ static int attend_to_cache(const psa_cache* cache, const void* Q, long long q_st
     if (!Q || !seqs || !q_starts || !out || (tree && !parents)) return PSA_ERR_NULL;
     if (!good_stride(q_stride, (long long)heads * cache->d_k) || (long long)rows * (heads / cache->kv_heads) > 0x7fffff00LL) return PSA_ERR_SHAPE;
     if (!aligned16(Q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) || !aligned4(q_starts) || !aligned4(parents)) return PSA_ERR_ALIGN;
-    return run_op(cache_attention_scratch_bytes(cache->d_k), stream, [&](const OpCall& c) {
+    const bool many = tree && tree_on_tiles(max_q, heads / cache->kv_heads, cache->d_k);
+    return run_op(many ? tree_attention_scratch_bytes(cache->d_k) : cache_attention_scratch_bytes(cache->d_k), stream, [&](const OpCall& c) {
+        if (many) return tree_attention(*cache, Q, q_stride, parents, seqs, q_starts, sequences, rows, heads, scale, dtype, out, lse, c.ws + COUNTER_BYTES, c.dc, c.dc_next, static_cast<cudaStream_t>(stream));
         return cache_attention(*cache, Q, q_stride, parents, seqs, q_starts, sequences, rows, heads, max_q, scale, dtype, out, lse, c.ws + COUNTER_BYTES, c.dc, c.dc_next,
                                static_cast<cudaStream_t>(stream));
     });

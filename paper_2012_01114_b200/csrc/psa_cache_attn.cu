@@ -238,7 +238,7 @@ cache_attn_kernel(const AttnArgs a, DeviceCounters* dc, DeviceCounters* dc_next)
     bool descends = false;
     for (int b = tid; b < a.sequences; b += THREADS) {
         const Seq x = sequence<COLS, TREE>(a, b);
-        if (TREE && x.nq == 0 && a.q_starts[b + 1] > a.q_starts[b] && blockIdx.x == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);       // (a tree that is too large, or rows that are not there)
+        if (TREE && x.nq != a.q_starts[b + 1] - a.q_starts[b] && blockIdx.x == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);       // (a tree that is too large, or rows that are not there)
         descends |= a.q_starts[b + 1] < a.q_starts[b];
         if (b == tid) s0 = x;
         if (MANY) seq_s[b] = make_uint2((uint32_t)x.steps, (uint32_t)x.qtiles);

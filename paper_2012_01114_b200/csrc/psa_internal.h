@@ -90,7 +90,7 @@ int bf16_attention_persist(const void* Q, const void* K, const void* V, void* ou
                            float scale, int scheme, DeviceCounters* dc, unsigned int* cursor, DeviceCounters* dc_next,
                            cudaStream_t stream);
 
-// ---- serving (psa_prompt.cu, psa_cache_append.cu, psa_cache_attn.cu, psa_drafts.cu, psa_pages.cu) ----
+// ---- serving (psa_prompt.cu, psa_cache_append.cu, psa_cache_attn.cu, psa_tree.cu, psa_drafts.cu, psa_pages.cu) ----
 // Arguments are checked by the caller; each returns a psa_status.  dc: the call's counter block, dc_next (may be null): cleared by the call's first kernel.
 int prompt_attention(const void* Q, const void* K, const void* V, long long q_stride, long long k_stride, long long v_stride, const int* q_starts, const int* k_starts,
                      int sequences, int q_rows, int k_rows, int heads, int kv_heads, int d, float scale, int dtype, void* out, float* lse, void* scratch, int call, DeviceCounters* dc,
@@ -105,6 +105,10 @@ size_t cache_attention_scratch_bytes(int d);
 // parents null: a sequence's queries are a chain.
 int cache_attention(const psa_cache& c, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads, int max_q,
                     float scale, int dtype, void* out, float* lse, void* scratch, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
+// psa_tree.cu: the same for trees with many rows a key/value head, d up to 128.
+size_t tree_attention_scratch_bytes(int d);
+int tree_attention(const psa_cache& c, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads, float scale, int dtype,
+                   void* out, float* lse, void* scratch, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream);
 int verify_drafts(const void* logits, long long logit_stride, const void* drafts, long long draft_stride, int vocab, int dtype, const int* tokens, const int* parents, const int* starts,
                   int sequences, int rows, const float* temperatures, const float* uniform, int distinct, int* path, int* accepted, int* next, DeviceCounters* dc,
                   DeviceCounters* dc_next, cudaStream_t stream);

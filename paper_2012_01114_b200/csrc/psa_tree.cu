@@ -1,0 +1,703 @@
+// Attention of trees of drafted tokens over the cache held in 4 bits (layout: psa_cache.cuh), where a key/value head has more than a few query rows (a row: a token of the tree and a query
+// head of the group; psa_cache_attn.cu takes the others).
+//
+//     S_ij = scale q_i k_j,  w_ij = exp(S_ij),  out_i = sum_j w_ij v_j / sum_j w_ij,   j ahead of the tree, or i itself, or an ancestor of i
+//
+// 128 rows are a tile of the tensor core, so that a code is made a number once for all of them: at d = 128 a tile of 128 tokens is 20 KB of cache, 890 cycles at an SM's share of the memory's rate,
+// and 1600 cycles of MMAs.  Eight warps turn codes into operands, eight are the softmax's, one thread issues MMAs:
+//   K    k = M + S (1 + c / 16) goes in without a rounding.  S is split into its upper seven bits and the rest, S = S' + S'', so that S' c / 16 and S'' c / 16 are numbers of fp16 (one fma of 1 + c / 16 each):
+//        two operands, and the rest of the sum, sum_w (M_w + S_w) (sum of q over group w), in one more step of 16 columns, with the queries' sums in two parts each.  (k rounded to fp16 instead is a third
+//        fewer cycles, and 2.5e-4 off in every score: 5e-5 in the log-sum-exp of a short sequence, and twice the error of fp16 outputs.)
+//   V    rounded to fp16, as in psa_cache_attn.cu
+//   P    in tensor memory, fp16, held 2^7 times as large (HEADROOM in psa_prompt.cu)
+// There is room for one tile of each operand, and that is enough: while S of tile j + 1 runs V of tile j is written, and K of tile j + 2 while P V of tile j does; scores have two places, and the
+// softmax of tile j runs under the scores of tile j + 1.  Every warp that turns codes has a block of 16 tokens of each tile, and a ring of its own filled by bulk copies.
+//
+// Work is the list of all tiles of all rows' tiles, cut into as many equal pieces as there are CTAs, whatever the lengths: a CTA ends one row tile, has some whole, and begins another.  Parts of a row tile
+// are stored in fp32 and joined in their order by a second small kernel, since no CTA waits for another; rows with one part are finished where they are.
+#include <type_traits>
+
+#include "psa_cache.cuh"
+#include "psa_internal.h"
+#include "psa_sched.h"
+#include "psa_softmax.cuh"
+#include "sm100.cuh"
+
+namespace psa {
+
+namespace {
+
+constexpr int ROWS = 128, KEYS = 128;
+constexpr int MMA_WARP = 0, SOFT0 = 4, SOFTS = 8, TURN0 = SOFT0 + SOFTS, TURNS = 8, T_WARPS = TURN0 + TURNS, T_THREADS = 32 * T_WARPS;
+constexpr int T_SEQS = 512;                     // sequences of one launch
+constexpr int T_CTAS = 160;                     // at most
+constexpr int LEAST = 4;                        // tiles of a piece
+constexpr int TREE_WORDS = PSA_TREE_MOST / 32 + 1;
+constexpr float UP = 7.f;                       // log2 of what weights are held larger by
+constexpr float T_LN2 = 0.6931471805599453f;
+
+template <int D>
+struct TCfg {
+    static constexpr int DT = D <= 64 ? 64 : 128, SUB = DT / 64, KS = D / 16, G = D / 32;
+    static constexpr int TILE = 128 * DT * 2;   // bytes of an operand tile: sub-tiles of 64 columns, 128-byte rows swizzled
+    static constexpr int HALF = 10 * D;         // bytes of K, and of V, in a block
+    static constexpr int K_RING = 2, V_RING = 3;
+    static constexpr int Q = 0, K1 = TILE, K2 = 2 * TILE, V = 3 * TILE, E = 4 * TILE, RAW_K = E + 16384, RAW_V = RAW_K + K_RING * TURNS * HALF, TREE = RAW_V + V_RING * TURNS * HALF;
+    static constexpr int SMEM = TREE + ROWS * TREE_WORDS * 4 + 1024;
+};
+constexpr int TM_S = 0, TM_P = 256, TM_O = 384;  // columns of tensor memory: S twice, P, O
+
+struct TreeArgs {
+    const uint8_t* pool;
+    const int *tables, *lens, *seqs, *q_starts, *parents;
+    const uint16_t* q;
+    uint16_t* out;
+    float *lse, *part;
+    struct TreeRow* rows_cut;
+    long long q_stride;
+    int pages, slots, width, page_size, kv_heads, group, sequences, rows, f16, d;
+    float scale;
+    FastDiv by_group, by_blocks;
+};
+// A row tile that is cut: by the CTA that has its first part.  parts 0: none.
+struct TreeRow {
+    int parts, q0, nq, h, qt;
+};
+// Part `p` of the row tile that CTA c begins: [ROWS][d] sums, then as many maxima (log2) and sums of weights.
+__device__ __forceinline__ float* part_at(float* part, int c, int p, int d) { return part + (size_t)(p == 0 ? 2 * c + 1 : 2 * (c + p)) * ROWS * (d + 2); }
+
+struct TBars {
+    uint64_t raw_k[TURNS][2], raw_v[TURNS][3];
+    uint64_t k_full, k_empty, v_full, o_done, s_full[2], s_free[2], p_ready;
+};
+
+__device__ __forceinline__ uint32_t t_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+__device__ __forceinline__ __half2 t_h2(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
+__device__ __forceinline__ uint32_t t_weights(float lo, float hi) {
+    uint32_t v;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
+    return v;
+}
+__host__ __device__ constexpr uint32_t t_idesc(uint32_t n, uint32_t b_major) { return umma_idesc_bf16(128, n, UMMA_K_MAJOR, b_major) & ~((1u << 7) | (1u << 10)); }      // fp16 operands
+
+template <int D>
+__global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, DeviceCounters* dc, DeviceCounters* dc_next) {
+    using Cfg = TCfg<D>;
+    using B = CacheBlock<D>;
+    constexpr int G = Cfg::G;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint32_t* const tree = reinterpret_cast<uint32_t*>(smem + Cfg::TREE);       // [ROWS][TREE_WORDS]: by token of the row tile, the tree's tokens that it sees
+    __shared__ TBars bars;
+    __shared__ uint32_t tmem_s;
+    __shared__ int abort_flag, bad_s;
+    __shared__ long long base_s[T_SEQS + 1], scan_s[T_WARPS];
+    __shared__ int len_s[T_SEQS], q0_s[T_SEQS], nq_s[T_SEQS], slot_s[T_SEQS];
+    __shared__ float factor_s[ROWS];            // of a row's scores, to log2 units
+    __shared__ __align__(8) uint8_t have_s[4][TURNS];        // blocks of a tile that are there, by tile modulo 4
+    __shared__ uint32_t nan_s[G][PSA_TREE_MOST / 32];            // tokens of the tree whose group of V reads back as NaN or infinite
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        abort_flag = 0;
+        for (int w = 0; w < TURNS; ++w) {
+            for (int s = 0; s < 2; ++s) mbar_init(&bars.raw_k[w][s], 1);
+            for (int s = 0; s < 3; ++s) mbar_init(&bars.raw_v[w][s], 1);
+        }
+        mbar_init(&bars.k_full, TURNS);
+        mbar_init(&bars.v_full, TURNS);
+        mbar_init(&bars.k_empty, 1);
+        mbar_init(&bars.o_done, 1);
+        mbar_init(&bars.p_ready, SOFTS);
+        for (int s = 0; s < 2; ++s) { mbar_init(&bars.s_full[s], 1); mbar_init(&bars.s_free[s], SOFTS); }
+        fence_mbar_init();
+    }
+    if (warp == 1) { tmem_alloc(&tmem_s, 512); tmem_relinquish(); }
+    for (int i = tid; i < 16384 / 16; i += T_THREADS) reinterpret_cast<uint4*>(smem + Cfg::E)[i] = make_uint4(0, 0, 0, 0);       // (columns that no group has stay zero)
+    volatile int* const abortp = &abort_flag;
+    grid_dependency_wait();
+    if (tid == 0 && blockIdx.x == 0 && dc_next) *dc_next = DeviceCounters{0, 0, 0, 0, 0, 0, 0};
+    if (tid == 0) a.rows_cut[blockIdx.x].parts = 0;
+    // ---- the list: tiles ahead of every sequence
+    bool descends = false, strange = false;
+    long long ahead = 0;
+    for (int b0 = 0; b0 < a.sequences; b0 += T_THREADS) {
+        const int b = b0 + tid;
+        long long n = 0;
+        if (b < a.sequences) {
+            const int slot = a.seqs[b], s0 = a.q_starts[b], s1 = a.q_starts[b + 1];
+            const bool there = slot >= 0 && slot < a.slots;
+            descends |= s1 < s0;
+            const int q0 = min(max(s0, 0), a.rows), all = max(min(max(s1, 0), a.rows) - q0, 0), nq = all > PSA_TREE_MOST ? 0 : all;
+            const int held = there ? max(a.lens[slot], 0) : 0, len = (int)min((long long)held, (long long)a.width * a.page_size);
+            strange |= (nq > 0 && (!there || held != len)) || nq != s1 - s0;
+            const int tiles = max((int)(((uint32_t)len + KEYS - 1) / KEYS), 1), row_tiles = (nq * a.group + ROWS - 1) / ROWS;
+            n = (long long)row_tiles * a.kv_heads * tiles;
+            len_s[b] = len;
+            q0_s[b] = q0;
+            nq_s[b] = nq;
+            slot_s[b] = there ? slot : 0;
+        }
+        long long x = n;
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, s);
+            if (lane >= s) x += y;
+        }
+        __syncthreads();
+        if (lane == 31) scan_s[warp] = x;
+        __syncthreads();
+        long long before = ahead;
+        for (int w = 0; w < T_WARPS; ++w) { if (w < warp) before += scan_s[w]; ahead += scan_s[w]; }
+        if (b < a.sequences) base_s[b] = before + x - n;
+    }
+    if (tid == 0) base_s[a.sequences] = ahead;
+    if (strange && blockIdx.x == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
+    const bool refused = __syncthreads_or(descends) != 0;        // rows named more than once: nothing is computed, and the call reports it
+    if (refused && tid == 0 && blockIdx.x == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
+    const long long per = max((ahead + gridDim.x - 1) / (long long)gridDim.x, (long long)LEAST);
+    const long long mine0 = min(per * (long long)blockIdx.x, ahead), mine1 = refused ? mine0 : min(mine0 + per, ahead);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_s;
+
+    uint32_t done = 0;                          // tiles that the CTA has worked off: the phases of all barriers but the rings' follow from it
+    uint32_t ring_k = 0, ring_v = 0;            // a turning warp's blocks so far
+    bool ok = true;
+    for (long long at = mine0; at < mine1;) {
+        // ---- the item: tiles t0 .. t1 - 1 of row tile qt of head h of sequence b
+        int lo = 0, hi = a.sequences - 1;       // the last sequence that begins at or before it (and has tiles: those without begin where the next one does)
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (base_s[mid] <= at) lo = mid; else hi = mid - 1;
+        }
+        const int b = lo, len = len_s[b], nq = nq_s[b], q0 = q0_s[b], slot = slot_s[b], tiles = max((int)(((uint32_t)len + KEYS - 1) / KEYS), 1);
+        const long long inside = at - base_s[b];
+        const int row = (int)(inside / tiles), t0 = (int)(inside - (long long)row * tiles), t1 = (int)min((long long)tiles, t0 + (mine1 - at)), nt = len > 0 ? t1 - t0 : 0;
+        const int row_tiles = (nq * a.group + ROWS - 1) / ROWS, h = row / row_tiles, qt = row - h * row_tiles;
+        const int ctx = len - nq;                // the tree's first token
+        const long long row0 = at - t0;          // of the row tile, in the list
+        const int first_cta = (int)(row0 / per), parts = (int)((row0 + tiles - 1) / per) - first_cta + 1, part = (int)blockIdx.x - first_cta;
+        at += t1 - t0;
+        const int tok0 = (int)fastdiv((uint32_t)(qt * ROWS), a.by_group);       // first token of the row tile
+        const bool meets_tree = t1 * KEYS > ctx;
+        __syncthreads();                         // (the item before it is done with)
+        if (warp >= SOFT0) {
+            // ---- the queries: four lanes a row, a group of 32 channels each
+            const int r = (tid - 32 * SOFT0) >> 2, w = lane & 3, rho = qt * ROWS + r, token = (int)fastdiv((uint32_t)rho, a.by_group);
+            uint4 raw[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
+            if (w < G && token < nq) {
+                const uint4* from = reinterpret_cast<const uint4*>(a.q + (size_t)(q0 + token) * a.q_stride + ((size_t)h * a.group + (rho - token * a.group)) * D + 32 * w);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw[i] = from[i];
+            }
+            float top = 0.f;
+            auto number = [&](int i, int k) {    // pair k of word i
+                const uint32_t x = (&raw[i].x)[k];
+                return a.f16 ? __half22float2(t_h2(x)) : make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+            };
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 f = number(i, k);
+                    top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+                }
+            top = quad_max(top);
+            // 2^e <= top < 2^(e + 1): the row goes in as q 2^(8 - e), exact but for what lies 2^32 below its largest number; sums of 32 stay below 2^14
+            const uint32_t e = min(max(__float_as_uint(top) >> 23, 1u), 253u);
+            const float down = __uint_as_float((254u - e) << 23), up = __uint_as_float(e << 23);
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 f = number(i, k);
+                    const __half2 v = __floats2half2_rn(f.x * down * 256.f, f.y * down * 256.f);
+                    y[k] = t_bits(v);
+                    sum += __low2float(v) + __high2float(v);
+                }
+                const int chunk = 4 * w + i;
+                if (w < G) *reinterpret_cast<uint4*>(smem + Cfg::Q + (chunk >> 3) * 16384 + swz128_offset(r, chunk & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+            if (w < G) {                         // columns 16 + 4 w ..: the sum in two parts, twice
+                const __half hi16 = __float2half_rn(sum), lo16 = __float2half_rn(sum - __half2float(hi16));
+                const uint32_t both = t_bits(__halves2half2(hi16, lo16));
+                *reinterpret_cast<uint2*>(smem + Cfg::E + swz128_offset(r, 2 + (w >> 1)) + 8 * (w & 1)) = make_uint2(both, both);
+            }
+            if (w == 0) factor_s[r] = fmaxf(up * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
+        } else {
+            // ---- the tokens' sets of the tree: each its own and its ancestors
+            const int words = (nq + 31) / 32, tok = tok0 + tid;
+            for (int i = tid; i < G * (PSA_TREE_MOST / 32); i += 32 * SOFT0) (&nan_s[0][0])[i] = 0u;
+            if (meets_tree && tok < nq && tok <= (int)fastdiv((uint32_t)(qt * ROWS + ROWS - 1), a.by_group)) {
+                uint32_t* const mine = tree + tid * TREE_WORDS;
+                for (int i = 0; i < words; ++i) mine[i] = 0u;
+                int k = tok;
+                while (k >= 0) {
+                    mine[k >> 5] |= 1u << (k & 31);
+                    const int up = __ldg(a.parents + q0 + k);
+                    if (up < -1 || up >= k) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);         // (no earlier token: taken for the root of a tree of its own)
+                    k = up < k ? up : -1;
+                }
+            }
+        }
+        fence_async_smem();
+        if (__syncthreads_or(abort_flag)) { ok = false; break; }
+
+        if (warp == MMA_WARP) {
+            if (lane == 0 && nt > 0) {
+                constexpr uint32_t idescS = t_idesc(KEYS, UMMA_K_MAJOR), idescO = t_idesc(D, UMMA_MN_MAJOR);
+                const uint32_t q_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::Q)), k1_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K1)), k2_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K2));
+                const uint32_t e_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::E)), v_lo = umma_desc_lo_mnmajor(smem_u32(smem + Cfg::V), 16384);
+                for (int j = 0; j <= nt && ok; ++j) {
+                    const uint32_t n = done + j;
+                    if (j < nt) {
+                        ok = mbar_wait(&bars.k_full, n & 1, abortp);
+                        if (ok && n >= 2) ok = mbar_wait(&bars.s_free[n & 1], ((n >> 1) - 1) & 1, abortp);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t dS = tmem + TM_S + (n & 1) * KEYS;
+                        umma_ss(dS, umma_desc_join(e_lo + (32 >> 4), UMMA_DESC_HI_SW128), umma_desc_join(e_lo, UMMA_DESC_HI_SW128), idescS, 0);
+#pragma unroll
+                        for (int kk = 0; kk < Cfg::KS; ++kk) {
+                            const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+                            umma_ss(dS, umma_desc_join(q_lo + off, UMMA_DESC_HI_SW128), umma_desc_join(k1_lo + off, UMMA_DESC_HI_SW128), idescS, 1);
+                        }
+#pragma unroll
+                        for (int kk = 0; kk < Cfg::KS; ++kk) {
+                            const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+                            umma_ss(dS, umma_desc_join(q_lo + off, UMMA_DESC_HI_SW128), umma_desc_join(k2_lo + off, UMMA_DESC_HI_SW128), idescS, 1);
+                        }
+                        umma_commit(&bars.s_full[n & 1]);
+                        umma_commit(&bars.k_empty);
+                    }
+                    if (j > 0) {
+                        ok = mbar_wait(&bars.v_full, (n - 1) & 1, abortp) && mbar_wait(&bars.p_ready, (n - 1) & 1, abortp);
+                        if (!ok) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int kk = 0; kk < KEYS / 16; ++kk)
+                            umma_ts(tmem + TM_O, tmem + TM_P + kk * 8, umma_desc_join(v_lo + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, j > 1 || kk > 0);
+                        umma_commit(&bars.o_done);
+                    }
+                }
+            }
+        } else if (warp >= TURN0) {
+            // ------------------------------------------------------------ codes into operands: block `me` of every tile
+            const int me = warp - TURN0;
+            uint8_t* const raw_k = smem + Cfg::RAW_K + me * Cfg::HALF;
+            uint8_t* const raw_v = smem + Cfg::RAW_V + me * Cfg::HALF;
+            // lane l: the block's address in tile l of the last 32 (looked up 16 at a time, so that what is still to be asked for of V stays), null where it is not there
+            const uint8_t* addr = nullptr;
+            uint32_t there = 0, asked_k = ring_k, asked_v = ring_v;         // blocks asked for so far
+            auto look_up = [&](int i0) {
+                if ((lane >> 4) == (i0 >> 4 & 1)) {
+                    const int i = i0 + (lane & 15), block = (t0 + i) * TURNS + me;
+                    addr = nullptr;
+                    if (i < nt && (long long)block * CACHE_BLOCK < len) {
+                        const int blocks = (int)a.by_blocks.d, col = (int)fastdiv((uint32_t)block, a.by_blocks);
+                        const int page = a.tables[(size_t)slot * a.width + col];
+                        if (page >= 0 && page < a.pages) addr = a.pool + (((size_t)page * a.kv_heads + h) * blocks + (block - col * blocks)) * B::BYTES;
+                        else atomicExch(&dc->status, (int)PSA_ERR_SHAPE);                       // (no such page: its tokens are left out, and the call reports it)
+                    }
+                }
+                there = __ballot_sync(0xffffffffu, addr != nullptr);
+            };
+            // K of tile i is asked for ahead of V of tile i
+            auto load = [&](int i, bool is_k) {
+                if (i >= nt) return;
+                if (is_k && (i & 15) == 0) look_up(i);
+                const uint32_t count = is_k ? asked_k++ : asked_v++;
+                uint64_t* const bar = is_k ? &bars.raw_k[me][count % Cfg::K_RING] : &bars.raw_v[me][count % Cfg::V_RING];
+                if (lane == (i & 31)) {
+                    if (addr) {
+                        mbar_arrive_expect_tx(bar, Cfg::HALF);
+                        if (is_k) bulk_load_1d(raw_k + (count % Cfg::K_RING) * (TURNS * Cfg::HALF), addr, Cfg::HALF, bar);
+                        else bulk_load_1d(raw_v + (count % Cfg::V_RING) * (TURNS * Cfg::HALF), addr + Cfg::HALF, Cfg::HALF, bar);
+                    } else {
+                        mbar_arrive(bar);
+                    }
+                }
+                __syncwarp();
+            };
+            auto is_there = [&](int i) { return (there >> (i & 31) & 1u) != 0; };
+            for (int i = 0; i < Cfg::V_RING; ++i) {
+                if (i < Cfg::K_RING) load(i, true);
+                load(i, false);
+            }
+            const CacheOnes ones;
+            auto turn_k = [&](int i) {
+                const uint32_t n = done + i, c = ring_k;
+                ok = __all_sync(0xffffffffu, mbar_wait(&bars.raw_k[me][c % Cfg::K_RING], (c / Cfg::K_RING) & 1, abortp));
+                ring_k += ok;
+                if (ok && n > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_empty, (n - 1) & 1, abortp));
+                if (!ok) return;
+                const bool have = is_there(i);
+                if (lane == 0) have_s[n & 3][me] = have;
+                if (have) {
+                    const uint8_t* const from = raw_k + (c % Cfg::K_RING) * (TURNS * Cfg::HALF);
+#pragma unroll
+                    for (int x = 0; x < 2 * G; ++x) {            // 16 tokens of 4 G words of eight channels, chunk by chunk of 16 bytes
+                        const int e = x * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), w = chunk >> 2, r = me * CACHE_BLOCK + tok;
+                        const uint32_t codes = *reinterpret_cast<const uint32_t*>(from + tok * (D / 2) + ((chunk & 3) * G + w) * 4);
+                        const uint32_t sm = *reinterpret_cast<const uint32_t*>(from + B::K_SCALES + (tok * G + w) * 4);
+                        const uint32_t S = __byte_perm(sm, sm, 0x1010), S1 = S & 0xfff0fff0u, S2 = t_bits(__hsub2(t_h2(S), t_h2(S1)));
+                        const __half2 s1 = t_h2(S1), s2 = t_h2(S2), m1 = __hneg2(s1), m2 = __hneg2(s2);
+                        uint32_t y1[4], y2[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const __half2 one = t_h2(ones(codes, k));
+                            y1[k] = t_bits(__hfma2(one, s1, m1));
+                            y2[k] = t_bits(__hfma2(one, s2, m2));
+                        }
+                        const uint32_t to = (chunk >> 3) * 16384 + swz128_offset(r, chunk & 7);
+                        *reinterpret_cast<uint4*>(smem + Cfg::K1 + to) = make_uint4(y1[0], y1[1], y1[2], y1[3]);
+                        *reinterpret_cast<uint4*>(smem + Cfg::K2 + to) = make_uint4(y2[0], y2[1], y2[2], y2[3]);
+                        if ((chunk & 3) == 0) *reinterpret_cast<uint2*>(smem + Cfg::E + swz128_offset(r, w >> 1) + 8 * (w & 1)) = make_uint2(__byte_perm(sm, sm, 0x3232), S);
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.k_full);
+                load(i + Cfg::K_RING, true);
+            };
+            auto turn_v = [&](int i) {
+                const uint32_t n = done + i, c = ring_v;
+                ok = __all_sync(0xffffffffu, mbar_wait(&bars.raw_v[me][c % Cfg::V_RING], (c / Cfg::V_RING) & 1, abortp));
+                ring_v += ok;
+                if (ok && n > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (n - 1) & 1, abortp));
+                if (!ok) return;
+                const bool have = is_there(i);
+                const int first = (t0 + i) * KEYS + me * CACHE_BLOCK;        // the block's first token
+                const uint8_t* const from = raw_v + (c % Cfg::V_RING) * (TURNS * Cfg::HALF);
+                const bool looks = first + CACHE_BLOCK > ctx;                // has tokens that not all rows see, or that are none of the sequence's
+#pragma unroll
+                for (int x = 0; x < G; ++x) {    // 8 pairs of tokens of 4 G chunks of eight channels
+                    const int e = x * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), w = chunk >> 2, g = 2 * (chunk & 3), r = me * CACHE_BLOCK + 2 * pair;
+                    uint4 even = make_uint4(0, 0, 0, 0), odd = even;
+                    if (have) {
+                        const uint32_t c0 = *reinterpret_cast<const uint32_t*>(from + pair * D + (g * G + w) * 4), c1 = *reinterpret_cast<const uint32_t*>(from + pair * D + ((g + 1) * G + w) * 4);
+                        uint2 sm = *reinterpret_cast<const uint2*>(from + (B::V_SCALES - B::V_CODES) + (pair * G + w) * 8);
+                        if (looks) {
+                            // Behind the sequence's end lies whatever the page held before, and a weight of zero does not keep a NaN out of the sum: such tokens, and groups of the tree's that
+                            // are not finite, go in as zeros; rows that see these get a NaN at the end.
+                            const int t = first + 2 * pair;
+                            const uint32_t keep = (t < len ? 0xffffu : 0u) | (t + 1 < len ? 0xffff0000u : 0u);
+                            sm.x &= keep;
+                            sm.y &= keep;
+                            uint32_t bad = (((sm.x & 0x7c007c00u) + 0x04000400u) | ((sm.y & 0x7c007c00u) + 0x04000400u)) & 0x80008000u;      // an exponent of all ones
+                            if (t < ctx) bad &= 0x80000000u;
+                            if (t + 1 < ctx) bad = 0;
+                            if (bad) {
+                                const uint32_t drop = (bad >> 15) * 0xffffu;
+                                sm.x &= ~drop;
+                                sm.y &= ~drop;
+                                if ((bad & 0x8000u) && t >= ctx && t - ctx < nq) atomicOr(&nan_s[w][(t - ctx) >> 5], 1u << ((t - ctx) & 31));
+                                if ((bad & 0x80000000u) && t + 1 - ctx < nq) atomicOr(&nan_s[w][(t + 1 - ctx) >> 5], 1u << ((t + 1 - ctx) & 31));
+                            }
+                        }
+                        const __half2 S = t_h2(sm.x), M = t_h2(sm.y);
+                        uint32_t v[8];           // channels 8 (chunk) + k: of the even token in the lower half, of the odd one in the upper
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            v[k] = t_bits(__hfma2(t_h2(ones(c0, k)), S, M));
+                            v[4 + k] = t_bits(__hfma2(t_h2(ones(c1, k)), S, M));
+                        }
+                        even = make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[4], v[5], 0x5410), __byte_perm(v[6], v[7], 0x5410));
+                        odd = make_uint4(__byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632), __byte_perm(v[4], v[5], 0x7632), __byte_perm(v[6], v[7], 0x7632));
+                    }
+                    uint8_t* const to = smem + Cfg::V + (chunk >> 3) * 16384;
+                    *reinterpret_cast<uint4*>(to + swz128_offset(r, chunk & 7)) = even;
+                    *reinterpret_cast<uint4*>(to + swz128_offset(r + 1, chunk & 7)) = odd;
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.v_full);
+                load(i + Cfg::V_RING, false);
+            };
+            static_assert(Cfg::K_RING <= Cfg::V_RING && Cfg::V_RING <= Cfg::K_RING + 1, "V of a tile is asked for behind K of it, and its address is kept for 16 tiles");
+            if (nt > 0) turn_k(0);
+            for (int i = 0; i < nt && ok; ++i) {
+                if (i + 1 < nt) turn_k(i + 1);
+                if (ok) turn_v(i);
+            }
+            if (!ok) {                           // copies already asked for land before shared memory is released
+                for (; ring_k != asked_k; ++ring_k) mbar_wait_drain(&bars.raw_k[me][ring_k % Cfg::K_RING], (ring_k / Cfg::K_RING) & 1);
+                for (; ring_v != asked_v; ++ring_v) mbar_wait_drain(&bars.raw_v[me][ring_v % Cfg::V_RING], (ring_v / Cfg::V_RING) & 1);
+            }
+        } else if (warp >= SOFT0) {
+            // ------------------------------------------------------------ softmax: 16 rows a warp, in the quad layout
+            const int sw = warp - SOFT0, quarter = warp & 3, r0 = quarter * 32 + (sw >> 2) * 16, rA = r0 + (lane >> 2), rB = rA + 8, cq = 2 * (lane & 3);
+            const uint32_t lanes = (uint32_t)r0 << 16;
+            const uint32_t tP = tmem + TM_P + lanes, tO = tmem + TM_O + lanes;
+            const float fA = factor_s[rA], fB = factor_s[rB];
+            const int rhoA = qt * ROWS + rA, rhoB = qt * ROWS + rB, tokA = (int)fastdiv((uint32_t)rhoA, a.by_group), tokB = (int)fastdiv((uint32_t)rhoB, a.by_group);
+            const uint32_t* const setA = tree + (min(tokA, nq - 1) - tok0) * TREE_WORDS;
+            const uint32_t* const setB = tree + (min(tokB, nq - 1) - tok0) * TREE_WORDS;
+            const int words = (nq + 31) / 32;
+            float mA = -INFINITY, mB = -INFINITY, lA = 0.f, lB = 0.f;
+            for (int j = 0; j < nt && ok; ++j) {
+                const uint32_t n = done + j;
+                ok = __all_sync(0xffffffffu, mbar_wait(&bars.s_full[n & 1], (n >> 1) & 1, abortp));
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t s0[32], s1[32];
+                tmem_ld_quad64(tmem + TM_S + (n & 1) * KEYS + lanes, s0);
+                tmem_ld_quad64(tmem + TM_S + (n & 1) * KEYS + 64 + lanes, s1);
+                const unsigned long long have = *reinterpret_cast<const unsigned long long*>(have_s[n & 3]);
+                tc_wait_ld();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.s_free[n & 1]);
+                const int key0 = (t0 + j) * KEYS;
+                if (key0 + KEYS > ctx || have != 0x0101010101010101ull) {
+                    // the tile's tokens that a row sees, 32 a word: all ahead of the tree, and the row's set in it; none of blocks that are not there
+                    auto mask = [&](uint32_t (&s)[32], int half) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const int at32 = key0 + 64 * half + 32 * x - ctx, word = at32 >> 5;
+                            const uint32_t both = ((have >> (16 * (2 * half + x)) & 1) ? 0xffffu : 0u) | ((have >> (16 * (2 * half + x) + 8) & 1) ? 0xffff0000u : 0u);
+                            auto seen = [&](const uint32_t* set) {
+                                const uint32_t l = word < 0 ? 0xffffffffu : word < words ? set[word] : 0u, u = word + 1 < 0 ? 0xffffffffu : word + 1 < words ? set[word + 1] : 0u;
+                                return __funnelshift_r(l, u, at32) & both;
+                            };
+                            const uint32_t A = seen(setA) >> cq, Bm = seen(setB) >> cq;
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) {
+                                uint32_t* const v = s + 16 * x + 4 * g;
+                                if (!(A >> (8 * g) & 1u)) v[0] = 0xff800000u;
+                                if (!(A >> (8 * g + 1) & 1u)) v[1] = 0xff800000u;
+                                if (!(Bm >> (8 * g) & 1u)) v[2] = 0xff800000u;
+                                if (!(Bm >> (8 * g + 1) & 1u)) v[3] = 0xff800000u;
+                            }
+                        }
+                    };
+                    mask(s0, 0);
+                    mask(s1, 1);
+                }
+                float bA = -INFINITY, bB = -INFINITY;
+                max_quad64(s0, bA, bB);
+                max_quad64(s1, bA, bB);
+                bA = quad_max(bA) * fA;
+                bB = quad_max(bB) * fB;
+                float alphaA = 1.f, alphaB = 1.f;
+                if (bA > mA + RESCALE_THRESHOLD) { alphaA = ex2_mufu(mA - bA); mA = bA; }        // (also the first tile that the row sees anything of)
+                if (bB > mB + RESCALE_THRESHOLD) { alphaB = ex2_mufu(mB - bB); mB = bB; }
+                const float nA = mA == -INFINITY ? 0.f : UP - mA, nB = mB == -INFINITY ? 0.f : UP - mB;
+                float sumA = 0.f, sumB = 0.f;
+                auto weights = [&](const uint32_t (&s)[32], uint32_t (&p)[16]) {
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const float p0 = ex2_mufu(fmaf(__uint_as_float(s[4 * g]), fA, nA)), p1 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 1]), fA, nA));
+                        const float p2 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 2]), fB, nB)), p3 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 3]), fB, nB));
+                        sumA += p0 + p1;
+                        sumB += p2 + p3;
+                        p[2 * g] = t_weights(p0, p1);
+                        p[2 * g + 1] = t_weights(p2, p3);
+                    }
+                };
+                uint32_t p0[16], p1[16];
+                weights(s0, p0);
+                weights(s1, p1);
+                lA = fmaf(lA, alphaA, sumA);
+                lB = fmaf(lB, alphaB, sumB);
+                if (j > 0) {                     // P and O are in use by the product before this one
+                    ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (n - 1) & 1, abortp));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (__any_sync(0xffffffffu, alphaA != 1.f || alphaB != 1.f)) {
+#pragma unroll 1
+                        for (int c = 0; c < Cfg::SUB; ++c) {
+                            uint32_t v[32];
+                            tmem_ld_quad64(tO + 64 * c, v);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int g = 0; g < 8; ++g) {
+                                v[4 * g] = __float_as_uint(__uint_as_float(v[4 * g]) * alphaA);
+                                v[4 * g + 1] = __float_as_uint(__uint_as_float(v[4 * g + 1]) * alphaA);
+                                v[4 * g + 2] = __float_as_uint(__uint_as_float(v[4 * g + 2]) * alphaB);
+                                v[4 * g + 3] = __float_as_uint(__uint_as_float(v[4 * g + 3]) * alphaB);
+                            }
+                            tmem_st_quad64(tO + 64 * c, v);
+                        }
+                    }
+                }
+                tmem_st_quad32(tP, p0);
+                tmem_st_quad32(tP + 32, p1);
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.p_ready);
+            }
+            if (ok && nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (done + nt - 1) & 1, abortp));
+            if (ok) {
+                // ---- the rows' results
+                tc_fence_after();
+                lA = quad_sum(lA);
+                lB = quad_sum(lB);
+                const bool whole = parts == 1, isA = tokA < nq, isB = tokB < nq;
+                float* const to = whole ? nullptr : part_at(a.part, first_cta, part, D);
+                const size_t outA = ((size_t)(q0 + tokA) * a.kv_heads * a.group + (size_t)h * a.group + (rhoA - tokA * a.group)), outB = ((size_t)(q0 + tokB) * a.kv_heads * a.group + (size_t)h * a.group + (rhoB - tokB * a.group));
+                const float iA = lA == 0.f ? 0.f : 1.f / lA, iB = lB == 0.f ? 0.f : 1.f / lB;
+                uint32_t nanA = 0, nanB = 0;     // groups of V in which the row sees a NaN
+                if (nt > 0 && meets_tree)
+                    for (int i = lane & 3; i < words; i += 4)
+#pragma unroll
+                        for (int w = 0; w < G; ++w) {
+                            if (nan_s[w][i] & setA[i]) nanA |= 1u << w;
+                            if (nan_s[w][i] & setB[i]) nanB |= 1u << w;
+                        }
+                nanA |= __shfl_xor_sync(0xffffffffu, nanA, 1); nanA |= __shfl_xor_sync(0xffffffffu, nanA, 2);
+                nanB |= __shfl_xor_sync(0xffffffffu, nanB, 1); nanB |= __shfl_xor_sync(0xffffffffu, nanB, 2);
+#pragma unroll 1
+                for (int c = 0; c < Cfg::SUB; ++c) {
+                    uint32_t v[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0u;
+                    if (nt > 0) {
+                        tmem_ld_quad64(tO + 64 * c, v);
+                        tc_wait_ld();
+                    }
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const int col = 64 * c + 8 * g + cq;
+                        if (D < Cfg::DT && col >= D) continue;
+                        float x0 = __uint_as_float(v[4 * g]), x1 = __uint_as_float(v[4 * g + 1]), y0 = __uint_as_float(v[4 * g + 2]), y1 = __uint_as_float(v[4 * g + 3]);
+                        if (nanA >> (col >> 5) & 1u) x0 = x1 = NAN;
+                        if (nanB >> (col >> 5) & 1u) y0 = y1 = NAN;
+                        if (whole) {
+                            auto both = [&](float x, float y) { return a.f16 ? t_bits(__floats2half2_rn(x, y)) : pack_bf16x2(x, y); };
+                            if (isA) *reinterpret_cast<uint32_t*>(a.out + outA * D + col) = both(x0 * iA, x1 * iA);
+                            if (isB) *reinterpret_cast<uint32_t*>(a.out + outB * D + col) = both(y0 * iB, y1 * iB);
+                        } else {
+                            if (isA) __stcg(reinterpret_cast<float2*>(to + rA * D + col), make_float2(x0, x1));
+                            if (isB) __stcg(reinterpret_cast<float2*>(to + rB * D + col), make_float2(y0, y1));
+                        }
+                    }
+                }
+                if ((lane & 3) == 0) {
+                    auto stats = [&](bool is, int r, size_t out, float m, float l) {
+                        if (!is) return;
+                        if (!whole) { __stcg(to + ROWS * D + r, m); __stcg(to + ROWS * (D + 1) + r, l); }
+                        else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) - UP + log2f(l)) * T_LN2;
+                    };
+                    stats(isA, rA, outA, mA, lA);
+                    stats(isB, rB, outB, mB, lB);
+                }
+                tc_fence_before();
+            }
+        }
+        if (tid == 0 && part == 0 && parts > 1) a.rows_cut[blockIdx.x] = TreeRow{parts, q0, nq, h, qt};
+        done += nt;
+    }
+    // ---- the end, for all: also of a CTA whose waits ran out
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, 512);
+    if (tid == 0 && abort_flag) atomicExch(&dc->status, (int)PSA_ERR_TIMEOUT);
+}
+
+// Joins the parts of the row tiles that were cut: four rows a CTA, a thread four channels, parts in their order.
+constexpr int JOIN_ROWS = 4;
+template <int D>
+__global__ void __launch_bounds__(JOIN_ROWS * D / 4) tree_join_kernel(const TreeArgs a) {
+    grid_dependency_wait();
+    const TreeRow x = a.rows_cut[blockIdx.x];
+    const int r = blockIdx.y * JOIN_ROWS + threadIdx.x / (D / 4), ch = threadIdx.x % (D / 4) * 4, rho = x.qt * ROWS + r;
+    if (x.parts == 0 || rho >= x.nq * a.group) return;
+    const int c = (int)blockIdx.x, token = (int)fastdiv((uint32_t)rho, a.by_group);
+    float top = -INFINITY, sum = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int AHEAD = 8;
+    for (int p0 = 0; p0 < x.parts; p0 += AHEAD) {
+        float4 o[AHEAD];
+        float m[AHEAD], l[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const float* from = part_at(a.part, c, min(p0 + k, x.parts - 1), D);
+            o[k] = __ldcg(reinterpret_cast<const float4*>(from + r * D + ch));
+            m[k] = p0 + k < x.parts ? __ldcg(from + ROWS * D + r) : -INFINITY;
+            l[k] = p0 + k < x.parts ? __ldcg(from + ROWS * (D + 1) + r) : 0.f;
+        }
+        float most = top;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) most = fmaxf(most, m[k]);
+        const float from = most == -INFINITY ? 0.f : most, old = ex2_mufu(top - from);
+        top = most;
+        sum *= old;
+        v.x *= old; v.y *= old; v.z *= old; v.w *= old;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (p0 + k >= x.parts) break;
+            const float f = ex2_mufu(m[k] - from);
+            sum = fmaf(f, l[k], sum);
+            // (a part in which the row sees nothing: its sums are zeros and its factor is too, and a NaN among them is the row's)
+            v.x = fmaf(f, o[k].x, v.x); v.y = fmaf(f, o[k].y, v.y); v.z = fmaf(f, o[k].z, v.z); v.w = fmaf(f, o[k].w, v.w);
+        }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const size_t row = (size_t)(x.q0 + token) * a.kv_heads * a.group + (size_t)x.h * a.group + (rho - token * a.group);
+    uint2 y;
+    if (a.f16) y = make_uint2(t_bits(__floats2half2_rn(v.x * inv, v.y * inv)), t_bits(__floats2half2_rn(v.z * inv, v.w * inv)));
+    else y = make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+    *reinterpret_cast<uint2*>(a.out + row * D + ch) = y;
+    if (a.lse && ch == 0) a.lse[row] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) - UP + log2f(sum)) * T_LN2;
+}
+
+template <int D>
+int launch_tree(const TreeArgs& all, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
+    static DeviceSetup setup;
+    const int sms = device_setup(&setup, [] { return cudaFuncSetAttribute(tree_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, TCfg<D>::SMEM); }, "tree attention set-up");
+    if (sms <= 0) return PSA_ERR_CUDA;
+    const int grid = sms < T_CTAS ? sms : T_CTAS;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    for (int b0 = 0; b0 < all.sequences; b0 += T_SEQS) {
+        TreeArgs a = all;
+        a.sequences = all.sequences - b0 < T_SEQS ? all.sequences - b0 : T_SEQS;
+        a.seqs += b0;
+        a.q_starts += b0;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(grid);
+        cfg.blockDim = dim3(T_THREADS);
+        cfg.dynamicSmemBytes = TCfg<D>::SMEM;
+        cfg.stream = stream;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        cudaError_t e = cudaLaunchKernelEx(&cfg, tree_kernel<D>, a, dc, b0 == 0 ? dc_next : nullptr);
+        cfg.gridDim = dim3(grid, ROWS / JOIN_ROWS);
+        cfg.blockDim = dim3(JOIN_ROWS * D / 4);
+        cfg.dynamicSmemBytes = 0;
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, tree_join_kernel<D>, a);
+        if (e != cudaSuccess) { set_cuda_error(e, "tree_kernel launch"); return PSA_ERR_CUDA; }
+    }
+    return PSA_OK;
+}
+
+}  // namespace
+
+// (the rows that are cut, then the parts)
+size_t tree_attention_scratch_bytes(int d) { return d > 128 ? 0 : (size_t)T_CTAS * 32 + (size_t)(2 * T_CTAS + 1) * ROWS * (d + 2) * sizeof(float); }
+
+int tree_attention(const psa_cache& c, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads, float scale, int dtype,
+                   void* out, float* lse, void* scratch, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
+    static_assert(sizeof(TreeRow) <= 32, "");
+    const int group = heads / c.kv_heads;
+    const TreeArgs a = {static_cast<const uint8_t*>(c.pool), c.tables, c.lens, seqs, q_starts, parents, static_cast<const uint16_t*>(Q), static_cast<uint16_t*>(out), lse,
+                        reinterpret_cast<float*>(static_cast<char*>(scratch) + (size_t)T_CTAS * 32), static_cast<TreeRow*>(scratch), q_stride, c.pages, c.slots, c.width, c.page_size, c.kv_heads,
+                        group, sequences, rows, dtype == PSA_F16, c.d_k, scale, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
+    switch (c.d_k) {
+        case 32: return launch_tree<32>(a, dc, dc_next, stream);
+        case 64: return launch_tree<64>(a, dc, dc_next, stream);
+        case 96: return launch_tree<96>(a, dc, dc_next, stream);
+        case 128: return launch_tree<128>(a, dc, dc_next, stream);
+        default: return PSA_ERR_UNSUPPORTED;
+    }
+}
+
+}  // namespace psa
