@@ -42,10 +42,10 @@ struct TCfg {
     static constexpr int TILE = 128 * DT * 2;   // bytes of an operand tile: sub-tiles of 64 columns, 128-byte rows swizzled
     static constexpr int HALF = 10 * D;         // bytes of K, and of V, in a block
     static constexpr int K_RING = 2, V_RING = 3;
-    static constexpr int Q = 0, K1 = TILE, K2 = 2 * TILE, V = 3 * TILE, E = 4 * TILE, RAW_K = E + 16384, RAW_V = RAW_K + K_RING * TURNS * HALF, TREE = RAW_V + V_RING * TURNS * HALF;
+    static constexpr int K1 = 0, K2 = TILE, V = 2 * TILE, E = 3 * TILE, RAW_K = E + 16384, RAW_V = RAW_K + K_RING * TURNS * HALF, TREE = RAW_V + V_RING * TURNS * HALF;
     static constexpr int SMEM = TREE + ROWS * TREE_WORDS * 4 + 1024;
 };
-constexpr int TM_S = 0, TM_P = 256, TM_O = 384;  // columns of tensor memory: S twice, P, O
+constexpr int TM_S = 0, TM_O = 256, TM_Q = 384, TM_E = 448;     // columns of tensor memory: S twice (P over its first half), O, the queries and their sums
 
 struct TreeArgs {
     const uint8_t* pool;
@@ -68,7 +68,7 @@ __device__ __forceinline__ float* part_at(float* part, int c, int p, int d) { re
 
 struct TBars {
     uint64_t raw_k[TURNS][2], raw_v[TURNS][3];
-    uint64_t k_full, k_empty, v_full, o_done, s_full[2], s_free[2], p_ready;
+    uint64_t k_full, k_empty, v_full, o_done, s_full[2], p_ready;
 };
 
 __device__ __forceinline__ uint32_t t_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
@@ -77,6 +77,27 @@ __device__ __forceinline__ uint32_t t_weights(float lo, float hi) {
     uint32_t v;
     asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
     return v;
+}
+// Two numbers at a time.
+__device__ __forceinline__ uint64_t t_pair(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 t_pair(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t t_add2(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t t_fma2(uint64_t x, uint64_t y, uint64_t z) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+    return r;
 }
 __host__ __device__ constexpr uint32_t t_idesc(uint32_t n, uint32_t b_major) { return umma_idesc_bf16(128, n, UMMA_K_MAJOR, b_major) & ~((1u << 7) | (1u << 10)); }      // fp16 operands
 
@@ -93,7 +114,6 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     __shared__ int abort_flag, bad_s;
     __shared__ long long base_s[T_SEQS + 1], scan_s[T_WARPS];
     __shared__ int len_s[T_SEQS], q0_s[T_SEQS], nq_s[T_SEQS], slot_s[T_SEQS];
-    __shared__ float factor_s[ROWS];            // of a row's scores, to log2 units
     __shared__ __align__(8) uint8_t have_s[4][TURNS];        // blocks of a tile that are there, by tile modulo 4
     __shared__ uint32_t nan_s[G][PSA_TREE_MOST / 32];            // tokens of the tree whose group of V reads back as NaN or infinite
 
@@ -109,7 +129,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
         mbar_init(&bars.k_empty, 1);
         mbar_init(&bars.o_done, 1);
         mbar_init(&bars.p_ready, SOFTS);
-        for (int s = 0; s < 2; ++s) { mbar_init(&bars.s_full[s], 1); mbar_init(&bars.s_free[s], SOFTS); }
+        for (int s = 0; s < 2; ++s) mbar_init(&bars.s_full[s], 1);
         fence_mbar_init();
     }
     if (warp == 1) { tmem_alloc(&tmem_s, 512); tmem_relinquish(); }
@@ -183,54 +203,65 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
         const int tok0 = (int)fastdiv((uint32_t)(qt * ROWS), a.by_group);       // first token of the row tile
         const bool meets_tree = t1 * KEYS > ctx;
         __syncthreads();                         // (the item before it is done with)
-        if (warp >= SOFT0) {
-            // ---- the queries: four lanes a row, a group of 32 channels each
-            const int r = (tid - 32 * SOFT0) >> 2, w = lane & 3, rho = qt * ROWS + r, token = (int)fastdiv((uint32_t)rho, a.by_group);
-            uint4 raw[4];
+        const int sw = warp - SOFT0, r0 = (warp & 3) * 32 + (sw >> 2) * 16, rA = r0 + (lane >> 2), rB = rA + 8, cq = 2 * (lane & 3);       // a softmax warp's 16 rows, in the quad layout
+        const uint32_t lanes = (uint32_t)r0 << 16;
+        const int rhoA = qt * ROWS + rA, rhoB = qt * ROWS + rB, tokA = (int)fastdiv((uint32_t)rhoA, a.by_group), tokB = (int)fastdiv((uint32_t)rhoB, a.by_group);
+        float fA = 1.f, fB = 1.f;                // factors of the rows' scores, to log2 units
+        if (warp >= SOFT0 && warp < TURN0) {
+            // ---- the queries into tensor memory: 64 columns of K, 32 words, at a time
+            uint32_t raw[Cfg::SUB][16];          // [2 g]: channels 64 u + 8 g + cq .. of row A, [2 g + 1] of row B
+            float topA = 0.f, topB = 0.f;
+            auto number = [&](uint32_t x) { return a.f16 ? __half22float2(t_h2(x)) : make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); };
+            auto from = [&](int token, int rho) { return a.q + (size_t)(q0 + token) * a.q_stride + ((size_t)h * a.group + (rho - token * a.group)) * D + cq; };
+            const uint16_t *const qA = from(tokA, rhoA), *const qB = from(tokB, rhoB);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
-            if (w < G && token < nq) {
-                const uint4* from = reinterpret_cast<const uint4*>(a.q + (size_t)(q0 + token) * a.q_stride + ((size_t)h * a.group + (rho - token * a.group)) * D + 32 * w);
+            for (int u = 0; u < Cfg::SUB; ++u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) raw[i] = from[i];
-            }
-            float top = 0.f;
-            auto number = [&](int i, int k) {    // pair k of word i
-                const uint32_t x = (&raw[i].x)[k];
-                return a.f16 ? __half22float2(t_h2(x)) : make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
-            };
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 f = number(i, k);
-                    top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+                for (int g = 0; g < 8; ++g) {
+                    const bool is = 64 * u + 8 * g < D;
+                    raw[u][2 * g] = is && tokA < nq ? *reinterpret_cast<const uint32_t*>(qA + 64 * u + 8 * g) : 0u;
+                    raw[u][2 * g + 1] = is && tokB < nq ? *reinterpret_cast<const uint32_t*>(qB + 64 * u + 8 * g) : 0u;
                 }
-            top = quad_max(top);
-            // 2^e <= top < 2^(e + 1): the row goes in as q 2^(8 - e), exact but for what lies 2^32 below its largest number; sums of 32 stay below 2^14
-            const uint32_t e = min(max(__float_as_uint(top) >> 23, 1u), 253u);
-            const float down = __uint_as_float((254u - e) << 23), up = __uint_as_float(e << 23);
-            float sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t y[4];
+            for (int u = 0; u < Cfg::SUB; ++u)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 f = number(i, k);
-                    const __half2 v = __floats2half2_rn(f.x * down * 256.f, f.y * down * 256.f);
-                    y[k] = t_bits(v);
-                    sum += __low2float(v) + __high2float(v);
+                for (int g = 0; g < 8; ++g) {
+                    const float2 x = number(raw[u][2 * g]), y = number(raw[u][2 * g + 1]);
+                    topA = max3(topA, fabsf(x.x), fabsf(x.y));
+                    topB = max3(topB, fabsf(y.x), fabsf(y.y));
                 }
-                const int chunk = 4 * w + i;
-                if (w < G) *reinterpret_cast<uint4*>(smem + Cfg::Q + (chunk >> 3) * 16384 + swz128_offset(r, chunk & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
+            // 2^e <= top < 2^(e + 1): a row goes in as q 2^(8 - e), exact but for what lies 2^32 below its largest number; sums of 32 stay below 2^14
+            const uint32_t eA = min(max(__float_as_uint(quad_max(topA)) >> 23, 1u), 253u), eB = min(max(__float_as_uint(quad_max(topB)) >> 23, 1u), 253u);
+            const float downA = __uint_as_float((254u - eA) << 23), downB = __uint_as_float((254u - eB) << 23);
+            fA = fmaxf(__uint_as_float(eA << 23) * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
+            fB = fmaxf(__uint_as_float(eB << 23) * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
+            uint32_t sums[4] = {0, 0, 0, 0};     // columns 4 w ..: the sum of the row over group w in two parts, twice.  This thread's words c and 4 + c of row A, then of row B
+#pragma unroll
+            for (int u = 0; u < Cfg::SUB; ++u) {
+                float sA[2] = {0.f, 0.f}, sB[2] = {0.f, 0.f};
+#pragma unroll
+                for (int g = 0; g < 8; ++g) {
+                    const float2 x = number(raw[u][2 * g]), y = number(raw[u][2 * g + 1]);
+                    const __half2 v = __floats2half2_rn(x.x * downA * 256.f, x.y * downA * 256.f), z = __floats2half2_rn(y.x * downB * 256.f, y.y * downB * 256.f);
+                    raw[u][2 * g] = t_bits(v);
+                    raw[u][2 * g + 1] = t_bits(z);
+                    sA[g >> 2] += __low2float(v) + __high2float(v);
+                    sB[g >> 2] += __low2float(z) + __high2float(z);
+                }
+                tmem_st_quad32(tmem + TM_Q + 32 * u + lanes, raw[u]);
+                auto two = [&](float s) {
+                    s = quad_sum(s);
+                    const __half hi16 = __float2half_rn(s);
+                    return t_bits(__halves2half2(hi16, __float2half_rn(s - __half2float(hi16))));
+                };
+                const uint32_t a0 = two(sA[0]), a1 = two(sA[1]), b0 = two(sB[0]), b1 = two(sB[1]);
+                sums[2 * u] = lane & 2 ? a1 : a0;                // (words 4 u + c: of group 2 u + c / 2)
+                sums[2 * u + 1] = lane & 2 ? b1 : b0;
             }
-            if (w < G) {                         // columns 16 + 4 w ..: the sum in two parts, twice
-                const __half hi16 = __float2half_rn(sum), lo16 = __float2half_rn(sum - __half2float(hi16));
-                const uint32_t both = t_bits(__halves2half2(hi16, lo16));
-                *reinterpret_cast<uint2*>(smem + Cfg::E + swz128_offset(r, 2 + (w >> 1)) + 8 * (w & 1)) = make_uint2(both, both);
-            }
-            if (w == 0) factor_s[r] = fmaxf(up * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
-        } else {
+            asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};" ::"r"(tmem + TM_E + lanes), "r"(sums[0]), "r"(sums[1]), "r"(sums[2]), "r"(sums[3]) : "memory");
+            tc_wait_st();
+            tc_fence_before();
+        } else if (warp < SOFT0) {
             // ---- the tokens' sets of the tree: each its own and its ancestors
             const int words = (nq + 31) / 32, tok = tok0 + tid;
             for (int i = tid; i < G * (PSA_TREE_MOST / 32); i += 32 * SOFT0) (&nan_s[0][0])[i] = 0u;
@@ -248,30 +279,31 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
         }
         fence_async_smem();
         if (__syncthreads_or(abort_flag)) { ok = false; break; }
+        tc_fence_after();
 
         if (warp == MMA_WARP) {
             if (lane == 0 && nt > 0) {
                 constexpr uint32_t idescS = t_idesc(KEYS, UMMA_K_MAJOR), idescO = t_idesc(D, UMMA_MN_MAJOR);
-                const uint32_t q_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::Q)), k1_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K1)), k2_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K2));
+                const uint32_t k1_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K1)), k2_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K2));
                 const uint32_t e_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::E)), v_lo = umma_desc_lo_mnmajor(smem_u32(smem + Cfg::V), 16384);
                 for (int j = 0; j <= nt && ok; ++j) {
                     const uint32_t n = done + j;
                     if (j < nt) {
                         ok = mbar_wait(&bars.k_full, n & 1, abortp);
-                        if (ok && n >= 2) ok = mbar_wait(&bars.s_free[n & 1], ((n >> 1) - 1) & 1, abortp);
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t dS = tmem + TM_S + (n & 1) * KEYS;
-                        umma_ss(dS, umma_desc_join(e_lo + (32 >> 4), UMMA_DESC_HI_SW128), umma_desc_join(e_lo, UMMA_DESC_HI_SW128), idescS, 0);
+                        // (where P of tile j - 2 was: its product has been issued)
+                        umma_ts(dS, tmem + TM_E, umma_desc_join(e_lo, UMMA_DESC_HI_SW128), idescS, 0);
 #pragma unroll
                         for (int kk = 0; kk < Cfg::KS; ++kk) {
                             const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
-                            umma_ss(dS, umma_desc_join(q_lo + off, UMMA_DESC_HI_SW128), umma_desc_join(k1_lo + off, UMMA_DESC_HI_SW128), idescS, 1);
+                            umma_ts(dS, tmem + TM_Q + kk * 8, umma_desc_join(k1_lo + off, UMMA_DESC_HI_SW128), idescS, 1);
                         }
 #pragma unroll
                         for (int kk = 0; kk < Cfg::KS; ++kk) {
                             const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
-                            umma_ss(dS, umma_desc_join(q_lo + off, UMMA_DESC_HI_SW128), umma_desc_join(k2_lo + off, UMMA_DESC_HI_SW128), idescS, 1);
+                            umma_ts(dS, tmem + TM_Q + kk * 8, umma_desc_join(k2_lo + off, UMMA_DESC_HI_SW128), idescS, 1);
                         }
                         umma_commit(&bars.s_full[n & 1]);
                         umma_commit(&bars.k_empty);
@@ -282,7 +314,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                         tc_fence_after();
 #pragma unroll
                         for (int kk = 0; kk < KEYS / 16; ++kk)
-                            umma_ts(tmem + TM_O, tmem + TM_P + kk * 8, umma_desc_join(v_lo + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, j > 1 || kk > 0);
+                            umma_ts(tmem + TM_O, tmem + TM_S + ((n - 1) & 1) * KEYS + kk * 8, umma_desc_join(v_lo + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, j > 1 || kk > 0);
                         umma_commit(&bars.o_done);
                     }
                 }
@@ -432,11 +464,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             }
         } else if (warp >= SOFT0) {
             // ------------------------------------------------------------ softmax: 16 rows a warp, in the quad layout
-            const int sw = warp - SOFT0, quarter = warp & 3, r0 = quarter * 32 + (sw >> 2) * 16, rA = r0 + (lane >> 2), rB = rA + 8, cq = 2 * (lane & 3);
-            const uint32_t lanes = (uint32_t)r0 << 16;
-            const uint32_t tP = tmem + TM_P + lanes, tO = tmem + TM_O + lanes;
-            const float fA = factor_s[rA], fB = factor_s[rB];
-            const int rhoA = qt * ROWS + rA, rhoB = qt * ROWS + rB, tokA = (int)fastdiv((uint32_t)rhoA, a.by_group), tokB = (int)fastdiv((uint32_t)rhoB, a.by_group);
+            const uint32_t tO = tmem + TM_O + lanes;
             const uint32_t* const setA = tree + (min(tokA, nq - 1) - tok0) * TREE_WORDS;
             const uint32_t* const setB = tree + (min(tokB, nq - 1) - tok0) * TREE_WORDS;
             const int words = (nq + 31) / 32;
@@ -446,67 +474,67 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 ok = __all_sync(0xffffffffu, mbar_wait(&bars.s_full[n & 1], (n >> 1) & 1, abortp));
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t s0[32], s1[32];
-                tmem_ld_quad64(tmem + TM_S + (n & 1) * KEYS + lanes, s0);
-                tmem_ld_quad64(tmem + TM_S + (n & 1) * KEYS + 64 + lanes, s1);
+                const uint32_t tS = tmem + TM_S + (n & 1) * KEYS + lanes;
                 const unsigned long long have = *reinterpret_cast<const unsigned long long*>(have_s[n & 3]);
-                tc_wait_ld();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.s_free[n & 1]);
                 const int key0 = (t0 + j) * KEYS;
-                if (key0 + KEYS > ctx || have != 0x0101010101010101ull) {
+                const bool masked = key0 + KEYS > ctx || have != 0x0101010101010101ull;
+                // 64 columns of the scores (read twice, for the maximum and for the weights: held in between they would not fit the registers)
+                auto scores = [&](uint32_t (&s)[32], int half) {
+                    tmem_ld_quad64(tS + 64 * half, s);
+                    tc_wait_ld();
+                    if (!masked) return;
                     // the tile's tokens that a row sees, 32 a word: all ahead of the tree, and the row's set in it; none of blocks that are not there
-                    auto mask = [&](uint32_t (&s)[32], int half) {
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const int at32 = key0 + 64 * half + 32 * x - ctx, word = at32 >> 5;
-                            const uint32_t both = ((have >> (16 * (2 * half + x)) & 1) ? 0xffffu : 0u) | ((have >> (16 * (2 * half + x) + 8) & 1) ? 0xffff0000u : 0u);
-                            auto seen = [&](const uint32_t* set) {
-                                const uint32_t l = word < 0 ? 0xffffffffu : word < words ? set[word] : 0u, u = word + 1 < 0 ? 0xffffffffu : word + 1 < words ? set[word + 1] : 0u;
-                                return __funnelshift_r(l, u, at32) & both;
-                            };
-                            const uint32_t A = seen(setA) >> cq, Bm = seen(setB) >> cq;
+                    for (int x = 0; x < 2; ++x) {
+                        const int at32 = key0 + 64 * half + 32 * x - ctx, word = at32 >> 5;
+                        const uint32_t both = ((have >> (16 * (2 * half + x)) & 1) ? 0xffffu : 0u) | ((have >> (16 * (2 * half + x) + 8) & 1) ? 0xffff0000u : 0u);
+                        auto seen = [&](const uint32_t* set) {
+                            const uint32_t l = word < 0 ? 0xffffffffu : word < words ? set[word] : 0u, u = word + 1 < 0 ? 0xffffffffu : word + 1 < words ? set[word + 1] : 0u;
+                            return (__funnelshift_r(l, u, at32) & both) >> cq;
+                        };
+                        const uint32_t A = seen(setA), Bm = seen(setB);
 #pragma unroll
-                            for (int g = 0; g < 4; ++g) {
-                                uint32_t* const v = s + 16 * x + 4 * g;
-                                if (!(A >> (8 * g) & 1u)) v[0] = 0xff800000u;
-                                if (!(A >> (8 * g + 1) & 1u)) v[1] = 0xff800000u;
-                                if (!(Bm >> (8 * g) & 1u)) v[2] = 0xff800000u;
-                                if (!(Bm >> (8 * g + 1) & 1u)) v[3] = 0xff800000u;
-                            }
+                        for (int g = 0; g < 4; ++g) {
+                            uint32_t* const v = s + 16 * x + 4 * g;
+                            if (!(A >> (8 * g) & 1u)) v[0] = 0xff800000u;
+                            if (!(A >> (8 * g + 1) & 1u)) v[1] = 0xff800000u;
+                            if (!(Bm >> (8 * g) & 1u)) v[2] = 0xff800000u;
+                            if (!(Bm >> (8 * g + 1) & 1u)) v[3] = 0xff800000u;
                         }
-                    };
-                    mask(s0, 0);
-                    mask(s1, 1);
-                }
+                    }
+                };
+                uint32_t s[32];
                 float bA = -INFINITY, bB = -INFINITY;
-                max_quad64(s0, bA, bB);
-                max_quad64(s1, bA, bB);
+                scores(s, 0);
+                max_quad64(s, bA, bB);
+                scores(s, 1);
+                max_quad64(s, bA, bB);
                 bA = quad_max(bA) * fA;
                 bB = quad_max(bB) * fB;
                 float alphaA = 1.f, alphaB = 1.f;
                 if (bA > mA + RESCALE_THRESHOLD) { alphaA = ex2_mufu(mA - bA); mA = bA; }        // (also the first tile that the row sees anything of)
                 if (bB > mB + RESCALE_THRESHOLD) { alphaB = ex2_mufu(mB - bB); mB = bB; }
                 const float nA = mA == -INFINITY ? 0.f : UP - mA, nB = mB == -INFINITY ? 0.f : UP - mB;
-                float sumA = 0.f, sumB = 0.f;
-                auto weights = [&](const uint32_t (&s)[32], uint32_t (&p)[16]) {
+                uint64_t sumA = 0, sumB = 0;
+                const uint64_t fA2 = t_pair(fA, fA), fB2 = t_pair(fB, fB), nA2 = t_pair(nA, nA), nB2 = t_pair(nB, nB);
+                uint32_t p1[16], p0[16];
+                auto weights = [&](uint32_t (&p)[16]) {
 #pragma unroll
                     for (int g = 0; g < 8; ++g) {
-                        const float p0 = ex2_mufu(fmaf(__uint_as_float(s[4 * g]), fA, nA)), p1 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 1]), fA, nA));
-                        const float p2 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 2]), fB, nB)), p3 = ex2_mufu(fmaf(__uint_as_float(s[4 * g + 3]), fB, nB));
-                        sumA += p0 + p1;
-                        sumB += p2 + p3;
-                        p[2 * g] = t_weights(p0, p1);
-                        p[2 * g + 1] = t_weights(p2, p3);
+                        const float2 x = t_pair(t_fma2(t_pair(__uint_as_float(s[4 * g]), __uint_as_float(s[4 * g + 1])), fA2, nA2)), y = t_pair(t_fma2(t_pair(__uint_as_float(s[4 * g + 2]), __uint_as_float(s[4 * g + 3])), fB2, nB2));
+                        const float x0 = ex2_mufu(x.x), x1 = ex2_mufu(x.y), y0 = ex2_mufu(y.x), y1 = ex2_mufu(y.y);
+                        sumA = t_add2(sumA, t_pair(x0, x1));
+                        sumB = t_add2(sumB, t_pair(y0, y1));
+                        p[2 * g] = t_weights(x0, x1);
+                        p[2 * g + 1] = t_weights(y0, y1);
                     }
                 };
-                uint32_t p0[16], p1[16];
-                weights(s0, p0);
-                weights(s1, p1);
-                lA = fmaf(lA, alphaA, sumA);
-                lB = fmaf(lB, alphaB, sumB);
-                if (j > 0) {                     // P and O are in use by the product before this one
+                weights(p1);
+                scores(s, 0);
+                weights(p0);
+                lA = fmaf(lA, alphaA, t_pair(sumA).x + t_pair(sumA).y);
+                lB = fmaf(lB, alphaB, t_pair(sumB).x + t_pair(sumB).y);
+                if (j > 0) {                     // O is in use by the product before this one
                     ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (n - 1) & 1, abortp));
                     if (!ok) break;
                     tc_fence_after();
@@ -527,8 +555,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                         }
                     }
                 }
-                tmem_st_quad32(tP, p0);
-                tmem_st_quad32(tP + 32, p1);
+                tmem_st_quad32(tS, p0);          // (over the scores, which this warp alone reads in these rows)
+                tmem_st_quad32(tS + 32, p1);
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
