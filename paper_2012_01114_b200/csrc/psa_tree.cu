@@ -28,10 +28,11 @@ namespace psa {
 namespace {
 
 constexpr int ROWS = 128, KEYS = 128;
-constexpr int MMA_WARP = 0, SOFT0 = 4, SOFTS = 8, TURN0 = SOFT0 + SOFTS, TURNS = 8, T_WARPS = TURN0 + TURNS, T_THREADS = 32 * T_WARPS;
+constexpr int MMA_WARP = 0, K_WARP = 1, V_WARP = 2, SET_WARP = 3, SOFT0 = 4, SOFTS = 8, TURN0 = SOFT0 + SOFTS, TURNS = 8, T_WARPS = TURN0 + TURNS, T_THREADS = 32 * T_WARPS;
 constexpr int T_SEQS = 512;                     // sequences of one launch
 constexpr int T_CTAS = 160;                     // at most
-constexpr int LEAST = 4;                        // tiles of a piece
+constexpr int LEAST = 4;                        // tiles of a piece, or what takes as long
+constexpr int ROW_COST = 3;                     // what a row tile costs beside its tiles of keys, in such
 constexpr int TREE_WORDS = PSA_TREE_MOST / 32 + 1;
 constexpr float UP = 7.f;                       // log2 of what weights are held larger by
 constexpr float T_LN2 = 0.6931471805599453f;
@@ -41,7 +42,7 @@ struct TCfg {
     static constexpr int DT = D <= 64 ? 64 : 128, SUB = DT / 64, KS = D / 16, G = D / 32;
     static constexpr int TILE = 128 * DT * 2;   // bytes of an operand tile: sub-tiles of 64 columns, 128-byte rows swizzled
     static constexpr int HALF = 10 * D;         // bytes of K, and of V, in a block
-    static constexpr int K_RING = 2, V_RING = 3;
+    static constexpr int K_RING = 3, V_RING = 4;
     static constexpr int K1 = 0, K2 = TILE, V = 2 * TILE, E = 3 * TILE, RAW_K = E + 16384, RAW_V = RAW_K + K_RING * TURNS * HALF, TREE = RAW_V + V_RING * TURNS * HALF;
     static constexpr int SMEM = TREE + ROWS * TREE_WORDS * 4 + 1024;
 };
@@ -67,8 +68,14 @@ struct TreeRow {
 __device__ __forceinline__ float* part_at(float* part, int c, int p, int d) { return part + (size_t)(p == 0 ? 2 * c + 1 : 2 * (c + p)) * ROWS * (d + 2); }
 
 struct TBars {
-    uint64_t raw_k[TURNS][2], raw_v[TURNS][3];
-    uint64_t k_full, k_empty, v_full, o_done, s_full[2], p_ready;
+    uint64_t k_raw[4], k_raw_free[4], v_raw[4], v_raw_free[4];
+    uint64_t q_full, k_full, k_empty, v_full, o_done, s_full[2], p_ready, sets_full, sets_free;
+};
+// Tiles t0 .. t0 + nt - 1 of row tile qt of head h of a sequence.
+struct TItem {
+    int len, nq, q0, slot, t0, nt, h, qt, ctx, tok0;       // ctx: the tree's first token; tok0: the row tile's first
+    int first_cta, part, parts;                             // of the row tile; a CTA has one part of it
+    bool meets_tree;
 };
 
 __device__ __forceinline__ uint32_t t_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
@@ -111,25 +118,25 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     uint32_t* const tree = reinterpret_cast<uint32_t*>(smem + Cfg::TREE);       // [ROWS][TREE_WORDS]: by token of the row tile, the tree's tokens that it sees
     __shared__ TBars bars;
     __shared__ uint32_t tmem_s;
-    __shared__ int abort_flag, bad_s;
+    __shared__ int abort_flag;
     __shared__ long long base_s[T_SEQS + 1], scan_s[T_WARPS];
     __shared__ int len_s[T_SEQS], q0_s[T_SEQS], nq_s[T_SEQS], slot_s[T_SEQS];
-    __shared__ __align__(8) uint8_t have_s[4][TURNS];        // blocks of a tile that are there, by tile modulo 4
-    __shared__ uint32_t nan_s[G][PSA_TREE_MOST / 32];            // tokens of the tree whose group of V reads back as NaN or infinite
+    __shared__ __align__(8) uint8_t have_s[8][TURNS];            // blocks of a tile that are there, by tile modulo 8
+    __shared__ uint32_t nan_s[2][G][PSA_TREE_MOST / 32];         // by items in turn: tokens of the tree whose group of V reads back as NaN or infinite
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         abort_flag = 0;
-        for (int w = 0; w < TURNS; ++w) {
-            for (int s = 0; s < 2; ++s) mbar_init(&bars.raw_k[w][s], 1);
-            for (int s = 0; s < 3; ++s) mbar_init(&bars.raw_v[w][s], 1);
+        for (int s = 0; s < 4; ++s) {
+            mbar_init(&bars.k_raw[s], TURNS); mbar_init(&bars.k_raw_free[s], TURNS);
+            mbar_init(&bars.v_raw[s], TURNS); mbar_init(&bars.v_raw_free[s], TURNS);
         }
-        mbar_init(&bars.k_full, TURNS);
-        mbar_init(&bars.v_full, TURNS);
-        mbar_init(&bars.k_empty, 1);
-        mbar_init(&bars.o_done, 1);
+        mbar_init(&bars.q_full, SOFTS);
+        mbar_init(&bars.k_full, TURNS); mbar_init(&bars.k_empty, 1);
+        mbar_init(&bars.v_full, TURNS); mbar_init(&bars.o_done, 1);
+        mbar_init(&bars.s_full[0], 1); mbar_init(&bars.s_full[1], 1);
         mbar_init(&bars.p_ready, SOFTS);
-        for (int s = 0; s < 2; ++s) mbar_init(&bars.s_full[s], 1);
+        mbar_init(&bars.sets_full, 1); mbar_init(&bars.sets_free, SOFTS);
         fence_mbar_init();
     }
     if (warp == 1) { tmem_alloc(&tmem_s, 512); tmem_relinquish(); }
@@ -152,7 +159,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             const int held = there ? max(a.lens[slot], 0) : 0, len = (int)min((long long)held, (long long)a.width * a.page_size);
             strange |= (nq > 0 && (!there || held != len)) || nq != s1 - s0;
             const int tiles = max((int)(((uint32_t)len + KEYS - 1) / KEYS), 1), row_tiles = (nq * a.group + ROWS - 1) / ROWS;
-            n = (long long)row_tiles * a.kv_heads * tiles;
+            n = (long long)row_tiles * a.kv_heads * (tiles + ROW_COST);
             len_s[b] = len;
             q0_s[b] = q0;
             nq_s[b] = nq;
@@ -182,117 +189,59 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     tc_fence_after();
     const uint32_t tmem = tmem_s;
 
-    uint32_t done = 0;                          // tiles that the CTA has worked off: the phases of all barriers but the rings' follow from it
-    uint32_t ring_k = 0, ring_v = 0;            // a turning warp's blocks so far
+    // ---- Every role walks the CTA's items by itself: its share of the list.  A row tile is ROW_COST units and one for each tile of keys.
+    auto next_item = [&](long long& at, TItem& x) -> bool {
+        while (at < mine1) {
+            int lo = 0, hi = a.sequences - 1;    // the last sequence that begins at or before it (and has tiles: those without begin where the next one does)
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (base_s[mid] <= at) lo = mid; else hi = mid - 1;
+            }
+            x.len = len_s[lo];
+            x.nq = nq_s[lo];
+            x.q0 = q0_s[lo];
+            x.slot = slot_s[lo];
+            const int tiles = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1);
+            const long long units = tiles + ROW_COST, inside = at - base_s[lo], row = inside / units, u0 = inside - row * units, u1 = min(units, u0 + (mine1 - at)), row0 = at - u0;
+            const int row_tiles = (x.nq * a.group + ROWS - 1) / ROWS;
+            at += u1 - u0;
+            x.t0 = (int)max(u0 - ROW_COST, 0LL);
+            const int t1 = (int)max(u1 - ROW_COST, 0LL);
+            if (t1 <= x.t0) continue;
+            x.nt = x.len > 0 ? t1 - x.t0 : 0;
+            x.h = (int)row / row_tiles;
+            x.qt = (int)row - x.h * row_tiles;
+            x.ctx = x.len - x.nq;
+            x.tok0 = (int)fastdiv((uint32_t)(x.qt * ROWS), a.by_group);
+            x.first_cta = (int)((row0 + ROW_COST) / per);
+            x.parts = (int)((row0 + units - 1) / per) - x.first_cta + 1;
+            x.part = (int)blockIdx.x - x.first_cta;
+            x.meets_tree = x.nt > 0 && t1 * (long long)KEYS > x.ctx;
+            return true;
+        }
+        return false;
+    };
+    long long at = mine0;
+    TItem x;
+    uint32_t n = 0;                             // tiles of the CTA so far: the phases of all barriers follow from it, but those that go by items
     bool ok = true;
-    for (long long at = mine0; at < mine1;) {
-        // ---- the item: tiles t0 .. t1 - 1 of row tile qt of head h of sequence b
-        int lo = 0, hi = a.sequences - 1;       // the last sequence that begins at or before it (and has tiles: those without begin where the next one does)
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (base_s[mid] <= at) lo = mid; else hi = mid - 1;
-        }
-        const int b = lo, len = len_s[b], nq = nq_s[b], q0 = q0_s[b], slot = slot_s[b], tiles = max((int)(((uint32_t)len + KEYS - 1) / KEYS), 1);
-        const long long inside = at - base_s[b];
-        const int row = (int)(inside / tiles), t0 = (int)(inside - (long long)row * tiles), t1 = (int)min((long long)tiles, t0 + (mine1 - at)), nt = len > 0 ? t1 - t0 : 0;
-        const int row_tiles = (nq * a.group + ROWS - 1) / ROWS, h = row / row_tiles, qt = row - h * row_tiles;
-        const int ctx = len - nq;                // the tree's first token
-        const long long row0 = at - t0;          // of the row tile, in the list
-        const int first_cta = (int)(row0 / per), parts = (int)((row0 + tiles - 1) / per) - first_cta + 1, part = (int)blockIdx.x - first_cta;
-        at += t1 - t0;
-        const int tok0 = (int)fastdiv((uint32_t)(qt * ROWS), a.by_group);       // first token of the row tile
-        const bool meets_tree = t1 * KEYS > ctx;
-        __syncthreads();                         // (the item before it is done with)
-        const int sw = warp - SOFT0, r0 = (warp & 3) * 32 + (sw >> 2) * 16, rA = r0 + (lane >> 2), rB = rA + 8, cq = 2 * (lane & 3);       // a softmax warp's 16 rows, in the quad layout
-        const uint32_t lanes = (uint32_t)r0 << 16;
-        const int rhoA = qt * ROWS + rA, rhoB = qt * ROWS + rB, tokA = (int)fastdiv((uint32_t)rhoA, a.by_group), tokB = (int)fastdiv((uint32_t)rhoB, a.by_group);
-        float fA = 1.f, fB = 1.f;                // factors of the rows' scores, to log2 units
-        if (warp >= SOFT0 && warp < TURN0) {
-            // ---- the queries into tensor memory: 64 columns of K, 32 words, at a time
-            uint32_t raw[Cfg::SUB][16];          // [2 g]: channels 64 u + 8 g + cq .. of row A, [2 g + 1] of row B
-            float topA = 0.f, topB = 0.f;
-            auto number = [&](uint32_t x) { return a.f16 ? __half22float2(t_h2(x)) : make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); };
-            auto from = [&](int token, int rho) { return a.q + (size_t)(q0 + token) * a.q_stride + ((size_t)h * a.group + (rho - token * a.group)) * D + cq; };
-            const uint16_t *const qA = from(tokA, rhoA), *const qB = from(tokB, rhoB);
-#pragma unroll
-            for (int u = 0; u < Cfg::SUB; ++u)
-#pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    const bool is = 64 * u + 8 * g < D;
-                    raw[u][2 * g] = is && tokA < nq ? *reinterpret_cast<const uint32_t*>(qA + 64 * u + 8 * g) : 0u;
-                    raw[u][2 * g + 1] = is && tokB < nq ? *reinterpret_cast<const uint32_t*>(qB + 64 * u + 8 * g) : 0u;
-                }
-#pragma unroll
-            for (int u = 0; u < Cfg::SUB; ++u)
-#pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    const float2 x = number(raw[u][2 * g]), y = number(raw[u][2 * g + 1]);
-                    topA = max3(topA, fabsf(x.x), fabsf(x.y));
-                    topB = max3(topB, fabsf(y.x), fabsf(y.y));
-                }
-            // 2^e <= top < 2^(e + 1): a row goes in as q 2^(8 - e), exact but for what lies 2^32 below its largest number; sums of 32 stay below 2^14
-            const uint32_t eA = min(max(__float_as_uint(quad_max(topA)) >> 23, 1u), 253u), eB = min(max(__float_as_uint(quad_max(topB)) >> 23, 1u), 253u);
-            const float downA = __uint_as_float((254u - eA) << 23), downB = __uint_as_float((254u - eB) << 23);
-            fA = fmaxf(__uint_as_float(eA << 23) * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
-            fB = fmaxf(__uint_as_float(eB << 23) * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
-            uint32_t sums[4] = {0, 0, 0, 0};     // columns 4 w ..: the sum of the row over group w in two parts, twice.  This thread's words c and 4 + c of row A, then of row B
-#pragma unroll
-            for (int u = 0; u < Cfg::SUB; ++u) {
-                float sA[2] = {0.f, 0.f}, sB[2] = {0.f, 0.f};
-#pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    const float2 x = number(raw[u][2 * g]), y = number(raw[u][2 * g + 1]);
-                    const __half2 v = __floats2half2_rn(x.x * downA * 256.f, x.y * downA * 256.f), z = __floats2half2_rn(y.x * downB * 256.f, y.y * downB * 256.f);
-                    raw[u][2 * g] = t_bits(v);
-                    raw[u][2 * g + 1] = t_bits(z);
-                    sA[g >> 2] += __low2float(v) + __high2float(v);
-                    sB[g >> 2] += __low2float(z) + __high2float(z);
-                }
-                tmem_st_quad32(tmem + TM_Q + 32 * u + lanes, raw[u]);
-                auto two = [&](float s) {
-                    s = quad_sum(s);
-                    const __half hi16 = __float2half_rn(s);
-                    return t_bits(__halves2half2(hi16, __float2half_rn(s - __half2float(hi16))));
-                };
-                const uint32_t a0 = two(sA[0]), a1 = two(sA[1]), b0 = two(sB[0]), b1 = two(sB[1]);
-                sums[2 * u] = lane & 2 ? a1 : a0;                // (words 4 u + c: of group 2 u + c / 2)
-                sums[2 * u + 1] = lane & 2 ? b1 : b0;
-            }
-            asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};" ::"r"(tmem + TM_E + lanes), "r"(sums[0]), "r"(sums[1]), "r"(sums[2]), "r"(sums[3]) : "memory");
-            tc_wait_st();
-            tc_fence_before();
-        } else if (warp < SOFT0) {
-            // ---- the tokens' sets of the tree: each its own and its ancestors
-            const int words = (nq + 31) / 32, tok = tok0 + tid;
-            for (int i = tid; i < G * (PSA_TREE_MOST / 32); i += 32 * SOFT0) (&nan_s[0][0])[i] = 0u;
-            if (meets_tree && tok < nq && tok <= (int)fastdiv((uint32_t)(qt * ROWS + ROWS - 1), a.by_group)) {
-                uint32_t* const mine = tree + tid * TREE_WORDS;
-                for (int i = 0; i < words; ++i) mine[i] = 0u;
-                int k = tok;
-                while (k >= 0) {
-                    mine[k >> 5] |= 1u << (k & 31);
-                    const int up = __ldg(a.parents + q0 + k);
-                    if (up < -1 || up >= k) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);         // (no earlier token: taken for the root of a tree of its own)
-                    k = up < k ? up : -1;
-                }
-            }
-        }
-        fence_async_smem();
-        if (__syncthreads_or(abort_flag)) { ok = false; break; }
-        tc_fence_after();
 
-        if (warp == MMA_WARP) {
-            if (lane == 0 && nt > 0) {
-                constexpr uint32_t idescS = t_idesc(KEYS, UMMA_K_MAJOR), idescO = t_idesc(D, UMMA_MN_MAJOR);
-                const uint32_t k1_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K1)), k2_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K2));
-                const uint32_t e_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::E)), v_lo = umma_desc_lo_mnmajor(smem_u32(smem + Cfg::V), 16384);
-                for (int j = 0; j <= nt && ok; ++j) {
-                    const uint32_t n = done + j;
-                    if (j < nt) {
-                        ok = mbar_wait(&bars.k_full, n & 1, abortp);
+    if (warp == MMA_WARP) {
+        if (lane == 0) {
+            constexpr uint32_t idescS = t_idesc(KEYS, UMMA_K_MAJOR), idescO = t_idesc(D, UMMA_MN_MAJOR);
+            const uint32_t k1_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K1)), k2_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K2));
+            const uint32_t e_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::E)), v_lo = umma_desc_lo_mnmajor(smem_u32(smem + Cfg::V), 16384);
+            uint32_t items = 0;                  // that have tiles
+            while (ok && next_item(at, x)) {
+                if (x.nt == 0) continue;
+                ok = mbar_wait(&bars.q_full, items++ & 1, abortp);
+                for (int j = 0; j <= x.nt && ok; ++j) {
+                    const uint32_t m = n + j;
+                    if (j < x.nt) {
+                        ok = mbar_wait(&bars.k_full, m & 1, abortp);
                         if (!ok) break;
                         tc_fence_after();
-                        const uint32_t dS = tmem + TM_S + (n & 1) * KEYS;
+                        const uint32_t dS = tmem + TM_S + (m & 1) * KEYS;
                         // (where P of tile j - 2 was: its product has been issued)
                         umma_ts(dS, tmem + TM_E, umma_desc_join(e_lo, UMMA_DESC_HI_SW128), idescS, 0);
 #pragma unroll
@@ -305,179 +254,292 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                             const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
                             umma_ts(dS, tmem + TM_Q + kk * 8, umma_desc_join(k2_lo + off, UMMA_DESC_HI_SW128), idescS, 1);
                         }
-                        umma_commit(&bars.s_full[n & 1]);
+                        umma_commit(&bars.s_full[m & 1]);
                         umma_commit(&bars.k_empty);
                     }
                     if (j > 0) {
-                        ok = mbar_wait(&bars.v_full, (n - 1) & 1, abortp) && mbar_wait(&bars.p_ready, (n - 1) & 1, abortp);
+                        ok = mbar_wait(&bars.v_full, (m - 1) & 1, abortp) && mbar_wait(&bars.p_ready, (m - 1) & 1, abortp);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll
                         for (int kk = 0; kk < KEYS / 16; ++kk)
-                            umma_ts(tmem + TM_O, tmem + TM_S + ((n - 1) & 1) * KEYS + kk * 8, umma_desc_join(v_lo + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, j > 1 || kk > 0);
+                            umma_ts(tmem + TM_O, tmem + TM_S + ((m - 1) & 1) * KEYS + kk * 8, umma_desc_join(v_lo + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, j > 1 || kk > 0);
                         umma_commit(&bars.o_done);
                     }
                 }
+                n += x.nt;
             }
-        } else if (warp >= TURN0) {
-            // ------------------------------------------------------------ codes into operands: block `me` of every tile
-            const int me = warp - TURN0;
-            uint8_t* const raw_k = smem + Cfg::RAW_K + me * Cfg::HALF;
-            uint8_t* const raw_v = smem + Cfg::RAW_V + me * Cfg::HALF;
-            // lane l: the block's address in tile l of the last 32 (looked up 16 at a time, so that what is still to be asked for of V stays), null where it is not there
-            const uint8_t* addr = nullptr;
-            uint32_t there = 0, asked_k = ring_k, asked_v = ring_v;         // blocks asked for so far
-            auto look_up = [&](int i0) {
-                if ((lane >> 4) == (i0 >> 4 & 1)) {
-                    const int i = i0 + (lane & 15), block = (t0 + i) * TURNS + me;
-                    addr = nullptr;
-                    if (i < nt && (long long)block * CACHE_BLOCK < len) {
-                        const int blocks = (int)a.by_blocks.d, col = (int)fastdiv((uint32_t)block, a.by_blocks);
-                        const int page = a.tables[(size_t)slot * a.width + col];
-                        if (page >= 0 && page < a.pages) addr = a.pool + (((size_t)page * a.kv_heads + h) * blocks + (block - col * blocks)) * B::BYTES;
-                        else atomicExch(&dc->status, (int)PSA_ERR_SHAPE);                       // (no such page: its tokens are left out, and the call reports it)
-                    }
-                }
-                there = __ballot_sync(0xffffffffu, addr != nullptr);
+        }
+    } else if (warp == K_WARP || warp == V_WARP) {
+        // ------------------------------------------------------------ codes of K, and of V, into their rings: a block of 16 tokens a lane, four tiles looked up at a time, four ahead of their use
+        const bool is_k = warp == K_WARP;
+        const int stages = is_k ? Cfg::K_RING : Cfg::V_RING;
+        uint64_t *const full = is_k ? bars.k_raw : bars.v_raw, *const empty = is_k ? bars.k_raw_free : bars.v_raw_free;
+        uint8_t* const ring = smem + (is_k ? Cfg::RAW_K : Cfg::RAW_V);
+        const int blocks = (int)a.by_blocks.d;
+        while (ok && next_item(at, x)) {
+            auto look_up = [&](int i0) -> const uint8_t* {
+                const int i = i0 + (lane >> 3);
+                const long long block = (long long)(x.t0 + i) * TURNS + (lane & 7);
+                if (i >= x.nt || block * CACHE_BLOCK >= x.len) return nullptr;
+                const int col = (int)fastdiv((uint32_t)block, a.by_blocks), page = a.tables[(size_t)x.slot * a.width + col];
+                if (page >= 0 && page < a.pages) return a.pool + (((size_t)page * a.kv_heads + x.h) * blocks + ((int)block - col * blocks)) * B::BYTES + (is_k ? 0 : Cfg::HALF);
+                atomicExch(&dc->status, (int)PSA_ERR_SHAPE);             // (no such page: its tokens are left out, and the call reports it)
+                return nullptr;
             };
-            // K of tile i is asked for ahead of V of tile i
-            auto load = [&](int i, bool is_k) {
-                if (i >= nt) return;
-                if (is_k && (i & 15) == 0) look_up(i);
-                const uint32_t count = is_k ? asked_k++ : asked_v++;
-                uint64_t* const bar = is_k ? &bars.raw_k[me][count % Cfg::K_RING] : &bars.raw_v[me][count % Cfg::V_RING];
-                if (lane == (i & 31)) {
-                    if (addr) {
-                        mbar_arrive_expect_tx(bar, Cfg::HALF);
-                        if (is_k) bulk_load_1d(raw_k + (count % Cfg::K_RING) * (TURNS * Cfg::HALF), addr, Cfg::HALF, bar);
-                        else bulk_load_1d(raw_v + (count % Cfg::V_RING) * (TURNS * Cfg::HALF), addr + Cfg::HALF, Cfg::HALF, bar);
+            const uint8_t *from = look_up(0), *ahead = nullptr;
+            for (int i = 0; i < x.nt; ++i, ++n) {
+                if ((i & 3) == 0) {
+                    if (i > 0) from = ahead;
+                    ahead = look_up(i + 4);
+                }
+                const int s = n % stages;
+                if (n >= (uint32_t)stages) ok = __all_sync(0xffffffffu, mbar_wait(&empty[s], (n / stages - 1) & 1, abortp));
+                if (!ok) break;
+                if ((lane >> 3) == (i & 3)) {
+                    if (is_k) have_s[n & 7][lane & 7] = from != nullptr;
+                    if (from) {
+                        mbar_arrive_expect_tx(&full[s], Cfg::HALF);
+                        bulk_load_1d(ring + (s * TURNS + (lane & 7)) * Cfg::HALF, from, Cfg::HALF, &full[s]);
                     } else {
-                        mbar_arrive(bar);
+                        mbar_arrive(&full[s]);
                     }
                 }
                 __syncwarp();
-            };
-            auto is_there = [&](int i) { return (there >> (i & 31) & 1u) != 0; };
-            for (int i = 0; i < Cfg::V_RING; ++i) {
-                if (i < Cfg::K_RING) load(i, true);
-                load(i, false);
             }
-            const CacheOnes ones;
-            auto turn_k = [&](int i) {
-                const uint32_t n = done + i, c = ring_k;
-                ok = __all_sync(0xffffffffu, mbar_wait(&bars.raw_k[me][c % Cfg::K_RING], (c / Cfg::K_RING) & 1, abortp));
-                ring_k += ok;
-                if (ok && n > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_empty, (n - 1) & 1, abortp));
-                if (!ok) return;
-                const bool have = is_there(i);
-                if (lane == 0) have_s[n & 3][me] = have;
-                if (have) {
-                    const uint8_t* const from = raw_k + (c % Cfg::K_RING) * (TURNS * Cfg::HALF);
-#pragma unroll
-                    for (int x = 0; x < 2 * G; ++x) {            // 16 tokens of 4 G words of eight channels, chunk by chunk of 16 bytes
-                        const int e = x * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), w = chunk >> 2, r = me * CACHE_BLOCK + tok;
-                        const uint32_t codes = *reinterpret_cast<const uint32_t*>(from + tok * (D / 2) + ((chunk & 3) * G + w) * 4);
-                        const uint32_t sm = *reinterpret_cast<const uint32_t*>(from + B::K_SCALES + (tok * G + w) * 4);
-                        const uint32_t S = __byte_perm(sm, sm, 0x1010), S1 = S & 0xfff0fff0u, S2 = t_bits(__hsub2(t_h2(S), t_h2(S1)));
-                        const __half2 s1 = t_h2(S1), s2 = t_h2(S2), m1 = __hneg2(s1), m2 = __hneg2(s2);
-                        uint32_t y1[4], y2[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const __half2 one = t_h2(ones(codes, k));
-                            y1[k] = t_bits(__hfma2(one, s1, m1));
-                            y2[k] = t_bits(__hfma2(one, s2, m2));
-                        }
-                        const uint32_t to = (chunk >> 3) * 16384 + swz128_offset(r, chunk & 7);
-                        *reinterpret_cast<uint4*>(smem + Cfg::K1 + to) = make_uint4(y1[0], y1[1], y1[2], y1[3]);
-                        *reinterpret_cast<uint4*>(smem + Cfg::K2 + to) = make_uint4(y2[0], y2[1], y2[2], y2[3]);
-                        if ((chunk & 3) == 0) *reinterpret_cast<uint2*>(smem + Cfg::E + swz128_offset(r, w >> 1) + 8 * (w & 1)) = make_uint2(__byte_perm(sm, sm, 0x3232), S);
+        }
+        if (!ok)                                 // copies already asked for land before shared memory is released
+            for (uint32_t m = n > (uint32_t)stages ? n - stages : 0; m < n; ++m) mbar_wait_drain(&full[m % stages], (m / stages) & 1);
+    } else if (warp == SET_WARP) {
+        // ------------------------------------------------------------ the tokens' sets of the tree: each its own and its ancestors
+        for (uint32_t it = 0; ok && next_item(at, x); ++it) {
+            if (it > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_free, (it - 1) & 1, abortp));
+            if (!ok) break;
+            for (int i = lane; i < G * (PSA_TREE_MOST / 32); i += 32) (&nan_s[it & 1][0][0])[i] = 0u;
+            if (x.meets_tree) {
+                const int words = (x.nq + 31) / 32, last = min((int)fastdiv((uint32_t)(x.qt * ROWS + ROWS - 1), a.by_group), x.nq - 1);
+                for (int tok = x.tok0 + lane; tok <= last; tok += 32) {
+                    uint32_t* const mine = tree + (tok - x.tok0) * TREE_WORDS;
+                    for (int i = 0; i < words; ++i) mine[i] = 0u;
+                    int k = tok;
+                    while (k >= 0) {
+                        mine[k >> 5] |= 1u << (k & 31);
+                        const int up = __ldg(a.parents + x.q0 + k);
+                        if (up < -1 || up >= k) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);         // (no earlier token: taken for the root of a tree of its own)
+                        k = up < k ? up : -1;
                     }
                 }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.k_full);
-                load(i + Cfg::K_RING, true);
-            };
-            auto turn_v = [&](int i) {
-                const uint32_t n = done + i, c = ring_v;
-                ok = __all_sync(0xffffffffu, mbar_wait(&bars.raw_v[me][c % Cfg::V_RING], (c / Cfg::V_RING) & 1, abortp));
-                ring_v += ok;
-                if (ok && n > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (n - 1) & 1, abortp));
-                if (!ok) return;
-                const bool have = is_there(i);
-                const int first = (t0 + i) * KEYS + me * CACHE_BLOCK;        // the block's first token
-                const uint8_t* const from = raw_v + (c % Cfg::V_RING) * (TURNS * Cfg::HALF);
-                const bool looks = first + CACHE_BLOCK > ctx;                // has tokens that not all rows see, or that are none of the sequence's
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.sets_full);
+        }
+    } else if (warp >= TURN0) {
+        // ------------------------------------------------------------ codes into operands: block `me` of every tile.  K of a tile is worked on ahead of V of the one before, also from item to item.
+        const int me = warp - TURN0;
+        const CacheOnes ones;
+        auto turn_k = [&](uint32_t m) {
+            const int s = m % Cfg::K_RING;
+            ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_raw[s], (m / Cfg::K_RING) & 1, abortp));
+            const bool have = have_s[m & 7][me] != 0;
+            // 16 tokens of 4 G words of eight channels, chunk by chunk of 16 bytes.  (All are read ahead of the first store: the compiler cannot know that they lie apart.)
+            const uint8_t* const from = smem + Cfg::RAW_K + (s * TURNS + me) * Cfg::HALF;
+            uint32_t codes[2 * G], sm[2 * G];
 #pragma unroll
-                for (int x = 0; x < G; ++x) {    // 8 pairs of tokens of 4 G chunks of eight channels
-                    const int e = x * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), w = chunk >> 2, g = 2 * (chunk & 3), r = me * CACHE_BLOCK + 2 * pair;
-                    uint4 even = make_uint4(0, 0, 0, 0), odd = even;
-                    if (have) {
-                        const uint32_t c0 = *reinterpret_cast<const uint32_t*>(from + pair * D + (g * G + w) * 4), c1 = *reinterpret_cast<const uint32_t*>(from + pair * D + ((g + 1) * G + w) * 4);
-                        uint2 sm = *reinterpret_cast<const uint2*>(from + (B::V_SCALES - B::V_CODES) + (pair * G + w) * 8);
-                        if (looks) {
-                            // Behind the sequence's end lies whatever the page held before, and a weight of zero does not keep a NaN out of the sum: such tokens, and groups of the tree's that
-                            // are not finite, go in as zeros; rows that see these get a NaN at the end.
-                            const int t = first + 2 * pair;
-                            const uint32_t keep = (t < len ? 0xffffu : 0u) | (t + 1 < len ? 0xffff0000u : 0u);
-                            sm.x &= keep;
-                            sm.y &= keep;
-                            uint32_t bad = (((sm.x & 0x7c007c00u) + 0x04000400u) | ((sm.y & 0x7c007c00u) + 0x04000400u)) & 0x80008000u;      // an exponent of all ones
-                            if (t < ctx) bad &= 0x80000000u;
-                            if (t + 1 < ctx) bad = 0;
-                            if (bad) {
-                                const uint32_t drop = (bad >> 15) * 0xffffu;
-                                sm.x &= ~drop;
-                                sm.y &= ~drop;
-                                if ((bad & 0x8000u) && t >= ctx && t - ctx < nq) atomicOr(&nan_s[w][(t - ctx) >> 5], 1u << ((t - ctx) & 31));
-                                if ((bad & 0x80000000u) && t + 1 - ctx < nq) atomicOr(&nan_s[w][(t + 1 - ctx) >> 5], 1u << ((t + 1 - ctx) & 31));
-                            }
-                        }
-                        const __half2 S = t_h2(sm.x), M = t_h2(sm.y);
-                        uint32_t v[8];           // channels 8 (chunk) + k: of the even token in the lower half, of the odd one in the upper
+            for (int i = 0; i < 2 * G; ++i) {
+                const int e = i * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), w = chunk >> 2;
+                codes[i] = *reinterpret_cast<const uint32_t*>(from + tok * (D / 2) + ((chunk & 3) * G + w) * 4);
+                sm[i] = *reinterpret_cast<const uint32_t*>(from + B::K_SCALES + (tok * G + w) * 4);
+            }
+            if (ok && m > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_empty, (m - 1) & 1, abortp));
+            if (!ok) return;
+            if (have) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            v[k] = t_bits(__hfma2(t_h2(ones(c0, k)), S, M));
-                            v[4 + k] = t_bits(__hfma2(t_h2(ones(c1, k)), S, M));
-                        }
-                        even = make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[4], v[5], 0x5410), __byte_perm(v[6], v[7], 0x5410));
-                        odd = make_uint4(__byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632), __byte_perm(v[4], v[5], 0x7632), __byte_perm(v[6], v[7], 0x7632));
+                for (int i = 0; i < 2 * G; ++i) {
+                    const int e = i * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), w = chunk >> 2, r = me * CACHE_BLOCK + tok;
+                    const uint32_t S = __byte_perm(sm[i], sm[i], 0x1010), S1 = S & 0xfff0fff0u, S2 = t_bits(__hsub2(t_h2(S), t_h2(S1)));
+                    const __half2 s1 = t_h2(S1), s2 = t_h2(S2), m1 = __hneg2(s1), m2 = __hneg2(s2);
+                    uint32_t y1[4], y2[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const __half2 one = t_h2(ones(codes[i], k));
+                        y1[k] = t_bits(__hfma2(one, s1, m1));
+                        y2[k] = t_bits(__hfma2(one, s2, m2));
                     }
-                    uint8_t* const to = smem + Cfg::V + (chunk >> 3) * 16384;
-                    *reinterpret_cast<uint4*>(to + swz128_offset(r, chunk & 7)) = even;
-                    *reinterpret_cast<uint4*>(to + swz128_offset(r + 1, chunk & 7)) = odd;
+                    const uint32_t to = (chunk >> 3) * 16384 + swz128_offset(r, chunk & 7);
+                    *reinterpret_cast<uint4*>(smem + Cfg::K1 + to) = make_uint4(y1[0], y1[1], y1[2], y1[3]);
+                    *reinterpret_cast<uint4*>(smem + Cfg::K2 + to) = make_uint4(y2[0], y2[1], y2[2], y2[3]);
+                    if ((chunk & 3) == 0) *reinterpret_cast<uint2*>(smem + Cfg::E + swz128_offset(r, w >> 1) + 8 * (w & 1)) = make_uint2(__byte_perm(sm[i], sm[i], 0x3232), S);
                 }
-                fence_async_smem();
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(&bars.k_full); mbar_arrive(&bars.k_raw_free[s]); }
+        };
+        // first: the block's first token; ctx, len, nq and nan of its item
+        auto turn_v = [&](uint32_t m, long long first, int ctx, int len, int nq, uint32_t (*nan)[PSA_TREE_MOST / 32]) {
+            const int s = m % Cfg::V_RING;
+            ok = __all_sync(0xffffffffu, mbar_wait(&bars.v_raw[s], (m / Cfg::V_RING) & 1, abortp));
+            const bool have = have_s[m & 7][me] != 0;
+            // 8 pairs of tokens of 4 G chunks of eight channels
+            const uint8_t* const from = smem + Cfg::RAW_V + (s * TURNS + me) * Cfg::HALF;
+            uint32_t c0[G], c1[G];
+            uint2 sm[G];
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const int e = i * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), w = chunk >> 2, g = 2 * (chunk & 3);
+                c0[i] = *reinterpret_cast<const uint32_t*>(from + pair * D + (g * G + w) * 4);
+                c1[i] = *reinterpret_cast<const uint32_t*>(from + pair * D + ((g + 1) * G + w) * 4);
+                sm[i] = *reinterpret_cast<const uint2*>(from + (B::V_SCALES - B::V_CODES) + (pair * G + w) * 8);
+            }
+            if (first + CACHE_BLOCK > ctx || !have) {
+                // The block has tokens that not all rows see, or that are none of the sequence's.  Behind the sequence's end lies whatever the page held before, and a weight of zero does not keep a NaN out
+                // of the sum: such tokens, and groups of the tree's that are not finite, go in as zeros; rows that see these get a NaN at the end.
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    const int e = i * 32 + lane, pair = e / (4 * G), w = (e - pair * (4 * G)) >> 2;
+                    const long long t = first + 2 * pair;
+                    const uint32_t keep = have ? (t < len ? 0xffffu : 0u) | (t + 1 < len ? 0xffff0000u : 0u) : 0u;
+                    sm[i].x &= keep;
+                    sm[i].y &= keep;
+                    uint32_t bad = (((sm[i].x & 0x7c007c00u) + 0x04000400u) | ((sm[i].y & 0x7c007c00u) + 0x04000400u)) & 0x80008000u;      // an exponent of all ones
+                    if (t < ctx) bad &= 0x80000000u;
+                    if (t + 1 < ctx) bad = 0;
+                    if (bad) {
+                        const uint32_t drop = (bad >> 15) * 0xffffu;
+                        sm[i].x &= ~drop;
+                        sm[i].y &= ~drop;
+                        const int at0 = (int)(t - ctx);
+                        if ((bad & 0x8000u) && at0 < nq) atomicOr(&nan[w][at0 >> 5], 1u << (at0 & 31));
+                        if ((bad & 0x80000000u) && at0 + 1 < nq) atomicOr(&nan[w][(at0 + 1) >> 5], 1u << ((at0 + 1) & 31));
+                    }
+                }
+            }
+            if (ok && m > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (m - 1) & 1, abortp));
+            if (!ok) return;
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const int e = i * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), r = me * CACHE_BLOCK + 2 * pair;
+                const __half2 S = t_h2(sm[i].x), M = t_h2(sm[i].y);
+                uint32_t v[8];                   // channels 8 (chunk) + k: of the even token in the lower half, of the odd one in the upper
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    v[k] = t_bits(__hfma2(t_h2(ones(c0[i], k)), S, M));
+                    v[4 + k] = t_bits(__hfma2(t_h2(ones(c1[i], k)), S, M));
+                }
+                uint8_t* const to = smem + Cfg::V + (chunk >> 3) * 16384;
+                *reinterpret_cast<uint4*>(to + swz128_offset(r, chunk & 7)) =
+                    make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[4], v[5], 0x5410), __byte_perm(v[6], v[7], 0x5410));
+                *reinterpret_cast<uint4*>(to + swz128_offset(r + 1, chunk & 7)) =
+                    make_uint4(__byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632), __byte_perm(v[4], v[5], 0x7632), __byte_perm(v[6], v[7], 0x7632));
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(&bars.v_full); mbar_arrive(&bars.v_raw_free[s]); }
+        };
+        // the tile before the present one: what its V needs
+        long long first = 0;
+        int ctx = 0, len = 0, nq = 0;
+        uint32_t it = 0, its = 0;
+        auto turn_last_v = [&] {
+            if (first + KEYS > ctx) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_full, its & 1, abortp));       // (the item's marks of NaN are clear)
+            if (ok) turn_v(n - 1, first + me * CACHE_BLOCK, ctx, len, nq, nan_s[its & 1]);
+        };
+        for (; ok && next_item(at, x); ++it)
+            for (int i = 0; i < x.nt && ok; ++i) {
+                turn_k(n);
+                if (ok && n > 0) turn_last_v();
+                if (!ok) break;
+                ++n;
+                first = (long long)(x.t0 + i) * KEYS;
+                ctx = x.ctx;
+                len = x.len;
+                nq = x.nq;
+                its = it;
+            }
+        if (ok && n > 0) turn_last_v();
+    } else {
+        // ------------------------------------------------------------ softmax: 16 rows a warp, in the quad layout
+        const int sw = warp - SOFT0, r0 = (warp & 3) * 32 + (sw >> 2) * 16, rA = r0 + (lane >> 2), rB = rA + 8, cq = 2 * (lane & 3);
+        const uint32_t lanes = (uint32_t)r0 << 16, tO = tmem + TM_O + lanes;
+        for (uint32_t it = 0; ok && next_item(at, x); ++it) {
+            const int rhoA = x.qt * ROWS + rA, rhoB = x.qt * ROWS + rB, tokA = (int)fastdiv((uint32_t)rhoA, a.by_group), tokB = (int)fastdiv((uint32_t)rhoB, a.by_group);
+            float fA = 1.f, fB = 1.f;            // factors of the rows' scores, to log2 units
+            if (x.nt > 0) {
+                // ---- the queries into tensor memory: 64 columns of K, 32 words, at a time
+                uint32_t raw[Cfg::SUB][16];          // [2 g]: channels 64 u + 8 g + cq .. of row A, [2 g + 1] of row B
+                float topA = 0.f, topB = 0.f;
+                auto number = [&](uint32_t w) { return a.f16 ? __half22float2(t_h2(w)) : make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); };
+                auto from = [&](int token, int rho) { return a.q + (size_t)(x.q0 + token) * a.q_stride + ((size_t)x.h * a.group + (rho - token * a.group)) * D + cq; };
+                const uint16_t *const qA = from(tokA, rhoA), *const qB = from(tokB, rhoB);
+#pragma unroll
+                for (int u = 0; u < Cfg::SUB; ++u)
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const bool is = 64 * u + 8 * g < D;
+                        raw[u][2 * g] = is && tokA < x.nq ? *reinterpret_cast<const uint32_t*>(qA + 64 * u + 8 * g) : 0u;
+                        raw[u][2 * g + 1] = is && tokB < x.nq ? *reinterpret_cast<const uint32_t*>(qB + 64 * u + 8 * g) : 0u;
+                    }
+#pragma unroll
+                for (int u = 0; u < Cfg::SUB; ++u)
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const float2 v0 = number(raw[u][2 * g]), v1 = number(raw[u][2 * g + 1]);
+                        topA = max3(topA, fabsf(v0.x), fabsf(v0.y));
+                        topB = max3(topB, fabsf(v1.x), fabsf(v1.y));
+                    }
+                // 2^e <= top < 2^(e + 1): a row goes in as q 2^(8 - e), exact but for what lies 2^32 below its largest number; sums of 32 stay below 2^14
+                const uint32_t eA = min(max(__float_as_uint(quad_max(topA)) >> 23, 1u), 253u), eB = min(max(__float_as_uint(quad_max(topB)) >> 23, 1u), 253u);
+                const float downA = __uint_as_float((254u - eA) << 23), downB = __uint_as_float((254u - eB) << 23);
+                fA = fmaxf(__uint_as_float(eA << 23) * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
+                fB = fmaxf(__uint_as_float(eB << 23) * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
+                uint32_t sums[4] = {0, 0, 0, 0};     // columns 4 w ..: the sum of the row over group w in two parts, twice.  This thread's words c and 4 + c of row A, then of row B
+#pragma unroll
+                for (int u = 0; u < Cfg::SUB; ++u) {
+                    float sA[2] = {0.f, 0.f}, sB[2] = {0.f, 0.f};
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const float2 v0 = number(raw[u][2 * g]), v1 = number(raw[u][2 * g + 1]);
+                        const __half2 v = __floats2half2_rn(v0.x * downA * 256.f, v0.y * downA * 256.f), z = __floats2half2_rn(v1.x * downB * 256.f, v1.y * downB * 256.f);
+                        raw[u][2 * g] = t_bits(v);
+                        raw[u][2 * g + 1] = t_bits(z);
+                        sA[g >> 2] += __low2float(v) + __high2float(v);
+                        sB[g >> 2] += __low2float(z) + __high2float(z);
+                    }
+                    tmem_st_quad32(tmem + TM_Q + 32 * u + lanes, raw[u]);
+                    auto two = [&](float s) {
+                        s = quad_sum(s);
+                        const __half hi16 = __float2half_rn(s);
+                        return t_bits(__halves2half2(hi16, __float2half_rn(s - __half2float(hi16))));
+                    };
+                    const uint32_t a0 = two(sA[0]), a1 = two(sA[1]), b0 = two(sB[0]), b1 = two(sB[1]);
+                    sums[2 * u] = lane & 2 ? a1 : a0;                // (words 4 u + c: of group 2 u + c / 2)
+                    sums[2 * u + 1] = lane & 2 ? b1 : b0;
+                }
+                asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};" ::"r"(tmem + TM_E + lanes), "r"(sums[0]), "r"(sums[1]), "r"(sums[2]), "r"(sums[3]) : "memory");
+                tc_wait_st();
+                tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.v_full);
-                load(i + Cfg::V_RING, false);
-            };
-            static_assert(Cfg::K_RING <= Cfg::V_RING && Cfg::V_RING <= Cfg::K_RING + 1, "V of a tile is asked for behind K of it, and its address is kept for 16 tiles");
-            if (nt > 0) turn_k(0);
-            for (int i = 0; i < nt && ok; ++i) {
-                if (i + 1 < nt) turn_k(i + 1);
-                if (ok) turn_v(i);
+                if (lane == 0) mbar_arrive(&bars.q_full);
             }
-            if (!ok) {                           // copies already asked for land before shared memory is released
-                for (; ring_k != asked_k; ++ring_k) mbar_wait_drain(&bars.raw_k[me][ring_k % Cfg::K_RING], (ring_k / Cfg::K_RING) & 1);
-                for (; ring_v != asked_v; ++ring_v) mbar_wait_drain(&bars.raw_v[me][ring_v % Cfg::V_RING], (ring_v / Cfg::V_RING) & 1);
-            }
-        } else if (warp >= SOFT0) {
-            // ------------------------------------------------------------ softmax: 16 rows a warp, in the quad layout
-            const uint32_t tO = tmem + TM_O + lanes;
-            const uint32_t* const setA = tree + (min(tokA, nq - 1) - tok0) * TREE_WORDS;
-            const uint32_t* const setB = tree + (min(tokB, nq - 1) - tok0) * TREE_WORDS;
-            const int words = (nq + 31) / 32;
+            const uint32_t* const setA = tree + (min(tokA, x.nq - 1) - x.tok0) * TREE_WORDS;
+            const uint32_t* const setB = tree + (min(tokB, x.nq - 1) - x.tok0) * TREE_WORDS;
+            const int words = (x.nq + 31) / 32;
+            bool sets = false;                   // they are known to be there
             float mA = -INFINITY, mB = -INFINITY, lA = 0.f, lB = 0.f;
-            for (int j = 0; j < nt && ok; ++j) {
-                const uint32_t n = done + j;
-                ok = __all_sync(0xffffffffu, mbar_wait(&bars.s_full[n & 1], (n >> 1) & 1, abortp));
+            for (int j = 0; j < x.nt && ok; ++j) {
+                const uint32_t m = n + j;
+                ok = __all_sync(0xffffffffu, mbar_wait(&bars.s_full[m & 1], (m >> 1) & 1, abortp));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t tS = tmem + TM_S + (n & 1) * KEYS + lanes;
-                const unsigned long long have = *reinterpret_cast<const unsigned long long*>(have_s[n & 3]);
-                const int key0 = (t0 + j) * KEYS;
-                const bool masked = key0 + KEYS > ctx || have != 0x0101010101010101ull;
+                const uint32_t tS = tmem + TM_S + (m & 1) * KEYS + lanes;
+                const unsigned long long have = *reinterpret_cast<const unsigned long long*>(have_s[m & 7]);
+                const long long key0 = (long long)(x.t0 + j) * KEYS;
+                const bool masked = key0 + KEYS > x.ctx || have != 0x0101010101010101ull;
+                if (masked && x.meets_tree && !sets) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_full, it & 1, abortp));
+                    if (!ok) break;
+                    sets = true;
+                }
                 // 64 columns of the scores (read twice, for the maximum and for the weights: held in between they would not fit the registers)
                 auto scores = [&](uint32_t (&s)[32], int half) {
                     tmem_ld_quad64(tS + 64 * half, s);
@@ -485,9 +547,9 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                     if (!masked) return;
                     // the tile's tokens that a row sees, 32 a word: all ahead of the tree, and the row's set in it; none of blocks that are not there
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int at32 = key0 + 64 * half + 32 * x - ctx, word = at32 >> 5;
-                        const uint32_t both = ((have >> (16 * (2 * half + x)) & 1) ? 0xffffu : 0u) | ((have >> (16 * (2 * half + x) + 8) & 1) ? 0xffff0000u : 0u);
+                    for (int z = 0; z < 2; ++z) {
+                        const int at32 = (int)(key0 + 64 * half + 32 * z - x.ctx), word = at32 >> 5;
+                        const uint32_t both = ((have >> (16 * (2 * half + z)) & 1) ? 0xffffu : 0u) | ((have >> (16 * (2 * half + z) + 8) & 1) ? 0xffff0000u : 0u);
                         auto seen = [&](const uint32_t* set) {
                             const uint32_t l = word < 0 ? 0xffffffffu : word < words ? set[word] : 0u, u = word + 1 < 0 ? 0xffffffffu : word + 1 < words ? set[word + 1] : 0u;
                             return (__funnelshift_r(l, u, at32) & both) >> cq;
@@ -495,7 +557,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                         const uint32_t A = seen(setA), Bm = seen(setB);
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
-                            uint32_t* const v = s + 16 * x + 4 * g;
+                            uint32_t* const v = s + 16 * z + 4 * g;
                             if (!(A >> (8 * g) & 1u)) v[0] = 0xff800000u;
                             if (!(A >> (8 * g + 1) & 1u)) v[1] = 0xff800000u;
                             if (!(Bm >> (8 * g) & 1u)) v[2] = 0xff800000u;
@@ -521,8 +583,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 auto weights = [&](uint32_t (&p)[16]) {
 #pragma unroll
                     for (int g = 0; g < 8; ++g) {
-                        const float2 x = t_pair(t_fma2(t_pair(__uint_as_float(s[4 * g]), __uint_as_float(s[4 * g + 1])), fA2, nA2)), y = t_pair(t_fma2(t_pair(__uint_as_float(s[4 * g + 2]), __uint_as_float(s[4 * g + 3])), fB2, nB2));
-                        const float x0 = ex2_mufu(x.x), x1 = ex2_mufu(x.y), y0 = ex2_mufu(y.x), y1 = ex2_mufu(y.y);
+                        const float2 v0 = t_pair(t_fma2(t_pair(__uint_as_float(s[4 * g]), __uint_as_float(s[4 * g + 1])), fA2, nA2)), v1 = t_pair(t_fma2(t_pair(__uint_as_float(s[4 * g + 2]), __uint_as_float(s[4 * g + 3])), fB2, nB2));
+                        const float x0 = ex2_mufu(v0.x), x1 = ex2_mufu(v0.y), y0 = ex2_mufu(v1.x), y1 = ex2_mufu(v1.y);
                         sumA = t_add2(sumA, t_pair(x0, x1));
                         sumB = t_add2(sumB, t_pair(y0, y1));
                         p[2 * g] = t_weights(x0, x1);
@@ -535,7 +597,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 lA = fmaf(lA, alphaA, t_pair(sumA).x + t_pair(sumA).y);
                 lB = fmaf(lB, alphaB, t_pair(sumB).x + t_pair(sumB).y);
                 if (j > 0) {                     // O is in use by the product before this one
-                    ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (n - 1) & 1, abortp));
+                    ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (m - 1) & 1, abortp));
                     if (!ok) break;
                     tc_fence_after();
                     if (__any_sync(0xffffffffu, alphaA != 1.f || alphaB != 1.f)) {
@@ -562,66 +624,68 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars.p_ready);
             }
-            if (ok && nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (done + nt - 1) & 1, abortp));
-            if (ok) {
-                // ---- the rows' results
-                tc_fence_after();
-                lA = quad_sum(lA);
-                lB = quad_sum(lB);
-                const bool whole = parts == 1, isA = tokA < nq, isB = tokB < nq;
-                float* const to = whole ? nullptr : part_at(a.part, first_cta, part, D);
-                const size_t outA = ((size_t)(q0 + tokA) * a.kv_heads * a.group + (size_t)h * a.group + (rhoA - tokA * a.group)), outB = ((size_t)(q0 + tokB) * a.kv_heads * a.group + (size_t)h * a.group + (rhoB - tokB * a.group));
-                const float iA = lA == 0.f ? 0.f : 1.f / lA, iB = lB == 0.f ? 0.f : 1.f / lB;
-                uint32_t nanA = 0, nanB = 0;     // groups of V in which the row sees a NaN
-                if (nt > 0 && meets_tree)
-                    for (int i = lane & 3; i < words; i += 4)
+            if (ok && x.nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (n + x.nt - 1) & 1, abortp));
+            if (ok && x.meets_tree && !sets) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_full, it & 1, abortp));
+            if (!ok) break;
+            // ---- the rows' results
+            tc_fence_after();
+            lA = quad_sum(lA);
+            lB = quad_sum(lB);
+            const bool whole = x.parts == 1, isA = tokA < x.nq, isB = tokB < x.nq;
+            float* const to = whole ? nullptr : part_at(a.part, x.first_cta, x.part, D);
+            const size_t outA = ((size_t)(x.q0 + tokA) * a.kv_heads * a.group + (size_t)x.h * a.group + (rhoA - tokA * a.group)), outB = ((size_t)(x.q0 + tokB) * a.kv_heads * a.group + (size_t)x.h * a.group + (rhoB - tokB * a.group));
+            const float iA = lA == 0.f ? 0.f : 1.f / lA, iB = lB == 0.f ? 0.f : 1.f / lB;
+            uint32_t nanA = 0, nanB = 0;     // groups of V in which the row sees a NaN
+            if (x.meets_tree)
+                for (int i = lane & 3; i < words; i += 4)
 #pragma unroll
-                        for (int w = 0; w < G; ++w) {
-                            if (nan_s[w][i] & setA[i]) nanA |= 1u << w;
-                            if (nan_s[w][i] & setB[i]) nanB |= 1u << w;
-                        }
-                nanA |= __shfl_xor_sync(0xffffffffu, nanA, 1); nanA |= __shfl_xor_sync(0xffffffffu, nanA, 2);
-                nanB |= __shfl_xor_sync(0xffffffffu, nanB, 1); nanB |= __shfl_xor_sync(0xffffffffu, nanB, 2);
+                    for (int w = 0; w < G; ++w) {
+                        if (nan_s[it & 1][w][i] & setA[i]) nanA |= 1u << w;
+                        if (nan_s[it & 1][w][i] & setB[i]) nanB |= 1u << w;
+                    }
+            nanA |= __shfl_xor_sync(0xffffffffu, nanA, 1); nanA |= __shfl_xor_sync(0xffffffffu, nanA, 2);
+            nanB |= __shfl_xor_sync(0xffffffffu, nanB, 1); nanB |= __shfl_xor_sync(0xffffffffu, nanB, 2);
 #pragma unroll 1
-                for (int c = 0; c < Cfg::SUB; ++c) {
-                    uint32_t v[32];
+            for (int c = 0; c < Cfg::SUB; ++c) {
+                uint32_t v[32];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = 0u;
-                    if (nt > 0) {
-                        tmem_ld_quad64(tO + 64 * c, v);
-                        tc_wait_ld();
-                    }
+                for (int i = 0; i < 32; ++i) v[i] = 0u;
+                if (x.nt > 0) {
+                    tmem_ld_quad64(tO + 64 * c, v);
+                    tc_wait_ld();
+                }
 #pragma unroll
-                    for (int g = 0; g < 8; ++g) {
-                        const int col = 64 * c + 8 * g + cq;
-                        if (D < Cfg::DT && col >= D) continue;
-                        float x0 = __uint_as_float(v[4 * g]), x1 = __uint_as_float(v[4 * g + 1]), y0 = __uint_as_float(v[4 * g + 2]), y1 = __uint_as_float(v[4 * g + 3]);
-                        if (nanA >> (col >> 5) & 1u) x0 = x1 = NAN;
-                        if (nanB >> (col >> 5) & 1u) y0 = y1 = NAN;
-                        if (whole) {
-                            auto both = [&](float x, float y) { return a.f16 ? t_bits(__floats2half2_rn(x, y)) : pack_bf16x2(x, y); };
-                            if (isA) *reinterpret_cast<uint32_t*>(a.out + outA * D + col) = both(x0 * iA, x1 * iA);
-                            if (isB) *reinterpret_cast<uint32_t*>(a.out + outB * D + col) = both(y0 * iB, y1 * iB);
-                        } else {
-                            if (isA) __stcg(reinterpret_cast<float2*>(to + rA * D + col), make_float2(x0, x1));
-                            if (isB) __stcg(reinterpret_cast<float2*>(to + rB * D + col), make_float2(y0, y1));
-                        }
+                for (int g = 0; g < 8; ++g) {
+                    const int col = 64 * c + 8 * g + cq;
+                    if (D < Cfg::DT && col >= D) continue;
+                    float x0 = __uint_as_float(v[4 * g]), x1 = __uint_as_float(v[4 * g + 1]), y0 = __uint_as_float(v[4 * g + 2]), y1 = __uint_as_float(v[4 * g + 3]);
+                    if (nanA >> (col >> 5) & 1u) x0 = x1 = NAN;
+                    if (nanB >> (col >> 5) & 1u) y0 = y1 = NAN;
+                    if (whole) {
+                        auto both = [&](float u, float w) { return a.f16 ? t_bits(__floats2half2_rn(u, w)) : pack_bf16x2(u, w); };
+                        if (isA) *reinterpret_cast<uint32_t*>(a.out + outA * D + col) = both(x0 * iA, x1 * iA);
+                        if (isB) *reinterpret_cast<uint32_t*>(a.out + outB * D + col) = both(y0 * iB, y1 * iB);
+                    } else {
+                        if (isA) __stcg(reinterpret_cast<float2*>(to + rA * D + col), make_float2(x0, x1));
+                        if (isB) __stcg(reinterpret_cast<float2*>(to + rB * D + col), make_float2(y0, y1));
                     }
                 }
-                if ((lane & 3) == 0) {
-                    auto stats = [&](bool is, int r, size_t out, float m, float l) {
-                        if (!is) return;
-                        if (!whole) { __stcg(to + ROWS * D + r, m); __stcg(to + ROWS * (D + 1) + r, l); }
-                        else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) - UP + log2f(l)) * T_LN2;
-                    };
-                    stats(isA, rA, outA, mA, lA);
-                    stats(isB, rB, outB, mB, lB);
-                }
-                tc_fence_before();
             }
+            if ((lane & 3) == 0) {
+                auto stats = [&](bool is, int r, size_t out, float m, float l) {
+                    if (!is) return;
+                    if (!whole) { __stcg(to + ROWS * D + r, m); __stcg(to + ROWS * (D + 1) + r, l); }
+                    else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) - UP + log2f(l)) * T_LN2;
+                };
+                stats(isA, rA, outA, mA, lA);
+                stats(isB, rB, outB, mB, lB);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.sets_free);
+            if (warp == SOFT0 && lane == 0 && x.part == 0 && x.parts > 1) a.rows_cut[blockIdx.x] = TreeRow{x.parts, x.q0, x.nq, x.h, x.qt};
+            n += x.nt;
         }
-        if (tid == 0 && part == 0 && parts > 1) a.rows_cut[blockIdx.x] = TreeRow{parts, q0, nq, h, qt};
-        done += nt;
     }
     // ---- the end, for all: also of a CTA whose waits ran out
     __syncthreads();
