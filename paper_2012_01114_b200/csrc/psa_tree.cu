@@ -27,8 +27,9 @@ namespace psa {
 
 namespace {
 
-constexpr int ROWS = 128, KEYS = 128;
-constexpr int MMA_WARP = 0, K_WARP = 1, V_WARP = 2, SET_WARP = 3, SOFT0 = 4, SOFTS = 8, TURN0 = SOFT0 + SOFTS, TURNS = 8, T_WARPS = TURN0 + TURNS, T_THREADS = 32 * T_WARPS;
+constexpr int ROWS = 128, KEYS = 128, BLOCKS = KEYS / CACHE_BLOCK;
+constexpr int MMA_WARP = 0, K_WARP = 1, V_WARP = 2, SET_WARP = 3, SOFT0 = 4, SOFTS = 8, TURN_K = SOFT0 + SOFTS, TURN_V = TURN_K + BLOCKS, V_WARPS = BLOCKS / 2, T_WARPS = TURN_V + V_WARPS, T_THREADS = 32 * T_WARPS;
+constexpr int EXACT = 2048;                     // tokens of a sequence up to which keys go in in two parts
 constexpr int T_SEQS = 512;                     // sequences of one launch
 constexpr int T_CTAS = 160;                     // at most
 constexpr int LEAST = 4;                        // tiles of a piece, or what takes as long
@@ -40,13 +41,14 @@ constexpr float T_LN2 = 0.6931471805599453f;
 template <int D>
 struct TCfg {
     static constexpr int DT = D <= 64 ? 64 : 128, SUB = DT / 64, KS = D / 16, G = D / 32;
-    static constexpr int TILE = 128 * DT * 2;   // bytes of an operand tile: sub-tiles of 64 columns, 128-byte rows swizzled
+    static constexpr int SUBTILE = KEYS * 128, TILE = SUB * SUBTILE;         // an operand tile: sub-tiles of 64 columns, 128-byte rows swizzled
     static constexpr int HALF = 10 * D;         // bytes of K, and of V, in a block
-    static constexpr int K_RING = 3, V_RING = 4;
-    static constexpr int K1 = 0, K2 = TILE, V = 2 * TILE, E = 3 * TILE, RAW_K = E + 16384, RAW_V = RAW_K + K_RING * TURNS * HALF, TREE = RAW_V + V_RING * TURNS * HALF;
+    static constexpr int RING = 3;              // tiles of codes
+    // two of each operand, the rings, the sets
+    static constexpr int K = 0, V = K + 2 * TILE, RAW_K = V + 2 * TILE, RAW_V = RAW_K + RING * BLOCKS * HALF, TREE = RAW_V + RING * BLOCKS * HALF;
     static constexpr int SMEM = TREE + ROWS * TREE_WORDS * 4 + 1024;
 };
-constexpr int TM_S = 0, TM_O = 256, TM_Q = 384, TM_E = 448;     // columns of tensor memory: S twice (P over its first half), O, the queries and their sums
+constexpr int TM_S = 0, TM_O = 256, TM_Q = 384;  // columns of tensor memory: S twice (P over its first half), O, the queries
 
 struct TreeArgs {
     const uint8_t* pool;
@@ -68,14 +70,14 @@ struct TreeRow {
 __device__ __forceinline__ float* part_at(float* part, int c, int p, int d) { return part + (size_t)(p == 0 ? 2 * c + 1 : 2 * (c + p)) * ROWS * (d + 2); }
 
 struct TBars {
-    uint64_t k_raw[4], k_raw_free[4], v_raw[4], v_raw_free[4];
-    uint64_t q_full, k_full, k_empty, v_full, o_done, s_full[2], p_ready, sets_full, sets_free;
+    uint64_t k_raw[3], k_raw_free[3], v_raw[3], v_raw_free[3];
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], q_full, sets_full, sets_free;
 };
 // Tiles t0 .. t0 + nt - 1 of row tile qt of head h of a sequence.
 struct TItem {
     int len, nq, q0, slot, t0, nt, h, qt, ctx, tok0;       // ctx: the tree's first token; tok0: the row tile's first
     int first_cta, part, parts;                             // of the row tile; a CTA has one part of it
-    bool meets_tree;
+    bool meets_tree, exact;                                 // exact: keys in two parts
 };
 
 __device__ __forceinline__ uint32_t t_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
@@ -121,26 +123,26 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     __shared__ int abort_flag;
     __shared__ long long base_s[T_SEQS + 1], scan_s[T_WARPS];
     __shared__ int len_s[T_SEQS], q0_s[T_SEQS], nq_s[T_SEQS], slot_s[T_SEQS];
-    __shared__ __align__(8) uint8_t have_s[8][TURNS];            // blocks of a tile that are there, by tile modulo 8
+    __shared__ __align__(8) uint8_t have_s[2][16][BLOCKS];       // blocks of a tile that are there, by tile modulo 16; as the warp found them that fetches V, or K
     __shared__ uint32_t nan_s[2][G][PSA_TREE_MOST / 32];         // by items in turn: tokens of the tree whose group of V reads back as NaN or infinite
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         abort_flag = 0;
-        for (int s = 0; s < 4; ++s) {
-            mbar_init(&bars.k_raw[s], TURNS); mbar_init(&bars.k_raw_free[s], TURNS);
-            mbar_init(&bars.v_raw[s], TURNS); mbar_init(&bars.v_raw_free[s], TURNS);
+        for (int s = 0; s < 3; ++s) {
+            mbar_init(&bars.k_raw[s], BLOCKS); mbar_init(&bars.k_raw_free[s], BLOCKS);
+            mbar_init(&bars.v_raw[s], BLOCKS); mbar_init(&bars.v_raw_free[s], V_WARPS);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&bars.k_full[s], BLOCKS); mbar_init(&bars.k_empty[s], 1);
+            mbar_init(&bars.v_full[s], V_WARPS); mbar_init(&bars.v_empty[s], 1);
+            mbar_init(&bars.s_full[s], 1); mbar_init(&bars.p_ready[s], SOFTS);
         }
         mbar_init(&bars.q_full, SOFTS);
-        mbar_init(&bars.k_full, TURNS); mbar_init(&bars.k_empty, 1);
-        mbar_init(&bars.v_full, TURNS); mbar_init(&bars.o_done, 1);
-        mbar_init(&bars.s_full[0], 1); mbar_init(&bars.s_full[1], 1);
-        mbar_init(&bars.p_ready, SOFTS);
         mbar_init(&bars.sets_full, 1); mbar_init(&bars.sets_free, SOFTS);
         fence_mbar_init();
     }
     if (warp == 1) { tmem_alloc(&tmem_s, 512); tmem_relinquish(); }
-    for (int i = tid; i < 16384 / 16; i += T_THREADS) reinterpret_cast<uint4*>(smem + Cfg::E)[i] = make_uint4(0, 0, 0, 0);       // (columns that no group has stay zero)
     volatile int* const abortp = &abort_flag;
     grid_dependency_wait();
     if (tid == 0 && blockIdx.x == 0 && dc_next) *dc_next = DeviceCounters{0, 0, 0, 0, 0, 0, 0};
@@ -216,6 +218,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             x.first_cta = (int)((row0 + ROW_COST) / per);
             x.parts = (int)((row0 + units - 1) / per) - x.first_cta + 1;
             x.part = (int)blockIdx.x - x.first_cta;
+            x.exact = a.f16 || x.len <= EXACT;
             x.meets_tree = x.nt > 0 && t1 * (long long)KEYS > x.ctx;
             return true;
         }
@@ -227,44 +230,40 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     bool ok = true;
 
     if (warp == MMA_WARP) {
-        if (lane == 0) {
+        if (elect_one()) {
             constexpr uint32_t idescS = t_idesc(KEYS, UMMA_K_MAJOR), idescO = t_idesc(D, UMMA_MN_MAJOR);
-            const uint32_t k1_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K1)), k2_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K2));
-            const uint32_t e_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::E)), v_lo = umma_desc_lo_mnmajor(smem_u32(smem + Cfg::V), 16384);
-            uint32_t items = 0;                  // that have tiles
+            const uint32_t k_lo = umma_desc_lo_kmajor(smem_u32(smem + Cfg::K)), v_lo = umma_desc_lo_mnmajor(smem_u32(smem + Cfg::V), Cfg::SUBTILE);
+            uint32_t items = 0, fills = 0;       // items that have tiles; operands of K
             while (ok && next_item(at, x)) {
                 if (x.nt == 0) continue;
                 ok = mbar_wait(&bars.q_full, items++ & 1, abortp);
                 for (int j = 0; j <= x.nt && ok; ++j) {
                     const uint32_t m = n + j;
                     if (j < x.nt) {
-                        ok = mbar_wait(&bars.k_full, m & 1, abortp);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t dS = tmem + TM_S + (m & 1) * KEYS;
                         // (where P of tile j - 2 was: its product has been issued)
-                        umma_ts(dS, tmem + TM_E, umma_desc_join(e_lo, UMMA_DESC_HI_SW128), idescS, 0);
+                        const uint32_t dS = tmem + TM_S + (m & 1) * KEYS;
+                        for (int part = 0; part <= (int)x.exact; ++part, ++fills) {
+                            const uint32_t s = fills & 1, k = k_lo + s * (Cfg::TILE >> 4);
+                            ok = mbar_wait(&bars.k_full[s], (fills >> 1) & 1, abortp);
+                            if (!ok) break;
+                            tc_fence_after();
 #pragma unroll
-                        for (int kk = 0; kk < Cfg::KS; ++kk) {
-                            const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
-                            umma_ts(dS, tmem + TM_Q + kk * 8, umma_desc_join(k1_lo + off, UMMA_DESC_HI_SW128), idescS, 1);
+                            for (int kk = 0; kk < Cfg::KS; ++kk)
+                                umma_ts(dS, tmem + TM_Q + kk * 8, umma_desc_join(k + (((kk >> 2) * Cfg::SUBTILE + (kk & 3) * 32) >> 4), UMMA_DESC_HI_SW128), idescS, part > 0 || kk > 0);
+                            if (part == (int)x.exact) umma_commit(&bars.s_full[m & 1]);
+                            umma_commit(&bars.k_empty[s]);
                         }
-#pragma unroll
-                        for (int kk = 0; kk < Cfg::KS; ++kk) {
-                            const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
-                            umma_ts(dS, tmem + TM_Q + kk * 8, umma_desc_join(k2_lo + off, UMMA_DESC_HI_SW128), idescS, 1);
-                        }
-                        umma_commit(&bars.s_full[m & 1]);
-                        umma_commit(&bars.k_empty);
+                        if (!ok) break;
                     }
                     if (j > 0) {
-                        ok = mbar_wait(&bars.v_full, (m - 1) & 1, abortp) && mbar_wait(&bars.p_ready, (m - 1) & 1, abortp);
+                        const uint32_t s = (m - 1) & 1;
+                        ok = mbar_wait(&bars.v_full[s], ((m - 1) >> 1) & 1, abortp) && mbar_wait(&bars.p_ready[s], ((m - 1) >> 1) & 1, abortp);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll
                         for (int kk = 0; kk < KEYS / 16; ++kk)
-                            umma_ts(tmem + TM_O, tmem + TM_S + ((m - 1) & 1) * KEYS + kk * 8, umma_desc_join(v_lo + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, j > 1 || kk > 0);
-                        umma_commit(&bars.o_done);
+                            umma_ts(tmem + TM_O, tmem + TM_S + s * KEYS + kk * 8, umma_desc_join(v_lo + s * (Cfg::TILE >> 4) + kk * (2048 >> 4), UMMA_DESC_HI_SW128), idescO, j > 1 || kk > 0);
+                        umma_commit(&bars.v_empty[s]);
                     }
                 }
                 n += x.nt;
@@ -273,14 +272,14 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     } else if (warp == K_WARP || warp == V_WARP) {
         // ------------------------------------------------------------ codes of K, and of V, into their rings: a block of 16 tokens a lane, four tiles looked up at a time, four ahead of their use
         const bool is_k = warp == K_WARP;
-        const int stages = is_k ? Cfg::K_RING : Cfg::V_RING;
+        constexpr int stages = Cfg::RING;
         uint64_t *const full = is_k ? bars.k_raw : bars.v_raw, *const empty = is_k ? bars.k_raw_free : bars.v_raw_free;
         uint8_t* const ring = smem + (is_k ? Cfg::RAW_K : Cfg::RAW_V);
         const int blocks = (int)a.by_blocks.d;
         while (ok && next_item(at, x)) {
             auto look_up = [&](int i0) -> const uint8_t* {
-                const int i = i0 + (lane >> 3);
-                const long long block = (long long)(x.t0 + i) * TURNS + (lane & 7);
+                const int i = i0 + lane / BLOCKS;
+                const long long block = (long long)(x.t0 + i) * BLOCKS + lane % BLOCKS;
                 if (i >= x.nt || block * CACHE_BLOCK >= x.len) return nullptr;
                 const int col = (int)fastdiv((uint32_t)block, a.by_blocks), page = a.tables[(size_t)x.slot * a.width + col];
                 if (page >= 0 && page < a.pages) return a.pool + (((size_t)page * a.kv_heads + x.h) * blocks + ((int)block - col * blocks)) * B::BYTES + (is_k ? 0 : Cfg::HALF);
@@ -289,18 +288,18 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             };
             const uint8_t *from = look_up(0), *ahead = nullptr;
             for (int i = 0; i < x.nt; ++i, ++n) {
-                if ((i & 3) == 0) {
+                if (i % (32 / BLOCKS) == 0) {
                     if (i > 0) from = ahead;
-                    ahead = look_up(i + 4);
+                    ahead = look_up(i + 32 / BLOCKS);
                 }
                 const int s = n % stages;
                 if (n >= (uint32_t)stages) ok = __all_sync(0xffffffffu, mbar_wait(&empty[s], (n / stages - 1) & 1, abortp));
                 if (!ok) break;
-                if ((lane >> 3) == (i & 3)) {
-                    if (is_k) have_s[n & 7][lane & 7] = from != nullptr;
+                if (lane / BLOCKS == i % (32 / BLOCKS)) {
+                    have_s[is_k][n & 15][lane % BLOCKS] = from != nullptr;
                     if (from) {
                         mbar_arrive_expect_tx(&full[s], Cfg::HALF);
-                        bulk_load_1d(ring + (s * TURNS + (lane & 7)) * Cfg::HALF, from, Cfg::HALF, &full[s]);
+                        bulk_load_1d(ring + (s * BLOCKS + lane % BLOCKS) * Cfg::HALF, from, Cfg::HALF, &full[s]);
                     } else {
                         mbar_arrive(&full[s]);
                     }
@@ -333,130 +332,144 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.sets_full);
         }
-    } else if (warp >= TURN0) {
-        // ------------------------------------------------------------ codes into operands: block `me` of every tile.  K of a tile is worked on ahead of V of the one before, also from item to item.
-        const int me = warp - TURN0;
+    } else if (warp >= TURN_K && warp < TURN_V) {
+        // ------------------------------------------------------------ codes of K into operands: a block of 16 tokens of every tile a warp
+        const int me = warp - TURN_K;
         const CacheOnes ones;
-        auto turn_k = [&](uint32_t m) {
-            const int s = m % Cfg::K_RING;
-            ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_raw[s], (m / Cfg::K_RING) & 1, abortp));
-            const bool have = have_s[m & 7][me] != 0;
-            // 16 tokens of 4 G words of eight channels, chunk by chunk of 16 bytes.  (All are read ahead of the first store: the compiler cannot know that they lie apart.)
-            const uint8_t* const from = smem + Cfg::RAW_K + (s * TURNS + me) * Cfg::HALF;
-            uint32_t codes[2 * G], sm[2 * G];
+        uint32_t fills = 0;
+        for (; ok && next_item(at, x);)
+            for (int i = 0; i < x.nt && ok; ++i, ++n) {
+                const int s = n % Cfg::RING;
+                ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_raw[s], (n / Cfg::RING) & 1, abortp));
+                if (!ok) break;
+                const bool have = have_s[1][n & 15][me] != 0;
+                // 16 tokens of 4 G words of eight channels, chunk by chunk of 16 bytes: two rounds of 32 chunks at a time, read ahead of the stores of those before.  (The loop is not unrolled, see the softmax's;
+                // and the compiler cannot know that what is read and written lies apart.)
+                const uint8_t* const from = smem + Cfg::RAW_K + (s * BLOCKS + me) * Cfg::HALF;
+                auto fill = [&](auto rest) {     // rest: what fp16 leaves of the numbers
+                    if (fills >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_empty[fills & 1], ((fills >> 1) - 1) & 1, abortp));
+                    if (!ok) return;
+                    uint8_t* const to = smem + Cfg::K + (fills & 1) * Cfg::TILE;
+                    if (have) {
+                        uint32_t codes[2], sm[2];
+                        auto read = [&](int k) {
 #pragma unroll
-            for (int i = 0; i < 2 * G; ++i) {
-                const int e = i * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), w = chunk >> 2;
-                codes[i] = *reinterpret_cast<const uint32_t*>(from + tok * (D / 2) + ((chunk & 3) * G + w) * 4);
-                sm[i] = *reinterpret_cast<const uint32_t*>(from + B::K_SCALES + (tok * G + w) * 4);
-            }
-            if (ok && m > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_empty, (m - 1) & 1, abortp));
-            if (!ok) return;
-            if (have) {
+                            for (int z = 0; z < 2; ++z) {
+                                const int e = (k + z) * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), w = chunk >> 2;
+                                codes[z] = *reinterpret_cast<const uint32_t*>(from + tok * (D / 2) + ((chunk & 3) * G + w) * 4);
+                                sm[z] = *reinterpret_cast<const uint32_t*>(from + B::K_SCALES + (tok * G + w) * 4);
+                            }
+                        };
+                        read(0);
+#pragma unroll 1
+                        for (int k = 0; k < 2 * G; k += 2) {
+                            const uint32_t codes0[2] = {codes[0], codes[1]}, sm0[2] = {sm[0], sm[1]};
+                            if (k + 2 < 2 * G) read(k + 2);
 #pragma unroll
-                for (int i = 0; i < 2 * G; ++i) {
-                    const int e = i * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), w = chunk >> 2, r = me * CACHE_BLOCK + tok;
-                    const uint32_t S = __byte_perm(sm[i], sm[i], 0x1010), S1 = S & 0xfff0fff0u, S2 = t_bits(__hsub2(t_h2(S), t_h2(S1)));
-                    const __half2 s1 = t_h2(S1), s2 = t_h2(S2), m1 = __hneg2(s1), m2 = __hneg2(s2);
-                    uint32_t y1[4], y2[4];
+                            for (int z = 0; z < 2; ++z) {
+                                const int e = (k + z) * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), r = me * CACHE_BLOCK + tok;
+                                const __half2 S = t_h2(__byte_perm(sm0[z], sm0[z], 0x1010)), M = t_h2(__byte_perm(sm0[z], sm0[z], 0x3232));
+                                uint32_t y[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const __half2 one = t_h2(ones(codes[i], k));
-                        y1[k] = t_bits(__hfma2(one, s1, m1));
-                        y2[k] = t_bits(__hfma2(one, s2, m2));
+                                for (int c = 0; c < 4; ++c) {
+                                    const __half2 one = t_h2(ones(codes0[z], c)), v = __hfma2(one, S, M);
+                                    if constexpr (decltype(rest)::value) {
+                                        const float2 o = __half22float2(one), h = __half22float2(v);
+                                        const float Sf = __low2float(S), Mf = __low2float(M);
+                                        y[c] = t_bits(__floats2half2_rn(fmaf(o.x, Sf, Mf) - h.x, fmaf(o.y, Sf, Mf) - h.y));
+                                    } else {
+                                        y[c] = t_bits(v);
+                                    }
+                                }
+                                *reinterpret_cast<uint4*>(to + (chunk >> 3) * Cfg::SUBTILE + swz128_offset(r, chunk & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
+                            }
+                        }
                     }
-                    const uint32_t to = (chunk >> 3) * 16384 + swz128_offset(r, chunk & 7);
-                    *reinterpret_cast<uint4*>(smem + Cfg::K1 + to) = make_uint4(y1[0], y1[1], y1[2], y1[3]);
-                    *reinterpret_cast<uint4*>(smem + Cfg::K2 + to) = make_uint4(y2[0], y2[1], y2[2], y2[3]);
-                    if ((chunk & 3) == 0) *reinterpret_cast<uint2*>(smem + Cfg::E + swz128_offset(r, w >> 1) + 8 * (w & 1)) = make_uint2(__byte_perm(sm[i], sm[i], 0x3232), S);
-                }
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.k_full[fills & 1]);
+                    ++fills;
+                };
+                fill(std::false_type{});
+                if (ok && x.exact) fill(std::true_type{});
+                if (ok && lane == 0) mbar_arrive(&bars.k_raw_free[s]);
             }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) { mbar_arrive(&bars.k_full); mbar_arrive(&bars.k_raw_free[s]); }
-        };
-        // first: the block's first token; ctx, len, nq and nan of its item
-        auto turn_v = [&](uint32_t m, long long first, int ctx, int len, int nq, uint32_t (*nan)[PSA_TREE_MOST / 32]) {
-            const int s = m % Cfg::V_RING;
-            ok = __all_sync(0xffffffffu, mbar_wait(&bars.v_raw[s], (m / Cfg::V_RING) & 1, abortp));
-            const bool have = have_s[m & 7][me] != 0;
-            // 8 pairs of tokens of 4 G chunks of eight channels
-            const uint8_t* const from = smem + Cfg::RAW_V + (s * TURNS + me) * Cfg::HALF;
-            uint32_t c0[G], c1[G];
-            uint2 sm[G];
-#pragma unroll
-            for (int i = 0; i < G; ++i) {
+    } else if (warp >= TURN_V) {
+        // ------------------------------------------------------------ codes of V into its operand: two blocks of every tile a warp
+        const CacheOnes ones;
+        // block `me` of tile m; first: its first token
+        auto turn_v = [&](uint32_t m, int me, long long first, int ctx, int len, int nq, uint32_t (*nan)[PSA_TREE_MOST / 32]) {
+            const int s = m % Cfg::RING;
+            // 8 pairs of tokens of 4 G chunks of eight channels, 32 chunks at a time
+            const uint8_t* const from = smem + Cfg::RAW_V + (s * BLOCKS + me) * Cfg::HALF;
+            uint32_t c0, c1;
+            uint2 sm;
+            auto read = [&](int i) {
                 const int e = i * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), w = chunk >> 2, g = 2 * (chunk & 3);
-                c0[i] = *reinterpret_cast<const uint32_t*>(from + pair * D + (g * G + w) * 4);
-                c1[i] = *reinterpret_cast<const uint32_t*>(from + pair * D + ((g + 1) * G + w) * 4);
-                sm[i] = *reinterpret_cast<const uint2*>(from + (B::V_SCALES - B::V_CODES) + (pair * G + w) * 8);
-            }
-            if (first + CACHE_BLOCK > ctx || !have) {
-                // The block has tokens that not all rows see, or that are none of the sequence's.  Behind the sequence's end lies whatever the page held before, and a weight of zero does not keep a NaN out
-                // of the sum: such tokens, and groups of the tree's that are not finite, go in as zeros; rows that see these get a NaN at the end.
-#pragma unroll
-                for (int i = 0; i < G; ++i) {
-                    const int e = i * 32 + lane, pair = e / (4 * G), w = (e - pair * (4 * G)) >> 2;
+                c0 = *reinterpret_cast<const uint32_t*>(from + pair * D + (g * G + w) * 4);
+                c1 = *reinterpret_cast<const uint32_t*>(from + pair * D + ((g + 1) * G + w) * 4);
+                sm = *reinterpret_cast<const uint2*>(from + (B::V_SCALES - B::V_CODES) + (pair * G + w) * 8);
+            };
+            read(0);
+            const bool have = have_s[0][m & 15][me] != 0;
+#pragma unroll 1
+            for (int i = 0; i < G; ++i) {
+                const int e = i * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), w = chunk >> 2, r = me * CACHE_BLOCK + 2 * pair;
+                const uint32_t d0 = c0, d1 = c1;
+                uint2 sm0 = sm;
+                if (i + 1 < G) read(i + 1);
+                if (first + CACHE_BLOCK > ctx || !have) {
+                    // The block has tokens that not all rows see, or that are none of the sequence's.  Behind the sequence's end lies whatever the page held before, and a weight of zero does not keep a NaN out
+                    // of the sum: such tokens, and groups of the tree's that are not finite, go in as zeros; rows that see these get a NaN at the end.
                     const long long t = first + 2 * pair;
                     const uint32_t keep = have ? (t < len ? 0xffffu : 0u) | (t + 1 < len ? 0xffff0000u : 0u) : 0u;
-                    sm[i].x &= keep;
-                    sm[i].y &= keep;
-                    uint32_t bad = (((sm[i].x & 0x7c007c00u) + 0x04000400u) | ((sm[i].y & 0x7c007c00u) + 0x04000400u)) & 0x80008000u;      // an exponent of all ones
+                    sm0.x &= keep;
+                    sm0.y &= keep;
+                    uint32_t bad = (((sm0.x & 0x7c007c00u) + 0x04000400u) | ((sm0.y & 0x7c007c00u) + 0x04000400u)) & 0x80008000u;      // an exponent of all ones
                     if (t < ctx) bad &= 0x80000000u;
                     if (t + 1 < ctx) bad = 0;
                     if (bad) {
                         const uint32_t drop = (bad >> 15) * 0xffffu;
-                        sm[i].x &= ~drop;
-                        sm[i].y &= ~drop;
+                        sm0.x &= ~drop;
+                        sm0.y &= ~drop;
                         const int at0 = (int)(t - ctx);
                         if ((bad & 0x8000u) && at0 < nq) atomicOr(&nan[w][at0 >> 5], 1u << (at0 & 31));
                         if ((bad & 0x80000000u) && at0 + 1 < nq) atomicOr(&nan[w][(at0 + 1) >> 5], 1u << ((at0 + 1) & 31));
                     }
                 }
-            }
-            if (ok && m > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (m - 1) & 1, abortp));
-            if (!ok) return;
-#pragma unroll
-            for (int i = 0; i < G; ++i) {
-                const int e = i * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), r = me * CACHE_BLOCK + 2 * pair;
-                const __half2 S = t_h2(sm[i].x), M = t_h2(sm[i].y);
+                const __half2 S = t_h2(sm0.x), M = t_h2(sm0.y);
                 uint32_t v[8];                   // channels 8 (chunk) + k: of the even token in the lower half, of the odd one in the upper
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    v[k] = t_bits(__hfma2(t_h2(ones(c0[i], k)), S, M));
-                    v[4 + k] = t_bits(__hfma2(t_h2(ones(c1[i], k)), S, M));
+                    v[k] = t_bits(__hfma2(t_h2(ones(d0, k)), S, M));
+                    v[4 + k] = t_bits(__hfma2(t_h2(ones(d1, k)), S, M));
                 }
-                uint8_t* const to = smem + Cfg::V + (chunk >> 3) * 16384;
+                uint8_t* const to = smem + Cfg::V + (m & 1) * Cfg::TILE + (chunk >> 3) * Cfg::SUBTILE;
                 *reinterpret_cast<uint4*>(to + swz128_offset(r, chunk & 7)) =
                     make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[4], v[5], 0x5410), __byte_perm(v[6], v[7], 0x5410));
                 *reinterpret_cast<uint4*>(to + swz128_offset(r + 1, chunk & 7)) =
                     make_uint4(__byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632), __byte_perm(v[4], v[5], 0x7632), __byte_perm(v[6], v[7], 0x7632));
             }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) { mbar_arrive(&bars.v_full); mbar_arrive(&bars.v_raw_free[s]); }
         };
-        // the tile before the present one: what its V needs
-        long long first = 0;
-        int ctx = 0, len = 0, nq = 0;
-        uint32_t it = 0, its = 0;
-        auto turn_last_v = [&] {
-            if (first + KEYS > ctx) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_full, its & 1, abortp));       // (the item's marks of NaN are clear)
-            if (ok) turn_v(n - 1, first + me * CACHE_BLOCK, ctx, len, nq, nan_s[its & 1]);
-        };
-        for (; ok && next_item(at, x); ++it)
-            for (int i = 0; i < x.nt && ok; ++i) {
-                turn_k(n);
-                if (ok && n > 0) turn_last_v();
+        for (uint32_t it = 0; ok && next_item(at, x); ++it) {
+            bool sets = false;                   // the item's marks of NaN are known to be clear
+            for (int i = 0; i < x.nt && ok; ++i, ++n) {
+                const long long first = (long long)(x.t0 + i) * KEYS;
+                if (!sets && first + KEYS > x.ctx) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_full, it & 1, abortp));
+                    sets = true;
+                }
+                const int s = n % Cfg::RING;
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(&bars.v_raw[s], (n / Cfg::RING) & 1, abortp));
+                if (ok && n >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&bars.v_empty[n & 1], ((n >> 1) - 1) & 1, abortp));
                 if (!ok) break;
-                ++n;
-                first = (long long)(x.t0 + i) * KEYS;
-                ctx = x.ctx;
-                len = x.len;
-                nq = x.nq;
-                its = it;
+#pragma unroll 1
+                for (int me = warp - TURN_V; me < BLOCKS; me += V_WARPS) turn_v(n, me, first + me * CACHE_BLOCK, x.ctx, x.len, x.nq, nan_s[it & 1]);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) { mbar_arrive(&bars.v_full[n & 1]); mbar_arrive(&bars.v_raw_free[s]); }
             }
-        if (ok && n > 0) turn_last_v();
+        }
     } else {
         // ------------------------------------------------------------ softmax: 16 rows a warp, in the quad layout
         const int sw = warp - SOFT0, r0 = (warp & 3) * 32 + (sw >> 2) * 16, rA = r0 + (lane >> 2), rB = rA + 8, cq = 2 * (lane & 3);
@@ -487,35 +500,21 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                         topA = max3(topA, fabsf(v0.x), fabsf(v0.y));
                         topB = max3(topB, fabsf(v1.x), fabsf(v1.y));
                     }
-                // 2^e <= top < 2^(e + 1): a row goes in as q 2^(8 - e), exact but for what lies 2^32 below its largest number; sums of 32 stay below 2^14
+                // 2^e <= top < 2^(e + 1): a row goes in as q 2^(8 - e), exact but for what lies 2^32 below its largest number
                 const uint32_t eA = min(max(__float_as_uint(quad_max(topA)) >> 23, 1u), 253u), eB = min(max(__float_as_uint(quad_max(topB)) >> 23, 1u), 253u);
                 const float downA = __uint_as_float((254u - eA) << 23), downB = __uint_as_float((254u - eB) << 23);
                 fA = fmaxf(__uint_as_float(eA << 23) * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
                 fB = fmaxf(__uint_as_float(eB << 23) * (a.scale * LOG2E * 0.00390625f), 1.2e-38f);
-                uint32_t sums[4] = {0, 0, 0, 0};     // columns 4 w ..: the sum of the row over group w in two parts, twice.  This thread's words c and 4 + c of row A, then of row B
 #pragma unroll
                 for (int u = 0; u < Cfg::SUB; ++u) {
-                    float sA[2] = {0.f, 0.f}, sB[2] = {0.f, 0.f};
 #pragma unroll
                     for (int g = 0; g < 8; ++g) {
                         const float2 v0 = number(raw[u][2 * g]), v1 = number(raw[u][2 * g + 1]);
-                        const __half2 v = __floats2half2_rn(v0.x * downA * 256.f, v0.y * downA * 256.f), z = __floats2half2_rn(v1.x * downB * 256.f, v1.y * downB * 256.f);
-                        raw[u][2 * g] = t_bits(v);
-                        raw[u][2 * g + 1] = t_bits(z);
-                        sA[g >> 2] += __low2float(v) + __high2float(v);
-                        sB[g >> 2] += __low2float(z) + __high2float(z);
+                        raw[u][2 * g] = t_bits(__floats2half2_rn(v0.x * downA * 256.f, v0.y * downA * 256.f));
+                        raw[u][2 * g + 1] = t_bits(__floats2half2_rn(v1.x * downB * 256.f, v1.y * downB * 256.f));
                     }
                     tmem_st_quad32(tmem + TM_Q + 32 * u + lanes, raw[u]);
-                    auto two = [&](float s) {
-                        s = quad_sum(s);
-                        const __half hi16 = __float2half_rn(s);
-                        return t_bits(__halves2half2(hi16, __float2half_rn(s - __half2float(hi16))));
-                    };
-                    const uint32_t a0 = two(sA[0]), a1 = two(sA[1]), b0 = two(sB[0]), b1 = two(sB[1]);
-                    sums[2 * u] = lane & 2 ? a1 : a0;                // (words 4 u + c: of group 2 u + c / 2)
-                    sums[2 * u + 1] = lane & 2 ? b1 : b0;
                 }
-                asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};" ::"r"(tmem + TM_E + lanes), "r"(sums[0]), "r"(sums[1]), "r"(sums[2]), "r"(sums[3]) : "memory");
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -526,13 +525,18 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             const int words = (x.nq + 31) / 32;
             bool sets = false;                   // they are known to be there
             float mA = -INFINITY, mB = -INFINITY, lA = 0.f, lB = 0.f;
+            const bool some = x.qt * ROWS + r0 < x.nq * a.group;             // the warp has rows
             for (int j = 0; j < x.nt && ok; ++j) {
-                const uint32_t m = n + j;
-                ok = __all_sync(0xffffffffu, mbar_wait(&bars.s_full[m & 1], (m >> 1) & 1, abortp));
+                const uint32_t m = n + j, buf = m & 1;
+                ok = __all_sync(0xffffffffu, mbar_wait(&bars.s_full[buf], (m >> 1) & 1, abortp));
                 if (!ok) break;
+                if (!some) {                     // (what is there instead of weights stays in these rows)
+                    if (lane == 0) mbar_arrive(&bars.p_ready[buf]);
+                    continue;
+                }
                 tc_fence_after();
-                const uint32_t tS = tmem + TM_S + (m & 1) * KEYS + lanes;
-                const unsigned long long have = *reinterpret_cast<const unsigned long long*>(have_s[m & 7]);
+                const uint32_t tS = tmem + TM_S + buf * KEYS + lanes;
+                const unsigned long long have = *reinterpret_cast<const unsigned long long*>(have_s[1][m & 15]);
                 const long long key0 = (long long)(x.t0 + j) * KEYS;
                 const bool masked = key0 + KEYS > x.ctx || have != 0x0101010101010101ull;
                 if (masked && x.meets_tree && !sets) {
@@ -540,37 +544,38 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                     if (!ok) break;
                     sets = true;
                 }
-                // 64 columns of the scores (read twice, for the maximum and for the weights: held in between they would not fit the registers)
-                auto scores = [&](uint32_t (&s)[32], int half) {
-                    tmem_ld_quad64(tS + 64 * half, s);
-                    tc_wait_ld();
-                    if (!masked) return;
-                    // the tile's tokens that a row sees, 32 a word: all ahead of the tree, and the row's set in it; none of blocks that are not there
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const int at32 = (int)(key0 + 64 * half + 32 * z - x.ctx), word = at32 >> 5;
-                        const uint32_t both = ((have >> (16 * (2 * half + z)) & 1) ? 0xffffu : 0u) | ((have >> (16 * (2 * half + z) + 8) & 1) ? 0xffff0000u : 0u);
-                        auto seen = [&](const uint32_t* set) {
-                            const uint32_t l = word < 0 ? 0xffffffffu : word < words ? set[word] : 0u, u = word + 1 < 0 ? 0xffffffffu : word + 1 < words ? set[word + 1] : 0u;
-                            return (__funnelshift_r(l, u, at32) & both) >> cq;
-                        };
-                        const uint32_t A = seen(setA), Bm = seen(setB);
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            uint32_t* const v = s + 16 * z + 4 * g;
-                            if (!(A >> (8 * g) & 1u)) v[0] = 0xff800000u;
-                            if (!(A >> (8 * g + 1) & 1u)) v[1] = 0xff800000u;
-                            if (!(Bm >> (8 * g) & 1u)) v[2] = 0xff800000u;
-                            if (!(Bm >> (8 * g + 1) & 1u)) v[3] = 0xff800000u;
-                        }
-                    }
-                };
+                // Twice over the scores, 64 columns at a time, in loops that are not unrolled: instructions of five kinds of warps share the caches next to the pipes.
                 uint32_t s[32];
                 float bA = -INFINITY, bB = -INFINITY;
-                scores(s, 0);
-                max_quad64(s, bA, bB);
-                scores(s, 1);
-                max_quad64(s, bA, bB);
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    tmem_ld_quad64(tS + 64 * half, s);
+                    tc_wait_ld();
+                    if (masked) {
+                        // the tile's tokens that a row sees, 32 a word: all ahead of the tree, and the row's set in it; none of blocks that are not there
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const int at32 = (int)(key0 + 64 * half + 32 * z - x.ctx), word = at32 >> 5;
+                            const uint32_t both = ((have >> (16 * (2 * half + z)) & 1) ? 0xffffu : 0u) | ((have >> (16 * (2 * half + z) + 8) & 1) ? 0xffff0000u : 0u);
+                            auto seen = [&](const uint32_t* set) {
+                                const uint32_t l = word < 0 ? 0xffffffffu : word < words ? set[word] : 0u, u = word + 1 < 0 ? 0xffffffffu : word + 1 < words ? set[word + 1] : 0u;
+                                return (__funnelshift_r(l, u, at32) & both) >> cq;
+                            };
+                            const uint32_t A = seen(setA), Bm = seen(setB);
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) {
+                                uint32_t* const v = s + 16 * z + 4 * g;
+                                if (!(A >> (8 * g) & 1u)) v[0] = 0xff800000u;
+                                if (!(A >> (8 * g + 1) & 1u)) v[1] = 0xff800000u;
+                                if (!(Bm >> (8 * g) & 1u)) v[2] = 0xff800000u;
+                                if (!(Bm >> (8 * g + 1) & 1u)) v[3] = 0xff800000u;
+                            }
+                        }
+                        tmem_st_quad64(tS + 64 * half, s);
+                    }
+                    max_quad64(s, bA, bB);
+                }
+                if (masked) tc_wait_st();
                 bA = quad_max(bA) * fA;
                 bB = quad_max(bB) * fB;
                 float alphaA = 1.f, alphaB = 1.f;
@@ -579,8 +584,11 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 const float nA = mA == -INFINITY ? 0.f : UP - mA, nB = mB == -INFINITY ? 0.f : UP - mB;
                 uint64_t sumA = 0, sumB = 0;
                 const uint64_t fA2 = t_pair(fA, fA), fB2 = t_pair(fB, fB), nA2 = t_pair(nA, nA), nB2 = t_pair(nB, nB);
-                uint32_t p1[16], p0[16];
-                auto weights = [&](uint32_t (&p)[16]) {
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    tmem_ld_quad64(tS + 64 * half, s);
+                    tc_wait_ld();
+                    uint32_t p[16];
 #pragma unroll
                     for (int g = 0; g < 8; ++g) {
                         const float2 v0 = t_pair(t_fma2(t_pair(__uint_as_float(s[4 * g]), __uint_as_float(s[4 * g + 1])), fA2, nA2)), v1 = t_pair(t_fma2(t_pair(__uint_as_float(s[4 * g + 2]), __uint_as_float(s[4 * g + 3])), fB2, nB2));
@@ -590,41 +598,36 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                         p[2 * g] = t_weights(x0, x1);
                         p[2 * g + 1] = t_weights(y0, y1);
                     }
-                };
-                weights(p1);
-                scores(s, 0);
-                weights(p0);
+                    tmem_st_quad32(tS + 32 * half, p);       // (over scores that this warp alone reads, and has read)
+                }
                 lA = fmaf(lA, alphaA, t_pair(sumA).x + t_pair(sumA).y);
                 lB = fmaf(lB, alphaB, t_pair(sumB).x + t_pair(sumB).y);
-                if (j > 0) {                     // O is in use by the product before this one
-                    ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (m - 1) & 1, abortp));
+                if (j > 0 && __any_sync(0xffffffffu, alphaA != 1.f || alphaB != 1.f)) {
+                    // O is in use by the product before this one.  (That of tile m - 2 is done: scores of this tile have come behind it.)
+                    ok = __all_sync(0xffffffffu, mbar_wait(&bars.v_empty[buf ^ 1], ((m - 1) >> 1) & 1, abortp));
                     if (!ok) break;
                     tc_fence_after();
-                    if (__any_sync(0xffffffffu, alphaA != 1.f || alphaB != 1.f)) {
 #pragma unroll 1
-                        for (int c = 0; c < Cfg::SUB; ++c) {
-                            uint32_t v[32];
-                            tmem_ld_quad64(tO + 64 * c, v);
-                            tc_wait_ld();
+                    for (int c = 0; c < Cfg::SUB; ++c) {
+                        uint32_t v[32];
+                        tmem_ld_quad64(tO + 64 * c, v);
+                        tc_wait_ld();
 #pragma unroll
-                            for (int g = 0; g < 8; ++g) {
-                                v[4 * g] = __float_as_uint(__uint_as_float(v[4 * g]) * alphaA);
-                                v[4 * g + 1] = __float_as_uint(__uint_as_float(v[4 * g + 1]) * alphaA);
-                                v[4 * g + 2] = __float_as_uint(__uint_as_float(v[4 * g + 2]) * alphaB);
-                                v[4 * g + 3] = __float_as_uint(__uint_as_float(v[4 * g + 3]) * alphaB);
-                            }
-                            tmem_st_quad64(tO + 64 * c, v);
+                        for (int g = 0; g < 8; ++g) {
+                            v[4 * g] = __float_as_uint(__uint_as_float(v[4 * g]) * alphaA);
+                            v[4 * g + 1] = __float_as_uint(__uint_as_float(v[4 * g + 1]) * alphaA);
+                            v[4 * g + 2] = __float_as_uint(__uint_as_float(v[4 * g + 2]) * alphaB);
+                            v[4 * g + 3] = __float_as_uint(__uint_as_float(v[4 * g + 3]) * alphaB);
                         }
+                        tmem_st_quad64(tO + 64 * c, v);
                     }
                 }
-                tmem_st_quad32(tS, p0);          // (over the scores, which this warp alone reads in these rows)
-                tmem_st_quad32(tS + 32, p1);
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.p_ready);
+                if (lane == 0) mbar_arrive(&bars.p_ready[buf]);
             }
-            if (ok && x.nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.o_done, (n + x.nt - 1) & 1, abortp));
+            if (ok && x.nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.v_empty[(n + x.nt - 1) & 1], ((n + x.nt - 1) >> 1) & 1, abortp));
             if (ok && x.meets_tree && !sets) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_full, it & 1, abortp));
             if (!ok) break;
             // ---- the rows' results
