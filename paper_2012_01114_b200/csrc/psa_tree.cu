@@ -32,8 +32,8 @@ constexpr int MMA_WARP = 0, K_WARP = 1, V_WARP = 2, SET_WARP = 3, SOFT0 = 4, SOF
 constexpr int EXACT = 2048;                     // tokens of a sequence up to which keys go in in two parts
 constexpr int T_SEQS = 512;                     // sequences of one launch
 constexpr int T_CTAS = 160;                     // at most
-constexpr int LEAST = 4;                        // tiles of a piece, or what takes as long
-constexpr int ROW_COST = 3;                     // what a row tile costs beside its tiles of keys, in such
+// What work takes, in halves of a tile of keys: a tile, one with keys in two parts, and what a row tile takes beside its tiles; the least that a CTA is given.
+constexpr int COST = 2, COST_EXACT = 3, COST_ROW = 8, LEAST = 8;
 constexpr int TREE_WORDS = PSA_TREE_MOST / 32 + 1;
 constexpr float UP = 7.f;                       // log2 of what weights are held larger by
 constexpr float T_LN2 = 0.6931471805599453f;
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             const int held = there ? max(a.lens[slot], 0) : 0, len = (int)min((long long)held, (long long)a.width * a.page_size);
             strange |= (nq > 0 && (!there || held != len)) || nq != s1 - s0;
             const int tiles = max((int)(((uint32_t)len + KEYS - 1) / KEYS), 1), row_tiles = (nq * a.group + ROWS - 1) / ROWS;
-            n = (long long)row_tiles * a.kv_heads * (tiles + ROW_COST);
+            n = (long long)row_tiles * a.kv_heads * ((long long)tiles * (a.f16 || len <= EXACT ? COST_EXACT : COST) + COST_ROW);
             len_s[b] = len;
             q0_s[b] = q0;
             nq_s[b] = nq;
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     tc_fence_after();
     const uint32_t tmem = tmem_s;
 
-    // ---- Every role walks the CTA's items by itself: its share of the list.  A row tile is ROW_COST units and one for each tile of keys.
+    // ---- Every role walks the CTA's items by itself: its share of the list.  A row tile is COST_ROW units and COST or COST_EXACT for each tile of keys, which belongs to the CTA that has its first unit.
     auto next_item = [&](long long& at, TItem& x) -> bool {
         while (at < mine1) {
             int lo = 0, hi = a.sequences - 1;    // the last sequence that begins at or before it (and has tiles: those without begin where the next one does)
@@ -204,21 +204,22 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             x.q0 = q0_s[lo];
             x.slot = slot_s[lo];
             const int tiles = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1);
-            const long long units = tiles + ROW_COST, inside = at - base_s[lo], row = inside / units, u0 = inside - row * units, u1 = min(units, u0 + (mine1 - at)), row0 = at - u0;
+            x.exact = a.f16 || x.len <= EXACT;
+            const int cost = x.exact ? COST_EXACT : COST;
+            const long long units = (long long)tiles * cost + COST_ROW, inside = at - base_s[lo], row = inside / units, u0 = inside - row * units, u1 = min(units, u0 + (mine1 - at)), row0 = at - u0;
             const int row_tiles = (x.nq * a.group + ROWS - 1) / ROWS;
             at += u1 - u0;
-            x.t0 = (int)max(u0 - ROW_COST, 0LL);
-            const int t1 = (int)max(u1 - ROW_COST, 0LL);
+            x.t0 = (int)((max(u0 - COST_ROW, 0LL) + cost - 1) / cost);
+            const int t1 = (int)((max(u1 - COST_ROW, 0LL) + cost - 1) / cost);
             if (t1 <= x.t0) continue;
             x.nt = x.len > 0 ? t1 - x.t0 : 0;
             x.h = (int)row / row_tiles;
             x.qt = (int)row - x.h * row_tiles;
             x.ctx = x.len - x.nq;
             x.tok0 = (int)fastdiv((uint32_t)(x.qt * ROWS), a.by_group);
-            x.first_cta = (int)((row0 + ROW_COST) / per);
-            x.parts = (int)((row0 + units - 1) / per) - x.first_cta + 1;
+            x.first_cta = (int)((row0 + COST_ROW) / per);
+            x.parts = (int)((row0 + units - cost) / per) - x.first_cta + 1;
             x.part = (int)blockIdx.x - x.first_cta;
-            x.exact = a.f16 || x.len <= EXACT;
             x.meets_tree = x.nt > 0 && t1 * (long long)KEYS > x.ctx;
             return true;
         }
@@ -696,8 +697,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     if (tid == 0 && abort_flag) atomicExch(&dc->status, (int)PSA_ERR_TIMEOUT);
 }
 
-// Joins the parts of the row tiles that were cut: four rows a CTA, a thread four channels, parts in their order.
-constexpr int JOIN_ROWS = 4;
+// Joins the parts of the row tiles that were cut: sixteen rows a CTA, a thread four channels, parts in their order.
+constexpr int JOIN_ROWS = 16;
 template <int D>
 __global__ void __launch_bounds__(JOIN_ROWS * D / 4) tree_join_kernel(const TreeArgs a) {
     grid_dependency_wait();
