@@ -338,42 +338,43 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
         const int me = warp - TURN_K;
         const CacheOnes ones;
         uint32_t fills = 0;
+        // Eight tokens are G rounds of 32 chunks of 16 bytes (chunk: eight channels of a token); where a lane's are in the codes, the scales and the operand.  The other eight lie behind them.
+        int from_codes[G], from_scales[G], to_chunk[G];
+#pragma unroll
+        for (int z = 0; z < G; ++z) {
+            const int e = z * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), w = chunk >> 2;
+            from_codes[z] = tok * (D / 2) + ((chunk & 3) * G + w) * 4;
+            from_scales[z] = B::K_SCALES + (tok * G + w) * 4;
+            to_chunk[z] = (chunk >> 3) * Cfg::SUBTILE + (int)swz128_offset(me * CACHE_BLOCK + tok, chunk & 7);
+        }
         for (; ok && next_item(at, x);)
             for (int i = 0; i < x.nt && ok; ++i, ++n) {
                 const int s = n % Cfg::RING;
                 ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_raw[s], (n / Cfg::RING) & 1, abortp));
                 if (!ok) break;
                 const bool have = have_s[1][n & 15][me] != 0;
-                // 16 tokens of 4 G words of eight channels, chunk by chunk of 16 bytes: two rounds of 32 chunks at a time, read ahead of the stores of those before.  (The loop is not unrolled, see the softmax's;
-                // and the compiler cannot know that what is read and written lies apart.)
                 const uint8_t* const from = smem + Cfg::RAW_K + (s * BLOCKS + me) * Cfg::HALF;
                 auto fill = [&](auto rest) {     // rest: what fp16 leaves of the numbers
                     if (fills >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&bars.k_empty[fills & 1], ((fills >> 1) - 1) & 1, abortp));
                     if (!ok) return;
                     uint8_t* const to = smem + Cfg::K + (fills & 1) * Cfg::TILE;
                     if (have) {
-                        uint32_t codes[2], sm[2];
-                        auto read = [&](int k) {
-#pragma unroll
-                            for (int z = 0; z < 2; ++z) {
-                                const int e = (k + z) * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), w = chunk >> 2;
-                                codes[z] = *reinterpret_cast<const uint32_t*>(from + tok * (D / 2) + ((chunk & 3) * G + w) * 4);
-                                sm[z] = *reinterpret_cast<const uint32_t*>(from + B::K_SCALES + (tok * G + w) * 4);
-                            }
-                        };
-                        read(0);
+                        // (All of eight tokens is read ahead of the first store: the compiler cannot know that what is read and written lies apart.)
 #pragma unroll 1
-                        for (int k = 0; k < 2 * G; k += 2) {
-                            const uint32_t codes0[2] = {codes[0], codes[1]}, sm0[2] = {sm[0], sm[1]};
-                            if (k + 2 < 2 * G) read(k + 2);
+                        for (int eight = 0; eight < 2; ++eight) {
+                            uint32_t codes[G], sm[G];
 #pragma unroll
-                            for (int z = 0; z < 2; ++z) {
-                                const int e = (k + z) * 32 + lane, tok = e / (4 * G), chunk = e - tok * (4 * G), r = me * CACHE_BLOCK + tok;
-                                const __half2 S = t_h2(__byte_perm(sm0[z], sm0[z], 0x1010)), M = t_h2(__byte_perm(sm0[z], sm0[z], 0x3232));
+                            for (int z = 0; z < G; ++z) {
+                                codes[z] = *reinterpret_cast<const uint32_t*>(from + from_codes[z] + eight * (8 * D / 2));
+                                sm[z] = *reinterpret_cast<const uint32_t*>(from + from_scales[z] + eight * (8 * G * 4));
+                            }
+#pragma unroll
+                            for (int z = 0; z < G; ++z) {
+                                const __half2 S = t_h2(__byte_perm(sm[z], sm[z], 0x1010)), M = t_h2(__byte_perm(sm[z], sm[z], 0x3232));
                                 uint32_t y[4];
 #pragma unroll
                                 for (int c = 0; c < 4; ++c) {
-                                    const __half2 one = t_h2(ones(codes0[z], c)), v = __hfma2(one, S, M);
+                                    const __half2 one = t_h2(ones(codes[z], c)), v = __hfma2(one, S, M);
                                     if constexpr (decltype(rest)::value) {
                                         const float2 o = __half22float2(one), h = __half22float2(v);
                                         const float Sf = __low2float(S), Mf = __low2float(M);
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                                         y[c] = t_bits(v);
                                     }
                                 }
-                                *reinterpret_cast<uint4*>(to + (chunk >> 3) * Cfg::SUBTILE + swz128_offset(r, chunk & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
+                                *reinterpret_cast<uint4*>(to + to_chunk[z] + eight * 1024) = make_uint4(y[0], y[1], y[2], y[3]);
                             }
                         }
                     }
@@ -398,57 +399,64 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     } else if (warp >= TURN_V) {
         // ------------------------------------------------------------ codes of V into its operand: two blocks of every tile a warp
         const CacheOnes ones;
+        // A block is G rounds of 32 chunks (chunk: eight channels of a pair of tokens); where a lane's are in the codes, the scales and the operand.
+        int from_codes[G], from_scales[G], to_chunk[G];
+#pragma unroll
+        for (int z = 0; z < G; ++z) {
+            const int e = z * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), w = chunk >> 2;
+            from_codes[z] = pair * D + (2 * (chunk & 3) * G + w) * 4;
+            from_scales[z] = (B::V_SCALES - B::V_CODES) + (pair * G + w) * 8;
+            to_chunk[z] = (chunk >> 3) * Cfg::SUBTILE + (int)swz128_offset(2 * pair, chunk & 7);
+        }
         // block `me` of tile m; first: its first token
         auto turn_v = [&](uint32_t m, int me, long long first, int ctx, int len, int nq, uint32_t (*nan)[PSA_TREE_MOST / 32]) {
             const int s = m % Cfg::RING;
-            // 8 pairs of tokens of 4 G chunks of eight channels, 32 chunks at a time
             const uint8_t* const from = smem + Cfg::RAW_V + (s * BLOCKS + me) * Cfg::HALF;
-            uint32_t c0, c1;
-            uint2 sm;
-            auto read = [&](int i) {
-                const int e = i * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), w = chunk >> 2, g = 2 * (chunk & 3);
-                c0 = *reinterpret_cast<const uint32_t*>(from + pair * D + (g * G + w) * 4);
-                c1 = *reinterpret_cast<const uint32_t*>(from + pair * D + ((g + 1) * G + w) * 4);
-                sm = *reinterpret_cast<const uint2*>(from + (B::V_SCALES - B::V_CODES) + (pair * G + w) * 8);
-            };
-            read(0);
+            uint8_t* const to = smem + Cfg::V + (m & 1) * Cfg::TILE + me * (CACHE_BLOCK * 128);
+            uint32_t c0[G], c1[G];
+            uint2 sm[G];
+#pragma unroll
+            for (int z = 0; z < G; ++z) {
+                c0[z] = *reinterpret_cast<const uint32_t*>(from + from_codes[z]);
+                c1[z] = *reinterpret_cast<const uint32_t*>(from + from_codes[z] + 4 * G);
+                sm[z] = *reinterpret_cast<const uint2*>(from + from_scales[z]);
+            }
             const bool have = have_s[0][m & 15][me] != 0;
-#pragma unroll 1
-            for (int i = 0; i < G; ++i) {
-                const int e = i * 32 + lane, pair = e / (4 * G), chunk = e - pair * (4 * G), w = chunk >> 2, r = me * CACHE_BLOCK + 2 * pair;
-                const uint32_t d0 = c0, d1 = c1;
-                uint2 sm0 = sm;
-                if (i + 1 < G) read(i + 1);
-                if (first + CACHE_BLOCK > ctx || !have) {
-                    // The block has tokens that not all rows see, or that are none of the sequence's.  Behind the sequence's end lies whatever the page held before, and a weight of zero does not keep a NaN out
-                    // of the sum: such tokens, and groups of the tree's that are not finite, go in as zeros; rows that see these get a NaN at the end.
-                    const long long t = first + 2 * pair;
-                    const uint32_t keep = have ? (t < len ? 0xffffu : 0u) | (t + 1 < len ? 0xffff0000u : 0u) : 0u;
-                    sm0.x &= keep;
-                    sm0.y &= keep;
-                    uint32_t bad = (((sm0.x & 0x7c007c00u) + 0x04000400u) | ((sm0.y & 0x7c007c00u) + 0x04000400u)) & 0x80008000u;      // an exponent of all ones
-                    if (t < ctx) bad &= 0x80000000u;
-                    if (t + 1 < ctx) bad = 0;
+            if (first + CACHE_BLOCK > ctx || !have) {
+                // The block has tokens that not all rows see, or that are none of the sequence's.  Behind the sequence's end lies whatever the page held before, and a weight of zero does not keep a NaN out
+                // of the sum: such tokens, and groups of the tree's that are not finite, go in as zeros; rows that see these get a NaN at the end.
+#pragma unroll
+                for (int z = 0; z < G; ++z) {
+                    const int e = z * 32 + lane, pair = e / (4 * G), w = (e - pair * (4 * G)) >> 2;
+                    const long long tok = first + 2 * pair;
+                    const uint32_t keep = have ? (tok < len ? 0xffffu : 0u) | (tok + 1 < len ? 0xffff0000u : 0u) : 0u;
+                    sm[z].x &= keep;
+                    sm[z].y &= keep;
+                    uint32_t bad = (((sm[z].x & 0x7c007c00u) + 0x04000400u) | ((sm[z].y & 0x7c007c00u) + 0x04000400u)) & 0x80008000u;      // an exponent of all ones
+                    if (tok < ctx) bad &= 0x80000000u;
+                    if (tok + 1 < ctx) bad = 0;
                     if (bad) {
                         const uint32_t drop = (bad >> 15) * 0xffffu;
-                        sm0.x &= ~drop;
-                        sm0.y &= ~drop;
-                        const int at0 = (int)(t - ctx);
+                        sm[z].x &= ~drop;
+                        sm[z].y &= ~drop;
+                        const int at0 = (int)(tok - ctx);
                         if ((bad & 0x8000u) && at0 < nq) atomicOr(&nan[w][at0 >> 5], 1u << (at0 & 31));
                         if ((bad & 0x80000000u) && at0 + 1 < nq) atomicOr(&nan[w][(at0 + 1) >> 5], 1u << ((at0 + 1) & 31));
                     }
                 }
-                const __half2 S = t_h2(sm0.x), M = t_h2(sm0.y);
+            }
+#pragma unroll
+            for (int z = 0; z < G; ++z) {
+                const __half2 S = t_h2(sm[z].x), M = t_h2(sm[z].y);
                 uint32_t v[8];                   // channels 8 (chunk) + k: of the even token in the lower half, of the odd one in the upper
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    v[k] = t_bits(__hfma2(t_h2(ones(d0, k)), S, M));
-                    v[4 + k] = t_bits(__hfma2(t_h2(ones(d1, k)), S, M));
+                    v[k] = t_bits(__hfma2(t_h2(ones(c0[z], k)), S, M));
+                    v[4 + k] = t_bits(__hfma2(t_h2(ones(c1[z], k)), S, M));
                 }
-                uint8_t* const to = smem + Cfg::V + (m & 1) * Cfg::TILE + (chunk >> 3) * Cfg::SUBTILE;
-                *reinterpret_cast<uint4*>(to + swz128_offset(r, chunk & 7)) =
+                *reinterpret_cast<uint4*>(to + to_chunk[z]) =
                     make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[4], v[5], 0x5410), __byte_perm(v[6], v[7], 0x5410));
-                *reinterpret_cast<uint4*>(to + swz128_offset(r + 1, chunk & 7)) =
+                *reinterpret_cast<uint4*>(to + ((to_chunk[z] ^ 16) + 128)) =
                     make_uint4(__byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632), __byte_perm(v[4], v[5], 0x7632), __byte_perm(v[6], v[7], 0x7632));
             }
         };
