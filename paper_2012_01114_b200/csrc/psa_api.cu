@@ -2,7 +2,6 @@
 // scheduler (psa_skip_count) and dispatch to the fp32 and bf16 kernel families.
 #include <math.h>
 #include <stdio.h>
-#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -963,10 +962,15 @@ int psa_cache_append_rotary(const psa_cache* cache, const psa_rotary* rotary, co
 
 size_t psa_cache_workspace_bytes(int d_k) { return cache_head(d_k) ? COUNTER_BYTES + cache_attention_scratch_bytes(d_k) : 0; }
 
-// Whether a tree's rows go to the tensor core's tiles of 128 rows (psa_tree.cu) or, sixteen at a time, to psa_cache_attn.cu.
-static bool tree_on_tiles(int max_q, int group, int d) {
-    static const int C = getenv("TC") ? atoi(getenv("TC")) : 16;
-    return d <= 128 && (long long)max_q * group > C;
+// Whether a tree's rows go to tiles of 128 rows (psa_tree.cu) or, sixteen at a time, through psa_cache_attn.cu, by the most rows that a head of K can have and the keys that the block table has
+// room for.  The second reads the keys once for every sixteen rows and its time goes with their number; the first takes its 20 us for the smallest call and the same for 16 rows as for 128.
+// 8 heads of K, d 128, microseconds of tiles and of the other at 32, 48, 64, 96 rows: 16 sequences of 8,000 tokens 118 : 116, 119 : 170, 120 : 225, 125 : 334; 64 of 2,000 220 : 127, 220 : 224,
+// 220 : 224, 220 : 333; 16 of 1,000 at 48 and 64 45 : 39, 46 : 50; one of 4,000 at 128 26 : 24; one of 300 at 48 21 : 10.5.
+static bool tree_on_tiles(const psa_cache& c, int sequences, int max_q, int group) {
+    const long long rows = (long long)max_q * group;
+    if (c.d_k > 128 || rows <= 32) return false;
+    const double keys = (double)sequences * c.width * c.page_size * c.kv_heads * (c.d_k / 128.0);
+    return keys * ((rows + 15) / 16) > 400000.0;
 }
 
 size_t psa_tree_workspace_bytes(int d_k) { return cache_head(d_k) ? COUNTER_BYTES + std::max(cache_attention_scratch_bytes(d_k), tree_attention_scratch_bytes(d_k)) : 0; }
@@ -982,7 +986,7 @@ static int attend_to_cache(const psa_cache* cache, const void* Q, long long q_st
     if (!Q || !seqs || !q_starts || !out || (tree && !parents)) return PSA_ERR_NULL;
     if (!good_stride(q_stride, (long long)heads * cache->d_k) || (long long)rows * (heads / cache->kv_heads) > 0x7fffff00LL) return PSA_ERR_SHAPE;
     if (!aligned16(Q) || !aligned16(out) || !aligned4(lse) || !aligned4(seqs) || !aligned4(q_starts) || !aligned4(parents)) return PSA_ERR_ALIGN;
-    const bool many = tree && tree_on_tiles(max_q, heads / cache->kv_heads, cache->d_k);
+    const bool many = tree && tree_on_tiles(*cache, sequences, max_q, heads / cache->kv_heads);
     return run_op(many ? tree_attention_scratch_bytes(cache->d_k) : cache_attention_scratch_bytes(cache->d_k), stream, [&](const OpCall& c) {
         if (many) return tree_attention(*cache, Q, q_stride, parents, seqs, q_starts, sequences, rows, heads, scale, dtype, out, lse, c.ws + COUNTER_BYTES, c.dc, c.dc_next, static_cast<cudaStream_t>(stream));
         return cache_attention(*cache, Q, q_stride, parents, seqs, q_starts, sequences, rows, heads, max_q, scale, dtype, out, lse, c.ws + COUNTER_BYTES, c.dc, c.dc_next,

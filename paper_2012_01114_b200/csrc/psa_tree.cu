@@ -29,7 +29,7 @@ namespace {
 
 constexpr int ROWS = 128, KEYS = 128, BLOCKS = KEYS / CACHE_BLOCK;
 constexpr int MMA_WARP = 0, K_WARP = 1, V_WARP = 2, SET_WARP = 3, SOFT0 = 4, SOFTS = 8, TURN_K = SOFT0 + SOFTS, TURN_V = TURN_K + BLOCKS, V_WARPS = BLOCKS / 2, T_WARPS = TURN_V + V_WARPS, T_THREADS = 32 * T_WARPS;
-constexpr int EXACT = 2048;                     // tokens of a sequence up to which keys go in in two parts
+constexpr int EXACT = 2048;                     // tokens ahead of a sequence's tree up to which keys go in in two parts
 constexpr int T_SEQS = 512;                     // sequences of one launch
 constexpr int T_CTAS = 160;                     // at most
 // What work takes, in halves of a tile of keys: a tile, one with keys in two parts, and what a row tile takes beside its tiles; the least that a CTA is given.
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             const int held = there ? max(a.lens[slot], 0) : 0, len = (int)min((long long)held, (long long)a.width * a.page_size);
             strange |= (nq > 0 && (!there || held != len)) || nq != s1 - s0;
             const int tiles = max((int)(((uint32_t)len + KEYS - 1) / KEYS), 1), row_tiles = (nq * a.group + ROWS - 1) / ROWS;
-            n = (long long)row_tiles * a.kv_heads * ((long long)tiles * (a.f16 || len <= EXACT ? COST_EXACT : COST) + COST_ROW);
+            n = (long long)row_tiles * a.kv_heads * ((long long)tiles * (a.f16 || len - nq <= EXACT ? COST_EXACT : COST) + COST_ROW);
             len_s[b] = len;
             q0_s[b] = q0;
             nq_s[b] = nq;
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             x.q0 = q0_s[lo];
             x.slot = slot_s[lo];
             const int tiles = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1);
-            x.exact = a.f16 || x.len <= EXACT;
+            x.exact = a.f16 || x.len - x.nq <= EXACT;
             const int cost = x.exact ? COST_EXACT : COST;
             const long long units = (long long)tiles * cost + COST_ROW, inside = at - base_s[lo], row = inside / units, u0 = inside - row * units, u1 = min(units, u0 + (mine1 - at)), row0 = at - u0;
             const int row_tiles = (x.nq * a.group + ROWS - 1) / ROWS;

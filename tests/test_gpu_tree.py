@@ -14,6 +14,26 @@ pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
 
 
+@pytest.fixture(params=["sixteens", "tiles"], autouse=True)
+def form(request, monkeypatch):
+    """Both kernels: which one runs goes by the most rows and by the keys that the tables have room for."""
+    monkeypatch.setitem(FORM, "tiles", request.param == "tiles")
+
+
+FORM = {}
+
+
+def _made(*args):
+    c = Made(*args)
+    if FORM["tiles"]:
+        c.tables = torch.nn.functional.pad(c.tables, (0, 32768 // c.page - c.tables.shape[1]), value=-1)
+    return c
+
+
+def _most(n):
+    return 1024 if FORM["tiles"] else n
+
+
 def _trees(sizes, seed=0, **kw):
     r = random.Random(seed)
     return [ref.random_tree(n, r, **kw)[0] for n in sizes]
@@ -27,7 +47,7 @@ def _attend(c, trees, G, dtype, Q=None, max_q=None, scale=None, lse=None, out=No
     n = [len(t) for t in trees]
     Q = _queries(sum(n), c.Hkv * G, c.d, dtype, 3) if Q is None else Q
     parents = _ints([p for t in trees for p in t]) if parents is None else parents
-    return Q, psa.psa_tree_attention(Q, c.pool, c.tables, c.lens, c.seqs, sref.starts(n), parents, c.Hkv, c.page, max(n + [1]) if max_q is None else max_q, scale=scale, out=out, lse=lse)
+    return Q, psa.psa_tree_attention(Q, c.pool, c.tables, c.lens, c.seqs, sref.starts(n), parents, c.Hkv, c.page, _most(max(n + [1])) if max_q is None else max_q, scale=scale, out=out, lse=lse)
 
 
 def _check(c, trees, G, dtype, Q=None, max_q=None, scale=None, status=psa.OK):
@@ -49,14 +69,14 @@ def _check(c, trees, G, dtype, Q=None, max_q=None, scale=None, status=psa.OK):
 def test_trees(G, Hkv, d, page, dtype):
     """Also trees of one token, none, as many as are held, and more than are held (the first ones have no place, and their descendants see what there is)."""
     lens, sizes = [1, 15, 33, 64, 200, 0, 333, 6, 130], [1, 7, 33, 20, 13, 3, 0, 9, 64]
-    _check(Made(lens, Hkv, d, page, d), _trees(sizes, d), G, dtype)
+    _check(_made(lens, Hkv, d, page, d), _trees(sizes, d), G, dtype)
 
 
 @pytest.mark.parametrize("d,G", [(64, 4), (128, 8), (128, 1), (96, 2), (256, 2)])
 def test_long_and_short_together(d, G):
     """Rows that are cut into parts, the tree at the end of the last one, beside short ones; the same twice."""
     lens, sizes = [6000, 40, 900, 1], [26, 5, 64, 1]
-    c = Made(lens, 2, d, 64, 7)
+    c = _made(lens, 2, d, 64, 7)
     a = _check(c, _trees(sizes, 1), G, BF)
     assert torch.equal(a, _check(c, _trees(sizes, 1), G, BF))
 
@@ -65,20 +85,20 @@ def test_long_and_short_together(d, G):
 def test_where_the_tree_begins(G, d):
     """Every offset of the tree's first token inside a step of 32 tokens and a tile of 128, and trees that fill words of 32 bits."""
     lens = list(range(40, 73)) + [127, 128, 129, 160, 255, 256, 257]
-    c = Made(lens, 1, d, 16, 9)
+    c = _made(lens, 1, d, 16, 9)
     for size in (1, 2, 31, 32, 33):
         _check(c, _trees([size] * len(lens), size), G, HF)
 
 
 def test_shapes_of_trees():
-    c = Made([70, 90, 64, 80], 2, 64, 16, 11)
+    c = _made([70, 90, 64, 80], 2, 64, 16, 11)
     n = 40
     chain, star, forest = [i - 1 for i in range(n)], [-1] + [0] * (n - 1), [-1] * n
     _check(c, [chain, star, forest, _trees([n], 5, forest=True)[0]], 4, BF)
 
 
 def test_a_chain_is_the_causal_form():
-    c = Made([50, 300, 17], 2, 128, 16, 12)
+    c = _made([50, 300, 17], 2, 128, 16, 12)
     n = [5, 3, 4]
     Q, out = _attend(c, [[i - 1 for i in range(k)] for k in n], 2, BF)
     want = c.attend(Q, n, max_q=5)
@@ -86,20 +106,20 @@ def test_a_chain_is_the_causal_form():
 
 
 def test_large_trees():
-    c = Made([1500, 1024, 1030], 1, 64, 64, 13)
+    c = _made([1500, 1024, 1030], 1, 64, 64, 13)
     r = random.Random(2)
     trees = [[i - 1 for i in range(1024)], ref.random_tree(1000, r, depth=40)[0], ref.random_tree(517, r)[0]]
     _check(c, trees, 2, BF)
 
 
 def test_one_that_is_too_large_is_left_out():
-    c = Made([1500, 40, 60], 1, 64, 64, 14)
+    c = _made([1500, 40, 60], 1, 64, 64, 14)
     trees = [[i - 1 for i in range(1025)], _trees([7])[0], _trees([9], 1)[0]]
     n = [len(t) for t in trees]
     out = torch.full((sum(n) + 3, 2 * 64), 9.0, dtype=BF, device="cuda")
     Q = _queries(sum(n) + 3, 2, 64, BF)
     parents = _ints([p for t in trees for p in t] + [0] * 3)
-    psa.psa_tree_attention(Q, c.pool, c.tables, c.lens, c.seqs, sref.starts(n), parents, 1, 64, 9, out=out)
+    psa.psa_tree_attention(Q, c.pool, c.tables, c.lens, c.seqs, sref.starts(n), parents, 1, 64, _most(9), out=out)
     assert psa.psa_last_issued()[0] == psa.ERR_SHAPE
     assert (out[:1025] == 9).all() and (out[-3:] == 9).all()
     assert torch.isfinite(out[1025:-3]).all() and not (out[1025:-3] == 9).any(-1).any()
@@ -107,7 +127,7 @@ def test_one_that_is_too_large_is_left_out():
 
 def test_parents_that_are_none():
     """Later tokens, itself and numbers below -1: taken for -1, and reported."""
-    c = Made([60], 1, 64, 16, 15)
+    c = _made([60], 1, 64, 16, 15)
     bad = [-1, 0, 2, -7, 3, 9, 5, 1 << 30]
     good = [-1, 0, -1, -1, 3, -1, 5, -1]
     Q, out = _attend(c, [good], 4, BF)
@@ -119,7 +139,7 @@ def test_parents_that_are_none():
 @pytest.mark.parametrize("G,n", [(1, 6), (4, 6), (4, 40)])
 @pytest.mark.parametrize("which", [0, 1])
 def test_a_nan_is_seen_by_its_descendants(which, G, n):
-    c = Made([100], 1, 64, 16, 16)
+    c = _made([100], 1, 64, 16, 16)
     tree = ref.random_tree(n, random.Random(4))[0]
     K, V = torch.randn(1, 1, 64, device="cuda").to(BF), torch.randn(1, 1, 64, device="cuda").to(BF)
     Q, plain = _attend(c, [tree], G, BF)
@@ -136,7 +156,7 @@ def test_a_nan_is_seen_by_its_descendants(which, G, n):
 
 
 def test_scale_strides_and_small_numbers():
-    c = Made([50, 700], 2, 64, 16, 17)
+    c = _made([50, 700], 2, 64, 16, 17)
     trees = _trees([9, 30], 6)
     _check(c, trees, 4, BF, scale=0.9)
     buf = _queries(39, 20, 64, BF, 5)
@@ -147,7 +167,7 @@ def test_scale_strides_and_small_numbers():
 
 @pytest.mark.parametrize("G", [1, 4])
 def test_bounds_that_are_too_small_or_large(G):
-    c = Made([50, 700, 90], 2, 128, 16, 18)
+    c = _made([50, 700, 90], 2, 128, 16, 18)
     trees = _trees([9, 30, 2], 7)
     for max_q in (1, 30, 1024):
         _check(c, trees, G, BF, max_q=max_q)
@@ -156,12 +176,12 @@ def test_bounds_that_are_too_small_or_large(G):
 def test_many_sequences():
     r = random.Random(19)
     lens = [r.choice([0, 3, 40, 130, 300]) for _ in range(600)]
-    _check(Made(lens, 1, 32, 16, 19), _trees([r.choice([0, 1, 5, 12, 40]) for _ in lens], 8), 2, BF)
+    _check(_made(lens, 1, 32, 16, 19), _trees([r.choice([0, 1, 5, 12, 40]) for _ in lens], 8), 2, BF)
 
 
 def test_missing_pages_and_slots():
     """Tokens of a page that does not exist are left out; a slot that does not exist has no tokens; both are reported."""
-    c = Made([60, 50, 40], 1, 64, 16, 20)
+    c = _made([60, 50, 40], 1, 64, 16, 20)
     trees = _trees([6, 4, 5], 9)
     Q, good = _attend(c, trees, 4, BF)
     c.tables[c.slot[0], 1] = -1
@@ -177,14 +197,14 @@ def test_missing_pages_and_slots():
 
 
 def test_captured_and_on_another_stream():
-    c = Made([2000, 90], 2, 128, 64, 21)
+    c = _made([2000, 90], 2, 128, 64, 21)
     trees = _trees([20, 9], 10)
     parents = _ints([p for t in trees for p in t])
     Q, want = _attend(c, trees, 4, BF, parents=parents)
     out, s = torch.zeros_like(want), torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     starts = sref.starts([20, 9])
-    call = lambda: psa.psa_tree_attention(Q, c.pool, c.tables, c.lens, c.seqs, starts, parents, 2, 64, 20, out=out)  # noqa: E731
+    call = lambda: psa.psa_tree_attention(Q, c.pool, c.tables, c.lens, c.seqs, starts, parents, 2, 64, _most(20), out=out)  # noqa: E731
     with torch.cuda.stream(s):
         call()
     s.synchronize()
@@ -202,8 +222,8 @@ def test_captured_and_on_another_stream():
 
 
 def test_starts_that_descend_are_reported():
-    c = Made([60, 50], 1, 64, 16, 22)
+    c = _made([60, 50], 1, 64, 16, 22)
     Q = _queries(10, 4, 64, BF)
     out = torch.full((10, 256), 3.0, dtype=BF, device="cuda")
-    psa.psa_tree_attention(Q, c.pool, c.tables, c.lens, c.seqs, _ints([0, 8, 5]), _ints([-1] * 10), 1, 16, 8, out=out)
+    psa.psa_tree_attention(Q, c.pool, c.tables, c.lens, c.seqs, _ints([0, 8, 5]), _ints([-1] * 10), 1, 16, _most(8), out=out)
     assert psa.psa_last_issued()[0] == psa.ERR_SHAPE and (out == 3).all()
