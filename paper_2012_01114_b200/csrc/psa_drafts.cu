@@ -29,7 +29,7 @@ namespace psa {
 namespace {
 
 constexpr int MOST_CLUSTER = 8;
-constexpr int V_CTAS = 3;                       // an SM
+constexpr int V_CTAS = 4;                       // an SM: with 64 registers a thread.  (With three, 80 registers and two rounds 156 us where this takes 128)
 // Relative error of a sum of 32-bit exponentials: their argument goes through two roundings of 2^-24 of itself, 30 at most where a weight counts (2^-18.6 of the weight), ex2 gives 2^-22, a number
 // takes part in no more than 36 additions before the sums go on in 64 bits and in 13 of the threads', warps' and CTAs' sums (2^-18.4): below 2^-17 altogether.
 constexpr float COARSE = 1.f / 65536;
@@ -773,10 +773,11 @@ cudaLaunchConfig_t config(dim3 grid, int threads, size_t smem, cudaStream_t stre
 
 template <class T>
 int launch_verify(VerifyArgs a, DeviceCounters* dc, DeviceCounters* dc_next, cudaStream_t stream) {
-    // As many CTAs a sequence as make two rounds of those that the GPU holds (sequences end at different levels), of 2048 numbers at least; with no more than one an SM, of 16 warps, else of 8.
-    // (us a call, with one / two / four rounds: 64 chains of 6, 128,000 numbers 182, 174, 196; with 8 and 16 warps: the same 139, 175, 16 trees of 33, 50,001 numbers 74, 59.)
+    // As many CTAs a sequence as the GPU holds at a time, eight at most and of 2048 numbers at least; with no more than one an SM, of 16 warps, else of 8.  (us of chains in bf16 with drafts, with at most
+    // one / two rounds of CTAs: 100 of 128,000 numbers 193, 219, 200 of 64,000 176, 190, 400 of 32,000 156, 166; with 8 / 16 warps: 4 of 128,000 90, 59, 64 of 128,000 152, 219, 16 trees of
+    // 50,000 numbers in fp32 82, 68; with one CTA a sequence 64 of 128,000 498.  Sixteen CTAs a sequence take longer than eight: a level costs a warp 800 instructions beside 9 a 32 numbers.)
     int ranks = 1;
-    while (ranks < MOST_CLUSTER && 2LL * ranks * a.sequences <= 2 * V_CTAS * 148 && a.vocab > 2048 * ranks) ranks *= 2;
+    while (ranks < MOST_CLUSTER && 2LL * ranks * a.sequences <= V_CTAS * 148 && a.vocab > 2048 * ranks) ranks *= 2;
     const bool few = (long long)ranks * a.sequences <= 148;
     a.slice = ((a.vocab + ranks - 1) / ranks + 7) / 8 * 8;
     cudaLaunchAttribute attr[2];
