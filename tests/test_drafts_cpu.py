@@ -129,3 +129,10 @@ def test_reference_trees():
     for n in (1, 2, 30):
         parents, level = ref.random_tree(n, r)
         assert len(parents) == n and all(-1 <= p < i for i, p in enumerate(parents)) and all(level[i] == (0 if p < 0 else level[p] + 1) for i, p in enumerate(parents))
+
+
+def test_workspace_of_a_tree(lib):
+    for d in (32, 64, 96, 128, 256):
+        assert lib.psa_tree_workspace_bytes(d) >= lib.psa_cache_workspace_bytes(d) > 0
+    for d in (0, -64, 16, 48, 512):
+        assert lib.psa_tree_workspace_bytes(d) == 0
