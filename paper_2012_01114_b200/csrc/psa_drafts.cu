@@ -647,24 +647,36 @@ struct KeepArgs {
 struct Kept {
     int slot, first, count, base, keep;         // keep: tokens that stay, 0: none of this sequence's arguments hold
 };
-// One sequence, by a warp: its path ascends from 0 and ends inside the tree.
-__device__ __forceinline__ Kept kept_of(const KeepArgs& a, int b, int lane) {
+__device__ __forceinline__ Kept claimed(const KeepArgs& a, int b) {
     Kept k;
     k.slot = a.seqs[b];
     k.first = min(max(a.starts[b], 0), a.rows);
     k.count = max(min(max(a.starts[b + 1], 0), a.rows) - k.first, 0);
     const bool known = k.slot >= 0 && k.slot < a.slots;
-    const int len = known ? a.lens[k.slot] : 0;
+    const int len = known ? a.lens[k.slot] : 0, stand = a.accepted[b];
     k.base = len - k.count;
-    k.keep = 0;
-    const int stand = a.accepted[b];
-    if (!known || k.base < 0 || (long long)len > (long long)a.width * a.page_size || stand < 0 || stand >= k.count) return k;
+    k.keep = known && k.base >= 0 && (long long)len <= (long long)a.width * a.page_size && stand >= 0 && stand < k.count ? stand + 1 : 0;
+    return k;
+}
+// Whether a path goes on at its place i: it ascends from 0 and ends inside the tree.
+__device__ __forceinline__ bool ascends(const KeepArgs& a, const Kept& k, int i) {
+    const int p = a.path[k.first + i];
+    return i == 0 ? p == 0 : p > a.path[k.first + i - 1] && p < k.count;
+}
+// One sequence, by a warp, and by a thread.
+__device__ __forceinline__ Kept kept_of(const KeepArgs& a, int b, int lane) {
+    Kept k = claimed(a, b);
     bool good = true;
-    for (int i = lane; i <= stand; i += 32) {
-        const int p = a.path[k.first + i];
-        good &= i == 0 ? p == 0 : p > a.path[k.first + i - 1] && p < k.count;
-    }
-    if (__all_sync(0xffffffffu, good)) k.keep = stand + 1;
+    for (int i = lane; i < k.keep; i += 32) good &= ascends(a, k, i);
+    if (!__all_sync(0xffffffffu, good)) k.keep = 0;
+    return k;
+}
+__device__ __forceinline__ Kept kept_of(const KeepArgs& a, int b) {
+    Kept k = claimed(a, b);
+    bool good = true;
+#pragma unroll 4
+    for (int i = 0; i < k.keep; ++i) good &= ascends(a, k, i);
+    if (!good) k.keep = 0;
     return k;
 }
 
@@ -747,11 +759,10 @@ __global__ void __launch_bounds__(32 * KEEP_WARPS) cache_keep_kernel(const KeepA
         __threadfence();
     }
     __syncthreads();
-    if (last_s)
-        for (int b = warp; b < a.sequences; b += KEEP_WARPS) {
-            const Kept k = kept_of(a, b, lane);
-            __syncwarp();
-            if (lane == 0 && k.keep > 0) a.new_lens[k.slot] = k.base + k.keep;
+    if (last_s)                                  // (a thread a sequence: with a warp a sequence this took 14 of 20 us for 64 of them)
+        for (int b = threadIdx.x; b < a.sequences; b += 32 * KEEP_WARPS) {
+            const Kept k = kept_of(a, b);
+            if (k.keep > 0) a.new_lens[k.slot] = k.base + k.keep;
         }
 }
 
