@@ -698,15 +698,18 @@ __global__ void __launch_bounds__(32 * KEEP_WARPS) cache_keep_kernel(const KeepA
         const Kept k = kept_of(a, b, lane);
         if (k.count > 0 && k.keep == 0 && rest == 0 && lane == 0) atomicExch(&dc->status, (int)PSA_ERR_SHAPE);
         uint8_t* const pool = a.pool + (size_t)layer * a.layer_bytes;
-        // where the lane's elements of a token lie: behind its block's beginning, for an even token and an odd one
-        auto place = [&](int round, int tok) {
-            const int e = round * 32 + lane;
-            if (e < 4 * G) return B::K_CODES + tok * (D / 2) + 4 * e;
-            if (e < WORDS) return B::K_SCALES + tok * 4 * G + 4 * (e - 4 * G);
-            if (e < WORDS + 8 * G) return B::V_CODES + (tok >> 1) * D + 4 * (e - WORDS) + 2 * (tok & 1);
-            return B::V_SCALES + (tok >> 1) * 8 * G + 4 * (e - WORDS - 8 * G) + 2 * (tok & 1);
-        };
-        for (int i0 = 0; i0 < k.keep; i0 += KEEP_TOKENS) {
+        // where the lane's element of each round lies behind its block's beginning: base, and what a pair of tokens and the odd one of a pair add
+        int base[ROUNDS], of_pair[ROUNDS], of_odd[ROUNDS];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int e = r * 32 + lane;
+            if (e < 4 * G) { base[r] = B::K_CODES + 4 * e; of_pair[r] = D; of_odd[r] = D / 2; }
+            else if (e < WORDS) { base[r] = B::K_SCALES + 4 * (e - 4 * G); of_pair[r] = 8 * G; of_odd[r] = 4 * G; }
+            else if (e < WORDS + 8 * G) { base[r] = B::V_CODES + 4 * (e - WORDS); of_pair[r] = D; of_odd[r] = 2; }
+            else { base[r] = B::V_SCALES + 4 * (e - WORDS - 8 * G); of_pair[r] = 8 * G; of_odd[r] = 2; }
+        }
+        auto place = [&](int r, int tok) { return base[r] + (tok >> 1) * of_pair[r] + (tok & 1) * of_odd[r]; };
+        for (int i0 = 1; i0 < k.keep; i0 += KEEP_TOKENS) {       // (the root stays where it is)
             // lane l looks up: source of token i0 + l, destination of token i0 + l - KEEP_TOKENS
             const int i = i0 + lane % KEEP_TOKENS;
             uint8_t* at = nullptr;
@@ -731,23 +734,25 @@ __global__ void __launch_bounds__(32 * KEEP_WARPS) cache_keep_kernel(const KeepA
                 const int from_tok = __shfl_sync(0xffffffffu, tok, t);
                 to_tok[t] = __shfl_sync(0xffffffffu, tok, t + KEEP_TOKENS);
                 if (!from) to[t] = nullptr;
+                if (!to[t]) continue;
 #pragma unroll
                 for (int r = 0; r < ROUNDS; ++r) {
                     const int e = r * 32 + lane;
-                    x[t][r] = 0;
-                    if (to[t] && e < WORDS) x[t][r] = *reinterpret_cast<const uint32_t*>(from + place(r, from_tok));
-                    else if (to[t] && e < WORDS + HALVES) x[t][r] = *reinterpret_cast<const uint16_t*>(from + place(r, from_tok));
+                    if (e < WORDS) x[t][r] = *reinterpret_cast<const uint32_t*>(from + place(r, from_tok));
+                    else if (e < WORDS + HALVES) x[t][r] = *reinterpret_cast<const uint16_t*>(from + place(r, from_tok));
                 }
             }
             __syncwarp();
 #pragma unroll
-            for (int t = 0; t < KEEP_TOKENS; ++t)
+            for (int t = 0; t < KEEP_TOKENS; ++t) {
+                if (!to[t]) continue;
 #pragma unroll
                 for (int r = 0; r < ROUNDS; ++r) {
                     const int e = r * 32 + lane;
-                    if (to[t] && e < WORDS) *reinterpret_cast<uint32_t*>(to[t] + place(r, to_tok[t])) = x[t][r];
-                    else if (to[t] && e < WORDS + HALVES) *reinterpret_cast<uint16_t*>(to[t] + place(r, to_tok[t])) = (uint16_t)x[t][r];
+                    if (e < WORDS) *reinterpret_cast<uint32_t*>(to[t] + place(r, to_tok[t])) = x[t][r];
+                    else if (e < WORDS + HALVES) *reinterpret_cast<uint16_t*>(to[t] + place(r, to_tok[t])) = (uint16_t)x[t][r];
                 }
+            }
             __syncwarp();
         }
     }
