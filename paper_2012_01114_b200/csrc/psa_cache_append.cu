@@ -117,19 +117,23 @@ __device__ __forceinline__ void turn_queries(const AppendArgs& a, const RotaryAr
     const uint32_t id = (blockIdx.x - ro.key_blocks) * (32 * APPEND_WARPS) + threadIdx.x;
     const uint32_t rest = fastdiv(id, ro.by_slots), row_of = fastdiv(rest, ro.by_groups);
     const int slot = (int)(id - rest * ro.by_slots.d), h0 = (int)(rest - row_of * ro.by_groups.d);
+    // the last sequence that begins at or before the row: for the warp's first row together, from there on by each thread
+    const int r = (int)min(row_of, (uint32_t)a.rows - 1), r0 = __shfl_sync(0xffffffffu, r, 0);
+    int lo = 0;
+    for (int n = a.sequences; n > 1;) {
+        const int step = (n + 31) / 32, lane = threadIdx.x & 31;
+        const uint32_t m = __ballot_sync(0xffffffffu, lane * step < n && a.starts[lo + min(lane * step, n - 1)] <= r0);
+        const int k = m ? 31 - __clz(m) : 0;
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
     if (row_of >= (uint32_t)a.rows) return;
-    const int r = (int)row_of;
+    while (lo + 1 < a.sequences && a.starts[lo + 1] <= r) ++lo;
     const bool turns = 8 * slot < ro.rot;
     long long f[4] = {0, 0, 0, 0};
     if (turns)
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = turns_of(ro.freqs[4 * slot + e]);
-    int lo = 0, n = a.sequences;                // the last sequence that begins at or before the row
-    while (n > 1) {
-        const int half = n / 2;
-        if (a.starts[lo + half] <= r) lo += half;
-        n -= half;
-    }
     const int first = max(a.starts[lo], 0), end = min(max(a.starts[lo + 1], 0), a.rows), seq = a.seqs[lo];
     if (r < first || r >= end || seq < 0 || seq >= a.slots) return;
     const long long position = (long long)a.lens[seq] - (end - first) + (ro.depths ? ro.depths[r] : r - first);
@@ -399,6 +403,8 @@ cudaError_t launch_append(const AppendArgs& a, RotaryArgs ro, DeviceCounters* dc
         long long groups = ro.heads;
         if (groups * slots * a.rows > full) groups = std::max(std::max((long long)(ro.heads + 7) / 8, std::min(groups, full / (slots * a.rows))), 1LL);
         if (groups * slots * a.rows > most) groups = std::max(most / (slots * a.rows), 1LL);
+        const long long each = (ro.heads + groups - 1) / groups;                       // (as many heads for all, up to the last group)
+        groups = (ro.heads + each - 1) / each;
         if (groups * slots * a.rows > most) return cudaErrorInvalidConfiguration;      // (refused ahead of this)
         ro.by_slots = fastdiv_make((uint32_t)slots);
         ro.by_groups = fastdiv_make((uint32_t)groups);
