@@ -77,6 +77,7 @@ struct TBars {
 struct TItem {
     int len, nq, q0, slot, t0, nt, h, qt, ctx, tok0;       // ctx: the tree's first token; tok0: the row tile's first
     int first_cta, part, parts;                             // of the row tile; a CTA has one part of it
+    int row, rows;                                          // the row tile's place among those of its sequence (heads times row tiles), and their number
     bool meets_tree, exact;                                 // exact: keys in two parts
 };
 
@@ -97,6 +98,14 @@ __device__ __forceinline__ float2 t_pair(uint64_t x) {
     float2 r;
     asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
     return r;
+}
+// Sixteen rows, 32 columns of fp32 in the quad layout.
+__device__ __forceinline__ void t_ld_quad32(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+                   "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr)
+                 : "memory");
 }
 __device__ __forceinline__ uint64_t t_add2(uint64_t x, uint64_t y) {
     uint64_t r;
@@ -124,6 +133,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     __shared__ long long base_s[T_SEQS + 1], scan_s[T_WARPS];
     __shared__ int len_s[T_SEQS], q0_s[T_SEQS], nq_s[T_SEQS], slot_s[T_SEQS];
     __shared__ __align__(8) uint8_t have_s[2][16][BLOCKS];       // blocks of a tile that are there, by tile modulo 16; as the warp found them that fetches V, or K
+    __shared__ int any_nan_s[2];                // by items in turn: whether there are marks in
     __shared__ uint32_t nan_s[2][G][PSA_TREE_MOST / 32];         // by items in turn: tokens of the tree whose group of V reads back as NaN or infinite
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -192,33 +202,53 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     const uint32_t tmem = tmem_s;
 
     // ---- Every role walks the CTA's items by itself: its share of the list.  A row tile is COST_ROW units and COST or COST_EXACT for each tile of keys, which belongs to the CTA that has its first unit.
+    // Behind an item comes the next row tile from its beginning: only the first one takes divisions, and those that are cut.
     auto next_item = [&](long long& at, TItem& x) -> bool {
         while (at < mine1) {
-            int lo = 0, hi = a.sequences - 1;    // the last sequence that begins at or before it (and has tiles: those without begin where the next one does)
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) / 2;
-                if (base_s[mid] <= at) lo = mid; else hi = mid - 1;
+            int u0 = 0;
+            const bool first = x.rows < 0;
+            if (x.row + 1 < x.rows) {
+                ++x.row;
+                if (++x.qt * ROWS >= x.nq * a.group) { x.qt = 0; ++x.h; }
+            } else {
+                int lo = 0, hi = a.sequences - 1;    // the last sequence that begins at or before it (and has tiles: those without begin where the next one does)
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) / 2;
+                    if (base_s[mid] <= at) lo = mid; else hi = mid - 1;
+                }
+                x.len = len_s[lo];
+                x.nq = nq_s[lo];
+                x.q0 = q0_s[lo];
+                x.slot = slot_s[lo];
+                x.ctx = x.len - x.nq;
+                x.exact = a.f16 || x.ctx <= EXACT;
+                x.row = x.h = x.qt = 0;
+                const int row_tiles = (x.nq * a.group + ROWS - 1) / ROWS;
+                x.rows = row_tiles * a.kv_heads;
+                if (first) {
+                    const int units = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1) * (x.exact ? COST_EXACT : COST) + COST_ROW;
+                    const long long inside = at - base_s[lo];
+                    x.row = (int)(inside / units);
+                    u0 = (int)(inside - (long long)x.row * units);
+                    x.h = x.row / row_tiles;
+                    x.qt = x.row - x.h * row_tiles;
+                }
             }
-            x.len = len_s[lo];
-            x.nq = nq_s[lo];
-            x.q0 = q0_s[lo];
-            x.slot = slot_s[lo];
-            const int tiles = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1);
-            x.exact = a.f16 || x.len - x.nq <= EXACT;
-            const int cost = x.exact ? COST_EXACT : COST;
-            const long long units = (long long)tiles * cost + COST_ROW, inside = at - base_s[lo], row = inside / units, u0 = inside - row * units, u1 = min(units, u0 + (mine1 - at)), row0 = at - u0;
-            const int row_tiles = (x.nq * a.group + ROWS - 1) / ROWS;
+            const int cost = x.exact ? COST_EXACT : COST, units = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1) * cost + COST_ROW, u1 = (int)min((long long)units, u0 + (mine1 - at));
+            const long long row0 = at - u0;
             at += u1 - u0;
-            x.t0 = (int)((max(u0 - COST_ROW, 0LL) + cost - 1) / cost);
-            const int t1 = (int)((max(u1 - COST_ROW, 0LL) + cost - 1) / cost);
+            auto tile_of = [&](int u) { return x.exact ? (max(u - COST_ROW, 0) + COST_EXACT - 1) / COST_EXACT : (max(u - COST_ROW, 0) + COST - 1) / COST; };
+            x.t0 = tile_of(u0);
+            const int t1 = tile_of(u1);
             if (t1 <= x.t0) continue;
             x.nt = x.len > 0 ? t1 - x.t0 : 0;
-            x.h = (int)row / row_tiles;
-            x.qt = (int)row - x.h * row_tiles;
-            x.ctx = x.len - x.nq;
             x.tok0 = (int)fastdiv((uint32_t)(x.qt * ROWS), a.by_group);
-            x.first_cta = (int)((row0 + COST_ROW) / per);
-            x.parts = (int)((row0 + units - cost) / per) - x.first_cta + 1;
+            x.first_cta = (int)blockIdx.x;
+            x.parts = 1;
+            if (u1 - u0 < units) {
+                x.first_cta = (int)((row0 + COST_ROW) / per);
+                x.parts = (int)((row0 + units - cost) / per) - x.first_cta + 1;
+            }
             x.part = (int)blockIdx.x - x.first_cta;
             x.meets_tree = x.nt > 0 && t1 * (long long)KEYS > x.ctx;
             return true;
@@ -227,6 +257,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     };
     long long at = mine0;
     TItem x;
+    x.row = 0;
+    x.rows = -1;
     uint32_t n = 0;                             // tiles of the CTA so far: the phases of all barriers follow from it, but those that go by items
     bool ok = true;
 
@@ -316,6 +348,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             if (it > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_free, (it - 1) & 1, abortp));
             if (!ok) break;
             for (int i = lane; i < G * (PSA_TREE_MOST / 32); i += 32) (&nan_s[it & 1][0][0])[i] = 0u;
+            if (lane == 0) any_nan_s[it & 1] = 0;
             if (x.meets_tree) {
                 const int words = (x.nq + 31) / 32, last = min((int)fastdiv((uint32_t)(x.qt * ROWS + ROWS - 1), a.by_group), x.nq - 1);
                 for (int tok = x.tok0 + lane; tok <= last; tok += 32) {
@@ -409,7 +442,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             to_chunk[z] = (chunk >> 3) * Cfg::SUBTILE + (int)swz128_offset(2 * pair, chunk & 7);
         }
         // block `me` of tile m; first: its first token
-        auto turn_v = [&](uint32_t m, int me, long long first, int ctx, int len, int nq, uint32_t (*nan)[PSA_TREE_MOST / 32]) {
+        auto turn_v = [&](uint32_t m, int me, long long first, int ctx, int len, int nq, uint32_t (*nan)[PSA_TREE_MOST / 32], int& any_nan) {
             const int s = m % Cfg::RING;
             const uint8_t* const from = smem + Cfg::RAW_V + (s * BLOCKS + me) * Cfg::HALF;
             uint8_t* const to = smem + Cfg::V + (m & 1) * Cfg::TILE + me * (CACHE_BLOCK * 128);
@@ -440,6 +473,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                         sm[z].x &= ~drop;
                         sm[z].y &= ~drop;
                         const int at0 = (int)(tok - ctx);
+                        any_nan = 1;
                         if ((bad & 0x8000u) && at0 < nq) atomicOr(&nan[w][at0 >> 5], 1u << (at0 & 31));
                         if ((bad & 0x80000000u) && at0 + 1 < nq) atomicOr(&nan[w][(at0 + 1) >> 5], 1u << ((at0 + 1) & 31));
                     }
@@ -473,7 +507,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 if (ok && n >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&bars.v_empty[n & 1], ((n >> 1) - 1) & 1, abortp));
                 if (!ok) break;
 #pragma unroll 1
-                for (int me = warp - TURN_V; me < BLOCKS; me += V_WARPS) turn_v(n, me, first + me * CACHE_BLOCK, x.ctx, x.len, x.nq, nan_s[it & 1]);
+                for (int me = warp - TURN_V; me < BLOCKS; me += V_WARPS) turn_v(n, me, first + me * CACHE_BLOCK, x.ctx, x.len, x.nq, nan_s[it & 1], any_nan_s[it & 1]);
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(&bars.v_full[n & 1]); mbar_arrive(&bars.v_raw_free[s]); }
@@ -560,7 +594,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 for (int half = 0; half < 2; ++half) {
                     tmem_ld_quad64(tS + 64 * half, s);
                     tc_wait_ld();
-                    if (masked) {
+                    const bool mask = masked && (have != 0x0101010101010101ull || key0 + 64 * half + 64 > x.ctx);
+                    if (mask) {
                         // the tile's tokens that a row sees, 32 a word: all ahead of the tree, and the row's set in it; none of blocks that are not there
 #pragma unroll
                         for (int z = 0; z < 2; ++z) {
@@ -648,49 +683,51 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             const size_t outA = ((size_t)(x.q0 + tokA) * a.kv_heads * a.group + (size_t)x.h * a.group + (rhoA - tokA * a.group)), outB = ((size_t)(x.q0 + tokB) * a.kv_heads * a.group + (size_t)x.h * a.group + (rhoB - tokB * a.group));
             const float iA = lA == 0.f ? 0.f : 1.f / lA, iB = lB == 0.f ? 0.f : 1.f / lB;
             uint32_t nanA = 0, nanB = 0;     // groups of V in which the row sees a NaN
-            if (x.meets_tree)
+            if (x.meets_tree && any_nan_s[it & 1]) {
                 for (int i = lane & 3; i < words; i += 4)
 #pragma unroll
                     for (int w = 0; w < G; ++w) {
                         if (nan_s[it & 1][w][i] & setA[i]) nanA |= 1u << w;
                         if (nan_s[it & 1][w][i] & setB[i]) nanB |= 1u << w;
                     }
-            nanA |= __shfl_xor_sync(0xffffffffu, nanA, 1); nanA |= __shfl_xor_sync(0xffffffffu, nanA, 2);
-            nanB |= __shfl_xor_sync(0xffffffffu, nanB, 1); nanB |= __shfl_xor_sync(0xffffffffu, nanB, 2);
+                nanA |= __shfl_xor_sync(0xffffffffu, nanA, 1); nanA |= __shfl_xor_sync(0xffffffffu, nanA, 2);
+                nanB |= __shfl_xor_sync(0xffffffffu, nanB, 1); nanB |= __shfl_xor_sync(0xffffffffu, nanB, 2);
+            }
+            // (32 columns at a time, in a loop that is not unrolled: this code is fetched anew for every item, and its length is its time)
+            const size_t rowA = whole ? outA * D : (size_t)rA * D, rowB = whole ? outB * D : (size_t)rB * D;
 #pragma unroll 1
-            for (int c = 0; c < Cfg::SUB; ++c) {
-                uint32_t v[32];
+            for (int w = 0; w < G; ++w) {
+                uint32_t v[16];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = 0u;
+                for (int i = 0; i < 16; ++i) v[i] = 0u;
                 if (x.nt > 0) {
-                    tmem_ld_quad64(tO + 64 * c, v);
+                    t_ld_quad32(tO + 32 * w, v);
                     tc_wait_ld();
                 }
+                const float gA = nanA >> w & 1u ? NAN : whole ? iA : 1.f, gB = nanB >> w & 1u ? NAN : whole ? iB : 1.f;
 #pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    const int col = 64 * c + 8 * g + cq;
-                    if (D < Cfg::DT && col >= D) continue;
-                    float x0 = __uint_as_float(v[4 * g]), x1 = __uint_as_float(v[4 * g + 1]), y0 = __uint_as_float(v[4 * g + 2]), y1 = __uint_as_float(v[4 * g + 3]);
-                    if (nanA >> (col >> 5) & 1u) x0 = x1 = NAN;
-                    if (nanB >> (col >> 5) & 1u) y0 = y1 = NAN;
+                for (int g = 0; g < 4; ++g) {
+                    const int col = 32 * w + 8 * g + cq;
+                    const float x0 = __uint_as_float(v[4 * g]) * gA, x1 = __uint_as_float(v[4 * g + 1]) * gA, y0 = __uint_as_float(v[4 * g + 2]) * gB, y1 = __uint_as_float(v[4 * g + 3]) * gB;
                     if (whole) {
                         auto both = [&](float u, float w) { return a.f16 ? t_bits(__floats2half2_rn(u, w)) : pack_bf16x2(u, w); };
-                        if (isA) *reinterpret_cast<uint32_t*>(a.out + outA * D + col) = both(x0 * iA, x1 * iA);
-                        if (isB) *reinterpret_cast<uint32_t*>(a.out + outB * D + col) = both(y0 * iB, y1 * iB);
+                        if (isA) *reinterpret_cast<uint32_t*>(a.out + rowA + col) = both(x0, x1);
+                        if (isB) *reinterpret_cast<uint32_t*>(a.out + rowB + col) = both(y0, y1);
                     } else {
-                        if (isA) __stcg(reinterpret_cast<float2*>(to + rA * D + col), make_float2(x0, x1));
-                        if (isB) __stcg(reinterpret_cast<float2*>(to + rB * D + col), make_float2(y0, y1));
+                        if (isA) __stcg(reinterpret_cast<float2*>(to + rowA + col), make_float2(x0, x1));
+                        if (isB) __stcg(reinterpret_cast<float2*>(to + rowB + col), make_float2(y0, y1));
                     }
                 }
             }
-            if ((lane & 3) == 0) {
-                auto stats = [&](bool is, int r, size_t out, float m, float l) {
-                    if (!is) return;
+            // the rows' maxima and sums: the first lane of a quad those of row A, the second of row B
+            if ((lane & 3) < 2) {
+                const bool second = lane & 1;
+                const float m = second ? mB : mA, l = second ? lB : lA;
+                const int r = second ? rB : rA;
+                if (second ? isB : isA) {
                     if (!whole) { __stcg(to + ROWS * D + r, m); __stcg(to + ROWS * (D + 1) + r, l); }
-                    else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) - UP + log2f(l)) * T_LN2;
-                };
-                stats(isA, rA, outA, mA, lA);
-                stats(isB, rB, outB, mB, lB);
+                    else if (a.lse) a.lse[second ? outB : outA] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) - UP + log2f(l)) * T_LN2;
+                }
             }
             tc_fence_before();
             __syncwarp();
