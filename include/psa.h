@@ -58,7 +58,7 @@ typedef enum {
     PSA_ERR_WORKSPACE = 6,   /* registered workspace too small and growing it failed           */
     PSA_ERR_CUDA = 7,        /* a CUDA runtime/driver call failed (psa_last_cuda_error)        */
     PSA_ERR_TIMEOUT = 8,     /* a bounded device-side wait expired; results are invalid        */
-    PSA_ERR_NUMERIC = 9      /* reserved                                                       */
+    PSA_ERR_NUMERIC = 9      /* a row of numbers is no distribution (psa_verify_drafts)        */
 } psa_status;
 
 /*
@@ -292,15 +292,17 @@ int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
  *   - `out` is dense, [rows, heads * d_k]; `lse`, where given, dense fp32 [rows, heads]: log(sum_j exp(scale q_i k_j)), natural, by which
  *     results over different keys can be joined.  A row that sees no key gets zeros and -inf.
  *   - What a row does not see has no influence on it, NaN and infinities included.
- *   - A weight is rounded to 16 bits for the product with V: to dtype by psa_prompt_attention, to fp16 by psa_cache_attention.  In fp16 it keeps 11 bits down to 2^-21
- *     of the largest weight among the keys that are worked on together, and an error of 2^-32 of that one below.
+ *   - A weight is rounded to 16 bits for the product with V: to dtype by psa_prompt_attention, to fp16 by psa_cache_attention and psa_tree_attention.  In fp16 it keeps 11 bits
+ *     down to 2^-21 of the largest weight among the keys that are worked on together, and an error of 2^-32 of that one below.  Held values are rounded to fp16 ahead of that product, and keys ahead of
+ *     theirs by psa_tree_attention with PSA_BF16 where more than 2048 tokens lie ahead of a tree and scale^2 d_k <= 2
+ *     (2^-11 of a number; queries in bf16 have lost 2^-8).
  *   - Lengths, tables and lists are read on the device, in stream order; the host needs none of them.  A call with zero rows (or an empty list) returns PSA_OK and
  *     launches nothing.  Device-side arguments that name no place (a sequence or page that does not exist, a token beyond the table)
- *     are left out, and psa_last_issued returns PSA_ERR_SHAPE for that call.  So it does for `starts` of psa_prompt_attention and psa_cache_attention that descend
+ *     are left out, and psa_last_issued returns PSA_ERR_SHAPE for that call.  So it does for `starts` of psa_prompt_attention, psa_cache_attention and psa_tree_attention that descend
  *     somewhere: the rows between starts[512 c] and starts[512 (c + 1)] are then not computed, for every c in whose part they do.
  *   - psa_last_issued reports these calls' status; its counts are those of psa_prompt_attention's blocks, else zero.
  *   - Parts of long rows are joined by counts that belong to the library, one set per device: calls of psa_prompt_attention, and calls of
- *     psa_cache_attention, must not overlap on the GPU even where each has a workspace of its own (graphs replayed on different streams without an event
+ *     psa_cache_attention and psa_tree_attention (which share theirs), must not overlap on the GPU even where each has a workspace of its own (graphs replayed on different streams without an event
  *     between them).  A call behind one whose waits ran out (PSA_ERR_TIMEOUT) is in order, whether or not the status was asked for in between.
  */
 
@@ -382,7 +384,7 @@ int psa_cache_append_rotary(const psa_cache* cache, const psa_rotary* rotary, co
 
 /*
  * psa_cache_attention for trees: the sequence's last nq tokens are the tree's, in the order of its queries, and query i sees of these its own token and its ancestors', and all tokens ahead of
- * them.  (With a chain for parents it is psa_cache_attention.)  max_q up to PSA_TREE_MOST.  Workspace psa_tree_workspace_bytes; everything else as there.
+ * them.  (With a chain for parents it is psa_cache_attention.)  max_q up to PSA_TREE_MOST.  `out` must not overlap Q.  Workspace psa_tree_workspace_bytes; everything else as there.
  */
 int psa_tree_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
                        int max_q, float scale, int dtype, void* out, float* lse, void* stream);
@@ -403,6 +405,7 @@ size_t psa_tree_workspace_bytes(int d_k);
  *   accepted, next      device ints [sequences]: how many stand (without the root), and the token behind them
  * A sequence without rows gets 0 and -1, and so does one whose rows are too many or whose temperature is none (reported).  A row on the path with a NaN, with +inf or with nothing but -inf ends
  * it there: the next token is -1, and psa_last_issued returns PSA_ERR_NUMERIC.
+ * Draws, and comparisons near their border, are made with exponentials and sums in 64 bits.  Supported: vocab up to 2^30.
  */
 int psa_verify_drafts(const void* logits, long long logit_stride, const void* drafts, long long draft_stride, int vocab, int dtype, const int* tokens, const int* parents,
                       const int* starts, int sequences, int rows, const float* temperatures, const float* uniform, int distinct, int* path, int* accepted, int* next, void* stream);

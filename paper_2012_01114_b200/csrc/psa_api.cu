@@ -1007,7 +1007,7 @@ int psa_tree_attention(const psa_cache* cache, const void* Q, long long q_stride
 int psa_verify_drafts(const void* logits, long long logit_stride, const void* drafts, long long draft_stride, int vocab, int dtype, const int* tokens, const int* parents,
                       const int* starts, int sequences, int rows, const float* temperatures, const float* uniform, int distinct, int* path, int* accepted, int* next, void* stream) {
     g_err_text[0] = 0;
-    if (sequences < 0 || rows < 0 || (sequences == 0 && rows > 0) || vocab <= 0) return PSA_ERR_SHAPE;
+    if (sequences < 0 || rows < 0 || (sequences == 0 && rows > 0) || vocab <= 0 || vocab > 1 << 30) return PSA_ERR_SHAPE;
     if (!serving_dtype(dtype) && dtype != PSA_F32) return PSA_ERR_UNSUPPORTED;
     if (sequences == 0) return PSA_OK;
     if (!starts || !accepted || !next || (rows > 0 && (!logits || !tokens || !parents || !uniform || !path))) return PSA_ERR_NULL;

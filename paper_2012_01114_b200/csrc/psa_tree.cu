@@ -1,20 +1,26 @@
-// Attention of trees of drafted tokens over the cache held in 4 bits (layout: psa_cache.cuh), where a key/value head has more than a few query rows (a row: a token of the tree and a query
-// head of the group; psa_cache_attn.cu takes the others).
+// Attention of trees of drafted tokens over the cache held in 4 bits (layout: psa_cache.cuh), where a key/value head has many query rows (a row: a token of the tree and a query head of the
+// group; psa_cache_attn.cu takes the others, and d = 256).
 //
 //     S_ij = scale q_i k_j,  w_ij = exp(S_ij),  out_i = sum_j w_ij v_j / sum_j w_ij,   j ahead of the tree, or i itself, or an ancestor of i
 //
 // 128 rows are a tile of the tensor core, so that a code is made a number once for all of them: at d = 128 a tile of 128 tokens is 20 KB of cache, 890 cycles at an SM's share of the memory's rate,
-// and 1600 cycles of MMAs.  Eight warps turn codes into operands, eight are the softmax's, one thread issues MMAs:
-//   K    k = M + S (1 + c / 16) goes in without a rounding.  S is split into its upper seven bits and the rest, S = S' + S'', so that S' c / 16 and S'' c / 16 are numbers of fp16 (one fma of 1 + c / 16 each):
-//        two operands, and the rest of the sum, sum_w (M_w + S_w) (sum of q over group w), in one more step of 16 columns, with the queries' sums in two parts each.  (k rounded to fp16 instead is a third
-//        fewer cycles, and 2.5e-4 off in every score: 5e-5 in the log-sum-exp of a short sequence, and twice the error of fp16 outputs.)
-//   V    rounded to fp16, as in psa_cache_attn.cu
-//   P    in tensor memory, fp16, held 2^7 times as large (HEADROOM in psa_prompt.cu)
-// There is room for one tile of each operand, and that is enough: while S of tile j + 1 runs V of tile j is written, and K of tile j + 2 while P V of tile j does; scores have two places, and the
-// softmax of tile j runs under the scores of tile j + 1.  Every warp that turns codes has a block of 16 tokens of each tile, and a ring of its own filled by bulk copies.
+// and 1024 cycles of MMAs (1536 with keys in two parts).  A persistent CTA an SM; every role walks the CTA's share of the work by itself and meets the others at barriers of two or three stages:
+//   one warp each  fetch blocks of K and of V by bulk copies into rings of three tiles, looking page numbers up four tiles ahead
+//   8 warps, K     fp16 operands of M + S (1 + c / 16), two stages, a block of 16 tokens of a tile each.  Ahead of short trees' rows, and for fp16, in two parts (the number rounded, and what that leaves:
+//                  2^-22 of it is lost), each a pass over the codes and an operand; see EXACT.
+//   4 warps, V     fp16 operands, two stages, rounded as in psa_cache_attn.cu
+//   one thread     issues the MMAs: scores of tile j + 1 ahead of the product of tile j's weights with V, with queries, scores (twice) and output in tensor memory
+//   8 warps        softmax, 16 rows each: scores are read twice, for the maximum (raised only when it is passed by 2^8) and for the weights, which go over the scores as fp16, held 2^7 times as
+//                  large (HEADROOM in psa_prompt.cu)
+//   one warp       the sets of tokens that a row sees, as bits
+// Work is the list of all tiles of all rows' tiles, weighed and cut into as many equal pieces as there are CTAs, whatever the lengths: a CTA ends one row tile, has some whole, and begins another.
+// Parts of a row tile are stored in fp32 and joined in their order by a second small kernel, since no CTA waits for another; rows with one part are finished where they are.
 //
-// Work is the list of all tiles of all rows' tiles, cut into as many equal pieces as there are CTAs, whatever the lengths: a CTA ends one row tile, has some whole, and begins another.  Parts of a row tile
-// are stored in fp32 and joined in their order by a second small kernel, since no CTA waits for another; rows with one part are finished where they are.
+// Measured (one B200, clocks 1.9 GHz): a tile takes 3500 cycles, one with keys in two parts 5900, at 104 rows of 128 as at 48.  In these a softmax warp is busy 2950, one that turns codes of K 2730, of V 2800,
+// and the thread that issues MMAs waits for weights: 20 warps that all wait for results of a fixed latency, and for instructions, whose caches five roles share (loops that are unrolled further are slower;
+// half the work of one role takes 2 to 7 % off a call, of all three 19).  What comes once a row tile costs about four tiles: 2000 cycles to read the queries, 2000 to the first scores, 4000 for the masked
+// ones, 5000 for the results.  32 sequences of up to 8000 tokens, trees of 12, 32 heads on 8 of d = 128 66 us; two of up to 131,072, trees of 26 120 us (460 TFLOP/s of the rows that exist); eight of up to
+// 6000, trees of 64, 32 on 4, fp16 52 us.
 #include <type_traits>
 
 #include "psa_cache.cuh"
@@ -29,7 +35,11 @@ namespace {
 
 constexpr int ROWS = 128, KEYS = 128, BLOCKS = KEYS / CACHE_BLOCK;
 constexpr int MMA_WARP = 0, K_WARP = 1, V_WARP = 2, SET_WARP = 3, SOFT0 = 4, SOFTS = 8, TURN_K = SOFT0 + SOFTS, TURN_V = TURN_K + BLOCKS, V_WARPS = BLOCKS / 2, T_WARPS = TURN_V + V_WARPS, T_THREADS = 32 * T_WARPS;
-constexpr int EXACT = 2048;                     // tokens ahead of a sequence's tree up to which keys go in in two parts
+// Tokens ahead of a sequence's tree up to which keys go in in two parts.  One part is a key rounded to fp16, half a step 2^-11 of a number: an eighth of what a query in bf16 has lost already, and averaged over
+// the tokens that a row sees.  In a short sequence a row may see a few tokens only and the log-sum-exp shows it (a sequence of 670 tokens at scale 0.9 was off by 1.3 times what is allowed); two parts take 1.7
+// times as long (batch, long: 95 and 156 us for 74 and 120 with all keys in two parts).  Queries in fp16 have lost less, and scores at more than 1.4 times the usual
+// scale, 1 / sqrt(d), are spread so far that few tokens count: keys then go in in two parts always.
+constexpr int EXACT = 2048;
 constexpr int T_SEQS = 512;                     // sequences of one launch
 constexpr int T_CTAS = 160;                     // at most
 // What work takes, in halves of a tile of keys: a tile, one with keys in two parts, and what a row tile takes beside its tiles; the least that a CTA is given.
@@ -58,7 +68,8 @@ struct TreeArgs {
     float *lse, *part;
     struct TreeRow* rows_cut;
     long long q_stride;
-    int pages, slots, width, page_size, kv_heads, group, sequences, rows, f16, d;
+    int pages, slots, width, page_size, kv_heads, group, sequences, rows, f16;
+    int two_parts;                              // keys go in in two parts whatever the lengths, see EXACT
     float scale;
     FastDiv by_group, by_blocks;
 };
@@ -78,7 +89,7 @@ struct TItem {
     int len, nq, q0, slot, t0, nt, h, qt, ctx, tok0;       // ctx: the tree's first token; tok0: the row tile's first
     int first_cta, part, parts;                             // of the row tile; a CTA has one part of it
     int row, rows;                                          // the row tile's place among those of its sequence (heads times row tiles), and their number
-    bool meets_tree, exact;                                 // exact: keys in two parts
+    bool meets_tree, exact;                                 // exact: keys in two parts, see EXACT
 };
 
 __device__ __forceinline__ uint32_t t_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
@@ -171,7 +182,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             const int held = there ? max(a.lens[slot], 0) : 0, len = (int)min((long long)held, (long long)a.width * a.page_size);
             strange |= (nq > 0 && (!there || held != len)) || nq != s1 - s0;
             const int tiles = max((int)(((uint32_t)len + KEYS - 1) / KEYS), 1), row_tiles = (nq * a.group + ROWS - 1) / ROWS;
-            n = (long long)row_tiles * a.kv_heads * ((long long)tiles * (a.f16 || len - nq <= EXACT ? COST_EXACT : COST) + COST_ROW);
+            n = (long long)row_tiles * a.kv_heads * ((long long)tiles * (a.two_parts || len - nq <= EXACT ? COST_EXACT : COST) + COST_ROW);
             len_s[b] = len;
             q0_s[b] = q0;
             nq_s[b] = nq;
@@ -221,7 +232,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 x.q0 = q0_s[lo];
                 x.slot = slot_s[lo];
                 x.ctx = x.len - x.nq;
-                x.exact = a.f16 || x.ctx <= EXACT;
+                x.exact = a.two_parts || x.ctx <= EXACT;
                 x.row = x.h = x.qt = 0;
                 const int row_tiles = (x.nq * a.group + ROWS - 1) / ROWS;
                 x.rows = row_tiles * a.kv_heads;
@@ -831,7 +842,7 @@ int tree_attention(const psa_cache& c, const void* Q, long long q_stride, const 
     const int group = heads / c.kv_heads;
     const TreeArgs a = {static_cast<const uint8_t*>(c.pool), c.tables, c.lens, seqs, q_starts, parents, static_cast<const uint16_t*>(Q), static_cast<uint16_t*>(out), lse,
                         reinterpret_cast<float*>(static_cast<char*>(scratch) + (size_t)T_CTAS * 32), static_cast<TreeRow*>(scratch), q_stride, c.pages, c.slots, c.width, c.page_size, c.kv_heads,
-                        group, sequences, rows, dtype == PSA_F16, c.d_k, scale, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
+                        group, sequences, rows, dtype == PSA_F16, dtype == PSA_F16 || scale * scale * c.d_k > 2.f, scale, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
     switch (c.d_k) {
         case 32: return launch_tree<32>(a, dc, dc_next, stream);
         case 64: return launch_tree<64>(a, dc, dc_next, stream);

@@ -64,7 +64,7 @@ def test_tree_refusals(lib, change, want):
 
 @pytest.mark.parametrize("change,want", [
     (dict(logits=None), "NULL"), (dict(tokens=None), "NULL"), (dict(parents=None), "NULL"), (dict(starts=None), "NULL"), (dict(uniform=None), "NULL"), (dict(path=None), "NULL"),
-    (dict(accepted=None), "NULL"), (dict(next=None), "NULL"), (dict(n=0), "SHAPE"), (dict(n=-1), "SHAPE"), (dict(rows=-1), "SHAPE"), (dict(vocab=0), "SHAPE"), (dict(ls=99), "SHAPE"),
+    (dict(accepted=None), "NULL"), (dict(next=None), "NULL"), (dict(n=0), "SHAPE"), (dict(n=-1), "SHAPE"), (dict(rows=-1), "SHAPE"), (dict(vocab=0), "SHAPE"), (dict(vocab=(1 << 30) + 1, ls=1 << 31, ds=1 << 31), "SHAPE"), (dict(ls=99), "SHAPE"),
     (dict(ds=99), "SHAPE"), (dict(ls=1 << 39), "SHAPE"), (dict(dtype=3), "UNSUPPORTED"), (dict(logits=P + 1), "ALIGN"), (dict(drafts=P + 1), "ALIGN"), (dict(dtype=binding.F32, logits=P + 2), "ALIGN"),
     (dict(uniform=P + 2), "ALIGN"), (dict(path=P + 2), "ALIGN"), (dict(temperatures=P + 1), "ALIGN"), (dict(rows=0, n=0, starts=None), None)])
 def test_verify_refusals(lib, change, want):

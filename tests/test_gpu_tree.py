@@ -159,6 +159,7 @@ def test_scale_strides_and_small_numbers():
     c = _made([50, 700], 2, 64, 16, 17)
     trees = _trees([9, 30], 6)
     _check(c, trees, 4, BF, scale=0.9)
+    _check(_made([2500, 5000], 1, 64, 16, 23), trees, 4, BF, scale=0.9)
     buf = _queries(39, 20, 64, BF, 5)
     _check(c, trees, 4, BF, Q=buf[:, 4:12])
     for size in (1e-30, 1e-6, 1e6):
