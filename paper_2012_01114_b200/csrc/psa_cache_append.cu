@@ -17,6 +17,8 @@
 // frequency becomes one once, and the product with the position wraps by itself where whole turns drop out, so that position 2^31 costs no accuracy and no division; sine and
 // cosine of what is left are good to 2^-23.  They are worked out once a token and channel for all heads that a warp takes.  The queries are turned by further blocks of the
 // same launch: a thread has four pairs of channels of one token, for one head after another.
+// Measured: 16 packed prompts of up to 2500 tokens, 32 heads on 8 of 128, half of each turning, with held values (123 MB) 29.6 us, 4.2 TB/s, 52 % of the issue slots; 64 trees of up to 16 tokens 6.0 us;
+// one token 4.4.
 #include <algorithm>
 #include <type_traits>
 
@@ -30,6 +32,7 @@ namespace psa {
 namespace {
 
 constexpr int APPEND_WARPS = 8;
+constexpr int ROT_CTAS = 3;                     // an SM, with rotation: 80 registers a thread.  (With two, three, four: 16 packed prompts of up to 2500 tokens, 32 heads on 8 of 128, 35.4, 29.6, 32.3 us)
 
 struct AppendArgs {
     uint8_t* pool;
@@ -186,7 +189,7 @@ __device__ __forceinline__ void turn_queries(const AppendArgs& a, const RotaryAr
 }
 
 template <int D, bool F16, bool ROT>
-__global__ void __launch_bounds__(32 * APPEND_WARPS) cache_append_kernel(const AppendArgs a, const RotaryArgs ro, DeviceCounters* dc, DeviceCounters* dc_next) {
+__global__ void __launch_bounds__(32 * APPEND_WARPS, ROT && D <= 128 ? ROT_CTAS : 1) cache_append_kernel(const AppendArgs a, const RotaryArgs ro, DeviceCounters* dc, DeviceCounters* dc_next) {
     constexpr int G = D / 32;
     constexpr bool SAME_LANE = G % 4 == 0;      // both tokens' codes come to the same lane, G / 4 rounds apart: whole words of V
     using B = CacheBlock<D>;
@@ -398,8 +401,9 @@ cudaError_t launch_append(const AppendArgs& a, RotaryArgs ro, DeviceCounters* dc
     ro.key_blocks = (int)((warps + APPEND_WARPS - 1) / APPEND_WARPS);
     long long blocks = ro.key_blocks;
     if (ro.q) {
-        // A thread takes one head while the GPU has room for more threads, then up to eight (the angles are worked out once), or so many that all threads can be counted.
-        const long long slots = D / 8, full = 148LL * 2048, most = 0x7fffff00LL - 64 * APPEND_WARPS;
+        // A thread takes one head while an SM has room for more blocks, then up to eight (the angles are worked out once), or so many that all threads can be counted.  (64 trees of up to 16 tokens, 32
+        // heads: 6.0 us; one head a thread up to 2048 threads an SM, in rounds, 7.6.)
+        const long long slots = D / 8, full = 148LL * 32 * APPEND_WARPS * ROT_CTAS, most = 0x7fffff00LL - 64 * APPEND_WARPS;
         long long groups = ro.heads;
         if (groups * slots * a.rows > full) groups = std::max(std::max((long long)(ro.heads + 7) / 8, std::min(groups, full / (slots * a.rows))), 1LL);
         if (groups * slots * a.rows > most) groups = std::max(most / (slots * a.rows), 1LL);
