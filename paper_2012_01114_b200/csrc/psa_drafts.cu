@@ -12,6 +12,10 @@
 // 32-bit exponentials first, and only where both sides are nearer to each other than those may be off, or where a child with drafts is refused, with the others.
 // Sums are formed in an order that depends on the sizes alone.
 //
+// Measured (one B200): 64 chains of 6 rows of 128,000 numbers in bf16 with drafts 127 us (the bytes alone 13, the exponentials in 64 bits 20); 16 trees of 33 in fp32, 50,001 numbers, 60 us; one greedy chain of 5,
+// 32,000 numbers, 6.5 us.  46 % of the issue slots at the first: a level costs a warp 800 instructions beside 9 for every 32 numbers of a row, an exponential in 64 bits 60, and the sequence with the longest path
+// decides.  (Neither rows in shared memory by bulk copies nor exponentials with half the 64-bit operations make it faster.)
+//
 // To read: the rows of the tokens on the path, and no others; which ones these are is known one after the other, so that what counts is how fast one row is read.  A
 // cluster of CTAs shares the rows of a sequence; a row costs one pass with a running maximum and one exchange of partial maxima and sums between the CTAs, a child with drafts that is refused two
 // more passes over what is then in the L2 cache.
