@@ -3,8 +3,9 @@
 // Verification walks a sequence's tree from its root.  At a token with target probabilities p = softmax(logits / T) and children x_1, x_2, .. (drawn from draft
 // probabilities q = softmax(drafts / T)), child x_m stands if u_m q_m(x_m) < w(x_m) / Z, where w = p, Z = 1 at first, and behind every child that does not stand
 //     w <- max(w / Z - q_m, 0),   Z <- sum_v w(v).
-// As q_m is q times a number (1, or 1 / (1 - what was drawn before) where siblings are drawn without replacement; tokens drawn before have w = 0 already), w is
-// max(a p - b q, 0) throughout, and a child that is refused costs two numbers and one sum over the row.  Where nobody stands the next token is the first one at
+// As q_m is q times a number (1, or 1 / (1 - what was drawn before) where siblings are drawn without replacement; tokens drawn before have w = 0 already), a child that is refused costs two
+// numbers, by which w follows from p and q wherever it is needed, and one sum over the row.  (In one step w is max(a p - b q, 0), but a grows with 1 / Z, and behind a few refused children of drafts
+// near p nothing is left of the difference.)  Where nobody stands the next token is the first one at
 // which the sum of w along the vocabulary passes u_root times the whole.
 //
 // A number next to a border decides about a token.  A draw has as many borders as the vocabulary has tokens, and with sums in 32 bits one draw in a hundred would fall on the other side of one:
@@ -37,6 +38,10 @@ constexpr int V_CTAS = 4;                       // an SM: with 64 registers a th
 // Relative error of a sum of 32-bit exponentials: their argument goes through two roundings of 2^-24 of itself, 30 at most where a weight counts (2^-18.6 of the weight), ex2 gives 2^-22, a number
 // takes part in no more than 36 additions before the sums go on in 64 bits and in 13 of the threads', warps' and CTAs' sums (2^-18.4): below 2^-17 altogether.
 constexpr float COARSE = 1.f / 65536;
+
+// What is left of two distributions of sum one that are the same but for roundings: tokens that could not have been drawn get there (a child with q = 0 behind all others), a drawn one with less than this
+// probability.
+constexpr double NOTHING = 1e-13;
 
 struct VerifyArgs {
     const void *logits, *drafts;
@@ -162,15 +167,31 @@ __device__ __noinline__ Sums sum_both(const T* p, const T* q, int low, int high,
     });
     return s;
 }
-// Sum of max(exp_p - k exp_q, 0).
+// What `n` refused children leave of a weight, by the numbers of each.
+struct Refused {
+    double up, less;                             // 1 / Z ahead of it; what exp_q is multiplied with
+};
+__device__ __forceinline__ double left_of(double pw, double qw, double first, const Refused* refused, int n) {       // first: refused[0].less (up is one there)
+    if (n > 0) pw = fma(-first, qw, pw);
+    for (int j = 1; j < n; ++j) pw = fma(-refused[j].less, qw, pw * refused[j].up);      // (what is below zero stays there)
+    return fmax(pw, 0.0);
+}
+// Its sum.
 template <class T>
-__device__ __noinline__ double sum_rest(const T* p, const T* q, int low, int high, const Exp& exp_p, const Exp& exp_q, double k, int lane) {
+__device__ __noinline__ double sum_rest(const T* p, const T* q, int low, int high, const Exp& exp_p, const Exp& exp_q, const Refused* refused, int n, int lane) {
     const Exp ep = exp_p, eq = exp_q;
+    const double first = refused[0].less;
     double sum = 0;
-    over<T, true>(p, q, low, high, lane, [&](float x, float y, int) {
-        const double pw = ep(x), qw = eq(y);
-        sum += fmax(fma(-k, qw, pw), 0.0);
-    });
+    if (n == 1)                                  // (the usual one, without the loop over children)
+        over<T, true>(p, q, low, high, lane, [&](float x, float y, int) {
+            const double pw = ep(x), qw = eq(y);
+            sum += fmax(fma(-first, qw, pw), 0.0);
+        });
+    else
+        over<T, true>(p, q, low, high, lane, [&](float x, float y, int) {
+            const double pw = ep(x), qw = eq(y);
+            sum += left_of(pw, qw, first, refused, n);
+        });
     return sum;
 }
 
@@ -292,6 +313,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
     __shared__ Record warps_s[V_WARPS];
     __shared__ Sums parts_s[V_WARPS];
     __shared__ double sums_s[V_WARPS], fine_s[V_WARPS];
+    __shared__ Refused refused_s[PSA_TREE_MOST];
     __shared__ int drawn_s;
     // What the CTAs tell each other, in two places by turns: written ahead of a barrier, read behind it.  (Each writes to all others.  Read from there by every warp it was 3 us a token with 32 warps.)
     __shared__ Record records[2][MOST_CLUSTER];
@@ -437,7 +459,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
                 continue;
             }
         }
-        // ---- in 64 bits from here on: w = max(p - k q, 0) with k = kb / ka times what brings q to p's size, or p without the children that were refused
+        // ---- in 64 bits from here on, w in units of p's sum: left_of, or p without the children that were refused
         const double power = exp2(lane / 32.0);
         const Exp exp_p(power, top, C), exp_q(power, q_top, C);
         Sums told = {0, 0, 0, 0};                // of all CTAs, by `exchange`, which leaves the warps' in parts_s
@@ -470,7 +492,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
         };
         double p_sum = 0, q_sum = 0;
         bool sharp = false;                      // these are known
-        double ka = 1, kb = 0, Z = 1, rest = 1, k = 0;
+        double Z = 1, rest = 1, k = 0;
         int tried = 0;
         bool only_p = true;                      // nothing was refused yet, or nothing is left
         // How the sums of w follow from parts_s and sums: a part's is p, or a - k b where both were summed over the numbers that are left.
@@ -478,7 +500,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
         auto part_sum = [&](const Sums& s) { return by_ab ? fmax(fma(-k, s.b, s.a), 0.0) : s.p; };
         auto sum_weights = [&] {
             by_ab = false;
-            const double s = !only_p && use_q ? sum_rest(lrow, qrow, w_low, w_high, exp_p, exp_q, k, lane) : sum_one(lrow, w_low, w_high, exp_p, tried_s, only_p ? 0 : tried, lane);
+            const double s = !only_p && use_q ? sum_rest(lrow, qrow, w_low, w_high, exp_p, exp_q, refused_s, tried, lane) : sum_one(lrow, w_low, w_high, exp_p, tried_s, only_p ? 0 : tried, lane);
             exchange(Sums{s, 0, 0, 0});
             summed = true;
         };
@@ -492,6 +514,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
             const double u = a.uniform[first + i], px = exp_p(number(lrow[x])), qx = use_q ? exp_q(number(qrow[x])) : 0.0;
             // Refused for certain by the sums in 32 bits?  (Without drafts the comparison is sharpened only where it is near; with drafts w needs the sums anyway.)
             const bool clear = !sharp && only_p && use_q && u * (qx / (double)row.q_sum) - px / (double)row.p_sum > 3 * (double)COARSE * u * (qx / (double)row.q_sum);
+            double part = 1.0;                   // q_m over q, for tokens that are left
             if (clear) {
                 // both rows' sums and those over the numbers that are left, by k in 32 bits, in one pass.  The numbers that k's last bits move from one side to the other are second order in its error,
                 // relative to what is left squared; where that is more than 1e-12 the pass is made again.
@@ -514,29 +537,34 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
                         for (int n = 0; n < tried; ++n) Z -= exp_p(number(lrow[tried_s[n]])) / p_sum;
                     }
                 }
-                const double part = use_q && a.distinct ? 1.0 / fmax(rest, 1e-300) : 1.0, pp = px / (sharp ? p_sum : (double)row.p_sum), qq = use_q ? qx / q_sum : 0.0;
-                if (use_q ? u * (qq * part) * Z < (only_p ? pp : fmax(ka * pp - kb * qq, 0.0)) : u * Z < pp) {
+                // What siblings leave of q is one minus a sum; where that is nearly nothing (a distribution with one likely token) it is summed itself, over the others.
+                if (use_q && a.distinct && rest < 1e-6 && tried > 0) {
+                    exchange(Sums{sum_one(qrow, w_low, w_high, exp_q, tried_s, tried, lane), 0, 0, 0});
+                    rest = told.p / q_sum;
+                }
+                if (use_q && a.distinct) part = rest > 1e-290 ? 1.0 / rest : 0.0;                // (nothing is left of q: zero everywhere)
+                const double pp = px / (sharp ? p_sum : (double)row.p_sum), qq = use_q ? qx / q_sum : 0.0;
+                if (use_q ? u * (qq * part) * Z < left_of(px, qx, refused_s[0].less, refused_s, tried) / p_sum : u * Z < pp) {
                     taken = i;
                     continue;
                 }
                 by_ab = summed = false;
                 if (!use_q) Z -= pp;
             }
-            if (use_q) {
-                kb = kb / Z + (a.distinct ? 1.0 / fmax(rest, 1e-300) : 1.0);
-                ka = ka / Z;
-                rest -= qx / q_sum;
-                k = kb / ka * (p_sum / q_sum);
-            }
+            const Refused by = {1.0 / Z, use_q ? fmin(part * (p_sum / q_sum), 1e300) : 0.0};
+            if (use_q) rest -= qx / q_sum;
             __syncthreads();
-            if (tid == 0) tried_s[tried] = x;
+            if (tid == 0) {
+                tried_s[tried] = x;
+                refused_s[tried] = by;
+            }
             ++tried;
             __syncthreads();
             only_p = false;
             if (use_q) {
                 if (!summed) sum_weights();
-                Z = ka * (by_ab ? fmax(fma(-k, told.b, told.a), 0.0) : told.p) / p_sum;
-                nothing = !(Z > 0);
+                Z = (by_ab ? fmax(fma(-k, told.b, told.a), 0.0) : told.p) / p_sum;
+                nothing = !(Z > NOTHING);
             }
         }
         if (taken >= 0) {
@@ -595,13 +623,13 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
                 const double pw = exp_p(v < f_high ? number(lrow[v]) : -INFINITY);
                 if (two) {
                     const double qw = exp_q(v < f_high ? number(qrow[v]) : -INFINITY);
-                    return fmax(fma(-k, qw, pw), 0.0);
+                    return left_of(pw, qw, refused_s[0].less, refused_s, tried);
                 }
                 bool gone = false;
                 for (int n = 0; n < tried && !only_p; ++n) gone |= tried_s[n] == v;
                 return gone ? 0.0 : pw;
             };
-            const double s = warp_sum(two ? sum_rest(lrow, qrow, f_low, f_high, exp_p, exp_q, k, lane) : sum_one(lrow, f_low, f_high, exp_p, tried_s, only_p ? 0 : tried, lane));
+            const double s = warp_sum(two ? sum_rest(lrow, qrow, f_low, f_high, exp_p, exp_q, refused_s, tried, lane) : sum_one(lrow, f_low, f_high, exp_p, tried_s, only_p ? 0 : tried, lane));
             if (lane == 0) fine_s[warp] = s;
             __syncthreads();
             if (warp == pick(fine_s)) {

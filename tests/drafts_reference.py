@@ -116,7 +116,7 @@ def verify(logits, drafts, tokens, parents, uniform, T, distinct):
                 q = q0.copy()
                 q[tried] = 0
                 q = q / q.sum() if q.sum() > 0 else q
-            if not w.sum() > 0:
+            if not w.sum() > 1e-13:              # (nothing but roundings is left, by definition)
                 w = p.copy()
                 break
         if taken is not None:

@@ -83,6 +83,15 @@ def test_sizes(V, seqs):
     assert m.check(True)[0] >= 0.9 * seqs
 
 
+@pytest.mark.parametrize("temperature", [1e-3, 0.01, 0.03])
+@pytest.mark.parametrize("kind", ["certain", "distinct", "replaced"])
+def test_siblings_behind_a_likely_one(kind, temperature):
+    """Drafts of which one token is nearly certain, and siblings drawn from the 1e-6 to 1e-40 that it leaves; the large model likes all tokens alike, or as the drafts do."""
+    for spread in (0.0, 2.0):
+        m = Made([20, 9, 33, 5] * 4, 96, torch.bfloat16, 31, branch=8, depth=3, spread=spread, distinct=kind != "replaced")
+        assert m.check(kind != "certain", [temperature] * 16, kind == "distinct")[0] > 0
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("stride", [0, 1, 2, 3, 5, 6, 14])
 def test_strides_and_alignment(stride, dtype):
