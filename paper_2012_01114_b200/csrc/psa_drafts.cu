@@ -13,7 +13,7 @@
 // 32-bit exponentials first, and only where both sides are nearer to each other than those may be off, or where a child with drafts is refused, with the others.
 // Sums are formed in an order that depends on the sizes alone.
 //
-// Measured (one B200): 64 chains of 6 rows of 128,000 numbers in bf16 with drafts 127 us (the bytes alone 13, the exponentials in 64 bits 20); 16 trees of 33 in fp32, 50,001 numbers, 60 us; one greedy chain of 5,
+// Measured (one B200): 64 chains of 6 rows of 128,000 numbers in bf16 with drafts 127 us (the bytes alone 13, the exponentials in 64 bits 20); 16 trees of 33 in fp32, 50,001 numbers, 61 us; one greedy chain of 5,
 // 32,000 numbers, 6.5 us.  46 % of the issue slots at the first: a level costs a warp 800 instructions beside 9 for every 32 numbers of a row, an exponential in 64 bits 60, and the sequence with the longest path
 // decides.  (Neither rows in shared memory by bulk copies nor exponentials with half the 64-bit operations make it faster.)
 //
@@ -171,27 +171,32 @@ __device__ __noinline__ Sums sum_both(const T* p, const T* q, int low, int high,
 struct Refused {
     double up, less;                             // 1 / Z ahead of it; what exp_q is multiplied with
 };
-__device__ __forceinline__ double left_of(double pw, double qw, double first, const Refused* refused, int n) {       // first: refused[0].less (up is one there)
-    if (n > 0) pw = fma(-first, qw, pw);
-    for (int j = 1; j < n; ++j) pw = fma(-refused[j].less, qw, pw * refused[j].up);      // (what is below zero stays there)
+__device__ __forceinline__ double left_of(double pw, double qw, const Refused* refused, int n) {
+    for (int j = 0; j < n; ++j) pw = fma(-refused[j].less, qw, pw * refused[j].up);      // (what is below zero stays there)
     return fmax(pw, 0.0);
 }
 // Its sum.
 template <class T>
 __device__ __noinline__ double sum_rest(const T* p, const T* q, int low, int high, const Exp& exp_p, const Exp& exp_q, const Refused* refused, int n, int lane) {
     const Exp ep = exp_p, eq = exp_q;
-    const double first = refused[0].less;
-    double sum = 0;
-    if (n == 1)                                  // (the usual one, without the loop over children)
+    double sum = 0, a = 1, b = 0;                // in one step: max(a p - b q, 0)
+    for (int j = 0; j < n; ++j) {
+        a *= refused[j].up;
+        b = fma(b, refused[j].up, refused[j].less);
+    }
+    if (a <= 1e4) {                              // (nearly always: what cancels is 1e-12 of the sum at most.  16 trees of 33: 61 us, child by child 65)
+        const double k = b / a;
         over<T, true>(p, q, low, high, lane, [&](float x, float y, int) {
             const double pw = ep(x), qw = eq(y);
-            sum += fmax(fma(-first, qw, pw), 0.0);
+            sum += fmax(fma(-k, qw, pw), 0.0);
         });
-    else
+        sum *= a;
+    } else {
         over<T, true>(p, q, low, high, lane, [&](float x, float y, int) {
             const double pw = ep(x), qw = eq(y);
-            sum += left_of(pw, qw, first, refused, n);
+            sum += left_of(pw, qw, refused, n);
         });
+    }
     return sum;
 }
 
@@ -544,7 +549,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
                 }
                 if (use_q && a.distinct) part = rest > 1e-290 ? 1.0 / rest : 0.0;                // (nothing is left of q: zero everywhere)
                 const double pp = px / (sharp ? p_sum : (double)row.p_sum), qq = use_q ? qx / q_sum : 0.0;
-                if (use_q ? u * (qq * part) * Z < left_of(px, qx, refused_s[0].less, refused_s, tried) / p_sum : u * Z < pp) {
+                if (use_q ? u * (qq * part) * Z < left_of(px, qx, refused_s, tried) / p_sum : u * Z < pp) {
                     taken = i;
                     continue;
                 }
@@ -623,7 +628,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
                 const double pw = exp_p(v < f_high ? number(lrow[v]) : -INFINITY);
                 if (two) {
                     const double qw = exp_q(v < f_high ? number(qrow[v]) : -INFINITY);
-                    return left_of(pw, qw, refused_s[0].less, refused_s, tried);
+                    return left_of(pw, qw, refused_s, tried);
                 }
                 bool gone = false;
                 for (int n = 0; n < tried && !only_p; ++n) gone |= tried_s[n] == v;
