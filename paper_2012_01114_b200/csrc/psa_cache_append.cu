@@ -17,7 +17,7 @@
 // frequency becomes one once, and the product with the position wraps by itself where whole turns drop out, so that position 2^31 costs no accuracy and no division; sine and
 // cosine of what is left are good to 2^-23.  They are worked out once a token and channel for all heads that a warp takes.  The queries are turned by further blocks of the
 // same launch: a thread has four pairs of channels of one token, for one head after another.
-// Measured: 16 packed prompts of up to 2500 tokens, 32 heads on 8 of 128, half of each turning, with held values (123 MB) 29.6 us, 4.2 TB/s, 52 % of the issue slots; 64 trees of up to 16 tokens 6.0 us;
+// Measured: 16 packed prompts of up to 2500 tokens, 32 heads on 8 of 128, half of each turning, with held values (123 MB) 29.6 us, 4.2 TB/s; 64 trees of up to 16 tokens 6.0 us;
 // one token 4.4.
 #include <algorithm>
 #include <type_traits>
