@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             mbar_init(&bars.s_full[s], 1); mbar_init(&bars.p_ready[s], SOFTS);
         }
         mbar_init(&bars.q_full, SOFTS);
-        mbar_init(&bars.sets_full, 1); mbar_init(&bars.sets_free, SOFTS);
+        mbar_init(&bars.sets_full, 1); mbar_init(&bars.sets_free, SOFTS + V_WARPS);
         fence_mbar_init();
     }
     if (warp == 1) { tmem_alloc(&tmem_s, 512); tmem_relinquish(); }
@@ -354,7 +354,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
         if (!ok)                                 // copies already asked for land before shared memory is released
             for (uint32_t m = n > (uint32_t)stages ? n - stages : 0; m < n; ++m) mbar_wait_drain(&full[m % stages], (m / stages) & 1);
     } else if (warp == SET_WARP) {
-        // ------------------------------------------------------------ the tokens' sets of the tree: each its own and its ancestors
+        // ------------------------------------------------------------ the tokens' sets of the tree: each its own and its ancestors.  A barrier's parity tells one phase from the next and no further: all
+        // who read the sets or write marks wait for sets_full of every item, those without keys or tree tokens too, and let go of every item, so that nobody is more than one phase away from this warp.
         for (uint32_t it = 0; ok && next_item(at, x); ++it) {
             if (it > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_free, (it - 1) & 1, abortp));
             if (!ok) break;
@@ -523,6 +524,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(&bars.v_full[n & 1]); mbar_arrive(&bars.v_raw_free[s]); }
             }
+            if (ok && !sets) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_full, it & 1, abortp));
+            if (ok && lane == 0) mbar_arrive(&bars.sets_free);       // (its marks are written: __syncwarp above)
         }
     } else {
         // ------------------------------------------------------------ softmax: 16 rows a warp, in the quad layout
@@ -683,7 +686,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 if (lane == 0) mbar_arrive(&bars.p_ready[buf]);
             }
             if (ok && x.nt > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bars.v_empty[(n + x.nt - 1) & 1], ((n + x.nt - 1) >> 1) & 1, abortp));
-            if (ok && x.meets_tree && !sets) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_full, it & 1, abortp));
+            if (ok && !sets) ok = __all_sync(0xffffffffu, mbar_wait(&bars.sets_full, it & 1, abortp));
             if (!ok) break;
             // ---- the rows' results
             tc_fence_after();
