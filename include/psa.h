@@ -293,9 +293,8 @@ int psa_selftest_wait_expiry(unsigned limit_us, void* stream);
  *     results over different keys can be joined.  A row that sees no key gets zeros and -inf.
  *   - What a row does not see has no influence on it, NaN and infinities included.
  *   - A weight is rounded to 16 bits for the product with V: to dtype by psa_prompt_attention, to fp16 by psa_cache_attention and psa_tree_attention.  In fp16 it keeps 11 bits
- *     down to 2^-21 of the largest weight among the keys that are worked on together, and an error of 2^-32 of that one below.  Held values are rounded to fp16 ahead of that product, and keys ahead of
- *     theirs by psa_tree_attention with PSA_BF16 where more than 2048 tokens lie ahead of a tree and scale^2 d_k <= 2
- *     (2^-11 of a number; queries in bf16 have lost 2^-8).
+ *     down to 2^-21 of the largest weight among the keys that are worked on together, and an error of 2^-32 of that one below.  Held values are rounded to fp16 ahead of that product; of a
+ *     key psa_tree_attention may lose 2^-22, or 2^-25 where that is more (it goes in as two fp16 numbers).
  *   - Lengths, tables and lists are read on the device, in stream order; the host needs none of them.  A call with zero rows (or an empty list) returns PSA_OK and
  *     launches nothing.  Device-side arguments that name no place (a sequence or page that does not exist, a token beyond the table)
  *     are left out, and psa_last_issued returns PSA_ERR_SHAPE for that call.  So it does for `starts` of psa_prompt_attention, psa_cache_attention and psa_tree_attention that descend
@@ -384,7 +383,8 @@ int psa_cache_append_rotary(const psa_cache* cache, const psa_rotary* rotary, co
 
 /*
  * psa_cache_attention for trees: the sequence's last nq tokens are the tree's, in the order of its queries, and query i sees of these its own token and its ancestors', and all tokens ahead of
- * them.  (With a chain for parents it is psa_cache_attention.)  max_q up to PSA_TREE_MOST.  `out` must not overlap Q.  Workspace psa_tree_workspace_bytes; everything else as there.
+ * them.  (With a chain for parents it is psa_cache_attention.)  max_q up to PSA_TREE_MOST; with it, the
+ * group and the room in the tables choose one of two kernels, whose results differ by roundings.  `out` must not overlap Q.  Workspace psa_tree_workspace_bytes; everything else as there.
  */
 int psa_tree_attention(const psa_cache* cache, const void* Q, long long q_stride, const int* parents, const int* seqs, const int* q_starts, int sequences, int rows, int heads,
                        int max_q, float scale, int dtype, void* out, float* lse, void* stream);

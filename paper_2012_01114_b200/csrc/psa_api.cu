@@ -963,9 +963,10 @@ int psa_cache_append_rotary(const psa_cache* cache, const psa_rotary* rotary, co
 size_t psa_cache_workspace_bytes(int d_k) { return cache_head(d_k) ? COUNTER_BYTES + cache_attention_scratch_bytes(d_k) : 0; }
 
 // Whether a tree's rows go to tiles of 128 rows (psa_tree.cu) or, sixteen at a time, through psa_cache_attn.cu, by the most rows that a head of K can have and the keys that the block table has
-// room for.  The second reads the keys once for every sixteen rows and its time goes with their number; the first takes its 20 us for the smallest call and the same for 16 rows as for 128.
-// 8 heads of K, d 128, microseconds of tiles and of the other at 32, 48, 64, 96 rows: 16 sequences of 8,000 tokens 118 : 116, 119 : 170, 120 : 225, 125 : 334; 64 of 2,000 220 : 127, 220 : 224,
-// 220 : 224, 220 : 333; 16 of 1,000 at 48 and 64 45 : 39, 46 : 50; one of 4,000 at 128 26 : 24; one of 300 at 48 21 : 10.5.
+// room for.  The second reads the keys once for every sixteen rows and its time goes with their number; the first takes its 25 us for the smallest call and the same for 16 rows as for 128.
+// 8 heads of K, d 128, microseconds of tiles and of the other at 32, 48, 64, 96 rows: 16 sequences of 8,000 tokens 171 : 149, 173 : 218, 172 : 254, 173 : 381; 64 of 2,000 208 : 158, 209 : 284,
+// 209 : 285, 213 : 424; 16 of 1,000 44 : 32, 46 : 46, 46 : 58, 49 : 81; 8 of 2,000 41 : 27, 42 : 48, 43 : 50, 45 : 72; 2 of 131,072 301 : 283, 303 : 372, 302 : 550, 301 : 1084; one of 4,000 at 64 and 128
+// 29 : 22, 30 : 31; one of 300 at 48 25 : 13.  Against it go many short sequences (128 of 300 at 48 127 : 92), and tables with far more room than tokens, of which the host knows nothing.
 static bool tree_on_tiles(const psa_cache& c, int sequences, int max_q, int group) {
     const long long rows = (long long)max_q * group;
     if (c.d_k > 128 || rows <= 32) return false;

@@ -4,10 +4,11 @@
 //     S_ij = scale q_i k_j,  w_ij = exp(S_ij),  out_i = sum_j w_ij v_j / sum_j w_ij,   j ahead of the tree, or i itself, or an ancestor of i
 //
 // 128 rows are a tile of the tensor core, so that a code is made a number once for all of them: at d = 128 a tile of 128 tokens is 20 KB of cache, 890 cycles at an SM's share of the memory's rate,
-// and 1024 cycles of MMAs (1536 with keys in two parts).  A persistent CTA an SM; every role walks the CTA's share of the work by itself and meets the others at barriers of two or three stages:
+// and 1536 cycles of MMAs.  A persistent CTA an SM; every role walks the CTA's share of the work by itself and meets the others at barriers of two or three stages:
 //   one warp each  fetch blocks of K and of V by bulk copies into rings of three tiles, looking page numbers up four tiles ahead
-//   8 warps, K     fp16 operands of M + S (1 + c / 16), two stages, a block of 16 tokens of a tile each.  Ahead of short trees' rows, and for fp16, in two parts (the number rounded, and what that leaves:
-//                  2^-22 of it is lost), each a pass over the codes and an operand; see EXACT.
+//   8 warps, K     fp16 operands of M + S (1 + c / 16), two stages, a block of 16 tokens of a tile each.  A key goes in in two parts (the number rounded, and what that leaves: 2^-22 of it, or 2^-25
+//                  where that is more, is lost), each a pass over the codes and an operand.  One part would lose 2^-12 of a key, and a log-sum-exp as much of scale sum_c |q_c k_c|, however long
+//                  the context is where a row attends to a few tokens or channels are large (with it 32 sequences of up to 8000 tokens took 66 us, two of up to 131,072 122).
 //   4 warps, V     fp16 operands, two stages, rounded as in psa_cache_attn.cu
 //   one thread     issues the MMAs: scores of tile j + 1 ahead of the product of tile j's weights with V, with queries, scores (twice) and output in tensor memory
 //   8 warps        softmax, 16 rows each: scores are read twice, for the maximum (raised only when it is passed by 2^8) and for the weights, which go over the scores as fp16, held 2^7 times as
@@ -16,11 +17,11 @@
 // Work is the list of all tiles of all rows' tiles, weighed and cut into as many equal pieces as there are CTAs, whatever the lengths: a CTA ends one row tile, has some whole, and begins another.
 // Parts of a row tile are stored in fp32 and joined in their order by a second small kernel, since no CTA waits for another; rows with one part are finished where they are.
 //
-// Measured (one B200, clocks 1.9 GHz): a tile takes 3500 cycles, one with keys in two parts 5900, at 104 rows of 128 as at 48.  In these a softmax warp is busy 2950, one that turns codes of K 2730, of V 2800,
+// Measured (one B200, clocks 1.9 GHz): a tile takes 5900 cycles, at 104 rows of 128 as at 48.  In these a softmax warp is busy 2950, one that turns codes of K twice 2730, of V 2800,
 // and the thread that issues MMAs waits for weights: 20 warps that all wait for results of a fixed latency, and for instructions, whose caches five roles share (loops that are unrolled further are slower;
-// half the work of one role takes 2 to 7 % off a call, of all three 19).  What comes once a row tile costs about four tiles: 2000 cycles to read the queries, 2000 to the first scores, 4000 for the masked
-// ones, 5000 for the results.  32 sequences of up to 8000 tokens, trees of 12, 32 heads on 8 of d = 128 66 us; two of up to 131,072, trees of 26 120 us (460 TFLOP/s of the rows that exist); eight of up to
-// 6000, trees of 64, 32 on 4, fp16 52 us.
+// half the work of one role takes 2 to 7 % off a call, of all three 19).  What comes once a row tile costs about two tiles and a half: 2000 cycles to read the queries, 2000 to the first scores, 4000 for the masked
+// ones, 5000 for the results.  32 sequences of up to 8000 tokens, trees of 12, 32 heads on 8 of d = 128 90 us; two of up to 131,072, trees of 26 164 us (340 TFLOP/s of the rows that exist); eight of up to
+// 6000, trees of 64, 32 on 4, fp16 51 us.
 #include <type_traits>
 
 #include "psa_cache.cuh"
@@ -35,15 +36,10 @@ namespace {
 
 constexpr int ROWS = 128, KEYS = 128, BLOCKS = KEYS / CACHE_BLOCK;
 constexpr int MMA_WARP = 0, K_WARP = 1, V_WARP = 2, SET_WARP = 3, SOFT0 = 4, SOFTS = 8, TURN_K = SOFT0 + SOFTS, TURN_V = TURN_K + BLOCKS, V_WARPS = BLOCKS / 2, T_WARPS = TURN_V + V_WARPS, T_THREADS = 32 * T_WARPS;
-// Tokens ahead of a sequence's tree up to which keys go in in two parts.  One part is a key rounded to fp16, half a step 2^-11 of a number: an eighth of what a query in bf16 has lost already, and averaged over
-// the tokens that a row sees.  In a short sequence a row may see a few tokens only and the log-sum-exp shows it (a sequence of 670 tokens at scale 0.9 was off by 1.3 times what is allowed); two parts take 1.7
-// times as long (batch, long: 95 and 156 us for 74 and 120 with all keys in two parts).  Queries in fp16 have lost less, and scores at more than 1.4 times the usual
-// scale, 1 / sqrt(d), are spread so far that few tokens count: keys then go in in two parts always.
-constexpr int EXACT = 2048;
 constexpr int T_SEQS = 512;                     // sequences of one launch
 constexpr int T_CTAS = 160;                     // at most
-// What work takes, in halves of a tile of keys: a tile, one with keys in two parts, and what a row tile takes beside its tiles; the least that a CTA is given.
-constexpr int COST = 2, COST_EXACT = 3, COST_ROW = 8, LEAST = 8;
+// What work takes, in thirds of a tile of keys: a tile, and what a row tile takes beside its tiles; the least that a CTA is given.
+constexpr int COST = 3, COST_ROW = 8, LEAST = 8;
 constexpr int TREE_WORDS = PSA_TREE_MOST / 32 + 1;
 constexpr float UP = 7.f;                       // log2 of what weights are held larger by
 constexpr float T_LN2 = 0.6931471805599453f;
@@ -69,7 +65,6 @@ struct TreeArgs {
     struct TreeRow* rows_cut;
     long long q_stride;
     int pages, slots, width, page_size, kv_heads, group, sequences, rows, f16;
-    int two_parts;                              // keys go in in two parts whatever the lengths, see EXACT
     float scale;
     FastDiv by_group, by_blocks;
 };
@@ -89,7 +84,7 @@ struct TItem {
     int len, nq, q0, slot, t0, nt, h, qt, ctx, tok0;       // ctx: the tree's first token; tok0: the row tile's first
     int first_cta, part, parts;                             // of the row tile; a CTA has one part of it
     int row, rows;                                          // the row tile's place among those of its sequence (heads times row tiles), and their number
-    bool meets_tree, exact;                                 // exact: keys in two parts, see EXACT
+    bool meets_tree;
 };
 
 __device__ __forceinline__ uint32_t t_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
@@ -182,7 +177,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             const int held = there ? max(a.lens[slot], 0) : 0, len = (int)min((long long)held, (long long)a.width * a.page_size);
             strange |= (nq > 0 && (!there || held != len)) || nq != s1 - s0;
             const int tiles = max((int)(((uint32_t)len + KEYS - 1) / KEYS), 1), row_tiles = (nq * a.group + ROWS - 1) / ROWS;
-            n = (long long)row_tiles * a.kv_heads * ((long long)tiles * (a.two_parts || len - nq <= EXACT ? COST_EXACT : COST) + COST_ROW);
+            n = (long long)row_tiles * a.kv_heads * ((long long)tiles * COST + COST_ROW);
             len_s[b] = len;
             q0_s[b] = q0;
             nq_s[b] = nq;
@@ -212,7 +207,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
     tc_fence_after();
     const uint32_t tmem = tmem_s;
 
-    // ---- Every role walks the CTA's items by itself: its share of the list.  A row tile is COST_ROW units and COST or COST_EXACT for each tile of keys, which belongs to the CTA that has its first unit.
+    // ---- Every role walks the CTA's items by itself: its share of the list.  A row tile is COST_ROW units and COST for each tile of keys, which belongs to the CTA that has its first unit.
     // Behind an item comes the next row tile from its beginning: only the first one takes divisions, and those that are cut.
     auto next_item = [&](long long& at, TItem& x) -> bool {
         while (at < mine1) {
@@ -232,12 +227,11 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                 x.q0 = q0_s[lo];
                 x.slot = slot_s[lo];
                 x.ctx = x.len - x.nq;
-                x.exact = a.two_parts || x.ctx <= EXACT;
                 x.row = x.h = x.qt = 0;
                 const int row_tiles = (x.nq * a.group + ROWS - 1) / ROWS;
                 x.rows = row_tiles * a.kv_heads;
                 if (first) {
-                    const int units = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1) * (x.exact ? COST_EXACT : COST) + COST_ROW;
+                    const int units = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1) * COST + COST_ROW;
                     const long long inside = at - base_s[lo];
                     x.row = (int)(inside / units);
                     u0 = (int)(inside - (long long)x.row * units);
@@ -245,10 +239,10 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                     x.qt = x.row - x.h * row_tiles;
                 }
             }
-            const int cost = x.exact ? COST_EXACT : COST, units = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1) * cost + COST_ROW, u1 = (int)min((long long)units, u0 + (mine1 - at));
+            const int units = max((int)(((uint32_t)x.len + KEYS - 1) / KEYS), 1) * COST + COST_ROW, u1 = (int)min((long long)units, u0 + (mine1 - at));
             const long long row0 = at - u0;
             at += u1 - u0;
-            auto tile_of = [&](int u) { return x.exact ? (max(u - COST_ROW, 0) + COST_EXACT - 1) / COST_EXACT : (max(u - COST_ROW, 0) + COST - 1) / COST; };
+            auto tile_of = [](int u) { return (max(u - COST_ROW, 0) + COST - 1) / COST; };
             x.t0 = tile_of(u0);
             const int t1 = tile_of(u1);
             if (t1 <= x.t0) continue;
@@ -258,7 +252,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
             x.parts = 1;
             if (u1 - u0 < units) {
                 x.first_cta = (int)((row0 + COST_ROW) / per);
-                x.parts = (int)((row0 + units - cost) / per) - x.first_cta + 1;
+                x.parts = (int)((row0 + units - COST) / per) - x.first_cta + 1;
             }
             x.part = (int)blockIdx.x - x.first_cta;
             x.meets_tree = x.nt > 0 && t1 * (long long)KEYS > x.ctx;
@@ -286,7 +280,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                     if (j < x.nt) {
                         // (where P of tile j - 2 was: its product has been issued)
                         const uint32_t dS = tmem + TM_S + (m & 1) * KEYS;
-                        for (int part = 0; part <= (int)x.exact; ++part, ++fills) {
+                        for (int part = 0; part < 2; ++part, ++fills) {
                             const uint32_t s = fills & 1, k = k_lo + s * (Cfg::TILE >> 4);
                             ok = mbar_wait(&bars.k_full[s], (fills >> 1) & 1, abortp);
                             if (!ok) break;
@@ -294,7 +288,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
 #pragma unroll
                             for (int kk = 0; kk < Cfg::KS; ++kk)
                                 umma_ts(dS, tmem + TM_Q + kk * 8, umma_desc_join(k + (((kk >> 2) * Cfg::SUBTILE + (kk & 3) * 32) >> 4), UMMA_DESC_HI_SW128), idescS, part > 0 || kk > 0);
-                            if (part == (int)x.exact) umma_commit(&bars.s_full[m & 1]);
+                            if (part == 1) umma_commit(&bars.s_full[m & 1]);
                             umma_commit(&bars.k_empty[s]);
                         }
                         if (!ok) break;
@@ -438,7 +432,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) tree_kernel(const TreeArgs a, De
                     ++fills;
                 };
                 fill(std::false_type{});
-                if (ok && x.exact) fill(std::true_type{});
+                if (ok) fill(std::true_type{});
                 if (ok && lane == 0) mbar_arrive(&bars.k_raw_free[s]);
             }
     } else if (warp >= TURN_V) {
@@ -845,7 +839,7 @@ int tree_attention(const psa_cache& c, const void* Q, long long q_stride, const 
     const int group = heads / c.kv_heads;
     const TreeArgs a = {static_cast<const uint8_t*>(c.pool), c.tables, c.lens, seqs, q_starts, parents, static_cast<const uint16_t*>(Q), static_cast<uint16_t*>(out), lse,
                         reinterpret_cast<float*>(static_cast<char*>(scratch) + (size_t)T_CTAS * 32), static_cast<TreeRow*>(scratch), q_stride, c.pages, c.slots, c.width, c.page_size, c.kv_heads,
-                        group, sequences, rows, dtype == PSA_F16, dtype == PSA_F16 || scale * scale * c.d_k > 2.f, scale, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
+                        group, sequences, rows, dtype == PSA_F16, scale, fastdiv_make((uint32_t)group), fastdiv_make((uint32_t)(c.page_size / CACHE_BLOCK))};
     switch (c.d_k) {
         case 32: return launch_tree<32>(a, dc, dc_next, stream);
         case 64: return launch_tree<64>(a, dc, dc_next, stream);
