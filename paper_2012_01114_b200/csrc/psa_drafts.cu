@@ -35,9 +35,14 @@ namespace {
 
 constexpr int MOST_CLUSTER = 8;
 constexpr int V_CTAS = 4;                       // an SM: with 64 registers a thread.  (With three, 80 registers and two rounds 156 us where this takes 128)
-// Relative error of a sum of 32-bit exponentials: their argument goes through two roundings of 2^-24 of itself, 30 at most where a weight counts (2^-18.6 of the weight), ex2 gives 2^-22, a number
-// takes part in no more than 36 additions before the sums go on in 64 bits and in 13 of the threads', warps' and CTAs' sums (2^-18.4): below 2^-17 altogether.
+// Relative error of a sum of 32-bit exponentials, in 2^-24.  The number that weights are relative to is raised when it is passed by 2^8 only, so that a weight 2^-a of the greatest one has gone through
+// arguments of a + 16 and (a + 16) / 8 raises; over the sum's weights a is 30 on average at most (their entropy, 2^30 of them).  An argument goes through three roundings (1 / T ln 2, difference, product):
+// 3 ln 2 46 = 96; a weight's own ex2 4 (2^-22), a raise 5 with its product: 29; the factors of thread, warp, CTA and cluster 5 each: 20; 36 additions before the sums go on in 64 bits and 14 in those of the
+// threads, warps and CTAs: 50.  199 altogether, below 2^-16.
 constexpr float COARSE = 1.f / 65536;
+// A comparison is certain where its sides are further apart than this, relative to the greater one (absolute without drafts, where both are 1 at most): a sum on each, and a weight, which is
+// 3 ln 2 100 + 5 off where it is 1e-30 of the sum or more.  825 of 2^-24 together.
+constexpr float SURE = 4 * COARSE, LEAST_SURE = 1e-30f;
 
 // What is left of two distributions of sum one that are the same but for roundings: tokens that could not have been drawn get there (a child with q = 0 behind all others), a drawn one with less than this
 // probability.
@@ -228,7 +233,8 @@ __device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
 }
 
 // Of a thread's share of a part of a row (vectors of 16 bytes in turn): the greatest number, the first place that has it (GREEDY), whether a number is NaN or +inf, and the sum of
-// 2^(c (x - greatest)) in 32 bits (not GREEDY).  Bound by ex2, 16 a clock on an SM: everything else is done two numbers at a time, and a NaN is found in the sum.
+// 2^(c (x - greatest)) in 32 bits (not GREEDY; on the way relative to a number that the greatest one passes by no more than 2^8, see COARSE).  Bound by ex2, 16 a clock on an SM: everything else is
+// done two numbers at a time, and a NaN is found in the sum.
 struct Part {
     float top, sum;
     int arg;
@@ -241,13 +247,16 @@ __device__ __forceinline__ Part part_of_row(const T* row, int low, int high, flo
     uint64_t sum2 = 0;
     double whole = 0;
     int chain = 0;
+    float most = -INFINITY, limit = -INFINITY;   // the greatest number; where the one that weights are relative to (r.top) is raised
+    const float slack = fminf(8.f / c, 1e38f);
     const uintptr_t at = reinterpret_cast<uintptr_t>(row + low);
     const int n = high - low, lead = min((int)((16 - (at & 15u)) % 16 / sizeof(T)), n), vecs = (n - lead) / VEC, done = lead + vecs * VEC;
-    auto raise = [&](float m) {                  // a new greatest number
+    auto raise = [&](float m) {
         const float f = r.top > -INFINITY ? exp2_fast(c * (r.top - m)) : 0.f;
         sum2 = mul2(sum2, pair_of(f, f));
         whole *= (double)f;
         r.top = m;
+        limit = m + slack;
     };
     auto one = [&](int v) {
         const float x = number(row[v]);
@@ -255,7 +264,8 @@ __device__ __forceinline__ Part part_of_row(const T* row, int low, int high, flo
             r.bad |= !(x <= 3.402823466e38f);
             if (x > r.top || (x == r.top && v < r.arg)) { r.top = x; r.arg = v; }
         } else {
-            if (x > r.top) raise(x);
+            most = fmaxf(most, x);
+            if (x > limit) raise(x);
             sum2 = add2(sum2, pair_of(exp2_fast(c * (x - (r.top > -INFINITY ? r.top : 0.f))), 0.f));
         }
     };
@@ -286,7 +296,8 @@ __device__ __forceinline__ Part part_of_row(const T* row, int low, int high, flo
                             if (y[e] == m) r.arg = low + lead + i * VEC + e;
                     }
                 } else {
-                    if (m > r.top) raise(m);
+                    most = fmaxf(most, m);
+                    if (m > limit) raise(m);
                     const float from = r.top > -INFINITY ? -r.top : 0.f;
                     const uint64_t from2 = pair_of(from, from), c2 = pair_of(c, c);
 #pragma unroll
@@ -305,7 +316,10 @@ __device__ __forceinline__ Part part_of_row(const T* row, int low, int high, flo
     }
     if (tid < n - done) one(low + done + tid);
     if (!GREEDY) {
-        r.sum = (float)(whole + (double)(pair_as(sum2).x + pair_as(sum2).y));
+        whole += (double)(pair_as(sum2).x + pair_as(sum2).y);
+        if (most > r.top) whole *= (double)exp2_fast(c * (r.top - most));
+        r.top = most;
+        r.sum = (float)whole;
         r.bad = !(r.sum < INFINITY) || r.top == INFINITY;
     }
     return r;
@@ -457,7 +471,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
         if (child < count && token_s[child] >= 0) {
             const float px = exp2_fast(c * (child_l - top)) / row.p_sum;
             const float left = use_q ? child_u * (exp2_fast(c * (child_q - q_top)) / row.q_sum) : child_u, right = px;
-            if (right - left > 3 * COARSE * (use_q ? right : 1.f)) {
+            if (right - left > SURE * (use_q ? right : 1.f) && right > LEAST_SURE) {
                 node = child;
                 ++stood;
                 if (rank == 0 && tid == 0) a.path[first + stood] = child;
@@ -518,7 +532,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
             if (again) continue;
             const double u = a.uniform[first + i], px = exp_p(number(lrow[x])), qx = use_q ? exp_q(number(qrow[x])) : 0.0;
             // Refused for certain by the sums in 32 bits?  (Without drafts the comparison is sharpened only where it is near; with drafts w needs the sums anyway.)
-            const bool clear = !sharp && only_p && use_q && u * (qx / (double)row.q_sum) - px / (double)row.p_sum > 3 * (double)COARSE * u * (qx / (double)row.q_sum);
+            const bool clear = !sharp && only_p && use_q && u * (qx / (double)row.q_sum) - px / (double)row.p_sum > (double)SURE * u * (qx / (double)row.q_sum);
             double part = 1.0;                   // q_m over q, for tokens that are left
             if (clear) {
                 // both rows' sums and those over the numbers that are left, by k in 32 bits, in one pass.  The numbers that k's last bits move from one side to the other are second order in its error,
@@ -532,7 +546,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
                 const double off = k0 / k - 1, left = fmax(fma(-k, told.b, told.a), 0.0) / p_sum;
                 by_ab = summed = off * off <= 1e-12 * left * left;
             } else {
-                if (!sharp && (use_q || fabs(u * Z - px / (double)row.p_sum) <= 3 * (double)COARSE)) {
+                if (!sharp && (use_q || fabs(u * Z - px / (double)row.p_sum) <= (double)SURE)) {
                     exchange(Sums{sum_one(lrow, w_low, w_high, exp_p, tried_s, 0, lane), use_q ? sum_one(qrow, w_low, w_high, exp_q, tried_s, 0, lane) : 0.0, 0, 0});
                     p_sum = told.p;
                     q_sum = told.q;
