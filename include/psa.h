@@ -414,7 +414,7 @@ int psa_verify_drafts(const void* logits, long long logit_stride, const void* dr
  * The cache keeps what stands: of a sequence's last nq = starts[b + 1] - starts[b] tokens those at places path[starts[b] + i], i = 0 .. accepted[b], become the first ones, in all layers, and the
  * length becomes lens - nq + 1 + accepted[b].  (path and accepted as psa_verify_drafts leaves them.)  cache->pool is [layers][pages][page bytes]; the pages must be the sequence's own as
  * far as the tree's tokens are in them, as psa_pages_reserve makes them.  Pages behind the new length are given back by the next psa_pages_reserve.
- *   new_lens   device ints [slots], may be cache->lens; lengths of the listed slots are written, of the others not
+ *   new_lens   device ints [slots], may be cache->lens; lengths of the listed slots are written (the old ones where a sequence is left as it is, also in a call without rows), of the others not
  * Lists hold distinct slots.  A sequence whose path does not ascend from 0 within the tree, or that holds fewer tokens than the tree, is left as it is and reported; one without rows is left as it is.
  */
 int psa_cache_keep(const psa_cache* cache, int layers, const int* seqs, const int* starts, const int* path, const int* accepted, int sequences, int rows, int* new_lens, void* stream);

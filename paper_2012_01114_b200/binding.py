@@ -465,7 +465,7 @@ def psa_verify_drafts(logits, tokens, parents, starts, uniform, path=None, accep
 
 def psa_cache_keep(pool, tables, lens, seqs, starts, path, accepted, kv_heads, page_size, new_lens=None, stream=None):
     """The tokens on the path move to the front of their tree, in all layers of the pool ([pages, page bytes] or [layers, pages, page bytes]), and the sequences end behind them.  new_lens: where
-    the lengths go (None: lens)."""
+    the lengths of all listed slots go (None: lens)."""
     (_marshal or marshal()).keep(pool, tables, lens, seqs, starts, path, accepted, kv_heads, page_size, new_lens, _handle(stream))
 
 

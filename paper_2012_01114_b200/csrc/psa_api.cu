@@ -1029,8 +1029,8 @@ int psa_cache_keep(const psa_cache* cache, int layers, const int* seqs, const in
     const int rc = check_cache(cache);
     if (rc != PSA_OK) return rc;
     if (layers <= 0 || sequences < 0 || rows < 0 || (sequences == 0 && rows > 0)) return PSA_ERR_SHAPE;
-    if (sequences == 0 || rows == 0) return PSA_OK;
-    if (!seqs || !starts || !path || !accepted || !new_lens) return PSA_ERR_NULL;
+    if (sequences == 0 || (rows == 0 && (!new_lens || new_lens == cache->lens))) return PSA_OK;       // (lengths that go elsewhere are written without rows too)
+    if (!seqs || !starts || (!path && rows > 0) || !accepted || !new_lens) return PSA_ERR_NULL;
     if ((long long)layers * cache->kv_heads > 0x7fffffffLL || (long long)layers * cache->kv_heads * sequences > 0x7fffff00LL) return PSA_ERR_SHAPE;
     if (!aligned4(seqs) || !aligned4(starts) || !aligned4(path) || !aligned4(accepted) || !aligned4(new_lens)) return PSA_ERR_ALIGN;
     return run_op(0, stream, [&](const OpCall& c) {

@@ -819,6 +819,7 @@ __global__ void __launch_bounds__(32 * KEEP_WARPS) cache_keep_kernel(const KeepA
         for (int b = threadIdx.x; b < a.sequences; b += 32 * KEEP_WARPS) {
             const Kept k = kept_of(a, b);
             if (k.keep > 0) a.new_lens[k.slot] = k.base + k.keep;
+            else if (a.new_lens != a.lens && k.slot >= 0 && k.slot < a.slots) a.new_lens[k.slot] = a.lens[k.slot];       // (left as it is)
         }
 }
 
