@@ -189,7 +189,7 @@ __device__ __forceinline__ void turn_queries(const AppendArgs& a, const RotaryAr
 }
 
 template <int D, bool F16, bool ROT>
-__global__ void __launch_bounds__(32 * APPEND_WARPS, ROT && D <= 128 ? ROT_CTAS : 1) cache_append_kernel(const AppendArgs a, const RotaryArgs ro, DeviceCounters* dc, DeviceCounters* dc_next) {
+__global__ void __launch_bounds__(32 * APPEND_WARPS, ROT ? (D <= 128 ? ROT_CTAS : 1) : 0) cache_append_kernel(const AppendArgs a, const RotaryArgs ro, DeviceCounters* dc, DeviceCounters* dc_next) {
     constexpr int G = D / 32;
     constexpr bool SAME_LANE = G % 4 == 0;      // both tokens' codes come to the same lane, G / 4 rounds apart: whole words of V
     using B = CacheBlock<D>;
