@@ -57,11 +57,12 @@ struct RotaryArgs {
     FastDiv by_slots, by_groups;                // by threads of a head (eight channels each), by groups of heads of a row
 };
 
-// Position times frequency, as sine and cosine.  freq / 2 pi is rounded to 2^-54 of itself, to 2^-64 of a turn, and what is left of the product to 2^-25 of half a turn.
+// Position times frequency, as sine and cosine.  freq / 2 pi is formed in two doubles (in one a frequency of 50 was off by 2^-17 of an angle at position 2^31) and rounded to 2^-63 of a turn, what is left of
+// the product to 2^-25 of half a turn.
 __device__ __forceinline__ long long turns_of(double freq) {
-    double t = freq * 0.15915494309189533577;                                // 1 / 2 pi
-    t -= rint(t);
-    return __double2ll_rn(t * 18446744073709551616.0);
+    constexpr double HIGH = 0.15915494309189535, LOW = -9.839338337591243e-18, ONE = 18446744073709551616.0;      // 1 / 2 pi in two parts; a turn
+    const double t = freq * HIGH, rest = fma(freq, LOW, fma(freq, HIGH, -t));
+    return (long long)((unsigned long long)__double2ll_rn((t - rint(t)) * ONE) + (unsigned long long)__double2ll_rn((rest - rint(rest)) * ONE));
 }
 __device__ __forceinline__ void sin_cos(long long turns, long long position, float& s, float& c) {
     const unsigned long long at = (unsigned long long)turns * (unsigned long long)position;
