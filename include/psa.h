@@ -396,7 +396,7 @@ size_t psa_tree_workspace_bytes(int d_k);
  * its number in `uniform`; otherwise w becomes max(w / Z - q, 0) and Z its sum.  distinct != 0: siblings were drawn without replacement, and q, behind every one of them, is what is left
  * of it without that token, made to sum to one again (a token that a sibling has had is passed over).  drafts NULL: the drafts are certain, q is one at the child's token (with these, too, a token
  * that a sibling has had is passed over).  The path goes on from a child that stands.  Where none does, the next token is drawn: the first one at which the sum of w over tokens 0, 1, .. passes
- * u of the root's row times Z (from p, where nothing is left of w: Z below 1e-13).  Tokens that stand, with the next one behind them, are distributed as the large model's own.
+ * u of the root's row times Z.  (Where nothing is left of w, Z below 1e-13, no further child is tried, and the draw is from p.)  Tokens that stand, with the next one behind them, are distributed as the large model's own.
  * temperature 0 (or below 2^-126): a child stands if its token is the likeliest (the first of equal ones), which is else the next token; drafts and uniform are not used.
  *   logits, drafts      device, [rows, vocab] with row strides >= vocab (any, and of any alignment), of dtype PSA_F32, PSA_BF16 or PSA_F16; -inf: never.  Rows that are not on the path are not read
  *   tokens, parents     device ints [rows]; the roots' are not used (a root's parent is -1).  Rows of -1 but the first are not reached.  A token outside 0 .. vocab - 1 never stands, and is reported

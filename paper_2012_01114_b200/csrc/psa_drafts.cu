@@ -584,6 +584,10 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
                 if (!summed) sum_weights();
                 Z = (by_ab ? fmax(fma(-k, told.b, told.a), 0.0) : told.p) / p_sum;
                 nothing = !(Z > NOTHING);
+            } else if (Z < 1e-6) {               // one minus a sum again (the sums are sharp: in 32 bits nothing is refused that leaves so little)
+                sum_weights();
+                Z = told.p / p_sum;
+                nothing = !(Z > NOTHING);
             }
         }
         if (taken >= 0) {
@@ -600,12 +604,7 @@ __global__ void __launch_bounds__(32 * V_WARPS, V_WARPS == 8 ? V_CTAS : 1) verif
             for (int n = 0; n < ranks; ++n) s += part_sum(sums[turn ^ 1][n]);
             return s;
         };
-        double all = whole();
-        if (!(all > 0)) {                        // (all of p refused)
-            only_p = true;
-            sum_weights();
-            all = whole();
-        }
+        const double all = whole();
         // which CTA, then which warp's part; where roundings leave none behind the target, the last one with any weight
         double target = (double)a.uniform[first] * all, before = 0;
         int owner = -1, last = 0;

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import drafts_reference as ref
 import serving_reference as sref
 from paper_2012_01114_b200 import binding as psa
 
@@ -60,3 +61,42 @@ def test_rows_that_rise_slowly_for_many_sequences():
     u = torch.tensor(u, dtype=torch.float64).float().cuda()
     path, accepted, following = psa.psa_verify_drafts(rows, _ints([0, V - 1] * B), _ints([-1, 0] * B), sref.starts([2] * B), u)
     assert psa.psa_last_issued()[0] == psa.OK and accepted.tolist() == want
+
+
+@pytest.mark.parametrize("left", [1e-8, 1e-10, 1e-12, 1e-14])
+def test_certain_drafts_behind_a_nearly_certain_token(left):
+    """Children that take all but `left` of a row are refused (u = 1 - 2^-24), the next one is 1e-5 on either side of its border with what is left, which one minus a sum in 64 bits gives to 1e-16 / left.
+    Behind what is left of 1e-14 no child is tried, and the token is drawn from the row as it is."""
+    B, V = 128, 40
+    g = torch.Generator().manual_seed(7)
+    rows, u, tokens, want = [], [], [], []
+    for b in range(B):
+        row = torch.full((V,), -60.0)
+        a, c, d = torch.rand(3, generator=g).tolist()
+        heads = [0.0, -15.5 - a] if left < 5e-8 else [0.0]
+        row[:len(heads)] = torch.tensor(heads)
+        n = len(heads)
+        row[n], row[n + 1], row[n + 2] = torch.log(torch.tensor(left, dtype=torch.float64)).float() - c, torch.log(torch.tensor(left, dtype=torch.float64)).float() - 1 - d, -55.0
+        order = torch.randperm(V, generator=g)
+        e = torch.exp(row.double())
+        border = float(e[n] / e[n:].sum())
+        near = 1e-5 if b % 2 else -1e-5
+        logits = torch.empty(V)
+        logits[order] = row
+        rows += [logits] * (n + 2)
+        tokens += [0] + [int(order[i]) for i in range(n + 1)]
+        first = float(torch.rand(1, generator=g))
+        u += [first] + [1 - 2.0 ** -24] * n + [border * (1 + near)]
+    n += 1
+    uniform = torch.tensor(u, dtype=torch.float64).float()
+    parents = [-1] + [0] * n
+    path, accepted, following = psa.psa_verify_drafts(torch.stack(rows).cuda(), _ints(tokens), _ints(parents * B), sref.starts([n + 1] * B), uniform.cuda())
+    assert psa.psa_last_issued()[0] == psa.OK
+    sure = 0
+    for b in range(B):
+        at = slice(b * (n + 1), (b + 1) * (n + 1))
+        p, k, x, margin = ref.verify(torch.stack(rows[at]), None, tokens[at], parents, uniform[at], 1.0, True)
+        if margin > 1e-7 / V:
+            assert (path[at].tolist(), int(accepted[b]), int(following[b])) == (p + [-1] * (n + 1 - len(p)), k, x), (b, margin)
+            sure += 1
+    assert sure > 0.9 * B
