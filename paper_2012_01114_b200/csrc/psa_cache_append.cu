@@ -17,8 +17,8 @@
 // frequency becomes one once, and the product with the position wraps by itself where whole turns drop out, so that position 2^31 costs no accuracy and no division; sine and
 // cosine of what is left are good to 2^-23.  They are worked out once a token and channel for all heads that a warp takes.  The queries are turned by further blocks of the
 // same launch: a thread has four pairs of channels of one token, for one head after another.
-// Measured: 16 packed prompts of up to 2500 tokens, 32 heads on 8 of 128, half of each turning, with held values (123 MB) 29.6 us, 4.2 TB/s; 64 trees of up to 16 tokens 6.0 us;
-// one token 4.4.
+// Measured: 16 packed prompts of up to 2500 tokens, 32 heads on 8 of 128, half of each turning, with held values (123 MB) 29.9 us, 4.1 TB/s; 64 trees of up to 16 tokens 6.3 us;
+// one token 4.5.
 #include <algorithm>
 #include <type_traits>
 
@@ -32,7 +32,7 @@ namespace psa {
 namespace {
 
 constexpr int APPEND_WARPS = 8;
-constexpr int ROT_CTAS = 3;                     // an SM, with rotation: 80 registers a thread.  (With two, three, four: 16 packed prompts of up to 2500 tokens, 32 heads on 8 of 128, 35.4, 29.6, 32.3 us)
+constexpr int ROT_CTAS = 3;                     // an SM, with rotation: 80 registers a thread.  (With two, three, four: 16 packed prompts of up to 2500 tokens, 32 heads on 8 of 128, 35.4, 29.6, 32.3 us with a frequency's fraction in one double)
 
 struct AppendArgs {
     uint8_t* pool;
@@ -403,7 +403,7 @@ cudaError_t launch_append(const AppendArgs& a, RotaryArgs ro, DeviceCounters* dc
     long long blocks = ro.key_blocks;
     if (ro.q) {
         // A thread takes one head while an SM has room for more blocks, then up to eight (the angles are worked out once), or so many that all threads can be counted.  (64 trees of up to 16 tokens, 32
-        // heads: 6.0 us; one head a thread up to 2048 threads an SM, in rounds, 7.6.)
+        // heads: 6.3 us; one head a thread up to 2048 threads an SM, in rounds, 1.6 more.)
         const long long slots = D / 8, full = 148LL * 32 * APPEND_WARPS * ROT_CTAS, most = 0x7fffff00LL - 64 * APPEND_WARPS;
         long long groups = ro.heads;
         if (groups * slots * a.rows > full) groups = std::max(std::max((long long)(ro.heads + 7) / 8, std::min(groups, full / (slots * a.rows))), 1LL);

@@ -13,8 +13,8 @@
 // 32-bit exponentials first, and only where both sides are nearer to each other than those may be off, or where a child with drafts is refused, with the others.
 // Sums are formed in an order that depends on the sizes alone.
 //
-// Measured (one B200): 64 chains of 6 rows of 128,000 numbers in bf16 with drafts 127 us (the bytes alone 13, the exponentials in 64 bits 20); 16 trees of 33 in fp32, 50,001 numbers, 61 us; one greedy chain of 5,
-// 32,000 numbers, 6.5 us.  46 % of the issue slots at the first: a level costs a warp 800 instructions beside 9 for every 32 numbers of a row, an exponential in 64 bits 60, and the sequence with the longest path
+// Measured (one B200; by chance more or fewer tokens stand): 64 chains of 6 rows of 128,000 numbers in bf16 with drafts 125 to 133 us (the bytes alone 13, the exponentials in 64 bits 20); 16 trees of 33 in fp32,
+// 50,001 numbers, 59 to 68 us; one greedy chain of 5, 32,000 numbers, 4.9 us where none stands, 8.4 to 13 where all do.  46 % of the issue slots at the first: a level costs a warp 800 instructions beside 9 for every 32 numbers of a row, an exponential in 64 bits 60, and the sequence with the longest path
 // decides.  (Neither rows in shared memory by bulk copies nor exponentials with half the 64-bit operations make it faster.)
 //
 // To read: the rows of the tokens on the path, and no others; which ones these are is known one after the other, so that what counts is how fast one row is read.  A
@@ -90,8 +90,8 @@ __device__ __forceinline__ void tell(X* to, const X& x, uint32_t rank) {
     }
 }
 
-// exp((x - top) / T) for x <= top, called by all lanes of a warp together, to 2^-50: with z = 32 (x - top) / (T ln 2), 2^(k / 32) (1 + e), k being the nearest whole number, the power from a table of
-// 32 (one a lane), e by its Taylor series (table-driven exponentials: Tang, 1989).  Zero below 2^-1018 and for -inf.
+// exp((x - top) / T) for x <= top, called by all lanes of a warp together, to 2^-48 beside 2^-53 of the exponent: with z = 32 (x - top) / (T ln 2), 2^(k / 32) (1 + e), k being the nearest whole number, the power from a table of
+// 32 (one a lane), e by its Taylor series up to the fifth power, which leaves 2^-48.7 (table-driven exponentials: Tang, 1989).  Zero below 2^-1018 and for -inf.
 struct Exp {
     double power, top, C;                        // 2^(lane / 32); C: 32 / (T ln 2)
     float top32, c;                              // the same in 32 bits; c: 1 / (T ln 2)

@@ -17,9 +17,9 @@
 // Work is the list of all tiles of all rows' tiles, weighed and cut into as many equal pieces as there are CTAs, whatever the lengths: a CTA ends one row tile, has some whole, and begins another.
 // Parts of a row tile are stored in fp32 and joined in their order by a second small kernel, since no CTA waits for another; rows with one part are finished where they are.
 //
-// Measured (one B200, clocks 1.9 GHz): a tile takes 5900 cycles, at 104 rows of 128 as at 48.  In these a softmax warp is busy 2950, one that turns codes of K twice 2730, of V 2800,
-// and the thread that issues MMAs waits for weights: 20 warps that all wait for results of a fixed latency, and for instructions, whose caches five roles share (loops that are unrolled further are slower;
-// half the work of one role takes 2 to 7 % off a call, of all three 19).  What comes once a row tile costs about two tiles and a half: 2000 cycles to read the queries, 2000 to the first scores, 4000 for the masked
+// Measured (one B200, clocks 1.9 GHz): a tile takes 5900 cycles, at 104 rows of 128 as at 48.  With keys in one part it took 3500, in which a softmax warp was busy 2950, one that
+// turns codes of K 2730, of V 2800, and the thread that issues MMAs waited for weights: 20 warps that all wait for results of a fixed latency, and for instructions, whose caches five roles share (loops that are unrolled further are slower;
+// half the work of one role took 2 to 7 % off a call, of all three 19).  What comes once a row tile costs about two tiles and a half: 2000 cycles to read the queries, 2000 to the first scores, 4000 for the masked
 // ones, 5000 for the results.  32 sequences of up to 8000 tokens, trees of 12, 32 heads on 8 of d = 128 90 us; two of up to 131,072, trees of 26 164 us (340 TFLOP/s of the rows that exist); eight of up to
 // 6000, trees of 64, 32 on 4, fp16 51 us.
 #include <type_traits>
